@@ -435,6 +435,114 @@ CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 CMC_API int cmc_test_stall_attention_waits(int on);
 
 /* ------------------------------------------------------------------------ *
+ * The two-tier cache in 8 bits (not a step of the paper's method: the same  *
+ * cache and attention at half the bytes)                                    *
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Format.  T tokens of every (sequence, layer, KV head) are held as
+ *
+ *   kv      e4m3 [B, L, Hkv, 2, T, d]   codes: keys, then values
+ *   scales  e8m0 [B, L, Hkv, 2, S]      S = cmc_q8_scale_bytes(T) = 4 ceil(T / 128):
+ *                                       byte j is the power of two 2^(c - 127) of
+ *                                       tokens 32 j .. 32 j + 31; bytes past
+ *                                       ceil(T / 32) are padding and not looked at
+ *
+ * and stand for code * 2^(c - 127).  The block's byte c is the smallest with
+ * amax <= 448 * 2^(c - 127), amax being the largest finite magnitude of the
+ * block's tokens (c = 0 where that is 0); a code is the value times 2^(127 - c),
+ * rounded to the nearest e4m3 value, ties to even.  An infinity or NaN is stored
+ * as NaN.  c = 255 is NaN: the block's values are.  e4m3 and e8m0 are the types
+ * that torch calls float8_e4m3fn and float8_e8m0fnu.
+ *
+ * A code is within 2^-4 of its value, relatively, for values down to 2^-15 of the
+ * block's amax, and within 2^-19 of amax below.
+ */
+
+/* S of the format above for T = rows tokens; 0 for rows < 0 or > 2^24. */
+CMC_API int cmc_q8_scale_bytes(int rows);
+
+/*
+ * Quantises rows of a bf16 K/V bank (or of a bf16 ring) into an 8-bit cache:
+ * row i of the cache is bank row idx[b, i], or bank row i when idx is NULL, for
+ * i < k.  Rows i >= count[b] hold no token: they are stored as zeros and do not
+ * count for their block.
+ *
+ *   bank_k, bank_v  bf16 [B, L, Hkv, N, d]
+ *   idx             int32 [B, k] or NULL
+ *   count           int64 [B] tokens that each sequence's k rows hold (any
+ *                   value; a ring's pos will do), or NULL for k
+ *   kv, scales      output, the format above with T = k; must not overlap the
+ *                   bank.  The padding bytes of scales are zeroed
+ *   status          NULL, or a device uint32 word that receives
+ *                   CMC_DEVFLAG_BAD_INDEX when an idx entry of a row that holds
+ *                   a token is outside [0, N); that row holds none then
+ *
+ * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
+ * launches nothing.
+ */
+CMC_API int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int32_t* idx,
+                               const int64_t* count, const cmc_dims* dims, void* kv, void* scales,
+                               uint32_t* status, void* stream);
+
+/*
+ * Reads an 8-bit cache back to bf16: out row i is cache row idx[b, i], or row i
+ * when idx is NULL, for i < k.  Exact (an e4m3 value has four significant bits)
+ * but for values below bf16's smallest.
+ *
+ *   kv, scales    the format above with T = N
+ *   idx           int32 [B, k] or NULL
+ *   out_k, out_v  bf16 [B, L, Hkv, k, d]  output; must not overlap the cache
+ *   status        as above; a row with a bad index is zeroed
+ *
+ * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
+ * launches nothing.
+ */
+CMC_API int cmc_dequantize_cache(const void* kv, const void* scales, const int32_t* idx,
+                                 const cmc_dims* dims, void* out_k, void* out_v, uint32_t* status,
+                                 void* stream);
+
+/*
+ * cmc_window_append for an 8-bit ring: token pos[b] goes to slot s = pos[b] mod W.
+ * Where s is the first slot of its block, the block's power of two is set anew,
+ * from the token and the block's other slots that hold one; elsewhere it grows
+ * where the token needs it and never shrinks.  Where it changes, the codes of
+ * the block's other slots that hold a token are multiplied by the ratio and
+ * rounded again (exact but for codes that go below 2^-6).  Slots that hold no
+ * token are neither read nor written.
+ *
+ *   ring_kv, ring_scales  the format above with T = W; updated in place
+ *   pos                   int64 [B]; updated
+ *   k_new, v_new          bf16 [B, L, Hkv, d]
+ *
+ * dims->Hq, N and k are ignored.  A sequence with pos[b] < 0 is left unchanged.
+ */
+CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos, const void* k_new,
+                                 const void* v_new, const cmc_dims* dims, void* stream);
+
+/*
+ * cmc_two_tier_decode_attn over a cache in 8 bits: Tier-1 is rows 0 .. k-1 of
+ * its cache (as cmc_quantize_cache leaves the selected rows), Tier-2 the
+ * occupied slots of the ring.
+ *
+ *   q                         bf16 [B, L, Hq, d]
+ *   tier1_kv, tier1_scales    the format above with T = N (may be NULL when k == 0)
+ *   ring_kv, ring_scales      the format above with T = W
+ *   pos                       int64 [B]  tokens appended so far (read only)
+ *   scale, out, workspace     as for cmc_two_tier_decode_attn: the workspace is
+ *                             that of cmc_decode_attn_workspace_size(dims), and one
+ *                             workspace serves both
+ *
+ * Products and sums are exact or fp32.  A sequence with pos[b] < 0 gets a zero
+ * output and sets CMC_DEVFLAG_BAD_POS.
+ */
+CMC_API int cmc_two_tier_decode_attn_q8(const void* q, const void* tier1_kv, const void* tier1_scales,
+                                        const void* ring_kv, const void* ring_scales,
+                                        const int64_t* pos, const cmc_dims* dims, float scale,
+                                        void* out, void* workspace, size_t workspace_bytes,
+                                        void* stream);
+
+/* ------------------------------------------------------------------------ *
  * Staging copies for a serving loop (not a step of the paper's method: the  *
  * input and output traffic of the decode loop around it)                    *
  * ------------------------------------------------------------------------ */

@@ -16,7 +16,10 @@ from .cmc import (  # noqa: F401
     decode_attn_workspace_size,
     decode_step,
     denoise,
+    dequantize_cache,
     dims_of,
+    q8_scale_bytes,
+    quantize_cache,
     question_select,
     score_select,
     score_select_workspace_size,
@@ -24,6 +27,8 @@ from .cmc import (  # noqa: F401
     stage_copies,
     tier1_gather,
     two_tier_decode_attn,
+    two_tier_decode_attn_q8,
     window_append,
+    window_append_q8,
 )
 from ._lib import CmcError, EXPORTS, LIB_PATH, lib  # noqa: F401

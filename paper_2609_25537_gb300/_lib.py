@@ -34,6 +34,11 @@ EXPORTS = (
     "cmc_read_status",
     "cmc_set_l2_prefetch_tiles",
     "cmc_test_stall_attention_waits",
+    "cmc_q8_scale_bytes",
+    "cmc_quantize_cache",
+    "cmc_dequantize_cache",
+    "cmc_window_append_q8",
+    "cmc_two_tier_decode_attn_q8",
     "cmc_stage_copies",
     "cmc_score_select_static",
 )
@@ -110,6 +115,12 @@ _SIGNATURES = {
     "cmc_read_status": (_i, [_vp, _i, ctypes.POINTER(ctypes.c_uint32), _vp]),
     "cmc_set_l2_prefetch_tiles": (_i, [_i]),
     "cmc_test_stall_attention_waits": (_i, [_i]),
+    "cmc_q8_scale_bytes": (_i, [_i]),
+    "cmc_quantize_cache": (_i, [_vp, _vp, _vp, _vp, _dims_p, _vp, _vp, _vp, _vp]),
+    "cmc_dequantize_cache": (_i, [_vp, _vp, _vp, _dims_p, _vp, _vp, _vp, _vp]),
+    "cmc_window_append_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _dims_p, _vp]),
+    "cmc_two_tier_decode_attn_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float, _vp,
+                                         _vp, _sz, _vp]),
     "cmc_stage_copies": (_i, [_vp, _i, _i, _vp]),
     "cmc_score_select_static": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp]),
 }

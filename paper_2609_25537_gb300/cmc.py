@@ -13,6 +13,11 @@ Tensor layouts (row-major, last index fastest):
   ring_k/v      bf16 [B, L, Hkv, W, d] pos       int64 [B]
   k_new/v_new   bf16 [B, L, Hkv, d]
 
+and of the cache in 8 bits (T tokens, see cmc.h for the format):
+
+  kv            float8_e4m3fn  [B, L, Hkv, 2, T, d]   keys, then values
+  scales        float8_e8m0fnu [B, L, Hkv, 2, q8_scale_bytes(T)]
+
 Tier-1 selection in the attention calls: an ``idx`` tensor [B, k] gathers
 rows of the bank by index at every step; ``idx=None`` takes every row of
 ``tier1_k``/``tier1_v`` in order (k = N), which is how the dense Tier-1 cache
@@ -44,6 +49,11 @@ __all__ = [
     "tier1_gather",
     "decode_attn_workspace_size",
     "decode_attn_plan",
+    "quantize_cache",
+    "dequantize_cache",
+    "window_append_q8",
+    "two_tier_decode_attn_q8",
+    "q8_scale_bytes",
     "set_l2_prefetch_tiles",
     "dims_of",
     "stage_copies",
@@ -491,6 +501,188 @@ def window_append(ring_k: torch.Tensor, ring_v: torch.Tensor, pos: torch.Tensor,
     st = lib().cmc_window_append(_p(ring_k), _p(ring_v), _p(pos), _p(k_new), _p(v_new),
                                  ctypes.byref(dims), _stream(dev))
     check(st, "cmc_window_append")
+
+
+# ----------------------------------------------------------------------------
+# The two-tier cache in 8 bits
+# ----------------------------------------------------------------------------
+
+_E4M3 = torch.float8_e4m3fn
+_E8M0 = torch.float8_e8m0fnu
+
+
+def q8_scale_bytes(rows: int) -> int:
+    """Powers of two of an 8-bit cache of `rows` tokens, per (unit, K or V):
+    4 ceil(rows / 128)."""
+    return (rows + 127) // 128 * 4
+
+
+def _need_q8(kv: torch.Tensor, scales: torch.Tensor, name: str, device) -> Tuple:
+    """Checks an 8-bit cache; returns its shape."""
+    _need(kv, name + "_kv", _E4M3, 6, device)
+    _need(scales, name + "_scales", _E8M0, 5, device)
+    shape = kv.shape
+    if shape[3] != 2:
+        raise ValueError(f"{name}_kv must be [B, L, Hkv, 2, T, d], got shape {tuple(shape)}")
+    if scales.shape != (shape[0], shape[1], shape[2], 2, q8_scale_bytes(shape[4])):
+        raise ValueError(f"{name}_scales shape {tuple(scales.shape)} does not go with {name}_kv "
+                         f"{tuple(shape)}")
+    return shape
+
+
+def _need_rows(idx, count, B, N, dev) -> int:
+    """Checks the row index and the token counts of a call; returns the rows."""
+    if idx is not None:
+        _need(idx, "idx", torch.int32, 2, dev)
+        if int(idx.shape[0]) != B:
+            raise ValueError(f"idx shape {tuple(idx.shape)} does not match batch {B}")
+    if count is not None:
+        _need(count, "count", torch.int64, 1, dev)
+        if int(count.shape[0]) != B:
+            raise ValueError("count must be [B]")
+    return N if idx is None else int(idx.shape[1])
+
+
+def _call(dev: torch.device, name: str, *args) -> None:
+    """Calls a library function whose last argument is the stream, with the
+    tensors' device current (a launch goes to the current one)."""
+    fn = getattr(lib(), name)
+    if dev.index != torch.cuda.current_device():
+        with torch.cuda.device(dev):
+            st = fn(*args, _stream(dev))
+    else:
+        st = fn(*args, _stream(dev))
+    if st:
+        check(st, name)
+
+
+@_ranged
+def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor] = None, *,
+                   count: Optional[torch.Tensor] = None, out_kv: Optional[torch.Tensor] = None,
+                   out_scales: Optional[torch.Tensor] = None,
+                   workspace: Optional[DecodeWorkspace] = None
+                   ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """An 8-bit cache (kv, scales) of rows of a bf16 bank or ring k, v [B, L, Hkv, N, d]:
+    all N, or those that ``idx`` [B, k] names.  Rows from ``count[b]`` on (int64 [B]; a
+    ring's pos will do) hold no token.  See cmc_quantize_cache.  Out-of-range
+    indices raise DEVFLAG_BAD_INDEX in ``workspace``'s status word when one is given."""
+    _need(k, "k", torch.bfloat16, 5)
+    dev = k.device
+    _need(v, "v", torch.bfloat16, 5, dev)
+    if v.shape != k.shape:
+        raise ValueError("v must have the shape of k")
+    B, L, Hkv, N, d = k.shape
+    rows = _need_rows(idx, count, B, N, dev)
+    shape, sshape = (B, L, Hkv, 2, rows, d), (B, L, Hkv, 2, q8_scale_bytes(rows))
+    if out_kv is None:
+        out_kv = torch.empty(shape, dtype=_E4M3, device=dev)
+    if out_scales is None:
+        out_scales = torch.empty(sshape, dtype=_E8M0, device=dev)
+    if _need_q8(out_kv, out_scales, "out", dev) != shape:
+        raise ValueError(f"out_kv must be {shape}")
+    dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
+    _call(dev, "cmc_quantize_cache", _p(k), _p(v), _p(idx), _p(count), ctypes.byref(dims), _p(out_kv),
+          _p(out_scales), 0 if workspace is None else _p(workspace.buf))
+    return out_kv, out_scales
+
+
+@_ranged
+def dequantize_cache(kv: torch.Tensor, scales: torch.Tensor, idx: Optional[torch.Tensor] = None, *,
+                     out_k: Optional[torch.Tensor] = None, out_v: Optional[torch.Tensor] = None,
+                     workspace: Optional[DecodeWorkspace] = None
+                     ) -> Tuple[torch.Tensor, torch.Tensor]:
+    """K and V of an 8-bit cache in bf16 [B, L, Hkv, rows, d]: all its rows, or
+    those that ``idx`` [B, k] names.  See cmc_dequantize_cache."""
+    _need(kv, "kv", _E4M3, 6)
+    dev = kv.device
+    B, L, Hkv, _, N, d = _need_q8(kv, scales, "cache", dev)
+    rows = _need_rows(idx, None, B, N, dev)
+    want = (B, L, Hkv, rows, d)
+    if out_k is None:
+        out_k = torch.empty(want, dtype=torch.bfloat16, device=dev)
+    if out_v is None:
+        out_v = torch.empty(want, dtype=torch.bfloat16, device=dev)
+    for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+        _need(t, name, torch.bfloat16, 5, dev)
+        if tuple(t.shape) != want:
+            raise ValueError(f"{name} must be {want}")
+    dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
+    _call(dev, "cmc_dequantize_cache", _p(kv), _p(scales), _p(idx), ctypes.byref(dims), _p(out_k),
+          _p(out_v), 0 if workspace is None else _p(workspace.buf))
+    return out_k, out_v
+
+
+@_ranged
+def window_append_q8(ring_kv: torch.Tensor, ring_scales: torch.Tensor, pos: torch.Tensor,
+                     k_new: torch.Tensor, v_new: torch.Tensor) -> None:
+    """Append one token per sequence to an 8-bit ring, in place; see
+    cmc_window_append_q8."""
+    _need(ring_kv, "ring_kv", _E4M3, 6)
+    dev = ring_kv.device
+    B, L, Hkv, _, W, d = _need_q8(ring_kv, ring_scales, "ring", dev)
+    _need(pos, "pos", torch.int64, 1, dev)
+    _need(k_new, "k_new", torch.bfloat16, 4, dev)
+    _need(v_new, "v_new", torch.bfloat16, 4, dev)
+    want = (B, L, Hkv, d)
+    if k_new.shape != want or v_new.shape != want:
+        raise ValueError(f"k_new/v_new must be {want}")
+    if int(pos.shape[0]) != B:
+        raise ValueError("pos must be [B]")
+    dims = CmcDims(B, L, Hkv, Hkv, d, 1, 0, W)
+    _call(dev, "cmc_window_append_q8", _p(ring_kv), _p(ring_scales), _p(pos), _p(k_new), _p(v_new),
+          ctypes.byref(dims))
+
+
+def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out, workspace):
+    _need(q, "q", torch.bfloat16, 4)
+    dev = q.device
+    B, L, Hq, d = q.shape
+    ring = _need_q8(ring_kv, ring_scales, "ring", dev)
+    Hkv, W = ring[2], ring[4]
+    k = 0
+    if tier1_kv is not None or tier1_scales is not None:
+        t1 = _need_q8(tier1_kv, tier1_scales, "tier1", dev)
+        k = t1[4]
+        if t1 != (B, L, Hkv, 2, k, d):
+            raise ValueError(f"inconsistent shapes: q {tuple(q.shape)}, tier1_kv {tuple(t1)}, "
+                             f"ring_kv {tuple(ring)}")
+    if ring != (B, L, Hkv, 2, W, d):
+        raise ValueError(f"inconsistent shapes: q {tuple(q.shape)}, ring_kv {tuple(ring)}")
+    _need(pos, "pos", torch.int64, 1, dev)
+    if int(pos.shape[0]) != B:
+        raise ValueError(f"pos shape {tuple(pos.shape)} does not match batch {B}")
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, "out", torch.bfloat16, 4, dev)
+        if out.shape != q.shape:
+            raise ValueError("out must have the shape of q")
+    sizes = (B, L, Hq, Hkv, d, max(k, 1), k, W)
+    dims = CmcDims(*sizes)
+    if workspace is None:
+        # A call that is being captured gets a workspace of its graph's own: the
+        # kept ones are zero-filled once, outside of it, and other calls use them.
+        if torch.cuda.is_current_stream_capturing():
+            workspace = DecodeWorkspace(dims, dev)
+        else:
+            workspace = _workspace_for(sizes, dims, dev, _stream(dev))
+    return dims, dev, out, workspace
+
+
+@_ranged
+def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, *,
+                            scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                            workspace: Optional[DecodeWorkspace] = None) -> torch.Tensor:
+    """Decode attention over [Tier-1 | occupied ring slots], both caches in 8 bits
+    (tier1_kv and tier1_scales None: the ring alone); see
+    cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  Without a ``workspace``
+    the call keeps one per stream and shape; a captured call then gets one of its own,
+    zero-filled at every replay."""
+    dims, dev, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out,
+                                       workspace)
+    _call(dev, "cmc_two_tier_decode_attn_q8", _p(q), _p(tier1_kv), _p(tier1_scales), _p(ring_kv),
+          _p(ring_scales), _p(pos), ctypes.byref(dims), _scale(scale), _p(out), _p(ws.buf), ws.nbytes)
+    return out
 
 
 # ----------------------------------------------------------------------------

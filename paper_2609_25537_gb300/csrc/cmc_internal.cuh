@@ -29,6 +29,9 @@ inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // The setting of cmc_set_l2_prefetch_tiles.
 int l2_prefetch_setting();
 
+// The setting of cmc_test_stall_attention_waits.
+uint32_t stall_tx_setting();
+
 // Validates the shape fields of a cmc_dims that the attention path uses.
 int validate_dims(const cmc_dims* dims, bool need_bank);
 
@@ -77,6 +80,13 @@ __device__ __forceinline__ uint32_t f32_to_bf16_bits(float f) {
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   return f32_to_bf16_bits(lo) | (f32_to_bf16_bits(hi) << 16);
+}
+
+// Two fp32 -> bf16x2 (round to nearest even); `lo` lands in the low half.
+__device__ __forceinline__ uint32_t pack_bf16_rn(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 
 // 16-byte streaming load that does not allocate in L1 (data read once).

@@ -1,0 +1,422 @@
+"""The two-tier cache in 8 bits on the GPU against the fp64 oracle.
+
+Codes and powers of two are compared bit for bit.  Attention outputs are held to a bound
+computed for each output (see attn_bound)."""
+
+import numpy as np
+import pytest
+import torch
+
+import oracle
+import paper_2609_25537_gb300 as cmc
+from oracle import q8
+from _gpu_helpers import to_f64
+
+pytestmark = pytest.mark.gpu
+
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+
+def rows_bf16(rng, *shape, spread=3.0):
+    """Rows whose magnitude varies from block to block by some powers of two, as bf16."""
+    x = rng.standard_normal(shape) * 2.0 ** rng.uniform(-spread, spread, shape[:-1] + (1,))
+    return torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16)
+
+
+def bytes_of(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def to_dev(codes, scales, dev):
+    return (torch.from_numpy(codes).to(dev).view(E4M3), torch.from_numpy(scales).to(dev).view(E8M0))
+
+
+def used(scales, T):
+    return scales[..., :(T + 31) // 32]
+
+
+def cache(rng, B, L, H, T, d, live=None):
+    """Random rows quantised by the oracle; where no row lives the codes are NaN and the powers of
+    two of blocks without a token NaN, as unwritten memory may be."""
+    k, v = (to_f64(rows_bf16(rng, B, L, H, T, d)) for _ in range(2))
+    live = np.ones((B, T), dtype=bool) if live is None else live
+    codes, scales = q8.quantize(k, v, live)
+    codes[~np.broadcast_to(live[:, None, None, None, :], codes.shape[:-1])] = 0x7F
+    scales[..., (T + 31) // 32:] = 0xFF
+    for b in range(B):
+        for j in range((T + 31) // 32):
+            if not live[b, 32 * j:32 * j + 32].any():
+                scales[b, ..., j] = 0xFF
+    return codes, scales
+
+
+# ---- writing and reading back ----
+
+SHAPES = [  # B, L, Hkv, N, d
+    (1, 1, 1, 1, 64), (2, 1, 2, 31, 128), (1, 3, 2, 32, 64), (3, 2, 1, 33, 128), (2, 1, 1, 128, 64),
+    (1, 2, 3, 129, 128), (2, 1, 2, 300, 128)]
+
+
+@pytest.mark.parametrize("B,L,H,N,d", SHAPES)
+def test_quantize_whole(cuda_device, B, L, H, N, d):
+    rng = np.random.default_rng(N)
+    k, v = (rows_bf16(rng, B, L, H, N, d) for _ in range(2))
+    kv, scales = cmc.quantize_cache(k.to(cuda_device), v.to(cuda_device))
+    codes, want = q8.quantize(to_f64(k), to_f64(v), np.ones((B, N), dtype=bool))
+    np.testing.assert_array_equal(bytes_of(scales), want)  # the padding, zeroed, among it
+    np.testing.assert_array_equal(bytes_of(kv), codes)
+
+
+@pytest.mark.parametrize("B,L,H,N,d,k", [(2, 2, 2, 50, 128, 1), (1, 1, 2, 300, 64, 33), (3, 1, 1, 7, 128, 40),
+                                         (2, 1, 2, 129, 64, 128)])
+def test_quantize_rows_by_index_with_counts(cuda_device, B, L, H, N, d, k):
+    rng = np.random.default_rng(k)
+    bank_k, bank_v = (rows_bf16(rng, B, L, H, N, d) for _ in range(2))
+    idx = rng.integers(0, N, (B, k)).astype(np.int32)  # any order, the same row more than once
+    count = np.array([k // 2, -3, 10 ** 12][:B])
+    kv, scales = cmc.quantize_cache(bank_k.to(cuda_device), bank_v.to(cuda_device),
+                                    torch.from_numpy(idx).to(cuda_device),
+                                    count=torch.from_numpy(count).to(cuda_device))
+    rows = [np.stack([to_f64(x)[b][:, :, idx[b]] for b in range(B)]) for x in (bank_k, bank_v)]
+    codes, want = q8.quantize(*rows, np.arange(k)[None] < count[:, None])
+    np.testing.assert_array_equal(bytes_of(scales), want)
+    np.testing.assert_array_equal(bytes_of(kv), codes)
+
+
+def test_quantize_special_values(cuda_device):
+    """Zeros, infinities, NaN, bf16's largest, smallest normal and subnormal values, and magnitudes on both
+    sides of 1.75 times a power of two, each with a block of its own or with others."""
+    x = torch.zeros(1, 1, 1, 320, 64)
+    top = torch.finfo(torch.bfloat16).max
+    x[..., 32, :4] = torch.tensor([float("inf"), -float("inf"), float("nan"), 3.0])
+    x[..., 64, 5], x[..., 65, 5] = top, -top
+    x[..., 96, 1], x[..., 97, 1] = 2.0 ** -126, -(2.0 ** -133)
+    x[..., 128, 2], x[..., 160, 2], x[..., 192, 2] = 1.75, 1.7578125, 448.0
+    x[..., 224, 0], x[..., 225, 0] = 1.0, 2.0 ** -17  # rounds to the smallest code, or to 0
+    x[..., 256, :] = float("nan")
+    x[..., 288, :] = -0.0
+    x = x.to(torch.bfloat16)
+    v = x.flip(3).contiguous()
+    kv, scales = cmc.quantize_cache(x.to(cuda_device), v.to(cuda_device))
+    codes, want = q8.quantize(to_f64(x), to_f64(v), np.ones((1, 320), dtype=bool))
+    np.testing.assert_array_equal(bytes_of(scales), want)
+    np.testing.assert_array_equal(bytes_of(kv), codes)
+
+
+def test_quantize_bad_index(cuda_device):
+    rng = np.random.default_rng(5)
+    bank = rows_bf16(rng, 2, 1, 2, 40, 128)
+    idx = np.arange(40, dtype=np.int32)[None].repeat(2, 0)
+    idx[0, 3], idx[1, 7], idx[1, 39] = -1, 40, 2 ** 31 - 1
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 1, 2, 2, 128, 40, 40, 1), cuda_device)
+    count = torch.tensor([40, 39], device=cuda_device)
+    kv, scales = cmc.quantize_cache(bank.to(cuda_device), bank.to(cuda_device),
+                                    torch.from_numpy(idx).to(cuda_device), count=count, workspace=ws)
+    assert ws.status() == cmc.DEVFLAG_BAD_INDEX
+    live = np.ones((2, 40), dtype=bool)
+    live[0, 3] = live[1, 7] = live[1, 39] = False
+    x = np.stack([to_f64(bank)[b][:, :, np.clip(idx[b], 0, 39)] for b in range(2)])
+    codes, want = q8.quantize(x, x, live)
+    np.testing.assert_array_equal(bytes_of(scales), want)
+    np.testing.assert_array_equal(bytes_of(kv), codes)
+    # a bad index of a row that holds no token is not looked at
+    cmc.quantize_cache(bank.to(cuda_device), bank.to(cuda_device), torch.from_numpy(idx).to(cuda_device),
+                       count=torch.tensor([3, 7], device=cuda_device), workspace=ws)
+    assert ws.status() == 0
+
+
+def test_quantize_no_rows(cuda_device):
+    bank = torch.zeros(2, 1, 1, 5, 64, dtype=torch.bfloat16, device=cuda_device)
+    kv, scales = cmc.quantize_cache(bank, bank, torch.empty(2, 0, dtype=torch.int32, device=cuda_device))
+    assert kv.shape == (2, 1, 1, 2, 0, 64) and scales.shape == (2, 1, 1, 2, 0)
+    k, v = cmc.dequantize_cache(kv, scales) if kv.shape[4] else (kv, kv)
+    assert k.numel() == v.numel() == 0
+
+
+@pytest.mark.parametrize("B,L,H,N,d", SHAPES)
+@pytest.mark.parametrize("by_index", [False, True])
+def test_dequantize(cuda_device, B, L, H, N, d, by_index):
+    rng = np.random.default_rng(N + d)
+    codes = rng.integers(0, 256, (B, L, H, 2, N, d), dtype=np.uint8)  # every code, NaN among them
+    scales = rng.integers(20, 240, (B, L, H, 2, q8.scale_bytes(N)), dtype=np.uint8)
+    kv, s = to_dev(codes, scales, cuda_device)
+    x = q8.values(codes, scales)
+    idx = None
+    if by_index:
+        idx = rng.integers(0, N, (B, 2 * N + 1)).astype(np.int32)
+        x = np.stack([x[b][..., idx[b], :] for b in range(B)])
+        idx = torch.from_numpy(idx).to(cuda_device)
+    k, v = cmc.dequantize_cache(kv, s, idx)
+    np.testing.assert_array_equal(to_f64(k), x[:, :, :, 0])  # exact: four significant bits
+    np.testing.assert_array_equal(to_f64(v), x[:, :, :, 1])
+
+
+def test_dequantize_extreme_powers_and_bad_index(cuda_device):
+    codes = np.full((1, 1, 1, 2, 96, 64), 0x38, dtype=np.uint8)  # 1.0
+    codes[..., 0, 0] = 0x01                                    # 2^-9
+    scales = np.zeros((1, 1, 1, 2, 4), dtype=np.uint8)
+    scales[..., 1], scales[..., 2] = 254, 255
+    kv, s = to_dev(codes, scales, cuda_device)
+    k, v = cmc.dequantize_cache(kv, s)
+    got = to_f64(k)[0, 0, 0]
+    assert got[0, 0] == 0.0 and (got[1:32] == 2.0 ** -127).all()  # 2^-136 is below bf16's smallest
+    assert (got[32:64] == 2.0 ** 127).all() and np.isnan(got[64:]).all()
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 1, 1, 64, 96, 3, 1), cuda_device)
+    idx = torch.tensor([[1, 96, -5]], dtype=torch.int32, device=cuda_device)
+    k, v = cmc.dequantize_cache(kv, s, idx, workspace=ws)
+    assert ws.status() == cmc.DEVFLAG_BAD_INDEX
+    assert (to_f64(v)[0, 0, 0, 1:] == 0).all() and (to_f64(v)[0, 0, 0, 0] == 2.0 ** -127).all()
+
+
+def test_quantise_then_read_back_is_within_half_a_step(cuda_device):
+    x = torch.rand(2, 2, 2, 200, 128, device=cuda_device).add(0.01).to(torch.bfloat16)
+    k, v = cmc.dequantize_cache(*cmc.quantize_cache(x, x))
+    assert torch.equal(k, v)
+    # amax < 1.01 and values above 0.01 > 2^-15 amax: half a step of e4m3
+    assert ((k.double() - x.double()).abs() / x.double()).max().item() <= 2.0 ** -4
+
+
+# ---- append ----
+
+@pytest.mark.parametrize("B,L,H,W,d", [(1, 1, 1, 1, 64), (3, 1, 2, 7, 128), (2, 2, 2, 32, 64),
+                                       (2, 1, 3, 33, 128), (4, 1, 1, 130, 128), (1, 40, 8, 64, 128)])
+def test_append(cuda_device, B, L, H, W, d):
+    """More tokens than the ring holds, from sequences at different places in it."""
+    rng = np.random.default_rng(W)
+    pos = np.array([0, W // 2, 3 * W + 1, 2 ** 33 + 5][:B], dtype=np.int64)
+    codes, scales = cache(rng, B, L, H, W, d, np.arange(W)[None] < pos[:, None])
+    kv, s = to_dev(codes, scales, cuda_device)
+    p = torch.from_numpy(pos.copy()).to(cuda_device)
+    steps = min(2 * W + 3, 70) if B * L * H < 100 else 4
+    for t in range(steps):
+        k_new, v_new = (rows_bf16(rng, B, L, H, d, spread=6.0) for _ in range(2))
+        cmc.window_append_q8(kv, s, p, k_new.to(cuda_device), v_new.to(cuda_device))
+        q8.append(codes, scales, pos, to_f64(k_new), to_f64(v_new))
+        np.testing.assert_array_equal(bytes_of(s), scales, err_msg=f"step {t}")
+        np.testing.assert_array_equal(bytes_of(kv), codes, err_msg=f"step {t}")
+    np.testing.assert_array_equal(p.cpu().numpy(), pos)
+
+
+def test_append_special_rows(cuda_device):
+    """Zero, infinite and NaN rows, rows far above and far below the block, a negative position."""
+    rng = np.random.default_rng(9)
+    W, d = 40, 64
+    codes, scales = cache(rng, 2, 1, 1, W, d)
+    pos = np.array([W + 3, -1], dtype=np.int64)
+    kv, s = to_dev(codes, scales, cuda_device)
+    p = torch.from_numpy(pos.copy()).to(cuda_device)
+    rows = [torch.zeros(d), torch.full((d,), float("nan")), torch.full((d,), -float("inf")),
+            torch.full((d,), 3e38), torch.full((d,), 2.0 ** -130), torch.randn(d),
+            torch.cat([torch.tensor([float("inf"), float("nan")]), torch.randn(d - 2) * 1e30])]
+    for t in range(45):
+        row = rows[t % len(rows)].to(torch.bfloat16)[None, None, None].repeat(2, 1, 1, 1)
+        cmc.window_append_q8(kv, s, p, row.to(cuda_device), row.to(cuda_device))
+        q8.append(codes, scales, pos, to_f64(row), to_f64(row))
+        np.testing.assert_array_equal(bytes_of(s), scales, err_msg=f"step {t}")
+        np.testing.assert_array_equal(bytes_of(kv), codes, err_msg=f"step {t}")
+    assert p.tolist() == pos.tolist() == [W + 48, -1]
+
+
+# ---- attention ----
+
+def attn_bound(q, tier1, ring, pos, scale, out, mag, q_error=0.0):
+    """How far an output may be off, from the roundings on the way to it.
+
+    * The output is rounded to bf16: 2^-8 of it.
+    * A probability is rounded to two e4m3 pieces through fp16: 2^-8 + 2^-11 of it, and 2^-18 of the
+      largest for those far below; the sum that divides is not rounded.
+    * A score is off by what the query's two pieces leave (2^-21 of its largest element, times
+      the key's sum of magnitudes; `q_error` of every product where the query was computed), by the
+      roundings of d products' fp32 sum and of a few more products (2^-24 each), and 2^x by 2^-21.
+      An error e of all scores changes the quotient by at most 2 e of the sum of p |v|."""
+    B, L, Hq, d = q.shape
+    bound = np.zeros_like(out)
+    for b in range(B):
+        n = max(0, min(int(pos[b]), ring.shape[4]))
+        for l in range(L):
+            for h in range(Hq):
+                g = h // (Hq // ring.shape[2])
+                K = np.concatenate([tier1[b, l, g, 0], ring[b, l, g, 0, :n]])
+                V = np.concatenate([tier1[b, l, g, 1], ring[b, l, g, 1, :n]])
+                if not len(K):
+                    continue
+                a = np.abs(q[b, l, h])
+                e = scale * (2.0 ** -21 * a.max() * np.abs(K).sum(axis=1)
+                             + ((d + 8) * 2.0 ** -24 + q_error) * (np.abs(K) @ a)).max()
+                bound[b, l, h] = (2.0 ** -8 * np.abs(out[b, l, h])
+                                  + (2.0 ** -8 + 2.0 ** -10 + 2 * (e + 2.0 ** -21)) * mag[b, l, h]
+                                  + 2.0 ** -18 * np.abs(V).sum(axis=0))
+    return bound
+
+
+def check_attention(got, q, t1, ring, pos, scale=None, q_error=0.0, what=""):
+    """got [B, L, Hq, d] (device) against the oracle over caches (codes, scales) of the host."""
+    B, L, Hq, d = q.shape
+    scale = 1 / np.sqrt(d) if scale is None else scale
+    H = ring[0].shape[2]
+    tier1 = q8.values(*t1) if t1 is not None else np.zeros((B, L, H, 2, 0, d))
+    x = q8.values(*ring)
+    out, mag = q8.attention(q, tier1, x, pos, scale)
+    err = np.abs(to_f64(got) - out)
+    bound = attn_bound(q, tier1, x, pos, scale, out, mag, q_error)
+    assert np.isfinite(out).all() and (err <= bound).all(), (
+        what, float((err / np.maximum(bound, 1e-300)).max()))
+    if np.linalg.norm(out) > 0:
+        # half-step roundings of the output and of the probabilities, independent of each other: well below
+        # 2^-7 of the outputs' norm together; a dropped key among 300 is 4 %
+        rel = np.linalg.norm(err) / np.linalg.norm(out)
+        assert rel <= 2.0 ** -7 + 2 * q_error, (what, rel)
+
+
+ATTN = [  # B, L, Hq, Hkv, d, k, W, pos
+    (1, 1, 1, 1, 64, 0, 1, [1]),
+    (1, 1, 8, 2, 64, 32, 128, [128]),
+    (2, 1, 8, 1, 128, 1, 7, [3, 100]),
+    (1, 2, 4, 2, 128, 31, 33, [20]),
+    (3, 1, 4, 4, 64, 33, 130, [0, 129, 131]),
+    (2, 2, 16, 4, 128, 127, 64, [2 ** 33 + 5, 64]),
+    (2, 1, 16, 2, 128, 128, 257, [200, 1]),
+    (1, 1, 16, 2, 64, 129, 31, [2]),
+    (2, 1, 8, 8, 128, 300, 300, [299, 301]),
+    (1, 1, 32, 8, 128, 700, 1100, [1100]),
+    (40, 4, 8, 2, 64, 5, 40, list(range(1, 41))),
+    (60, 2, 8, 4, 128, 40, 150, [150 + i for i in range(60)]),
+]
+
+
+def problem(rng, B, L, Hq, H, d, k, W, pos):
+    pos = np.array(pos, dtype=np.int64)
+    ring = cache(rng, B, L, H, W, d, np.arange(W)[None] < pos[:, None])
+    t1 = cache(rng, B, L, H, k, d) if k else None
+    q = rows_bf16(rng, B, L, Hq, d, spread=1.0)
+    return q, t1, ring, pos
+
+
+def device_args(q, t1, ring, pos, dev):
+    t = (None, None) if t1 is None else to_dev(*t1, dev)
+    return [q.to(dev), *t, *to_dev(*ring, dev), torch.from_numpy(pos.copy()).to(dev)]
+
+
+@pytest.mark.parametrize("B,L,Hq,H,d,k,W,pos", ATTN)
+def test_attention(cuda_device, B, L, Hq, H, d, k, W, pos):
+    rng = np.random.default_rng(W + k)
+    q, t1, ring, pos = problem(rng, B, L, Hq, H, d, k, W, pos)
+    args = device_args(q, t1, ring, pos, cuda_device)
+    got = cmc.two_tier_decode_attn_q8(*args)
+    check_attention(got, to_f64(q), t1, ring, pos)
+    assert torch.equal(cmc.two_tier_decode_attn_q8(*args), got)  # and the same bits again
+    # nothing but the output is written
+    for a, b in zip(args, device_args(q, t1, ring, pos, cuda_device)):
+        assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_attention_empty_and_negative(cuda_device):
+    rng = np.random.default_rng(3)
+    q, t1, ring, pos = problem(rng, 3, 1, 4, 2, 64, 0, 40, [0, -7, 4])
+    args = device_args(q, t1, ring, pos, cuda_device)
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(3, 1, 4, 2, 64, 1, 0, 40), cuda_device)
+    got = cmc.two_tier_decode_attn_q8(*args, workspace=ws)
+    assert (got[:2] == 0).all()
+    assert ws.status() == cmc.DEVFLAG_BAD_POS
+    check_attention(got, to_f64(q), t1, ring, pos)
+
+
+def test_attention_scale_and_sharp_scores(cuda_device):
+    """A given scale; scores of hundreds, where one key takes all."""
+    rng = np.random.default_rng(4)
+    q, t1, ring, pos = problem(rng, 2, 1, 8, 2, 128, 60, 200, [150, 500])
+    q = (q.float() * 8).to(torch.bfloat16)
+    for scale in (1.0, 0.01):
+        got = cmc.two_tier_decode_attn_q8(*device_args(q, t1, ring, pos, cuda_device), scale=scale)
+        check_attention(got, to_f64(q), t1, ring, pos, scale, what=str(scale))
+
+
+def test_attention_blocks_of_very_different_size(cuda_device):
+    """Blocks whose values differ by 2^60 and more, in either order, and tiny and huge queries."""
+    rng = np.random.default_rng(6)
+    for order in (1, -1):
+        q, t1, ring, pos = problem(rng, 1, 1, 4, 1, 128, 256, 256, [256])
+        for codes, scales in (t1, ring):
+            step = np.arange(8)[::order] * 8
+            scales[..., 1, :8] = (scales[..., 1, :8].astype(int) - 30 + step).astype(np.uint8)
+        q[:, :, 0] = (q[:, :, 0].float() * 1e-20).to(torch.bfloat16)
+        q[:, :, 1] = (q[:, :, 1].float() * 1e4).to(torch.bfloat16)
+        q[:, :, 2] = 0.0
+        got = cmc.two_tier_decode_attn_q8(*device_args(q, t1, ring, pos, cuda_device))
+        check_attention(got, to_f64(q), t1, ring, pos, what=str(order))
+
+
+def test_attention_nan_reaches_the_output_only_from_live_tokens(cuda_device):
+    rng = np.random.default_rng(7)
+    q, t1, ring, pos = problem(rng, 2, 1, 4, 2, 128, 40, 100, [70, 100])
+    t1[0][0, 0, 1, 1, 5, 3] = 0x7F  # a NaN among Tier-1's values of sequence 0, head 1
+    ring[0][1, 0, 0, 0, 99, 0] = 0xFF  # and among the ring's keys of sequence 1, head 0
+    got = to_f64(cmc.two_tier_decode_attn_q8(*device_args(q, t1, ring, pos, cuda_device)))
+    assert np.isnan(got[0, 0, 2:, 3]).all() and np.isnan(got[1, 0, :2]).all()
+    bad = np.isnan(got)
+    assert bad.sum() == 2 + 2 * 128
+
+
+@pytest.mark.parametrize("graph", [False, True])
+def test_attention_on_other_streams_and_captured(cuda_device, graph):
+    """Two calls at once on two streams, and two captured ones replayed on two streams, each with
+    the workspace that the call chooses."""
+    rng = np.random.default_rng(8)
+    probs = [problem(rng, 60, 1, 8, 4, 128, 40, 150, [150 + i + s for i in range(60)]) for s in range(2)]
+    args = [device_args(*x, cuda_device) for x in probs]
+    want = [cmc.two_tier_decode_attn_q8(*a).clone() for a in args]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    outs = [torch.empty_like(w) for w in want]
+    torch.cuda.synchronize()
+    runs = []
+    for a, o, s in zip(args, outs, streams):
+        def call(a=a, o=o):
+            cmc.two_tier_decode_attn_q8(*a, out=o)
+        if graph:
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=streams[0]):
+                call()
+            call = g.replay
+        runs.append((call, s))
+    for _ in range(20):
+        for call, s in runs:
+            with torch.cuda.stream(s):
+                call()
+    torch.cuda.synchronize()
+    for o, w in zip(outs, want):
+        assert torch.equal(o, w)
+
+
+# ---- refusals of the binding ----
+
+def test_binding_refusals(cuda_device):
+    dev = cuda_device
+    bank = torch.zeros(2, 1, 2, 40, 64, dtype=torch.bfloat16, device=dev)
+    kv, scales = cmc.quantize_cache(bank, bank)
+    pos = torch.zeros(2, dtype=torch.int64, device=dev)
+    q = torch.zeros(2, 1, 4, 64, dtype=torch.bfloat16, device=dev)
+    row = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16, device=dev)
+    attn = cmc.two_tier_decode_attn_q8
+    for exc, call in [
+            (TypeError, lambda: cmc.quantize_cache(bank.float(), bank)),
+            (ValueError, lambda: cmc.quantize_cache(bank, bank[:, :, :, :39].contiguous())),
+            (ValueError, lambda: cmc.quantize_cache(bank.transpose(3, 4), bank)),
+            (TypeError, lambda: cmc.quantize_cache(bank, bank, pos[:, None])),
+            (TypeError, lambda: cmc.quantize_cache(bank, bank, count=pos.int())),
+            (ValueError, lambda: cmc.quantize_cache(bank, bank, out_kv=kv[:1].contiguous())),
+            (TypeError, lambda: cmc.dequantize_cache(kv.view(torch.uint8), scales)),
+            (ValueError, lambda: cmc.dequantize_cache(kv, scales[..., :2].contiguous())),
+            (ValueError, lambda: cmc.dequantize_cache(kv[:, :, :, :1].contiguous(), scales)),
+            (ValueError, lambda: cmc.window_append_q8(kv, scales, pos[:1], row, row)),
+            (ValueError, lambda: cmc.window_append_q8(kv, scales, pos, row[:, :, :1].contiguous(), row)),
+            (ValueError, lambda: attn(q[:1].contiguous(), None, None, kv, scales, pos)),
+            (TypeError, lambda: attn(q, kv, None, kv, scales, pos)),
+            (ValueError, lambda: attn(q, kv[:1].contiguous(), scales[:1].contiguous(), kv, scales, pos)),
+            (ValueError, lambda: attn(q, None, None, kv, scales, pos, out=q[:1].contiguous())),
+            (ValueError, lambda: attn(q[:, :, :3].contiguous(), None, None, kv, scales, pos)),  # 3 over 2 heads
+    ]:
+        with pytest.raises(exc):
+            call()
+    small = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 2, 2, 64, 1, 0, 1), dev)
+    with pytest.raises(cmc.CmcError):
+        attn(q, None, None, kv, scales, pos, workspace=small)
