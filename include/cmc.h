@@ -533,14 +533,42 @@ CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos,
  *                             that of cmc_decode_attn_workspace_size(dims), and one
  *                             workspace serves both
  *
- * Products and sums are exact or fp32.  A sequence with pos[b] < 0 gets a zero
- * output and sets CMC_DEVFLAG_BAD_POS.
+ * Products are exact and sums fp32.  A probability is rounded to eight significant
+ * bits (as to bf16), or to 2^-18 of the largest where it is far below that; a
+ * query element to 2^-22 of its head's largest.  A NaN among the tokens reaches the
+ * outputs of its KV head's queries; slots that hold no token may hold anything.
+ * A sequence with pos[b] < 0 gets a zero output and sets CMC_DEVFLAG_BAD_POS.
  */
 CMC_API int cmc_two_tier_decode_attn_q8(const void* q, const void* tier1_kv, const void* tier1_scales,
                                         const void* ring_kv, const void* ring_scales,
                                         const int64_t* pos, const cmc_dims* dims, float scale,
                                         void* out, void* workspace, size_t workspace_bytes,
                                         void* stream);
+
+/*
+ * One fused decode step over a cache in 8 bits: cmc_window_append_q8 followed by
+ * cmc_two_tier_decode_attn_q8 in one launch (plus a combine launch where units
+ * are cut, see cmc_decode_attn_q8_plan).  The token attends to itself, as
+ * stored.  A sequence with pos[b] < 0 is left unchanged, its output is zero and
+ * CMC_DEVFLAG_BAD_POS is set.
+ *
+ * rope_theta == 0: keys and queries as given.  rope_theta > 0: the step of a
+ * GQA layer, as cmc_decode_step_rope: q and k_new are rotated inside the launch at
+ * position rope_offset + pos[b] (pos before the append).  The rotated key is
+ * quantised from fp32; the rotated query is rounded to eight significant bits.
+ *
+ * Errors: as the two calls; rope_theta negative, infinite or NaN, or rope_offset
+ * outside [0, 2^32] with a rope_theta: CMC_ERR_RANGE.
+ */
+CMC_API int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* tier1_scales,
+                               void* ring_kv, void* ring_scales, int64_t* pos, const void* k_new,
+                               const void* v_new, const cmc_dims* dims, float scale,
+                               double rope_theta, int64_t rope_offset, void* out, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
+/* cmc_decode_attn_plan for the calls over a cache in 8 bits (fused == 0:
+ * cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8).  Their tiles are of 128 keys. */
+CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas, int* launches);
 
 /* ------------------------------------------------------------------------ *
  * Staging copies for a serving loop (not a step of the paper's method: the  *

@@ -13,8 +13,10 @@ from .cmc import (  # noqa: F401
     DEVFLAG_TIMEOUT,
     bridge_epilogue,
     decode_attn_plan,
+    decode_attn_q8_plan,
     decode_attn_workspace_size,
     decode_step,
+    decode_step_q8,
     denoise,
     dequantize_cache,
     dims_of,

@@ -39,6 +39,8 @@ EXPORTS = (
     "cmc_dequantize_cache",
     "cmc_window_append_q8",
     "cmc_two_tier_decode_attn_q8",
+    "cmc_decode_step_q8",
+    "cmc_decode_attn_q8_plan",
     "cmc_stage_copies",
     "cmc_score_select_static",
 )
@@ -121,6 +123,9 @@ _SIGNATURES = {
     "cmc_window_append_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _dims_p, _vp]),
     "cmc_two_tier_decode_attn_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float, _vp,
                                          _vp, _sz, _vp]),
+    "cmc_decode_step_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float,
+                                ctypes.c_double, ctypes.c_int64, _vp, _vp, _sz, _vp]),
+    "cmc_decode_attn_q8_plan": (_i, [_dims_p, _i, ctypes.POINTER(_i), ctypes.POINTER(_i)]),
     "cmc_stage_copies": (_i, [_vp, _i, _i, _vp]),
     "cmc_score_select_static": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp]),
 }

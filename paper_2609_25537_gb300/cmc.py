@@ -53,6 +53,8 @@ __all__ = [
     "dequantize_cache",
     "window_append_q8",
     "two_tier_decode_attn_q8",
+    "decode_step_q8",
+    "decode_attn_q8_plan",
     "q8_scale_bytes",
     "set_l2_prefetch_tiles",
     "dims_of",
@@ -683,6 +685,40 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     _call(dev, "cmc_two_tier_decode_attn_q8", _p(q), _p(tier1_kv), _p(tier1_scales), _p(ring_kv),
           _p(ring_scales), _p(pos), ctypes.byref(dims), _scale(scale), _p(out), _p(ws.buf), ws.nbytes)
     return out
+
+
+@_ranged
+def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, v_new, *,
+                   scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                   workspace: Optional[DecodeWorkspace] = None,
+                   rope_theta: Optional[float] = None, rope_offset: int = 0) -> torch.Tensor:
+    """Fused decode step over a cache in 8 bits: append (k_new, v_new) to the ring, then
+    attend; see cmc_decode_step_q8.  Updates ring_kv, ring_scales and pos in place.
+    ``rope_theta`` and ``rope_offset`` as for :func:`decode_step`, ``workspace`` as for
+    :func:`two_tier_decode_attn_q8`."""
+    dims, dev, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out,
+                                       workspace)
+    _need(k_new, "k_new", torch.bfloat16, 4, dev)
+    _need(v_new, "v_new", torch.bfloat16, 4, dev)
+    want = (dims.B, dims.L, dims.Hkv, dims.d)
+    if k_new.shape != want or v_new.shape != want:
+        raise ValueError(f"k_new/v_new must be {want}")
+    if rope_theta is not None and not rope_theta > 0:
+        raise ValueError("rope_theta must be positive")
+    _call(dev, "cmc_decode_step_q8", _p(q), _p(tier1_kv), _p(tier1_scales), _p(ring_kv),
+          _p(ring_scales), _p(pos), _p(k_new), _p(v_new), ctypes.byref(dims), _scale(scale),
+          0.0 if rope_theta is None else float(rope_theta), int(rope_offset), _p(out), _p(ws.buf),
+          ws.nbytes)
+    return out
+
+
+def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> Tuple[int, int]:
+    """(grid size, kernel launches per call) of the attention over a cache in 8
+    bits; see cmc_decode_attn_q8_plan."""
+    ctas, launches = ctypes.c_int(0), ctypes.c_int(0)
+    check(lib().cmc_decode_attn_q8_plan(ctypes.byref(dims), 1 if fused else 0, ctypes.byref(ctas),
+                                        ctypes.byref(launches)), "cmc_decode_attn_q8_plan")
+    return int(ctas.value), int(launches.value)
 
 
 # ----------------------------------------------------------------------------

@@ -1115,7 +1115,7 @@ static WsLayout ws_layout(const cmc_dims& m) {
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
   const int G = m.Hq / m.Hkv;
   w.tickets_off = kWsHeader;
-  w.partials_off = w.tickets_off + ((static_cast<size_t>(m.B) * 8 + 255) / 256) * 256;
+  w.partials_off = ws_partials_off(m.B);
   w.total = w.partials_off + static_cast<size_t>(units) * tiles_per_unit(m) * rec_floats(G, m.d) * sizeof(float);
   return w;
 }

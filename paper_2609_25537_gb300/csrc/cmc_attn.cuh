@@ -44,7 +44,7 @@ struct AttnParams {
   float* partials;        // [units, tpu, G * (d + 2)]
   int B, L, Hq, Hkv, N, k, W;
   int tpu;                // tiles per unit: t1_tiles Tier-1 tiles, then the ring tiles
-  int t1_tiles;           // ceil(k / 64)
+  int t1_tiles;           // of them Tier-1 tiles
   int rot;                // in-unit processing order: tile (j + rot) % tpu at position j
   int LH;                 // units per sequence: L * Hkv
   int base;               // granules per CTA (CTAs below `rem` take one more); cluster plan:
@@ -553,6 +553,12 @@ two_tier_combine_kernel(const AttnParams p) {
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
+
+// A workspace: [0, 256) status word; then one 8-byte pos-read count per sequence
+// (padded to 256 bytes); then the partial records.
+static inline size_t ws_partials_off(int B) {
+  return kWsHeader + ((static_cast<size_t>(B) * 8 + 255) / 256) * 256;
+}
 
 // cuTensorMapEncodeTiled, reached through the runtime's driver entry point.
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*,

@@ -387,6 +387,194 @@ def test_attention_on_other_streams_and_captured(cuda_device, graph):
         assert torch.equal(o, w)
 
 
+# ---- the fused step ----
+
+STEP = ATTN + [
+    (5, 1, 8, 2, 128, 10, 33, [0, 31, 32, 33, 2 ** 33 + 5]),  # blocks' first slots, and a wrap
+    (20, 10, 4, 2, 64, 0, 100, [7 * i for i in range(20)]),
+]
+
+
+@pytest.mark.parametrize("B,L,Hq,H,d,k,W,pos", STEP)
+def test_step_is_append_then_attention(cuda_device, B, L, Hq, H, d, k, W, pos):
+    """Three steps: ring, powers of two and pos bit for bit those of the append, the outputs those of
+    attention over them."""
+    rng = np.random.default_rng(W + k + 1)
+    q, t1, ring, pos = problem(rng, B, L, Hq, H, d, k, W, pos)
+    args = device_args(q, t1, ring, pos, cuda_device)
+    codes, scales = (x.copy() for x in ring)
+    for t in range(3):
+        q, k_new, v_new = (rows_bf16(rng, B, L, h, d, spread=4.0 if h == H else 1.0) for h in (Hq, H, H))
+        args[0] = q.to(cuda_device)
+        got = cmc.decode_step_q8(*args, k_new.to(cuda_device), v_new.to(cuda_device))
+        q8.append(codes, scales, pos, to_f64(k_new), to_f64(v_new))
+        np.testing.assert_array_equal(bytes_of(args[4]), scales, err_msg=f"step {t}")
+        np.testing.assert_array_equal(bytes_of(args[3]), codes, err_msg=f"step {t}")
+        np.testing.assert_array_equal(args[5].cpu().numpy(), pos)
+        check_attention(got, to_f64(q), t1, (codes, scales), pos, what=f"step {t}")
+
+
+def test_step_negative_position(cuda_device):
+    rng = np.random.default_rng(11)
+    q, t1, ring, pos = problem(rng, 2, 2, 8, 2, 128, 30, 50, [-4, 20])
+    args = device_args(q, t1, ring, pos, cuda_device)
+    new = [rows_bf16(rng, 2, 2, 2, 128) for _ in range(2)]
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 2, 8, 2, 128, 30, 30, 50), cuda_device)
+    got = cmc.decode_step_q8(*args, *(x.to(cuda_device) for x in new), workspace=ws)
+    assert ws.status() == cmc.DEVFLAG_BAD_POS and (got[0] == 0).all()
+    codes, scales = (x.copy() for x in ring)
+    q8.append(codes, scales, pos, *(to_f64(x) for x in new))
+    np.testing.assert_array_equal(bytes_of(args[3]), codes)
+    np.testing.assert_array_equal(bytes_of(args[4]), scales)
+    assert args[5].tolist() == pos.tolist() == [-4, 21]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("theta,offset,start", [(1e4, 0, 0), (5e5, 30, 130), (5e5, 2 ** 31, 2 ** 20 + 7)])
+def test_step_with_rotary_embedding(cuda_device, d, theta, offset, start):
+    rng = np.random.default_rng(d)
+    B, L, Hq, H, k, W = 3, 2, 8, 2, 30, 130
+    q, t1, ring, pos = problem(rng, B, L, Hq, H, d, k, W, [start, start + 40, start + 200])
+    args = device_args(q, t1, ring, pos, cuda_device)
+    for t in range(2):
+        q, k_new, v_new = (rows_bf16(rng, B, L, h, d) for h in (Hq, H, H))
+        args[0] = q.to(cuda_device)
+        before = (bytes_of(args[3]).copy(), bytes_of(args[4]).copy())
+        got = cmc.decode_step_q8(*args, k_new.to(cuda_device), v_new.to(cuda_device), rope_theta=theta,
+                                 rope_offset=offset)
+        rq, rk = np.zeros(q.shape), np.zeros(k_new.shape)
+        for b in range(B):
+            rq[b] = oracle.rope_rotate(to_f64(q)[b], float(offset + pos[b]), theta)
+            rk[b] = oracle.rope_rotate(to_f64(k_new)[b], float(offset + pos[b]), theta)
+        codes, scales = before
+        q8.append(codes, scales, pos, rk, to_f64(v_new))
+        got_codes = bytes_of(args[3])
+        # The rotated key is within 2^-21 of its row's largest element (angles to 1e-7, fp32), so its
+        # codes may be one step off where the exact value is that near a rounding border: rarely.
+        same = got_codes == codes
+        np.testing.assert_array_equal(got_codes[:, :, :, 1], codes[:, :, :, 1])
+        assert (~same).sum() <= 4
+        assert np.abs(got_codes.astype(int) - codes.astype(int)).max() <= 1
+        np.testing.assert_array_equal(bytes_of(args[4]), scales)
+        np.testing.assert_array_equal(args[5].cpu().numpy(), pos)
+        # a rotated query element is rounded to eight significant bits: 2^-8 of every product
+        check_attention(got, rq, t1, (got_codes, scales), pos, q_error=2.0 ** -8, what=f"step {t}")
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 8, 2, 64, 32, 128), (2, 1, 16, 2, 128, 400, 900),
+                                   (60, 2, 8, 4, 128, 40, 150)])
+def test_step_captured_and_replayed(cuda_device, shape):
+    """A captured step, replayed, does what that many direct calls do, with the workspace that the
+    call chooses; eager calls of the same shape on the same stream in between do not disturb it."""
+    rng = np.random.default_rng(12)
+    B = shape[0]
+    q, t1, ring, pos = problem(rng, *shape, [50 + b for b in range(B)])
+    new = [rows_bf16(rng, B, shape[1], shape[3], shape[4]).to(cuda_device) for _ in range(2)]
+    one, two = (device_args(q, t1, ring, pos, cuda_device) for _ in range(2))
+    out = torch.empty_like(one[0])
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        cmc.decode_step_q8(*one, *new, out=out, rope_theta=1e4)
+    with torch.cuda.stream(stream):
+        for _ in range(5):
+            graph.replay()
+            want = cmc.decode_step_q8(*two, *new, rope_theta=1e4)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
+    for a, b in zip(one[3:], two[3:]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    assert one[5].tolist() == [55 + b for b in range(B)]
+
+
+def test_steps_of_two_requests_on_two_streams(cuda_device):
+    rng = np.random.default_rng(13)
+    probs = [problem(rng, 4, 3, 8, 2, 128, 100, 300, [290 + s] * 4) for s in range(2)]
+    new = [[rows_bf16(rng, 4, 3, 2, 128).to(cuda_device) for _ in range(2)] for _ in range(2)]
+    serial = [device_args(*x, cuda_device) for x in probs]
+    want = [[cmc.decode_step_q8(*a, *n).clone() for _ in range(15)] for a, n in zip(serial, new)]
+    par = [device_args(*x, cuda_device) for x in probs]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for t in range(15):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(cmc.decode_step_q8(*par[i], *new[i]))
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(got[i], want[i]))
+        for a, b in zip(par[i][3:], serial[i][3:]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def test_whole_path(cuda_device):
+    """A request as it is served: select, quantise the selected rows and the prefilled window, decode; and
+    the same with the bank kept in 8 bits, whose rows are read back for the bf16 path."""
+    rng = np.random.default_rng(14)
+    B, L, Hq, H, d, N, k, W = 2, 2, 8, 2, 64, 200, 40, 70
+    bank = [rows_bf16(rng, B, L, H, N, d, spread=0.5).to(cuda_device) for _ in range(2)]
+    window = [rows_bf16(rng, B, L, H, W, d, spread=0.5).to(cuda_device) for _ in range(2)]
+    pos = torch.tensor([30, W + 5], device=cuda_device)
+    cmes, question = torch.randn(B, N, 32, device=cuda_device), torch.randn(B, 32, device=cuda_device)
+    idx = cmc.score_select(question, cmes, k)
+    t1 = cmc.quantize_cache(*bank, idx)
+    ring = cmc.quantize_cache(*window, count=pos)
+    bank8 = cmc.quantize_cache(*bank)
+    d1 = cmc.dequantize_cache(*bank8, idx)
+    ring16 = [x.clone() for x in cmc.dequantize_cache(*ring)]
+    pos16 = pos.clone()
+    for t in range(50):
+        q, k_new, v_new = (rows_bf16(rng, B, L, h, d, spread=0.5).to(cuda_device) for h in (Hq, H, H))
+        got = cmc.decode_step_q8(q, *t1, *ring, pos, k_new, v_new)
+        n = [int(x) for x in pos]
+        host = [(bytes_of(c), bytes_of(s)) for c, s in (t1, ring)]
+        check_attention(got, to_f64(q), host[0], host[1], np.array(n), what=f"step {t}")
+        near = cmc.decode_step(q, *d1, None, *ring16, pos16, k_new, v_new)
+        # the two caches differ by roundings of single values to e4m3, 2^-4 of a value at most
+        far = (near.double() - got.double()).norm() / near.double().norm()
+        assert far <= 2.0 ** -3, (t, float(far))
+    assert pos.tolist() == pos16.tolist() == [80, W + 55]
+
+
+@pytest.mark.parametrize("shape", [(1, 1, 8, 2, 64, 32, 128), (60, 2, 8, 4, 128, 40, 150)])
+def test_step_timeout_is_reported(cuda_device, shape):
+    """With every stage's wait made to run out, the launch ends, the workspace's status word says so, and
+    the context stays usable."""
+    rng = np.random.default_rng(15)
+    B = shape[0]
+    q, t1, ring, pos = problem(rng, *shape, [5] * B)
+    new = [rows_bf16(rng, B, shape[1], shape[3], shape[4]).to(cuda_device) for _ in range(2)]
+    args = device_args(q, t1, ring, pos, cuda_device)
+    dims = cmc.CmcDims(*shape[:5], shape[5], shape[5], shape[6])
+    ws = cmc.DecodeWorkspace(dims, cuda_device)
+    cmc.lib().cmc_test_stall_attention_waits(1)
+    try:
+        cmc.decode_step_q8(*args, *new, workspace=ws)
+    finally:
+        cmc.lib().cmc_test_stall_attention_waits(0)
+    assert ws.status() & cmc.DEVFLAG_TIMEOUT
+    ws.buf.zero_()
+    args = device_args(q, t1, ring, pos, cuda_device)
+    got = cmc.decode_step_q8(*args, *new, workspace=ws)
+    assert ws.status() == 0
+    codes, scales = (x.copy() for x in ring)
+    q8.append(codes, scales, pos, *(to_f64(x) for x in new))
+    check_attention(got, to_f64(q), t1, (codes, scales), pos)
+
+
+def test_plan(cuda_device):
+    """Clusters, one CTA a unit, whole units and cut ones."""
+    def plan(B, L, H, k, W):
+        return cmc.decode_attn_q8_plan(cmc.CmcDims(B, L, 4 * H, H, 128, max(k, 1), k, W))
+    assert plan(1, 1, 2, 32, 128) == (4, 1)        # two tiles a unit, a cluster of two
+    assert plan(1, 32, 8, 128, 512) == (256, 1)    # one CTA a unit
+    ctas, launches = plan(40, 1, 8, 128, 512)      # 320 units on fewer CTAs: cut
+    assert ctas < 320 and launches == 2
+    assert plan(64, 32, 8, 128, 512)[0] == ctas
+
+
 # ---- refusals of the binding ----
 
 def test_binding_refusals(cuda_device):
@@ -413,6 +601,8 @@ def test_binding_refusals(cuda_device):
             (TypeError, lambda: attn(q, kv, None, kv, scales, pos)),
             (ValueError, lambda: attn(q, kv[:1].contiguous(), scales[:1].contiguous(), kv, scales, pos)),
             (ValueError, lambda: attn(q, None, None, kv, scales, pos, out=q[:1].contiguous())),
+            (ValueError, lambda: cmc.decode_step_q8(q, None, None, kv, scales, pos, row[:1].contiguous(), row)),
+            (ValueError, lambda: cmc.decode_step_q8(q, None, None, kv, scales, pos, row, row, rope_theta=0.0)),
             (ValueError, lambda: attn(q[:, :, :3].contiguous(), None, None, kv, scales, pos)),  # 3 over 2 heads
     ]:
         with pytest.raises(exc):

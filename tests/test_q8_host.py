@@ -161,6 +161,28 @@ def test_attention_q8_argument_checks(L):
     assert f(ws=0) == f(wsb=16) == WORKSPACE
 
 
+@host_only
+def test_decode_step_q8_argument_checks(L):
+    def f(theta=0.0, off=0, k_new=FAKE, ring=FAKE, wsb=1 << 30, **kw):
+        return L.cmc_decode_step_q8(FAKE, FAKE, FAKE, ring, FAKE, FAKE, k_new, FAKE,
+                                    ctypes.byref(_dims(**kw)), 0.0, theta, off, FAKE, FAKE, wsb, None)
+    assert f(k_new=0) == f(ring=0) == NULL
+    assert f(k_new=FAKE + 8) == ALIGN
+    assert f(d=96) == f(Hq=32) == SHAPE
+    assert f(k=101) == f(theta=-1.0) == f(theta=float("inf")) == f(theta=float("nan")) == RANGE
+    assert f(theta=1e4, off=-1) == f(theta=1e4, off=2 ** 32 + 1) == RANGE
+    assert f(wsb=16) == WORKSPACE
+
+
+def test_decode_attn_q8_plan_argument_checks(L):
+    ctas, launches = ctypes.c_int(0), ctypes.c_int(0)
+    def f(dims, a=ctypes.byref(ctas)):
+        return L.cmc_decode_attn_q8_plan(dims, 1, a, ctypes.byref(launches))
+    assert f(None) == f(ctypes.byref(_dims()), None) == NULL
+    assert f(ctypes.byref(_dims(d=96))) == SHAPE
+    assert f(ctypes.byref(_dims(k=101))) == RANGE
+
+
 def test_binding_refuses_cpu_tensors():
     kv = torch.zeros(1, 1, 1, 2, 32, 64).to(torch.float8_e4m3fn)
     scales = torch.zeros(1, 1, 1, 2, 4, dtype=torch.uint8).view(torch.float8_e8m0fnu)
@@ -169,6 +191,7 @@ def test_binding_refuses_cpu_tensors():
     row = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16)
     for call in (lambda: cmc.quantize_cache(bank, bank), lambda: cmc.dequantize_cache(kv, scales),
                  lambda: cmc.window_append_q8(kv, scales, pos, row, row),
-                 lambda: cmc.two_tier_decode_attn_q8(row, kv, scales, kv, scales, pos)):
+                 lambda: cmc.two_tier_decode_attn_q8(row, kv, scales, kv, scales, pos),
+                 lambda: cmc.decode_step_q8(row, kv, scales, kv, scales, pos, row, row)):
         with pytest.raises(ValueError, match="CUDA"):
             call()
