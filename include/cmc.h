@@ -520,6 +520,15 @@ CMC_API int cmc_dequantize_cache(const void* kv, const void* scales, const int32
 CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos, const void* k_new,
                                  const void* v_new, const cmc_dims* dims, void* stream);
 
+/* Bytes of workspace cmc_two_tier_decode_attn_q8 and cmc_decode_step_q8 need for
+ * `dims`: the device status word (read by cmc_read_status), one 8-byte counter
+ * per sequence, and, above 128 (sequence, layer, KV head) units, fp32 partial
+ * results.  Zero-fill it once before its first use, and again after a call
+ * that raised CMC_DEVFLAG_TIMEOUT; every other call leaves the counters at zero.
+ * It depends on B, Hq / Hkv, d and on whether there are more than 128 units:
+ * one workspace serves every call alike in these, whatever its k, N and W. */
+CMC_API size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims);
+
 /*
  * cmc_two_tier_decode_attn over a cache in 8 bits: Tier-1 is rows 0 .. k-1 of
  * its cache (as cmc_quantize_cache leaves the selected rows), Tier-2 the
@@ -529,9 +538,8 @@ CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos,
  *   tier1_kv, tier1_scales    the format above with T = N (may be NULL when k == 0)
  *   ring_kv, ring_scales      the format above with T = W
  *   pos                       int64 [B]  tokens appended so far (read only)
- *   scale, out, workspace     as for cmc_two_tier_decode_attn: the workspace is
- *                             that of cmc_decode_attn_workspace_size(dims), and one
- *                             workspace serves both
+ *   scale, out                as for cmc_two_tier_decode_attn
+ *   workspace                 see cmc_decode_attn_q8_workspace_size
  *
  * Products are exact and sums fp32.  A probability is rounded to eight significant
  * bits (as to bf16), or to 2^-18 of the largest where it is far below that; a
@@ -567,7 +575,10 @@ CMC_API int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* 
                                size_t workspace_bytes, void* stream);
 
 /* cmc_decode_attn_plan for the calls over a cache in 8 bits (fused == 0:
- * cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8).  Their tiles are of 128 keys. */
+ * cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8): *launches is 1 when every
+ * (sequence, layer, KV head) unit has a CTA or a cluster of CTAs of its own, 2 when
+ * there are more units than resident CTAs (then the live keys of all of them
+ * are shared out evenly, and a kernel merges the units that this cuts). */
 CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas, int* launches);
 
 /* ------------------------------------------------------------------------ *

@@ -14,6 +14,7 @@ from .cmc import (  # noqa: F401
     bridge_epilogue,
     decode_attn_plan,
     decode_attn_q8_plan,
+    decode_attn_q8_workspace_size,
     decode_attn_workspace_size,
     decode_step,
     decode_step_q8,

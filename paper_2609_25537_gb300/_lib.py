@@ -38,6 +38,7 @@ EXPORTS = (
     "cmc_quantize_cache",
     "cmc_dequantize_cache",
     "cmc_window_append_q8",
+    "cmc_decode_attn_q8_workspace_size",
     "cmc_two_tier_decode_attn_q8",
     "cmc_decode_step_q8",
     "cmc_decode_attn_q8_plan",
@@ -121,6 +122,7 @@ _SIGNATURES = {
     "cmc_quantize_cache": (_i, [_vp, _vp, _vp, _vp, _dims_p, _vp, _vp, _vp, _vp]),
     "cmc_dequantize_cache": (_i, [_vp, _vp, _vp, _dims_p, _vp, _vp, _vp, _vp]),
     "cmc_window_append_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _dims_p, _vp]),
+    "cmc_decode_attn_q8_workspace_size": (_sz, [_dims_p]),
     "cmc_two_tier_decode_attn_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float, _vp,
                                          _vp, _sz, _vp]),
     "cmc_decode_step_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float,

@@ -55,6 +55,7 @@ __all__ = [
     "two_tier_decode_attn_q8",
     "decode_step_q8",
     "decode_attn_q8_plan",
+    "decode_attn_q8_workspace_size",
     "q8_scale_bytes",
     "set_l2_prefetch_tiles",
     "dims_of",
@@ -320,14 +321,19 @@ def decode_attn_plan(dims: CmcDims, fused: bool = True, rope: bool = False) -> T
     return int(ctas.value), int(launches.value)
 
 
+def decode_attn_q8_workspace_size(dims: CmcDims) -> int:
+    return int(lib().cmc_decode_attn_q8_workspace_size(ctypes.byref(dims)))
+
+
 class DecodeWorkspace:
-    """Zero-filled device workspace for the attention entry points.
+    """Zero-filled device workspace for the attention entry points (with ``q8`` for
+    those over a cache in 8 bits).
 
     Holds the device status word and the fp32 partial results of keys split
     between CTAs.  Calls sharing one workspace must be ordered on one stream."""
 
-    def __init__(self, dims: CmcDims, device: torch.device):
-        n = decode_attn_workspace_size(dims)
+    def __init__(self, dims: CmcDims, device: torch.device, q8: bool = False):
+        n = decode_attn_q8_workspace_size(dims) if q8 else decode_attn_workspace_size(dims)
         if n == 0:
             raise ValueError(f"unsupported dims {dims.key()}")
         self.dims = dims
@@ -509,6 +515,8 @@ def window_append(ring_k: torch.Tensor, ring_v: torch.Tensor, pos: torch.Tensor,
 # The two-tier cache in 8 bits
 # ----------------------------------------------------------------------------
 
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
 _E4M3 = torch.float8_e4m3fn
 _E8M0 = torch.float8_e8m0fnu
 
@@ -532,30 +540,58 @@ def _need_q8(kv: torch.Tensor, scales: torch.Tensor, name: str, device) -> Tuple
     return shape
 
 
-def _need_rows(idx, count, B, N, dev) -> int:
-    """Checks the row index and the token counts of a call; returns the rows."""
-    if idx is not None:
-        _need(idx, "idx", torch.int32, 2, dev)
-        if int(idx.shape[0]) != B:
-            raise ValueError(f"idx shape {tuple(idx.shape)} does not match batch {B}")
+def _need_new(k_new, v_new, want, dev) -> None:
+    """Checks a new token's rows."""
+    _need(k_new, "k_new", torch.bfloat16, 4, dev)
+    _need(v_new, "v_new", torch.bfloat16, 4, dev)
+    if k_new.shape != want or v_new.shape != want:
+        raise ValueError(f"k_new/v_new must be {want}")
+
+
+def _need_rows(idx, count, source, dim, dev) -> int:
+    """Checks the row index and the token counts of a call; returns the rows
+    (without an index all of `source`, whose dimension `dim` they are)."""
+    B = source.shape[0]
     if count is not None:
         _need(count, "count", torch.int64, 1, dev)
-        if int(count.shape[0]) != B:
+        if count.shape[0] != B:
             raise ValueError("count must be [B]")
-    return N if idx is None else int(idx.shape[1])
+    if idx is None:
+        return source.shape[dim]
+    _need(idx, "idx", torch.int32, 2, dev)
+    if idx.shape[0] != B:
+        raise ValueError(f"idx shape {tuple(idx.shape)} does not match batch {B}")
+    return idx.shape[1]
 
 
-def _call(dev: torch.device, name: str, *args) -> None:
-    """Calls a library function whose last argument is the stream, with the
-    tensors' device current (a launch goes to the current one)."""
-    fn = getattr(lib(), name)
-    if dev.index != torch.cuda.current_device():
-        with torch.cuda.device(dev):
-            st = fn(*args, _stream(dev))
-    else:
-        st = fn(*args, _stream(dev))
-    if st:
-        check(st, name)
+def _elsewhere(index: int, fn, *args) -> int:
+    """Calls a library function with the tensors' device current (a launch goes to
+    the current one)."""
+    with torch.cuda.device(index):
+        return fn(*args)
+
+
+# Shapes that go together, and the sizes that they give: what a call can tell from
+# its tensors' shapes alone is worked out once for each combination of them.  What
+# is left for every call are the types, layouts and devices.  (A decode step's call
+# takes 10 us on the host with this and took 21 without, more than the GPU needs for
+# it up to some 60 MB of cache.)
+_shapes_cache: Dict[Tuple, Tuple] = {}
+_SHAPES_MOST = 4096  # combinations kept; beyond, each call works its own out
+
+
+def _kept(key: Tuple, value: Tuple) -> Tuple:
+    if len(_shapes_cache) < _SHAPES_MOST:
+        _shapes_cache[key] = value
+    return value
+
+
+def _as(dtype: torch.dtype, index: int, *tensors) -> bool:
+    """Whether all tensors (None: none) have this type and device and are contiguous."""
+    for t in tensors:
+        if t is not None and not (t.dtype is dtype and t.is_contiguous() and t.get_device() == index):
+            return False
+    return True
 
 
 @_ranged
@@ -570,21 +606,33 @@ def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor]
     indices raise DEVFLAG_BAD_INDEX in ``workspace``'s status word when one is given."""
     _need(k, "k", torch.bfloat16, 5)
     dev = k.device
-    _need(v, "v", torch.bfloat16, 5, dev)
-    if v.shape != k.shape:
+    index = dev.index
+    if not _as(torch.bfloat16, index, v) or v.shape != k.shape:
+        _need(v, "v", torch.bfloat16, 5, dev)
         raise ValueError("v must have the shape of k")
-    B, L, Hkv, N, d = k.shape
-    rows = _need_rows(idx, count, B, N, dev)
-    shape, sshape = (B, L, Hkv, 2, rows, d), (B, L, Hkv, 2, q8_scale_bytes(rows))
+    rows = _need_rows(idx, count, k, 3, dev)
+    key = ("quantize", k.shape, rows)
+    kept = _shapes_cache.get(key)
+    if kept is None:
+        B, L, Hkv, N, d = k.shape
+        dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
+        kept = _kept(key, ((B, L, Hkv, 2, rows, d), (B, L, Hkv, 2, q8_scale_bytes(rows)), dims,
+                           ctypes.byref(dims)))
+    shape, sshape, _, dims = kept
     if out_kv is None:
         out_kv = torch.empty(shape, dtype=_E4M3, device=dev)
     if out_scales is None:
         out_scales = torch.empty(sshape, dtype=_E8M0, device=dev)
-    if _need_q8(out_kv, out_scales, "out", dev) != shape:
+    if not (_as(_E4M3, index, out_kv) and _as(_E8M0, index, out_scales) and out_kv.shape == shape
+            and out_scales.shape == sshape):
+        _need_q8(out_kv, out_scales, "out", dev)
         raise ValueError(f"out_kv must be {shape}")
-    dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
-    _call(dev, "cmc_quantize_cache", _p(k), _p(v), _p(idx), _p(count), ctypes.byref(dims), _p(out_kv),
-          _p(out_scales), 0 if workspace is None else _p(workspace.buf))
+    fn = lib().cmc_quantize_cache
+    args = (k.data_ptr(), v.data_ptr(), _p(idx), _p(count), dims, out_kv.data_ptr(), out_scales.data_ptr(), 0 if workspace is None else _p(workspace.buf),
+            _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_quantize_cache")
     return out_kv, out_scales
 
 
@@ -597,20 +645,30 @@ def dequantize_cache(kv: torch.Tensor, scales: torch.Tensor, idx: Optional[torch
     those that ``idx`` [B, k] names.  See cmc_dequantize_cache."""
     _need(kv, "kv", _E4M3, 6)
     dev = kv.device
-    B, L, Hkv, _, N, d = _need_q8(kv, scales, "cache", dev)
-    rows = _need_rows(idx, None, B, N, dev)
-    want = (B, L, Hkv, rows, d)
+    index = dev.index
+    rows = _need_rows(idx, None, kv, 4, dev)
+    key = ("dequantize", kv.shape, scales.shape, rows)
+    kept = _shapes_cache.get(key)
+    if kept is None or not _as(_E8M0, index, scales):
+        B, L, Hkv, _, N, d = _need_q8(kv, scales, "cache", dev)
+        dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
+        kept = _kept(key, ((B, L, Hkv, rows, d), dims, ctypes.byref(dims)))
+    want, _, dims = kept
     if out_k is None:
         out_k = torch.empty(want, dtype=torch.bfloat16, device=dev)
     if out_v is None:
         out_v = torch.empty(want, dtype=torch.bfloat16, device=dev)
-    for t, name in ((out_k, "out_k"), (out_v, "out_v")):
-        _need(t, name, torch.bfloat16, 5, dev)
-        if tuple(t.shape) != want:
-            raise ValueError(f"{name} must be {want}")
-    dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
-    _call(dev, "cmc_dequantize_cache", _p(kv), _p(scales), _p(idx), ctypes.byref(dims), _p(out_k),
-          _p(out_v), 0 if workspace is None else _p(workspace.buf))
+    if not (_as(torch.bfloat16, index, out_k, out_v) and out_k.shape == want and out_v.shape == want):
+        for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+            _need(t, name, torch.bfloat16, 5, dev)
+            if tuple(t.shape) != want:
+                raise ValueError(f"{name} must be {want}")
+    fn = lib().cmc_dequantize_cache
+    args = (kv.data_ptr(), scales.data_ptr(), _p(idx), dims, out_k.data_ptr(), out_v.data_ptr(), 0 if workspace is None else _p(workspace.buf),
+            _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_dequantize_cache")
     return out_k, out_v
 
 
@@ -621,21 +679,30 @@ def window_append_q8(ring_kv: torch.Tensor, ring_scales: torch.Tensor, pos: torc
     cmc_window_append_q8."""
     _need(ring_kv, "ring_kv", _E4M3, 6)
     dev = ring_kv.device
-    B, L, Hkv, _, W, d = _need_q8(ring_kv, ring_scales, "ring", dev)
-    _need(pos, "pos", torch.int64, 1, dev)
-    _need(k_new, "k_new", torch.bfloat16, 4, dev)
-    _need(v_new, "v_new", torch.bfloat16, 4, dev)
-    want = (B, L, Hkv, d)
-    if k_new.shape != want or v_new.shape != want:
-        raise ValueError(f"k_new/v_new must be {want}")
-    if int(pos.shape[0]) != B:
-        raise ValueError("pos must be [B]")
-    dims = CmcDims(B, L, Hkv, Hkv, d, 1, 0, W)
-    _call(dev, "cmc_window_append_q8", _p(ring_kv), _p(ring_scales), _p(pos), _p(k_new), _p(v_new),
-          ctypes.byref(dims))
+    index = dev.index
+    key = None
+    if (_as(_E8M0, index, ring_scales) and _as(torch.int64, index, pos)
+            and _as(torch.bfloat16, index, k_new, v_new)):
+        key = ("append", ring_kv.shape, ring_scales.shape, pos.shape, k_new.shape, v_new.shape)
+    kept = _shapes_cache.get(key)
+    if kept is None:
+        B, L, Hkv, _, W, d = _need_q8(ring_kv, ring_scales, "ring", dev)
+        _need(pos, "pos", torch.int64, 1, dev)
+        if int(pos.shape[0]) != B:
+            raise ValueError("pos must be [B]")
+        _need_new(k_new, v_new, (B, L, Hkv, d), dev)
+        dims = CmcDims(B, L, Hkv, Hkv, d, 1, 0, W)
+        kept = _kept(key, (dims, ctypes.byref(dims)))
+    fn = lib().cmc_window_append_q8
+    args = (ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), kept[1],
+            _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_window_append_q8")
 
 
-def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out, workspace):
+def _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new) -> CmcDims:
+    """Checks the tensors of an attention call over 8-bit caches one by one."""
     _need(q, "q", torch.bfloat16, 4)
     dev = q.device
     B, L, Hq, d = q.shape
@@ -653,22 +720,46 @@ def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out, wor
     _need(pos, "pos", torch.int64, 1, dev)
     if int(pos.shape[0]) != B:
         raise ValueError(f"pos shape {tuple(pos.shape)} does not match batch {B}")
+    if new is not None:
+        _need_new(*new, (B, L, Hkv, d), dev)
+    return CmcDims(B, L, Hq, Hkv, d, max(k, 1), k, W)
+
+
+def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, out, workspace):
+    """(device index, dims by reference, output, workspace) of an attention call."""
+    key = None
+    index = q.get_device() if isinstance(q, torch.Tensor) else -1
+    if (index >= 0 and _as(torch.bfloat16, index, q) and _as(_E4M3, index, ring_kv, tier1_kv)
+            and _as(_E8M0, index, ring_scales, tier1_scales) and _as(torch.int64, index, pos)
+            and (new is None or _as(torch.bfloat16, index, *new))):
+        key = ("attend", q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
+               None if tier1_kv is None else tier1_kv.shape,
+               None if tier1_scales is None else tier1_scales.shape,
+               None if new is None else (new[0].shape, new[1].shape))
+    kept = _shapes_cache.get(key)
+    if kept is None:
+        dims = _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new)
+        units = dims.B * dims.L * dims.Hkv
+        # (what the size of a workspace depends on, with room for other shapes alike in it)
+        kept = _kept(key, (dims, ctypes.byref(dims),
+                           ("q8", dims.B, dims.Hq // dims.Hkv, dims.d, units > 128)))
+    dims, ref, sizes = kept
     if out is None:
         out = torch.empty_like(q)
-    else:
-        _need(out, "out", torch.bfloat16, 4, dev)
-        if out.shape != q.shape:
-            raise ValueError("out must have the shape of q")
-    sizes = (B, L, Hq, Hkv, d, max(k, 1), k, W)
-    dims = CmcDims(*sizes)
+    elif not _as(torch.bfloat16, index, out) or out.shape != q.shape:
+        _need(out, "out", torch.bfloat16, 4, q.device)
+        raise ValueError("out must have the shape of q")
     if workspace is None:
         # A call that is being captured gets a workspace of its graph's own: the
         # kept ones are zero-filled once, outside of it, and other calls use them.
-        if torch.cuda.is_current_stream_capturing():
-            workspace = DecodeWorkspace(dims, dev)
+        if torch._C._cuda_isCurrentStreamCapturing():
+            workspace = DecodeWorkspace(dims, q.device, q8=True)
         else:
-            workspace = _workspace_for(sizes, dims, dev, _stream(dev))
-    return dims, dev, out, workspace
+            stream = _raw_stream(index)
+            workspace = _ws_cache.get((index, stream, sizes))
+            if workspace is None:
+                workspace = _ws_cache[(index, stream, sizes)] = DecodeWorkspace(dims, q.device, q8=True)
+    return index, ref, out, workspace
 
 
 @_ranged
@@ -677,13 +768,17 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
                             workspace: Optional[DecodeWorkspace] = None) -> torch.Tensor:
     """Decode attention over [Tier-1 | occupied ring slots], both caches in 8 bits
     (tier1_kv and tier1_scales None: the ring alone); see
-    cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  Without a ``workspace``
-    the call keeps one per stream and shape; a captured call then gets one of its own,
-    zero-filled at every replay."""
-    dims, dev, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out,
-                                       workspace)
-    _call(dev, "cmc_two_tier_decode_attn_q8", _p(q), _p(tier1_kv), _p(tier1_scales), _p(ring_kv),
-          _p(ring_scales), _p(pos), ctypes.byref(dims), _scale(scale), _p(out), _p(ws.buf), ws.nbytes)
+    cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a
+    DecodeWorkspace(dims, device, q8=True); without one the call keeps one per stream and
+    kind of shape, and a captured call gets one of its own, zero-filled at every replay."""
+    index, dims, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
+                                         out, workspace)
+    fn = lib().cmc_two_tier_decode_attn_q8
+    args = (q.data_ptr(), _p(tier1_kv), _p(tier1_scales), ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), dims, _scale(scale), out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+            _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_two_tier_decode_attn_q8")
     return out
 
 
@@ -696,19 +791,16 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     attend; see cmc_decode_step_q8.  Updates ring_kv, ring_scales and pos in place.
     ``rope_theta`` and ``rope_offset`` as for :func:`decode_step`, ``workspace`` as for
     :func:`two_tier_decode_attn_q8`."""
-    dims, dev, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, out,
-                                       workspace)
-    _need(k_new, "k_new", torch.bfloat16, 4, dev)
-    _need(v_new, "v_new", torch.bfloat16, 4, dev)
-    want = (dims.B, dims.L, dims.Hkv, dims.d)
-    if k_new.shape != want or v_new.shape != want:
-        raise ValueError(f"k_new/v_new must be {want}")
     if rope_theta is not None and not rope_theta > 0:
         raise ValueError("rope_theta must be positive")
-    _call(dev, "cmc_decode_step_q8", _p(q), _p(tier1_kv), _p(tier1_scales), _p(ring_kv),
-          _p(ring_scales), _p(pos), _p(k_new), _p(v_new), ctypes.byref(dims), _scale(scale),
-          0.0 if rope_theta is None else float(rope_theta), int(rope_offset), _p(out), _p(ws.buf),
-          ws.nbytes)
+    index, dims, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos,
+                                         (k_new, v_new), out, workspace)
+    fn = lib().cmc_decode_step_q8
+    args = (q.data_ptr(), _p(tier1_kv), _p(tier1_scales), ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), dims, _scale(scale), 0.0 if rope_theta is None else float(rope_theta), int(rope_offset), out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
+            _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_decode_step_q8")
     return out
 
 

@@ -1,16 +1,27 @@
 // Decode attention over the two-tier cache held in 8 bits (format: cmc_q8.cuh),
 // alone and fused with the append of the step's token.
 //
-// Work decomposition, pipeline and merges are those of the attention over a bf16
-// cache (cmc_attn.cu): units (sequence, layer, KV head), a producer warp and four
-// consumer warps a CTA, clusters for few long units, runs of whole units or
-// stream-K for many.  What differs follows from the 8 bits.
+// The unit of work is a warp's: a block of 32 keys of one unit (sequence, layer, KV
+// head), which is one block of the format, with one power of two for K and one for
+// V.  A CTA is four warps that have little to do with each other: each loads its own
+// blocks into its own ring of stages, a TMA box of 32 rows of K and of V each (8 KB
+// at d = 128), and refills a stage as soon as it is done with it, so there is no
+// producer and no barrier between loading and computing but the stage's "full" one.
 //
-// Tiles of 128 keys: 128 codes rows of K and of V, 32 KB at d = 128, come as one TMA
-// box of a [2 units, T, d] tensor (rows past T are not read), as many bytes as
-// the 64-key tiles of the bf16 kernel.  A warp owns 32 keys, which are one block
-// with one power of two for K and one for V; the tile's four of each are one
-// aligned word, copied by cp.async next to the tile.
+// Plans.  A unit's blocks are ceil(k / 32) of Tier-1, then those of the ring's live
+// slots.
+//   strided  (no more units than resident CTAs): one CTA, or a cluster of cm CTAs,
+//            per unit; warp w of the unit's 4 cm takes blocks w, w + 4 cm, ...  Its
+//            first blocks do not depend on pos, so they are requested before pos is
+//            known.  The warps' states are merged in shared memory, the CTAs' in
+//            distributed shared memory (as in cmc_attn.cu).
+//   flat     (more units): every CTA works out from all of pos how many live blocks
+//            there are and every warp of the grid takes an equal, contiguous run of
+//            them.  A unit that lies whole in a warp's run (the rule where units are
+//            short) is written by that warp alone; of a unit that is cut the pieces
+//            go to global memory, merged by a small kernel that follows.  Runs of
+//            live blocks are equal whatever the rings' fill: 64 sequences with rings
+//            filled to a third in the mean, 256 + 2,048 keys at most: see DESIGN.
 //
 // Both products run on e4m3 operands (mma.sync m16n8k32, fp32 accumulation,
 // exact products), so no code is ever converted: K by ldmatrix, V by the byte
@@ -26,7 +37,7 @@
 // pieces are the columns 4 .. 7 of the same products, so they cost nothing; for
 // G = 8 they take products of their own.
 //   S^T = K Q^T   16 keys as the rows, d in k-steps of 32
-//   O^T += V^T P^T  16 rows of the head dimension, the warp's 32 keys as the k-step
+//   O^T += V^T P^T  16 rows of the head dimension, the block's 32 keys as the k-step
 // K's power of two joins the softmax scale.  V's cannot (it changes from block to
 // block): O is kept in units of 2^(E - 127) with E the byte of a recent block, and
 // rescaled, as for a new maximum, when a block's byte is above E or more than four
@@ -45,50 +56,54 @@
 
 namespace cmc {
 
-constexpr int kQ8Tile = 128;  // keys per pipeline tile; each consumer warp owns 32 of them
-constexpr int kQ8Stages = 3;
-static_assert(kQ8Tile == kWarps * kQ8Block, "a warp's keys are one block");
-enum { H_KSCALES = H_BADLO, H_VSCALES = H_BADHI };  // the tile's four bytes of K and of V
+// The flat plan's grid is limited so that a workspace's size does not depend on the
+// device: two records for each of its warps.
+constexpr int kQ8MaxCtas = 320;
+constexpr int kQ8RecHead = 4;  // words before a record's maxima: valid, ends
+// Units up to which a call never takes the flat plan (and its workspace holds no records).
+constexpr int kQ8StridedUnits = 128;
 
 struct Q8Maps {
-  CUtensorMap t1, ring;  // [2 units, T, d] bytes, box 2 x 128 rows
+  CUtensorMap t1, ring;  // [2 units, T, d] bytes, box 2 x 32 rows
 };
 
-struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx are not used
+struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the split of cmc_attn.cu are not used
   uint8_t* ring_kv;           // [B, L, Hkv, 2, W, d]
   uint8_t* ring_scales;       // [B, L, Hkv, 2, ringS]
   const uint8_t* t1_scales;   // [B, L, Hkv, 2, t1S]
   int ringS, t1S;
+  int nb1, nb2;               // blocks of Tier-1, and of the whole ring
   int rope;                   // rotate q and the new key (fused step)
-};
+};                            // cm: CTAs per unit (strided plan), 0: flat plan
 
-// Shared memory: the stages (codes of K, then of V), one slot per stage with what a
-// unit needs besides (its query rows, the new token's rows, the rotary table),
-// the headers, the warps' (max, sum) for the merge.
-//
-// Slots go by unit, in turn: a unit's slot is taken again three units later, when
-// at least three tiles were handed back since.  Under a cluster plan a CTA has
-// one unit, so slots 1 and 2 are free for what its peers send (see recv_group).
+// Shared memory of a CTA: per warp a query slot, two slots for the new token's rows, a
+// rotary table and the headers of its stages; the warps' (max, sum) and what a
+// cluster's peers send; then, 1,024-byte aligned, the stages.
 template <int D, int G>
 struct Q8Smem {
-  static constexpr int kV = kQ8Tile * D;
-  static constexpr int kStage = 2 * kQ8Tile * D;
-  static constexpr int kQ = 0;                   // query rows [G][D] bf16
-  static constexpr int kNew = G * D * 2;         // new token K row, V row (bf16)
-  static constexpr int kRope = kNew + 2 * D * 2; // d/2 (cos, sin) pairs
-  static constexpr int kSlot = kRope + D * 4;
-  static constexpr int kSlots = kQ8Stages * kStage;  // offsets from the aligned base
-  static constexpr int kHdrs = kSlots + kQ8Stages * kSlot;
-  static constexpr int kMergeM = kHdrs + kQ8Stages * 32;
-  static constexpr int kMergeL = kMergeM + kWarps * 8 * 4;
-  static constexpr int kBytes = kMergeL + kWarps * 8 * 4 + 1008;  // the base is 16-byte aligned
-  // received: cm * ceil(G D / 4 / cm) groups of 16 bytes, then (max, sum) of G heads from each rank
-  static constexpr int kRecv = kSlots + kSlot;
+  // 96 KB of stages a CTA, two CTAs an SM; at d = 128 and G = 8 the rest does not fit beside
+  // that twice, and one CTA an SM has them all.
+  static constexpr int NST = D == 64 || G == 8 ? 6 : 3;
+  static constexpr int kV = kQ8Block * D;
+  static constexpr int kStage = 2 * kQ8Block * D;
+  static constexpr int kQ = 0;                                // [warp][G][D] bf16
+  static constexpr int kNew = kQ + kWarps * G * D * 2;        // [warp][2][K row, V row] bf16
+  static constexpr int kRope = kNew + kWarps * 2 * 2 * D * 2; // [warp][d/2] (cos, sin)
+  static constexpr int kHdr = kRope + kWarps * D * 4;         // [warp][NST][8] words
+  static constexpr int kMergeM = kHdr + kWarps * NST * 32;    // [warp][8]
+  static constexpr int kMergeL = kMergeM + kWarps * 32;
+  static constexpr int kRecv = kMergeL + kWarps * 32;         // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
-  static_assert(kRecvMl + kMaxClusterCtas * G * 8 <= kHdrs, "slots 1 and 2 hold what the peers send");
+  static constexpr int kSmall = kRecvMl + kMaxClusterCtas * G * 8;
+  static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
 };
+// Header words of a stage: what the warp has to know of the block in it.
+enum { Q_WHAT = 0, Q_UNIT = 1, Q_SLOT = 2, Q_LEFT = 3, Q_KS = 4, Q_VS = 5, Q_POS = 6 };
+// Q_WHAT: rows that hold a key (0 .. 32) | the new token's row (255: none) << 8 |
+// the block's byte in the words of powers of two << 16 | flags << 24
+enum { QF_FIRST = 1, QF_LAST = 2 };  // the unit's first / last block
 
-// Offset of 16-byte chunk c of row r in a K or V region: TMA's 128-byte swizzle, or the
+// Offset of 16-byte chunk c of row r of a stage's K or V: TMA's 128-byte swizzle, or the
 // 64-byte one for rows of 64 codes.
 template <int D>
 __device__ __forceinline__ uint32_t swz8(int r, int c) {
@@ -154,50 +169,93 @@ __device__ __forceinline__ void two_pieces(float a, float b, uint32_t& hi, uint3
   lo = l;
 }
 
-__device__ __forceinline__ int tile_row(const AttnQ8Params& p, const TileCursor& c) {
-  return (c.lt < p.t1_tiles ? c.lt : c.lt - p.t1_tiles) * kQ8Tile;
-}
-__device__ __forceinline__ const CUtensorMap* tile_map(const AttnQ8Params& p, const Q8Maps& maps,
-                                                       const TileCursor& c) {
-  return c.lt < p.t1_tiles ? &maps.t1 : &maps.ring;
-}
-// The producer's lanes 0 and 1: the tile's powers of two of K and of V into the header.
-__device__ __forceinline__ void load_scales(const AttnQ8Params& p, const TileCursor& c, uint8_t* hdr,
-                                            int lane) {
-  const bool t1 = c.lt < p.t1_tiles;
-  const int S = t1 ? p.t1S : p.ringS;
-  const uint8_t* from = (t1 ? p.t1_scales : p.ring_scales) + (2LL * c.u + lane) * S +
-                        (t1 ? c.lt : c.lt - p.t1_tiles) * 4;
-  cp_async_4(smem_addr(hdr + 4 * (lane ? H_VSCALES : H_KSCALES)), from, 4u);
+// Live blocks of a unit whose sequence's state is sq (one, empty, where there are none: its
+// output is still to be written).
+__device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState& sq) {
+  const int n = sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
+  return n > 0 ? n : 1;
 }
 
-// The new token in its block, by the consumer warp that owns it: the token's codes over
-// the stale ones, in the tile and in the ring; the block's other codes too where
-// its power of two changes.  `others`: the block's rows that hold another token.
-// Returns the block's byte.  (The rules are window_append_q8_kernel's.)
+// Requests block j of unit u: the codes by TMA, the two words that hold its powers of
+// two by lanes 0 and 1.  Called by the whole warp, converged.
 template <int D>
-__device__ __forceinline__ int patch_block(uint8_t* rows /* the tile's K or V */, uint8_t* ring_row0,
+__device__ __forceinline__ void load_block(const AttnQ8Params& p, const Q8Maps& maps, int u, int j,
+                                           uint8_t* stage, uint8_t* hdr, uint64_t* full, int lane) {
+  const bool t1 = j < p.nb1;
+  const int jj = t1 ? j : j - p.nb1;
+  if (lane < 2) {
+    const int S = t1 ? p.t1S : p.ringS;
+    const uint8_t* from = (t1 ? p.t1_scales : p.ring_scales) + (2LL * u + lane) * S + (jj & ~3);
+    cp_async_4(smem_addr(hdr + 4 * (Q_KS + lane)), from, 4u);
+    mbar_arrive_cp_async(full);
+  }
+  __syncwarp();
+  if (lane == 0) {
+    mbar_arrive_expect_tx(full, 2 * kQ8Block * D + p.stall_tx);
+    tma_box3_hint(smem_addr(stage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * u, full,
+                  policy_evict_first());
+  }
+}
+
+// The header of block j of unit u; `left`: blocks of the unit from here on in the warp's run.
+template <bool FUSED>
+__device__ __forceinline__ void write_header(const AttnQ8Params& p, uint8_t* hdr, int u, int j, int nb,
+                                             int left, const SeqState& sq) {
+  int n, new_row = 255;
+  if (j < p.nb1) {
+    n = sq.bad ? 0 : min(p.k - j * kQ8Block, kQ8Block);
+  } else {
+    const int r0 = (j - p.nb1) * kQ8Block;
+    n = min(max(sq.count - r0, 0), kQ8Block);
+    if (FUSED && sq.new_slot >= r0 && sq.new_slot - r0 < n) new_row = sq.new_slot - r0;
+  }
+  const int flags = (j == 0 ? QF_FIRST : 0) | (j == nb - 1 ? QF_LAST : 0);
+  const int sel = (j < p.nb1 ? j : j - p.nb1) & 3;
+  *reinterpret_cast<int4*>(hdr) = make_int4(n | (new_row << 8) | (sel << 16) | (flags << 24), u, sq.new_slot, left);
+  *reinterpret_cast<long long*>(hdr + 4 * Q_POS) = sq.pos;
+}
+
+// A unit's query rows and, for the fused step, its new token's rows.
+template <int D, int G, bool FUSED>
+__device__ __forceinline__ void load_query(const AttnQ8Params& p, int u, uint8_t* q, uint8_t* fresh,
+                                           uint64_t* bar) {
+  mbar_arrive_expect_tx(bar, G * D * 2 + (FUSED ? 2 * D * 2 : 0) + p.stall_tx);
+  bulk_copy(smem_addr(q), p.q + static_cast<long long>(u) * (G * D), G * D * 2, bar);
+  if (FUSED) {
+    bulk_copy(smem_addr(fresh), p.k_new + static_cast<long long>(u) * D, D * 2, bar);
+    bulk_copy(smem_addr(fresh + D * 2), p.v_new + static_cast<long long>(u) * D, D * 2, bar);
+  }
+}
+
+// The new token in its block: the token's codes over the stale ones, in the stage and in
+// the ring; the block's other codes too where its power of two changes.  `others`: the
+// block's rows that hold another token.  Returns the block's byte.  (The rules are
+// window_append_q8_kernel's.)
+template <int D>
+__device__ __forceinline__ int patch_block(uint8_t* rows /* the stage's K or V */, uint8_t* ring_row0,
                                            uint8_t* ring_scale, const float (&x)[4], int r, int c_old,
-                                           bool first, uint32_t others, int lane, int warp) {
+                                           bool first, uint32_t others, int lane) {
   uint32_t top = 0u;
 #pragma unroll
   for (int e = 0; e < D / 32; ++e) top = max(top, finite_bits(x[e]));
   top = __reduce_max_sync(0xffffffffu, top);
   const bool mine = (others >> lane) & 1u;  // the lane's row of the block
-  const int row = 32 * warp + lane;
   int c;
   if (first) {
     uint32_t m = 0u;
-    if (mine)
-      for (int q = 0; q < D / 16; ++q) m = max_codes16(m, *reinterpret_cast<const uint4*>(rows + swz8<D>(row, q)));
+    if (mine) {
+#pragma unroll
+      for (int q = 0; q < D / 16; ++q) m = max_codes16(m, *reinterpret_cast<const uint4*>(rows + swz8<D>(lane, q)));
+    }
     c = block_code(max(top, __reduce_max_sync(0xffffffffu, held_bits(m, c_old))));
   } else {
     c = max(block_code(top), c_old);
   }
   if (c != c_old && mine) {
     const float f = recode_factor(c_old, c);
+#pragma unroll
     for (int q = 0; q < D / 16; ++q) {
-      uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(row, q));
+      uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(lane, q));
       const uint4 y = recode16(*at, f);
       *at = y;
       reinterpret_cast<uint4*>(ring_row0 + static_cast<long long>(lane) * D)[q] = y;
@@ -207,102 +265,84 @@ __device__ __forceinline__ int patch_block(uint8_t* rows /* the tile's K or V */
   uint8_t* to = ring_row0 + static_cast<long long>(r) * D;
   if (D == 128) {
     const uint32_t w = encode4(x[0], x[1], x[2], x[3], f);
-    *reinterpret_cast<uint32_t*>(rows + swz8<D>(32 * warp + r, lane >> 2) + (lane & 3) * 4) = w;
+    *reinterpret_cast<uint32_t*>(rows + swz8<D>(r, lane >> 2) + (lane & 3) * 4) = w;
     reinterpret_cast<uint32_t*>(to)[lane] = w;
   } else {
     const uint16_t w = static_cast<uint16_t>(e4m3_pair(scaled(x[0], f), scaled(x[1], f)));
-    *reinterpret_cast<uint16_t*>(rows + swz8<D>(32 * warp + r, lane >> 3) + (lane & 7) * 2) = w;
+    *reinterpret_cast<uint16_t*>(rows + swz8<D>(r, lane >> 3) + (lane & 7) * 2) = w;
     reinterpret_cast<uint16_t*>(to)[lane] = w;
   }
   if (lane == 0) *ring_scale = static_cast<uint8_t>(c);
   return c;
 }
 
+// One warp's place in the flat plan's list of live blocks.
+struct FlatWalk {
+  int u, j, nb;   // unit, block, the unit's blocks
+  int b, x;       // sequence, unit within it
+  SeqState sq;
+};
+
 template <int D, int G, bool FUSED>
-__global__ void __maxnreg__(D == 64 ? 96 : 128)
+__global__ void __maxnreg__(168)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   using S = Q8Smem<D, G>;
-  constexpr int NST = kQ8Stages;
+  constexpr int NST = S::NST;
   constexpr int KS = D / 32;         // k-steps of the Q K^T product
   constexpr int MT = D / 16;         // m-tiles of O^T
   constexpr bool PAIRED = G <= 4;    // hi and lo pieces in one product
   constexpr int NV = PAIRED ? 2 : 4; // scores a thread has of each of its two heads
-  extern __shared__ __align__(16) uint8_t smem_raw[];
-  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-  uint8_t* slot0 = smem + S::kSlots;
-  uint8_t* hdr0 = smem + S::kHdrs;
-  float* merge_m = reinterpret_cast<float*>(smem + S::kMergeM);  // [kWarps][8]
-  float* merge_l = reinterpret_cast<float*>(smem + S::kMergeL);
-  __shared__ __align__(8) uint64_t full_bar[NST];
-  __shared__ __align__(8) uint64_t empty_bar[NST];
-  __shared__ __align__(8) uint64_t recv_bar;  // cluster plan: the peers' stores
+  constexpr int NGR = G * D / 4;     // groups of four rows of the head dimension of a unit's output
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ __align__(8) uint64_t full_bar[kWarps][NST];
+  __shared__ __align__(8) uint64_t q_bar[kWarps];
+  __shared__ __align__(8) uint64_t recv_bar;  // clusters: the peers' stores
+  __shared__ long long s_pos[kWarps];         // pos of the warps' first sequences
+  __shared__ int s_first[kWarps][2], s_last[kWarps], s_sum[kWarps];
 
   const int tid = threadIdx.x;
   const int lane = tid & 31;
   const int warp = tid >> 5;
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem + S::kSmall) + 1023) & ~uintptr_t(1023)) +
+                    warp * (NST * S::kStage);
+  uint8_t* hdrs = smem + S::kHdr + warp * (NST * 32);
+  uint8_t* q_slot = smem + S::kQ + warp * (G * D * 2);
+  uint8_t* new_slots = smem + S::kNew + warp * (2 * 2 * D * 2);
+  float2* rope_tab = reinterpret_cast<float2*>(smem + S::kRope + warp * (D * 4));
+  float* merge_m = reinterpret_cast<float*>(smem + S::kMergeM);  // [kWarps][8]
+  float* merge_l = reinterpret_cast<float*>(smem + S::kMergeL);
+  uint64_t* full = full_bar[warp];
 
-  // This CTA's first tile and its tiles, in order.
-  int u_begin, j_begin = 0, n_tiles;
-  {
-    const int cta = static_cast<int>(blockIdx.x);
-    if (p.cm > 0) {
-      u_begin = static_cast<int>(cluster_id());
-      j_begin = static_cast<int>(cluster_ctarank());
-      n_tiles = p.base + (j_begin < p.rem ? 1 : 0);
-    } else {
-      const int first = cta * p.base + min(cta, p.rem);
-      const int n = p.base + (cta < p.rem ? 1 : 0);
-      if (p.gran > 1) {  // whole units
-        u_begin = first;
-        n_tiles = n * p.gran;
-      } else {
-        u_begin = static_cast<int>(static_cast<unsigned>(first) / static_cast<unsigned>(p.tpu));
-        j_begin = first - u_begin * p.tpu;
-        n_tiles = n;
-      }
-    }
-  }
-  TileCursor c0;
-  c0.init(u_begin, j_begin, p);
+  // strided plan: the CTA's unit, the warp's first block and their distance
+  const int cm = p.cm;
+  const int su = cm > 1 ? static_cast<int>(cluster_id()) : static_cast<int>(blockIdx.x);
+  const int rank = cm > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+  const int g0 = rank * kWarps + warp, step = cm * kWarps;
+  const int nb_all = p.nb1 + p.nb2;
 
-  if (tid == 0) {
-    for (int s = 0; s < NST; ++s) {
-      mbar_init(&full_bar[s], 1);        // the producer's arrive (plus tracked cp.async arrivals)
-      mbar_init(&empty_bar[s], kWarps);  // one arrive per consumer warp
+  if (lane == 0) {
+    for (int s = 0; s < NST; ++s) mbar_init(&full[s], 1);  // lane 0's arrive (plus tracked cp.async arrivals)
+    mbar_init(&q_bar[warp], 1);
+    if (warp == 0) attn_abort = 0;
+    if (warp == 1 && cm > 1) {  // the groups this CTA finishes and the heads' (max, sum), from each rank
+      const int mine = min(max(NGR - rank * p.slice, 0), p.slice);
+      mbar_init(&recv_bar, 1);
+      mbar_arrive_expect_tx(&recv_bar, static_cast<uint32_t>(cm * (mine * 16 + G * 8)) + p.stall_tx);
     }
-    attn_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-  }
-  if (tid == 32 && p.cm > 0) {  // the groups this CTA finishes and the heads' (max, sum), from each rank
-    const int mine = min(max(G * D / 4 - j_begin * p.slice, 0), p.slice);
-    mbar_init(&recv_bar, 1);
-    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
-    mbar_arrive_expect_tx(&recv_bar, static_cast<uint32_t>(p.cm * (mine * 16 + G * 8)) + p.stall_tx);
   }
   __syncthreads();
-  if (p.cm > 0) cluster_arrive();  // waited for before the first store into a peer
-  // Before the grid dependency wait: the first tiles into L2.
-  if (lane == 0 && warp < kWarps) {
-    prefetch_map((warp & 1) && p.k > 0 ? &maps.t1 : &maps.ring);
-    TileCursor cp = c0;
-    const int npf = n_tiles < p.l2_prefetch ? n_tiles : p.l2_prefetch;
-    for (int i = 0; i < npf; ++i) {
-      if (i % kWarps == warp) tma_box3_prefetch(tile_map(p, maps, cp), tile_row(p, cp), 2 * cp.u);
-      cp.next(p);
+  if (cm > 1) cluster_arrive();  // waited for before the first store into a peer
+  // Before the grid dependency wait: the strided plan's first blocks into L2.
+  if (lane == 0) prefetch_map((warp & 1) && p.k > 0 ? &maps.t1 : &maps.ring);
+  if (cm > 0 && lane == 0) {
+    for (int i = 0; i < p.l2_prefetch && g0 + i * step < nb_all; ++i) {
+      const int j = g0 + i * step;
+      tma_box3_prefetch(j < p.nb1 ? &maps.t1 : &maps.ring, (j < p.nb1 ? j : j - p.nb1) * kQ8Block, 2 * su);
     }
   }
-  int last_b = c0.b;  // the sequence of the CTA's last tile (how far pos is read ahead)
-  if (warp == kWarps) {
-    if (lane == 0 && p.l2_prefetch > 0)
-      bulk_prefetch_l2(p.q + static_cast<long long>(c0.u) * (G * D), G * D * 2);
-    if (p.cm == 0 && n_tiles > p.tpu)
-      last_b = static_cast<int>(static_cast<unsigned>(c0.u + (c0.j + n_tiles - 1) / p.tpu) /
-                                static_cast<unsigned>(p.LH));
-    else if (p.cm == 0 && c0.j + n_tiles > p.tpu && c0.left == 1)
-      last_b = c0.b + 1;
-  }
-  unsigned long long turns[2] = {0ull, 0ull};  // this producer lane's rotary frequencies
-  if (FUSED && warp == kWarps && p.rope) {
+  unsigned long long turns[2] = {0ull, 0ull};  // this lane's rotary frequencies
+  if (FUSED && p.rope) {
     if (p.rope_slot >= 0) {
       turns[0] = g_rope_tables[p.rope_slot][lane];
       if (lane + 32 < D / 2) turns[1] = g_rope_tables[p.rope_slot][lane + 32];
@@ -314,150 +354,174 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
-  if (warp == kWarps) {
-    // ======================= producer warp =======================
-    long long* pos_s = reinterpret_cast<long long*>(hdr0 + 4 * H_POS);
-    if (lane == 0) {
-      cp_async_8(smem_addr(pos_s), p.pos + c0.b);
-      bulk_copy(smem_addr(slot0 + S::kQ), p.q + static_cast<long long>(c0.u) * (G * D), G * D * 2,
-                &full_bar[0]);
+  int n_run = 0;       // blocks of the warp's run
+  int issued = 0;      // of them requested
+  FlatWalk w;          // the next block to request
+  w.u = su;
+  w.j = g0;
+  w.nb = 0;
+  w.b = 0;
+  w.x = 0;
+  long long pos_next = 0;  // flat plan: pos of the next sequence, ahead of its use
+  int last_b = 0;          // the run's last sequence
+  bool counted = false;    // this warp's reading of pos is done and counted
+  if (cm > 0) {
+    // ---- strided: the first blocks at once, then pos ----
+    if (lane == 0 && g0 < nb_all) load_query<D, G, FUSED>(p, su, q_slot, new_slots, &q_bar[warp]);
+    for (; issued < NST && g0 + issued * step < nb_all; ++issued)
+      load_block<D>(p, maps, su, g0 + issued * step, stages + issued * S::kStage, hdrs + issued * 32, &full[issued],
+                    lane);
+    w.b = static_cast<int>(static_cast<unsigned>(su) / static_cast<unsigned>(p.LH));
+    if (tid == 0) s_pos[0] = ld_pos(p, w.b);
+    __syncthreads();
+    w.sq = seq_state<FUSED>(p, s_pos[0]);
+    if (tid == 0) {
+      if (w.sq.bad && rank == 0 && su % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+      if (FUSED) {  // the last CTA to have read pos[b] advances it
+        const unsigned long long old = atomicAdd(p.tickets + w.b, 1ull);
+        if (old + 1 == static_cast<unsigned long long>(p.LH) * cm) {
+          if (!w.sq.bad) p.pos[w.b] = w.sq.pos + 1;
+          p.tickets[w.b] = 0ull;
+        }
+      }
     }
-    cp_async_commit();
-    // the first stages' powers of two: they do not depend on pos
-    TileCursor ci = c0;
+    w.nb = live_blocks(p, w.sq);
+    n_run = w.nb > g0 ? (w.nb - g0 + step - 1) / step : 0;
+    w.j = g0 + issued * step;
+    if (n_run < issued) n_run = issued;  // blocks that were requested in vain hold no key
+    if (lane == 0)
+      for (int i = 0; i < issued; ++i)
+        write_header<FUSED>(p, hdrs + i * 32, su, g0 + i * step, 0, n_run - i, w.sq);
+  } else {
+    // ---- flat: the runs from all of pos ----
+    const int chunk = (p.B + kThreads - 1) / kThreads;
+    const int b0 = tid * chunk, b1 = min(b0 + chunk, p.B);
+    int sum = 0;
+    for (int b = b0; b < b1; ++b) {
+      const SeqState sq = seq_state<FUSED>(p, ld_pos(p, b));
+      if (sq.bad && blockIdx.x == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+      sum += live_blocks(p, sq);
+    }
+    int scan = sum;  // inclusive, over the warp
 #pragma unroll
-    for (int i = 0; i < NST; ++i) {
-      if (i < n_tiles && lane < 2) {
-        load_scales(p, ci, hdr0 + i * 32, lane);
-        mbar_arrive_cp_async(&full_bar[i]);
-      }
-      ci.next(p);
+    for (int off = 1; off < 32; off <<= 1) {
+      const int up = __shfl_up_sync(0xffffffffu, scan, off);
+      if (lane >= off) scan += up;
     }
-    cp_async_commit();
-    ci = c0;
-    int run_b = ci.b;        // sequence of the current run of tiles
-    long long pos_next = 0;  // pos of the sequence after it, ahead of its use
-    if (run_b < last_b) pos_next = ld_pos(p, run_b + 1);
-    int issued = 0;
-    int run_tiles = 0;       // tiles in that run so far
-    int slot = 0;            // the unit's slot
-    float2 rope[2] = {make_float2(1.f, 0.f), make_float2(1.f, 0.f)};
-    cp_async_wait<1>();
-    __syncwarp();  // pos has landed
-    SeqState sq = seq_state<FUSED>(p, *pos_s);
-    if (FUSED && p.rope && !sq.bad) rope_pairs<D>(p, sq.pos, turns, lane, rope);
-    for (int i = 0; i < n_tiles; ++i) {
-      const int s = i % NST;
-      uint8_t* hdr = hdr0 + s * 32;
-      if (i >= NST) {
-        int ok = 0;
-        if (lane == 0) ok = mbar_wait(&empty_bar[s], static_cast<uint32_t>((i / NST - 1) & 1)) ? 1 : 0;
-        __syncwarp();
-        ok = __shfl_sync(0xffffffffu, ok, 0);
-        if (!ok) break;
-      }
-      const bool with_q = i == 0 || (p.cm == 0 && ci.j == 0);  // a unit's first tile in this CTA
-      if (with_q && i > 0) slot = slot == NST - 1 ? 0 : slot + 1;
-      uint8_t* aux = slot0 + slot * S::kSlot;
-      if (ci.b != run_b) {  // a new sequence: pos-derived state, once per run
-        if (FUSED && lane == 0) seq_run_done(p, run_b, run_tiles, sq);
-        run_b = ci.b;
-        run_tiles = 0;
-        sq = seq_state<FUSED>(p, pos_next);
-        if (FUSED && p.rope && !sq.bad) rope_pairs<D>(p, sq.pos, turns, lane, rope);
-        if (run_b < last_b) pos_next = ld_pos(p, run_b + 1);
-      }
-      ++run_tiles;
-      const bool t1 = ci.lt < p.t1_tiles;
-      const int r0 = tile_row(p, ci);
-      int n_rows, new_row = -1;
-      if (t1) {
-        n_rows = sq.bad ? 0 : min(p.k - r0, kQ8Tile);
-      } else {
-        n_rows = min(max(sq.count - r0, 0), kQ8Tile);
-        if (FUSED && sq.new_slot >= r0 && sq.new_slot - r0 < n_rows) new_row = sq.new_slot - r0;
-      }
-      // (a tile without keys is loaded only among the first stages, before pos is known)
-      const bool loaded = i < NST || n_rows > 0;
-      if (i >= NST && loaded) {
-        if (lane < 2) {
-          load_scales(p, ci, hdr, lane);
-          mbar_arrive_cp_async(&full_bar[s]);
-        }
-        if (lane == 0)
-          tma_box3_hint(smem_addr(smem + s * S::kStage), tile_map(p, maps, ci), r0, 2 * ci.u, &full_bar[s],
-                        policy_evict_first());
-      }
-      if (FUSED && p.rope && with_q) {
-        float2* tab = reinterpret_cast<float2*>(aux + S::kRope);
-        tab[lane] = rope[0];
-        if (lane + 32 < D / 2) tab[lane + 32] = rope[1];
-      }
-      __syncwarp();
-      if (lane == 0) {
-        if (sq.bad && ci.lt == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-        int* hw = reinterpret_cast<int*>(hdr);
-        hw[H_NROWS] = n_rows;
-        hw[H_NEWSLOT] = sq.new_slot;
-        hw[H_NEWROW] = new_row;
-        uint32_t tx = p.stall_tx;
-        if (loaded) tx += S::kStage;
-        if (with_q) tx += G * D * 2;
-        if (new_row >= 0) tx += 2 * D * 2;
-        mbar_arrive_expect_tx(&full_bar[s], tx);  // releases the header
-        if (with_q && i > 0)
-          bulk_copy(smem_addr(aux + S::kQ), p.q + static_cast<long long>(ci.u) * (G * D), G * D * 2,
-                    &full_bar[s]);
-        if (new_row >= 0) {
-          bulk_copy(smem_addr(aux + S::kNew), p.k_new + static_cast<long long>(ci.u) * D, D * 2, &full_bar[s]);
-          bulk_copy(smem_addr(aux + S::kNew + D * 2), p.v_new + static_cast<long long>(ci.u) * D, D * 2,
-                    &full_bar[s]);
+    if (lane == 31) s_sum[warp] = scan;
+    __syncthreads();
+    int before = scan - sum, all = 0;
+#pragma unroll
+    for (int v = 0; v < kWarps; ++v) {
+      if (v < warp) before += s_sum[v];
+      all += s_sum[v];
+    }
+    const unsigned total = static_cast<unsigned>(all) * static_cast<unsigned>(p.LH);
+    const unsigned nw = gridDim.x * kWarps;
+    const unsigned base = total / nw, rem = total - base * nw;
+    for (int v = 0; v < kWarps; ++v) {
+      const unsigned wid = blockIdx.x * kWarps + v;
+      const unsigned a = wid * base + min(wid, rem), n = base + (wid < rem ? 1u : 0u);
+      if (v == warp) n_run = static_cast<int>(n);
+      if (n == 0) continue;
+      // the thread in whose sequences the run begins, and the one in whose it ends
+      const unsigned lo = static_cast<unsigned>(before) * p.LH, hi = static_cast<unsigned>(before + sum) * p.LH;
+#pragma unroll 1
+      for (int e = 0; e < 2; ++e) {
+        const unsigned at = e ? a + n - 1 : a;
+        if (at < lo || at >= hi) continue;
+        unsigned from = lo;
+        for (int b = b0; b < b1; ++b) {
+          const long long pb = ld_pos(p, b);
+          const unsigned len = static_cast<unsigned>(live_blocks(p, seq_state<FUSED>(p, pb))) * p.LH;
+          if (at < from + len) {
+            if (e) {
+              s_last[v] = b;
+            } else {
+              s_first[v][0] = b;
+              s_first[v][1] = static_cast<int>(at - from);
+              s_pos[v] = pb;
+            }
+            break;
+          }
+          from += len;
         }
       }
-      ci.next(p);
-      issued = i + 1;
     }
-    if (FUSED && issued == n_tiles && lane == 0) seq_run_done(p, run_b, run_tiles, sq);
-    cp_async_wait<0>();
-    // No CTA exits while loads it issued may still be writing into its shared
-    // memory: the last stage's barrier covers them, and after a timeout, when
-    // barriers are no evidence, kDrainNs does (every load was issued before it).
-    if (lane == 0 && issued > 0 &&
-        (!mbar_wait(&full_bar[(issued - 1) % NST], static_cast<uint32_t>(((issued - 1) / NST) & 1)) ||
-         attn_aborted())) {
-      const uint32_t t0 = global_ns32();
-      for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
+    __syncthreads();
+    if (n_run > 0) {
+      w.b = s_first[warp][0];
+      last_b = s_last[warp];
+      w.sq = seq_state<FUSED>(p, s_pos[warp]);
+      w.nb = live_blocks(p, w.sq);
+      const int off = s_first[warp][1];
+      w.x = off / w.nb;
+      w.j = off - w.x * w.nb;
+      w.u = w.b * p.LH + w.x;
+      if (lane == 0) load_query<D, G, FUSED>(p, w.u, q_slot, new_slots, &q_bar[warp]);
+      if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
     }
-    if (lane == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
-    __syncwarp();
-    if (p.cm > 0) cluster_wait();  // every thread that arrived waits
-    return;
   }
-
-  // ======================= consumer warps =======================
-  // The boxes of the first stages, one warp each: they do not depend on pos.
-  if (lane == 0) {
-    TileCursor cl = c0;
-#pragma unroll
-    for (int i = 0; i < NST; ++i) {
-      if (i == warp && i < n_tiles)
-        tma_box3_hint(smem_addr(smem + i * S::kStage), tile_map(p, maps, cl), tile_row(p, cl), 2 * cl.u,
-                      &full_bar[i], policy_evict_first());
-      cl.next(p);
+  // Flat plan: the last warp to have read pos of all its sequences advances every pos.
+  auto count_reads = [&]() {
+    counted = true;
+    unsigned last = 0;
+    if (lane == 0) {
+      __threadfence();
+      const unsigned long long old = atomicAdd(p.tickets, 1ull);
+      last = old + 1 == static_cast<unsigned long long>(gridDim.x) * kWarps;
+      if (last) p.tickets[0] = 0ull;
     }
+    if (__shfl_sync(0xffffffffu, last, 0)) {
+      for (int b = lane; b < p.B; b += 32) {
+        const long long v = ld_pos(p, b);
+        if (v >= 0) p.pos[b] = v + 1;
+      }
+    }
+  };
+  // Requests the run's next block into stage s, with its header.
+  auto request = [&](int s) {
+    load_block<D>(p, maps, w.u, w.j, stages + s * S::kStage, hdrs + s * 32, &full[s], lane);
+    if (lane == 0)
+      write_header<FUSED>(p, hdrs + s * 32, w.u, w.j, cm > 0 ? 0 : w.nb,
+                          cm > 0 ? n_run - issued : min(w.nb - w.j, n_run - issued), w.sq);
+    ++issued;
+    if (cm > 0) {
+      w.j += step;
+      return;
+    }
+    if (++w.j == w.nb) {
+      w.j = 0;
+      ++w.u;
+      if (++w.x == p.LH && w.b < last_b) {
+        w.x = 0;
+        ++w.b;
+        w.sq = seq_state<FUSED>(p, pos_next);
+        w.nb = live_blocks(p, w.sq);
+        if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
+      }
+    }
+    if (FUSED && !counted && w.b == last_b) count_reads();
+  };
+  if (cm == 0) {
+    if (FUSED && (n_run == 0 || w.b == last_b)) count_reads();
+    while (issued < NST && issued < n_run) request(issued);
   }
   __syncwarp();
+
   // gq = lane / 4, tq = lane % 4.  A thread's two heads (columns 2 tq, 2 tq + 1 of the
   // products): h0 + e, e = 0, 1; for G <= 4 threads with tq >= 2 have the lo pieces.
   const int gq = lane >> 2;
   const int tq = lane & 3;
   const int h0 = PAIRED ? 2 * (tq & 1) : 2 * tq;
-  TileCursor cc = c0;
-  int cur_u = -1, first_j = 0, slot = -1;
+  int n_units = 0;                             // units begun
+  bool begun_first = false;                    // the present one with its first block
+  bool head = false, tail = false;             // flat plan: records written
+  long long rope_pos = -1;                     // position that the rotary table is for
   uint32_t qa[KS][2], qb[PAIRED ? 1 : KS][2];  // Q^T fragments: hi (or both pieces); G = 8: lo
   float qs[2] = {0.f, 0.f};                    // softmax scale * log2(e) * the heads' powers of two
   float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-  int e_cur = 0, e_top = 0;                    // the byte O is in units of; the largest so far
+  int e_cur = -1, e_top = -1;                  // the byte O is in units of; the largest so far
   float o[MT][4];
 #pragma unroll
   for (int j = 0; j < MT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -466,84 +530,99 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     qa[ks][0] = qa[ks][1] = 0u;
     if (!PAIRED) qb[ks][0] = qb[ks][1] = 0u;
   }
-  int release = lane;  // 0: this lane hands the warp's stages back
-
-  for (int i = 0; i < n_tiles; ++i) {
-    const int s = i % NST;
-    uint8_t* stage = smem + s * S::kStage;
-    uint8_t* hdr = hdr0 + s * 32;
-    // A stage whose wait gave up is skipped by every lane alike: no key, no patch.
-    const bool dead = __any_sync(0xffffffffu, !mbar_wait_stage(&full_bar[s], static_cast<uint32_t>((i / NST) & 1),
-                                                               reinterpret_cast<int*>(hdr), release));
-    const int4 hw = reinterpret_cast<const int4*>(hdr)[0];  // rows, slot, row
-    const int u = cc.u;
-    if (u != cur_u) slot = slot == NST - 1 ? 0 : slot + 1;
-    const uint8_t* aux = slot0 + slot * S::kSlot;
-    int kc = hdr[4 * H_KSCALES + warp], vc = hdr[4 * H_VSCALES + warp];
-    // bit r: row r of this warp's 32 holds a key
-    const int nk = dead ? 0 : min(max(hw.x - 32 * warp, 0), 32);
-    const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;
-    const int new_row = dead ? -1 : hw.z;
-    bool wrote_stage = false;  // generic-proxy writes into the stage by this warp
-
-    if (FUSED && new_row >= 0 && (new_row >> 5) == warp) {
-      const int r = new_row & 31;
-      const uint32_t others = mk & ~(1u << r);
-      const bool first = (hw.y & 31) == 0;
-      // ring rows of the block: slot hw.y is row r
+  // Sums the warp's l over its lanes and leaves O in true units in `ow`: 8 columns of D
+  // floats, columns of odd pairs shifted so that the stores hit distinct banks.
+  auto leave = [&](float* ow) {
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const uint16_t* row = reinterpret_cast<const uint16_t*>(aux + S::kNew + w * D * 2);
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-        constexpr int E = D / 32;
+    for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = bf16lo_to_f32(row[E * lane + e]);
-        if (w == 0 && p.rope) {  // elements c pair with c + d/2
-          const float2* tab = reinterpret_cast<const float2*>(aux + S::kRope);
-          const float sg = lane < 16 ? -1.f : 1.f;
+      for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
+        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
+    __syncwarp();  // the warp is done with the stage
+    const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float2 cs = tab[(E * lane + e) & (D / 2 - 1)];
-            x[e] = fmaf(x[e], cs.x, sg * bf16lo_to_f32(row[(E * lane + e) ^ (D / 2)]) * cs.y);
-          }
-        }
-        const long long uw = 2LL * u + w;
-        uint8_t* ring0 = p.ring_kv + (uw * p.W + hw.y - r) * D;
-        const int c = patch_block<D>(stage + w * S::kV, ring0, p.ring_scales + uw * p.ringS + (hw.y >> 5), x, r,
-                                     w ? vc : kc, first, others, lane, warp);
-        if (w) vc = c;
-        else kc = c;
+    for (int e = 0; e < 2; ++e) {
+      float* col = ow + (2 * tq + e) * D;
+#pragma unroll
+      for (int j = 0; j < MT; ++j) {
+        col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
+        col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
       }
-      __syncwarp();
-      wrote_stage = true;
     }
+  };
+  // Rows c .. c + 3 of head hh from what leave() wrote.
+  auto taken = [&](const float* ow, int hh, int c) {
+    float4 y = *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
+    if (PAIRED) {
+      const float4 z = *reinterpret_cast<const float4*>(ow + (hh + 4) * D + (c ^ (8 * ((hh + 4) >> 1))));
+      y.x = fmaf(z.x, 0.0625f, y.x); y.y = fmaf(z.y, 0.0625f, y.y);
+      y.z = fmaf(z.z, 0.0625f, y.z); y.w = fmaf(z.w, 0.0625f, y.w);
+    }
+    return y;
+  };
 
-    if (u != cur_u) {  // first tile of a unit in this CTA
-      cur_u = u;
-      first_j = cc.j;
+  bool gave_up = false;
+  int s = 0;             // stage
+  uint32_t phase = 0;    // its parity
+  for (int i = 0; i < n_run; ++i) {
+    uint8_t* stage = stages + s * S::kStage;
+    const uint8_t* hdr = hdrs + s * 32;
+    if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {
+      gave_up = true;
+      break;
+    }
+    const int4 hw = *reinterpret_cast<const int4*>(hdr);
+    const int nk = hw.x & 255, new_row = (hw.x >> 8) & 255, sel = (hw.x >> 16) & 255, flags = hw.x >> 24;
+    const int u = hw.y;
+    int kc = hdr[4 * Q_KS + sel], vc = hdr[4 * Q_VS + sel];
+    const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;  // bit r: row r holds a key
+    const bool starts = cm > 0 ? i == 0 : (i == 0 || (flags & QF_FIRST));
+    const bool ends = hw.w == 1;  // the unit's last block in this run
+    bool wrote_stage = false;     // generic-proxy writes into the stage
+
+    if (starts) {
+      if (__any_sync(0xffffffffu, !mbar_wait(&q_bar[warp], static_cast<uint32_t>(n_units & 1)))) {
+        gave_up = true;
+        break;
+      }
+      begun_first = flags & QF_FIRST;
+      if (FUSED && p.rope) {
+        const long long pos = *reinterpret_cast<const long long*>(hdr + 4 * Q_POS);
+        if (pos >= 0 && pos != rope_pos) {
+          rope_pos = pos;
+          float2 cs[2];
+          rope_pairs<D>(p, pos, turns, lane, cs);
+          rope_tab[lane] = cs[0];
+          if (lane + 32 < D / 2) rope_tab[lane + 32] = cs[1];
+          __syncwarp();
+        }
+      }
       // The query as two e4m3 pieces.  Thread: head (column) gq, of the elements
       // 32 ks + 16 hf + 4 tq .. + 3; those and the other three tq's are the head.
-      const int head = PAIRED ? (gq & 3) : gq;
-      const uint8_t* qrow = aux + S::kQ + head * D * 2;
+      const int hq = PAIRED ? (gq & 3) : gq;
+      const uint8_t* qrow = q_slot + hq * D * 2;
       float x[KS][2][4];
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
         for (int hf = 0; hf < 2; ++hf) {
-          uint2 w = make_uint2(0u, 0u);
-          if (head < G && !dead) w = *reinterpret_cast<const uint2*>(qrow + (32 * ks + 16 * hf + 4 * tq) * 2);
-          x[ks][hf][0] = bf16lo_to_f32(w.x); x[ks][hf][1] = bf16hi_to_f32(w.x);
-          x[ks][hf][2] = bf16lo_to_f32(w.y); x[ks][hf][3] = bf16hi_to_f32(w.y);
+          uint2 v = make_uint2(0u, 0u);
+          if (hq < G) v = *reinterpret_cast<const uint2*>(qrow + (32 * ks + 16 * hf + 4 * tq) * 2);
+          x[ks][hf][0] = bf16lo_to_f32(v.x); x[ks][hf][1] = bf16hi_to_f32(v.x);
+          x[ks][hf][2] = bf16lo_to_f32(v.y); x[ks][hf][3] = bf16hi_to_f32(v.y);
         }
-      if (FUSED && p.rope && !dead) {  // k-steps ks and ks + KS/2 hold the partners
-        const float2* tab = reinterpret_cast<const float2*>(aux + S::kRope);
+      __syncwarp();  // the query slot is free
+      // the next unit's rows, which follow where the run goes on behind this unit
+      if (cm == 0 && lane == 0 && i + hw.w < n_run)
+        load_query<D, G, FUSED>(p, u + 1, q_slot, new_slots + ((n_units + 1) & 1) * (2 * D * 2), &q_bar[warp]);
+      if (FUSED && p.rope) {  // k-steps ks and ks + KS/2 hold the partners
 #pragma unroll
         for (int ks = 0; ks < KS / 2; ++ks)
 #pragma unroll
           for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float2 cs = tab[32 * ks + 16 * hf + 4 * tq + e];
+              const float2 cs = rope_tab[32 * ks + 16 * hf + 4 * tq + e];
               const float a = x[ks][hf][e], b = x[ks + KS / 2][hf][e];
               x[ks][hf][e] = fmaf(a, cs.x, -b * cs.y);
               x[ks + KS / 2][hf][e] = fmaf(b, cs.x, a * cs.y);
@@ -589,6 +668,37 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       e_cur = e_top = -1;
 #pragma unroll
       for (int j = 0; j < MT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+      ++n_units;
+    }
+
+    if (FUSED && new_row != 255) {
+      const uint32_t others = mk & ~(1u << new_row);
+      const bool first = (hw.z & 31) == 0;
+      const uint16_t* rows = reinterpret_cast<const uint16_t*>(new_slots + ((n_units - 1) & 1) * (2 * D * 2));
+      constexpr int E = D / 32;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const uint16_t* row = rows + v * D;
+        float x[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = bf16lo_to_f32(row[E * lane + e]);
+        if (v == 0 && p.rope) {  // elements c pair with c + d/2
+          const float sg = lane < 16 ? -1.f : 1.f;
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float2 cs = rope_tab[(E * lane + e) & (D / 2 - 1)];
+            x[e] = fmaf(x[e], cs.x, sg * bf16lo_to_f32(row[(E * lane + e) ^ (D / 2)]) * cs.y);
+          }
+        }
+        const long long uv = 2LL * u + v;
+        uint8_t* ring0 = p.ring_kv + (uv * p.W + hw.z - new_row) * D;
+        const int c = patch_block<D>(stage + v * S::kV, ring0, p.ring_scales + uv * p.ringS + (hw.z >> 5), x,
+                                     new_row, v ? vc : kc, first, others, lane);
+        if (v) vc = c;
+        else kc = c;
+      }
+      __syncwarp();
+      wrote_stage = true;
     }
 
     if (mk != 0u) {
@@ -597,7 +707,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         if (!((mk >> lane) & 1u)) {
 #pragma unroll
           for (int q = 0; q < D / 16; ++q)
-            *reinterpret_cast<uint4*>(stage + S::kV + swz8<D>(32 * warp + lane, q)) = make_uint4(0u, 0u, 0u, 0u);
+            *reinterpret_cast<uint4*>(stage + S::kV + swz8<D>(lane, q)) = make_uint4(0u, 0u, 0u, 0u);
         }
         __syncwarp();
         wrote_stage = true;
@@ -610,7 +720,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       for (int t = 0; t < 2; ++t) {
         // lanes 0-7 / 8-15 / 16-23 / 24-31: rows 0-7 / 8-15 / 0-7 / 8-15 of the product, at
         // bytes 32 ks .. + 15 / same / 32 ks + 16 .. + 31 / same
-        const int key = 32 * warp + 16 * t + ((lane & 7) ^ (4 * t)) + ((lane >> 3) & 1) * 8;
+        const int key = 16 * t + ((lane & 7) ^ (4 * t)) + ((lane >> 3) & 1) * 8;
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) {
           uint32_t a0, a1, a2, a3;
@@ -732,7 +842,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       // ---- O^T += V^T P^T: lane's V row is k = lane of the product ----
       {
         const int row = 2 * ((lane & 15) >> 2) + ((lane >> 1) & 1) + 8 * (lane >> 4);
-        const int key = 32 * warp + ((lane & 1) ? 16 + (row ^ 4) : row);
+        const int key = ((lane & 1) ? 16 + (row ^ 4) : row);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           uint32_t a0, a1, a2, a3;
@@ -748,178 +858,254 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       }
     }
 
-    // ---- end of a unit within this CTA: merge warps, write out or a partial ----
-    const bool unit_end = (i + 1 == n_tiles) || (p.cm == 0 && cc.j == p.tpu - 1);
-    if (unit_end) {
-      // Every warp leaves its maximum and sum, and its unnormalised output in its own 32
-      // rows of the stage's K (8 columns of d floats: just their size), columns of odd
-      // pairs shifted so that the stores hit distinct banks.  After a barrier each
-      // thread takes four rows of the head dimension of one head, rescales and adds
-      // the warps' in warp order.
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
-          l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
-      __syncwarp();  // the warp is done with its K rows
-      {
-        float* ow = reinterpret_cast<float*>(stage) + warp * 8 * D;
-        const float fo = e_cur < 0 ? 0.f : e8m0_to_f32(e_cur);
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float* col = ow + (2 * tq + e) * D;
-#pragma unroll
-          for (int j = 0; j < MT; ++j) {
-            col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
-            col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
-          }
-          if (gq == 0 && (!PAIRED || tq < 2)) {
-            merge_m[warp * 8 + h0 + e] = m_run[e];
-            merge_l[warp * 8 + h0 + e] = l_run[e];
-          }
-        }
-      }
-      wrote_stage = true;
-      consumer_sync();
 
-      const bool whole = p.cm == 0 && first_j == 0 && cc.j == p.tpu - 1;
-      const long long out_base = static_cast<long long>(u) * (G * D);
-      constexpr int NGR = G * D / 4;                        // 4-row groups of the unit's output
-      constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
-      const bool clus = !whole && p.cm > 0;
-      float4 cacc[XPT];
-      float cls[XPT], cmx[XPT];
+    if (ends && cm == 0) {
+      // The unit's share of this run is done: written out where it is the whole unit, else left
+      // as a record (the first of the run's if the unit began before it).
+      float* ow = reinterpret_cast<float*>(stage);  // K's part: just the size
+      leave(ow);
+      __syncwarp();
+      wrote_stage = true;
+      const bool whole = begun_first && (flags & QF_LAST);
+      float* rec = nullptr;
+      if (!whole) {
+        const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
+        rec = p.partials + (2 * wid + (begun_first ? 1 : 0)) * (kQ8RecHead + rec_floats(G, D));
+        if (lane == 0) *reinterpret_cast<int2*>(rec) = make_int2(1, flags & QF_LAST ? 1 : 0);
+        if (begun_first) tail = true;
+        else head = true;
+        rec += kQ8RecHead;
+      }
 #pragma unroll
-      for (int xi = 0; xi < XPT; ++xi) {
-        const int x = tid + xi * kThreads;
-        if (x >= NGR) break;
-        const int hh = (4 * x) / D;
+      for (int xi = 0; xi < (NGR + 31) / 32; ++xi) {
+        const int x = lane + 32 * xi;
+        const int hh = x < NGR ? (4 * x) / D : 0;
         const int c = (4 * x) % D;
-        float M = merge_m[hh];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) M = fmaxf(M, merge_m[w * 8 + hh]);
-        const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
-        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-        float Ls = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float f = ex2(merge_m[w * 8 + hh] - Mr);
-          const float* ow = reinterpret_cast<const float*>(stage) + w * 8 * D;
-          float4 y = *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
-          if (PAIRED) {
-            const int hl = hh + 4;
-            const float4 z = *reinterpret_cast<const float4*>(ow + hl * D + (c ^ (8 * (hl >> 1))));
-            y.x = fmaf(z.x, 0.0625f, y.x); y.y = fmaf(z.y, 0.0625f, y.y);
-            y.z = fmaf(z.z, 0.0625f, y.z); y.w = fmaf(z.w, 0.0625f, y.w);
-          }
-          acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
-          acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-          Ls = fmaf(f, merge_l[w * 8 + hh], Ls);
-        }
-        if (whole) {
-          const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
-          *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-              make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
-        } else if (clus) {  // merged across the cluster below
-          cacc[xi] = acc;
-          cls[xi] = Ls;
-          cmx[xi] = M;
-        } else {  // merged by two_tier_combine_kernel
-          constexpr int PW = rec_floats(G, D);
-          float* rec = p.partials + (static_cast<long long>(u) * p.tpu + first_j) * PW;
-          if (c == 0) {
-            rec[hh] = M;
-            rec[G + hh] = Ls;
-          }
-          *reinterpret_cast<float4*>(rec + rec_out_offset(G) + hh * D + c) = acc;
-        }
-      }
-      if (clus) {
-        // One share of the unit per CTA: stored into the peers' receive areas, to each the
-        // groups that peer finishes; then merged in rank order (see cmc_attn.cu).
-        const int cm = p.cm;
-        const int rank = static_cast<int>(cluster_ctarank());
-        const int SL = p.slice;
-        const uint32_t recv_a = smem_addr(smem + S::kRecv), ml_a = smem_addr(smem + S::kRecvMl);
-        const uint32_t bar_a = smem_addr(&recv_bar);
-        cluster_wait();
-#pragma unroll
-        for (int xi = 0; xi < XPT; ++xi) {
-          const int x = tid + xi * kThreads;
-          if (x >= NGR) break;
-          const int hh = (4 * x) / D;
-          const int to = x / SL;
-          st_peer_f4(peer_smem(recv_a + (rank * SL + x - to * SL) * 16, to), cacc[xi], peer_smem(bar_a, to));
-          if ((4 * x) % D == 0) {
-            for (int r = 0; r < cm; ++r)
-              st_peer_f2(peer_smem(ml_a + (rank * G + hh) * 8, r), cmx[xi], cls[xi], peer_smem(bar_a, r));
-          }
-        }
-        mbar_wait_peers(&recv_bar);
-        const int x0 = rank * SL, x1 = min(x0 + SL, NGR);
-        for (int x = x0 + tid; x < x1; x += kThreads) {
-          const int hh = (4 * x) / D;
-          const int c = (4 * x) % D;
-          const float2* ml = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
-          float M = -INFINITY;
-#pragma unroll
-          for (int r = 0; r < kMaxClusterCtas; ++r)
-            if (r < cm) M = fmaxf(M, ml[r * G].x);
-          if (M == -INFINITY) M = 0.f;
-          float Ls = 0.f;
-          float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-          for (int r = 0; r < kMaxClusterCtas; ++r) {
-            if (r < cm) {
-              const float2 mr = ml[r * G];
-              const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
-              const float f = ex2(mr.x - M);
-              Ls = fmaf(f, mr.y, Ls);
-              O.x = fmaf(f, o4.x, O.x);
-              O.y = fmaf(f, o4.y, O.y);
-              O.z = fmaf(f, o4.z, O.z);
-              O.w = fmaf(f, o4.w, O.w);
+        const float l0 = __shfl_sync(0xffffffffu, l_run[0], hh >> 1), l1 = __shfl_sync(0xffffffffu, l_run[1], hh >> 1);
+        const float m0 = __shfl_sync(0xffffffffu, m_run[0], hh >> 1), m1 = __shfl_sync(0xffffffffu, m_run[1], hh >> 1);
+        const float l = hh & 1 ? l1 : l0, m = hh & 1 ? m1 : m0;
+        if (x < NGR) {
+          const float4 y = taken(ow, hh, c);
+          if (whole) {
+            const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
+            *reinterpret_cast<uint2*>(p.out + static_cast<long long>(u) * (G * D) + hh * D + c) =
+                make_uint2(pack_bf16_rn(y.x * inv, y.y * inv), pack_bf16_rn(y.z * inv, y.w * inv));
+          } else {
+            if (c == 0) {
+              rec[hh] = m;
+              rec[G + hh] = l;
             }
+            *reinterpret_cast<float4*>(rec + rec_out_offset(G) + hh * D + c) = y;
           }
-          const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
-          *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-              make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
         }
       }
-      if (i + 1 < n_tiles) consumer_sync();  // merge_m and merge_l are written again by the next unit
+      if (!whole && lane == 0 && begun_first)  // which unit it is
+        reinterpret_cast<int*>(rec - kQ8RecHead)[2] = u;
     }
     if (wrote_stage) {
-      // generic-proxy writes to this stage are ordered before the producer's next box
+      // generic-proxy writes to this stage are ordered before the next box into it
       asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
     }
     __syncwarp();
-    if (release == 0) mbar_arrive(&empty_bar[s]);  // this warp is done with stage s
-    cc.next(p);
+    if (issued < n_run) request(s);
+    if (++s == NST) {
+      s = 0;
+      phase ^= 1u;
+    }
+  }
+  if (gave_up) {
+    // Loads of this warp may still be on their way into its shared memory, and its barriers are no
+    // evidence: kDrainNs covers them (no load was requested since the flag went up).
+    cp_async_wait<0>();
+    const uint32_t t0 = global_ns32();
+    for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
+    if (lane == 0) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
+  }
+  if (cm == 0) {
+    if (FUSED && !counted) count_reads();  // (after a timeout)
+    // the merge kernel reads both records' first words
+    if (lane == 0) {
+      const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
+      float* rec = p.partials + 2 * wid * (kQ8RecHead + rec_floats(G, D));
+      if (!head) *reinterpret_cast<int*>(rec) = 0;
+      if (!tail) *reinterpret_cast<int*>(rec + kQ8RecHead + rec_floats(G, D)) = 0;
+    }
+    return;
+  }
+
+  // ---- strided plan: the four warps' states, then the cluster's CTAs' ----
+  // Every warp leaves its output in its first stage; after a barrier each thread takes four
+  // rows of the head dimension of one head, rescales and adds the warps' in warp order.
+  {
+    leave(reinterpret_cast<float*>(stages));
+    if (gq == 0 && (!PAIRED || tq < 2)) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        merge_m[warp * 8 + h0 + e] = m_run[e];
+        merge_l[warp * 8 + h0 + e] = l_run[e];
+      }
+    }
+  }
+  __syncthreads();
+  const float* all_o = reinterpret_cast<const float*>(stages - warp * (NST * S::kStage));
+  const long long out_base = static_cast<long long>(su) * (G * D);
+  constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
+  float4 cacc[XPT];
+  float cls[XPT], cmx[XPT];
+#pragma unroll
+  for (int xi = 0; xi < XPT; ++xi) {
+    const int x = tid + xi * kThreads;
+    if (x >= NGR) break;
+    const int hh = (4 * x) / D;
+    const int c = (4 * x) % D;
+    float M = merge_m[hh];
+#pragma unroll
+    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, merge_m[v * 8 + hh]);
+    const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    float Ls = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWarps; ++v) {
+      const float f = ex2(merge_m[v * 8 + hh] - Mr);
+      const float4 y = taken(all_o + v * (NST * S::kStage / 4), hh, c);
+      acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
+      acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
+      Ls = fmaf(f, merge_l[v * 8 + hh], Ls);
+    }
+    if (cm == 1) {
+      const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
+      *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
+          make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
+    } else {
+      cacc[xi] = acc;
+      cls[xi] = Ls;
+      cmx[xi] = M;
+    }
+  }
+  if (cm == 1) return;
+  // One share of the unit per CTA: stored into the peers' receive areas, to each the groups that
+  // peer finishes; then merged in rank order.
+  const int SL = p.slice;
+  const uint32_t recv_a = smem_addr(smem + S::kRecv), ml_a = smem_addr(smem + S::kRecvMl);
+  const uint32_t bar_a = smem_addr(&recv_bar);
+  cluster_wait();
+#pragma unroll
+  for (int xi = 0; xi < XPT; ++xi) {
+    const int x = tid + xi * kThreads;
+    if (x >= NGR) break;
+    const int hh = (4 * x) / D;
+    const int to = x / SL;
+    st_peer_f4(peer_smem(recv_a + (rank * SL + x - to * SL) * 16, to), cacc[xi], peer_smem(bar_a, to));
+    if ((4 * x) % D == 0) {
+      for (int r = 0; r < cm; ++r)
+        st_peer_f2(peer_smem(ml_a + (rank * G + hh) * 8, r), cmx[xi], cls[xi], peer_smem(bar_a, r));
+    }
+  }
+  mbar_wait_peers(&recv_bar);
+  const int x0 = rank * SL, x1 = min(x0 + SL, NGR);
+  for (int x = x0 + tid; x < x1; x += kThreads) {
+    const int hh = (4 * x) / D;
+    const int c = (4 * x) % D;
+    const float2* ml = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
+    float M = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < kMaxClusterCtas; ++r)
+      if (r < cm) M = fmaxf(M, ml[r * G].x);
+    if (M == -INFINITY) M = 0.f;
+    float Ls = 0.f;
+    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int r = 0; r < kMaxClusterCtas; ++r) {
+      if (r < cm) {
+        const float2 mr = ml[r * G];
+        const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
+        const float f = ex2(mr.x - M);
+        Ls = fmaf(f, mr.y, Ls);
+        O.x = fmaf(f, o4.x, O.x);
+        O.y = fmaf(f, o4.y, O.y);
+        O.z = fmaf(f, o4.z, O.z);
+        O.w = fmaf(f, o4.w, O.w);
+      }
+    }
+    const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
+    *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
+        make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
   }
   if (tid == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
+}
+
+// Merges the units that the flat plan cut.  One CTA for each warp of the attention grid: where
+// that warp's run ended inside a unit that began in it, its record and the first
+// records of the warps behind it, up to the one where the unit ends.
+template <int D, int G>
+__global__ void __launch_bounds__(kThreads)
+attn_q8_merge_kernel(const float* __restrict__ recs, uint16_t* __restrict__ out) {
+  constexpr int PW = kQ8RecHead + rec_floats(G, D);
+  pdl_wait();  // the attention kernel's records
+  pdl_trigger();
+  const long long w = blockIdx.x;
+  const float* own = recs + (2 * w + 1) * PW;
+  const int4 h = *reinterpret_cast<const int4*>(own);
+  if (h.x == 0) return;
+  for (int x = threadIdx.x; x < G * D / 4; x += kThreads) {
+    const int hh = (4 * x) / D;
+    const int c = (4 * x) % D;
+    float M = own[kQ8RecHead + hh], L = own[kQ8RecHead + G + hh];
+    float4 O = *reinterpret_cast<const float4*>(own + kQ8RecHead + rec_out_offset(G) + hh * D + c);
+    // (the last warp's run ends with the last unit's last block, so the chain ends inside the grid)
+    for (long long r = w + 1; r < gridDim.x; ++r) {
+      const float* rec = recs + 2 * r * PW;
+      const int2 rh = *reinterpret_cast<const int2*>(rec);
+      if (rh.x == 0) break;  // (after a timeout)
+      const float m = rec[kQ8RecHead + hh];
+      const float4 y = *reinterpret_cast<const float4*>(rec + kQ8RecHead + rec_out_offset(G) + hh * D + c);
+      const float mn = fmaxf(M, m), ref = mn == -INFINITY ? 0.f : mn;
+      const float fa = ex2(M - ref), fb = ex2(m - ref);
+      M = mn;
+      L = fmaf(fb, rec[kQ8RecHead + G + hh], L * fa);
+      O.x = fmaf(fb, y.x, O.x * fa); O.y = fmaf(fb, y.y, O.y * fa);
+      O.z = fmaf(fb, y.z, O.z * fa); O.w = fmaf(fb, y.w, O.w * fa);
+      if (rh.y) break;
+    }
+    const float inv = L > 0.f ? __fdividef(1.f, L) : 0.f;
+    *reinterpret_cast<uint2*>(out + static_cast<long long>(h.z) * (G * D) + hh * D + c) =
+        make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
+  }
 }
 
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
 
-// rows of T codes rows of every (unit, K or V), `stride` rows apart.
+// T rows of codes of every (unit, K or V), `stride` rows apart.
 static bool encode_q8(CUtensorMap* map, const void* base, long long units2, int T, int stride, int d) {
   EncodeTiledFn enc = encode_fn();
   if (!enc) return false;
   cuuint64_t dims[3] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(T), static_cast<cuuint64_t>(units2)};
   cuuint64_t strides[2] = {static_cast<cuuint64_t>(d), static_cast<cuuint64_t>(stride) * d};
-  cuuint32_t box[3] = {static_cast<cuuint32_t>(d), kQ8Tile, 2};
+  cuuint32_t box[3] = {static_cast<cuuint32_t>(d), kQ8Block, 2};
   cuuint32_t es[3] = {1, 1, 1};
   return enc(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void*>(base), dims, strides, box, es,
              CU_TENSOR_MAP_INTERLEAVE_NONE, d == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-static int q8_tiles(int rows) { return (rows + kQ8Tile - 1) / kQ8Tile; }
+static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
+
+static size_t q8_workspace_size(const cmc_dims& m) {
+  const int G = m.Hq / m.Hkv;
+  const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
+  const size_t recs = units > kQ8StridedUnits ? 2 * kWarps * kQ8MaxCtas : 0;
+  return ws_partials_off(m.B) + recs * (kQ8RecHead + rec_floats(G, m.d)) * sizeof(float);
+}
+
+struct Q8Plan {
+  int ctas;  // grid size
+  int cm;    // strided plan: CTAs per unit; 0: flat plan
+};
 
 template <int D, int G, bool FUSED>
-static int plan_q8(long long tiles, int tpu, AttnPlan* pl) {
+static int plan_q8(long long units, int nb, Q8Plan* pl) {
   constexpr int smem = Q8Smem<D, G>::kBytes;
   auto kern = attn_q8_kernel<D, G, FUSED>;
   static std::atomic<int> configured[64];  // per device: attribute set and occupancy known (idempotent)
@@ -930,43 +1116,53 @@ static int plan_q8(long long tiles, int tpu, AttnPlan* pl) {
   if (per_sm <= 0) {
     st = record_cuda_error(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     if (st != CMC_OK) return st;
-    st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, kThreads + 32, smem));
+    st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, kThreads, smem));
     if (st != CMC_OK) return st;
     if (per_sm < 1) per_sm = 1;
     if (dev >= 0 && dev < 64) configured[dev].store(per_sm, std::memory_order_release);
   }
-  plan_grid(tiles, tpu, per_sm, pl);
+  long long slots = static_cast<long long>(per_sm) * sm_count();
+  if (slots > kQ8MaxCtas) slots = kQ8MaxCtas;
+  if (units <= slots || units <= kQ8StridedUnits) {
+    long long m = slots / units;
+    const long long most = (nb + kWarps - 1) / kWarps;  // a block for every warp
+    if (m > most) m = most;
+    if (m > kMaxClusterCtas) m = kMaxClusterCtas;
+    if (m < 1) m = 1;
+    pl->cm = static_cast<int>(m);
+    pl->ctas = static_cast<int>(units * m);
+  } else {
+    pl->cm = 0;
+    pl->ctas = static_cast<int>(slots);
+  }
   return CMC_OK;
 }
 
 template <int D, int G, bool FUSED>
-static int launch_q8(const Q8Maps& maps, AttnQ8Params p, long long tiles, cudaStream_t s) {
-  AttnPlan pl;
-  int st = plan_q8<D, G, FUSED>(tiles, p.tpu, &pl);
+static int launch_q8(const Q8Maps& maps, AttnQ8Params p, long long units, cudaStream_t s) {
+  Q8Plan pl;
+  int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
   if (st != CMC_OK) return st;
-  p.base = static_cast<int>(pl.base);
-  p.rem = static_cast<int>(pl.rem);
   p.cm = pl.cm;
-  p.gran = pl.gran;
-  p.slice = pl.cm > 0 ? (G * D / 4 + pl.cm - 1) / pl.cm : 0;
+  p.slice = pl.cm > 1 ? (G * D / 4 + pl.cm - 1) / pl.cm : 0;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(pl.cm > 0 ? pl.cm : 1);
+  attr[1].val.clusterDim.x = static_cast<unsigned>(pl.cm > 1 ? pl.cm : 1);
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(pl.ctas));
-  cfg.blockDim = dim3(kThreads + 32);
+  cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = Q8Smem<D, G>::kBytes;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = pl.cm > 0 ? 2 : 1;
+  cfg.numAttrs = pl.cm > 1 ? 2 : 1;
   st = record_cuda_error(cudaLaunchKernelEx(&cfg, attn_q8_kernel<D, G, FUSED>, maps, p));
-  if (st != CMC_OK || !pl.split) return st;
-  return launch_pdl(two_tier_combine_kernel<D, G>, dim3(static_cast<unsigned>(tiles / p.tpu)), dim3(kThreads),
-                    0, s, static_cast<const AttnParams&>(p));
+  if (st != CMC_OK || pl.cm > 0) return st;
+  return launch_pdl(attn_q8_merge_kernel<D, G>, dim3(static_cast<unsigned>(pl.ctas * kWarps)), dim3(kThreads), 0, s,
+                    static_cast<const float*>(p.partials), p.out);
 }
 
 // Calls F<D, G>::run(args...) for the call's head dimension and group size.
@@ -989,14 +1185,14 @@ static int by_shape(int d, int G, Args&&... args) {
 }
 template <int D, int G>
 struct PlanQ8 {
-  static int run(bool fused, long long tiles, int tpu, AttnPlan* pl) {
-    return fused ? plan_q8<D, G, true>(tiles, tpu, pl) : plan_q8<D, G, false>(tiles, tpu, pl);
+  static int run(bool fused, long long units, int nb, Q8Plan* pl) {
+    return fused ? plan_q8<D, G, true>(units, nb, pl) : plan_q8<D, G, false>(units, nb, pl);
   }
 };
 template <int D, int G>
 struct LaunchQ8 {
-  static int run(bool fused, const Q8Maps& maps, const AttnQ8Params& p, long long tiles, cudaStream_t s) {
-    return fused ? launch_q8<D, G, true>(maps, p, tiles, s) : launch_q8<D, G, false>(maps, p, tiles, s);
+  static int run(bool fused, const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
+    return fused ? launch_q8<D, G, true>(maps, p, units, s) : launch_q8<D, G, false>(maps, p, units, s);
   }
 };
 
@@ -1018,14 +1214,12 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
     return CMC_ERR_ALIGN;
   if (m.k > 0 && (!aligned16(t1_kv) || !aligned16(t1_scales))) return CMC_ERR_ALIGN;
   if (fused && (!aligned16(k_new) || !aligned16(v_new))) return CMC_ERR_ALIGN;
-  if (!workspace || workspace_bytes < cmc_decode_attn_workspace_size(dims)) return CMC_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < q8_workspace_size(m)) return CMC_ERR_WORKSPACE;
   if (!aligned16(workspace)) return CMC_ERR_ALIGN;
 
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  const int t1_tiles = q8_tiles(m.k);
-  const int tpu = t1_tiles + q8_tiles(m.W);
-  const long long tiles = units * tpu;
-  if (tiles >= (1LL << 31)) return CMC_ERR_SHAPE;
+  const int nb1 = q8_blocks(m.k), nb2 = q8_blocks(m.W);
+  if (units * (nb1 + nb2) >= (1LL << 31)) return CMC_ERR_SHAPE;  // blocks are counted in 32 bits
 
   Q8Maps maps;
   memset(&maps, 0, sizeof(maps));
@@ -1043,9 +1237,9 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
   p.tickets = reinterpret_cast<unsigned long long*>(ws + kWsHeader);
   p.partials = reinterpret_cast<float*>(ws + ws_partials_off(m.B));
   p.B = m.B; p.L = m.L; p.Hq = m.Hq; p.Hkv = m.Hkv; p.N = m.N; p.k = m.k; p.W = m.W;
-  p.tpu = tpu;
   p.LH = m.L * m.Hkv;
-  p.t1_tiles = t1_tiles;
+  p.nb1 = nb1;
+  p.nb2 = nb2;
   const float sc = scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(m.d));
   p.scale_log2 = sc * 1.4426950408889634f;
   p.l2_prefetch = l2_prefetch_setting();
@@ -1063,12 +1257,16 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
     rope_turns_table(rope_theta, m.d, p.rope_turns);
     p.rope_slot = rope_slot(rope_theta, m.d, p.rope_turns, s);
   }
-  return by_shape<LaunchQ8>(m.d, m.Hq / m.Hkv, fused, maps, p, tiles, s);
+  return by_shape<LaunchQ8>(m.d, m.Hq / m.Hkv, fused, maps, p, units, s);
 }
 
 }  // namespace cmc
 
 extern "C" {
+
+size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims) {
+  return cmc::validate_dims(dims, true) == CMC_OK ? cmc::q8_workspace_size(*dims) : 0;
+}
 
 int cmc_two_tier_decode_attn_q8(const void* q, const void* tier1_kv, const void* tier1_scales,
                                 const void* ring_kv, const void* ring_scales, const int64_t* pos,
@@ -1093,14 +1291,14 @@ int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas, int* lau
   if (st != CMC_OK) return st;
   if (!ctas || !launches) return CMC_ERR_NULL;
   const cmc_dims& m = *dims;
-  const int tpu = q8_tiles(m.k) + q8_tiles(m.W);
-  const long long tiles = static_cast<long long>(m.B) * m.L * m.Hkv * tpu;
-  if (tiles >= (1LL << 31)) return CMC_ERR_SHAPE;
-  AttnPlan pl;
-  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, tiles, tpu, &pl);
+  const int nb = q8_blocks(m.k) + q8_blocks(m.W);
+  const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
+  if (units * nb >= (1LL << 31)) return CMC_ERR_SHAPE;
+  Q8Plan pl;
+  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, nb, &pl);
   if (st != CMC_OK) return st;
-  *ctas = static_cast<int>(pl.ctas);
-  *launches = pl.split ? 2 : 1;
+  *ctas = pl.ctas;
+  *launches = pl.cm > 0 ? 1 : 2;
   return CMC_OK;
 }
 

@@ -284,6 +284,15 @@ ATTN = [  # B, L, Hq, Hkv, d, k, W, pos
 ]
 
 
+ATTN += [  # more units than resident CTAs: whole ones, cut ones, runs over many sequences
+    (200, 1, 8, 4, 128, 30, 130, [(7 * i) % 150 for i in range(200)]),
+    (20, 16, 8, 2, 64, 0, 40, [3 * i - 5 for i in range(20)]),
+    (700, 1, 1, 1, 64, 0, 33, [(i * 37) % 60 - 3 for i in range(700)]),
+    (45, 1, 64, 8, 128, 70, 500, [(i * 131) % 700 for i in range(45)]),
+    (170, 1, 8, 1, 64, 3, 300, [(i * 17) % 400 for i in range(170)]),
+]
+
+
 def problem(rng, B, L, Hq, H, d, k, W, pos):
     pos = np.array(pos, dtype=np.int64)
     ring = cache(rng, B, L, H, W, d, np.arange(W)[None] < pos[:, None])
@@ -314,7 +323,7 @@ def test_attention_empty_and_negative(cuda_device):
     rng = np.random.default_rng(3)
     q, t1, ring, pos = problem(rng, 3, 1, 4, 2, 64, 0, 40, [0, -7, 4])
     args = device_args(q, t1, ring, pos, cuda_device)
-    ws = cmc.DecodeWorkspace(cmc.CmcDims(3, 1, 4, 2, 64, 1, 0, 40), cuda_device)
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(3, 1, 4, 2, 64, 1, 0, 40), cuda_device, q8=True)
     got = cmc.two_tier_decode_attn_q8(*args, workspace=ws)
     assert (got[:2] == 0).all()
     assert ws.status() == cmc.DEVFLAG_BAD_POS
@@ -419,7 +428,7 @@ def test_step_negative_position(cuda_device):
     q, t1, ring, pos = problem(rng, 2, 2, 8, 2, 128, 30, 50, [-4, 20])
     args = device_args(q, t1, ring, pos, cuda_device)
     new = [rows_bf16(rng, 2, 2, 2, 128) for _ in range(2)]
-    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 2, 8, 2, 128, 30, 30, 50), cuda_device)
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 2, 8, 2, 128, 30, 30, 50), cuda_device, q8=True)
     got = cmc.decode_step_q8(*args, *(x.to(cuda_device) for x in new), workspace=ws)
     assert ws.status() == cmc.DEVFLAG_BAD_POS and (got[0] == 0).all()
     codes, scales = (x.copy() for x in ring)
@@ -548,7 +557,7 @@ def test_step_timeout_is_reported(cuda_device, shape):
     new = [rows_bf16(rng, B, shape[1], shape[3], shape[4]).to(cuda_device) for _ in range(2)]
     args = device_args(q, t1, ring, pos, cuda_device)
     dims = cmc.CmcDims(*shape[:5], shape[5], shape[5], shape[6])
-    ws = cmc.DecodeWorkspace(dims, cuda_device)
+    ws = cmc.DecodeWorkspace(dims, cuda_device, q8=True)
     cmc.lib().cmc_test_stall_attention_waits(1)
     try:
         cmc.decode_step_q8(*args, *new, workspace=ws)
@@ -565,14 +574,14 @@ def test_step_timeout_is_reported(cuda_device, shape):
 
 
 def test_plan(cuda_device):
-    """Clusters, one CTA a unit, whole units and cut ones."""
+    """Clusters, one CTA a unit, and more units than resident CTAs."""
     def plan(B, L, H, k, W):
         return cmc.decode_attn_q8_plan(cmc.CmcDims(B, L, 4 * H, H, 128, max(k, 1), k, W))
-    assert plan(1, 1, 2, 32, 128) == (4, 1)        # two tiles a unit, a cluster of two
+    assert plan(1, 1, 2, 32, 128) == (4, 1)        # five blocks a unit, a cluster of two
     assert plan(1, 32, 8, 128, 512) == (256, 1)    # one CTA a unit
-    ctas, launches = plan(40, 1, 8, 128, 512)      # 320 units on fewer CTAs: cut
-    assert ctas < 320 and launches == 2
-    assert plan(64, 32, 8, 128, 512)[0] == ctas
+    ctas, launches = plan(41, 1, 8, 128, 512)      # 328 units on fewer CTAs
+    assert ctas <= 320 and launches == 2
+    assert plan(64, 32, 8, 128, 512) == (ctas, 2)
 
 
 # ---- refusals of the binding ----
@@ -607,6 +616,7 @@ def test_binding_refusals(cuda_device):
     ]:
         with pytest.raises(exc):
             call()
-    small = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 2, 2, 64, 1, 0, 1), dev)
+    small = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 2, 2, 64, 1, 0, 1), dev, q8=True)
+    small.nbytes = 256
     with pytest.raises(cmc.CmcError):
         attn(q, None, None, kv, scales, pos, workspace=small)
