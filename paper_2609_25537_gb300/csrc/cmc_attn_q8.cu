@@ -227,6 +227,31 @@ __device__ __forceinline__ void load_query(const AttnQ8Params& p, int u, uint8_t
   }
 }
 
+// The rare parts of an append, out of line and rolled: the code that a launch runs through once is
+// what it waits for most (its instructions come from L2), so what is not run should
+// not lie in between either.
+// The largest value that the block's other tokens hold (fp32 bits); `mine`: the lane's row is one.
+template <int D>
+static __device__ __noinline__ uint32_t block_held(const uint8_t* rows, bool mine, int lane, int c_old) {
+  uint32_t m = 0u;
+#pragma unroll 1
+  for (int q = 0; q < D / 16; ++q)
+    if (mine) m = max_codes16(m, *reinterpret_cast<const uint4*>(rows + swz8<D>(lane, q)));
+  return __reduce_max_sync(0xffffffffu, held_bits(m, c_old));
+}
+// The block's other tokens' codes for another power of two, in the stage and in the ring.
+template <int D>
+static __device__ __noinline__ void block_recode(uint8_t* rows, uint8_t* ring_row0, bool mine, int lane, float f) {
+  if (!mine) return;
+#pragma unroll 1
+  for (int q = 0; q < D / 16; ++q) {
+    uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(lane, q));
+    const uint4 y = recode16(*at, f);
+    *at = y;
+    reinterpret_cast<uint4*>(ring_row0 + static_cast<long long>(lane) * D)[q] = y;
+  }
+}
+
 // The new token in its block: the token's codes over the stale ones, in the stage and in
 // the ring; the block's other codes too where its power of two changes.  `others`: the
 // block's rows that hold another token.  Returns the block's byte.  (The rules are
@@ -240,27 +265,8 @@ __device__ __forceinline__ int patch_block(uint8_t* rows /* the stage's K or V *
   for (int e = 0; e < D / 32; ++e) top = max(top, finite_bits(x[e]));
   top = __reduce_max_sync(0xffffffffu, top);
   const bool mine = (others >> lane) & 1u;  // the lane's row of the block
-  int c;
-  if (first) {
-    uint32_t m = 0u;
-    if (mine) {
-#pragma unroll
-      for (int q = 0; q < D / 16; ++q) m = max_codes16(m, *reinterpret_cast<const uint4*>(rows + swz8<D>(lane, q)));
-    }
-    c = block_code(max(top, __reduce_max_sync(0xffffffffu, held_bits(m, c_old))));
-  } else {
-    c = max(block_code(top), c_old);
-  }
-  if (c != c_old && mine) {
-    const float f = recode_factor(c_old, c);
-#pragma unroll
-    for (int q = 0; q < D / 16; ++q) {
-      uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(lane, q));
-      const uint4 y = recode16(*at, f);
-      *at = y;
-      reinterpret_cast<uint4*>(ring_row0 + static_cast<long long>(lane) * D)[q] = y;
-    }
-  }
+  const int c = first ? block_code(max(top, block_held<D>(rows, mine, lane, c_old))) : max(block_code(top), c_old);
+  if (c != c_old) block_recode<D>(rows, ring_row0, mine, lane, recode_factor(c_old, c));
   const float f = code_factor(c);
   uint8_t* to = ring_row0 + static_cast<long long>(r) * D;
   if (D == 128) {
@@ -274,6 +280,22 @@ __device__ __forceinline__ int patch_block(uint8_t* rows /* the stage's K or V *
   }
   if (lane == 0) *ring_scale = static_cast<uint8_t>(c);
   return c;
+}
+
+// N bf16 values in shared memory, 2 N bytes aligned, to fp32.
+template <int N>
+__device__ __forceinline__ void load_row(const uint8_t* from, float (&x)[N]) {
+#pragma unroll
+  for (int e = 0; e < N; e += 8) {
+    uint4 w = make_uint4(0u, 0u, 0u, 0u);
+    if (N >= 8) w = *reinterpret_cast<const uint4*>(from + 2 * e);
+    else if (N == 4) { const uint2 v = *reinterpret_cast<const uint2*>(from); w.x = v.x; w.y = v.y; }
+    else w.x = *reinterpret_cast<const uint32_t*>(from);
+    float f[8];
+    unpack8(w, f);
+#pragma unroll
+    for (int q = 0; q < 8 && e + q < N; ++q) x[e + q] = f[q];
+  }
 }
 
 // One warp's place in the flat plan's list of live blocks.
@@ -397,8 +419,10 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     const int chunk = (p.B + kThreads - 1) / kThreads;
     const int b0 = tid * chunk, b1 = min(b0 + chunk, p.B);
     int sum = 0;
+    long long pos_b = 0;  // of sequence b1 - 1
     for (int b = b0; b < b1; ++b) {
-      const SeqState sq = seq_state<FUSED>(p, ld_pos(p, b));
+      pos_b = ld_pos(p, b);
+      const SeqState sq = seq_state<FUSED>(p, pos_b);
       if (sq.bad && blockIdx.x == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
       sum += live_blocks(p, sq);
     }
@@ -432,7 +456,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         if (at < lo || at >= hi) continue;
         unsigned from = lo;
         for (int b = b0; b < b1; ++b) {
-          const long long pb = ld_pos(p, b);
+          const long long pb = chunk == 1 ? pos_b : ld_pos(p, b);
           const unsigned len = static_cast<unsigned>(live_blocks(p, seq_state<FUSED>(p, pb))) * p.LH;
           if (at < from + len) {
             if (e) {
@@ -530,27 +554,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     qa[ks][0] = qa[ks][1] = 0u;
     if (!PAIRED) qb[ks][0] = qb[ks][1] = 0u;
   }
-  // Sums the warp's l over its lanes and leaves O in true units in `ow`: 8 columns of D
-  // floats, columns of odd pairs shifted so that the stores hit distinct banks.
-  auto leave = [&](float* ow) {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
-        l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
-    __syncwarp();  // the warp is done with the stage
-    const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      float* col = ow + (2 * tq + e) * D;
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
-        col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
-      }
-    }
-  };
-  // Rows c .. c + 3 of head hh from what leave() wrote.
+  // Rows c .. c + 3 of head hh from what a warp left (see below).
   auto taken = [&](const float* ow, int hh, int c) {
     float4 y = *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
     if (PAIRED) {
@@ -562,6 +566,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   };
 
   bool gave_up = false;
+  float* left_in = nullptr;  // strided plan: where the warp left its output
   int s = 0;             // stage
   uint32_t phase = 0;    // its parity
   for (int i = 0; i < n_run; ++i) {
@@ -597,73 +602,92 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
           __syncwarp();
         }
       }
-      // The query as two e4m3 pieces.  Thread: head (column) gq, of the elements
-      // 32 ks + 16 hf + 4 tq .. + 3; those and the other three tq's are the head.
-      const int hq = PAIRED ? (gq & 3) : gq;
-      const uint8_t* qrow = q_slot + hq * D * 2;
-      float x[KS][2][4];
+      // The query as two e4m3 pieces, by the whole warp: a lane takes EPL neighbouring elements
+      // of one head, the LPH lanes of a head share its largest.  The pieces, a byte each, go
+      // over the raw rows: hi [G][D], lo [G][D]; the fragments are read from there.
+      constexpr int EPL = G * D / 32, LPH = 32 / G;
+      float x[EPL];
+      load_row<EPL>(q_slot + lane * (EPL * 2), x);
+      if (FUSED && p.rope) {  // element c's partner c +- d/2 is the same of the lane LPH / 2 away
+        float y[EPL];
+        load_row<EPL>(q_slot + (lane ^ (LPH / 2)) * (EPL * 2), y);
+        const float sg = (lane & (LPH / 2)) ? 1.f : -1.f;
+        const float2* tab = rope_tab + (lane & (LPH / 2 - 1)) * EPL;
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          uint2 v = make_uint2(0u, 0u);
-          if (hq < G) v = *reinterpret_cast<const uint2*>(qrow + (32 * ks + 16 * hf + 4 * tq) * 2);
-          x[ks][hf][0] = bf16lo_to_f32(v.x); x[ks][hf][1] = bf16hi_to_f32(v.x);
-          x[ks][hf][2] = bf16lo_to_f32(v.y); x[ks][hf][3] = bf16hi_to_f32(v.y);
+        for (int e = 0; e < EPL; ++e) {
+          const float2 cs = tab[e];
+          x[e] = fmaf(x[e], cs.x, sg * y[e] * cs.y);
         }
-      __syncwarp();  // the query slot is free
-      // the next unit's rows, which follow where the run goes on behind this unit
-      if (cm == 0 && lane == 0 && i + hw.w < n_run)
-        load_query<D, G, FUSED>(p, u + 1, q_slot, new_slots + ((n_units + 1) & 1) * (2 * D * 2), &q_bar[warp]);
-      if (FUSED && p.rope) {  // k-steps ks and ks + KS/2 hold the partners
-#pragma unroll
-        for (int ks = 0; ks < KS / 2; ++ks)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float2 cs = rope_tab[32 * ks + 16 * hf + 4 * tq + e];
-              const float a = x[ks][hf][e], b = x[ks + KS / 2][hf][e];
-              x[ks][hf][e] = fmaf(a, cs.x, -b * cs.y);
-              x[ks + KS / 2][hf][e] = fmaf(b, cs.x, a * cs.y);
-            }
       }
-      uint32_t top = 0u;
+      float top = 0.f;  // (a NaN does not count)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int e = 0; e < EPL; ++e) top = fmaxf(top, fabsf(x[e]));
+      if (__any_sync(0xffffffffu, top == INFINITY)) {  // an infinity becomes NaN and does not count either
+        top = 0.f;
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf)
+        for (int e = 0; e < EPL; ++e) {
+          x[e] = fmaf(x[e], 0.f, x[e]);
+          top = fmaxf(top, fabsf(x[e]));
+        }
+      }
 #pragma unroll
-          for (int e = 0; e < 4; ++e) top = max(top, finite_bits(x[ks][hf][e]));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int qc = block_code(top);
-      const float f = code_factor(qc);
+      for (int off = 1; off < LPH; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const int qc = block_code(__float_as_uint(top));
+      const float qf = code_factor(qc);
+      uint32_t ph[(EPL + 3) / 4], pl[(EPL + 3) / 4];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+      for (int e = 0; e < EPL; e += 2) {
+        uint32_t hi, lo;
+        two_pieces(x[e] * qf, x[e + 1] * qf, hi, lo);
+        if (e & 2) {
+          ph[e / 4] |= hi << 16;
+          pl[e / 4] |= lo << 16;
+        } else {
+          ph[e / 4] = hi;
+          pl[e / 4] = lo;
+        }
+      }
+      __syncwarp();  // every lane has read its rows
+      {
+        uint8_t* hi_at = q_slot + lane * EPL;
+        uint8_t* lo_at = hi_at + G * D;
+        if (EPL == 2) {
+          *reinterpret_cast<uint16_t*>(hi_at) = static_cast<uint16_t>(ph[0]);
+          *reinterpret_cast<uint16_t*>(lo_at) = static_cast<uint16_t>(pl[0]);
+        } else {
 #pragma unroll
-        for (int hf = 0; hf < 2; ++hf) {
-          float y[4], h[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = scaled(x[ks][hf][e], f);
-          const uint32_t hi = e4m3_pair(y[0], y[1]) | (e4m3_pair(y[2], y[3]) << 16);
-          decode4(hi, h);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) y[e] = 16.f * (y[e] - h[e]);
-          const uint32_t lo = e4m3_pair(y[0], y[1]) | (e4m3_pair(y[2], y[3]) << 16);
-          if (PAIRED) {
-            qa[ks][hf] = gq < 4 ? hi : lo;
-          } else {
-            qa[ks][hf] = hi;
-            qb[ks][hf] = lo;
+          for (int e = 0; e < EPL / 4; ++e) {
+            reinterpret_cast<uint32_t*>(hi_at)[e] = ph[e];
+            reinterpret_cast<uint32_t*>(lo_at)[e] = pl[e];
           }
         }
+      }
+      __syncwarp();
+      // fragments: column gq, elements 32 ks + 16 hf + 4 tq .. + 3
+      const int hq = PAIRED ? (gq & 3) : gq;
+      if (hq < G) {
+        const uint8_t* from = q_slot + (PAIRED && gq >= 4 ? G * D : 0) + hq * D + 4 * tq;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            qa[ks][hf] = *reinterpret_cast<const uint32_t*>(from + 32 * ks + 16 * hf);
+            if (!PAIRED) qb[ks][hf] = *reinterpret_cast<const uint32_t*>(from + G * D + 32 * ks + 16 * hf);
+          }
+      }
       const float qscale = e8m0_to_f32(qc) * p.scale_log2;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        qs[e] = __shfl_sync(0xffffffffu, qscale, 4 * (h0 + e));
+        qs[e] = __shfl_sync(0xffffffffu, qscale, (h0 + e) * LPH);
         m_run[e] = -INFINITY;
         l_run[e] = 0.f;
+      }
+      // the next unit's rows into the slot, where the run goes on behind this unit
+      if (cm == 0 && i + hw.w < n_run) {
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+        if (lane == 0)
+          load_query<D, G, FUSED>(p, u + 1, q_slot, new_slots + ((n_units + 1) & 1) * (2 * D * 2), &q_bar[warp]);
       }
       e_cur = e_top = -1;
 #pragma unroll
@@ -676,7 +700,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       const bool first = (hw.z & 31) == 0;
       const uint16_t* rows = reinterpret_cast<const uint16_t*>(new_slots + ((n_units - 1) & 1) * (2 * D * 2));
       constexpr int E = D / 32;
-#pragma unroll
+#pragma unroll 1
       for (int v = 0; v < 2; ++v) {
         const uint16_t* row = rows + v * D;
         float x[4] = {0.f, 0.f, 0.f, 0.f};
@@ -859,11 +883,33 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     }
 
 
-    if (ends && cm == 0) {
-      // The unit's share of this run is done: written out where it is the whole unit, else left
-      // as a record (the first of the run's if the unit began before it).
-      float* ow = reinterpret_cast<float*>(stage);  // K's part: just the size
-      leave(ow);
+    if (ends) {
+      // The unit's share of this run is done.  The warp sums its l over the lanes and leaves O in
+      // true units in its stage: 8 columns of D floats, just the size of K's part, columns
+      // of odd pairs shifted so that the stores hit distinct banks.
+      float* ow = reinterpret_cast<float*>(stage);
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
+          l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
+      __syncwarp();  // the warp is done with the stage
+      const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float* col = ow + (2 * tq + e) * D;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) {
+          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
+          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
+        }
+      }
+      if (cm > 0) {
+        left_in = ow;
+        break;  // the run's last block
+      }
+      // Flat plan: written out where it is the whole unit, else left as a record (the first of the
+      // run's if the unit began before it).
       __syncwarp();
       wrote_stage = true;
       const bool whole = begun_first && (flags & QF_LAST);
@@ -934,20 +980,23 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   }
 
   // ---- strided plan: the four warps' states, then the cluster's CTAs' ----
-  // Every warp leaves its output in its first stage; after a barrier each thread takes four
-  // rows of the head dimension of one head, rescales and adds the warps' in warp order.
-  {
-    leave(reinterpret_cast<float*>(stages));
-    if (gq == 0 && (!PAIRED || tq < 2)) {
+  // After a barrier each thread takes four rows of the head dimension of one head, rescales and
+  // adds what the warps left, in warp order.
+  if (!left_in) {  // no blocks (or a timeout): nothing
+    left_in = reinterpret_cast<float*>(stages);
+    for (int x = lane; x < 8 * D; x += 32) left_in[x] = 0.f;
+    l_run[0] = l_run[1] = 0.f;
+    m_run[0] = m_run[1] = -INFINITY;
+  }
+  if (lane == 0) s_first[warp][0] = static_cast<int>(reinterpret_cast<uint8_t*>(left_in) - smem);
+  if (gq == 0 && (!PAIRED || tq < 2)) {
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        merge_m[warp * 8 + h0 + e] = m_run[e];
-        merge_l[warp * 8 + h0 + e] = l_run[e];
-      }
+    for (int e = 0; e < 2; ++e) {
+      merge_m[warp * 8 + h0 + e] = m_run[e];
+      merge_l[warp * 8 + h0 + e] = l_run[e];
     }
   }
   __syncthreads();
-  const float* all_o = reinterpret_cast<const float*>(stages - warp * (NST * S::kStage));
   const long long out_base = static_cast<long long>(su) * (G * D);
   constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
   float4 cacc[XPT];
@@ -967,7 +1016,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) {
       const float f = ex2(merge_m[v * 8 + hh] - Mr);
-      const float4 y = taken(all_o + v * (NST * S::kStage / 4), hh, c);
+      const float4 y = taken(reinterpret_cast<const float*>(smem + s_first[v][0]), hh, c);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
       acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
       Ls = fmaf(f, merge_l[v * 8 + hh], Ls);
