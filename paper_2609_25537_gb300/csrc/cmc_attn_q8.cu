@@ -23,32 +23,26 @@
 //            live blocks are equal whatever the rings' fill: 64 sequences with rings
 //            filled to a third in the mean, 256 + 2,048 keys at most: see DESIGN.
 //
-// Both products run on e4m3 operands (mma.sync m16n8k32, fp32 accumulation,
-// exact products), so no code is ever converted: K by ldmatrix, V by the byte
-// transposing ldmatrix of sm_100.  The other operands are written as two e4m3
-// pieces, x = hi + lo / 16, each with four significant bits:
-//   q    times a power of two so that its largest element is in (224, 448].  A bf16
-//        element has eight significant bits, so hi + lo / 16 is exact down to 2^-14 of
-//        the largest, and off by 2^-22 of the largest below.
-//   p    256 times the probability relative to the largest so far: rounded to eight
-//        significant bits (2^-8, as a bf16 probability) down to 2^-14, and off by 2^-22
-//        below.
-// A product has eight columns and a KV head G query heads.  For G <= 4 the lo
-// pieces are the columns 4 .. 7 of the same products, so they cost nothing; for
-// G = 8 they take products of their own.
-//   S^T = K Q^T   16 keys as the rows, d in k-steps of 32
-//   O^T += V^T P^T  16 rows of the head dimension, the block's 32 keys as the k-step
+// Both products run on fp16 operands with fp32 accumulation (mma.sync m16n8k16): the
+// codes are converted to fp16 in registers, exactly, one instruction for two.  (mma.sync
+// takes e4m3 operands too, but on this GPU it does the same conversions underneath, for
+// both operands, on every call: 672 instructions a block, which bounded the kernel.)
+//   S^T = K Q^T     16 keys as the rows, the G query heads as the columns, d in k-steps of 16
+//   O^T += V^T P^T  16 rows of the head dimension, the heads, the block's 32 keys in two k-steps
+//   q    is multiplied by a power of two so that its head's largest element is in (224, 448].  fp16
+//        holds a bf16 element exactly down to 2^-22 of that, and is off by 2^-33 of it below.
+//   p    relative to the largest so far, times 2^15: eleven significant bits down to 2^-29
+//        of the largest, off by 2^-40 of it below.
 // K's power of two joins the softmax scale.  V's cannot (it changes from block to
 // block): O is kept in units of 2^(E - 127) with E the byte of a recent block, and
-// rescaled, as for a new maximum, when a block's byte is above E or more than four
-// below it; in between p is multiplied by the difference.
+// rescaled, as for a new maximum, when a block's byte is above E or more than ten
+// below it; in between p takes the difference.
 //
-// P^T has to go from the accumulators of S^T (keys down the rows) to the B operand
-// (four neighbouring k a register).  A pair of codes is one 16-bit element of an
-// 8 x 8 transpose (movmatrix) if its two keys are those of the two 16-key products'
-// same row; the k order that this gives is met by the order of V's row addresses.
-// The second product's rows are exchanged by halves (row r is key 16 + (r ^ 4)) so
-// that eight consecutive k lie in eight different bank groups.
+// The order of d in a k-step is free: lane t of a quad has the bytes 4 t .. 4 t + 3 of a
+// 16-byte chunk of a key's codes, and they are its four k.  So is the order of the keys, which
+// P^T's way from the accumulators of S^T to the B operand (movmatrix) fixes for the row
+// addresses of V; rows 8 .. 15 of a product are keys 8 + (r ^ 4), so that eight
+// consecutive rows of V lie in eight different bank groups.
 #include <atomic>
 
 #include "cmc_attn.cuh"
@@ -58,7 +52,7 @@ namespace cmc {
 
 // The flat plan's grid is limited so that a workspace's size does not depend on the
 // device: two records for each of its warps.
-constexpr int kQ8MaxCtas = 320;
+constexpr int kQ8MaxCtas = 480;
 constexpr int kQ8RecHead = 4;  // words before a record's maxima: valid, ends
 // Units up to which a call never takes the flat plan (and its workspace holds no records).
 constexpr int kQ8StridedUnits = 128;
@@ -76,26 +70,26 @@ struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the spl
   int rope;                   // rotate q and the new key (fused step)
 };                            // cm: CTAs per unit (strided plan), 0: flat plan
 
-// Shared memory of a CTA: per warp a query slot, two slots for the new token's rows, a
-// rotary table and the headers of its stages; the warps' (max, sum) and what a
-// cluster's peers send; then, 1,024-byte aligned, the stages.
+// Shared memory of a CTA: per warp a query slot, a rotary table and the headers of its
+// stages (in the end the warp's maxima and sums); what a cluster's peers send; then,
+// 1,024-byte aligned, the stages.
 template <int D, int G>
 struct Q8Smem {
-  // 96 KB of stages a CTA, two CTAs an SM; at d = 128 and G = 8 the rest does not fit beside
-  // that twice, and one CTA an SM has them all.
-  static constexpr int NST = D == 64 || G == 8 ? 6 : 3;
+  // 64 KB of stages a CTA and three CTAs an SM (at d = 128 and G = 8: 96 KB, two an SM).
+#ifndef Q8NST
+#define Q8NST 3
+#endif
+  static constexpr int NST = D == 64 ? 2 * Q8NST : G == 8 ? 3 : Q8NST;
   static constexpr int kV = kQ8Block * D;
   static constexpr int kStage = 2 * kQ8Block * D;
   static constexpr int kQ = 0;                                // [warp][G][D] bf16
-  static constexpr int kNew = kQ + kWarps * G * D * 2;        // [warp][2][K row, V row] bf16
-  static constexpr int kRope = kNew + kWarps * 2 * 2 * D * 2; // [warp][d/2] (cos, sin)
+  static constexpr int kRope = kQ + kWarps * G * D * 2;       // [warp][d/2] (cos, sin)
   static constexpr int kHdr = kRope + kWarps * D * 4;         // [warp][NST][8] words
-  static constexpr int kMergeM = kHdr + kWarps * NST * 32;    // [warp][8]
-  static constexpr int kMergeL = kMergeM + kWarps * 32;
-  static constexpr int kRecv = kMergeL + kWarps * 32;         // groups of 16 bytes, rank by rank
+  static constexpr int kRecv = kHdr + kWarps * NST * 32;      // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
   static constexpr int kSmall = kRecvMl + kMaxClusterCtas * G * 8;
   static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
+  static_assert(NST >= 2, "a warp's headers hold its 8 maxima and 8 sums");
 };
 // Header words of a stage: what the warp has to know of the block in it.
 enum { Q_WHAT = 0, Q_UNIT = 1, Q_SLOT = 2, Q_LEFT = 3, Q_KS = 4, Q_VS = 5, Q_POS = 6 };
@@ -133,40 +127,34 @@ __device__ __forceinline__ void ldsm_b8_t(uint32_t addr, uint32_t& r0, uint32_t&
                : "r"(addr));
 }
 
-// C[16x8] += A[16x32] B[32x8], e4m3 inputs, fp32 accumulators.
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                         uint32_t a3, uint32_t b0, uint32_t b1) {
+// C[16x8] += A[16x16] B[16x8], fp16 inputs, fp32 accumulators.
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                        uint32_t b0, uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%0,%1,%2,%3};\n"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void mma_e4m3_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
-                                              uint32_t a3, uint32_t b0, uint32_t b1) {
+__device__ __forceinline__ void mma_f16_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                             uint32_t b0, uint32_t b1) {
   asm volatile(
-      "mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
       "{%8,%9}, {%10,%10,%10,%10};\n"
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-
-// Two probabilities as two e4m3 pieces each (a in the low byte): hi, and lo = 16 (x - hi).
-// Through fp16, whose 11 bits and steps of 2^-24 lose nothing that the pieces keep.
-__device__ __forceinline__ void two_pieces(float a, float b, uint32_t& hi, uint32_t& lo) {
-  uint16_t h, l;
-  asm("{\n .reg .b32 x, y, s;\n"
-      " cvt.rn.f16x2.f32 x, %3, %2;\n"
-      " cvt.rn.satfinite.e4m3x2.f16x2 %0, x;\n"
-      " cvt.rn.f16x2.e4m3x2 y, %0;\n"
-      " sub.rn.f16x2 y, x, y;\n"
-      " mov.b32 s, 0x4C004C00;\n"  // 16, 16
-      " mul.rn.f16x2 y, y, s;\n"
-      " cvt.rn.satfinite.e4m3x2.f16x2 %1, y;\n}\n"
-      : "=&h"(h), "=&h"(l)
-      : "f"(a), "f"(b));
-  hi = h;
-  lo = l;
+// Four codes to fp16 (lo: bytes 0 and 1).
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n"
+      " cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
+      : "=r"(lo), "=r"(hi)
+      : "r"(w));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
 }
 
 // Live blocks of a unit whose sequence's state is sq (one, empty, where there are none: its
@@ -215,16 +203,21 @@ __device__ __forceinline__ void write_header(const AttnQ8Params& p, uint8_t* hdr
   *reinterpret_cast<long long*>(hdr + 4 * Q_POS) = sq.pos;
 }
 
-// A unit's query rows and, for the fused step, its new token's rows.
-template <int D, int G, bool FUSED>
-__device__ __forceinline__ void load_query(const AttnQ8Params& p, int u, uint8_t* q, uint8_t* fresh,
-                                           uint64_t* bar) {
-  mbar_arrive_expect_tx(bar, G * D * 2 + (FUSED ? 2 * D * 2 : 0) + p.stall_tx);
+// A unit's query rows into the warp's slot.
+template <int D, int G>
+__device__ __forceinline__ void load_query(const AttnQ8Params& p, int u, uint8_t* q, uint64_t* bar) {
+  mbar_arrive_expect_tx(bar, G * D * 2 + p.stall_tx);
   bulk_copy(smem_addr(q), p.q + static_cast<long long>(u) * (G * D), G * D * 2, bar);
-  if (FUSED) {
-    bulk_copy(smem_addr(fresh), p.k_new + static_cast<long long>(u) * D, D * 2, bar);
-    bulk_copy(smem_addr(fresh + D * 2), p.v_new + static_cast<long long>(u) * D, D * 2, bar);
-  }
+}
+
+// The new token's rows of a unit (fused step): lanes 0-15 hold K's, lanes 16-31 V's, d / 16
+// neighbouring elements each.
+template <int D>
+__device__ __forceinline__ uint4 load_new(const AttnQ8Params& p, int u, int lane) {
+  const uint16_t* row = (lane < 16 ? p.k_new : p.v_new) + static_cast<long long>(u) * D + (lane & 15) * (D / 16);
+  if (D == 128) return __ldg(reinterpret_cast<const uint4*>(row));
+  const uint2 w = __ldg(reinterpret_cast<const uint2*>(row));
+  return make_uint4(w.x, w.y, 0u, 0u);
 }
 
 // The rare parts of an append, out of line and rolled: the code that a launch runs through once is
@@ -253,33 +246,74 @@ static __device__ __noinline__ void block_recode(uint8_t* rows, uint8_t* ring_ro
 }
 
 // The new token in its block: the token's codes over the stale ones, in the stage and in
-// the ring; the block's other codes too where its power of two changes.  `others`: the
-// block's rows that hold another token.  Returns the block's byte.  (The rules are
-// window_append_q8_kernel's.)
+// the ring; the block's other codes too where its power of two changes.  Half a warp
+// each for K and V (`fresh`: load_new's).  r: the token's row; `others`: the block's rows
+// that hold another token; slot: its ring slot; kc, vc: the block's bytes.  (The rules
+// are window_append_q8_kernel's.)
 template <int D>
-__device__ __forceinline__ int patch_block(uint8_t* rows /* the stage's K or V */, uint8_t* ring_row0,
-                                           uint8_t* ring_scale, const float (&x)[4], int r, int c_old,
-                                           bool first, uint32_t others, int lane) {
+__device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stage, int u, int r, int slot,
+                                            uint32_t others, const uint4& fresh, const float2* rope_tab, int& kc,
+                                            int& vc, int lane) {
+  constexpr int E = D / 16;  // elements a lane has of its row
+  const int half = lane >> 4;
+  float x[8];
+  unpack8(fresh, x);
+  if (p.rope) {  // K's element c pairs with c +- d/2, the same of the lane 8 away
+    uint4 w;
+    w.x = __shfl_xor_sync(0xffffffffu, fresh.x, 8);
+    w.y = __shfl_xor_sync(0xffffffffu, fresh.y, 8);
+    w.z = D == 128 ? __shfl_xor_sync(0xffffffffu, fresh.z, 8) : 0u;
+    w.w = D == 128 ? __shfl_xor_sync(0xffffffffu, fresh.w, 8) : 0u;
+    float y[8];
+    unpack8(w, y);
+    if (half == 0) {
+      const float sg = lane < 8 ? -1.f : 1.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float2 cs = rope_tab[(lane & 7) * E + e];
+        x[e] = fmaf(x[e], cs.x, sg * y[e] * cs.y);
+      }
+    }
+  }
   uint32_t top = 0u;
 #pragma unroll
-  for (int e = 0; e < D / 32; ++e) top = max(top, finite_bits(x[e]));
-  top = __reduce_max_sync(0xffffffffu, top);
-  const bool mine = (others >> lane) & 1u;  // the lane's row of the block
-  const int c = first ? block_code(max(top, block_held<D>(rows, mine, lane, c_old))) : max(block_code(top), c_old);
-  if (c != c_old) block_recode<D>(rows, ring_row0, mine, lane, recode_factor(c_old, c));
-  const float f = code_factor(c);
-  uint8_t* to = ring_row0 + static_cast<long long>(r) * D;
-  if (D == 128) {
-    const uint32_t w = encode4(x[0], x[1], x[2], x[3], f);
-    *reinterpret_cast<uint32_t*>(rows + swz8<D>(r, lane >> 2) + (lane & 3) * 4) = w;
-    reinterpret_cast<uint32_t*>(to)[lane] = w;
-  } else {
-    const uint16_t w = static_cast<uint16_t>(e4m3_pair(scaled(x[0], f), scaled(x[1], f)));
-    *reinterpret_cast<uint16_t*>(rows + swz8<D>(r, lane >> 3) + (lane & 7) * 2) = w;
-    reinterpret_cast<uint16_t*>(to)[lane] = w;
+  for (int e = 0; e < E; ++e) top = max(top, finite_bits(x[e]));
+#pragma unroll
+  for (int off = 1; off < 16; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+  const bool mine = (others >> lane) & 1u;  // the lane's row of the block, where codes change
+  const long long uv = 2LL * u;
+  uint8_t* ring_k = p.ring_kv + (uv * p.W + slot - r) * D;  // the block's first row
+  uint8_t* ring_v = ring_k + static_cast<long long>(p.W) * D;
+  const int c_old = half ? vc : kc;
+  int c = max(block_code(top), c_old);
+  if ((slot & (kQ8Block - 1)) == 0) {
+    const uint32_t hk = block_held<D>(stage, mine, lane, kc);
+    const uint32_t hv = block_held<D>(stage + kQ8Block * D, mine, lane, vc);
+    c = block_code(max(top, half ? hv : hk));
   }
-  if (lane == 0) *ring_scale = static_cast<uint8_t>(c);
-  return c;
+  if (__any_sync(0xffffffffu, c != c_old)) {
+    const float f = recode_factor(c_old, c);
+    const int same = c == c_old;
+    const float fk = __shfl_sync(0xffffffffu, f, 0), fv = __shfl_sync(0xffffffffu, f, 16);
+    if (!__shfl_sync(0xffffffffu, same, 0)) block_recode<D>(stage, ring_k, mine, lane, fk);
+    if (!__shfl_sync(0xffffffffu, same, 16)) block_recode<D>(stage + kQ8Block * D, ring_v, mine, lane, fv);
+  }
+  const float f = code_factor(c);
+  uint8_t* at = stage + half * (kQ8Block * D);
+  uint8_t* to = (half ? ring_v : ring_k) + static_cast<long long>(r) * D + (lane & 15) * E;
+  const uint32_t w0 = encode4(x[0], x[1], x[2], x[3], f);
+  if (D == 128) {
+    const uint2 w = make_uint2(w0, encode4(x[4], x[5], x[6], x[7], f));
+    *reinterpret_cast<uint2*>(at + swz8<D>(r, (lane & 15) >> 1) + (lane & 1) * 8) = w;
+    *reinterpret_cast<uint2*>(to) = w;
+  } else {
+    *reinterpret_cast<uint32_t*>(at + swz8<D>(r, (lane & 15) >> 2) + (lane & 3) * 4) = w0;
+    *reinterpret_cast<uint32_t*>(to) = w0;
+  }
+  if ((lane & 15) == 0) p.ring_scales[(uv + half) * p.ringS + slot / kQ8Block] = static_cast<uint8_t>(c);
+  kc = __shfl_sync(0xffffffffu, c, 0);
+  vc = __shfl_sync(0xffffffffu, c, 16);
+  __syncwarp();
 }
 
 // N bf16 values in shared memory, 2 N bytes aligned, to fp32.
@@ -310,11 +344,8 @@ __global__ void __maxnreg__(168)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   using S = Q8Smem<D, G>;
   constexpr int NST = S::NST;
-  constexpr int KS = D / 32;         // k-steps of the Q K^T product
-  constexpr int MT = D / 16;         // m-tiles of O^T
-  constexpr bool PAIRED = G <= 4;    // hi and lo pieces in one product
-  constexpr int NV = PAIRED ? 2 : 4; // scores a thread has of each of its two heads
-  constexpr int NGR = G * D / 4;     // groups of four rows of the head dimension of a unit's output
+  constexpr int KS = D / 16;      // k-steps of the Q K^T product, m-tiles of O^T
+  constexpr int NGR = G * D / 4;  // groups of four rows of the head dimension of a unit's output
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(8) uint64_t full_bar[kWarps][NST];
   __shared__ __align__(8) uint64_t q_bar[kWarps];
@@ -329,10 +360,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
                     warp * (NST * S::kStage);
   uint8_t* hdrs = smem + S::kHdr + warp * (NST * 32);
   uint8_t* q_slot = smem + S::kQ + warp * (G * D * 2);
-  uint8_t* new_slots = smem + S::kNew + warp * (2 * 2 * D * 2);
   float2* rope_tab = reinterpret_cast<float2*>(smem + S::kRope + warp * (D * 4));
-  float* merge_m = reinterpret_cast<float*>(smem + S::kMergeM);  // [kWarps][8]
-  float* merge_l = reinterpret_cast<float*>(smem + S::kMergeL);
   uint64_t* full = full_bar[warp];
 
   // strided plan: the CTA's unit, the warp's first block and their distance
@@ -387,25 +415,23 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   long long pos_next = 0;  // flat plan: pos of the next sequence, ahead of its use
   int last_b = 0;          // the run's last sequence
   bool counted = false;    // this warp's reading of pos is done and counted
+  unsigned long long ticket = 0;  // and how many were before it
+  uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows of the present unit
   if (cm > 0) {
     // ---- strided: the first blocks at once, then pos ----
-    if (lane == 0 && g0 < nb_all) load_query<D, G, FUSED>(p, su, q_slot, new_slots, &q_bar[warp]);
+    if (lane == 0 && g0 < nb_all) load_query<D, G>(p, su, q_slot, &q_bar[warp]);
     for (; issued < NST && g0 + issued * step < nb_all; ++issued)
       load_block<D>(p, maps, su, g0 + issued * step, stages + issued * S::kStage, hdrs + issued * 32, &full[issued],
                     lane);
+    if (FUSED) fresh = load_new<D>(p, su, lane);
     w.b = static_cast<int>(static_cast<unsigned>(su) / static_cast<unsigned>(p.LH));
     if (tid == 0) s_pos[0] = ld_pos(p, w.b);
     __syncthreads();
     w.sq = seq_state<FUSED>(p, s_pos[0]);
     if (tid == 0) {
       if (w.sq.bad && rank == 0 && su % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-      if (FUSED) {  // the last CTA to have read pos[b] advances it
-        const unsigned long long old = atomicAdd(p.tickets + w.b, 1ull);
-        if (old + 1 == static_cast<unsigned long long>(p.LH) * cm) {
-          if (!w.sq.bad) p.pos[w.b] = w.sq.pos + 1;
-          p.tickets[w.b] = 0ull;
-        }
-      }
+      // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
+      if (FUSED) ticket = atomicAdd(p.tickets + w.b, 1ull);
     }
     w.nb = live_blocks(p, w.sq);
     n_run = w.nb > g0 ? (w.nb - g0 + step - 1) / step : 0;
@@ -482,25 +508,19 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       w.x = off / w.nb;
       w.j = off - w.x * w.nb;
       w.u = w.b * p.LH + w.x;
-      if (lane == 0) load_query<D, G, FUSED>(p, w.u, q_slot, new_slots, &q_bar[warp]);
+      if (lane == 0) load_query<D, G>(p, w.u, q_slot, &q_bar[warp]);
       if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
     }
   }
-  // Flat plan: the last warp to have read pos of all its sequences advances every pos.
-  auto count_reads = [&]() {
+  // Flat plan: counts that this warp has read pos of all its sequences; the last one to be counted
+  // advances every pos, when its run is done (the count takes a trip to L2).  `nb` comes of
+  // the last pos, and makes the count wait for it.
+  auto count_reads = [&](int nb) {
     counted = true;
-    unsigned last = 0;
     if (lane == 0) {
-      __threadfence();
-      const unsigned long long old = atomicAdd(p.tickets, 1ull);
-      last = old + 1 == static_cast<unsigned long long>(gridDim.x) * kWarps;
-      if (last) p.tickets[0] = 0ull;
-    }
-    if (__shfl_sync(0xffffffffu, last, 0)) {
-      for (int b = lane; b < p.B; b += 32) {
-        const long long v = ld_pos(p, b);
-        if (v >= 0) p.pos[b] = v + 1;
-      }
+      int seen;
+      asm volatile("mov.b32 %0, %1;\n" : "=r"(seen) : "r"(nb));
+      ticket = atomicAdd(p.tickets, seen > 0 ? 1ull : 0ull);
     }
   };
   // Requests the run's next block into stage s, with its header.
@@ -525,44 +545,34 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
       }
     }
-    if (FUSED && !counted && w.b == last_b) count_reads();
+    if (FUSED && !counted && w.b == last_b) count_reads(w.nb);
   };
   if (cm == 0) {
-    if (FUSED && (n_run == 0 || w.b == last_b)) count_reads();
+    if (FUSED && (n_run == 0 || w.b == last_b)) count_reads(n_run == 0 ? 1 : w.nb);
     while (issued < NST && issued < n_run) request(issued);
   }
   __syncwarp();
 
-  // gq = lane / 4, tq = lane % 4.  A thread's two heads (columns 2 tq, 2 tq + 1 of the
-  // products): h0 + e, e = 0, 1; for G <= 4 threads with tq >= 2 have the lo pieces.
+  // gq = lane / 4, tq = lane % 4: a thread has columns (heads) 2 tq and 2 tq + 1 of the products
+  // (heads >= G are padding: zero queries, never written out).
   const int gq = lane >> 2;
   const int tq = lane & 3;
-  const int h0 = PAIRED ? 2 * (tq & 1) : 2 * tq;
   int n_units = 0;                             // units begun
   bool begun_first = false;                    // the present one with its first block
   bool head = false, tail = false;             // flat plan: records written
   long long rope_pos = -1;                     // position that the rotary table is for
-  uint32_t qa[KS][2], qb[PAIRED ? 1 : KS][2];  // Q^T fragments: hi (or both pieces); G = 8: lo
+  uint32_t qa[KS][2];                          // Q^T fragments
   float qs[2] = {0.f, 0.f};                    // softmax scale * log2(e) * the heads' powers of two
   float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
   int e_cur = -1, e_top = -1;                  // the byte O is in units of; the largest so far
-  float o[MT][4];
+  float o[KS][4];
 #pragma unroll
-  for (int j = 0; j < MT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+  for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
 #pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    qa[ks][0] = qa[ks][1] = 0u;
-    if (!PAIRED) qb[ks][0] = qb[ks][1] = 0u;
-  }
+  for (int ks = 0; ks < KS; ++ks) qa[ks][0] = qa[ks][1] = 0u;
   // Rows c .. c + 3 of head hh from what a warp left (see below).
   auto taken = [&](const float* ow, int hh, int c) {
-    float4 y = *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
-    if (PAIRED) {
-      const float4 z = *reinterpret_cast<const float4*>(ow + (hh + 4) * D + (c ^ (8 * ((hh + 4) >> 1))));
-      y.x = fmaf(z.x, 0.0625f, y.x); y.y = fmaf(z.y, 0.0625f, y.y);
-      y.z = fmaf(z.z, 0.0625f, y.z); y.w = fmaf(z.w, 0.0625f, y.w);
-    }
-    return y;
+    return *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
   };
 
   bool gave_up = false;
@@ -591,6 +601,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         break;
       }
       begun_first = flags & QF_FIRST;
+      if (FUSED && cm == 0) fresh = load_new<D>(p, u, lane);
       if (FUSED && p.rope) {
         const long long pos = *reinterpret_cast<const long long*>(hdr + 4 * Q_POS);
         if (pos >= 0 && pos != rope_pos) {
@@ -602,9 +613,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
           __syncwarp();
         }
       }
-      // The query as two e4m3 pieces, by the whole warp: a lane takes EPL neighbouring elements
-      // of one head, the LPH lanes of a head share its largest.  The pieces, a byte each, go
-      // over the raw rows: hi [G][D], lo [G][D]; the fragments are read from there.
+      // The query in fp16, by the whole warp: a lane takes EPL neighbouring elements of one
+      // head, the LPH lanes of a head share its largest.  It goes over the raw rows; the
+      // fragments are read from there.
       constexpr int EPL = G * D / 32, LPH = 32 / G;
       float x[EPL];
       load_row<EPL>(q_slot + lane * (EPL * 2), x);
@@ -634,51 +645,24 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       for (int off = 1; off < LPH; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
       const int qc = block_code(__float_as_uint(top));
       const float qf = code_factor(qc);
-      uint32_t ph[(EPL + 3) / 4], pl[(EPL + 3) / 4];
-#pragma unroll
-      for (int e = 0; e < EPL; e += 2) {
-        uint32_t hi, lo;
-        two_pieces(x[e] * qf, x[e + 1] * qf, hi, lo);
-        if (e & 2) {
-          ph[e / 4] |= hi << 16;
-          pl[e / 4] |= lo << 16;
-        } else {
-          ph[e / 4] = hi;
-          pl[e / 4] = lo;
-        }
-      }
       __syncwarp();  // every lane has read its rows
-      {
-        uint8_t* hi_at = q_slot + lane * EPL;
-        uint8_t* lo_at = hi_at + G * D;
-        if (EPL == 2) {
-          *reinterpret_cast<uint16_t*>(hi_at) = static_cast<uint16_t>(ph[0]);
-          *reinterpret_cast<uint16_t*>(lo_at) = static_cast<uint16_t>(pl[0]);
-        } else {
 #pragma unroll
-          for (int e = 0; e < EPL / 4; ++e) {
-            reinterpret_cast<uint32_t*>(hi_at)[e] = ph[e];
-            reinterpret_cast<uint32_t*>(lo_at)[e] = pl[e];
-          }
-        }
-      }
+      for (int e = 0; e < EPL; e += 2)
+        reinterpret_cast<uint32_t*>(q_slot + lane * (EPL * 2))[e / 2] = pack_f16(x[e] * qf, x[e + 1] * qf);
       __syncwarp();
-      // fragments: column gq, elements 32 ks + 16 hf + 4 tq .. + 3
-      const int hq = PAIRED ? (gq & 3) : gq;
-      if (hq < G) {
-        const uint8_t* from = q_slot + (PAIRED && gq >= 4 ? G * D : 0) + hq * D + 4 * tq;
+      // fragments: column gq, elements 16 ks + 4 tq .. + 3
+      if (gq < G) {
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            qa[ks][hf] = *reinterpret_cast<const uint32_t*>(from + 32 * ks + 16 * hf);
-            if (!PAIRED) qb[ks][hf] = *reinterpret_cast<const uint32_t*>(from + G * D + 32 * ks + 16 * hf);
-          }
+        for (int ks = 0; ks < KS; ++ks) {
+          const uint2 f = *reinterpret_cast<const uint2*>(q_slot + (gq * D + 16 * ks + 4 * tq) * 2);
+          qa[ks][0] = f.x;
+          qa[ks][1] = f.y;
+        }
       }
       const float qscale = e8m0_to_f32(qc) * p.scale_log2;
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        qs[e] = __shfl_sync(0xffffffffu, qscale, (h0 + e) * LPH);
+        qs[e] = __shfl_sync(0xffffffffu, qscale, (2 * tq + e) * LPH);
         m_run[e] = -INFINITY;
         l_run[e] = 0.f;
       }
@@ -687,41 +671,16 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
         __syncwarp();
         if (lane == 0)
-          load_query<D, G, FUSED>(p, u + 1, q_slot, new_slots + ((n_units + 1) & 1) * (2 * D * 2), &q_bar[warp]);
+          load_query<D, G>(p, u + 1, q_slot, &q_bar[warp]);
       }
       e_cur = e_top = -1;
 #pragma unroll
-      for (int j = 0; j < MT; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+      for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
       ++n_units;
     }
 
     if (FUSED && new_row != 255) {
-      const uint32_t others = mk & ~(1u << new_row);
-      const bool first = (hw.z & 31) == 0;
-      const uint16_t* rows = reinterpret_cast<const uint16_t*>(new_slots + ((n_units - 1) & 1) * (2 * D * 2));
-      constexpr int E = D / 32;
-#pragma unroll 1
-      for (int v = 0; v < 2; ++v) {
-        const uint16_t* row = rows + v * D;
-        float x[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = bf16lo_to_f32(row[E * lane + e]);
-        if (v == 0 && p.rope) {  // elements c pair with c + d/2
-          const float sg = lane < 16 ? -1.f : 1.f;
-#pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const float2 cs = rope_tab[(E * lane + e) & (D / 2 - 1)];
-            x[e] = fmaf(x[e], cs.x, sg * bf16lo_to_f32(row[(E * lane + e) ^ (D / 2)]) * cs.y);
-          }
-        }
-        const long long uv = 2LL * u + v;
-        uint8_t* ring0 = p.ring_kv + (uv * p.W + hw.z - new_row) * D;
-        const int c = patch_block<D>(stage + v * S::kV, ring0, p.ring_scales + uv * p.ringS + (hw.z >> 5), x,
-                                     new_row, v ? vc : kc, first, others, lane);
-        if (v) vc = c;
-        else kc = c;
-      }
-      __syncwarp();
+      patch_block<D>(p, stage, u, new_row, hw.z, mk & ~(1u << new_row), fresh, rope_tab, kc, vc, lane);
       wrote_stage = true;
     }
 
@@ -739,149 +698,112 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       const uint32_t sK = smem_addr(stage);
       const uint32_t sV = smem_addr(stage + S::kV);
       // ---- S^T = K Q^T, two products of 16 keys ----
-      float sa[2][4], sb[2][4];
+      float sc[2][4];  // product t: keys 16 t + gq (0, 1), 16 t + 8 + (gq ^ 4) (2, 3); heads 2 tq, 2 tq + 1
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         // lanes 0-7 / 8-15 / 16-23 / 24-31: rows 0-7 / 8-15 / 0-7 / 8-15 of the product, at
-        // bytes 32 ks .. + 15 / same / 32 ks + 16 .. + 31 / same
-        const int key = 16 * t + ((lane & 7) ^ (4 * t)) + ((lane >> 3) & 1) * 8;
+        // bytes 32 kk .. + 15 / same / 32 kk + 16 .. + 31 / same
+        const int key = 16 * t + ((lane & 8) ? 8 + ((lane & 7) ^ 4) : lane & 7);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          uint32_t a0, a1, a2, a3;
-          ldsm_x4(sK + swz8<D>(key, 2 * ks + (lane >> 4)), a0, a1, a2, a3);
-          if (ks == 0) mma_e4m3_zero(sa[t], a0, a1, a2, a3, qa[ks][0], qa[ks][1]);
-          else mma_e4m3(sa[t], a0, a1, a2, a3, qa[ks][0], qa[ks][1]);
-          if (!PAIRED) {
-            if (ks == 0) mma_e4m3_zero(sb[t], a0, a1, a2, a3, qb[ks][0], qb[ks][1]);
-            else mma_e4m3(sb[t], a0, a1, a2, a3, qb[ks][0], qb[ks][1]);
-          }
-        }
-      }
-      // ---- the thread's scores, log2 domain: v[e][t], head h0 + e of row gq (tq < 2) or
-      // gq + 8 of product t; for G = 8, v[e][2 t + r] of row gq + 8 r ----
-      const float ks2 = e8m0_to_f32(kc);
-      float v[2][NV];
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float f = qs[e] * ks2;
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (PAIRED) {
-            // threads tq < 2 have the hi column of rows gq and gq + 8, threads tq + 2 the lo
-            // column: they exchange what the other needs and keep one row each
-            const float give = tq < 2 ? sa[t][2 + e] : sa[t][e];
-            const float keep = tq < 2 ? sa[t][e] : sa[t][2 + e];
-            const float got = __shfl_xor_sync(0xffffffffu, give, 2);
-            v[e][t] = (tq < 2 ? fmaf(got, 0.0625f, keep) : fmaf(keep, 0.0625f, got)) * f;
-          } else {
-            v[e][2 * t] = fmaf(sb[t][e], 0.0625f, sa[t][e]) * f;
-            v[e][2 * t + 1] = fmaf(sb[t][2 + e], 0.0625f, sa[t][2 + e]) * f;
-          }
+        for (int kk = 0; kk < KS / 2; ++kk) {
+          uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+          ldsm_x4(sK + swz8<D>(key, 2 * kk + (lane >> 4)), r0, r1, r2, r3);
+          codes_f16(r0, a0, a2);
+          codes_f16(r1, a1, a3);
+          if (kk == 0) mma_f16_zero(sc[t], a0, a1, a2, a3, qa[0][0], qa[0][1]);
+          else mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk][0], qa[2 * kk][1]);
+          codes_f16(r2, a0, a2);
+          codes_f16(r3, a1, a3);
+          mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk + 1][0], qa[2 * kk + 1][1]);
         }
       }
       if (mk != 0xFFFFFFFFu) {
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int r = 0; r < NV / 2; ++r) {
-            const int row = gq + 8 * (PAIRED ? tq >> 1 : r);
-            if (!((mk >> (16 * t + (row ^ (4 * t)))) & 1u))
-              v[0][t * (NV / 2) + r] = v[1][t * (NV / 2) + r] = -INFINITY;
-          }
+        for (int t = 0; t < 2; ++t) {
+          if (!((mk >> (16 * t + gq)) & 1u)) sc[t][0] = sc[t][1] = -INFINITY;
+          if (!((mk >> (16 * t + 8 + (gq ^ 4))) & 1u)) sc[t][2] = sc[t][3] = -INFINITY;
+        }
       }
-      // ---- online softmax ----
-      float mx[2];
+      // ---- online softmax, log2 domain: f sc (f > 0) ----
+      const float ks2 = e8m0_to_f32(kc);
+      // (not below fp32's normal numbers: 0 times a masked score is no score)
+      constexpr float kLeast = 1.17549435e-38f;
+      float f0 = qs[0] * ks2, f1 = qs[1] * ks2;
+      if (f0 < kLeast) f0 = kLeast;
+      if (f1 < kLeast) f1 = kLeast;
+      float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2]));
+      float mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        mx[e] = v[e][0];
-#pragma unroll
-        for (int n = 1; n < NV; ++n) mx[e] = fmaxf(mx[e], v[e][n]);
-#pragma unroll
-        for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
-          mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], off));
+      for (int off = 4; off < 32; off <<= 1) {
+        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
       }
+      mx0 *= f0;
+      mx1 *= f1;
       // The unit of O: at least 2^-64 of the largest block's, so that O stays far inside fp32.
       int e_new = e_cur;
       if (vc != 255) {
         e_top = max(e_top, vc);
         const int want = max(vc, e_top - 64);
-        if (want > e_cur || want + 4 < e_cur) e_new = want;
+        if (want > e_cur || want + 10 < e_cur) e_new = want;
       }
-      const bool up0 = mx[0] > m_run[0], up1 = mx[1] > m_run[1];
+      const bool up0 = mx0 > m_run[0], up1 = mx1 > m_run[1];
       if (__any_sync(0xffffffffu, up0 || up1 || e_new != e_cur)) {
         // (with e_cur = -1, before the first block, O is zero)
         const float fe = e_cur < 0 ? 1.f : recode_factor(e_cur, max(e_new, 0));
         e_cur = e_new;
-        const float alpha0 = up0 ? ex2(m_run[0] - mx[0]) : 1.f;
-        const float alpha1 = up1 ? ex2(m_run[1] - mx[1]) : 1.f;
-        if (up0) m_run[0] = mx[0];
-        if (up1) m_run[1] = mx[1];
+        const float alpha0 = up0 ? ex2(m_run[0] - mx0) : 1.f;
+        const float alpha1 = up1 ? ex2(m_run[1] - mx1) : 1.f;
+        if (up0) m_run[0] = mx0;
+        if (up1) m_run[1] = mx1;
         l_run[0] *= alpha0;
         l_run[1] *= alpha1;
-        const float f0 = alpha0 * fe, f1 = alpha1 * fe;
+        const float g0 = alpha0 * fe, g1 = alpha1 * fe;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
-          o[j][0] *= f0;
-          o[j][1] *= f1;
-          o[j][2] *= f0;
-          o[j][3] *= f1;
+        for (int j = 0; j < KS; ++j) {
+          o[j][0] *= g0;
+          o[j][1] *= g1;
+          o[j][2] *= g0;
+          o[j][3] *= g1;
         }
       }
-      // 256 times the probabilities; times V's power of two in O's unit
-      const float pv = vc == 255 ? e8m0_to_f32(255) : recode_factor(vc, e_cur);
-      float pr[2][NV];
+      // 2^15 times the probabilities, times V's power of two in O's unit, 2^(vc - e_cur) <= 1
+      const float dv = vc == 255 ? e8m0_to_f32(255) : static_cast<float>(vc - e_cur);
+      const float ref0 = (m_run[0] == -INFINITY ? 0.f : m_run[0]) - 15.f - dv;
+      const float ref1 = (m_run[1] == -INFINITY ? 0.f : m_run[1]) - 15.f - dv;
+      uint32_t pb[2][2];  // P^T as the B operand of k-step t: heads down, keys across
+      float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float ref = m_run[e] == -INFINITY ? 0.f : m_run[e] - 8.f;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int n = 0; n < NV; ++n) {
-          pr[e][n] = ex2(v[e][n] - ref);
-          l_run[e] += pr[e][n];
-          pr[e][n] *= pv;
+        for (int r = 0; r < 2; ++r) {
+          const float p0 = ex2(fmaf(sc[t][2 * r], f0, -ref0));
+          const float p1 = ex2(fmaf(sc[t][2 * r + 1], f1, -ref1));
+          sum0 += p0;
+          sum1 += p1;
+          pb[t][r] = movmatrix_trans(pack_f16(p0, p1));
         }
-      }
-      // ---- P^T as the B operand: 16-bit elements (key of product 0, key of product 1) ----
-      uint32_t b0, b1, b2, b3;
-      if (PAIRED) {
-        uint32_t hi0, lo0, hi1, lo1;
-        two_pieces(pr[0][0], pr[0][1], hi0, lo0);
-        two_pieces(pr[1][0], pr[1][1], hi1, lo1);
-        const uint32_t hi = hi0 | (hi1 << 16), lo = lo0 | (lo1 << 16);
-        // columns 0-3 hi, 4-7 lo; first the rows gq, then the rows gq + 8
-        const uint32_t got = __shfl_xor_sync(0xffffffffu, tq < 2 ? lo : hi, 2);
-        b0 = movmatrix_trans(tq < 2 ? hi : got);
-        b1 = movmatrix_trans(tq < 2 ? got : lo);
-        b2 = b3 = 0u;
-      } else {
-        uint32_t hi[2][2], lo[2][2];  // [head][row]
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-          for (int r = 0; r < 2; ++r) two_pieces(pr[e][r], pr[e][2 % NV + r], hi[e][r], lo[e][r]);
-        b0 = movmatrix_trans(hi[0][0] | (hi[1][0] << 16));
-        b1 = movmatrix_trans(hi[0][1] | (hi[1][1] << 16));
-        b2 = movmatrix_trans(lo[0][0] | (lo[1][0] << 16));
-        b3 = movmatrix_trans(lo[0][1] | (lo[1][1] << 16));
-      }
-      // ---- O^T += V^T P^T: lane's V row is k = lane of the product ----
+      const float back = ex2(-dv);
+      l_run[0] = fmaf(sum0, back, l_run[0]);
+      l_run[1] = fmaf(sum1, back, l_run[1]);
+      // ---- O^T += V^T P^T: lane's V row is k = lane of the two k-steps ----
       {
-        const int row = 2 * ((lane & 15) >> 2) + ((lane >> 1) & 1) + 8 * (lane >> 4);
-        const int key = ((lane & 1) ? 16 + (row ^ 4) : row);
+        const int a = lane & 15;
+        const int r = 2 * (a >> 2) + (a & 1);
+        const int key = (lane & 16) + ((a & 2) ? 8 + (r ^ 4) : r);
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          uint32_t a0, a1, a2, a3;
-          ldsm_b8_t(sV + swz8<D>(key, mt), a0, a1, a2, a3);
-          mma_e4m3(o[mt], a0, a1, a2, a3, b0, b1);
-          if (!PAIRED) {
-            float x[4];
-            mma_e4m3_zero(x, a0, a1, a2, a3, b2, b3);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[mt][e] = fmaf(x[e], 0.0625f, o[mt][e]);
-          }
+        for (int mt = 0; mt < KS; ++mt) {
+          uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+          ldsm_b8_t(sV + swz8<D>(key, mt), r0, r1, r2, r3);
+          codes_f16(r0, a0, a2);
+          codes_f16(r1, a1, a3);
+          mma_f16(o[mt], a0, a1, a2, a3, pb[0][0], pb[0][1]);
+          codes_f16(r2, a0, a2);
+          codes_f16(r3, a1, a3);
+          mma_f16(o[mt], a0, a1, a2, a3, pb[1][0], pb[1][1]);
         }
       }
     }
-
 
     if (ends) {
       // The unit's share of this run is done.  The warp sums its l over the lanes and leaves O in
@@ -891,7 +813,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
 #pragma unroll
-        for (int off = PAIRED ? 2 : 4; off < 32; off <<= 1)
+        for (int off = 4; off < 32; off <<= 1)
           l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
       __syncwarp();  // the warp is done with the stage
       const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
@@ -899,7 +821,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       for (int e = 0; e < 2; ++e) {
         float* col = ow + (2 * tq + e) * D;
 #pragma unroll
-        for (int j = 0; j < MT; ++j) {
+        for (int j = 0; j < KS; ++j) {
           col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
           col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
         }
@@ -968,7 +890,16 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     if (lane == 0) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
   }
   if (cm == 0) {
-    if (FUSED && !counted) count_reads();  // (after a timeout)
+    if (FUSED) {
+      if (!counted) count_reads(1);  // (after a timeout)
+      if (__shfl_sync(0xffffffffu, ticket, 0) + 1 == static_cast<unsigned long long>(gridDim.x) * kWarps) {
+        for (int b = lane; b < p.B; b += 32) {
+          const long long v = ld_pos(p, b);
+          if (v >= 0) p.pos[b] = v + 1;
+        }
+        if (lane == 0) p.tickets[0] = 0ull;
+      }
+    }
     // the merge kernel reads both records' first words
     if (lane == 0) {
       const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
@@ -989,14 +920,19 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     m_run[0] = m_run[1] = -INFINITY;
   }
   if (lane == 0) s_first[warp][0] = static_cast<int>(reinterpret_cast<uint8_t*>(left_in) - smem);
-  if (gq == 0 && (!PAIRED || tq < 2)) {
+  float* ml = reinterpret_cast<float*>(smem + S::kHdr);  // [warp][NST * 8]: 8 maxima, 8 sums
+  if (gq == 0) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      merge_m[warp * 8 + h0 + e] = m_run[e];
-      merge_l[warp * 8 + h0 + e] = l_run[e];
+      ml[warp * (NST * 8) + 2 * tq + e] = m_run[e];
+      ml[warp * (NST * 8) + 8 + 2 * tq + e] = l_run[e];
     }
   }
   __syncthreads();
+  if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
+    if (!w.sq.bad) p.pos[w.b] = w.sq.pos + 1;
+    p.tickets[w.b] = 0ull;
+  }
   const long long out_base = static_cast<long long>(su) * (G * D);
   constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
   float4 cacc[XPT];
@@ -1007,19 +943,19 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     if (x >= NGR) break;
     const int hh = (4 * x) / D;
     const int c = (4 * x) % D;
-    float M = merge_m[hh];
+    float M = ml[hh];
 #pragma unroll
-    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, merge_m[v * 8 + hh]);
+    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * (NST * 8) + hh]);
     const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float Ls = 0.f;
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) {
-      const float f = ex2(merge_m[v * 8 + hh] - Mr);
+      const float f = ex2(ml[v * (NST * 8) + hh] - Mr);
       const float4 y = taken(reinterpret_cast<const float*>(smem + s_first[v][0]), hh, c);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
       acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-      Ls = fmaf(f, merge_l[v * 8 + hh], Ls);
+      Ls = fmaf(f, ml[v * (NST * 8) + 8 + hh], Ls);
     }
     if (cm == 1) {
       const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
@@ -1055,18 +991,18 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   for (int x = x0 + tid; x < x1; x += kThreads) {
     const int hh = (4 * x) / D;
     const int c = (4 * x) % D;
-    const float2* ml = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
+    const float2* pl = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
     float M = -INFINITY;
 #pragma unroll
     for (int r = 0; r < kMaxClusterCtas; ++r)
-      if (r < cm) M = fmaxf(M, ml[r * G].x);
+      if (r < cm) M = fmaxf(M, pl[r * G].x);
     if (M == -INFINITY) M = 0.f;
     float Ls = 0.f;
     float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int r = 0; r < kMaxClusterCtas; ++r) {
       if (r < cm) {
-        const float2 mr = ml[r * G];
+        const float2 mr = pl[r * G];
         const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
         const float f = ex2(mr.x - M);
         Ls = fmaf(f, mr.y, Ls);
@@ -1177,8 +1113,9 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
     const long long most = (nb + kWarps - 1) / kWarps;  // a block for every warp
     if (m > most) m = most;
     if (m > kMaxClusterCtas) m = kMaxClusterCtas;
-    if (m < 1) m = 1;
-    pl->cm = static_cast<int>(m);
+    // (a power of two: others may not fit the GPU's groups of SMs as often as slots / m)
+    pl->cm = m >= 8 ? 8 : m >= 4 ? 4 : m >= 2 ? 2 : 1;
+    m = pl->cm;
     pl->ctas = static_cast<int>(units * m);
   } else {
     pl->cm = 0;

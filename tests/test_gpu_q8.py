@@ -286,10 +286,10 @@ ATTN = [  # B, L, Hq, Hkv, d, k, W, pos
 
 ATTN += [  # more units than resident CTAs: whole ones, cut ones, runs over many sequences
     (200, 1, 8, 4, 128, 30, 130, [(7 * i) % 150 for i in range(200)]),
-    (20, 16, 8, 2, 64, 0, 40, [3 * i - 5 for i in range(20)]),
+    (20, 16, 8, 4, 64, 0, 40, [3 * i - 5 for i in range(20)]),
     (700, 1, 1, 1, 64, 0, 33, [(i * 37) % 60 - 3 for i in range(700)]),
     (45, 1, 64, 8, 128, 70, 500, [(i * 131) % 700 for i in range(45)]),
-    (170, 1, 8, 1, 64, 3, 300, [(i * 17) % 400 for i in range(170)]),
+    (500, 1, 8, 1, 64, 3, 300, [(i * 17) % 400 for i in range(500)]),
 ]
 
 
@@ -579,8 +579,8 @@ def test_plan(cuda_device):
         return cmc.decode_attn_q8_plan(cmc.CmcDims(B, L, 4 * H, H, 128, max(k, 1), k, W))
     assert plan(1, 1, 2, 32, 128) == (4, 1)        # five blocks a unit, a cluster of two
     assert plan(1, 32, 8, 128, 512) == (256, 1)    # one CTA a unit
-    ctas, launches = plan(41, 1, 8, 128, 512)      # 328 units on fewer CTAs
-    assert ctas <= 320 and launches == 2
+    ctas, launches = plan(61, 1, 8, 128, 512)      # 488 units on fewer CTAs
+    assert ctas <= 480 and launches == 2
     assert plan(64, 32, 8, 128, 512) == (ctas, 2)
 
 
