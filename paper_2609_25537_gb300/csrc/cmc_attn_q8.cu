@@ -57,6 +57,10 @@ constexpr int kQ8RecHead = 4;  // words before a record's maxima: valid, ends
 // Units up to which a call never takes the flat plan (and its workspace holds no records).
 constexpr int kQ8StridedUnits = 128;
 
+// Heads of units kept per warp: blocks are requested up to six ahead, but of short units'
+// (one block each) no more than that many begin between a request and its use.
+constexpr int kQ8Heads = 8;
+
 struct Q8Maps {
   CUtensorMap t1, ring;  // [2 units, T, d] bytes, box 2 x 32 rows
 };
@@ -70,33 +74,26 @@ struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the spl
   int rope;                   // rotate q and the new key (fused step)
 };                            // cm: CTAs per unit (strided plan), 0: flat plan
 
-// Shared memory of a CTA: per warp a query slot, a rotary table and the headers of its
-// stages (in the end the warp's maxima and sums); what a cluster's peers send; then,
-// 1,024-byte aligned, the stages.
+// Shared memory of a CTA: per warp a query slot, a rotary table, the stages' powers of two
+// and the heads of the units under way (in the end the warp's maxima and sums); what a
+// cluster's peers send; then, 1,024-byte aligned, the stages.
 template <int D, int G>
 struct Q8Smem {
-  // 64 KB of stages a CTA and three CTAs an SM (at d = 128 and G = 8: 96 KB, two an SM).
-#ifndef Q8NST
-#define Q8NST 3
-#endif
-  static constexpr int NST = D == 64 ? 2 * Q8NST : G == 8 ? 3 : Q8NST;
+  // 96 KB of stages a CTA, two CTAs an SM (at d = 128 and G = 8 that just fits).  With 64 KB and
+  // three CTAs, two blocks a warp, 64 x (256 + 2,048) keys took 73 us instead of 56.
+  static constexpr int NST = D == 64 ? 6 : 3;
   static constexpr int kV = kQ8Block * D;
   static constexpr int kStage = 2 * kQ8Block * D;
   static constexpr int kQ = 0;                                // [warp][G][D] bf16
   static constexpr int kRope = kQ + kWarps * G * D * 2;       // [warp][d/2] (cos, sin)
-  static constexpr int kHdr = kRope + kWarps * D * 4;         // [warp][NST][8] words
-  static constexpr int kRecv = kHdr + kWarps * NST * 32;      // groups of 16 bytes, rank by rank
+  static constexpr int kScale = kRope + kWarps * D * 4;       // [warp][NST][2] words
+  static constexpr int kHead = kScale + kWarps * NST * 8;     // [warp][kHeads][8] words
+  static constexpr int kRecv = kHead + kWarps * kQ8Heads * 32;  // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
   static constexpr int kSmall = kRecvMl + kMaxClusterCtas * G * 8;
   static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
-  static_assert(NST >= 2, "a warp's headers hold its 8 maxima and 8 sums");
+  static_assert(kHead % 16 == 0 && kRecv % 16 == 0, "read by 16 bytes");
 };
-// Header words of a stage: what the warp has to know of the block in it.
-enum { Q_WHAT = 0, Q_UNIT = 1, Q_SLOT = 2, Q_LEFT = 3, Q_KS = 4, Q_VS = 5, Q_POS = 6 };
-// Q_WHAT: rows that hold a key (0 .. 32) | the new token's row (255: none) << 8 |
-// the block's byte in the words of powers of two << 16 | flags << 24
-enum { QF_FIRST = 1, QF_LAST = 2 };  // the unit's first / last block
-
 // Offset of 16-byte chunk c of row r of a stage's K or V: TMA's 128-byte swizzle, or the
 // 64-byte one for rows of 64 codes.
 template <int D>
@@ -164,44 +161,13 @@ __device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState
   return n > 0 ? n : 1;
 }
 
-// Requests block j of unit u: the codes by TMA, the two words that hold its powers of
-// two by lanes 0 and 1.  Called by the whole warp, converged.
-template <int D>
-__device__ __forceinline__ void load_block(const AttnQ8Params& p, const Q8Maps& maps, int u, int j,
-                                           uint8_t* stage, uint8_t* hdr, uint64_t* full, int lane) {
-  const bool t1 = j < p.nb1;
-  const int jj = t1 ? j : j - p.nb1;
-  if (lane < 2) {
-    const int S = t1 ? p.t1S : p.ringS;
-    const uint8_t* from = (t1 ? p.t1_scales : p.ring_scales) + (2LL * u + lane) * S + (jj & ~3);
-    cp_async_4(smem_addr(hdr + 4 * (Q_KS + lane)), from, 4u);
-    mbar_arrive_cp_async(full);
-  }
-  __syncwarp();
-  if (lane == 0) {
-    mbar_arrive_expect_tx(full, 2 * kQ8Block * D + p.stall_tx);
-    tma_box3_hint(smem_addr(stage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * u, full,
-                  policy_evict_first());
-  }
-}
-
-// The header of block j of unit u; `left`: blocks of the unit from here on in the warp's run.
-template <bool FUSED>
-__device__ __forceinline__ void write_header(const AttnQ8Params& p, uint8_t* hdr, int u, int j, int nb,
-                                             int left, const SeqState& sq) {
-  int n, new_row = 255;
-  if (j < p.nb1) {
-    n = sq.bad ? 0 : min(p.k - j * kQ8Block, kQ8Block);
-  } else {
-    const int r0 = (j - p.nb1) * kQ8Block;
-    n = min(max(sq.count - r0, 0), kQ8Block);
-    if (FUSED && sq.new_slot >= r0 && sq.new_slot - r0 < n) new_row = sq.new_slot - r0;
-  }
-  const int flags = (j == 0 ? QF_FIRST : 0) | (j == nb - 1 ? QF_LAST : 0);
-  const int sel = (j < p.nb1 ? j : j - p.nb1) & 3;
-  *reinterpret_cast<int4*>(hdr) = make_int4(n | (new_row << 8) | (sel << 16) | (flags << 24), u, sq.new_slot, left);
-  *reinterpret_cast<long long*>(hdr + 4 * Q_POS) = sq.pos;
-}
+// What a warp has to know of a unit (or its part of it) besides the blocks.
+struct UnitHead {
+  int u, j0, nb, left;  // unit, first block, the unit's live blocks, blocks of this part
+  int count, new_slot;  // live ring slots, the new token's
+  long long pos;
+};
+static_assert(sizeof(UnitHead) == 32, "two 16-byte words");
 
 // A unit's query rows into the warp's slot.
 template <int D, int G>
@@ -332,15 +298,8 @@ __device__ __forceinline__ void load_row(const uint8_t* from, float (&x)[N]) {
   }
 }
 
-// One warp's place in the flat plan's list of live blocks.
-struct FlatWalk {
-  int u, j, nb;   // unit, block, the unit's blocks
-  int b, x;       // sequence, unit within it
-  SeqState sq;
-};
-
 template <int D, int G, bool FUSED>
-__global__ void __maxnreg__(168)
+__global__ void __maxnreg__(200)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   using S = Q8Smem<D, G>;
   constexpr int NST = S::NST;
@@ -358,7 +317,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   const int warp = tid >> 5;
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem + S::kSmall) + 1023) & ~uintptr_t(1023)) +
                     warp * (NST * S::kStage);
-  uint8_t* hdrs = smem + S::kHdr + warp * (NST * 32);
+  uint8_t* scale_words = smem + S::kScale + warp * (NST * 8);
+  UnitHead* heads = reinterpret_cast<UnitHead*>(smem + S::kHead) + warp * kQ8Heads;
   uint8_t* q_slot = smem + S::kQ + warp * (G * D * 2);
   float2* rope_tab = reinterpret_cast<float2*>(smem + S::kRope + warp * (D * 4));
   uint64_t* full = full_bar[warp];
@@ -404,50 +364,31 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
-  int n_run = 0;       // blocks of the warp's run
-  int issued = 0;      // of them requested
-  FlatWalk w;          // the next block to request
-  w.u = su;
-  w.j = g0;
-  w.nb = 0;
-  w.b = 0;
-  w.x = 0;
-  long long pos_next = 0;  // flat plan: pos of the next sequence, ahead of its use
-  int last_b = 0;          // the run's last sequence
-  bool counted = false;    // this warp's reading of pos is done and counted
+  int n_run = 0;          // blocks of the warp's run
+  int issued = 0;         // of them requested
+  int u = su, jn = g0;    // unit and block of the next request
+  int nb = 0;             // flat plan: live blocks of a unit of the sequence,
+  int b = 0, x = 0;       // the sequence, the unit within it,
+  int last_b = 0;         // the run's last sequence,
+  long long pos_next = 0; // pos of the next sequence, ahead of its use,
+  bool unit_new = false;  // whether the next request is the unit's first in this run,
+  int units_asked = 0;    // units begun to be requested
+  SeqState sq;
+  bool counted = false;   // this warp's reading of pos is done and counted
   unsigned long long ticket = 0;  // and how many were before it
   uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows of the present unit
   if (cm > 0) {
-    // ---- strided: the first blocks at once, then pos ----
-    if (lane == 0 && g0 < nb_all) load_query<D, G>(p, su, q_slot, &q_bar[warp]);
-    for (; issued < NST && g0 + issued * step < nb_all; ++issued)
-      load_block<D>(p, maps, su, g0 + issued * step, stages + issued * S::kStage, hdrs + issued * 32, &full[issued],
-                    lane);
+    if (g0 < nb_all) n_run = (nb_all - g0 + step - 1) / step;  // as far as known before pos
     if (FUSED) fresh = load_new<D>(p, su, lane);
-    w.b = static_cast<int>(static_cast<unsigned>(su) / static_cast<unsigned>(p.LH));
-    if (tid == 0) s_pos[0] = ld_pos(p, w.b);
-    __syncthreads();
-    w.sq = seq_state<FUSED>(p, s_pos[0]);
-    if (tid == 0) {
-      if (w.sq.bad && rank == 0 && su % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-      // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
-      if (FUSED) ticket = atomicAdd(p.tickets + w.b, 1ull);
-    }
-    w.nb = live_blocks(p, w.sq);
-    n_run = w.nb > g0 ? (w.nb - g0 + step - 1) / step : 0;
-    w.j = g0 + issued * step;
-    if (n_run < issued) n_run = issued;  // blocks that were requested in vain hold no key
-    if (lane == 0)
-      for (int i = 0; i < issued; ++i)
-        write_header<FUSED>(p, hdrs + i * 32, su, g0 + i * step, 0, n_run - i, w.sq);
   } else {
     // ---- flat: the runs from all of pos ----
     const int chunk = (p.B + kThreads - 1) / kThreads;
-    const int b0 = tid * chunk, b1 = min(b0 + chunk, p.B);
+    const int b0 = min(tid * chunk, p.B), b1 = min(b0 + chunk, p.B);
     int sum = 0;
     long long pos_b = 0;  // of sequence b1 - 1
-    for (int b = b0; b < b1; ++b) {
-      pos_b = ld_pos(p, b);
+#pragma unroll 1
+    for (int q = b0; q < b1; ++q) {
+      pos_b = ld_pos(p, q);
       const SeqState sq = seq_state<FUSED>(p, pos_b);
       if (sq.bad && blockIdx.x == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
       sum += live_blocks(p, sq);
@@ -469,6 +410,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     const unsigned total = static_cast<unsigned>(all) * static_cast<unsigned>(p.LH);
     const unsigned nw = gridDim.x * kWarps;
     const unsigned base = total / nw, rem = total - base * nw;
+#pragma unroll 1
     for (int v = 0; v < kWarps; ++v) {
       const unsigned wid = blockIdx.x * kWarps + v;
       const unsigned a = wid * base + min(wid, rem), n = base + (wid < rem ? 1u : 0u);
@@ -481,14 +423,15 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         const unsigned at = e ? a + n - 1 : a;
         if (at < lo || at >= hi) continue;
         unsigned from = lo;
-        for (int b = b0; b < b1; ++b) {
-          const long long pb = chunk == 1 ? pos_b : ld_pos(p, b);
+#pragma unroll 1
+        for (int q = b0; q < b1; ++q) {
+          const long long pb = chunk == 1 ? pos_b : ld_pos(p, q);
           const unsigned len = static_cast<unsigned>(live_blocks(p, seq_state<FUSED>(p, pb))) * p.LH;
           if (at < from + len) {
             if (e) {
-              s_last[v] = b;
+              s_last[v] = q;
             } else {
-              s_first[v][0] = b;
+              s_first[v][0] = q;
               s_first[v][1] = static_cast<int>(at - from);
               s_pos[v] = pb;
             }
@@ -500,56 +443,98 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     }
     __syncthreads();
     if (n_run > 0) {
-      w.b = s_first[warp][0];
+      b = s_first[warp][0];
       last_b = s_last[warp];
-      w.sq = seq_state<FUSED>(p, s_pos[warp]);
-      w.nb = live_blocks(p, w.sq);
+      sq = seq_state<FUSED>(p, s_pos[warp]);
+      nb = live_blocks(p, sq);
       const int off = s_first[warp][1];
-      w.x = off / w.nb;
-      w.j = off - w.x * w.nb;
-      w.u = w.b * p.LH + w.x;
-      if (lane == 0) load_query<D, G>(p, w.u, q_slot, &q_bar[warp]);
-      if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
+      x = off / nb;
+      jn = off - x * nb;
+      u = b * p.LH + x;
+      unit_new = true;
+      if (b < last_b) pos_next = ld_pos(p, b + 1);
     }
   }
   // Flat plan: counts that this warp has read pos of all its sequences; the last one to be counted
   // advances every pos, when its run is done (the count takes a trip to L2).  `nb` comes of
   // the last pos, and makes the count wait for it.
-  auto count_reads = [&](int nb) {
+  auto count_reads = [&]() {
     counted = true;
     if (lane == 0) {
       int seen;
       asm volatile("mov.b32 %0, %1;\n" : "=r"(seen) : "r"(nb));
-      ticket = atomicAdd(p.tickets, seen > 0 ? 1ull : 0ull);
+      ticket = atomicAdd(p.tickets, seen >= 0 ? 1ull : 0ull);
     }
   };
-  // Requests the run's next block into stage s, with its header.
-  auto request = [&](int s) {
-    load_block<D>(p, maps, w.u, w.j, stages + s * S::kStage, hdrs + s * 32, &full[s], lane);
-    if (lane == 0)
-      write_header<FUSED>(p, hdrs + s * 32, w.u, w.j, cm > 0 ? 0 : w.nb,
-                          cm > 0 ? n_run - issued : min(w.nb - w.j, n_run - issued), w.sq);
-    ++issued;
-    if (cm > 0) {
-      w.j += step;
-      return;
+  // The unit's powers of two: the rows of lane 0 (K) and lane 1 (V).
+  const uint8_t* t1_s = p.t1_scales + (2LL * u + (lane & 1)) * p.t1S;
+  const uint8_t* ring_s = p.ring_scales + (2LL * u + (lane & 1)) * p.ringS;
+  auto put_head = [&](int left) {
+    if (lane == 0) {
+      UnitHead* h = heads + (units_asked & (kQ8Heads - 1));
+      *reinterpret_cast<int4*>(h) = make_int4(u, cm > 0 ? g0 : jn, nb, left);
+      h->count = sq.count;
+      h->new_slot = sq.new_slot;
+      h->pos = sq.pos;
     }
-    if (++w.j == w.nb) {
-      w.j = 0;
-      ++w.u;
-      if (++w.x == p.LH && w.b < last_b) {
-        w.x = 0;
-        ++w.b;
-        w.sq = seq_state<FUSED>(p, pos_next);
-        w.nb = live_blocks(p, w.sq);
-        if (w.b < last_b) pos_next = ld_pos(p, w.b + 1);
+    ++units_asked;
+  };
+  // Requests the run's next block into stage s: the codes by TMA, the two words that hold its
+  // powers of two by lanes 0 and 1.  Called by the whole warp, converged.
+  auto request = [&](int s) {
+    if (unit_new) {
+      put_head(min(nb - jn, n_run - issued));
+      unit_new = false;
+    }
+    const bool t1 = jn < p.nb1;
+    const int jj = t1 ? jn : jn - p.nb1;
+    if (lane < 2) {
+      cp_async_4(smem_addr(scale_words + s * 8 + 4 * lane), (t1 ? t1_s : ring_s) + (jj & ~3), 4u);
+      mbar_arrive_cp_async(&full[s]);
+    }
+    __syncwarp();
+    if (lane == 0) {
+      mbar_arrive_expect_tx(&full[s], S::kStage + p.stall_tx);
+      tma_box3_hint(smem_addr(stages + s * S::kStage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * u, &full[s],
+                    policy_evict_first());
+    }
+    ++issued;
+    jn += cm > 0 ? step : 1;
+    if (cm == 0 && jn == nb) {
+      jn = 0;
+      ++u;
+      t1_s += 2 * p.t1S;
+      ring_s += 2 * p.ringS;
+      unit_new = true;
+      if (++x == p.LH && b < last_b) {
+        x = 0;
+        ++b;
+        sq = seq_state<FUSED>(p, pos_next);
+        nb = live_blocks(p, sq);
+        if (b < last_b) pos_next = ld_pos(p, b + 1);
+        else if (FUSED) count_reads();
       }
     }
-    if (FUSED && !counted && w.b == last_b) count_reads(w.nb);
   };
-  if (cm == 0) {
-    if (FUSED && (n_run == 0 || w.b == last_b)) count_reads(n_run == 0 ? 1 : w.nb);
-    while (issued < NST && issued < n_run) request(issued);
+  if (lane == 0 && n_run > 0) load_query<D, G>(p, u, q_slot, &q_bar[warp]);
+  if (FUSED && cm == 0 && b == last_b) count_reads();
+#pragma unroll 1
+  for (int s = 0; s < NST && s < n_run; ++s) request(s);
+  if (cm > 0) {
+    // ---- strided: the first blocks are on their way; now pos ----
+    b = static_cast<int>(static_cast<unsigned>(su) / static_cast<unsigned>(p.LH));
+    if (tid == 0) s_pos[0] = ld_pos(p, b);
+    __syncthreads();
+    sq = seq_state<FUSED>(p, s_pos[0]);
+    if (tid == 0) {
+      if (sq.bad && rank == 0 && su % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+      // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
+      if (FUSED) ticket = atomicAdd(p.tickets + b, 1ull);
+    }
+    nb = live_blocks(p, sq);
+    n_run = nb > g0 ? (nb - g0 + step - 1) / step : 0;
+    if (n_run < issued) n_run = issued;  // blocks that were requested in vain hold no key
+    put_head(n_run);
   }
   __syncwarp();
 
@@ -558,6 +543,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   const int gq = lane >> 2;
   const int tq = lane & 3;
   int n_units = 0;                             // units begun
+  int cu = 0, j = 0, last_j = 0, left = 0;     // the unit, its block, its last one, blocks left of the part
+  int count = 0, new_slot = -1;                // of its sequence
+  long long pos = 0;
   bool begun_first = false;                    // the present one with its first block
   bool head = false, tail = false;             // flat plan: records written
   long long rope_pos = -1;                     // position that the rotary table is for
@@ -581,29 +569,41 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   uint32_t phase = 0;    // its parity
   for (int i = 0; i < n_run; ++i) {
     uint8_t* stage = stages + s * S::kStage;
-    const uint8_t* hdr = hdrs + s * 32;
     if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {
       gave_up = true;
       break;
     }
-    const int4 hw = *reinterpret_cast<const int4*>(hdr);
-    const int nk = hw.x & 255, new_row = (hw.x >> 8) & 255, sel = (hw.x >> 16) & 255, flags = hw.x >> 24;
-    const int u = hw.y;
-    int kc = hdr[4 * Q_KS + sel], vc = hdr[4 * Q_VS + sel];
-    const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;  // bit r: row r holds a key
-    const bool starts = cm > 0 ? i == 0 : (i == 0 || (flags & QF_FIRST));
-    const bool ends = hw.w == 1;  // the unit's last block in this run
-    bool wrote_stage = false;     // generic-proxy writes into the stage
+    const bool starts = left == 0;
+    if (starts) {
+      const UnitHead* h = heads + (n_units & (kQ8Heads - 1));
+      const int4 a = *reinterpret_cast<const int4*>(h);
+      cu = a.x;
+      j = a.y;
+      last_j = a.z - 1;
+      left = a.w;
+      count = h->count;
+      new_slot = h->new_slot;
+      pos = h->pos;
+    }
+    // the block: its rows that hold a key (bit r of mk), its bytes, the new token's row
+    const bool t1 = j < p.nb1;
+    const int jj = t1 ? j : j - p.nb1;
+    const int live = t1 ? (pos < 0 ? 0 : p.k) : count;
+    const int nk = min(max(live - jj * kQ8Block, 0), kQ8Block);
+    const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;
+    int kc = scale_words[s * 8 + (jj & 3)], vc = scale_words[s * 8 + 4 + (jj & 3)];
+    const bool patched = FUSED && !t1 && new_slot >= 0 && new_slot / kQ8Block == jj;
+    const bool ends = left == 1;
+    bool wrote_stage = false;  // generic-proxy writes into the stage
 
     if (starts) {
       if (__any_sync(0xffffffffu, !mbar_wait(&q_bar[warp], static_cast<uint32_t>(n_units & 1)))) {
         gave_up = true;
         break;
       }
-      begun_first = flags & QF_FIRST;
-      if (FUSED && cm == 0) fresh = load_new<D>(p, u, lane);
+      begun_first = j == 0;
+      if (FUSED && cm == 0) fresh = load_new<D>(p, cu, lane);
       if (FUSED && p.rope) {
-        const long long pos = *reinterpret_cast<const long long*>(hdr + 4 * Q_POS);
         if (pos >= 0 && pos != rope_pos) {
           rope_pos = pos;
           float2 cs[2];
@@ -667,11 +667,11 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         l_run[e] = 0.f;
       }
       // the next unit's rows into the slot, where the run goes on behind this unit
-      if (cm == 0 && i + hw.w < n_run) {
+      if (cm == 0 && i + left < n_run) {
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
         __syncwarp();
         if (lane == 0)
-          load_query<D, G>(p, u + 1, q_slot, &q_bar[warp]);
+          load_query<D, G>(p, cu + 1, q_slot, &q_bar[warp]);
       }
       e_cur = e_top = -1;
 #pragma unroll
@@ -679,8 +679,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       ++n_units;
     }
 
-    if (FUSED && new_row != 255) {
-      patch_block<D>(p, stage, u, new_row, hw.z, mk & ~(1u << new_row), fresh, rope_tab, kc, vc, lane);
+    if (patched) {
+      const int r = new_slot & (kQ8Block - 1);
+      patch_block<D>(p, stage, cu, r, new_slot, mk & ~(1u << r), fresh, rope_tab, kc, vc, lane);
       wrote_stage = true;
     }
 
@@ -698,7 +699,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       const uint32_t sK = smem_addr(stage);
       const uint32_t sV = smem_addr(stage + S::kV);
       // ---- S^T = K Q^T, two products of 16 keys ----
-      float sc[2][4];  // product t: keys 16 t + gq (0, 1), 16 t + 8 + (gq ^ 4) (2, 3); heads 2 tq, 2 tq + 1
+      // (two accumulator chains a product)
+      float sc[2][4], sd[2][4];  // product t: keys 16 t + gq (0, 1), 16 t + 8 + (gq ^ 4) (2, 3); heads 2 tq, 2 tq + 1
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         // lanes 0-7 / 8-15 / 16-23 / 24-31: rows 0-7 / 8-15 / 0-7 / 8-15 of the product, at
@@ -714,8 +716,11 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
           else mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk][0], qa[2 * kk][1]);
           codes_f16(r2, a0, a2);
           codes_f16(r3, a1, a3);
-          mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk + 1][0], qa[2 * kk + 1][1]);
+          if (kk == 0) mma_f16_zero(sd[t], a0, a1, a2, a3, qa[1][0], qa[1][1]);
+          else mma_f16(sd[t], a0, a1, a2, a3, qa[2 * kk + 1][0], qa[2 * kk + 1][1]);
         }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[t][e] += sd[t][e];
       }
       if (mk != 0xFFFFFFFFu) {
 #pragma unroll
@@ -816,14 +821,16 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         for (int off = 4; off < 32; off <<= 1)
           l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
       __syncwarp();  // the warp is done with the stage
+      const bool whole = cm == 0 && begun_first && j == last_j;  // normalised too
       const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
+        const float f = !whole ? fo : l_run[e] > 0.f ? __fdividef(fo, l_run[e]) : 0.f;
         float* col = ow + (2 * tq + e) * D;
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * fo;
-          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * fo;
+          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
+          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
         }
       }
       if (cm > 0) {
@@ -834,41 +841,30 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       // run's if the unit began before it).
       __syncwarp();
       wrote_stage = true;
-      const bool whole = begun_first && (flags & QF_LAST);
-      float* rec = nullptr;
-      if (!whole) {
+      if (whole) {
+        uint16_t* out = p.out + static_cast<long long>(cu) * (G * D);
+        for (int x = lane; x < NGR; x += 32) {
+          const float4 y = taken(ow, (4 * x) / D, (4 * x) % D);
+          *reinterpret_cast<uint2*>(out + 4 * x) = make_uint2(pack_bf16_rn(y.x, y.y), pack_bf16_rn(y.z, y.w));
+        }
+      } else {
         const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
-        rec = p.partials + (2 * wid + (begun_first ? 1 : 0)) * (kQ8RecHead + rec_floats(G, D));
-        if (lane == 0) *reinterpret_cast<int2*>(rec) = make_int2(1, flags & QF_LAST ? 1 : 0);
+        float* rec = p.partials + (2 * wid + (begun_first ? 1 : 0)) * (kQ8RecHead + rec_floats(G, D));
         if (begun_first) tail = true;
         else head = true;
+        if (lane == 0) *reinterpret_cast<int4*>(rec) = make_int4(1, j == last_j ? 1 : 0, cu, 0);
         rec += kQ8RecHead;
-      }
+        if (gq == 0) {
 #pragma unroll
-      for (int xi = 0; xi < (NGR + 31) / 32; ++xi) {
-        const int x = lane + 32 * xi;
-        const int hh = x < NGR ? (4 * x) / D : 0;
-        const int c = (4 * x) % D;
-        const float l0 = __shfl_sync(0xffffffffu, l_run[0], hh >> 1), l1 = __shfl_sync(0xffffffffu, l_run[1], hh >> 1);
-        const float m0 = __shfl_sync(0xffffffffu, m_run[0], hh >> 1), m1 = __shfl_sync(0xffffffffu, m_run[1], hh >> 1);
-        const float l = hh & 1 ? l1 : l0, m = hh & 1 ? m1 : m0;
-        if (x < NGR) {
-          const float4 y = taken(ow, hh, c);
-          if (whole) {
-            const float inv = l > 0.f ? __fdividef(1.f, l) : 0.f;
-            *reinterpret_cast<uint2*>(p.out + static_cast<long long>(u) * (G * D) + hh * D + c) =
-                make_uint2(pack_bf16_rn(y.x * inv, y.y * inv), pack_bf16_rn(y.z * inv, y.w * inv));
-          } else {
-            if (c == 0) {
-              rec[hh] = m;
-              rec[G + hh] = l;
+          for (int e = 0; e < 2; ++e)
+            if (2 * tq + e < G) {
+              rec[2 * tq + e] = m_run[e];
+              rec[G + 2 * tq + e] = l_run[e];
             }
-            *reinterpret_cast<float4*>(rec + rec_out_offset(G) + hh * D + c) = y;
-          }
         }
+        for (int x = lane; x < NGR; x += 32)
+          *reinterpret_cast<float4*>(rec + rec_out_offset(G) + 4 * x) = taken(ow, (4 * x) / D, (4 * x) % D);
       }
-      if (!whole && lane == 0 && begun_first)  // which unit it is
-        reinterpret_cast<int*>(rec - kQ8RecHead)[2] = u;
     }
     if (wrote_stage) {
       // generic-proxy writes to this stage are ordered before the next box into it
@@ -876,6 +872,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     }
     __syncwarp();
     if (issued < n_run) request(s);
+    --left;
+    j += cm > 0 ? step : 1;
     if (++s == NST) {
       s = 0;
       phase ^= 1u;
@@ -891,7 +889,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   }
   if (cm == 0) {
     if (FUSED) {
-      if (!counted) count_reads(1);  // (after a timeout)
+      if (!counted) count_reads();  // (after a timeout)
       if (__shfl_sync(0xffffffffu, ticket, 0) + 1 == static_cast<unsigned long long>(gridDim.x) * kWarps) {
         for (int b = lane; b < p.B; b += 32) {
           const long long v = ld_pos(p, b);
@@ -920,18 +918,19 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     m_run[0] = m_run[1] = -INFINITY;
   }
   if (lane == 0) s_first[warp][0] = static_cast<int>(reinterpret_cast<uint8_t*>(left_in) - smem);
-  float* ml = reinterpret_cast<float*>(smem + S::kHdr);  // [warp][NST * 8]: 8 maxima, 8 sums
+  constexpr int kMl = kQ8Heads * 8;
+  float* ml = reinterpret_cast<float*>(smem + S::kHead);  // over each warp's heads: 8 maxima, 8 sums
   if (gq == 0) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      ml[warp * (NST * 8) + 2 * tq + e] = m_run[e];
-      ml[warp * (NST * 8) + 8 + 2 * tq + e] = l_run[e];
+      ml[warp * kMl + 2 * tq + e] = m_run[e];
+      ml[warp * kMl + 8 + 2 * tq + e] = l_run[e];
     }
   }
   __syncthreads();
   if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
-    if (!w.sq.bad) p.pos[w.b] = w.sq.pos + 1;
-    p.tickets[w.b] = 0ull;
+    if (!sq.bad) p.pos[b] = sq.pos + 1;
+    p.tickets[b] = 0ull;
   }
   const long long out_base = static_cast<long long>(su) * (G * D);
   constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
@@ -945,17 +944,17 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     const int c = (4 * x) % D;
     float M = ml[hh];
 #pragma unroll
-    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * (NST * 8) + hh]);
+    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * kMl + hh]);
     const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float Ls = 0.f;
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) {
-      const float f = ex2(ml[v * (NST * 8) + hh] - Mr);
+      const float f = ex2(ml[v * kMl + hh] - Mr);
       const float4 y = taken(reinterpret_cast<const float*>(smem + s_first[v][0]), hh, c);
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
       acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-      Ls = fmaf(f, ml[v * (NST * 8) + 8 + hh], Ls);
+      Ls = fmaf(f, ml[v * kMl + 8 + hh], Ls);
     }
     if (cm == 1) {
       const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
