@@ -521,12 +521,11 @@ CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos,
                                  const void* v_new, const cmc_dims* dims, void* stream);
 
 /* Bytes of workspace cmc_two_tier_decode_attn_q8 and cmc_decode_step_q8 need for
- * `dims`: the device status word (read by cmc_read_status), one 8-byte counter
- * per sequence, and, above 128 (sequence, layer, KV head) units, fp32 partial
- * results.  Zero-fill it once before its first use, and again after a call
+ * `dims`: the device status word (read by cmc_read_status) and one 8-byte counter per
+ * sequence.  Zero-fill it once before its first use, and again after a call
  * that raised CMC_DEVFLAG_TIMEOUT; every other call leaves the counters at zero.
- * It depends on B, Hq / Hkv, d and on whether there are more than 128 units:
- * one workspace serves every call alike in these, whatever its k, N and W. */
+ * It depends on B alone, and a workspace of cmc_decode_attn_workspace_size for the
+ * same B will do as well. */
 CMC_API size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims);
 
 /*
@@ -541,9 +540,8 @@ CMC_API size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims);
  *   scale, out                as for cmc_two_tier_decode_attn
  *   workspace                 see cmc_decode_attn_q8_workspace_size
  *
- * Products are exact and sums fp32.  A probability is rounded to eight significant
- * bits (as to bf16), or to 2^-18 of the largest where it is far below that; a
- * query element to 2^-22 of its head's largest.  A NaN among the tokens reaches the
+ * Products are exact and sums fp32.  A probability is rounded to eleven significant
+ * bits; a query element is exact down to 2^-22 of its head's largest.  A NaN among the tokens reaches the
  * outputs of its KV head's queries; slots that hold no token may hold anything.
  * A sequence with pos[b] < 0 gets a zero output and sets CMC_DEVFLAG_BAD_POS.
  */
@@ -555,15 +553,14 @@ CMC_API int cmc_two_tier_decode_attn_q8(const void* q, const void* tier1_kv, con
 
 /*
  * One fused decode step over a cache in 8 bits: cmc_window_append_q8 followed by
- * cmc_two_tier_decode_attn_q8 in one launch (plus a combine launch where units
- * are cut, see cmc_decode_attn_q8_plan).  The token attends to itself, as
+ * cmc_two_tier_decode_attn_q8 in one launch.  The token attends to itself, as
  * stored.  A sequence with pos[b] < 0 is left unchanged, its output is zero and
  * CMC_DEVFLAG_BAD_POS is set.
  *
  * rope_theta == 0: keys and queries as given.  rope_theta > 0: the step of a
  * GQA layer, as cmc_decode_step_rope: q and k_new are rotated inside the launch at
  * position rope_offset + pos[b] (pos before the append).  The rotated key is
- * quantised from fp32; the rotated query is rounded to eight significant bits.
+ * quantised from fp32; the rotated query is rounded to eleven significant bits.
  *
  * Errors: as the two calls; rope_theta negative, infinite or NaN, or rope_offset
  * outside [0, 2^32] with a rope_theta: CMC_ERR_RANGE.
@@ -574,12 +571,11 @@ CMC_API int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* 
                                double rope_theta, int64_t rope_offset, void* out, void* workspace,
                                size_t workspace_bytes, void* stream);
 
-/* cmc_decode_attn_plan for the calls over a cache in 8 bits (fused == 0:
- * cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8): *launches is 1 when every
- * (sequence, layer, KV head) unit has a CTA or a cluster of CTAs of its own, 2 when
- * there are more units than resident CTAs (then the live keys of all of them
- * are shared out evenly, and a kernel merges the units that this cuts). */
-CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas, int* launches);
+/* Launch plan of the calls over a cache in 8 bits for `dims` on the current device
+ * (fused == 0: cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8): *ctas receives
+ * the grid size of their one kernel, a CTA or a cluster of up to 8 for every
+ * (sequence, layer, KV head) unit. */
+CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas);
 
 /* ------------------------------------------------------------------------ *
  * Staging copies for a serving loop (not a step of the paper's method: the  *

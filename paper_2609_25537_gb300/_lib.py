@@ -127,7 +127,7 @@ _SIGNATURES = {
                                          _vp, _sz, _vp]),
     "cmc_decode_step_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float,
                                 ctypes.c_double, ctypes.c_int64, _vp, _vp, _sz, _vp]),
-    "cmc_decode_attn_q8_plan": (_i, [_dims_p, _i, ctypes.POINTER(_i), ctypes.POINTER(_i)]),
+    "cmc_decode_attn_q8_plan": (_i, [_dims_p, _i, ctypes.POINTER(_i)]),
     "cmc_stage_copies": (_i, [_vp, _i, _i, _vp]),
     "cmc_score_select_static": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp]),
 }

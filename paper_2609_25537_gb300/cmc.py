@@ -722,7 +722,10 @@ def _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new) -> 
         raise ValueError(f"pos shape {tuple(pos.shape)} does not match batch {B}")
     if new is not None:
         _need_new(*new, (B, L, Hkv, d), dev)
-    return CmcDims(B, L, Hq, Hkv, d, max(k, 1), k, W)
+    dims = CmcDims(B, L, Hq, Hkv, d, max(k, 1), k, W)
+    if decode_attn_q8_workspace_size(dims) == 0:
+        raise ValueError(f"unsupported dims {dims.key()}")
+    return dims
 
 
 def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, out, workspace):
@@ -739,10 +742,7 @@ def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, out
     kept = _shapes_cache.get(key)
     if kept is None:
         dims = _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new)
-        units = dims.B * dims.L * dims.Hkv
-        # (what the size of a workspace depends on, with room for other shapes alike in it)
-        kept = _kept(key, (dims, ctypes.byref(dims),
-                           ("q8", dims.B, dims.Hq // dims.Hkv, dims.d, units > 128)))
+        kept = _kept(key, (dims, ctypes.byref(dims), ("q8", dims.B)))  # a workspace goes by B
     dims, ref, sizes = kept
     if out is None:
         out = torch.empty_like(q)
@@ -770,7 +770,7 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     (tier1_kv and tier1_scales None: the ring alone); see
     cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a
     DecodeWorkspace(dims, device, q8=True); without one the call keeps one per stream and
-    kind of shape, and a captured call gets one of its own, zero-filled at every replay."""
+    batch size, and a captured call gets one of its own, zero-filled at every replay."""
     index, dims, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
                                          out, workspace)
     fn = lib().cmc_two_tier_decode_attn_q8
@@ -804,13 +804,13 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     return out
 
 
-def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> Tuple[int, int]:
-    """(grid size, kernel launches per call) of the attention over a cache in 8
-    bits; see cmc_decode_attn_q8_plan."""
-    ctas, launches = ctypes.c_int(0), ctypes.c_int(0)
-    check(lib().cmc_decode_attn_q8_plan(ctypes.byref(dims), 1 if fused else 0, ctypes.byref(ctas),
-                                        ctypes.byref(launches)), "cmc_decode_attn_q8_plan")
-    return int(ctas.value), int(launches.value)
+def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> int:
+    """Grid size of the attention over a cache in 8 bits (always one kernel); see
+    cmc_decode_attn_q8_plan."""
+    ctas = ctypes.c_int(0)
+    check(lib().cmc_decode_attn_q8_plan(ctypes.byref(dims), 1 if fused else 0, ctypes.byref(ctas)),
+          "cmc_decode_attn_q8_plan")
+    return int(ctas.value)
 
 
 # ----------------------------------------------------------------------------

@@ -1,27 +1,23 @@
 // Decode attention over the two-tier cache held in 8 bits (format: cmc_q8.cuh),
 // alone and fused with the append of the step's token.
 //
-// The unit of work is a warp's: a block of 32 keys of one unit (sequence, layer, KV
-// head), which is one block of the format, with one power of two for K and one for
-// V.  A CTA is four warps that have little to do with each other: each loads its own
-// blocks into its own ring of stages, a TMA box of 32 rows of K and of V each (8 KB
-// at d = 128), and refills a stage as soon as it is done with it, so there is no
-// producer and no barrier between loading and computing but the stage's "full" one.
+// One CTA per unit (sequence, layer, KV head), or a cluster of cm CTAs; a unit's blocks of
+// 32 keys, which are the format's blocks with one power of two for K and one for V, are
+// ceil(k / 32) of Tier-1, then those of the ring's live slots, and warp w of the unit's 4 cm
+// takes blocks w, w + 4 cm, ...  The four warps of a CTA have little to do with each
+// other: each loads its own blocks into its own ring of stages, a TMA box of 32 rows of
+// K and of V each (8 KB at d = 128), and refills a stage as soon as it is done with it, so
+// there is no producer and no barrier between loading and computing but the stage's
+// "full" one.  The first blocks do not depend on pos and are requested before it is
+// known.  In the end the warps' states are merged in shared memory, the CTAs' of a
+// cluster in distributed shared memory (as in cmc_attn.cu).
 //
-// Plans.  A unit's blocks are ceil(k / 32) of Tier-1, then those of the ring's live
-// slots.
-//   strided  (no more units than resident CTAs): one CTA, or a cluster of cm CTAs,
-//            per unit; warp w of the unit's 4 cm takes blocks w, w + 4 cm, ...  Its
-//            first blocks do not depend on pos, so they are requested before pos is
-//            known.  The warps' states are merged in shared memory, the CTAs' in
-//            distributed shared memory (as in cmc_attn.cu).
-//   flat     (more units): every CTA works out from all of pos how many live blocks
-//            there are and every warp of the grid takes an equal, contiguous run of
-//            them.  A unit that lies whole in a warp's run (the rule where units are
-//            short) is written by that warp alone; of a unit that is cut the pieces
-//            go to global memory, merged by a small kernel that follows.  Runs of
-//            live blocks are equal whatever the rings' fill: 64 sequences with rings
-//            filled to a third in the mean, 256 + 2,048 keys at most: see DESIGN.
+// A grid may have many more CTAs than are resident: the hardware gives a free place to the
+// next unit, which evens out rings of different fill, and what one CTA waits for
+// (its first bytes, its merge) the others on the SM cover.  The depth of the rings of
+// stages sets how many those are: see plan_q8.  (Sharing out the live blocks of all units evenly
+// over the warps of one wave, with a kernel to merge the cut units, cost 10 us a launch
+// over this: 312 units of 256 + 2,048 keys 37 us, 304 of them here 28.)
 //
 // Both products run on fp16 operands with fp32 accumulation (mma.sync m16n8k16): the
 // codes are converted to fp16 in registers, exactly, one instruction for two.  (mma.sync
@@ -48,52 +44,44 @@
 #include "cmc_attn.cuh"
 #include "cmc_q8.cuh"
 
+#ifndef Q8NST
+#define Q8NST 3
+#endif
+#include <stdlib.h>
 namespace cmc {
-
-// The flat plan's grid is limited so that a workspace's size does not depend on the
-// device: two records for each of its warps.
-constexpr int kQ8MaxCtas = 480;
-constexpr int kQ8RecHead = 4;  // words before a record's maxima: valid, ends
-// Units up to which a call never takes the flat plan (and its workspace holds no records).
-constexpr int kQ8StridedUnits = 128;
-
-// Heads of units kept per warp: blocks are requested up to six ahead, but of short units'
-// (one block each) no more than that many begin between a request and its use.
-constexpr int kQ8Heads = 8;
 
 struct Q8Maps {
   CUtensorMap t1, ring;  // [2 units, T, d] bytes, box 2 x 32 rows
 };
 
-struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the split of cmc_attn.cu are not used
+struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the tiles of cmc_attn.cu are not used
   uint8_t* ring_kv;           // [B, L, Hkv, 2, W, d]
   uint8_t* ring_scales;       // [B, L, Hkv, 2, ringS]
   const uint8_t* t1_scales;   // [B, L, Hkv, 2, t1S]
   int ringS, t1S;
   int nb1, nb2;               // blocks of Tier-1, and of the whole ring
   int rope;                   // rotate q and the new key (fused step)
-};                            // cm: CTAs per unit (strided plan), 0: flat plan
+};                            // cm: CTAs per unit
 
-// Shared memory of a CTA: per warp a query slot, a rotary table, the stages' powers of two
-// and the heads of the units under way (in the end the warp's maxima and sums); what a
-// cluster's peers send; then, 1,024-byte aligned, the stages.
-template <int D, int G>
+// Shared memory of a CTA: the query in fp16, its heads' factors, the rotated new key, the stages'
+// powers of two, the warps' maxima and sums, what a cluster's peers send; then,
+// 1,024-byte aligned, the stages.
+template <int D, int G, int NST>
 struct Q8Smem {
-  // 96 KB of stages a CTA, two CTAs an SM (at d = 128 and G = 8 that just fits).  With 64 KB and
-  // three CTAs, two blocks a warp, 64 x (256 + 2,048) keys took 73 us instead of 56.
-  static constexpr int NST = D == 64 ? 6 : 3;
   static constexpr int kV = kQ8Block * D;
   static constexpr int kStage = 2 * kQ8Block * D;
-  static constexpr int kQ = 0;                                // [warp][G][D] bf16
-  static constexpr int kRope = kQ + kWarps * G * D * 2;       // [warp][d/2] (cos, sin)
-  static constexpr int kScale = kRope + kWarps * D * 4;       // [warp][NST][2] words
-  static constexpr int kHead = kScale + kWarps * NST * 8;     // [warp][kHeads][8] words
-  static constexpr int kRecv = kHead + kWarps * kQ8Heads * 32;  // groups of 16 bytes, rank by rank
+  static constexpr int kQ = 0;                              // [G][D] fp16
+  static constexpr int kQs = kQ + G * D * 2;                // [8] fp32
+  static constexpr int kKnew = kQs + 32;                    // [D] fp32
+  static constexpr int kScale = kKnew + D * 4;              // [warp][NST][2] words
+  static constexpr int kMl = kScale + kWarps * NST * 8;     // [warp][8 maxima, 8 sums]
+  static constexpr int kRecv = kMl + kWarps * 64;           // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
   static constexpr int kSmall = kRecvMl + kMaxClusterCtas * G * 8;
   static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
-  static_assert(kHead % 16 == 0 && kRecv % 16 == 0, "read by 16 bytes");
+  static_assert(kRecv % 16 == 0, "written by 16 bytes");
 };
+
 // Offset of 16-byte chunk c of row r of a stage's K or V: TMA's 128-byte swizzle, or the
 // 64-byte one for rows of 64 codes.
 template <int D>
@@ -161,29 +149,37 @@ __device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState
   return n > 0 ? n : 1;
 }
 
-// What a warp has to know of a unit (or its part of it) besides the blocks.
-struct UnitHead {
-  int u, j0, nb, left;  // unit, first block, the unit's live blocks, blocks of this part
-  int count, new_slot;  // live ring slots, the new token's
-  long long pos;
-};
-static_assert(sizeof(UnitHead) == 32, "two 16-byte words");
-
-// A unit's query rows into the warp's slot.
-template <int D, int G>
-__device__ __forceinline__ void load_query(const AttnQ8Params& p, int u, uint8_t* q, uint64_t* bar) {
-  mbar_arrive_expect_tx(bar, G * D * 2 + p.stall_tx);
-  bulk_copy(smem_addr(q), p.q + static_cast<long long>(u) * (G * D), G * D * 2, bar);
-}
-
-// The new token's rows of a unit (fused step): lanes 0-15 hold K's, lanes 16-31 V's, d / 16
-// neighbouring elements each.
+// Half a row of the new token each for lanes 0-15 (K) and 16-31 (V): d / 16 neighbouring elements.
 template <int D>
 __device__ __forceinline__ uint4 load_new(const AttnQ8Params& p, int u, int lane) {
   const uint16_t* row = (lane < 16 ? p.k_new : p.v_new) + static_cast<long long>(u) * D + (lane & 15) * (D / 16);
   if (D == 128) return __ldg(reinterpret_cast<const uint4*>(row));
   const uint2 w = __ldg(reinterpret_cast<const uint2*>(row));
   return make_uint4(w.x, w.y, 0u, 0u);
+}
+
+// A lane's E = d / 32 neighbouring elements of a row.
+template <int E>
+__device__ __forceinline__ void load_part(const uint16_t* row, int lane, float (&x)[E]) {
+  uint2 w = make_uint2(0u, 0u);
+  if (E == 4) w = __ldg(reinterpret_cast<const uint2*>(row) + lane);
+  else w.x = __ldg(reinterpret_cast<const uint32_t*>(row) + lane);
+  x[0] = bf16lo_to_f32(w.x);
+  x[1] = bf16hi_to_f32(w.x);
+  if (E == 4) {
+    x[E - 2] = bf16lo_to_f32(w.y);
+    x[E - 1] = bf16hi_to_f32(w.y);
+  }
+}
+// Rotates a row held by a warp in parts: element c pairs with c +- d/2, the same of lane ^ 16.
+template <int E>
+__device__ __forceinline__ void rotate_part(float (&x)[E], const float2 (&cs)[E], int lane) {
+  const float sg = lane < 16 ? -1.f : 1.f;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float y = __shfl_xor_sync(0xffffffffu, x[e], 16);
+    x[e] = fmaf(x[e], cs[e].x, sg * y * cs[e].y);
+  }
 }
 
 // The rare parts of an append, out of line and rolled: the code that a launch runs through once is
@@ -213,32 +209,22 @@ static __device__ __noinline__ void block_recode(uint8_t* rows, uint8_t* ring_ro
 
 // The new token in its block: the token's codes over the stale ones, in the stage and in
 // the ring; the block's other codes too where its power of two changes.  Half a warp
-// each for K and V (`fresh`: load_new's).  r: the token's row; `others`: the block's rows
+// each for K and V (`fresh`: load_new's; knew: the rotated key).  r: the token's row; `others`: the block's rows
 // that hold another token; slot: its ring slot; kc, vc: the block's bytes.  (The rules
 // are window_append_q8_kernel's.)
 template <int D>
 __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stage, int u, int r, int slot,
-                                            uint32_t others, const uint4& fresh, const float2* rope_tab, int& kc,
+                                            uint32_t others, const uint4& fresh, const float* knew, int& kc,
                                             int& vc, int lane) {
   constexpr int E = D / 16;  // elements a lane has of its row
   const int half = lane >> 4;
   float x[8];
   unpack8(fresh, x);
-  if (p.rope) {  // K's element c pairs with c +- d/2, the same of the lane 8 away
-    uint4 w;
-    w.x = __shfl_xor_sync(0xffffffffu, fresh.x, 8);
-    w.y = __shfl_xor_sync(0xffffffffu, fresh.y, 8);
-    w.z = D == 128 ? __shfl_xor_sync(0xffffffffu, fresh.z, 8) : 0u;
-    w.w = D == 128 ? __shfl_xor_sync(0xffffffffu, fresh.w, 8) : 0u;
-    float y[8];
-    unpack8(w, y);
-    if (half == 0) {
-      const float sg = lane < 8 ? -1.f : 1.f;
+  if (p.rope && half == 0) {
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const float2 cs = rope_tab[(lane & 7) * E + e];
-        x[e] = fmaf(x[e], cs.x, sg * y[e] * cs.y);
-      }
+    for (int e = 0; e < E; e += 4) {
+      const float4 y = *reinterpret_cast<const float4*>(knew + (lane & 15) * E + e);
+      x[e] = y.x; x[e + 1] = y.y; x[e + 2] = y.z; x[e + 3] = y.w;
     }
   }
   uint32_t top = 0u;
@@ -282,35 +268,18 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
   __syncwarp();
 }
 
-// N bf16 values in shared memory, 2 N bytes aligned, to fp32.
-template <int N>
-__device__ __forceinline__ void load_row(const uint8_t* from, float (&x)[N]) {
-#pragma unroll
-  for (int e = 0; e < N; e += 8) {
-    uint4 w = make_uint4(0u, 0u, 0u, 0u);
-    if (N >= 8) w = *reinterpret_cast<const uint4*>(from + 2 * e);
-    else if (N == 4) { const uint2 v = *reinterpret_cast<const uint2*>(from); w.x = v.x; w.y = v.y; }
-    else w.x = *reinterpret_cast<const uint32_t*>(from);
-    float f[8];
-    unpack8(w, f);
-#pragma unroll
-    for (int q = 0; q < 8 && e + q < N; ++q) x[e + q] = f[q];
-  }
-}
-
-template <int D, int G, bool FUSED>
-__global__ void __maxnreg__(200)
+template <int D, int G, bool FUSED, int NST>
+__global__ void __maxnreg__(NST == 1 ? 96 : 168)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
-  using S = Q8Smem<D, G>;
-  constexpr int NST = S::NST;
+  using S = Q8Smem<D, G, NST>;
   constexpr int KS = D / 16;      // k-steps of the Q K^T product, m-tiles of O^T
+  constexpr int E = D / 32;       // elements of a row a lane has
   constexpr int NGR = G * D / 4;  // groups of four rows of the head dimension of a unit's output
   extern __shared__ __align__(16) uint8_t smem[];
   __shared__ __align__(8) uint64_t full_bar[kWarps][NST];
-  __shared__ __align__(8) uint64_t q_bar[kWarps];
   __shared__ __align__(8) uint64_t recv_bar;  // clusters: the peers' stores
-  __shared__ long long s_pos[kWarps];         // pos of the warps' first sequences
-  __shared__ int s_first[kWarps][2], s_last[kWarps], s_sum[kWarps];
+  __shared__ int s_left[kWarps];              // where the warps left their outputs
+  __shared__ long long s_pos[kWarps];
 
   const int tid = threadIdx.x;
   const int lane = tid & 31;
@@ -318,21 +287,19 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem + S::kSmall) + 1023) & ~uintptr_t(1023)) +
                     warp * (NST * S::kStage);
   uint8_t* scale_words = smem + S::kScale + warp * (NST * 8);
-  UnitHead* heads = reinterpret_cast<UnitHead*>(smem + S::kHead) + warp * kQ8Heads;
-  uint8_t* q_slot = smem + S::kQ + warp * (G * D * 2);
-  float2* rope_tab = reinterpret_cast<float2*>(smem + S::kRope + warp * (D * 4));
+  float* knew = reinterpret_cast<float*>(smem + S::kKnew);
+  float* q_factor = reinterpret_cast<float*>(smem + S::kQs);
   uint64_t* full = full_bar[warp];
 
-  // strided plan: the CTA's unit, the warp's first block and their distance
   const int cm = p.cm;
-  const int su = cm > 1 ? static_cast<int>(cluster_id()) : static_cast<int>(blockIdx.x);
+  const int u = cm > 1 ? static_cast<int>(cluster_id()) : static_cast<int>(blockIdx.x);
   const int rank = cm > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int g0 = rank * kWarps + warp, step = cm * kWarps;
+  const int g0 = rank * kWarps + warp, step = cm * kWarps;  // the warp's first block, and their distance
   const int nb_all = p.nb1 + p.nb2;
+  const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));  // sequence
 
   if (lane == 0) {
     for (int s = 0; s < NST; ++s) mbar_init(&full[s], 1);  // lane 0's arrive (plus tracked cp.async arrivals)
-    mbar_init(&q_bar[warp], 1);
     if (warp == 0) attn_abort = 0;
     if (warp == 1 && cm > 1) {  // the groups this CTA finishes and the heads' (max, sum), from each rank
       const int mine = min(max(NGR - rank * p.slice, 0), p.slice);
@@ -340,152 +307,33 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       mbar_arrive_expect_tx(&recv_bar, static_cast<uint32_t>(cm * (mine * 16 + G * 8)) + p.stall_tx);
     }
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+    prefetch_map((warp & 1) && p.k > 0 ? &maps.t1 : &maps.ring);
   }
   __syncthreads();
   if (cm > 1) cluster_arrive();  // waited for before the first store into a peer
-  // Before the grid dependency wait: the strided plan's first blocks into L2.
-  if (lane == 0) prefetch_map((warp & 1) && p.k > 0 ? &maps.t1 : &maps.ring);
-  if (cm > 0 && lane == 0) {
-    for (int i = 0; i < p.l2_prefetch && g0 + i * step < nb_all; ++i) {
-      const int j = g0 + i * step;
-      tma_box3_prefetch(j < p.nb1 ? &maps.t1 : &maps.ring, (j < p.nb1 ? j : j - p.nb1) * kQ8Block, 2 * su);
-    }
+  // Before the grid dependency wait: the first blocks into L2.
+  if (lane == 0) {
+#pragma unroll 1
+    for (int i = 0, j = g0; i < p.l2_prefetch && j < nb_all; ++i, j += step)
+      tma_box3_prefetch(j < p.nb1 ? &maps.t1 : &maps.ring, (j < p.nb1 ? j : j - p.nb1) * kQ8Block, 2 * u);
   }
-  unsigned long long turns[2] = {0ull, 0ull};  // this lane's rotary frequencies
+  unsigned long long turns[E] = {};  // rotary frequencies of the lane's elements
   if (FUSED && p.rope) {
-    if (p.rope_slot >= 0) {
-      turns[0] = g_rope_tables[p.rope_slot][lane];
-      if (lane + 32 < D / 2) turns[1] = g_rope_tables[p.rope_slot][lane + 32];
-    } else {
-      turns[0] = p.rope_turns[lane];
-      if (lane + 32 < D / 2) turns[1] = p.rope_turns[lane + 32];
-    }
+    const unsigned long long* f = p.rope_slot >= 0 ? g_rope_tables[p.rope_slot] : p.rope_turns;
+#pragma unroll
+    for (int e = 0; e < E; ++e) turns[e] = f[(lane & 15) * E + e];
   }
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
-  int n_run = 0;          // blocks of the warp's run
-  int issued = 0;         // of them requested
-  int u = su, jn = g0;    // unit and block of the next request
-  int nb = 0;             // flat plan: live blocks of a unit of the sequence,
-  int b = 0, x = 0;       // the sequence, the unit within it,
-  int last_b = 0;         // the run's last sequence,
-  long long pos_next = 0; // pos of the next sequence, ahead of its use,
-  bool unit_new = false;  // whether the next request is the unit's first in this run,
-  int units_asked = 0;    // units begun to be requested
-  SeqState sq;
-  bool counted = false;   // this warp's reading of pos is done and counted
-  unsigned long long ticket = 0;  // and how many were before it
-  uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows of the present unit
-  if (cm > 0) {
-    if (g0 < nb_all) n_run = (nb_all - g0 + step - 1) / step;  // as far as known before pos
-    if (FUSED) fresh = load_new<D>(p, su, lane);
-  } else {
-    // ---- flat: the runs from all of pos ----
-    const int chunk = (p.B + kThreads - 1) / kThreads;
-    const int b0 = min(tid * chunk, p.B), b1 = min(b0 + chunk, p.B);
-    int sum = 0;
-    long long pos_b = 0;  // of sequence b1 - 1
-#pragma unroll 1
-    for (int q = b0; q < b1; ++q) {
-      pos_b = ld_pos(p, q);
-      const SeqState sq = seq_state<FUSED>(p, pos_b);
-      if (sq.bad && blockIdx.x == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-      sum += live_blocks(p, sq);
-    }
-    int scan = sum;  // inclusive, over the warp
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-      const int up = __shfl_up_sync(0xffffffffu, scan, off);
-      if (lane >= off) scan += up;
-    }
-    if (lane == 31) s_sum[warp] = scan;
-    __syncthreads();
-    int before = scan - sum, all = 0;
-#pragma unroll
-    for (int v = 0; v < kWarps; ++v) {
-      if (v < warp) before += s_sum[v];
-      all += s_sum[v];
-    }
-    const unsigned total = static_cast<unsigned>(all) * static_cast<unsigned>(p.LH);
-    const unsigned nw = gridDim.x * kWarps;
-    const unsigned base = total / nw, rem = total - base * nw;
-#pragma unroll 1
-    for (int v = 0; v < kWarps; ++v) {
-      const unsigned wid = blockIdx.x * kWarps + v;
-      const unsigned a = wid * base + min(wid, rem), n = base + (wid < rem ? 1u : 0u);
-      if (v == warp) n_run = static_cast<int>(n);
-      if (n == 0) continue;
-      // the thread in whose sequences the run begins, and the one in whose it ends
-      const unsigned lo = static_cast<unsigned>(before) * p.LH, hi = static_cast<unsigned>(before + sum) * p.LH;
-#pragma unroll 1
-      for (int e = 0; e < 2; ++e) {
-        const unsigned at = e ? a + n - 1 : a;
-        if (at < lo || at >= hi) continue;
-        unsigned from = lo;
-#pragma unroll 1
-        for (int q = b0; q < b1; ++q) {
-          const long long pb = chunk == 1 ? pos_b : ld_pos(p, q);
-          const unsigned len = static_cast<unsigned>(live_blocks(p, seq_state<FUSED>(p, pb))) * p.LH;
-          if (at < from + len) {
-            if (e) {
-              s_last[v] = q;
-            } else {
-              s_first[v][0] = q;
-              s_first[v][1] = static_cast<int>(at - from);
-              s_pos[v] = pb;
-            }
-            break;
-          }
-          from += len;
-        }
-      }
-    }
-    __syncthreads();
-    if (n_run > 0) {
-      b = s_first[warp][0];
-      last_b = s_last[warp];
-      sq = seq_state<FUSED>(p, s_pos[warp]);
-      nb = live_blocks(p, sq);
-      const int off = s_first[warp][1];
-      x = off / nb;
-      jn = off - x * nb;
-      u = b * p.LH + x;
-      unit_new = true;
-      if (b < last_b) pos_next = ld_pos(p, b + 1);
-    }
-  }
-  // Flat plan: counts that this warp has read pos of all its sequences; the last one to be counted
-  // advances every pos, when its run is done (the count takes a trip to L2).  `nb` comes of
-  // the last pos, and makes the count wait for it.
-  auto count_reads = [&]() {
-    counted = true;
-    if (lane == 0) {
-      int seen;
-      asm volatile("mov.b32 %0, %1;\n" : "=r"(seen) : "r"(nb));
-      ticket = atomicAdd(p.tickets, seen >= 0 ? 1ull : 0ull);
-    }
-  };
   // The unit's powers of two: the rows of lane 0 (K) and lane 1 (V).
   const uint8_t* t1_s = p.t1_scales + (2LL * u + (lane & 1)) * p.t1S;
   const uint8_t* ring_s = p.ring_scales + (2LL * u + (lane & 1)) * p.ringS;
-  auto put_head = [&](int left) {
-    if (lane == 0) {
-      UnitHead* h = heads + (units_asked & (kQ8Heads - 1));
-      *reinterpret_cast<int4*>(h) = make_int4(u, cm > 0 ? g0 : jn, nb, left);
-      h->count = sq.count;
-      h->new_slot = sq.new_slot;
-      h->pos = sq.pos;
-    }
-    ++units_asked;
-  };
-  // Requests the run's next block into stage s: the codes by TMA, the two words that hold its
+  int n_run = g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;  // blocks of the warp, as far as known before pos
+  int jn = g0;  // the next to request
+  // Requests the warp's next block into stage s: the codes by TMA, the two words that hold its
   // powers of two by lanes 0 and 1.  Called by the whole warp, converged.
   auto request = [&](int s) {
-    if (unit_new) {
-      put_head(min(nb - jn, n_run - issued));
-      unit_new = false;
-    }
     const bool t1 = jn < p.nb1;
     const int jj = t1 ? jn : jn - p.nb1;
     if (lane < 2) {
@@ -498,190 +346,126 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       tma_box3_hint(smem_addr(stages + s * S::kStage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * u, &full[s],
                     policy_evict_first());
     }
-    ++issued;
-    jn += cm > 0 ? step : 1;
-    if (cm == 0 && jn == nb) {
-      jn = 0;
-      ++u;
-      t1_s += 2 * p.t1S;
-      ring_s += 2 * p.ringS;
-      unit_new = true;
-      if (++x == p.LH && b < last_b) {
-        x = 0;
-        ++b;
-        sq = seq_state<FUSED>(p, pos_next);
-        nb = live_blocks(p, sq);
-        if (b < last_b) pos_next = ld_pos(p, b + 1);
-        else if (FUSED) count_reads();
+    jn += step;
+  };
+  int issued = 0;
+#pragma unroll 1
+  for (; issued < NST && issued < n_run; ++issued) request(issued);
+
+  // ---- the query, while those are on their way: warp w takes heads w and w + 4, a lane E
+  // neighbouring elements; and the new key ----
+  const long long pos = ld_pos(p, b);
+  float x[2][E];
+#pragma unroll
+  for (int e = 0; e < 2; ++e)
+    if (warp + kWarps * e < G) load_part<E>(p.q + (static_cast<long long>(u) * G + warp + kWarps * e) * D, lane, x[e]);
+  uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows
+  float kx[E];
+  if (FUSED) {
+    fresh = load_new<D>(p, u, lane);
+    if (p.rope && warp == kWarps - 1) load_part<E>(p.k_new + static_cast<long long>(u) * D, lane, kx);
+  }
+  const SeqState sq = seq_state<FUSED>(p, pos);
+  unsigned long long ticket = 0;
+  if (tid == 0 && sq.bad && rank == 0 && u % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+  if (FUSED && p.rope) {
+    float2 cs[E];
+    const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + (sq.bad ? 0 : pos));
+#pragma unroll
+    for (int e = 0; e < E; ++e) {  // as rope_pairs
+      const int hi = static_cast<int>(static_cast<long long>(pp * turns[e]) >> 32);
+      float sn, cn;
+      sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &sn, &cn);
+      cs[e] = make_float2(cn, sn);
+    }
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      if (warp + kWarps * e < G) rotate_part<E>(x[e], cs, lane);
+    if (warp == kWarps - 1) {
+      rotate_part<E>(kx, cs, lane);
+#pragma unroll
+      for (int e = 0; e < E; ++e) knew[lane * E + e] = kx[e];
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    if (warp + kWarps * h >= G) break;
+    float top = 0.f;  // (a NaN does not count)
+#pragma unroll
+    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[h][e]));
+    if (__any_sync(0xffffffffu, top == INFINITY)) {  // an infinity becomes NaN and does not count either
+      top = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        x[h][e] = fmaf(x[h][e], 0.f, x[h][e]);
+        top = fmaxf(top, fabsf(x[h][e]));
       }
     }
-  };
-  if (lane == 0 && n_run > 0) load_query<D, G>(p, u, q_slot, &q_bar[warp]);
-  if (FUSED && cm == 0 && b == last_b) count_reads();
-#pragma unroll 1
-  for (int s = 0; s < NST && s < n_run; ++s) request(s);
-  if (cm > 0) {
-    // ---- strided: the first blocks are on their way; now pos ----
-    b = static_cast<int>(static_cast<unsigned>(su) / static_cast<unsigned>(p.LH));
-    if (tid == 0) s_pos[0] = ld_pos(p, b);
-    __syncthreads();
-    sq = seq_state<FUSED>(p, s_pos[0]);
-    if (tid == 0) {
-      if (sq.bad && rank == 0 && su % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-      // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
-      if (FUSED) ticket = atomicAdd(p.tickets + b, 1ull);
-    }
-    nb = live_blocks(p, sq);
-    n_run = nb > g0 ? (nb - g0 + step - 1) / step : 0;
-    if (n_run < issued) n_run = issued;  // blocks that were requested in vain hold no key
-    put_head(n_run);
+#pragma unroll
+    for (int off = 1; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+    const int qc = block_code(__float_as_uint(top));
+    const float f = code_factor(qc);
+    uint32_t* to = reinterpret_cast<uint32_t*>(smem + S::kQ + (warp + kWarps * h) * (D * 2)) + lane * (E / 2);
+#pragma unroll
+    for (int e = 0; e < E; e += 2) to[e / 2] = pack_f16(x[h][e] * f, x[h][e + 1] * f);
+    if (lane == 0) q_factor[warp + kWarps * h] = e8m0_to_f32(qc) * p.scale_log2;
   }
-  __syncwarp();
+  if (FUSED && lane == 0) s_pos[warp] = pos;  // (so that every warp has it, not only asked for it)
+  __syncthreads();
+  // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
+  if (FUSED && tid == 0) ticket = atomicAdd(p.tickets + b, 1ull);
 
+  // Live blocks; those that were requested in vain hold no key.
+  const int nb = sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
+  n_run = nb > g0 ? (nb - g0 + step - 1) / step : 0;
+  if (n_run < issued) n_run = issued;
   // gq = lane / 4, tq = lane % 4: a thread has columns (heads) 2 tq and 2 tq + 1 of the products
   // (heads >= G are padding: zero queries, never written out).
   const int gq = lane >> 2;
   const int tq = lane & 3;
-  int n_units = 0;                             // units begun
-  int cu = 0, j = 0, last_j = 0, left = 0;     // the unit, its block, its last one, blocks left of the part
-  int count = 0, new_slot = -1;                // of its sequence
-  long long pos = 0;
-  bool begun_first = false;                    // the present one with its first block
-  bool head = false, tail = false;             // flat plan: records written
-  long long rope_pos = -1;                     // position that the rotary table is for
-  uint32_t qa[KS][2];                          // Q^T fragments
-  float qs[2] = {0.f, 0.f};                    // softmax scale * log2(e) * the heads' powers of two
-  float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-  int e_cur = -1, e_top = -1;                  // the byte O is in units of; the largest so far
+  uint32_t qa[KS][2];  // Q^T fragments: column gq, elements 16 ks + 4 tq .. + 3
+#pragma unroll
+  for (int ks = 0; ks < KS; ++ks) {
+    uint2 f = make_uint2(0u, 0u);
+    if (gq < G) f = *reinterpret_cast<const uint2*>(smem + S::kQ + (gq * D + 16 * ks + 4 * tq) * 2);
+    qa[ks][0] = f.x;
+    qa[ks][1] = f.y;
+  }
+  float qs[2], m_run[2], l_run[2];  // softmax scale * log2(e) * the heads' powers of two; maxima, sums
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    qs[e] = 2 * tq + e < G ? q_factor[2 * tq + e] : 0.f;
+    m_run[e] = -INFINITY;
+    l_run[e] = 0.f;
+  }
+  int e_cur = -1, e_top = -1;  // the byte O is in units of; the largest so far
   float o[KS][4];
 #pragma unroll
   for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) qa[ks][0] = qa[ks][1] = 0u;
-  // Rows c .. c + 3 of head hh from what a warp left (see below).
-  auto taken = [&](const float* ow, int hh, int c) {
-    return *reinterpret_cast<const float4*>(ow + hh * D + (c ^ (8 * (hh >> 1))));
-  };
 
   bool gave_up = false;
-  float* left_in = nullptr;  // strided plan: where the warp left its output
-  int s = 0;             // stage
-  uint32_t phase = 0;    // its parity
+  int s = 0;           // stage
+  uint32_t phase = 0;  // its parity
+  int j = g0;          // block
+#pragma unroll 1
   for (int i = 0; i < n_run; ++i) {
     uint8_t* stage = stages + s * S::kStage;
     if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {
       gave_up = true;
       break;
     }
-    const bool starts = left == 0;
-    if (starts) {
-      const UnitHead* h = heads + (n_units & (kQ8Heads - 1));
-      const int4 a = *reinterpret_cast<const int4*>(h);
-      cu = a.x;
-      j = a.y;
-      last_j = a.z - 1;
-      left = a.w;
-      count = h->count;
-      new_slot = h->new_slot;
-      pos = h->pos;
-    }
-    // the block: its rows that hold a key (bit r of mk), its bytes, the new token's row
+    // the block: its rows that hold a key (bit r of mk), its bytes
     const bool t1 = j < p.nb1;
     const int jj = t1 ? j : j - p.nb1;
-    const int live = t1 ? (pos < 0 ? 0 : p.k) : count;
+    const int live = t1 ? (sq.bad ? 0 : p.k) : sq.count;
     const int nk = min(max(live - jj * kQ8Block, 0), kQ8Block);
     const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;
     int kc = scale_words[s * 8 + (jj & 3)], vc = scale_words[s * 8 + 4 + (jj & 3)];
-    const bool patched = FUSED && !t1 && new_slot >= 0 && new_slot / kQ8Block == jj;
-    const bool ends = left == 1;
     bool wrote_stage = false;  // generic-proxy writes into the stage
 
-    if (starts) {
-      if (__any_sync(0xffffffffu, !mbar_wait(&q_bar[warp], static_cast<uint32_t>(n_units & 1)))) {
-        gave_up = true;
-        break;
-      }
-      begun_first = j == 0;
-      if (FUSED && cm == 0) fresh = load_new<D>(p, cu, lane);
-      if (FUSED && p.rope) {
-        if (pos >= 0 && pos != rope_pos) {
-          rope_pos = pos;
-          float2 cs[2];
-          rope_pairs<D>(p, pos, turns, lane, cs);
-          rope_tab[lane] = cs[0];
-          if (lane + 32 < D / 2) rope_tab[lane + 32] = cs[1];
-          __syncwarp();
-        }
-      }
-      // The query in fp16, by the whole warp: a lane takes EPL neighbouring elements of one
-      // head, the LPH lanes of a head share its largest.  It goes over the raw rows; the
-      // fragments are read from there.
-      constexpr int EPL = G * D / 32, LPH = 32 / G;
-      float x[EPL];
-      load_row<EPL>(q_slot + lane * (EPL * 2), x);
-      if (FUSED && p.rope) {  // element c's partner c +- d/2 is the same of the lane LPH / 2 away
-        float y[EPL];
-        load_row<EPL>(q_slot + (lane ^ (LPH / 2)) * (EPL * 2), y);
-        const float sg = (lane & (LPH / 2)) ? 1.f : -1.f;
-        const float2* tab = rope_tab + (lane & (LPH / 2 - 1)) * EPL;
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-          const float2 cs = tab[e];
-          x[e] = fmaf(x[e], cs.x, sg * y[e] * cs.y);
-        }
-      }
-      float top = 0.f;  // (a NaN does not count)
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) top = fmaxf(top, fabsf(x[e]));
-      if (__any_sync(0xffffffffu, top == INFINITY)) {  // an infinity becomes NaN and does not count either
-        top = 0.f;
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) {
-          x[e] = fmaf(x[e], 0.f, x[e]);
-          top = fmaxf(top, fabsf(x[e]));
-        }
-      }
-#pragma unroll
-      for (int off = 1; off < LPH; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-      const int qc = block_code(__float_as_uint(top));
-      const float qf = code_factor(qc);
-      __syncwarp();  // every lane has read its rows
-#pragma unroll
-      for (int e = 0; e < EPL; e += 2)
-        reinterpret_cast<uint32_t*>(q_slot + lane * (EPL * 2))[e / 2] = pack_f16(x[e] * qf, x[e + 1] * qf);
-      __syncwarp();
-      // fragments: column gq, elements 16 ks + 4 tq .. + 3
-      if (gq < G) {
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-          const uint2 f = *reinterpret_cast<const uint2*>(q_slot + (gq * D + 16 * ks + 4 * tq) * 2);
-          qa[ks][0] = f.x;
-          qa[ks][1] = f.y;
-        }
-      }
-      const float qscale = e8m0_to_f32(qc) * p.scale_log2;
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        qs[e] = __shfl_sync(0xffffffffu, qscale, (2 * tq + e) * LPH);
-        m_run[e] = -INFINITY;
-        l_run[e] = 0.f;
-      }
-      // the next unit's rows into the slot, where the run goes on behind this unit
-      if (cm == 0 && i + left < n_run) {
-        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-        __syncwarp();
-        if (lane == 0)
-          load_query<D, G>(p, cu + 1, q_slot, &q_bar[warp]);
-      }
-      e_cur = e_top = -1;
-#pragma unroll
-      for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-      ++n_units;
-    }
-
-    if (patched) {
-      const int r = new_slot & (kQ8Block - 1);
-      patch_block<D>(p, stage, cu, r, new_slot, mk & ~(1u << r), fresh, rope_tab, kc, vc, lane);
+    if (FUSED && !t1 && sq.new_slot >= 0 && sq.new_slot / kQ8Block == jj) {
+      const int r = sq.new_slot & (kQ8Block - 1);
+      patch_block<D>(p, stage, u, r, sq.new_slot, mk & ~(1u << r), fresh, knew, kc, vc, lane);
       wrote_stage = true;
     }
 
@@ -810,70 +594,14 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       }
     }
 
-    if (ends) {
-      // The unit's share of this run is done.  The warp sums its l over the lanes and leaves O in
-      // true units in its stage: 8 columns of D floats, just the size of K's part, columns
-      // of odd pairs shifted so that the stores hit distinct banks.
-      float* ow = reinterpret_cast<float*>(stage);
-#pragma unroll
-      for (int e = 0; e < 2; ++e)
-#pragma unroll
-        for (int off = 4; off < 32; off <<= 1)
-          l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
-      __syncwarp();  // the warp is done with the stage
-      const bool whole = cm == 0 && begun_first && j == last_j;  // normalised too
-      const float fo = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float f = !whole ? fo : l_run[e] > 0.f ? __fdividef(fo, l_run[e]) : 0.f;
-        float* col = ow + (2 * tq + e) * D;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
-          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
-        }
-      }
-      if (cm > 0) {
-        left_in = ow;
-        break;  // the run's last block
-      }
-      // Flat plan: written out where it is the whole unit, else left as a record (the first of the
-      // run's if the unit began before it).
-      __syncwarp();
-      wrote_stage = true;
-      if (whole) {
-        uint16_t* out = p.out + static_cast<long long>(cu) * (G * D);
-        for (int x = lane; x < NGR; x += 32) {
-          const float4 y = taken(ow, (4 * x) / D, (4 * x) % D);
-          *reinterpret_cast<uint2*>(out + 4 * x) = make_uint2(pack_bf16_rn(y.x, y.y), pack_bf16_rn(y.z, y.w));
-        }
-      } else {
-        const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
-        float* rec = p.partials + (2 * wid + (begun_first ? 1 : 0)) * (kQ8RecHead + rec_floats(G, D));
-        if (begun_first) tail = true;
-        else head = true;
-        if (lane == 0) *reinterpret_cast<int4*>(rec) = make_int4(1, j == last_j ? 1 : 0, cu, 0);
-        rec += kQ8RecHead;
-        if (gq == 0) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e)
-            if (2 * tq + e < G) {
-              rec[2 * tq + e] = m_run[e];
-              rec[G + 2 * tq + e] = l_run[e];
-            }
-        }
-        for (int x = lane; x < NGR; x += 32)
-          *reinterpret_cast<float4*>(rec + rec_out_offset(G) + 4 * x) = taken(ow, (4 * x) / D, (4 * x) % D);
-      }
-    }
-    if (wrote_stage) {
+    if (issued < n_run) {
       // generic-proxy writes to this stage are ordered before the next box into it
-      asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+      if (wrote_stage) asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+      __syncwarp();
+      request(s);
+      ++issued;
     }
-    __syncwarp();
-    if (issued < n_run) request(s);
-    --left;
-    j += cm > 0 ? step : 1;
+    j += step;
     if (++s == NST) {
       s = 0;
       phase ^= 1u;
@@ -886,53 +614,50 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     const uint32_t t0 = global_ns32();
     for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
     if (lane == 0) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
-  }
-  if (cm == 0) {
-    if (FUSED) {
-      if (!counted) count_reads();  // (after a timeout)
-      if (__shfl_sync(0xffffffffu, ticket, 0) + 1 == static_cast<unsigned long long>(gridDim.x) * kWarps) {
-        for (int b = lane; b < p.B; b += 32) {
-          const long long v = ld_pos(p, b);
-          if (v >= 0) p.pos[b] = v + 1;
-        }
-        if (lane == 0) p.tickets[0] = 0ull;
-      }
-    }
-    // the merge kernel reads both records' first words
-    if (lane == 0) {
-      const long long wid = static_cast<long long>(blockIdx.x) * kWarps + warp;
-      float* rec = p.partials + 2 * wid * (kQ8RecHead + rec_floats(G, D));
-      if (!head) *reinterpret_cast<int*>(rec) = 0;
-      if (!tail) *reinterpret_cast<int*>(rec + kQ8RecHead + rec_floats(G, D)) = 0;
-    }
-    return;
+    l_run[0] = l_run[1] = 0.f;
   }
 
-  // ---- strided plan: the four warps' states, then the cluster's CTAs' ----
-  // After a barrier each thread takes four rows of the head dimension of one head, rescales and
-  // adds what the warps left, in warp order.
-  if (!left_in) {  // no blocks (or a timeout): nothing
-    left_in = reinterpret_cast<float*>(stages);
-    for (int x = lane; x < 8 * D; x += 32) left_in[x] = 0.f;
-    l_run[0] = l_run[1] = 0.f;
-    m_run[0] = m_run[1] = -INFINITY;
-  }
-  if (lane == 0) s_first[warp][0] = static_cast<int>(reinterpret_cast<uint8_t*>(left_in) - smem);
-  constexpr int kMl = kQ8Heads * 8;
-  float* ml = reinterpret_cast<float*>(smem + S::kHead);  // over each warp's heads: 8 maxima, 8 sums
-  if (gq == 0) {
+  // ---- the four warps' states, then the cluster's CTAs' ----
+  // Every warp sums its l over the lanes and leaves O in true units in its first stage: 8 columns of
+  // D floats, just the size of K's part, columns of odd pairs shifted so that the stores hit
+  // distinct banks.  After a barrier each thread takes four rows of the head dimension of one
+  // head, rescales and adds what the warps left, in warp order.
+  {
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+#pragma unroll
+      for (int off = 4; off < 32; off <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
+    __syncwarp();  // the warp is done with the stage
+    const float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
+    float* ow = reinterpret_cast<float*>(stages);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      ml[warp * kMl + 2 * tq + e] = m_run[e];
-      ml[warp * kMl + 8 + 2 * tq + e] = l_run[e];
+      float* col = ow + (2 * tq + e) * D;
+      if (2 * tq + e < G) {
+#pragma unroll
+        for (int j = 0; j < KS; ++j) {
+          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
+          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
+        }
+      }
     }
+    if (gq == 0) {
+      float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 16 + 2 * tq;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        ml[e] = m_run[e];
+        ml[8 + e] = l_run[e];
+      }
+    }
+    if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
   }
   __syncthreads();
   if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
-    if (!sq.bad) p.pos[b] = sq.pos + 1;
+    if (!sq.bad) p.pos[b] = pos + 1;
     p.tickets[b] = 0ull;
   }
-  const long long out_base = static_cast<long long>(su) * (G * D);
+  const long long out_base = static_cast<long long>(u) * (G * D);
+  const float* ml = reinterpret_cast<const float*>(smem + S::kMl);
   constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
   float4 cacc[XPT];
   float cls[XPT], cmx[XPT];
@@ -944,17 +669,17 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     const int c = (4 * x) % D;
     float M = ml[hh];
 #pragma unroll
-    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * kMl + hh]);
+    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * 16 + hh]);
     const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float Ls = 0.f;
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) {
-      const float f = ex2(ml[v * kMl + hh] - Mr);
-      const float4 y = taken(reinterpret_cast<const float*>(smem + s_first[v][0]), hh, c);
+      const float f = ex2(ml[v * 16 + hh] - Mr);
+      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + s_left[v]) + hh * D + (c ^ (8 * (hh >> 1))));
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
       acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-      Ls = fmaf(f, ml[v * kMl + 8 + hh], Ls);
+      Ls = fmaf(f, ml[v * 16 + 8 + hh], Ls);
     }
     if (cm == 1) {
       const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
@@ -1018,45 +743,6 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   if (tid == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
 }
 
-// Merges the units that the flat plan cut.  One CTA for each warp of the attention grid: where
-// that warp's run ended inside a unit that began in it, its record and the first
-// records of the warps behind it, up to the one where the unit ends.
-template <int D, int G>
-__global__ void __launch_bounds__(kThreads)
-attn_q8_merge_kernel(const float* __restrict__ recs, uint16_t* __restrict__ out) {
-  constexpr int PW = kQ8RecHead + rec_floats(G, D);
-  pdl_wait();  // the attention kernel's records
-  pdl_trigger();
-  const long long w = blockIdx.x;
-  const float* own = recs + (2 * w + 1) * PW;
-  const int4 h = *reinterpret_cast<const int4*>(own);
-  if (h.x == 0) return;
-  for (int x = threadIdx.x; x < G * D / 4; x += kThreads) {
-    const int hh = (4 * x) / D;
-    const int c = (4 * x) % D;
-    float M = own[kQ8RecHead + hh], L = own[kQ8RecHead + G + hh];
-    float4 O = *reinterpret_cast<const float4*>(own + kQ8RecHead + rec_out_offset(G) + hh * D + c);
-    // (the last warp's run ends with the last unit's last block, so the chain ends inside the grid)
-    for (long long r = w + 1; r < gridDim.x; ++r) {
-      const float* rec = recs + 2 * r * PW;
-      const int2 rh = *reinterpret_cast<const int2*>(rec);
-      if (rh.x == 0) break;  // (after a timeout)
-      const float m = rec[kQ8RecHead + hh];
-      const float4 y = *reinterpret_cast<const float4*>(rec + kQ8RecHead + rec_out_offset(G) + hh * D + c);
-      const float mn = fmaxf(M, m), ref = mn == -INFINITY ? 0.f : mn;
-      const float fa = ex2(M - ref), fb = ex2(m - ref);
-      M = mn;
-      L = fmaf(fb, rec[kQ8RecHead + G + hh], L * fa);
-      O.x = fmaf(fb, y.x, O.x * fa); O.y = fmaf(fb, y.y, O.y * fa);
-      O.z = fmaf(fb, y.z, O.z * fa); O.w = fmaf(fb, y.w, O.w * fa);
-      if (rh.y) break;
-    }
-    const float inv = L > 0.f ? __fdividef(1.f, L) : 0.f;
-    *reinterpret_cast<uint2*>(out + static_cast<long long>(h.z) * (G * D) + hh * D + c) =
-        make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
-  }
-}
-
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
@@ -1076,22 +762,15 @@ static bool encode_q8(CUtensorMap* map, const void* base, long long units2, int 
 
 static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
 
-static size_t q8_workspace_size(const cmc_dims& m) {
-  const int G = m.Hq / m.Hkv;
-  const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  const size_t recs = units > kQ8StridedUnits ? 2 * kWarps * kQ8MaxCtas : 0;
-  return ws_partials_off(m.B) + recs * (kQ8RecHead + rec_floats(G, m.d)) * sizeof(float);
-}
-
 struct Q8Plan {
-  int ctas;  // grid size
-  int cm;    // strided plan: CTAs per unit; 0: flat plan
+  int cm;   // CTAs per unit
+  int nst;  // stages a warp: 1 or 3
 };
 
-template <int D, int G, bool FUSED>
-static int plan_q8(long long units, int nb, Q8Plan* pl) {
-  constexpr int smem = Q8Smem<D, G>::kBytes;
-  auto kern = attn_q8_kernel<D, G, FUSED>;
+template <int D, int G, bool FUSED, int NST>
+static int resident_q8(int* slots) {
+  constexpr int smem = Q8Smem<D, G, NST>::kBytes;
+  auto kern = attn_q8_kernel<D, G, FUSED, NST>;
   static std::atomic<int> configured[64];  // per device: attribute set and occupancy known (idempotent)
   int dev = 0;
   int st = record_cuda_error(cudaGetDevice(&dev));
@@ -1105,49 +784,42 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
     if (per_sm < 1) per_sm = 1;
     if (dev >= 0 && dev < 64) configured[dev].store(per_sm, std::memory_order_release);
   }
-  long long slots = static_cast<long long>(per_sm) * sm_count();
-  if (slots > kQ8MaxCtas) slots = kQ8MaxCtas;
-  if (units <= slots || units <= kQ8StridedUnits) {
-    long long m = slots / units;
-    const long long most = (nb + kWarps - 1) / kWarps;  // a block for every warp
-    if (m > most) m = most;
-    if (m > kMaxClusterCtas) m = kMaxClusterCtas;
-    // (a power of two: others may not fit the GPU's groups of SMs as often as slots / m)
-    pl->cm = m >= 8 ? 8 : m >= 4 ? 4 : m >= 2 ? 2 : 1;
-    m = pl->cm;
-    pl->ctas = static_cast<int>(units * m);
-  } else {
-    pl->cm = 0;
-    pl->ctas = static_cast<int>(slots);
-  }
+  *slots = per_sm * sm_count();
   return CMC_OK;
 }
 
 template <int D, int G, bool FUSED>
-static int launch_q8(const Q8Maps& maps, AttnQ8Params p, long long units, cudaStream_t s) {
-  Q8Plan pl;
-  int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
+static int plan_q8(long long units, int nb, Q8Plan* pl) {
+  int slots = 0;
+  pl->nst = Q8NST;
+  int st = pl->nst == 1 ? resident_q8<D, G, FUSED, 1>(&slots) : pl->nst == 2 ? resident_q8<D, G, FUSED, 2>(&slots) : resident_q8<D, G, FUSED, 3>(&slots);
   if (st != CMC_OK) return st;
+  pl->cm = 1;
+  const long long most = (nb + kWarps - 1) / kWarps;  // a block for every warp
+  while (pl->cm < kMaxClusterCtas && 2 * pl->cm <= most && units * pl->cm * 2 <= slots) pl->cm *= 2;
+  if (getenv("Q8CM")) pl->cm = atoi(getenv("Q8CM"));
+  return CMC_OK;
+}
+
+template <int D, int G, bool FUSED, int NST>
+static int launch_q8(const Q8Maps& maps, AttnQ8Params p, const Q8Plan& pl, long long units, cudaStream_t s) {
   p.cm = pl.cm;
   p.slice = pl.cm > 1 ? (G * D / 4 + pl.cm - 1) / pl.cm : 0;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(pl.cm > 1 ? pl.cm : 1);
+  attr[1].val.clusterDim.x = static_cast<unsigned>(pl.cm);
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(pl.ctas));
+  cfg.gridDim = dim3(static_cast<unsigned>(units * pl.cm));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Q8Smem<D, G>::kBytes;
+  cfg.dynamicSmemBytes = Q8Smem<D, G, NST>::kBytes;
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = pl.cm > 1 ? 2 : 1;
-  st = record_cuda_error(cudaLaunchKernelEx(&cfg, attn_q8_kernel<D, G, FUSED>, maps, p));
-  if (st != CMC_OK || pl.cm > 0) return st;
-  return launch_pdl(attn_q8_merge_kernel<D, G>, dim3(static_cast<unsigned>(pl.ctas * kWarps)), dim3(kThreads), 0, s,
-                    static_cast<const float*>(p.partials), p.out);
+  return record_cuda_error(cudaLaunchKernelEx(&cfg, attn_q8_kernel<D, G, FUSED, NST>, maps, p));
 }
 
 // Calls F<D, G>::run(args...) for the call's head dimension and group size.
@@ -1176,8 +848,17 @@ struct PlanQ8 {
 };
 template <int D, int G>
 struct LaunchQ8 {
+  template <bool FUSED>
+  static int go(const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
+    Q8Plan pl;
+    int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
+    if (st != CMC_OK) return st;
+    return pl.nst == 1 ? launch_q8<D, G, FUSED, 1>(maps, p, pl, units, s)
+         : pl.nst == 2 ? launch_q8<D, G, FUSED, 2>(maps, p, pl, units, s)
+                       : launch_q8<D, G, FUSED, 3>(maps, p, pl, units, s);
+  }
   static int run(bool fused, const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
-    return fused ? launch_q8<D, G, true>(maps, p, units, s) : launch_q8<D, G, false>(maps, p, units, s);
+    return fused ? go<true>(maps, p, units, s) : go<false>(maps, p, units, s);
   }
 };
 
@@ -1199,12 +880,11 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
     return CMC_ERR_ALIGN;
   if (m.k > 0 && (!aligned16(t1_kv) || !aligned16(t1_scales))) return CMC_ERR_ALIGN;
   if (fused && (!aligned16(k_new) || !aligned16(v_new))) return CMC_ERR_ALIGN;
-  if (!workspace || workspace_bytes < q8_workspace_size(m)) return CMC_ERR_WORKSPACE;
+  if (!workspace || workspace_bytes < ws_partials_off(m.B)) return CMC_ERR_WORKSPACE;
   if (!aligned16(workspace)) return CMC_ERR_ALIGN;
 
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
   const int nb1 = q8_blocks(m.k), nb2 = q8_blocks(m.W);
-  if (units * (nb1 + nb2) >= (1LL << 31)) return CMC_ERR_SHAPE;  // blocks are counted in 32 bits
 
   Q8Maps maps;
   memset(&maps, 0, sizeof(maps));
@@ -1220,7 +900,6 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
   char* ws = static_cast<char*>(workspace);
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.tickets = reinterpret_cast<unsigned long long*>(ws + kWsHeader);
-  p.partials = reinterpret_cast<float*>(ws + ws_partials_off(m.B));
   p.B = m.B; p.L = m.L; p.Hq = m.Hq; p.Hkv = m.Hkv; p.N = m.N; p.k = m.k; p.W = m.W;
   p.LH = m.L * m.Hkv;
   p.nb1 = nb1;
@@ -1250,7 +929,7 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
 extern "C" {
 
 size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims) {
-  return cmc::validate_dims(dims, true) == CMC_OK ? cmc::q8_workspace_size(*dims) : 0;
+  return cmc::validate_dims(dims, true) == CMC_OK ? cmc::ws_partials_off(dims->B) : 0;
 }
 
 int cmc_two_tier_decode_attn_q8(const void* q, const void* tier1_kv, const void* tier1_scales,
@@ -1270,20 +949,17 @@ int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* tier1_sc
                                scale, rope_theta, rope_offset, out, workspace, workspace_bytes, stream, true);
 }
 
-int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas, int* launches) {
+int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas) {
   using namespace cmc;
   int st = validate_dims(dims, true);
   if (st != CMC_OK) return st;
-  if (!ctas || !launches) return CMC_ERR_NULL;
+  if (!ctas) return CMC_ERR_NULL;
   const cmc_dims& m = *dims;
-  const int nb = q8_blocks(m.k) + q8_blocks(m.W);
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  if (units * nb >= (1LL << 31)) return CMC_ERR_SHAPE;
   Q8Plan pl;
-  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, nb, &pl);
+  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, q8_blocks(m.k) + q8_blocks(m.W), &pl);
   if (st != CMC_OK) return st;
-  *ctas = pl.ctas;
-  *launches = pl.cm > 0 ? 1 : 2;
+  *ctas = static_cast<int>(units * pl.cm);
   return CMC_OK;
 }
 

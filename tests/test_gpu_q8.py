@@ -574,14 +574,14 @@ def test_step_timeout_is_reported(cuda_device, shape):
 
 
 def test_plan(cuda_device):
-    """Clusters, one CTA a unit, and more units than resident CTAs."""
+    """A cluster per unit, one CTA per unit, and more units than resident CTAs."""
     def plan(B, L, H, k, W):
         return cmc.decode_attn_q8_plan(cmc.CmcDims(B, L, 4 * H, H, 128, max(k, 1), k, W))
-    assert plan(1, 1, 2, 32, 128) == (4, 1)        # five blocks a unit, a cluster of two
-    assert plan(1, 32, 8, 128, 512) == (256, 1)    # one CTA a unit
-    ctas, launches = plan(61, 1, 8, 128, 512)      # 488 units on fewer CTAs
-    assert ctas <= 480 and launches == 2
-    assert plan(64, 32, 8, 128, 512) == (ctas, 2)
+    assert plan(1, 1, 2, 32, 128) == 4        # five blocks a unit: a cluster of two
+    assert plan(1, 1, 1, 0, 32) == 1          # one block
+    assert plan(1, 1, 2, 2048, 2048) == 16    # the largest cluster
+    assert plan(1, 32, 8, 128, 512) == 256
+    assert plan(64, 32, 8, 128, 512) == 64 * 256
 
 
 # ---- refusals of the binding ----
@@ -617,6 +617,6 @@ def test_binding_refusals(cuda_device):
         with pytest.raises(exc):
             call()
     small = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 2, 2, 64, 1, 0, 1), dev, q8=True)
-    small.nbytes = 256
+    small.nbytes = 511
     with pytest.raises(cmc.CmcError):
         attn(q, None, None, kv, scales, pos, workspace=small)
