@@ -44,10 +44,6 @@
 #include "cmc_attn.cuh"
 #include "cmc_q8.cuh"
 
-#ifndef Q8NST
-#define Q8NST 3
-#endif
-#include <stdlib.h>
 namespace cmc {
 
 struct Q8Maps {
@@ -59,6 +55,7 @@ struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the til
   uint8_t* ring_scales;       // [B, L, Hkv, 2, ringS]
   const uint8_t* t1_scales;   // [B, L, Hkv, 2, t1S]
   int ringS, t1S;
+  int units;
   int nb1, nb2;               // blocks of Tier-1, and of the whole ring
   int rope;                   // rotate q and the new key (fused step)
 };                            // cm: CTAs per unit
@@ -66,18 +63,19 @@ struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the til
 // Shared memory of a CTA: the query in fp16, its heads' factors, the rotated new key, the stages'
 // powers of two, the warps' maxima and sums, what a cluster's peers send; then,
 // 1,024-byte aligned, the stages.
-template <int D, int G, int NST>
+template <int D, int G, int NST, bool SOLO>
 struct Q8Smem {
   static constexpr int kV = kQ8Block * D;
   static constexpr int kStage = 2 * kQ8Block * D;
-  static constexpr int kQ = 0;                              // [G][D] fp16
-  static constexpr int kQs = kQ + G * D * 2;                // [8] fp32
-  static constexpr int kKnew = kQs + 32;                    // [D] fp32
-  static constexpr int kScale = kKnew + D * 4;              // [warp][NST][2] words
+  static constexpr int kUnits = SOLO ? kWarps : 1;          // units of the CTA
+  static constexpr int kQ = 0;                              // [unit][G][D] fp16
+  static constexpr int kQs = kQ + kUnits * G * D * 2;       // [unit][8] fp32
+  static constexpr int kKnew = kQs + kUnits * 32;           // [unit][D] fp32
+  static constexpr int kScale = kKnew + kUnits * D * 4;     // [warp][NST][2] words
   static constexpr int kMl = kScale + kWarps * NST * 8;     // [warp][8 maxima, 8 sums]
   static constexpr int kRecv = kMl + kWarps * 64;           // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
-  static constexpr int kSmall = kRecvMl + kMaxClusterCtas * G * 8;
+  static constexpr int kSmall = SOLO ? kMl : kRecvMl + kMaxClusterCtas * G * 8;
   static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
   static_assert(kRecv % 16 == 0, "written by 16 bytes");
 };
@@ -268,10 +266,13 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
   __syncwarp();
 }
 
-template <int D, int G, bool FUSED, int NST>
-__global__ void __maxnreg__(NST == 1 ? 96 : 168)
+// SOLO: a unit per warp, four a CTA, and no barrier but the warp's.
+template <int D, int G, bool FUSED, int NST, bool SOLO>
+// Registers: up to 200 a thread fit two CTAs an SM (with 168 some spill: 2,048 units of 640 keys 54 us
+// and 56), three take 168.
+__global__ void __maxnreg__(NST == 2 ? 168 : 200)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
-  using S = Q8Smem<D, G, NST>;
+  using S = Q8Smem<D, G, NST, SOLO>;
   constexpr int KS = D / 16;      // k-steps of the Q K^T product, m-tiles of O^T
   constexpr int E = D / 32;       // elements of a row a lane has
   constexpr int NGR = G * D / 4;  // groups of four rows of the head dimension of a unit's output
@@ -287,20 +288,28 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem + S::kSmall) + 1023) & ~uintptr_t(1023)) +
                     warp * (NST * S::kStage);
   uint8_t* scale_words = smem + S::kScale + warp * (NST * 8);
-  float* knew = reinterpret_cast<float*>(smem + S::kKnew);
-  float* q_factor = reinterpret_cast<float*>(smem + S::kQs);
+  constexpr int HPW = SOLO ? G : (G + kWarps - 1) / kWarps;  // heads whose query a warp converts:
+  constexpr int HSTEP = SOLO ? 1 : kWarps;                   // h0, h0 + HSTEP, ...
+  const int h0 = SOLO ? 0 : warp;
+  uint8_t* q_rows = smem + S::kQ + (SOLO ? warp * (G * D * 2) : 0);
+  float* knew = reinterpret_cast<float*>(smem + S::kKnew) + (SOLO ? warp * D : 0);
+  float* q_factor = reinterpret_cast<float*>(smem + S::kQs) + (SOLO ? warp * 8 : 0);
   uint64_t* full = full_bar[warp];
 
-  const int cm = p.cm;
-  const int u = cm > 1 ? static_cast<int>(cluster_id()) : static_cast<int>(blockIdx.x);
+  const int cm = SOLO ? 1 : p.cm;
+  const int u = SOLO     ? static_cast<int>(blockIdx.x) * kWarps + warp
+                : cm > 1 ? static_cast<int>(cluster_id())
+                         : static_cast<int>(blockIdx.x);
   const int rank = cm > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  const int g0 = rank * kWarps + warp, step = cm * kWarps;  // the warp's first block, and their distance
+  // the warp's first block, and their distance; which thread speaks for the unit
+  const int g0 = SOLO ? 0 : rank * kWarps + warp, step = SOLO ? 1 : cm * kWarps;
+  const bool first_thread = SOLO ? lane == 0 : tid == 0;
   const int nb_all = p.nb1 + p.nb2;
   const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));  // sequence
 
   if (lane == 0) {
     for (int s = 0; s < NST; ++s) mbar_init(&full[s], 1);  // lane 0's arrive (plus tracked cp.async arrivals)
-    if (warp == 0) attn_abort = 0;
+    if (SOLO || warp == 0) attn_abort = 0;
     if (warp == 1 && cm > 1) {  // the groups this CTA finishes and the heads' (max, sum), from each rank
       const int mine = min(max(NGR - rank * p.slice, 0), p.slice);
       mbar_init(&recv_bar, 1);
@@ -309,7 +318,12 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
     prefetch_map((warp & 1) && p.k > 0 ? &maps.t1 : &maps.ring);
   }
-  __syncthreads();
+  if (SOLO) {
+    __syncwarp();
+    if (u >= p.units) return;
+  } else {
+    __syncthreads();
+  }
   if (cm > 1) cluster_arrive();  // waited for before the first store into a peer
   // Before the grid dependency wait: the first blocks into L2.
   if (lane == 0) {
@@ -329,7 +343,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   // The unit's powers of two: the rows of lane 0 (K) and lane 1 (V).
   const uint8_t* t1_s = p.t1_scales + (2LL * u + (lane & 1)) * p.t1S;
   const uint8_t* ring_s = p.ring_scales + (2LL * u + (lane & 1)) * p.ringS;
-  int n_run = g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;  // blocks of the warp, as far as known before pos
+  int n_run = SOLO ? nb_all : g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;  // blocks of the warp, as far as known before pos
   int jn = g0;  // the next to request
   // Requests the warp's next block into stage s: the codes by TMA, the two words that hold its
   // powers of two by lanes 0 and 1.  Called by the whole warp, converged.
@@ -352,22 +366,22 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll 1
   for (; issued < NST && issued < n_run; ++issued) request(issued);
 
-  // ---- the query, while those are on their way: warp w takes heads w and w + 4, a lane E
-  // neighbouring elements; and the new key ----
+  // ---- the query, while those are on their way (warp w takes heads w and w + 4, a lane E
+  // neighbouring elements), and the new key ----
   const long long pos = ld_pos(p, b);
-  float x[2][E];
+  float x[HPW][E];
 #pragma unroll
-  for (int e = 0; e < 2; ++e)
-    if (warp + kWarps * e < G) load_part<E>(p.q + (static_cast<long long>(u) * G + warp + kWarps * e) * D, lane, x[e]);
+  for (int h = 0; h < HPW; ++h)
+    if (h0 + HSTEP * h < G) load_part<E>(p.q + (static_cast<long long>(u) * G + h0 + HSTEP * h) * D, lane, x[h]);
   uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows
   float kx[E];
   if (FUSED) {
     fresh = load_new<D>(p, u, lane);
-    if (p.rope && warp == kWarps - 1) load_part<E>(p.k_new + static_cast<long long>(u) * D, lane, kx);
+    if (p.rope && (SOLO || warp == kWarps - 1)) load_part<E>(p.k_new + static_cast<long long>(u) * D, lane, kx);
   }
   const SeqState sq = seq_state<FUSED>(p, pos);
   unsigned long long ticket = 0;
-  if (tid == 0 && sq.bad && rank == 0 && u % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+  if (first_thread && sq.bad && rank == 0 && u % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
   if (FUSED && p.rope) {
     float2 cs[E];
     const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + (sq.bad ? 0 : pos));
@@ -379,17 +393,18 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       cs[e] = make_float2(cn, sn);
     }
 #pragma unroll
-    for (int e = 0; e < 2; ++e)
-      if (warp + kWarps * e < G) rotate_part<E>(x[e], cs, lane);
-    if (warp == kWarps - 1) {
+    for (int h = 0; h < HPW; ++h)
+      if (h0 + HSTEP * h < G) rotate_part<E>(x[h], cs, lane);
+    if (SOLO || warp == kWarps - 1) {
       rotate_part<E>(kx, cs, lane);
 #pragma unroll
       for (int e = 0; e < E; ++e) knew[lane * E + e] = kx[e];
     }
   }
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    if (warp + kWarps * h >= G) break;
+  for (int h = 0; h < HPW; ++h) {
+    const int hh = h0 + HSTEP * h;
+    if (hh >= G) break;
     float top = 0.f;  // (a NaN does not count)
 #pragma unroll
     for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[h][e]));
@@ -405,19 +420,20 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     for (int off = 1; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
     const int qc = block_code(__float_as_uint(top));
     const float f = code_factor(qc);
-    uint32_t* to = reinterpret_cast<uint32_t*>(smem + S::kQ + (warp + kWarps * h) * (D * 2)) + lane * (E / 2);
+    uint32_t* to = reinterpret_cast<uint32_t*>(q_rows + hh * (D * 2)) + lane * (E / 2);
 #pragma unroll
     for (int e = 0; e < E; e += 2) to[e / 2] = pack_f16(x[h][e] * f, x[h][e + 1] * f);
-    if (lane == 0) q_factor[warp + kWarps * h] = e8m0_to_f32(qc) * p.scale_log2;
+    if (lane == 0) q_factor[hh] = e8m0_to_f32(qc) * p.scale_log2;
   }
   if (FUSED && lane == 0) s_pos[warp] = pos;  // (so that every warp has it, not only asked for it)
-  __syncthreads();
-  // The last CTA to have read pos[b] advances it (in the end: the count takes a trip to L2).
-  if (FUSED && tid == 0) ticket = atomicAdd(p.tickets + b, 1ull);
+  if (SOLO) __syncwarp();
+  else __syncthreads();
+  // The last to have read pos[b] advances it (in the end: the count takes a trip to L2).
+  if (FUSED && first_thread) ticket = atomicAdd(p.tickets + b, 1ull);
 
   // Live blocks; those that were requested in vain hold no key.
   const int nb = sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
-  n_run = nb > g0 ? (nb - g0 + step - 1) / step : 0;
+  n_run = SOLO ? nb : nb > g0 ? (nb - g0 + step - 1) / step : 0;
   if (n_run < issued) n_run = issued;
   // gq = lane / 4, tq = lane % 4: a thread has columns (heads) 2 tq and 2 tq + 1 of the products
   // (heads >= G are padding: zero queries, never written out).
@@ -427,7 +443,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll
   for (int ks = 0; ks < KS; ++ks) {
     uint2 f = make_uint2(0u, 0u);
-    if (gq < G) f = *reinterpret_cast<const uint2*>(smem + S::kQ + (gq * D + 16 * ks + 4 * tq) * 2);
+    if (gq < G) f = *reinterpret_cast<const uint2*>(q_rows + (gq * D + 16 * ks + 4 * tq) * 2);
     qa[ks][0] = f.x;
     qa[ks][1] = f.y;
   }
@@ -628,10 +644,11 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll
       for (int off = 4; off < 32; off <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
     __syncwarp();  // the warp is done with the stage
-    const float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
     float* ow = reinterpret_cast<float*>(stages);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
+      float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
+      if (SOLO) f = l_run[e] > 0.f ? __fdividef(f, l_run[e]) : 0.f;  // that is all of it
       float* col = ow + (2 * tq + e) * D;
       if (2 * tq + e < G) {
 #pragma unroll
@@ -640,6 +657,24 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
           col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
         }
       }
+    }
+    if (SOLO) {
+      __syncwarp();
+#pragma unroll
+      for (int xi = 0; xi < (NGR + 31) / 32; ++xi) {
+        const int x = lane + 32 * xi;
+        if (x < NGR) {
+          const int hh = (4 * x) / D;
+          const float4 y = *reinterpret_cast<const float4*>(ow + hh * D + ((4 * x) % D ^ (8 * (hh >> 1))));
+          *reinterpret_cast<uint2*>(p.out + static_cast<long long>(u) * (G * D) + 4 * x) =
+              make_uint2(pack_bf16_rn(y.x, y.y), pack_bf16_rn(y.z, y.w));
+        }
+      }
+      if (FUSED && lane == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH)) {
+        if (!sq.bad) p.pos[b] = pos + 1;
+        p.tickets[b] = 0ull;
+      }
+      return;
     }
     if (gq == 0) {
       float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 16 + 2 * tq;
@@ -762,15 +797,22 @@ static bool encode_q8(CUtensorMap* map, const void* base, long long units2, int 
 
 static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
 
+// How a call's units are put on the GPU.  Three variants of the kernel:
+//   wide   a CTA (or cluster) per unit, three stages a warp, two CTAs an SM: few or long units
+//   spread the same with two stages a warp and three CTAs an SM: when the units just miss one
+//          wave of the first
+//   solo   a warp per unit, three stages a warp, two CTAs (eight units) an SM: many short units
 struct Q8Plan {
-  int cm;   // CTAs per unit
-  int nst;  // stages a warp: 1 or 3
+  enum { kWide, kSpread, kSolo } variant;
+  int cm;    // CTAs per unit
+  int ctas;  // grid size
 };
 
-template <int D, int G, bool FUSED, int NST>
+// CTAs of a variant that the device holds at a time.
+template <int D, int G, bool FUSED, int NST, bool SOLO>
 static int resident_q8(int* slots) {
-  constexpr int smem = Q8Smem<D, G, NST>::kBytes;
-  auto kern = attn_q8_kernel<D, G, FUSED, NST>;
+  constexpr int smem = Q8Smem<D, G, NST, SOLO>::kBytes;
+  auto kern = attn_q8_kernel<D, G, FUSED, NST, SOLO>;
   static std::atomic<int> configured[64];  // per device: attribute set and occupancy known (idempotent)
   int dev = 0;
   int st = record_cuda_error(cudaGetDevice(&dev));
@@ -788,21 +830,49 @@ static int resident_q8(int* slots) {
   return CMC_OK;
 }
 
+// The variant and cluster size whose time comes out least by
+//   waves * (3 us + blocks of a warp * P),  P = 1.1 us with eight warps an SM and 1.5 with twelve,
+// a rough fit to the following (us a launch in a graph, G = 4, d = 128; wide with the largest
+// cluster that fits one wave / spread / solo):
+//   16 x  2 blocks 3.4 / 3.4 / 5.8       300 x  3   4.0 /  4.6 /  5.3    512 x  3   7.2 /  7.0 /  5.5
+//   256 x 20       9.3 / 10.4 / 18.7     512 x 10  12.9 / 12.3 / 11.5    768 x 20  29.1 / 25.6 / 23.6
+//   256 x 40      14.8 / 17.0 / 33.9    1024 x 10  24.3 / 20.7 / 14.8   1216 x 20  41.3 / 38.7 / 31.1
+//   312 x 72      40.4 / 30.6 / -       2048 x  6  33.5 / 26.6 / 21.9   2048 x 10  45.5 / 36.5 / 31.7
+//   512 x 72      47.9 / 56.6 / -       2048 x  1  21.3 / 16.4 /  8.1   2048 x 20  65.6 / 60.1 / 53.8
+// (The blocks are those of a full ring: pos is on the device.)
 template <int D, int G, bool FUSED>
 static int plan_q8(long long units, int nb, Q8Plan* pl) {
-  int slots = 0;
-  pl->nst = Q8NST;
-  int st = pl->nst == 1 ? resident_q8<D, G, FUSED, 1>(&slots) : pl->nst == 2 ? resident_q8<D, G, FUSED, 2>(&slots) : resident_q8<D, G, FUSED, 3>(&slots);
+  int wide = 0, spread = 0, solo = 0;  // CTAs resident at a time
+  int st = resident_q8<D, G, FUSED, 3, false>(&wide);
+  if (st == CMC_OK) st = resident_q8<D, G, FUSED, 2, false>(&spread);
+  if (st == CMC_OK) st = resident_q8<D, G, FUSED, 3, true>(&solo);
   if (st != CMC_OK) return st;
-  pl->cm = 1;
-  const long long most = (nb + kWarps - 1) / kWarps;  // a block for every warp
-  while (pl->cm < kMaxClusterCtas && 2 * pl->cm <= most && units * pl->cm * 2 <= slots) pl->cm *= 2;
-  if (getenv("Q8CM")) pl->cm = atoi(getenv("Q8CM"));
+  // in tenths of a microsecond
+  auto cost = [&](long long ctas, int slots, int blocks, int per_block) {
+    return (ctas + slots - 1) / slots * (30 + static_cast<long long>(blocks) * per_block);
+  };
+  const long long quads = (units + kWarps - 1) / kWarps;
+  *pl = {Q8Plan::kWide, 1, static_cast<int>(units)};
+  long long best = cost(units, wide, (nb + kWarps - 1) / kWarps, 11);
+  for (int cm = 2; cm <= kMaxClusterCtas && kWarps * cm / 2 < nb; cm *= 2) {  // a cluster's merge: 0.3 us
+    const long long t = cost(units * cm, wide, (nb + kWarps * cm - 1) / (kWarps * cm), 11) + 3;
+    if (t < best) {
+      best = t;
+      *pl = {Q8Plan::kWide, cm, static_cast<int>(units * cm)};
+    }
+  }
+  long long t = cost(units, spread, (nb + kWarps - 1) / kWarps, 15);
+  if (t < best) {
+    best = t;
+    *pl = {Q8Plan::kSpread, 1, static_cast<int>(units)};
+  }
+  t = cost(quads, solo, nb, 11);
+  if (t < best) *pl = {Q8Plan::kSolo, 1, static_cast<int>(quads)};
   return CMC_OK;
 }
 
-template <int D, int G, bool FUSED, int NST>
-static int launch_q8(const Q8Maps& maps, AttnQ8Params p, const Q8Plan& pl, long long units, cudaStream_t s) {
+template <int D, int G, bool FUSED, int NST, bool SOLO>
+static int launch_q8(const Q8Maps& maps, AttnQ8Params p, const Q8Plan& pl, cudaStream_t s) {
   p.cm = pl.cm;
   p.slice = pl.cm > 1 ? (G * D / 4 + pl.cm - 1) / pl.cm : 0;
   cudaLaunchAttribute attr[2];
@@ -813,13 +883,13 @@ static int launch_q8(const Q8Maps& maps, AttnQ8Params p, const Q8Plan& pl, long 
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(units * pl.cm));
+  cfg.gridDim = dim3(static_cast<unsigned>(pl.ctas));
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = Q8Smem<D, G, NST>::kBytes;
+  cfg.dynamicSmemBytes = Q8Smem<D, G, NST, SOLO>::kBytes;
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = pl.cm > 1 ? 2 : 1;
-  return record_cuda_error(cudaLaunchKernelEx(&cfg, attn_q8_kernel<D, G, FUSED, NST>, maps, p));
+  return record_cuda_error(cudaLaunchKernelEx(&cfg, attn_q8_kernel<D, G, FUSED, NST, SOLO>, maps, p));
 }
 
 // Calls F<D, G>::run(args...) for the call's head dimension and group size.
@@ -853,9 +923,11 @@ struct LaunchQ8 {
     Q8Plan pl;
     int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
     if (st != CMC_OK) return st;
-    return pl.nst == 1 ? launch_q8<D, G, FUSED, 1>(maps, p, pl, units, s)
-         : pl.nst == 2 ? launch_q8<D, G, FUSED, 2>(maps, p, pl, units, s)
-                       : launch_q8<D, G, FUSED, 3>(maps, p, pl, units, s);
+    switch (pl.variant) {
+      case Q8Plan::kSolo: return launch_q8<D, G, FUSED, 3, true>(maps, p, pl, s);
+      case Q8Plan::kSpread: return launch_q8<D, G, FUSED, 2, false>(maps, p, pl, s);
+      default: return launch_q8<D, G, FUSED, 3, false>(maps, p, pl, s);
+    }
   }
   static int run(bool fused, const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
     return fused ? go<true>(maps, p, units, s) : go<false>(maps, p, units, s);
@@ -902,6 +974,7 @@ static int run_attention_q8(const void* q, const void* t1_kv, const void* t1_sca
   p.tickets = reinterpret_cast<unsigned long long*>(ws + kWsHeader);
   p.B = m.B; p.L = m.L; p.Hq = m.Hq; p.Hkv = m.Hkv; p.N = m.N; p.k = m.k; p.W = m.W;
   p.LH = m.L * m.Hkv;
+  p.units = static_cast<int>(units);
   p.nb1 = nb1;
   p.nb2 = nb2;
   const float sc = scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(m.d));
@@ -959,7 +1032,7 @@ int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas) {
   Q8Plan pl;
   st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, q8_blocks(m.k) + q8_blocks(m.W), &pl);
   if (st != CMC_OK) return st;
-  *ctas = static_cast<int>(units * pl.cm);
+  *ctas = pl.ctas;
   return CMC_OK;
 }
 

@@ -581,7 +581,8 @@ def test_plan(cuda_device):
     assert plan(1, 1, 1, 0, 32) == 1          # one block
     assert plan(1, 1, 2, 2048, 2048) == 16    # the largest cluster
     assert plan(1, 32, 8, 128, 512) == 256
-    assert plan(64, 32, 8, 128, 512) == 64 * 256
+    assert plan(64, 1, 8, 30, 64) == 128      # 512 short units: a warp each, four a CTA
+    assert plan(64, 1, 8, 256, 2048) == 512
 
 
 # ---- refusals of the binding ----
