@@ -148,71 +148,113 @@ dequantize_kernel(const uint8_t* __restrict__ kv, const uint8_t* __restrict__ sc
   }
 }
 
-// The unfused append: one warp per (unit, K or V) writes the token's codes; where
-// its block's power of two changes it rounds the block's other tokens again.
-// One CTA per sequence, or a cluster of up to 8: pos is advanced after a barrier
-// over every thread that reads it.
+// The unfused append.  A warp appends to a unit at a time, half of it K's row and half V's,
+// d / 16 neighbouring elements a lane; the rows and powers of two of up to kAppendUnits units
+// are requested together.  Where a block's power of two changes (or is set anew, at the
+// block's first slot), the warp takes the whole block into registers, 16 bytes a lane
+// and load, all in flight together.  One CTA per sequence, or a cluster of up to 8: pos is advanced
+// after a barrier over every thread that reads it.
 constexpr int kAppendThreads = 512;
 constexpr int kAppendWarps = kAppendThreads / 32;
+constexpr int kAppendUnits = 2;
 constexpr int kMaxAppendCtas = 8;
 
+// A block's other tokens: their largest value (fp32 bits) where the byte is set anew, and their codes
+// for the byte that `top` (the new row's largest, fp32 bits) then gives.  `others`: the rows
+// that hold another token.  Returns the byte.
 template <int D>
-__global__ void __launch_bounds__(kAppendThreads)
-window_append_q8_kernel(uint8_t* __restrict__ ring, uint8_t* __restrict__ scales, int64_t* pos,
-                        const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new, int LH,
-                        int W, int S, int ctas) {
-  constexpr int E = D / 32;  // elements of the row a lane holds
+__device__ __forceinline__ int recode_block(uint8_t* block, uint32_t others, uint32_t top, int c_old, bool anew,
+                                            int lane) {
+  constexpr int CPR = D / 16;  // 16-byte chunks of a row
+  uint4 x[CPR];                // chunks lane, lane + 32, ... of the block
+#pragma unroll
+  for (int e = 0; e < CPR; ++e) {
+    x[e] = make_uint4(0u, 0u, 0u, 0u);
+    if ((others >> ((lane + 32 * e) / CPR)) & 1u) x[e] = reinterpret_cast<const uint4*>(block)[lane + 32 * e];
+  }
+  int c = max(block_code(top), c_old);
+  if (anew) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int e = 0; e < CPR; ++e) m = max_codes16(m, x[e]);
+    c = block_code(max(top, __reduce_max_sync(0xffffffffu, held_bits(m, c_old))));
+  }
+  if (c != c_old) {
+    const float f = recode_factor(c_old, c);
+#pragma unroll
+    for (int e = 0; e < CPR; ++e)
+      if ((others >> ((lane + 32 * e) / CPR)) & 1u) reinterpret_cast<uint4*>(block)[lane + 32 * e] = recode16(x[e], f);
+  }
+  return c;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kAppendThreads, 2)
+window_append_q8_kernel(uint8_t* ring, uint8_t* scales, int64_t* pos, const uint16_t* __restrict__ k_new,
+                        const uint16_t* __restrict__ v_new, int LH, int W, int S, int ctas) {
+  constexpr int E = D / 16;  // elements a lane has of its row
   pdl_wait();
   pdl_trigger();
   const int b = static_cast<int>(blockIdx.x) / ctas;
   const int rank = static_cast<int>(blockIdx.x) - b * ctas;
   const int lane = threadIdx.x & 31;
+  const int half = lane >> 4;
   const long long pb = *static_cast<volatile const int64_t*>(pos + b);
-  if (pb >= 0) {
-    const int slot = (pb >> 32) == 0
-                         ? static_cast<int>(static_cast<unsigned>(pb) % static_cast<unsigned>(W))
-                         : static_cast<int>(pb % W);
-    const int r0 = slot / kQ8Block * kQ8Block;
-    const int live = static_cast<int>(pb < W ? pb : W);  // slots that hold a token
-    const bool other = r0 + lane < live && r0 + lane != slot;  // this lane's row of the block does
-    for (int x = rank * kAppendWarps + static_cast<int>(threadIdx.x >> 5); x < 2 * LH; x += ctas * kAppendWarps) {
-      const long long u = static_cast<long long>(b) * LH + (x >> 1);
-      const long long uw = 2 * u + (x & 1);
-      float v[4] = {0.f, 0.f, 0.f, 0.f};
-      if (D == 128) {
-        const uint2 w = reinterpret_cast<const uint2*>((x & 1) ? v_new : k_new)[u * 32 + lane];
-        v[0] = bf16lo_to_f32(w.x); v[1] = bf16hi_to_f32(w.x);
-        v[2] = bf16lo_to_f32(w.y); v[3] = bf16hi_to_f32(w.y);
-      } else {
-        const uint32_t w = reinterpret_cast<const uint32_t*>((x & 1) ? v_new : k_new)[u * 32 + lane];
-        v[0] = bf16lo_to_f32(w); v[1] = bf16hi_to_f32(w);
+  const int slot = pb < 0           ? 0
+                   : (pb >> 32) == 0 ? static_cast<int>(static_cast<unsigned>(pb) % static_cast<unsigned>(W))
+                                     : static_cast<int>(pb % W);
+  const int r = slot & (kQ8Block - 1);
+  const int live = static_cast<int>(pb < W ? pb : W) - (slot - r);  // tokens from the block's first slot on
+  const uint32_t others = (live >= 32 ? 0xFFFFFFFFu : live <= 0 ? 0u : (1u << live) - 1u) & ~(1u << r);
+  for (int x0 = rank * kAppendWarps + static_cast<int>(threadIdx.x >> 5); pb >= 0 && x0 < LH;
+       x0 += ctas * kAppendWarps * kAppendUnits) {
+    uint4 row[kAppendUnits];
+    int old[kAppendUnits];
+#pragma unroll
+    for (int q = 0; q < kAppendUnits; ++q) {
+      const int x = x0 + q * ctas * kAppendWarps;
+      row[q] = make_uint4(0u, 0u, 0u, 0u);
+      old[q] = 0;
+      if (x < LH) {
+        const long long u = static_cast<long long>(b) * LH + x;
+        const uint16_t* from = (half ? v_new : k_new) + u * D + (lane & 15) * E;
+        if (D == 128) {
+          row[q] = *reinterpret_cast<const uint4*>(from);
+        } else {
+          const uint2 w = *reinterpret_cast<const uint2*>(from);
+          row[q] = make_uint4(w.x, w.y, 0u, 0u);
+        }
+        old[q] = scales[(2 * u + half) * S + slot / kQ8Block];
       }
+    }
+#pragma unroll
+    for (int q = 0; q < kAppendUnits; ++q) {
+      const int x = x0 + q * ctas * kAppendWarps;
+      if (x >= LH) break;
+      const long long u = static_cast<long long>(b) * LH + x;
+      uint8_t* block = ring + (2 * u * W + slot - r) * D;  // K's; V's is W rows on
+      float v[8];
+      unpack8(row[q], v);
       uint32_t top = 0u;
 #pragma unroll
       for (int e = 0; e < E; ++e) top = max(top, finite_bits(v[e]));
-      top = __reduce_max_sync(0xffffffffu, top);
-      uint8_t* sc = scales + uw * S + slot / kQ8Block;
-      const int c_old = *sc;
-      uint4* mine = reinterpret_cast<uint4*>(ring + (uw * W + r0 + lane) * D);  // this lane's row
-      int c;
-      if (slot == r0) {  // the block's power of two is set anew
-        uint32_t m = 0u;
-        if (other)
-          for (int q = 0; q < D / 16; ++q) m = max_codes16(m, mine[q]);
-        c = block_code(max(top, __reduce_max_sync(0xffffffffu, held_bits(m, c_old))));
-      } else {
-        c = max(block_code(top), c_old);
-      }
-      if (c != c_old && other) {
-        const float f = recode_factor(c_old, c);
-        for (int q = 0; q < D / 16; ++q) mine[q] = recode16(mine[q], f);
+#pragma unroll
+      for (int off = 1; off < 16; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const int c_old = old[q];
+      int c = max(block_code(top), c_old);
+      if (r == 0 || __any_sync(0xffffffffu, c != c_old)) {
+        const uint32_t tk = __shfl_sync(0xffffffffu, top, 0), tv = __shfl_sync(0xffffffffu, top, 16);
+        const int ok = __shfl_sync(0xffffffffu, c_old, 0), ov = __shfl_sync(0xffffffffu, c_old, 16);
+        const int ck = recode_block<D>(block, others, tk, ok, r == 0, lane);
+        const int cv = recode_block<D>(block + static_cast<long long>(W) * D, others, tv, ov, r == 0, lane);
+        c = half ? cv : ck;
       }
       const float f = code_factor(c);
-      uint8_t* row = ring + (uw * W + slot) * D;
-      if (D == 128) reinterpret_cast<uint32_t*>(row)[lane] = encode4(v[0], v[1], v[2], v[3], f);
-      else reinterpret_cast<uint16_t*>(row)[lane] = static_cast<uint16_t>(e4m3_pair(scaled(v[0], f), scaled(v[1], f)));
-      __syncwarp();  // every lane has read it
-      if (lane == 0) *sc = static_cast<uint8_t>(c);
+      uint8_t* to = block + (static_cast<long long>(half) * W + r) * D + (lane & 15) * E;
+      const uint32_t w0 = encode4(v[0], v[1], v[2], v[3], f);
+      if (D == 128) *reinterpret_cast<uint2*>(to) = make_uint2(w0, encode4(v[4], v[5], v[6], v[7], f));
+      else *reinterpret_cast<uint32_t*>(to) = w0;
+      if ((lane & 15) == 0 && c != c_old) scales[(2 * u + half) * S + slot / kQ8Block] = static_cast<uint8_t>(c);
     }
   }
   // every thread that reads pos[b] has read it
@@ -301,7 +343,7 @@ int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos, const v
   const cmc_dims& m = *dims;
   const int LH = m.L * m.Hkv;
   int ctas = 1;
-  while (ctas < kMaxAppendCtas && 2LL * LH > static_cast<long long>(ctas) * kAppendWarps) ctas *= 2;
+  while (ctas < kMaxAppendCtas && LH > static_cast<long long>(ctas) * kAppendWarps) ctas *= 2;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
