@@ -339,6 +339,7 @@ class DecodeWorkspace:
         self.dims = dims
         self.nbytes = n
         self.buf = torch.zeros(n, dtype=torch.uint8, device=device)
+        self.ptr = self.buf.data_ptr()
 
     def status(self, clear: bool = True) -> int:
         """CMC_DEVFLAG_* bits raised by kernels since the last clear (synchronises)."""
@@ -573,9 +574,8 @@ def _elsewhere(index: int, fn, *args) -> int:
 
 # Shapes that go together, and the sizes that they give: what a call can tell from
 # its tensors' shapes alone is worked out once for each combination of them.  What
-# is left for every call are the types, layouts and devices.  (A decode step's call
-# takes 10 us on the host with this and took 21 without, more than the GPU needs for
-# it up to some 60 MB of cache.)
+# is left for every call are the types, layouts and devices.  (The host side of a
+# decode step's call takes longer than the GPU needs for some 60 MB of cache.)
 _shapes_cache: Dict[Tuple, Tuple] = {}
 _SHAPES_MOST = 4096  # combinations kept; beyond, each call works its own out
 
@@ -589,7 +589,8 @@ def _kept(key: Tuple, value: Tuple) -> Tuple:
 def _as(dtype: torch.dtype, index: int, *tensors) -> bool:
     """Whether all tensors (None: none) have this type and device and are contiguous."""
     for t in tensors:
-        if t is not None and not (t.dtype is dtype and t.is_contiguous() and t.get_device() == index):
+        if t is not None and (t.dtype is not dtype or t.get_device() != index
+                              or not t.is_contiguous()):
             return False
     return True
 
@@ -619,17 +620,16 @@ def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor]
         kept = _kept(key, ((B, L, Hkv, 2, rows, d), (B, L, Hkv, 2, q8_scale_bytes(rows)), dims,
                            ctypes.byref(dims)))
     shape, sshape, _, dims = kept
+    given = out_kv is not None or out_scales is not None
     if out_kv is None:
         out_kv = torch.empty(shape, dtype=_E4M3, device=dev)
     if out_scales is None:
         out_scales = torch.empty(sshape, dtype=_E8M0, device=dev)
-    if not (_as(_E4M3, index, out_kv) and _as(_E8M0, index, out_scales) and out_kv.shape == shape
-            and out_scales.shape == sshape):
-        _need_q8(out_kv, out_scales, "out", dev)
+    if given and _need_q8(out_kv, out_scales, "out", dev) != shape:
         raise ValueError(f"out_kv must be {shape}")
     fn = lib().cmc_quantize_cache
-    args = (k.data_ptr(), v.data_ptr(), _p(idx), _p(count), dims, out_kv.data_ptr(), out_scales.data_ptr(), 0 if workspace is None else _p(workspace.buf),
-            _raw_stream(index))
+    args = (k.data_ptr(), v.data_ptr(), _p(idx), _p(count), dims, out_kv.data_ptr(),
+            out_scales.data_ptr(), 0 if workspace is None else workspace.ptr, _raw_stream(index))
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_quantize_cache")
@@ -654,18 +654,19 @@ def dequantize_cache(kv: torch.Tensor, scales: torch.Tensor, idx: Optional[torch
         dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
         kept = _kept(key, ((B, L, Hkv, rows, d), dims, ctypes.byref(dims)))
     want, _, dims = kept
-    if out_k is None:
-        out_k = torch.empty(want, dtype=torch.bfloat16, device=dev)
-    if out_v is None:
-        out_v = torch.empty(want, dtype=torch.bfloat16, device=dev)
-    if not (_as(torch.bfloat16, index, out_k, out_v) and out_k.shape == want and out_v.shape == want):
-        for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+    outs = []
+    for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+        if t is None:
+            t = torch.empty(want, dtype=torch.bfloat16, device=dev)
+        else:
             _need(t, name, torch.bfloat16, 5, dev)
-            if tuple(t.shape) != want:
+            if t.shape != want:
                 raise ValueError(f"{name} must be {want}")
+        outs.append(t)
+    out_k, out_v = outs
     fn = lib().cmc_dequantize_cache
-    args = (kv.data_ptr(), scales.data_ptr(), _p(idx), dims, out_k.data_ptr(), out_v.data_ptr(), 0 if workspace is None else _p(workspace.buf),
-            _raw_stream(index))
+    args = (kv.data_ptr(), scales.data_ptr(), _p(idx), dims, out_k.data_ptr(), out_v.data_ptr(),
+            0 if workspace is None else workspace.ptr, _raw_stream(index))
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_dequantize_cache")
@@ -684,7 +685,7 @@ def window_append_q8(ring_kv: torch.Tensor, ring_scales: torch.Tensor, pos: torc
     if (_as(_E8M0, index, ring_scales) and _as(torch.int64, index, pos)
             and _as(torch.bfloat16, index, k_new, v_new)):
         key = ("append", ring_kv.shape, ring_scales.shape, pos.shape, k_new.shape, v_new.shape)
-    kept = _shapes_cache.get(key)
+    kept = _shapes_cache.get(key) if key else None
     if kept is None:
         B, L, Hkv, _, W, d = _need_q8(ring_kv, ring_scales, "ring", dev)
         _need(pos, "pos", torch.int64, 1, dev)
@@ -694,8 +695,8 @@ def window_append_q8(ring_kv: torch.Tensor, ring_scales: torch.Tensor, pos: torc
         dims = CmcDims(B, L, Hkv, Hkv, d, 1, 0, W)
         kept = _kept(key, (dims, ctypes.byref(dims)))
     fn = lib().cmc_window_append_q8
-    args = (ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), kept[1],
-            _raw_stream(index))
+    args = (ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(),
+            v_new.data_ptr(), kept[1], _raw_stream(index))
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_window_append_q8")
@@ -728,38 +729,34 @@ def _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new) -> 
     return dims
 
 
-def _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, out, workspace):
-    """(device index, dims by reference, output, workspace) of an attention call."""
-    key = None
-    index = q.get_device() if isinstance(q, torch.Tensor) else -1
-    if (index >= 0 and _as(torch.bfloat16, index, q) and _as(_E4M3, index, ring_kv, tier1_kv)
-            and _as(_E8M0, index, ring_scales, tier1_scales) and _as(torch.int64, index, pos)
-            and (new is None or _as(torch.bfloat16, index, *new))):
-        key = ("attend", q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
-               None if tier1_kv is None else tier1_kv.shape,
-               None if tier1_scales is None else tier1_scales.shape,
-               None if new is None else (new[0].shape, new[1].shape))
-    kept = _shapes_cache.get(key)
-    if kept is None:
-        dims = _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new)
-        kept = _kept(key, (dims, ctypes.byref(dims), ("q8", dims.B)))  # a workspace goes by B
-    dims, ref, sizes = kept
-    if out is None:
-        out = torch.empty_like(q)
-    elif not _as(torch.bfloat16, index, out) or out.shape != q.shape:
-        _need(out, "out", torch.bfloat16, 4, q.device)
+def _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, name) -> Tuple:
+    """Checks the tensors of an attention call over 8-bit caches one by one; what the call keeps for
+    shapes like these: (the library function, dims by reference, dims)."""
+    dims = _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new)
+    key = (q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
+           None if tier1_kv is None else tier1_kv.shape,
+           None if tier1_scales is None else tier1_scales.shape)
+    return _kept(key if new is None else key + (new[0].shape, new[1].shape),
+                 (getattr(lib(), name), ctypes.byref(dims), dims))
+
+
+def _attn_q8_workspace(index: int, dims: CmcDims, q: torch.Tensor) -> DecodeWorkspace:
+    """The workspace of a call that is given none: one per stream and batch size."""
+    # A call that is being captured gets a workspace of its graph's own: the kept ones
+    # are zero-filled once, outside of it, and other calls use them.
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return DecodeWorkspace(dims, q.device, q8=True)
+    key = ("q8", index, _raw_stream(index), dims.B)
+    ws = _ws_cache.get(key)
+    if ws is None:
+        ws = _ws_cache[key] = DecodeWorkspace(dims, q.device, q8=True)
+    return ws
+
+
+def _check_out(out: torch.Tensor, q: torch.Tensor) -> None:
+    _need(out, "out", torch.bfloat16, 4, q.device)
+    if out.shape != q.shape:
         raise ValueError("out must have the shape of q")
-    if workspace is None:
-        # A call that is being captured gets a workspace of its graph's own: the
-        # kept ones are zero-filled once, outside of it, and other calls use them.
-        if torch._C._cuda_isCurrentStreamCapturing():
-            workspace = DecodeWorkspace(dims, q.device, q8=True)
-        else:
-            stream = _raw_stream(index)
-            workspace = _ws_cache.get((index, stream, sizes))
-            if workspace is None:
-                workspace = _ws_cache[(index, stream, sizes)] = DecodeWorkspace(dims, q.device, q8=True)
-    return index, ref, out, workspace
 
 
 @_ranged
@@ -771,11 +768,28 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a
     DecodeWorkspace(dims, device, q8=True); without one the call keeps one per stream and
     batch size, and a captured call gets one of its own, zero-filled at every replay."""
-    index, dims, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
-                                         out, workspace)
-    fn = lib().cmc_two_tier_decode_attn_q8
-    args = (q.data_ptr(), _p(tier1_kv), _p(tier1_scales), ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), dims, _scale(scale), out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
-            _raw_stream(index))
+    kept, index = None, -1
+    if isinstance(q, torch.Tensor) and isinstance(ring_kv, torch.Tensor):
+        index = q.get_device()
+        if (index >= 0 and _as(torch.bfloat16, index, q) and _as(_E4M3, index, ring_kv, tier1_kv)
+                and _as(_E8M0, index, ring_scales, tier1_scales) and _as(torch.int64, index, pos)):
+            kept = _shapes_cache.get((q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
+                                      None if tier1_kv is None else tier1_kv.shape,
+                                      None if tier1_scales is None else tier1_scales.shape))
+    if kept is None:
+        kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
+                             "cmc_two_tier_decode_attn_q8")
+    fn, ref, dims = kept
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_out(out, q)
+    if workspace is None:
+        workspace = _attn_q8_workspace(index, dims, q)
+    args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
+            0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
+            ring_scales.data_ptr(), pos.data_ptr(), ref, 0.0 if scale is None else scale,
+            out.data_ptr(), workspace.ptr, workspace.nbytes, _raw_stream(index))
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_two_tier_decode_attn_q8")
@@ -791,13 +805,35 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     attend; see cmc_decode_step_q8.  Updates ring_kv, ring_scales and pos in place.
     ``rope_theta`` and ``rope_offset`` as for :func:`decode_step`, ``workspace`` as for
     :func:`two_tier_decode_attn_q8`."""
-    if rope_theta is not None and not rope_theta > 0:
+    if rope_theta is None:
+        rope_theta = 0.0
+    elif not rope_theta > 0:
         raise ValueError("rope_theta must be positive")
-    index, dims, out, ws = _attn_q8_args(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos,
-                                         (k_new, v_new), out, workspace)
-    fn = lib().cmc_decode_step_q8
-    args = (q.data_ptr(), _p(tier1_kv), _p(tier1_scales), ring_kv.data_ptr(), ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), dims, _scale(scale), 0.0 if rope_theta is None else float(rope_theta), int(rope_offset), out.data_ptr(), ws.buf.data_ptr(), ws.nbytes,
-            _raw_stream(index))
+    kept, index = None, -1
+    if isinstance(q, torch.Tensor) and isinstance(k_new, torch.Tensor):
+        index = q.get_device()
+        if (index >= 0 and _as(torch.bfloat16, index, q, k_new, v_new)
+                and _as(_E4M3, index, ring_kv, tier1_kv)
+                and _as(_E8M0, index, ring_scales, tier1_scales) and _as(torch.int64, index, pos)):
+            kept = _shapes_cache.get((q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
+                                      None if tier1_kv is None else tier1_kv.shape,
+                                      None if tier1_scales is None else tier1_scales.shape,
+                                      k_new.shape, v_new.shape))
+    if kept is None:
+        kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, (k_new, v_new),
+                             "cmc_decode_step_q8")
+    fn, ref, dims = kept
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_out(out, q)
+    if workspace is None:
+        workspace = _attn_q8_workspace(index, dims, q)
+    args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
+            0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
+            ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ref,
+            0.0 if scale is None else scale, rope_theta, rope_offset, out.data_ptr(),
+            workspace.ptr, workspace.nbytes, _raw_stream(index))
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_decode_step_q8")
