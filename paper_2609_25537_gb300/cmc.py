@@ -743,10 +743,12 @@ def _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, nam
 def _attn_q8_workspace(index: int, dims: CmcDims, q: torch.Tensor) -> DecodeWorkspace:
     """The workspace of a call that is given none: one per stream and batch size."""
     # A call that is being captured gets a workspace of its graph's own: the kept ones
-    # are zero-filled once, outside of it, and other calls use them.
-    if torch._C._cuda_isCurrentStreamCapturing():
+    # are zero-filled once, outside of it, and other calls use them.  (The default
+    # stream, 0, is never captured.)
+    stream = _raw_stream(index)
+    if stream and torch._C._cuda_isCurrentStreamCapturing():
         return DecodeWorkspace(dims, q.device, q8=True)
-    key = ("q8", index, _raw_stream(index), dims.B)
+    key = ("q8", index, stream, dims.B)
     ws = _ws_cache.get(key)
     if ws is None:
         ws = _ws_cache[key] = DecodeWorkspace(dims, q.device, q8=True)

@@ -808,25 +808,40 @@ struct Q8Plan {
   int ctas;  // grid size
 };
 
-// CTAs of a variant that the device holds at a time.
+// CTAs of a variant that fit an SM of the current device.
 template <int D, int G, bool FUSED, int NST, bool SOLO>
-static int resident_q8(int* slots) {
+static int per_sm_q8(int* per_sm) {
   constexpr int smem = Q8Smem<D, G, NST, SOLO>::kBytes;
   auto kern = attn_q8_kernel<D, G, FUSED, NST, SOLO>;
-  static std::atomic<int> configured[64];  // per device: attribute set and occupancy known (idempotent)
+  int st = record_cuda_error(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  if (st != CMC_OK) return st;
+  st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(per_sm, kern, kThreads, smem));
+  if (st == CMC_OK && *per_sm < 1) *per_sm = 1;
+  return st;
+}
+
+// CTAs of the three variants that the current device holds at a time; looked up once per device
+// (idempotent), and kept as 20 bits each.
+template <int D, int G, bool FUSED>
+static int resident_q8(int* wide, int* spread, int* solo) {
+  static std::atomic<uint64_t> known[64];
   int dev = 0;
   int st = record_cuda_error(cudaGetDevice(&dev));
   if (st != CMC_OK) return st;
-  int per_sm = (dev >= 0 && dev < 64) ? configured[dev].load(std::memory_order_acquire) : 0;
-  if (per_sm <= 0) {
-    st = record_cuda_error(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  uint64_t v = dev >= 0 && dev < 64 ? known[dev].load(std::memory_order_acquire) : 0;
+  if (v == 0) {
+    int a = 0, b = 0, c = 0;
+    st = per_sm_q8<D, G, FUSED, 3, false>(&a);
+    if (st == CMC_OK) st = per_sm_q8<D, G, FUSED, 2, false>(&b);
+    if (st == CMC_OK) st = per_sm_q8<D, G, FUSED, 3, true>(&c);
     if (st != CMC_OK) return st;
-    st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, kThreads, smem));
-    if (st != CMC_OK) return st;
-    if (per_sm < 1) per_sm = 1;
-    if (dev >= 0 && dev < 64) configured[dev].store(per_sm, std::memory_order_release);
+    const uint64_t sms = static_cast<uint64_t>(sm_count());
+    v = (a * sms) | (b * sms) << 20 | (c * sms) << 40;
+    if (dev >= 0 && dev < 64) known[dev].store(v, std::memory_order_release);
   }
-  *slots = per_sm * sm_count();
+  *wide = static_cast<int>(v & 0xFFFFF);
+  *spread = static_cast<int>((v >> 20) & 0xFFFFF);
+  *solo = static_cast<int>((v >> 40) & 0xFFFFF);
   return CMC_OK;
 }
 
@@ -843,9 +858,7 @@ static int resident_q8(int* slots) {
 template <int D, int G, bool FUSED>
 static int plan_q8(long long units, int nb, Q8Plan* pl) {
   int wide = 0, spread = 0, solo = 0;  // CTAs resident at a time
-  int st = resident_q8<D, G, FUSED, 3, false>(&wide);
-  if (st == CMC_OK) st = resident_q8<D, G, FUSED, 2, false>(&spread);
-  if (st == CMC_OK) st = resident_q8<D, G, FUSED, 3, true>(&solo);
+  const int st = resident_q8<D, G, FUSED>(&wide, &spread, &solo);
   if (st != CMC_OK) return st;
   // in tenths of a microsecond
   auto cost = [&](long long ctas, int slots, int blocks, int per_block) {
@@ -872,7 +885,7 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
 }
 
 template <int D, int G, bool FUSED, int NST, bool SOLO>
-static int launch_q8(const Q8Maps& maps, AttnQ8Params p, const Q8Plan& pl, cudaStream_t s) {
+static int launch_q8(const Q8Maps& maps, AttnQ8Params& p, const Q8Plan& pl, cudaStream_t s) {
   p.cm = pl.cm;
   p.slice = pl.cm > 1 ? (G * D / 4 + pl.cm - 1) / pl.cm : 0;
   cudaLaunchAttribute attr[2];
@@ -919,7 +932,7 @@ struct PlanQ8 {
 template <int D, int G>
 struct LaunchQ8 {
   template <bool FUSED>
-  static int go(const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
+  static int go(const Q8Maps& maps, AttnQ8Params& p, long long units, cudaStream_t s) {
     Q8Plan pl;
     int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
     if (st != CMC_OK) return st;
@@ -929,7 +942,7 @@ struct LaunchQ8 {
       default: return launch_q8<D, G, FUSED, 3, false>(maps, p, pl, s);
     }
   }
-  static int run(bool fused, const Q8Maps& maps, const AttnQ8Params& p, long long units, cudaStream_t s) {
+  static int run(bool fused, const Q8Maps& maps, AttnQ8Params& p, long long units, cudaStream_t s) {
     return fused ? go<true>(maps, p, units, s) : go<false>(maps, p, units, s);
   }
 };

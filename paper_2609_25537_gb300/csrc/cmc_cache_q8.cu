@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include "cmc_attn.cuh"
 #include "cmc_q8.cuh"
 
 namespace cmc {
@@ -11,87 +12,165 @@ namespace cmc {
 constexpr int kRowThreads = 128;  // four warps, each with blocks of rows of its own
 constexpr int kRowWarps = kRowThreads / 32;
 
-// One warp quantises a block of 32 rows of one unit's K or V at a time: it holds
-// the whole block in registers (8 KB at d = 128, 16 loads of 16 bytes a lane, all
-// in flight together), so that the bf16 rows are read once for their maximum
-// and their codes.
-template <int D>
+// A warp quantises blocks of 32 rows of one unit's K or V, one after another, from a ring of
+// NST stages in shared memory that bulk copies fill ahead of it: one copy a block, or one a
+// row where an index gathers them; rows that hold no token are not read.  A block goes
+// through registers once, for its maximum and for its codes.
+//
+// HBM bounds it where there is enough to do: 1,024 rows of 256 units 33.0 us (90 % of the copy
+// rate), 16,384 rows of 64 units 127 us (94 %).  At d = 128 an SM holds 20 warps with one stage
+// each and 12 with two: one stage where every block then has a warp of its own (2,048 blocks
+// 4.9 us, 6.2 with two), else two (20,480 blocks, a third of their rows with a token, 24.4 us,
+// 28.7 with one).
+// Four bf16 values times a power of two (bf16, in both halves of f2) to codes.  The products are exact
+// but for those below bf16's smallest, which give 0 either way.
+__device__ __forceinline__ uint32_t encode4_bf16(uint32_t a, uint32_t b, uint32_t f2) {
+  asm("mul.rn.bf16x2 %0, %0, %1;\n" : "+r"(a) : "r"(f2));
+  asm("mul.rn.bf16x2 %0, %0, %1;\n" : "+r"(b) : "r"(f2));
+  return e4m3_pair(bf16lo_to_f32(a), bf16hi_to_f32(a)) | (e4m3_pair(bf16lo_to_f32(b), bf16hi_to_f32(b)) << 16);
+}
+
+template <int D, int NST>
 __global__ void __launch_bounds__(kRowThreads)
-quantize_kernel(const uint4* __restrict__ bank_k, const uint4* __restrict__ bank_v,
+quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict__ bank_v,
                 const int32_t* __restrict__ idx, const int64_t* __restrict__ count,
                 uint8_t* __restrict__ kv, uint8_t* __restrict__ scales, uint32_t* status,
                 long long jobs, int nb, int LH, int N, int k, int S) {
-  constexpr int CPR = D / 8;           // 16-byte chunks of a bf16 row
-  constexpr int RPP = 32 / CPR;        // rows of a pass of the warp
-  constexpr int NP = kQ8Block / RPP;   // passes
+  constexpr int kStage = kQ8Block * D * 2;
+  constexpr int NP = kStage / 512;  // passes of the warp over a block, 16 bytes a lane
+  constexpr int RPP = 512 / (D * 2);  // rows of a pass
+  extern __shared__ __align__(128) uint8_t smem[];
+  __shared__ __align__(8) uint64_t bars[kRowWarps][NST];
+  struct Job {  // of a stage: (unit, K or V), first row, the rows that hold a token
+    long long uw;
+    int r0;
+    uint32_t rows;
+  };
+  __shared__ Job stage_jobs[kRowWarps][NST];
+  const int lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5;
+  uint8_t* stages = smem + warp * (NST * kStage);
+  uint64_t* full = bars[warp];
+  Job* held = stage_jobs[warp];
+  if (lane == 0) {
+    for (int s = 0; s < NST; ++s) mbar_init(&full[s], 1);
+    if (warp == 0) attn_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;\n" ::: "memory");
+  }
+  __syncthreads();
   pdl_wait();
   pdl_trigger();
-  const int lane = threadIdx.x & 31;
-  const int chunk = lane % CPR, rsub = lane / CPR;
-  for (long long job = static_cast<long long>(blockIdx.x) * kRowWarps + (threadIdx.x >> 5); job < jobs;
-       job += static_cast<long long>(gridDim.x) * kRowWarps) {
-    const long long uw = job / nb;  // (unit, K or V)
-    const int j = static_cast<int>(job - uw * nb);
-    const long long u = uw >> 1;
-    const long long b = u / LH;
-    const int r0 = j * kQ8Block;
-    // lane r: the bank row behind row r of the block, -1 if it holds no token
-    int src = -1;
-    {
-      const int i = r0 + lane;
-      const long long n = count ? count[b] : k;
-      if (i < k && i < n) {
-        src = idx ? idx[b * k + i] : i;
-        if (static_cast<unsigned>(src) >= static_cast<unsigned>(N)) {
-          src = -1;
+  const long long first = static_cast<long long>(blockIdx.x) * kRowWarps + warp;
+  const long long stride = static_cast<long long>(gridDim.x) * kRowWarps;
+
+  // What a block's copies need: lane r has the bank row behind row r of the block, -1 if it holds none.
+  struct Plan {
+    long long uw;
+    int r0, src;
+  };
+  auto plan = [&](long long job) {
+    Plan m = {0, 0, -1};
+    if (job >= jobs) return m;
+    m.uw = job / nb;
+    m.r0 = static_cast<int>(job - m.uw * nb) * kQ8Block;
+    const long long b = (m.uw >> 1) / LH;
+    const int i = m.r0 + lane;
+    const long long n = count ? count[b] : k;
+    if (i < k) {
+      const int row = idx ? idx[b * k + i] : i;
+      if (i < n) {
+        m.src = row;
+        if (static_cast<unsigned>(row) >= static_cast<unsigned>(N)) {
+          m.src = -1;
           if (status) atomicOr(status, CMC_DEVFLAG_BAD_INDEX);
         }
       }
     }
-    const uint4* bank = ((uw & 1) ? bank_v : bank_k) + u * N * CPR + chunk;
+    return m;
+  };
+  auto request = [&](int s, const Plan& m) {
+    const uint32_t rows = __ballot_sync(0xffffffffu, m.src >= 0);
+    const uint16_t* bank = ((m.uw & 1) ? bank_v : bank_k) + (m.uw >> 1) * N * D;
+    if (lane == 0) {
+      held[s] = {m.uw, m.r0, rows};
+      mbar_arrive_expect_tx(&full[s], __popc(rows) * (D * 2));
+    }
+    __syncwarp();
+    const uint32_t to = smem_addr(stages + s * kStage);
+    if (idx) {
+      if (m.src >= 0) bulk_copy(to + lane * (D * 2), bank + static_cast<long long>(m.src) * D, D * 2, &full[s]);
+    } else if (lane == 0 && rows) {  // rows r0, r0 + 1, ...
+      bulk_copy(to, bank + static_cast<long long>(m.r0) * D, __popc(rows) * (D * 2), &full[s]);
+    }
+  };
+#pragma unroll 1
+  for (int s = 0; s < NST; ++s)
+    if (first + s * stride < jobs) request(s, plan(first + s * stride));
+  Plan next = plan(first + NST * stride);  // its loads are on their way while a block is worked on
+  __syncwarp();
+  int s = 0;
+  uint32_t phase = 0;
+#pragma unroll 1
+  for (long long job = first; job < jobs; job += stride) {
+    if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {  // never expected: see mbar_wait
+      const uint32_t t0 = global_ns32();
+      for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
+      if (lane == 0 && status) atomicOr(status, CMC_DEVFLAG_TIMEOUT);
+      return;
+    }
+    const Job h = held[s];
+    const uint8_t* from = stages + s * kStage + lane * 16;
+    uint8_t* dst = kv + (h.uw * k + h.r0) * D + lane * 8;
+    const int jb = h.r0 / kQ8Block;
+    uint8_t* sc = scales + h.uw * S;
+    if (jb == nb - 1 && nb + lane < S) sc[nb + lane] = 0;  // the padding, at most three bytes
     uint4 x[NP];
     uint32_t m = 0u;  // largest magnitude, bf16 bits in two halves
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
-      const int row = __shfl_sync(0xffffffffu, src, e * RPP + rsub);
       x[e] = make_uint4(0u, 0u, 0u, 0u);
-      if (row >= 0) x[e] = ld_stream_u4(bank + static_cast<long long>(row) * CPR);
-    }
-#pragma unroll
-    for (int e = 0; e < NP; ++e) {
+      if ((h.rows >> (e * RPP + lane / (32 / RPP))) & 1u) x[e] = *reinterpret_cast<const uint4*>(from + e * 512);
       m = __vmaxu2(m, x[e].x & 0x7FFF7FFFu);
       m = __vmaxu2(m, x[e].y & 0x7FFF7FFFu);
       m = __vmaxu2(m, x[e].z & 0x7FFF7FFFu);
       m = __vmaxu2(m, x[e].w & 0x7FFF7FFFu);
     }
+    __syncwarp();  // the stage is free
+    if (job + NST * stride < jobs) {
+      request(s, next);
+      next = plan(job + (NST + 1) * stride);
+    }
     uint32_t top = __reduce_max_sync(0xffffffffu, max(m & 0xFFFFu, m >> 16));
-    if (top >= 0x7F80u) {  // an infinity or NaN among them: the largest finite one
+    if (top >= 0x7F80u) {  // an infinity or NaN among them: both become NaN, and do not count
       top = 0u;
 #pragma unroll
       for (int e = 0; e < NP; ++e) {
-        float f[8];
-        unpack8(x[e], f);
+        uint32_t* w = reinterpret_cast<uint32_t*>(&x[e]);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) top = max(top, finite_bits(f[q]) >> 16);
+        for (int q = 0; q < 4; ++q) {
+#pragma unroll
+          for (int sh = 0; sh < 32; sh += 16) {
+            const uint32_t a = (w[q] >> sh) & 0x7FFFu;
+            if (a >= 0x7F80u) w[q] |= 0x7FFFu << sh;
+            else top = max(top, a);
+          }
+        }
       }
       top = __reduce_max_sync(0xffffffffu, top);
     }
     const int c = block_code(top << 16);
-    const float f = code_factor(c);
-    uint8_t* dst = kv + (uw * k + r0) * D + chunk * 8;
+    const uint32_t f2 = __byte_perm(__float_as_uint(code_factor(c)), 0u, 0x3232);  // in bf16, twice
 #pragma unroll
     for (int e = 0; e < NP; ++e) {
-      const int row = e * RPP + rsub;
-      if (r0 + row < k) {
-        float v[8];
-        unpack8(x[e], v);
-        *reinterpret_cast<uint2*>(dst + static_cast<long long>(row) * D) =
-            make_uint2(encode4(v[0], v[1], v[2], v[3], f), encode4(v[4], v[5], v[6], v[7], f));
-      }
+      if (h.r0 + e * RPP + lane / (32 / RPP) < k)
+        *reinterpret_cast<uint2*>(dst + e * 256) =
+            make_uint2(encode4_bf16(x[e].x, x[e].y, f2), encode4_bf16(x[e].z, x[e].w, f2));
     }
-    uint8_t* sc = scales + uw * S;
-    if (lane == 0) sc[j] = static_cast<uint8_t>(c);
-    if (j == nb - 1 && nb + lane < S) sc[nb + lane] = 0;  // the padding, at most three bytes
+    if (lane == 0) sc[jb] = static_cast<uint8_t>(c);
+    if (++s == NST) {
+      s = 0;
+      phase ^= 1u;
+    }
   }
 }
 
@@ -304,9 +383,20 @@ int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int32_t* id
     return CMC_ERR_ALIGN;
   const int nb = (m.k + kQ8Block - 1) / kQ8Block;
   const long long jobs = 2LL * m.B * m.L * m.Hkv * nb;
-  auto kern = m.d == 128 ? quantize_kernel<128> : quantize_kernel<64>;
-  return launch_pdl(kern, dim3(row_grid(jobs)), dim3(kRowThreads), 0, static_cast<cudaStream_t>(stream),
-                    static_cast<const uint4*>(bank_k), static_cast<const uint4*>(bank_v), idx, count,
+  const long long ctas = (jobs + kRowWarps - 1) / kRowWarps;
+  const long long one = 5LL * sm_count() * (m.d == 128 ? 1 : 2);  // CTAs of one wave with one stage a warp
+  const int nst = ctas <= one ? 1 : 2;
+  const long long wave = nst == 1 ? one : 3LL * sm_count() * (m.d == 128 ? 1 : 2);
+  auto kern = m.d == 128 ? (nst == 1 ? quantize_kernel<128, 1> : quantize_kernel<128, 2>)
+                         : (nst == 1 ? quantize_kernel<64, 1> : quantize_kernel<64, 2>);
+  const int smem = kRowWarps * nst * kQ8Block * m.d * 2;
+  if (smem > 48 * 1024) {
+    st = record_cuda_error(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    if (st != CMC_OK) return st;
+  }
+  return launch_pdl(kern, dim3(static_cast<unsigned>(ctas < wave ? ctas : wave)), dim3(kRowThreads), smem,
+                    static_cast<cudaStream_t>(stream), static_cast<const uint16_t*>(bank_k),
+                    static_cast<const uint16_t*>(bank_v), idx, count,
                     static_cast<uint8_t*>(kv), static_cast<uint8_t*>(scales), status, jobs, nb,
                     m.L * m.Hkv, m.N, m.k, q8_scale_bytes(m.k));
 }
