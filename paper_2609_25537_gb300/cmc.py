@@ -731,27 +731,27 @@ def _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new) -> 
 
 def _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new, name) -> Tuple:
     """Checks the tensors of an attention call over 8-bit caches one by one; what the call keeps for
-    shapes like these: (the library function, dims by reference, dims)."""
+    shapes like these: (the library function, dims by reference, dims, the workspaces of its
+    batch size by device and stream)."""
     dims = _attn_q8_dims(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, new)
     key = (q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
            None if tier1_kv is None else tier1_kv.shape,
            None if tier1_scales is None else tier1_scales.shape)
     return _kept(key if new is None else key + (new[0].shape, new[1].shape),
-                 (getattr(lib(), name), ctypes.byref(dims), dims))
+                 (getattr(lib(), name), ctypes.byref(dims), dims,
+                  _q8_workspaces.setdefault(dims.B, {})))
 
 
-def _attn_q8_workspace(index: int, dims: CmcDims, q: torch.Tensor) -> DecodeWorkspace:
-    """The workspace of a call that is given none: one per stream and batch size."""
-    # A call that is being captured gets a workspace of its graph's own: the kept ones
-    # are zero-filled once, outside of it, and other calls use them.  (The default
-    # stream, 0, is never captured.)
-    stream = _raw_stream(index)
-    if stream and torch._C._cuda_isCurrentStreamCapturing():
-        return DecodeWorkspace(dims, q.device, q8=True)
-    key = ("q8", index, stream, dims.B)
-    ws = _ws_cache.get(key)
-    if ws is None:
-        ws = _ws_cache[key] = DecodeWorkspace(dims, q.device, q8=True)
+_q8_workspaces: Dict[int, Dict[Tuple[int, int], DecodeWorkspace]] = {}
+
+
+def _attn_q8_workspace(kept: Dict, index: int, stream: int, dims: CmcDims) -> DecodeWorkspace:
+    """A workspace for a call that is given none.  One is kept per stream and batch size; a call that
+    is being captured gets one of its graph's own, since the kept ones are zero-filled
+    once, outside of it, and other calls use them."""
+    ws = DecodeWorkspace(dims, torch.device("cuda", index), q8=True)
+    if not (stream and torch._C._cuda_isCurrentStreamCapturing()):
+        kept[index, stream] = ws
     return ws
 
 
@@ -781,17 +781,22 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     if kept is None:
         kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
                              "cmc_two_tier_decode_attn_q8")
-    fn, ref, dims = kept
+    fn, ref, dims, workspaces = kept
     if out is None:
         out = torch.empty_like(q)
     else:
         _check_out(out, q)
+    stream = _raw_stream(index)
     if workspace is None:
-        workspace = _attn_q8_workspace(index, dims, q)
+        # (the default stream, 0, is never captured)
+        if not (stream and torch._C._cuda_isCurrentStreamCapturing()):
+            workspace = workspaces.get((index, stream))
+        if workspace is None:
+            workspace = _attn_q8_workspace(workspaces, index, stream, dims)
     args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
             0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
             ring_scales.data_ptr(), pos.data_ptr(), ref, 0.0 if scale is None else scale,
-            out.data_ptr(), workspace.ptr, workspace.nbytes, _raw_stream(index))
+            out.data_ptr(), workspace.ptr, workspace.nbytes, stream)
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_two_tier_decode_attn_q8")
@@ -824,18 +829,23 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     if kept is None:
         kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, (k_new, v_new),
                              "cmc_decode_step_q8")
-    fn, ref, dims = kept
+    fn, ref, dims, workspaces = kept
     if out is None:
         out = torch.empty_like(q)
     else:
         _check_out(out, q)
+    stream = _raw_stream(index)
     if workspace is None:
-        workspace = _attn_q8_workspace(index, dims, q)
+        # (the default stream, 0, is never captured)
+        if not (stream and torch._C._cuda_isCurrentStreamCapturing()):
+            workspace = workspaces.get((index, stream))
+        if workspace is None:
+            workspace = _attn_q8_workspace(workspaces, index, stream, dims)
     args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
             0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
             ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ref,
             0.0 if scale is None else scale, rope_theta, rope_offset, out.data_ptr(),
-            workspace.ptr, workspace.nbytes, _raw_stream(index))
+            workspace.ptr, workspace.nbytes, stream)
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
         check(st, "cmc_decode_step_q8")

@@ -260,7 +260,7 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
     *reinterpret_cast<uint32_t*>(at + swz8<D>(r, (lane & 15) >> 2) + (lane & 3) * 4) = w0;
     *reinterpret_cast<uint32_t*>(to) = w0;
   }
-  if ((lane & 15) == 0) p.ring_scales[(uv + half) * p.ringS + slot / kQ8Block] = static_cast<uint8_t>(c);
+  if ((lane & 15) == 0 && c != c_old) p.ring_scales[(uv + half) * p.ringS + slot / kQ8Block] = static_cast<uint8_t>(c);
   kc = __shfl_sync(0xffffffffu, c, 0);
   vc = __shfl_sync(0xffffffffu, c, 16);
   __syncwarp();
