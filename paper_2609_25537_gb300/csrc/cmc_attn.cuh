@@ -1,7 +1,8 @@
 // What the decode attention kernels over a bf16 cache (cmc_attn.cu) and over a
 // cache in 8 bits (cmc_attn_q8.cu) share: PTX wrappers with bounded waits, the
-// walk over a launch's (unit, tile) list, the sequence state, the merge of
-// split units, the launch plan and the rotary frequencies.  Everything here is
+// sequence state, the clusters' exchange, the workspace's layout and the rotary
+// frequencies; and what the first has to itself of the walk over a launch's (unit, tile)
+// list, the merge of split units and the plan.  Everything here is
 // internal to the translation unit that includes it.
 #pragma once
 
@@ -319,9 +320,8 @@ __device__ __forceinline__ void mbar_wait_peers(uint64_t* bar) {
 
 // Per-stage header words: rows of the tile that may hold a key, the new
 // token's ring slot and tile row (fused step; -1 if not in this tile),
-// whether any of the tile's rows holds no key (its V row must be zeroed), and,
-// over a bf16 cache, the bit masks of rows 0-31 / 32-63 whose Tier-1 index is out
-// of range (over a cache in 8 bits the blocks' powers of two lie there).
+// whether any of the tile's rows holds no key (its V row must be zeroed), and
+// the bit masks of rows 0-31 / 32-63 whose Tier-1 index is out of range.
 // Stage 0's also holds, in its last two words, pos of the CTA's first sequence
 // on its way to the producer.
 enum { H_NROWS = 0, H_NEWSLOT = 1, H_NEWROW = 2, H_MASKED = 3, H_BADLO = 4, H_BADHI = 5, H_POS = 6 };

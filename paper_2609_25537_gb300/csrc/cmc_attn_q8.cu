@@ -21,8 +21,8 @@
 //
 // Both products run on fp16 operands with fp32 accumulation (mma.sync m16n8k16): the
 // codes are converted to fp16 in registers, exactly, one instruction for two.  (mma.sync
-// takes e4m3 operands too, but on this GPU it does the same conversions underneath, for
-// both operands, on every call: 672 instructions a block, which bounded the kernel.)
+// takes e4m3 operands too; the kernel then executed 672 instructions a block by the counters,
+// 420 so, and was bound by them: 512 units of 312 to 2,304 keys 49.7 us, 30.8 so.)
 //   S^T = K Q^T     16 keys as the rows, the G query heads as the columns, d in k-steps of 16
 //   O^T += V^T P^T  16 rows of the head dimension, the heads, the block's 32 keys in two k-steps
 //   q    is multiplied by a power of two so that its head's largest element is in (224, 448].  fp16
@@ -343,7 +343,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   // The unit's powers of two: the rows of lane 0 (K) and lane 1 (V).
   const uint8_t* t1_s = p.t1_scales + (2LL * u + (lane & 1)) * p.t1S;
   const uint8_t* ring_s = p.ring_scales + (2LL * u + (lane & 1)) * p.ringS;
-  int n_run = SOLO ? nb_all : g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;  // blocks of the warp, as far as known before pos
+  // blocks of the warp, as far as known before pos
+  int n_run = SOLO ? nb_all : g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;
   int jn = g0;  // the next to request
   // Requests the warp's next block into stage s: the codes by TMA, the two words that hold its
   // powers of two by lanes 0 and 1.  Called by the whole warp, converged.
@@ -711,7 +712,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
 #pragma unroll
     for (int v = 0; v < kWarps; ++v) {
       const float f = ex2(ml[v * 16 + hh] - Mr);
-      const float4 y = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(smem + s_left[v]) + hh * D + (c ^ (8 * (hh >> 1))));
+      const float* left = reinterpret_cast<const float*>(smem + s_left[v]);
+      const float4 y = *reinterpret_cast<const float4*>(left + hh * D + (c ^ (8 * (hh >> 1))));
       acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
       acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
       Ls = fmaf(f, ml[v * 16 + 8 + hh], Ls);
@@ -799,8 +801,9 @@ static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
 
 // How a call's units are put on the GPU.  Three variants of the kernel:
 //   wide   a CTA (or cluster) per unit, three stages a warp, two CTAs an SM: few or long units
-//   spread the same with two stages a warp and three CTAs an SM: when the units just miss one
-//          wave of the first
+//   spread the same with two stages a warp and three CTAs an SM: when the units, or their
+//          clusters, just miss one wave of the first (176 x 61 blocks: two CTAs a unit in one
+//          wave 13.4 us, one a unit of the first 15.9)
 //   solo   a warp per unit, three stages a warp, two CTAs (eight units) an SM: many short units
 struct Q8Plan {
   enum { kWide, kSpread, kSolo } variant;
@@ -865,22 +868,23 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
     return (ctas + slots - 1) / slots * (30 + static_cast<long long>(blocks) * per_block);
   };
   const long long quads = (units + kWarps - 1) / kWarps;
-  *pl = {Q8Plan::kWide, 1, static_cast<int>(units)};
-  long long best = cost(units, wide, (nb + kWarps - 1) / kWarps, 11);
-  for (int cm = 2; cm <= kMaxClusterCtas && kWarps * cm / 2 < nb; cm *= 2) {  // a cluster's merge: 0.3 us
-    const long long t = cost(units * cm, wide, (nb + kWarps * cm - 1) / (kWarps * cm), 11) + 3;
-    if (t < best) {
-      best = t;
+  long long best = -1;
+  for (int cm = 1; cm <= kMaxClusterCtas && (cm == 1 || kWarps * cm / 2 < nb); cm *= 2) {
+    const int blocks = (nb + kWarps * cm - 1) / (kWarps * cm), merge = cm > 1 ? 3 : 0;  // a cluster's: 0.3 us
+    // A cluster lies in one group of SMs, and eight CTAs do not fill every group: 56 clusters of eight in
+    // 456 places took two waves (56 x 128 blocks 17.5 us, with clusters of four 12.8).
+    const int w = cm == 8 ? wide * 7 / 8 : wide, p3 = cm == 8 ? spread * 7 / 8 : spread;
+    const long long a = cost(units * cm, w, blocks, 11) + merge, c = cost(units * cm, p3, blocks, 15) + merge;
+    if (best < 0 || a < best) {
+      best = a;
       *pl = {Q8Plan::kWide, cm, static_cast<int>(units * cm)};
     }
+    if (c < best) {
+      best = c;
+      *pl = {Q8Plan::kSpread, cm, static_cast<int>(units * cm)};
+    }
   }
-  long long t = cost(units, spread, (nb + kWarps - 1) / kWarps, 15);
-  if (t < best) {
-    best = t;
-    *pl = {Q8Plan::kSpread, 1, static_cast<int>(units)};
-  }
-  t = cost(quads, solo, nb, 11);
-  if (t < best) *pl = {Q8Plan::kSolo, 1, static_cast<int>(quads)};
+  if (cost(quads, solo, nb, 11) < best) *pl = {Q8Plan::kSolo, 1, static_cast<int>(quads)};
   return CMC_OK;
 }
 
