@@ -39,6 +39,7 @@
 // P^T's way from the accumulators of S^T to the B operand (movmatrix) fixes for the row
 // addresses of V; rows 8 .. 15 of a product are keys 8 + (r ^ 4), so that eight
 // consecutive rows of V lie in eight different bank groups.
+#include <algorithm>
 #include <atomic>
 
 #include "cmc_attn.cuh"
@@ -127,24 +128,15 @@ __device__ __forceinline__ void mma_f16_zero(float (&c)[4], uint32_t a0, uint32_
       : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// Four codes to fp16 (lo: bytes 0 and 1).
-__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n"
-      " cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
-      : "=r"(lo), "=r"(hi)
-      : "r"(w));
-}
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
 
-// Live blocks of a unit whose sequence's state is sq (one, empty, where there are none: its
-// output is still to be written).
+// Live blocks of a unit whose sequence's state is sq.
 __device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState& sq) {
-  const int n = sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
-  return n > 0 ? n : 1;
+  return sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
 }
 
 // Half a row of the new token each for lanes 0-15 (K) and 16-31 (V): d / 16 neighbouring elements.
@@ -156,12 +148,14 @@ __device__ __forceinline__ uint4 load_new(const AttnQ8Params& p, int u, int lane
   return make_uint4(w.x, w.y, 0u, 0u);
 }
 
-// A lane's E = d / 32 neighbouring elements of a row.
+// A lane's E = d / 32 neighbouring elements of a row, and their values.
 template <int E>
-__device__ __forceinline__ void load_part(const uint16_t* row, int lane, float (&x)[E]) {
-  uint2 w = make_uint2(0u, 0u);
-  if (E == 4) w = __ldg(reinterpret_cast<const uint2*>(row) + lane);
-  else w.x = __ldg(reinterpret_cast<const uint32_t*>(row) + lane);
+__device__ __forceinline__ uint2 load_part(const uint16_t* row, int lane) {
+  if (E == 4) return __ldg(reinterpret_cast<const uint2*>(row) + lane);
+  return make_uint2(__ldg(reinterpret_cast<const uint32_t*>(row) + lane), 0u);
+}
+template <int E>
+__device__ __forceinline__ void unpack_part(const uint2& w, float (&x)[E]) {
   x[0] = bf16lo_to_f32(w.x);
   x[1] = bf16hi_to_f32(w.x);
   if (E == 4) {
@@ -180,28 +174,41 @@ __device__ __forceinline__ void rotate_part(float (&x)[E], const float2 (&cs)[E]
   }
 }
 
-// The rare parts of an append, out of line and rolled: the code that a launch runs through once is
-// what it waits for most (its instructions come from L2), so what is not run should
-// not lie in between either.
-// The largest value that the block's other tokens hold (fp32 bits); `mine`: the lane's row is one.
+// The rare parts of an append, out of line: the code that a launch runs through once is what it waits for
+// most (its instructions come from L2), so what is not run should not lie in between either.  Rare
+// for a unit, they set the time of most launches, which have some units that take them (1,216 units
+// of 6 blocks 14.5 us, 13.5 where none does, and 11.9 without an append).
+// A lane has 16-byte chunk lane % (d / 16) of every (512 / d)th row of a block.
+// The largest values that the block's other tokens hold in K and in V (fp32 bits).
 template <int D>
-static __device__ __noinline__ uint32_t block_held(const uint8_t* rows, bool mine, int lane, int c_old) {
-  uint32_t m = 0u;
-#pragma unroll 1
-  for (int q = 0; q < D / 16; ++q)
-    if (mine) m = max_codes16(m, *reinterpret_cast<const uint4*>(rows + swz8<D>(lane, q)));
-  return __reduce_max_sync(0xffffffffu, held_bits(m, c_old));
+static __device__ __noinline__ uint2 block_held(const uint8_t* stage, uint32_t others, int lane, int kc, int vc) {
+  constexpr int CPR = D / 16;
+  uint32_t mk = 0u, mv = 0u;
+#pragma unroll 2
+  for (int row = lane / CPR; row < kQ8Block; row += 32 / CPR) {
+    const uint8_t* at = stage + swz8<D>(row, lane % CPR);
+    if ((others >> row) & 1u) {
+      mk = max_codes16(mk, *reinterpret_cast<const uint4*>(at));
+      mv = max_codes16(mv, *reinterpret_cast<const uint4*>(at + kQ8Block * D));
+    }
+  }
+  return make_uint2(__reduce_max_sync(0xffffffffu, held_bits(mk, kc)),
+                    __reduce_max_sync(0xffffffffu, held_bits(mv, vc)));
 }
-// The block's other tokens' codes for another power of two, in the stage and in the ring.
+// The block's other tokens' codes of K or V for another power of two, in the stage and in the ring.
 template <int D>
-static __device__ __noinline__ void block_recode(uint8_t* rows, uint8_t* ring_row0, bool mine, int lane, float f) {
-  if (!mine) return;
-#pragma unroll 1
-  for (int q = 0; q < D / 16; ++q) {
-    uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(lane, q));
-    const uint4 y = recode16(*at, f);
-    *at = y;
-    reinterpret_cast<uint4*>(ring_row0 + static_cast<long long>(lane) * D)[q] = y;
+static __device__ __noinline__ void block_recode(uint8_t* rows, uint8_t* ring_row0, uint32_t others, int lane,
+                                                 int c_old, int c) {
+  constexpr int CPR = D / 16;
+  const Recode f = recode_by(c_old, c);
+#pragma unroll 2
+  for (int row = lane / CPR; row < kQ8Block; row += 32 / CPR) {
+    if ((others >> row) & 1u) {
+      uint4* at = reinterpret_cast<uint4*>(rows + swz8<D>(row, lane % CPR));
+      const uint4 y = recode16(*at, f);
+      *at = y;
+      *reinterpret_cast<uint4*>(ring_row0 + row * D + lane % CPR * 16) = y;
+    }
   }
 }
 
@@ -230,24 +237,20 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
   for (int e = 0; e < E; ++e) top = max(top, finite_bits(x[e]));
 #pragma unroll
   for (int off = 1; off < 16; off <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, off));
-  const bool mine = (others >> lane) & 1u;  // the lane's row of the block, where codes change
   const long long uv = 2LL * u;
   uint8_t* ring_k = p.ring_kv + (uv * p.W + slot - r) * D;  // the block's first row
   uint8_t* ring_v = ring_k + static_cast<long long>(p.W) * D;
   const int c_old = half ? vc : kc;
   int c = max(block_code(top), c_old);
   if ((slot & (kQ8Block - 1)) == 0) {
-    const uint32_t hk = block_held<D>(stage, mine, lane, kc);
-    const uint32_t hv = block_held<D>(stage + kQ8Block * D, mine, lane, vc);
-    c = block_code(max(top, half ? hv : hk));
+    const uint2 held = block_held<D>(stage, others, lane, kc, vc);
+    c = block_code(max(top, half ? held.y : held.x));
   }
-  if (__any_sync(0xffffffffu, c != c_old)) {
-    const float f = recode_factor(c_old, c);
-    const int same = c == c_old;
-    const float fk = __shfl_sync(0xffffffffu, f, 0), fv = __shfl_sync(0xffffffffu, f, 16);
-    if (!__shfl_sync(0xffffffffu, same, 0)) block_recode<D>(stage, ring_k, mine, lane, fk);
-    if (!__shfl_sync(0xffffffffu, same, 16)) block_recode<D>(stage + kQ8Block * D, ring_v, mine, lane, fv);
-  }
+  const int kc_old = kc, vc_old = vc;
+  kc = __shfl_sync(0xffffffffu, c, 0);
+  vc = __shfl_sync(0xffffffffu, c, 16);
+  if (kc != kc_old) block_recode<D>(stage, ring_k, others, lane, kc_old, kc);
+  if (vc != vc_old) block_recode<D>(stage + kQ8Block * D, ring_v, others, lane, vc_old, vc);
   const float f = code_factor(c);
   uint8_t* at = stage + half * (kQ8Block * D);
   uint8_t* to = (half ? ring_v : ring_k) + static_cast<long long>(r) * D + (lane & 15) * E;
@@ -261,16 +264,16 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
     *reinterpret_cast<uint32_t*>(to) = w0;
   }
   if ((lane & 15) == 0 && c != c_old) p.ring_scales[(uv + half) * p.ringS + slot / kQ8Block] = static_cast<uint8_t>(c);
-  kc = __shfl_sync(0xffffffffu, c, 0);
-  vc = __shfl_sync(0xffffffffu, c, 16);
   __syncwarp();
 }
 
-// SOLO: a unit per warp, four a CTA, and no barrier but the warp's.
+// SOLO: a unit per warp, four a CTA, and no barrier but the warp's; the warp goes on with the unit
+// gridDim x 4 after its own, whose query, position and first blocks are then already on
+// their way.
+// Registers: three CTAs an SM take 168 a thread (two of them with 168 instead of 200 spill: 2,048 units of 640
+// keys 56 us and 54); with d = 64 four SOLO CTAs fit with 128.
 template <int D, int G, bool FUSED, int NST, bool SOLO>
-// Registers: up to 200 a thread fit two CTAs an SM (with 168 some spill: 2,048 units of 640 keys 54 us
-// and 56), three take 168.
-__global__ void __maxnreg__(NST == 2 ? 168 : 200)
+__global__ void __maxnreg__(SOLO ? (D == 64 ? 128 : 240) : NST == 2 ? 168 : 200)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   using S = Q8Smem<D, G, NST, SOLO>;
   constexpr int KS = D / 16;      // k-steps of the Q K^T product, m-tiles of O^T
@@ -285,8 +288,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   const int tid = threadIdx.x;
   const int lane = tid & 31;
   const int warp = tid >> 5;
-  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem + S::kSmall) + 1023) & ~uintptr_t(1023)) +
-                    warp * (NST * S::kStage);
+  const uintptr_t small_end = reinterpret_cast<uintptr_t>(smem + S::kSmall);
+  uint8_t* stages = reinterpret_cast<uint8_t*>((small_end + 1023) & ~uintptr_t(1023)) + warp * (NST * S::kStage);
   uint8_t* scale_words = smem + S::kScale + warp * (NST * 8);
   constexpr int HPW = SOLO ? G : (G + kWarps - 1) / kWarps;  // heads whose query a warp converts:
   constexpr int HSTEP = SOLO ? 1 : kWarps;                   // h0, h0 + HSTEP, ...
@@ -297,15 +300,16 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   uint64_t* full = full_bar[warp];
 
   const int cm = SOLO ? 1 : p.cm;
-  const int u = SOLO     ? static_cast<int>(blockIdx.x) * kWarps + warp
-                : cm > 1 ? static_cast<int>(cluster_id())
-                         : static_cast<int>(blockIdx.x);
+  int u = SOLO     ? static_cast<int>(blockIdx.x) * kWarps + warp
+          : cm > 1 ? static_cast<int>(cluster_id())
+                   : static_cast<int>(blockIdx.x);
+  const int hop = static_cast<int>(gridDim.x) * kWarps;  // SOLO: to the warp's next unit
   const int rank = cm > 1 ? static_cast<int>(cluster_ctarank()) : 0;
   // the warp's first block, and their distance; which thread speaks for the unit
   const int g0 = SOLO ? 0 : rank * kWarps + warp, step = SOLO ? 1 : cm * kWarps;
   const bool first_thread = SOLO ? lane == 0 : tid == 0;
   const int nb_all = p.nb1 + p.nb2;
-  const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));  // sequence
+  int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));  // sequence
 
   if (lane == 0) {
     for (int s = 0; s < NST; ++s) mbar_init(&full[s], 1);  // lane 0's arrive (plus tracked cp.async arrivals)
@@ -340,12 +344,17 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
 
-  // The unit's powers of two: the rows of lane 0 (K) and lane 1 (V).
-  const uint8_t* t1_s = p.t1_scales + (2LL * u + (lane & 1)) * p.t1S;
-  const uint8_t* ring_s = p.ring_scales + (2LL * u + (lane & 1)) * p.ringS;
   // blocks of the warp, as far as known before pos
   int n_run = SOLO ? nb_all : g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;
-  int jn = g0;  // the next to request
+  int jn = g0, un = u;  // the next to request, and its unit
+  const uint8_t* t1_s;  // that unit's powers of two: the rows of lane 0 (K) and lane 1 (V)
+  const uint8_t* ring_s;
+  auto cursor_unit = [&](int x) {
+    un = x;
+    t1_s = p.t1_scales + (2LL * x + (lane & 1)) * p.t1S;
+    ring_s = p.ring_scales + (2LL * x + (lane & 1)) * p.ringS;
+  };
+  cursor_unit(u);
   // Requests the warp's next block into stage s: the codes by TMA, the two words that hold its
   // powers of two by lanes 0 and 1.  Called by the whole warp, converged.
   auto request = [&](int s) {
@@ -358,7 +367,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     __syncwarp();
     if (lane == 0) {
       mbar_arrive_expect_tx(&full[s], S::kStage + p.stall_tx);
-      tma_box3_hint(smem_addr(stages + s * S::kStage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * u, &full[s],
+      tma_box3_hint(smem_addr(stages + s * S::kStage), t1 ? &maps.t1 : &maps.ring, jj * kQ8Block, 2 * un, &full[s],
                     policy_evict_first());
     }
     jn += step;
@@ -366,418 +375,485 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   int issued = 0;
 #pragma unroll 1
   for (; issued < NST && issued < n_run; ++issued) request(issued);
-
-  // ---- the query, while those are on their way (warp w takes heads w and w + 4, a lane E
-  // neighbouring elements), and the new key ----
-  const long long pos = ld_pos(p, b);
-  float x[HPW][E];
-#pragma unroll
-  for (int h = 0; h < HPW; ++h)
-    if (h0 + HSTEP * h < G) load_part<E>(p.q + (static_cast<long long>(u) * G + h0 + HSTEP * h) * D, lane, x[h]);
-  uint4 fresh = make_uint4(0u, 0u, 0u, 0u);  // the new token's rows
-  float kx[E];
-  if (FUSED) {
-    fresh = load_new<D>(p, u, lane);
-    if (p.rope && (SOLO || warp == kWarps - 1)) load_part<E>(p.k_new + static_cast<long long>(u) * D, lane, kx);
-  }
-  const SeqState sq = seq_state<FUSED>(p, pos);
-  unsigned long long ticket = 0;
-  if (first_thread && sq.bad && rank == 0 && u % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-  if (FUSED && p.rope) {
-    float2 cs[E];
-    const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + (sq.bad ? 0 : pos));
-#pragma unroll
-    for (int e = 0; e < E; ++e) {  // as rope_pairs
-      const int hi = static_cast<int>(static_cast<long long>(pp * turns[e]) >> 32);
-      float sn, cn;
-      sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &sn, &cn);
-      cs[e] = make_float2(cn, sn);
-    }
-#pragma unroll
-    for (int h = 0; h < HPW; ++h)
-      if (h0 + HSTEP * h < G) rotate_part<E>(x[h], cs, lane);
-    if (SOLO || warp == kWarps - 1) {
-      rotate_part<E>(kx, cs, lane);
-#pragma unroll
-      for (int e = 0; e < E; ++e) knew[lane * E + e] = kx[e];
-    }
-  }
-#pragma unroll
-  for (int h = 0; h < HPW; ++h) {
-    const int hh = h0 + HSTEP * h;
-    if (hh >= G) break;
-    float top = 0.f;  // (a NaN does not count)
-#pragma unroll
-    for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[h][e]));
-    if (__any_sync(0xffffffffu, top == INFINITY)) {  // an infinity becomes NaN and does not count either
-      top = 0.f;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        x[h][e] = fmaf(x[h][e], 0.f, x[h][e]);
-        top = fmaxf(top, fabsf(x[h][e]));
-      }
-    }
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
-    const int qc = block_code(__float_as_uint(top));
-    const float f = code_factor(qc);
-    uint32_t* to = reinterpret_cast<uint32_t*>(q_rows + hh * (D * 2)) + lane * (E / 2);
-#pragma unroll
-    for (int e = 0; e < E; e += 2) to[e / 2] = pack_f16(x[h][e] * f, x[h][e + 1] * f);
-    if (lane == 0) q_factor[hh] = e8m0_to_f32(qc) * p.scale_log2;
-  }
-  if (FUSED && lane == 0) s_pos[warp] = pos;  // (so that every warp has it, not only asked for it)
-  if (SOLO) __syncwarp();
-  else __syncthreads();
-  // The last to have read pos[b] advances it (in the end: the count takes a trip to L2).
-  if (FUSED && first_thread) ticket = atomicAdd(p.tickets + b, 1ull);
-
-  // Live blocks; those that were requested in vain hold no key.
-  const int nb = sq.bad ? 0 : p.nb1 + (sq.count + kQ8Block - 1) / kQ8Block;
-  n_run = SOLO ? nb : nb > g0 ? (nb - g0 + step - 1) / step : 0;
-  if (n_run < issued) n_run = issued;
-  // gq = lane / 4, tq = lane % 4: a thread has columns (heads) 2 tq and 2 tq + 1 of the products
-  // (heads >= G are padding: zero queries, never written out).
-  const int gq = lane >> 2;
-  const int tq = lane & 3;
-  uint32_t qa[KS][2];  // Q^T fragments: column gq, elements 16 ks + 4 tq .. + 3
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks) {
-    uint2 f = make_uint2(0u, 0u);
-    if (gq < G) f = *reinterpret_cast<const uint2*>(q_rows + (gq * D + 16 * ks + 4 * tq) * 2);
-    qa[ks][0] = f.x;
-    qa[ks][1] = f.y;
-  }
-  float qs[2], m_run[2], l_run[2];  // softmax scale * log2(e) * the heads' powers of two; maxima, sums
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    qs[e] = 2 * tq + e < G ? q_factor[2 * tq + e] : 0.f;
-    m_run[e] = -INFINITY;
-    l_run[e] = 0.f;
-  }
-  int e_cur = -1, e_top = -1;  // the byte O is in units of; the largest so far
-  float o[KS][4];
-#pragma unroll
-  for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-
-  bool gave_up = false;
+  // SOLO: stages on their way or unread, the next to fill, the blocks of unit `un` to request
+  int fly = issued, fill = issued == NST ? 0 : issued, rn = n_run;
   int s = 0;           // stage
   uint32_t phase = 0;  // its parity
-  int j = g0;          // block
+
+  // A unit's position, query (warp w takes heads w and w + 4, a lane E neighbouring elements) and new rows.
+  long long pos = ld_pos(p, b);
+  uint2 qw[HPW], kw = make_uint2(0u, 0u);
+  uint4 fresh = make_uint4(0u, 0u, 0u, 0u), fresh_next = fresh;
+  auto load_unit = [&](int x, uint4& rows) {
+#pragma unroll
+    for (int h = 0; h < HPW; ++h)
+      if (h0 + HSTEP * h < G) qw[h] = load_part<E>(p.q + (static_cast<long long>(x) * G + h0 + HSTEP * h) * D, lane);
+    if (FUSED) rows = load_new<D>(p, x, lane);
+    if (FUSED && p.rope && (SOLO || warp == kWarps - 1))
+      kw = load_part<E>(p.k_new + static_cast<long long>(x) * D, lane);
+  };
+  load_unit(u, fresh);
 #pragma unroll 1
-  for (int i = 0; i < n_run; ++i) {
-    uint8_t* stage = stages + s * S::kStage;
-    if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {
-      gave_up = true;
-      break;
+  do {  // SOLO: the warp's units
+    // ---- the query, while the first blocks are on their way, and the new key ----
+    float x[HPW][E], kx[E];
+#pragma unroll
+    for (int h = 0; h < HPW; ++h)
+      if (h0 + HSTEP * h < G) unpack_part<E>(qw[h], x[h]);
+    if (FUSED && p.rope) unpack_part<E>(kw, kx);
+    const SeqState sq = seq_state<FUSED>(p, pos);
+    unsigned long long ticket = 0;
+    long long pos_next = 0;  // SOLO: what the next unit starts with
+    if (SOLO && u + hop < p.units) {
+      pos_next = ld_pos(p, static_cast<int>(static_cast<unsigned>(u + hop) / static_cast<unsigned>(p.LH)));
+      load_unit(u + hop, fresh_next);
     }
-    // the block: its rows that hold a key (bit r of mk), its bytes
-    const bool t1 = j < p.nb1;
-    const int jj = t1 ? j : j - p.nb1;
-    const int live = t1 ? (sq.bad ? 0 : p.k) : sq.count;
-    const int nk = min(max(live - jj * kQ8Block, 0), kQ8Block);
-    const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;
-    int kc = scale_words[s * 8 + (jj & 3)], vc = scale_words[s * 8 + 4 + (jj & 3)];
-    bool wrote_stage = false;  // generic-proxy writes into the stage
+    if (first_thread && sq.bad && rank == 0 && u % p.LH == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+    if (FUSED && p.rope) {
+      float2 cs[E];
+      const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + (sq.bad ? 0 : pos));
+#pragma unroll
+      for (int e = 0; e < E; ++e) {  // as rope_pairs
+        const int hi = static_cast<int>(static_cast<long long>(pp * turns[e]) >> 32);
+        float sn, cn;
+        sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &sn, &cn);
+        cs[e] = make_float2(cn, sn);
+      }
+#pragma unroll
+      for (int h = 0; h < HPW; ++h)
+        if (h0 + HSTEP * h < G) rotate_part<E>(x[h], cs, lane);
+      if (SOLO || warp == kWarps - 1) {
+        rotate_part<E>(kx, cs, lane);
+#pragma unroll
+        for (int e = 0; e < E; ++e) knew[lane * E + e] = kx[e];
+      }
+    }
+#pragma unroll
+    for (int h = 0; h < HPW; ++h) {
+      const int hh = h0 + HSTEP * h;
+      if (hh >= G) break;
+      float top = 0.f;  // (a NaN does not count)
+#pragma unroll
+      for (int e = 0; e < E; ++e) top = fmaxf(top, fabsf(x[h][e]));
+      if (__any_sync(0xffffffffu, top == INFINITY)) {  // an infinity becomes NaN and does not count either
+        top = 0.f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          x[h][e] = fmaf(x[h][e], 0.f, x[h][e]);
+          top = fmaxf(top, fabsf(x[h][e]));
+        }
+      }
+#pragma unroll
+      for (int off = 1; off < 32; off <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, off));
+      const int qc = block_code(__float_as_uint(top));
+      const float f = code_factor(qc);
+      uint32_t* to = reinterpret_cast<uint32_t*>(q_rows + hh * (D * 2)) + lane * (E / 2);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) to[e / 2] = pack_f16(x[h][e] * f, x[h][e + 1] * f);
+      if (lane == 0) q_factor[hh] = e8m0_to_f32(qc) * p.scale_log2;
+    }
+    if (FUSED && lane == 0) s_pos[warp] = pos;  // (so that every warp has it, not only asked for it)
+    if (SOLO) __syncwarp();
+    else __syncthreads();
+    // The last to have read pos[b] advances it (in the end: the count takes a trip to L2).
+    if (FUSED && first_thread) ticket = atomicAdd(p.tickets + b, 1ull);
 
-    if (FUSED && !t1 && sq.new_slot >= 0 && sq.new_slot / kQ8Block == jj) {
-      const int r = sq.new_slot & (kQ8Block - 1);
-      patch_block<D>(p, stage, u, r, sq.new_slot, mk & ~(1u << r), fresh, knew, kc, vc, lane);
-      wrote_stage = true;
+    // Live blocks; those that were requested in vain hold no key.
+    const int nb = live_blocks(p, sq);
+    n_run = SOLO ? nb : nb > g0 ? (nb - g0 + step - 1) / step : 0;
+    if (n_run < issued) n_run = issued;
+    // SOLO: as many blocks of this unit and the next are requested as there are stages
+    int n_next = 0;
+    if (SOLO && u + hop < p.units) n_next = live_blocks(p, seq_state<FUSED>(p, pos_next));
+    if (SOLO) {
+      if (un != u) {
+        cursor_unit(u);
+        jn = 0;
+      }
+      rn = n_run;
     }
-
-    if (mk != 0u) {
-      if (mk != 0xFFFFFFFFu) {
-        // Zero the V rows that hold no key: their probabilities are 0, but 0 times NaN is not.
-        if (!((mk >> lane) & 1u)) {
-#pragma unroll
-          for (int q = 0; q < D / 16; ++q)
-            *reinterpret_cast<uint4*>(stage + S::kV + swz8<D>(lane, q)) = make_uint4(0u, 0u, 0u, 0u);
+    auto top_up = [&]() {
+#pragma unroll 1
+      while (fly < NST) {
+        if (jn >= rn) {
+          if (un != u || n_next == 0) break;  // (no further ahead than the next unit)
+          cursor_unit(u + hop);
+          jn = 0;
+          rn = n_next;
         }
-        __syncwarp();
-        wrote_stage = true;
+        request(fill);
+        ++fly;
+        fill = fill + 1 == NST ? 0 : fill + 1;
       }
-      const uint32_t sK = smem_addr(stage);
-      const uint32_t sV = smem_addr(stage + S::kV);
-      // ---- S^T = K Q^T, two products of 16 keys ----
-      // (two accumulator chains a product)
-      float sc[2][4], sd[2][4];  // product t: keys 16 t + gq (0, 1), 16 t + 8 + (gq ^ 4) (2, 3); heads 2 tq, 2 tq + 1
+    };
+    // gq = lane / 4, tq = lane % 4: a thread has columns (heads) 2 tq and 2 tq + 1 of the products
+    // (heads >= G are padding: zero queries, never written out).
+    const int gq = lane >> 2;
+    const int tq = lane & 3;
+    uint32_t qa[KS][2];  // Q^T fragments: column gq, elements 16 ks + 4 tq .. + 3
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        // lanes 0-7 / 8-15 / 16-23 / 24-31: rows 0-7 / 8-15 / 0-7 / 8-15 of the product, at
-        // bytes 32 kk .. + 15 / same / 32 kk + 16 .. + 31 / same
-        const int key = 16 * t + ((lane & 8) ? 8 + ((lane & 7) ^ 4) : lane & 7);
-#pragma unroll
-        for (int kk = 0; kk < KS / 2; ++kk) {
-          uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
-          ldsm_x4(sK + swz8<D>(key, 2 * kk + (lane >> 4)), r0, r1, r2, r3);
-          codes_f16(r0, a0, a2);
-          codes_f16(r1, a1, a3);
-          if (kk == 0) mma_f16_zero(sc[t], a0, a1, a2, a3, qa[0][0], qa[0][1]);
-          else mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk][0], qa[2 * kk][1]);
-          codes_f16(r2, a0, a2);
-          codes_f16(r3, a1, a3);
-          if (kk == 0) mma_f16_zero(sd[t], a0, a1, a2, a3, qa[1][0], qa[1][1]);
-          else mma_f16(sd[t], a0, a1, a2, a3, qa[2 * kk + 1][0], qa[2 * kk + 1][1]);
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[t][e] += sd[t][e];
-      }
-      if (mk != 0xFFFFFFFFu) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (!((mk >> (16 * t + gq)) & 1u)) sc[t][0] = sc[t][1] = -INFINITY;
-          if (!((mk >> (16 * t + 8 + (gq ^ 4))) & 1u)) sc[t][2] = sc[t][3] = -INFINITY;
-        }
-      }
-      // ---- online softmax, log2 domain: f sc (f > 0) ----
-      const float ks2 = e8m0_to_f32(kc);
-      // (not below fp32's normal numbers: 0 times a masked score is no score)
-      constexpr float kLeast = 1.17549435e-38f;
-      float f0 = qs[0] * ks2, f1 = qs[1] * ks2;
-      if (f0 < kLeast) f0 = kLeast;
-      if (f1 < kLeast) f1 = kLeast;
-      float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2]));
-      float mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
-#pragma unroll
-      for (int off = 4; off < 32; off <<= 1) {
-        mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
-        mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
-      }
-      mx0 *= f0;
-      mx1 *= f1;
-      // The unit of O: at least 2^-64 of the largest block's, so that O stays far inside fp32.
-      int e_new = e_cur;
-      if (vc != 255) {
-        e_top = max(e_top, vc);
-        const int want = max(vc, e_top - 64);
-        if (want > e_cur || want + 10 < e_cur) e_new = want;
-      }
-      const bool up0 = mx0 > m_run[0], up1 = mx1 > m_run[1];
-      if (__any_sync(0xffffffffu, up0 || up1 || e_new != e_cur)) {
-        // (with e_cur = -1, before the first block, O is zero)
-        const float fe = e_cur < 0 ? 1.f : recode_factor(e_cur, max(e_new, 0));
-        e_cur = e_new;
-        const float alpha0 = up0 ? ex2(m_run[0] - mx0) : 1.f;
-        const float alpha1 = up1 ? ex2(m_run[1] - mx1) : 1.f;
-        if (up0) m_run[0] = mx0;
-        if (up1) m_run[1] = mx1;
-        l_run[0] *= alpha0;
-        l_run[1] *= alpha1;
-        const float g0 = alpha0 * fe, g1 = alpha1 * fe;
-#pragma unroll
-        for (int j = 0; j < KS; ++j) {
-          o[j][0] *= g0;
-          o[j][1] *= g1;
-          o[j][2] *= g0;
-          o[j][3] *= g1;
-        }
-      }
-      // 2^15 times the probabilities, times V's power of two in O's unit, 2^(vc - e_cur) <= 1
-      const float dv = vc == 255 ? e8m0_to_f32(255) : static_cast<float>(vc - e_cur);
-      const float ref0 = (m_run[0] == -INFINITY ? 0.f : m_run[0]) - 15.f - dv;
-      const float ref1 = (m_run[1] == -INFINITY ? 0.f : m_run[1]) - 15.f - dv;
-      uint32_t pb[2][2];  // P^T as the B operand of k-step t: heads down, keys across
-      float sum0 = 0.f, sum1 = 0.f;
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-          const float p0 = ex2(fmaf(sc[t][2 * r], f0, -ref0));
-          const float p1 = ex2(fmaf(sc[t][2 * r + 1], f1, -ref1));
-          sum0 += p0;
-          sum1 += p1;
-          pb[t][r] = movmatrix_trans(pack_f16(p0, p1));
-        }
-      const float back = ex2(-dv);
-      l_run[0] = fmaf(sum0, back, l_run[0]);
-      l_run[1] = fmaf(sum1, back, l_run[1]);
-      // ---- O^T += V^T P^T: lane's V row is k = lane of the two k-steps ----
-      {
-        const int a = lane & 15;
-        const int r = 2 * (a >> 2) + (a & 1);
-        const int key = (lane & 16) + ((a & 2) ? 8 + (r ^ 4) : r);
-#pragma unroll
-        for (int mt = 0; mt < KS; ++mt) {
-          uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
-          ldsm_b8_t(sV + swz8<D>(key, mt), r0, r1, r2, r3);
-          codes_f16(r0, a0, a2);
-          codes_f16(r1, a1, a3);
-          mma_f16(o[mt], a0, a1, a2, a3, pb[0][0], pb[0][1]);
-          codes_f16(r2, a0, a2);
-          codes_f16(r3, a1, a3);
-          mma_f16(o[mt], a0, a1, a2, a3, pb[1][0], pb[1][1]);
-        }
-      }
+    for (int ks = 0; ks < KS; ++ks) {
+      uint2 f = make_uint2(0u, 0u);
+      if (gq < G) f = *reinterpret_cast<const uint2*>(q_rows + (gq * D + 16 * ks + 4 * tq) * 2);
+      qa[ks][0] = f.x;
+      qa[ks][1] = f.y;
     }
-
-    if (issued < n_run) {
-      // generic-proxy writes to this stage are ordered before the next box into it
-      if (wrote_stage) asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-      __syncwarp();
-      request(s);
-      ++issued;
-    }
-    j += step;
-    if (++s == NST) {
-      s = 0;
-      phase ^= 1u;
-    }
-  }
-  if (gave_up) {
-    // Loads of this warp may still be on their way into its shared memory, and its barriers are no
-    // evidence: kDrainNs covers them (no load was requested since the flag went up).
-    cp_async_wait<0>();
-    const uint32_t t0 = global_ns32();
-    for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
-    if (lane == 0) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
-    l_run[0] = l_run[1] = 0.f;
-  }
-
-  // ---- the four warps' states, then the cluster's CTAs' ----
-  // Every warp sums its l over the lanes and leaves O in true units in its first stage: 8 columns of
-  // D floats, just the size of K's part, columns of odd pairs shifted so that the stores hit
-  // distinct banks.  After a barrier each thread takes four rows of the head dimension of one
-  // head, rescales and adds what the warps left, in warp order.
-  {
-#pragma unroll
-    for (int e = 0; e < 2; ++e)
-#pragma unroll
-      for (int off = 4; off < 32; off <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
-    __syncwarp();  // the warp is done with the stage
-    float* ow = reinterpret_cast<float*>(stages);
+    float qs[2], m_run[2], l_run[2];  // softmax scale * log2(e) * the heads' powers of two; maxima, sums
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
-      if (SOLO) f = l_run[e] > 0.f ? __fdividef(f, l_run[e]) : 0.f;  // that is all of it
-      float* col = ow + (2 * tq + e) * D;
-      if (2 * tq + e < G) {
+      qs[e] = 2 * tq + e < G ? q_factor[2 * tq + e] : 0.f;
+      m_run[e] = -INFINITY;
+      l_run[e] = 0.f;
+    }
+    int e_cur = -1, e_top = -1;  // the byte O is in units of; the largest so far
+    float o[KS][4];
+#pragma unroll
+    for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
+
+    bool gave_up = false;
+    int j = g0;  // block
+#pragma unroll 1
+    for (int i = 0;; ++i) {
+      if (SOLO) top_up();
+      if (i >= n_run) break;
+      uint8_t* stage = stages + s * S::kStage;
+      if (__any_sync(0xffffffffu, !mbar_wait(&full[s], phase))) {
+        gave_up = true;
+        break;
+      }
+      // the block: its rows that hold a key (bit r of mk), its bytes
+      const bool t1 = j < p.nb1;
+      const int jj = t1 ? j : j - p.nb1;
+      const int live = t1 ? (sq.bad ? 0 : p.k) : sq.count;
+      const int nk = min(max(live - jj * kQ8Block, 0), kQ8Block);
+      const uint32_t mk = nk == 32 ? 0xFFFFFFFFu : (1u << nk) - 1u;
+      int kc = scale_words[s * 8 + (jj & 3)], vc = scale_words[s * 8 + 4 + (jj & 3)];
+      bool wrote_stage = false;  // generic-proxy writes into the stage
+
+      if (FUSED && !t1 && sq.new_slot >= 0 && sq.new_slot / kQ8Block == jj) {
+        const int r = sq.new_slot & (kQ8Block - 1);
+        patch_block<D>(p, stage, u, r, sq.new_slot, mk & ~(1u << r), fresh, knew, kc, vc, lane);
+        wrote_stage = true;
+      }
+
+      if (mk != 0u) {
+        if (mk != 0xFFFFFFFFu) {
+          // Zero the V rows that hold no key: their probabilities are 0, but 0 times NaN is not.
+          if (!((mk >> lane) & 1u)) {
+#pragma unroll
+            for (int q = 0; q < D / 16; ++q)
+              *reinterpret_cast<uint4*>(stage + S::kV + swz8<D>(lane, q)) = make_uint4(0u, 0u, 0u, 0u);
+          }
+          __syncwarp();
+          wrote_stage = true;
+        }
+        const uint32_t sK = smem_addr(stage);
+        const uint32_t sV = smem_addr(stage + S::kV);
+        // ---- S^T = K Q^T, two products of 16 keys ----
+        // (two accumulator chains a product)
+        float sc[2][4], sd[2][4];  // product t: keys 16 t + gq (0, 1), 16 t + 8 + (gq ^ 4) (2, 3); heads 2 tq, 2 tq + 1
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          // lanes 0-7 / 8-15 / 16-23 / 24-31: rows 0-7 / 8-15 / 0-7 / 8-15 of the product, at
+          // bytes 32 kk .. + 15 / same / 32 kk + 16 .. + 31 / same
+          const int key = 16 * t + ((lane & 8) ? 8 + ((lane & 7) ^ 4) : lane & 7);
+#pragma unroll
+          for (int kk = 0; kk < KS / 2; ++kk) {
+            uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+            ldsm_x4(sK + swz8<D>(key, 2 * kk + (lane >> 4)), r0, r1, r2, r3);
+            codes_f16(r0, a0, a2);
+            codes_f16(r1, a1, a3);
+            if (kk == 0) mma_f16_zero(sc[t], a0, a1, a2, a3, qa[0][0], qa[0][1]);
+            else mma_f16(sc[t], a0, a1, a2, a3, qa[2 * kk][0], qa[2 * kk][1]);
+            codes_f16(r2, a0, a2);
+            codes_f16(r3, a1, a3);
+            if (kk == 0) mma_f16_zero(sd[t], a0, a1, a2, a3, qa[1][0], qa[1][1]);
+            else mma_f16(sd[t], a0, a1, a2, a3, qa[2 * kk + 1][0], qa[2 * kk + 1][1]);
+          }
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[t][e] += sd[t][e];
+        }
+        if (mk != 0xFFFFFFFFu) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (!((mk >> (16 * t + gq)) & 1u)) sc[t][0] = sc[t][1] = -INFINITY;
+            if (!((mk >> (16 * t + 8 + (gq ^ 4))) & 1u)) sc[t][2] = sc[t][3] = -INFINITY;
+          }
+        }
+        // ---- online softmax, log2 domain: f sc (f > 0) ----
+        const float ks2 = e8m0_to_f32(kc);
+        // (not below fp32's normal numbers: 0 times a masked score is no score)
+        constexpr float kLeast = 1.17549435e-38f;
+        float f0 = qs[0] * ks2, f1 = qs[1] * ks2;
+        if (f0 < kLeast) f0 = kLeast;
+        if (f1 < kLeast) f1 = kLeast;
+        float mx0 = fmaxf(fmaxf(sc[0][0], sc[0][2]), fmaxf(sc[1][0], sc[1][2]));
+        float mx1 = fmaxf(fmaxf(sc[0][1], sc[0][3]), fmaxf(sc[1][1], sc[1][3]));
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) {
+          mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
+          mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+        }
+        mx0 *= f0;
+        mx1 *= f1;
+        // The unit of O: at least 2^-64 of the largest block's, so that O stays far inside fp32.
+        int e_new = e_cur;
+        if (vc != 255) {
+          e_top = max(e_top, vc);
+          const int want = max(vc, e_top - 64);
+          if (want > e_cur || want + 10 < e_cur) e_new = want;
+        }
+        const bool up0 = mx0 > m_run[0], up1 = mx1 > m_run[1];
+        if (__any_sync(0xffffffffu, up0 || up1 || e_new != e_cur)) {
+          // (with e_cur = -1, before the first block, O is zero)
+          const float fe = e_cur < 0 ? 1.f : recode_factor(e_cur, max(e_new, 0));
+          e_cur = e_new;
+          const float alpha0 = up0 ? ex2(m_run[0] - mx0) : 1.f;
+          const float alpha1 = up1 ? ex2(m_run[1] - mx1) : 1.f;
+          if (up0) m_run[0] = mx0;
+          if (up1) m_run[1] = mx1;
+          l_run[0] *= alpha0;
+          l_run[1] *= alpha1;
+          const float g0 = alpha0 * fe, g1 = alpha1 * fe;
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            o[j][0] *= g0;
+            o[j][1] *= g1;
+            o[j][2] *= g0;
+            o[j][3] *= g1;
+          }
+        }
+        // 2^15 times the probabilities, times V's power of two in O's unit, 2^(vc - e_cur) <= 1
+        const float dv = vc == 255 ? e8m0_to_f32(255) : static_cast<float>(vc - e_cur);
+        const float ref0 = (m_run[0] == -INFINITY ? 0.f : m_run[0]) - 15.f - dv;
+        const float ref1 = (m_run[1] == -INFINITY ? 0.f : m_run[1]) - 15.f - dv;
+        uint32_t pb[2][2];  // P^T as the B operand of k-step t: heads down, keys across
+        float sum0 = 0.f, sum1 = 0.f;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int r = 0; r < 2; ++r) {
+            const float p0 = ex2(fmaf(sc[t][2 * r], f0, -ref0));
+            const float p1 = ex2(fmaf(sc[t][2 * r + 1], f1, -ref1));
+            sum0 += p0;
+            sum1 += p1;
+            pb[t][r] = movmatrix_trans(pack_f16(p0, p1));
+          }
+        const float back = ex2(-dv);
+        l_run[0] = fmaf(sum0, back, l_run[0]);
+        l_run[1] = fmaf(sum1, back, l_run[1]);
+        // ---- O^T += V^T P^T: lane's V row is k = lane of the two k-steps ----
+        {
+          const int a = lane & 15;
+          const int r = 2 * (a >> 2) + (a & 1);
+          const int key = (lane & 16) + ((a & 2) ? 8 + (r ^ 4) : r);
+#pragma unroll
+          for (int mt = 0; mt < KS; ++mt) {
+            uint32_t r0, r1, r2, r3, a0, a1, a2, a3;
+            ldsm_b8_t(sV + swz8<D>(key, mt), r0, r1, r2, r3);
+            codes_f16(r0, a0, a2);
+            codes_f16(r1, a1, a3);
+            mma_f16(o[mt], a0, a1, a2, a3, pb[0][0], pb[0][1]);
+            codes_f16(r2, a0, a2);
+            codes_f16(r3, a1, a3);
+            mma_f16(o[mt], a0, a1, a2, a3, pb[1][0], pb[1][1]);
+          }
+        }
+      }
+
+      // generic-proxy writes to this stage are ordered before the next box into it
+      if (SOLO ? jn < rn || u + hop < p.units : issued < n_run) {
+        if (wrote_stage) asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+      }
+      if (SOLO) {
+        --fly;
+      } else if (issued < n_run) {
+        request(s);
+        ++issued;
+      }
+      j += step;
+      if (++s == NST) {
+        s = 0;
+        phase ^= 1u;
+      }
+    }
+    if (gave_up) {
+      // Loads of this warp may still be on their way into its shared memory, and its barriers are no
+      // evidence: kDrainNs covers them (no load was requested since the flag went up).
+      cp_async_wait<0>();
+      const uint32_t t0 = global_ns32();
+      for (uint32_t it = 0; it < (1u << 16) && global_ns32() - t0 < kDrainNs; ++it) __nanosleep(1000);
+      if (lane == 0) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
+      l_run[0] = l_run[1] = 0.f;
+    }
+
+    // ---- the four warps' states, then the cluster's CTAs' ----
+    // Every warp sums its l over the lanes and leaves O in true units in its first stage: 8 columns of
+    // D floats, just the size of K's part, columns of odd pairs shifted so that the stores hit
+    // distinct banks.  After a barrier each thread takes four rows of the head dimension of one
+    // head, rescales and adds what the warps left, in warp order.
+    {
+#pragma unroll
+      for (int e = 0; e < 2; ++e)
+#pragma unroll
+        for (int off = 4; off < 32; off <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], off);
+      if constexpr (SOLO) {
+        // That is all of the unit: normalised and rounded, transposed back (head gq, two neighbours of
+        // the head dimension a lane) and left in the query's place, whose fragments are in registers;
+        // a head's 16-byte chunks are shifted by its number so that the stores hit distinct banks.
+        float f[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          f[e] = l_run[e] > 0.f ? __fdividef(e_cur < 0 ? 1.f : e8m0_to_f32(e_cur), l_run[e]) : 0.f;
+        uint32_t* row = reinterpret_cast<uint32_t*>(q_rows + gq * (D * 2));
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
-          col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
-          col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
+          const uint32_t y0 = movmatrix_trans(pack_bf16_rn(o[j][0] * f[0], o[j][1] * f[1]));
+          const uint32_t y1 = movmatrix_trans(pack_bf16_rn(o[j][2] * f[0], o[j][3] * f[1]));
+          if (gq < G) {
+            row[((2 * j) ^ gq) * 4 + tq] = y0;
+            row[((2 * j + 1) ^ gq) * 4 + tq] = y1;
+          }
         }
-      }
-    }
-    if (SOLO) {
-      __syncwarp();
+        __syncwarp();
 #pragma unroll
-      for (int xi = 0; xi < (NGR + 31) / 32; ++xi) {
-        const int x = lane + 32 * xi;
-        if (x < NGR) {
-          const int hh = (4 * x) / D;
-          const float4 y = *reinterpret_cast<const float4*>(ow + hh * D + ((4 * x) % D ^ (8 * (hh >> 1))));
-          *reinterpret_cast<uint2*>(p.out + static_cast<long long>(u) * (G * D) + 4 * x) =
-              make_uint2(pack_bf16_rn(y.x, y.y), pack_bf16_rn(y.z, y.w));
+        for (int x0 = 0; x0 < G * D / 8; x0 += 32) {
+          const int x = x0 + lane, hh = x / (D / 8), c = x % (D / 8);
+          if (x < G * D / 8)
+            *reinterpret_cast<uint4*>(p.out + static_cast<long long>(u) * (G * D) + 8 * x) =
+                *reinterpret_cast<const uint4*>(q_rows + hh * (D * 2) + (c ^ hh) * 16);
         }
+        if (FUSED && lane == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH)) {
+          if (!sq.bad) p.pos[b] = pos + 1;
+          p.tickets[b] = 0ull;
+        }
+        if (gave_up) return;
+        __syncwarp();
+        u += hop;
+        if (u >= p.units) return;
+        b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
+        pos = pos_next;
+        fresh = fresh_next;
+        issued = 0;
+        continue;
       }
-      if (FUSED && lane == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH)) {
-        if (!sq.bad) p.pos[b] = pos + 1;
-        p.tickets[b] = 0ull;
-      }
-      return;
-    }
-    if (gq == 0) {
-      float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 16 + 2 * tq;
+      __syncwarp();  // the warp is done with the stage
+      float* ow = reinterpret_cast<float*>(stages);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        ml[e] = m_run[e];
-        ml[8 + e] = l_run[e];
+        const float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
+        float* col = ow + (2 * tq + e) * D;
+        if (2 * tq + e < G) {
+#pragma unroll
+          for (int j = 0; j < KS; ++j) {
+            col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
+            col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
+          }
+        }
+      }
+      if (gq == 0) {
+        float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 16 + 2 * tq;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          ml[e] = m_run[e];
+          ml[8 + e] = l_run[e];
+        }
+      }
+      if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
+    }
+    __syncthreads();
+    if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
+      if (!sq.bad) p.pos[b] = pos + 1;
+      p.tickets[b] = 0ull;
+    }
+    const long long out_base = static_cast<long long>(u) * (G * D);
+    const float* ml = reinterpret_cast<const float*>(smem + S::kMl);
+    constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
+    float4 cacc[XPT];
+    float cls[XPT], cmx[XPT];
+#pragma unroll
+    for (int xi = 0; xi < XPT; ++xi) {
+      const int x = tid + xi * kThreads;
+      if (x >= NGR) break;
+      const int hh = (4 * x) / D;
+      const int c = (4 * x) % D;
+      float M = ml[hh];
+#pragma unroll
+      for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * 16 + hh]);
+      const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      float Ls = 0.f;
+#pragma unroll
+      for (int v = 0; v < kWarps; ++v) {
+        const float f = ex2(ml[v * 16 + hh] - Mr);
+        const float* left = reinterpret_cast<const float*>(smem + s_left[v]);
+        const float4 y = *reinterpret_cast<const float4*>(left + hh * D + (c ^ (8 * (hh >> 1))));
+        acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
+        acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
+        Ls = fmaf(f, ml[v * 16 + 8 + hh], Ls);
+      }
+      if (cm == 1) {
+        const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
+        *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
+            make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
+      } else {
+        cacc[xi] = acc;
+        cls[xi] = Ls;
+        cmx[xi] = M;
       }
     }
-    if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
-  }
-  __syncthreads();
-  if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
-    if (!sq.bad) p.pos[b] = pos + 1;
-    p.tickets[b] = 0ull;
-  }
-  const long long out_base = static_cast<long long>(u) * (G * D);
-  const float* ml = reinterpret_cast<const float*>(smem + S::kMl);
-  constexpr int XPT = (NGR + kThreads - 1) / kThreads;  // groups per thread
-  float4 cacc[XPT];
-  float cls[XPT], cmx[XPT];
+    if (cm == 1) return;
+    // One share of the unit per CTA: stored into the peers' receive areas, to each the groups that
+    // peer finishes; then merged in rank order.
+    const int SL = p.slice;
+    const uint32_t recv_a = smem_addr(smem + S::kRecv), ml_a = smem_addr(smem + S::kRecvMl);
+    const uint32_t bar_a = smem_addr(&recv_bar);
+    cluster_wait();
 #pragma unroll
-  for (int xi = 0; xi < XPT; ++xi) {
-    const int x = tid + xi * kThreads;
-    if (x >= NGR) break;
-    const int hh = (4 * x) / D;
-    const int c = (4 * x) % D;
-    float M = ml[hh];
-#pragma unroll
-    for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * 16 + hh]);
-    const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
-    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-    float Ls = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWarps; ++v) {
-      const float f = ex2(ml[v * 16 + hh] - Mr);
-      const float* left = reinterpret_cast<const float*>(smem + s_left[v]);
-      const float4 y = *reinterpret_cast<const float4*>(left + hh * D + (c ^ (8 * (hh >> 1))));
-      acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
-      acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-      Ls = fmaf(f, ml[v * 16 + 8 + hh], Ls);
+    for (int xi = 0; xi < XPT; ++xi) {
+      const int x = tid + xi * kThreads;
+      if (x >= NGR) break;
+      const int hh = (4 * x) / D;
+      const int to = x / SL;
+      st_peer_f4(peer_smem(recv_a + (rank * SL + x - to * SL) * 16, to), cacc[xi], peer_smem(bar_a, to));
+      if ((4 * x) % D == 0) {
+        for (int r = 0; r < cm; ++r)
+          st_peer_f2(peer_smem(ml_a + (rank * G + hh) * 8, r), cmx[xi], cls[xi], peer_smem(bar_a, r));
+      }
     }
-    if (cm == 1) {
-      const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
+    mbar_wait_peers(&recv_bar);
+    const int x0 = rank * SL, x1 = min(x0 + SL, NGR);
+    for (int x = x0 + tid; x < x1; x += kThreads) {
+      const int hh = (4 * x) / D;
+      const int c = (4 * x) % D;
+      const float2* pl = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
+      float M = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r)
+        if (r < cm) M = fmaxf(M, pl[r * G].x);
+      if (M == -INFINITY) M = 0.f;
+      float Ls = 0.f;
+      float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r) {
+        if (r < cm) {
+          const float2 mr = pl[r * G];
+          const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
+          const float f = ex2(mr.x - M);
+          Ls = fmaf(f, mr.y, Ls);
+          O.x = fmaf(f, o4.x, O.x);
+          O.y = fmaf(f, o4.y, O.y);
+          O.z = fmaf(f, o4.z, O.z);
+          O.w = fmaf(f, o4.w, O.w);
+        }
+      }
+      const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
       *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-          make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
-    } else {
-      cacc[xi] = acc;
-      cls[xi] = Ls;
-      cmx[xi] = M;
+          make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
     }
-  }
-  if (cm == 1) return;
-  // One share of the unit per CTA: stored into the peers' receive areas, to each the groups that
-  // peer finishes; then merged in rank order.
-  const int SL = p.slice;
-  const uint32_t recv_a = smem_addr(smem + S::kRecv), ml_a = smem_addr(smem + S::kRecvMl);
-  const uint32_t bar_a = smem_addr(&recv_bar);
-  cluster_wait();
-#pragma unroll
-  for (int xi = 0; xi < XPT; ++xi) {
-    const int x = tid + xi * kThreads;
-    if (x >= NGR) break;
-    const int hh = (4 * x) / D;
-    const int to = x / SL;
-    st_peer_f4(peer_smem(recv_a + (rank * SL + x - to * SL) * 16, to), cacc[xi], peer_smem(bar_a, to));
-    if ((4 * x) % D == 0) {
-      for (int r = 0; r < cm; ++r)
-        st_peer_f2(peer_smem(ml_a + (rank * G + hh) * 8, r), cmx[xi], cls[xi], peer_smem(bar_a, r));
-    }
-  }
-  mbar_wait_peers(&recv_bar);
-  const int x0 = rank * SL, x1 = min(x0 + SL, NGR);
-  for (int x = x0 + tid; x < x1; x += kThreads) {
-    const int hh = (4 * x) / D;
-    const int c = (4 * x) % D;
-    const float2* pl = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
-    float M = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < kMaxClusterCtas; ++r)
-      if (r < cm) M = fmaxf(M, pl[r * G].x);
-    if (M == -INFINITY) M = 0.f;
-    float Ls = 0.f;
-    float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int r = 0; r < kMaxClusterCtas; ++r) {
-      if (r < cm) {
-        const float2 mr = pl[r * G];
-        const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
-        const float f = ex2(mr.x - M);
-        Ls = fmaf(f, mr.y, Ls);
-        O.x = fmaf(f, o4.x, O.x);
-        O.y = fmaf(f, o4.y, O.y);
-        O.z = fmaf(f, o4.z, O.z);
-        O.w = fmaf(f, o4.w, O.w);
-      }
-    }
-    const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
-    *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-        make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
-  }
-  if (tid == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
+    if (tid == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
+  } while (SOLO);
 }
 
 // ---------------------------------------------------------------------------
@@ -803,8 +879,11 @@ static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
 //   wide   a CTA (or cluster) per unit, three stages a warp, two CTAs an SM: few or long units
 //   spread the same with two stages a warp and three CTAs an SM: when the units, or their
 //          clusters, just miss one wave of the first (176 x 61 blocks: two CTAs a unit in one
-//          wave 13.4 us, one a unit of the first 15.9)
-//   solo   a warp per unit, three stages a warp, two CTAs (eight units) an SM: many short units
+//          wave 15.9 us, one a unit of the first 20.1)
+//   solo   a warp per unit, three stages a warp, two CTAs (eight units) an SM: many short units.  Of
+//          units of up to twelve blocks a warp takes one after another, from a grid of one wave (8,192 of 6
+//          blocks 61.4 us, 75.7 with a CTA for every four; ragged 42.5 and 56.4; 2,048 19.9 and 22.0); longer
+//          ones are evened out better by the hardware (8,192 of 20 blocks 207.8 and 196.7)
 struct Q8Plan {
   enum { kWide, kSpread, kSolo } variant;
   int cm;    // CTAs per unit
@@ -855,8 +934,8 @@ static int resident_q8(int* wide, int* spread, int* solo) {
 //   16 x  2 blocks 3.4 / 3.4 / 5.8       300 x  3   4.0 /  4.6 /  5.3    512 x  3   7.2 /  7.0 /  5.5
 //   256 x 20       9.3 / 10.4 / 18.7     512 x 10  12.9 / 12.3 / 11.5    768 x 20  29.1 / 25.6 / 23.6
 //   256 x 40      14.8 / 17.0 / 33.9    1024 x 10  24.3 / 20.7 / 14.8   1216 x 20  41.3 / 38.7 / 31.1
-//   312 x 72      40.4 / 30.6 / -       2048 x  6  33.5 / 26.6 / 21.9   2048 x 10  45.5 / 36.5 / 31.7
-//   512 x 72      47.9 / 56.6 / -       2048 x  1  21.3 / 16.4 /  8.1   2048 x 20  65.6 / 60.1 / 53.8
+//   312 x 72      40.4 / 30.6 / -       2048 x  6  33.5 / 26.6 / 19.9   2048 x 10  45.5 / 36.5 / 29.2
+//   512 x 72      47.9 / 56.6 / -       2048 x  1  21.3 / 16.4 /  7.2   2048 x 20  65.6 / 60.1 / 53.8
 // (The blocks are those of a full ring: pos is on the device.)
 template <int D, int G, bool FUSED>
 static int plan_q8(long long units, int nb, Q8Plan* pl) {
@@ -884,7 +963,8 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
       *pl = {Q8Plan::kSpread, cm, static_cast<int>(units * cm)};
     }
   }
-  if (cost(quads, solo, nb, 11) < best) *pl = {Q8Plan::kSolo, 1, static_cast<int>(quads)};
+  if (cost(quads, solo, nb, 11) < best)
+    *pl = {Q8Plan::kSolo, 1, static_cast<int>(nb <= 12 ? std::min<long long>(quads, solo) : quads)};
   return CMC_OK;
 }
 

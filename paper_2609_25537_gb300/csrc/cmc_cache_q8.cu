@@ -265,7 +265,7 @@ __device__ __forceinline__ int recode_block(uint8_t* block, uint32_t others, uin
     c = block_code(max(top, __reduce_max_sync(0xffffffffu, held_bits(m, c_old))));
   }
   if (c != c_old) {
-    const float f = recode_factor(c_old, c);
+    const Recode f = recode_by(c_old, c);
 #pragma unroll
     for (int e = 0; e < CPR; ++e)
       if ((others >> ((lane + 32 * e) / CPR)) & 1u) reinterpret_cast<uint4*>(block)[lane + 32 * e] = recode16(x[e], f);

@@ -33,8 +33,7 @@ __device__ __forceinline__ float e8m0_to_f32(int c) {
 }
 // 2^(127 - c), what values are multiplied by to give codes.
 __device__ __forceinline__ float code_factor(int c) { return e8m0_to_f32(c == 255 ? 255 : 254 - c); }
-// 2^(c_old - c), what a block's codes are multiplied by when its byte goes from
-// c_old to c.  Limited to fp32's normal powers: below them every code gives 0.
+// 2^(c_old - c), limited to fp32's normal powers.
 __device__ __forceinline__ float recode_factor(int c_old, int c) {
   return c_old == 255 ? e8m0_to_f32(255)
                       : __uint_as_float(static_cast<uint32_t>(min(max(127 + c_old - c, 1), 254)) << 23);
@@ -61,47 +60,74 @@ __device__ __forceinline__ float scaled(float x, float f) { return fmaf(x, 0.f, 
 __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d, float f) {
   return e4m3_pair(scaled(a, f), scaled(b, f)) | (e4m3_pair(scaled(c, f), scaled(d, f)) << 16);
 }
-// Four codes to fp32.
-__device__ __forceinline__ void decode4(uint32_t w, float (&v)[4]) {
-  uint32_t lo, hi;
+// Four codes to fp16, exactly (lo: bytes 0 and 1).
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n"
       " cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
       : "=r"(lo), "=r"(hi)
       : "r"(w));
+}
+// Two fp16 values to fp32.
+__device__ __forceinline__ void f16x2_f32(uint32_t h, float& a, float& b) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.f32.f16 %0, a;\n cvt.f32.f16 %1, b;\n}\n"
-      : "=f"(v[0]), "=f"(v[1])
-      : "r"(lo));
-  asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.f32.f16 %0, a;\n cvt.f32.f16 %1, b;\n}\n"
-      : "=f"(v[2]), "=f"(v[3])
-      : "r"(hi));
+      : "=f"(a), "=f"(b)
+      : "r"(h));
+}
+// Four codes to fp32.
+__device__ __forceinline__ void decode4(uint32_t w, float (&v)[4]) {
+  uint32_t lo, hi;
+  codes_f16(w, lo, hi);
+  f16x2_f32(lo, v[0], v[1]);
+  f16x2_f32(hi, v[2], v[3]);
 }
 
-// 16 codes multiplied by f and rounded again.
-__device__ __forceinline__ uint32_t recode4(uint32_t w, float f) {
-  float v[4];
-  decode4(w, v);
-  return e4m3_pair(v[0] * f, v[1] * f) | (e4m3_pair(v[2] * f, v[3] * f) << 16);
+// Codes for another power of two are the old ones multiplied by 2^(c_old - c) and rounded again, in
+// fp16 and two steps (2^17, from the least code to the largest, is above fp16's largest).  Nothing is
+// lost on the way: codes are multiples of 2^-9, so a product below fp16's 2^-24 a step has no bits that
+// count, being below 2^-20, which e4m3 rounds to 0 (as it does all below 2^-10).
+struct Recode {
+  uint32_t first, second;  // fp16 factors, in both halves
+};
+__device__ __forceinline__ Recode recode_by(int c_old, int c) {
+  const int n = c_old - c, a = min(max(n, -14), 9), b = min(max(n - a, -14), 9);
+  return {c_old == 255 ? 0x7FFF7FFFu : static_cast<uint32_t>(15 + a) * 0x04000400u,
+          static_cast<uint32_t>(15 + b) * 0x04000400u};
 }
-__device__ __forceinline__ uint4 recode16(const uint4& x, float f) {
+__device__ __forceinline__ uint32_t recode4(uint32_t w, const Recode& f) {
+  uint32_t lo, hi, r;
+  codes_f16(w, lo, hi);
+  asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(lo) : "r"(f.first));
+  asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(hi) : "r"(f.first));
+  asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(lo) : "r"(f.second));
+  asm("mul.rn.f16x2 %0, %0, %1;\n" : "+r"(hi) : "r"(f.second));
+  asm("{\n .reg .b16 a, b;\n cvt.rn.satfinite.e4m3x2.f16x2 a, %1;\n cvt.rn.satfinite.e4m3x2.f16x2 b, %2;\n"
+      " mov.b32 %0, {a, b};\n}\n"
+      : "=r"(r)
+      : "r"(lo), "r"(hi));
+  return r;
+}
+__device__ __forceinline__ uint4 recode16(const uint4& x, const Recode& f) {
   return make_uint4(recode4(x.x, f), recode4(x.y, f), recode4(x.z, f), recode4(x.w, f));
 }
-// The largest magnitude code of 16 that are no NaN, bytewise in the result's
-// four bytes with `m`'s (e4m3 magnitudes are ordered as their bits).
+// The largest magnitudes of 16 codes that are no NaN and of `m`, in fp16, two at a time.  (In bytes, the
+// codes' bits being ordered as their magnitudes, it takes four times the instructions.)
 __device__ __forceinline__ uint32_t max_codes4(uint32_t m, uint32_t w) {
-  w &= 0x7F7F7F7Fu;
-  return __vmaxu4(m, w & ~__vcmpeq4(w, 0x7F7F7F7Fu));
+  uint32_t lo, hi;
+  codes_f16(w, lo, hi);
+  asm("{\n .reg .b32 a, b;\n abs.f16x2 a, %1;\n abs.f16x2 b, %2;\n max.f16x2 %0, %0, a;\n max.f16x2 %0, %0, b;\n}\n"
+      : "+r"(m)
+      : "r"(lo), "r"(hi));
+  return m;
 }
 __device__ __forceinline__ uint32_t max_codes16(uint32_t m, const uint4& x) {
   return max_codes4(max_codes4(max_codes4(max_codes4(m, x.x), x.y), x.z), x.w);
 }
-// The fp32 bits of the value of a largest magnitude code (see max_codes4) of a block with byte c,
+// The fp32 bits of the value of the larger of two largest magnitudes (max_codes16) of a block with byte c,
 // 0 if the byte is NaN.
 __device__ __forceinline__ uint32_t held_bits(uint32_t m, int c) {
-  m = __vmaxu4(m, m >> 16);
-  m = max(m & 0xFFu, (m >> 8) & 0xFFu);
-  float v[4];
-  decode4(m, v);
-  return c == 255 ? 0u : finite_bits(v[0] * e8m0_to_f32(c));
+  float a, b;
+  f16x2_f32(m, a, b);
+  return c == 255 ? 0u : finite_bits(fmaxf(a, b) * e8m0_to_f32(c));
 }
 
 }  // namespace cmc

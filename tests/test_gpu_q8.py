@@ -333,6 +333,11 @@ ATTN += [  # more units than resident CTAs: whole ones, cut ones, runs over many
     (700, 1, 1, 1, 64, 0, 33, [(i * 37) % 60 - 3 for i in range(700)]),
     (45, 1, 64, 8, 128, 70, 500, [(i * 131) % 700 for i in range(45)]),
     (500, 1, 8, 1, 64, 3, 300, [(i * 17) % 400 for i in range(500)]),
+    # a warp takes several units, of sequences with nothing, a little and a full ring
+    (700, 1, 4, 4, 128, 0, 40, [(i * 29) % 75 - 3 for i in range(700)]),
+    (2600, 1, 2, 1, 64, 0, 33, [(i * 11) % 50 - 2 for i in range(2600)]),
+    (7, 64, 8, 8, 64, 33, 70, [0, 1, 31, 64, 69, 70, 135]),
+    (170, 1, 64, 8, 128, 5, 20, [i % 25 for i in range(170)]),
     # clusters, three CTAs an SM: of two and of eight
     (44, 2, 8, 2, 64, 9, 1300, [(i * 131) % 1700 for i in range(44)]),
     (10, 1, 16, 4, 128, 1001, 2900, [1, 2, 40, 700, 1500, 2000, 2899, 2900, 2901, 9000]),
@@ -595,7 +600,8 @@ def test_whole_path(cuda_device):
     assert pos.tolist() == pos16.tolist() == [80, W + 55]
 
 
-@pytest.mark.parametrize("shape", [(1, 1, 8, 2, 64, 32, 128), (60, 2, 8, 4, 128, 40, 150)])
+@pytest.mark.parametrize("shape", [(1, 1, 8, 2, 64, 32, 128), (60, 2, 8, 4, 128, 40, 150),
+                                   (400, 1, 4, 4, 128, 3, 40)])
 def test_step_timeout_is_reported(cuda_device, shape):
     """With every stage's wait made to run out, the launch ends, the workspace's status word says so, and
     the context stays usable."""
