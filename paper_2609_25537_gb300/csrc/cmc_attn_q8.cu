@@ -12,12 +12,17 @@
 // known.  In the end the warps' states are merged in shared memory, the CTAs' of a
 // cluster in distributed shared memory (as in cmc_attn.cu).
 //
+// Many short units take a warp each instead, which needs no merge (SOLO).
+//
 // A grid may have many more CTAs than are resident: the hardware gives a free place to the
-// next unit, which evens out rings of different fill, and what one CTA waits for
-// (its first bytes, its merge) the others on the SM cover.  The depth of the rings of
-// stages sets how many those are: see plan_q8.  (Sharing out the live blocks of all units evenly
-// over the warps of one wave, with a kernel to merge the cut units, cost 10 us a launch
-// over this: 312 units of 256 + 2,048 keys 37 us, 304 of them here 28.)
+// next unit, and what one CTA waits for (its first bytes, its merge) the others on the SM
+// cover.  The depth of the rings of stages sets how many those are: see plan_q8.  Rings of
+// different fill are evened out by taking the longest sequences first (p.order): a long
+// unit that starts last sets the time of the launch.  512 units of 312 to 2,304 keys 25.0 us (in the order of
+// the batch 30.9), 1,024 48.8; full ones 48.9 and 97.8, which in batch order and the best variant take
+// 47.7 and 90.0: each CTA reads all positions, and sorts, before it knows its unit.  (Sharing out
+// the live blocks of all units evenly over the warps of one wave, with a kernel to merge the
+// cut units, cost 10 us a launch: 312 units of 256 + 2,048 keys 37 us, 304 of them here 28.)
 //
 // Both products run on fp16 operands with fp32 accumulation (mma.sync m16n8k16): the
 // codes are converted to fp16 in registers, exactly, one instruction for two.  (mma.sync
@@ -59,6 +64,7 @@ struct AttnQ8Params : AttnParams {  // t1k, t1v, ring_k, ring_v, idx and the til
   int units;
   int nb1, nb2;               // blocks of Tier-1, and of the whole ring
   int rope;                   // rotate q and the new key (fused step)
+  int order;                  // units of the longest sequences first
 };                            // cm: CTAs per unit
 
 // Shared memory of a CTA: the query in fp16, its heads' factors, the rotated new key, the stages'
@@ -284,6 +290,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   __shared__ __align__(8) uint64_t recv_bar;  // clusters: the peers' stores
   __shared__ int s_left[kWarps];              // where the warps left their outputs
   __shared__ long long s_pos[kWarps];
+  __shared__ __align__(16) int s_live[kThreads];  // p.order: the sequences' lengths
+  __shared__ int s_seq;                           // and the CTA's sequence
+  __shared__ bool s_last;                         // fused: the last of the CTAs that tickets count
 
   const int tid = threadIdx.x;
   const int lane = tid & 31;
@@ -330,7 +339,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   }
   if (cm > 1) cluster_arrive();  // waited for before the first store into a peer
   // Before the grid dependency wait: the first blocks into L2.
-  if (lane == 0) {
+  if (lane == 0 && !p.order) {
 #pragma unroll 1
     for (int i = 0, j = g0; i < p.l2_prefetch && j < nb_all; ++i, j += step)
       tma_box3_prefetch(j < p.nb1 ? &maps.t1 : &maps.ring, (j < p.nb1 ? j : j - p.nb1) * kQ8Block, 2 * u);
@@ -343,6 +352,30 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
   }
   asm volatile("griddepcontrol.wait;\n" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  if (!SOLO && p.order) {
+    // The unit of place u / LH in the sequences' order by length, the longest first.  All CTAs see the
+    // same positions, which the last of them advances in the end.
+    int mine = -2;
+    if (tid < p.B) {
+      const long long x = ld_pos(p, tid);
+      mine = static_cast<int>(x < 0 ? -1 : x < p.W ? x : p.W);
+    }
+    s_live[tid] = mine;
+    __syncthreads();
+    if (tid < p.B) {
+      int place = 0;
+#pragma unroll 4
+      for (int i = 0; i < p.B; i += 4) {
+        const int4 x = *reinterpret_cast<const int4*>(s_live + i);
+        place += (x.x > mine || (x.x == mine && i < tid)) + (x.y > mine || (x.y == mine && i + 1 < tid)) +
+                 (x.z > mine || (x.z == mine && i + 2 < tid)) + (x.w > mine || (x.w == mine && i + 3 < tid));
+      }
+      if (place == b) s_seq = tid;
+    }
+    __syncthreads();
+    u += (s_seq - b) * p.LH;
+    b = s_seq;
+  }
 
   // blocks of the warp, as far as known before pos
   int n_run = SOLO ? nb_all : g0 < nb_all ? (nb_all - g0 + step - 1) / step : 0;
@@ -456,7 +489,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     if (SOLO) __syncwarp();
     else __syncthreads();
     // The last to have read pos[b] advances it (in the end: the count takes a trip to L2).
-    if (FUSED && first_thread) ticket = atomicAdd(p.tickets + b, 1ull);
+    if (FUSED && first_thread) ticket = atomicAdd(p.tickets + (p.order ? 0 : b), 1ull);
 
     // Live blocks; those that were requested in vain hold no key.
     const int nb = live_blocks(p, sq);
@@ -761,11 +794,13 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         }
       }
       if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
+      if (FUSED && tid == 0) s_last = ticket + 1 == static_cast<unsigned long long>(p.order ? p.units : p.LH) * cm;
     }
     __syncthreads();
-    if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * cm) {
-      if (!sq.bad) p.pos[b] = pos + 1;
-      p.tickets[b] = 0ull;
+    if (FUSED && s_last && tid < (p.order ? p.B : 1)) {
+      const long long x = p.order ? ld_pos(p, tid) : pos;
+      if (x >= 0) p.pos[p.order ? tid : b] = x + 1;
+      if (tid == 0) p.tickets[p.order ? 0 : b] = 0ull;
     }
     const long long out_base = static_cast<long long>(u) * (G * D);
     const float* ml = reinterpret_cast<const float*>(smem + S::kMl);
@@ -886,8 +921,9 @@ static int q8_blocks(int rows) { return (rows + kQ8Block - 1) / kQ8Block; }
 //          ones are evened out better by the hardware (8,192 of 20 blocks 207.8 and 196.7)
 struct Q8Plan {
   enum { kWide, kSpread, kSolo } variant;
-  int cm;    // CTAs per unit
-  int ctas;  // grid size
+  int cm;      // CTAs per unit
+  int ctas;    // grid size
+  bool order;  // the units of the longest sequences first
 };
 
 // CTAs of a variant that fit an SM of the current device.
@@ -936,9 +972,11 @@ static int resident_q8(int* wide, int* spread, int* solo) {
 //   256 x 40      14.8 / 17.0 / 33.9    1024 x 10  24.3 / 20.7 / 14.8   1216 x 20  41.3 / 38.7 / 31.1
 //   312 x 72      40.4 / 30.6 / -       2048 x  6  33.5 / 26.6 / 19.9   2048 x 10  45.5 / 36.5 / 29.2
 //   512 x 72      47.9 / 56.6 / -       2048 x  1  21.3 / 16.4 /  7.2   2048 x 20  65.6 / 60.1 / 53.8
-// (The blocks are those of a full ring: pos is on the device.)
+// (The blocks are those of a full ring: pos is on the device.)  Several waves of long units, ordered by
+// length, count for 85 % of their time: where rings differ they are evened out, which a warp with a long unit of its own
+// is not (1,024 x 72 blocks, wide / solo: full 97.8 / 90.0 us, ragged 48.8 / 72.5).
 template <int D, int G, bool FUSED>
-static int plan_q8(long long units, int nb, Q8Plan* pl) {
+static int plan_q8(long long units, int B, int nb, Q8Plan* pl) {
   int wide = 0, spread = 0, solo = 0;  // CTAs resident at a time
   const int st = resident_q8<D, G, FUSED>(&wide, &spread, &solo);
   if (st != CMC_OK) return st;
@@ -947,24 +985,33 @@ static int plan_q8(long long units, int nb, Q8Plan* pl) {
     return (ctas + slots - 1) / slots * (30 + static_cast<long long>(blocks) * per_block);
   };
   const long long quads = (units + kWarps - 1) / kWarps;
+  const bool order = B > 1 && B <= kThreads;
   long long best = -1;
   for (int cm = 1; cm <= kMaxClusterCtas && (cm == 1 || kWarps * cm / 2 < nb); cm *= 2) {
     const int blocks = (nb + kWarps * cm - 1) / (kWarps * cm), merge = cm > 1 ? 3 : 0;  // a cluster's: 0.3 us
     // A cluster lies in one group of SMs, and eight CTAs do not fill every group: 56 clusters of eight in
     // 456 places took two waves (56 x 128 blocks 17.5 us, with clusters of four 12.8).
     const int w = cm == 8 ? wide * 7 / 8 : wide, p3 = cm == 8 ? spread * 7 / 8 : spread;
-    const long long a = cost(units * cm, w, blocks, 11) + merge, c = cost(units * cm, p3, blocks, 15) + merge;
-    if (best < 0 || a < best) {
-      best = a;
-      *pl = {Q8Plan::kWide, cm, static_cast<int>(units * cm)};
+    // several waves of whole units only
+    if (cm == 1 || units * cm <= w) {
+      const bool ordered = order && units * cm > w;
+      long long t = cost(units * cm, w, blocks, 11) + merge;
+      if (ordered && nb >= 32) t = t * 17 / 20;
+      if (best < 0 || t < best) {
+        best = t;
+        *pl = {Q8Plan::kWide, cm, static_cast<int>(units * cm), ordered};
+      }
     }
-    if (c < best) {
-      best = c;
-      *pl = {Q8Plan::kSpread, cm, static_cast<int>(units * cm)};
+    if (cm == 1 || units * cm <= p3) {
+      const long long t = cost(units * cm, p3, blocks, 15) + merge;
+      if (t < best) {
+        best = t;
+        *pl = {Q8Plan::kSpread, cm, static_cast<int>(units * cm), order && units * cm > p3};
+      }
     }
   }
   if (cost(quads, solo, nb, 11) < best)
-    *pl = {Q8Plan::kSolo, 1, static_cast<int>(nb <= 12 ? std::min<long long>(quads, solo) : quads)};
+    *pl = {Q8Plan::kSolo, 1, static_cast<int>(nb <= 12 ? std::min<long long>(quads, solo) : quads), false};
   return CMC_OK;
 }
 
@@ -1009,8 +1056,8 @@ static int by_shape(int d, int G, Args&&... args) {
 }
 template <int D, int G>
 struct PlanQ8 {
-  static int run(bool fused, long long units, int nb, Q8Plan* pl) {
-    return fused ? plan_q8<D, G, true>(units, nb, pl) : plan_q8<D, G, false>(units, nb, pl);
+  static int run(bool fused, long long units, int B, int nb, Q8Plan* pl) {
+    return fused ? plan_q8<D, G, true>(units, B, nb, pl) : plan_q8<D, G, false>(units, B, nb, pl);
   }
 };
 template <int D, int G>
@@ -1018,8 +1065,9 @@ struct LaunchQ8 {
   template <bool FUSED>
   static int go(const Q8Maps& maps, AttnQ8Params& p, long long units, cudaStream_t s) {
     Q8Plan pl;
-    int st = plan_q8<D, G, FUSED>(units, p.nb1 + p.nb2, &pl);
+    int st = plan_q8<D, G, FUSED>(units, p.B, p.nb1 + p.nb2, &pl);
     if (st != CMC_OK) return st;
+    p.order = pl.order;
     switch (pl.variant) {
       case Q8Plan::kSolo: return launch_q8<D, G, FUSED, 3, true>(maps, p, pl, s);
       case Q8Plan::kSpread: return launch_q8<D, G, FUSED, 2, false>(maps, p, pl, s);
@@ -1127,7 +1175,7 @@ int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas) {
   const cmc_dims& m = *dims;
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
   Q8Plan pl;
-  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, q8_blocks(m.k) + q8_blocks(m.W), &pl);
+  st = by_shape<PlanQ8>(m.d, m.Hq / m.Hkv, fused != 0, units, m.B, q8_blocks(m.k) + q8_blocks(m.W), &pl);
   if (st != CMC_OK) return st;
   *ctas = pl.ctas;
   return CMC_OK;
