@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t encode4_bf16(uint32_t a, uint32_t b, uint32_
 // rate), 16,384 rows of 64 units 127 us (94 %).  At d = 128 an SM holds 20 warps with one stage
 // each and 12 with two: one stage where every block then has a warp of its own (2,048 blocks
 // 4.9 us, 6.2 with two), else two (20,480 blocks, a third of their rows with a token, 24.4 us,
-// 28.7 with one).
+// 28.7 with one; 22.1 since blocks without a token are only written).
 template <int D, int NST>
 __global__ void __launch_bounds__(kRowThreads)
 quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict__ bank_v,
@@ -126,45 +126,54 @@ quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict_
     if (jb == nb - 1 && nb + lane < S) sc[nb + lane] = 0;  // the padding, at most three bytes
     uint4 x[NP];
     uint32_t m = 0u;  // largest magnitude, bf16 bits in two halves
+    if (h.rows != 0u) {
 #pragma unroll
-    for (int e = 0; e < NP; ++e) {
-      x[e] = make_uint4(0u, 0u, 0u, 0u);
-      if ((h.rows >> (e * RPP + lane / (32 / RPP))) & 1u) x[e] = *reinterpret_cast<const uint4*>(from + e * 512);
-      m = __vmaxu2(m, x[e].x & 0x7FFF7FFFu);
-      m = __vmaxu2(m, x[e].y & 0x7FFF7FFFu);
-      m = __vmaxu2(m, x[e].z & 0x7FFF7FFFu);
-      m = __vmaxu2(m, x[e].w & 0x7FFF7FFFu);
+      for (int e = 0; e < NP; ++e) {
+        x[e] = make_uint4(0u, 0u, 0u, 0u);
+        if ((h.rows >> (e * RPP + lane / (32 / RPP))) & 1u) x[e] = *reinterpret_cast<const uint4*>(from + e * 512);
+        m = __vmaxu2(m, x[e].x & 0x7FFF7FFFu);
+        m = __vmaxu2(m, x[e].y & 0x7FFF7FFFu);
+        m = __vmaxu2(m, x[e].z & 0x7FFF7FFFu);
+        m = __vmaxu2(m, x[e].w & 0x7FFF7FFFu);
+      }
     }
     __syncwarp();  // the stage is free
     if (job + NST * stride < jobs) {
       request(s, next);
       next = plan(job + (NST + 1) * stride);
     }
-    uint32_t top = __reduce_max_sync(0xffffffffu, max(m & 0xFFFFu, m >> 16));
-    if (top >= 0x7F80u) {  // an infinity or NaN among them: both become NaN, and do not count
-      top = 0u;
+    int c = 0;
+    if (h.rows != 0u) {
+      uint32_t top = __reduce_max_sync(0xffffffffu, max(m & 0xFFFFu, m >> 16));
+      if (top >= 0x7F80u) {  // an infinity or NaN among them: both become NaN, and do not count
+        top = 0u;
 #pragma unroll
-      for (int e = 0; e < NP; ++e) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&x[e]);
+        for (int e = 0; e < NP; ++e) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&x[e]);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < 4; ++q) {
 #pragma unroll
-          for (int sh = 0; sh < 32; sh += 16) {
-            const uint32_t a = (w[q] >> sh) & 0x7FFFu;
-            if (a >= 0x7F80u) w[q] |= 0x7FFFu << sh;
-            else top = max(top, a);
+            for (int sh = 0; sh < 32; sh += 16) {
+              const uint32_t a = (w[q] >> sh) & 0x7FFFu;
+              if (a >= 0x7F80u) w[q] |= 0x7FFFu << sh;
+              else top = max(top, a);
+            }
           }
         }
+        top = __reduce_max_sync(0xffffffffu, top);
       }
-      top = __reduce_max_sync(0xffffffffu, top);
-    }
-    const int c = block_code(top << 16);
-    const uint32_t f2 = __byte_perm(__float_as_uint(code_factor(c)), 0u, 0x3232);  // in bf16, twice
+      c = block_code(top << 16);
+      const uint32_t f2 = __byte_perm(__float_as_uint(code_factor(c)), 0u, 0x3232);  // in bf16, twice
 #pragma unroll
-    for (int e = 0; e < NP; ++e) {
-      if (h.r0 + e * RPP + lane / (32 / RPP) < k)
-        *reinterpret_cast<uint2*>(dst + e * 256) =
-            make_uint2(encode4_bf16(x[e].x, x[e].y, f2), encode4_bf16(x[e].z, x[e].w, f2));
+      for (int e = 0; e < NP; ++e) {
+        if (h.r0 + e * RPP + lane / (32 / RPP) < k)
+          *reinterpret_cast<uint2*>(dst + e * 256) =
+              make_uint2(encode4_bf16(x[e].x, x[e].y, f2), encode4_bf16(x[e].z, x[e].w, f2));
+      }
+    } else {  // no token: codes and power of two are zero
+#pragma unroll
+      for (int e = 0; e < NP; ++e)
+        if (h.r0 + e * RPP + lane / (32 / RPP) < k) *reinterpret_cast<uint2*>(dst + e * 256) = make_uint2(0u, 0u);
     }
     if (lane == 0) sc[jb] = static_cast<uint8_t>(c);
     if (++s == NST) {

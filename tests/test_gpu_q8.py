@@ -339,8 +339,8 @@ ATTN += [  # more units than resident CTAs: whole ones, cut ones, runs over many
     (7, 64, 8, 8, 64, 33, 70, [0, 1, 31, 64, 69, 70, 135]),
     (170, 1, 64, 8, 128, 5, 20, [i % 25 for i in range(170)]),
     # several waves of whole units, the longest sequences first
-    (64, 1, 8, 8, 128, 37, 1500, [(i * 131) % 1900 - 3 for i in range(64)]),
-    (128, 6, 2, 1, 64, 0, 1700, [0, 5, 5, 1700, 1701, 3400] + [(i * 97) % 1800 for i in range(122)]),
+    (64, 1, 8, 8, 128, 37, 1000, [(i * 131) % 1900 - 3 for i in range(64)]),
+    (128, 6, 2, 1, 64, 0, 1060, [0, 5, 5, 1060, 1061, 3400] + [(i * 97) % 1800 for i in range(122)]),
     # clusters, three CTAs an SM: of two and of eight
     (44, 2, 8, 2, 64, 9, 1300, [(i * 131) % 1700 for i in range(44)]),
     (10, 1, 16, 4, 128, 1001, 2900, [1, 2, 40, 700, 1500, 2000, 2899, 2900, 2901, 9000]),
