@@ -20,9 +20,10 @@
  * ---------------------------------------
  *  - Every tensor argument is a DEVICE pointer to memory the caller owns.  The
  *    library allocates no memory and keeps no state between calls apart from
- *    the thread-local last CUDA error, a per-device SM-count cache, the
- *    rotary frequency tables of cmc_decode_step_rope (at most 16 on the host
- *    and 16 per device, each written once per (theta, d)), the static score array of cmc_score_select_static and
+ *    the thread-local last CUDA error, per-device counts of SMs and of what
+ *    they hold of a kernel, the rotary frequency tables of cmc_decode_step_rope
+ *    and of cmc_decode_step_q8 (for each at most 16 on the host and 16 per device,
+ *    each written once per (theta, d)), the static score array of cmc_score_select_static and
  *    two process-wide settings of the attention launches
  *    (cmc_set_l2_prefetch_tiles, cmc_test_stall_attention_waits).
  *  - All work is enqueued on `stream` (a cudaStream_t passed as void*; NULL is
@@ -573,8 +574,9 @@ CMC_API int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* 
 
 /* Launch plan of the calls over a cache in 8 bits for `dims` on the current device
  * (fused == 0: cmc_two_tier_decode_attn_q8, else cmc_decode_step_q8): *ctas receives
- * the grid size of their one kernel, a CTA or a cluster of up to 8 for every
- * (sequence, layer, KV head) unit. */
+ * the grid size of their one kernel: a CTA or a cluster of up to 8 for every
+ * (sequence, layer, KV head) unit, or a CTA of four warps that take a unit each, and
+ * more units one after another where they are short. */
 CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas);
 
 /* ------------------------------------------------------------------------ *
