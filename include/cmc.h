@@ -408,8 +408,8 @@ CMC_API int cmc_decode_step_rope(const void* q, const void* tier1_k, const void*
  * bits) into *flags, waiting for `stream`, and clears it when `clear` != 0. */
 CMC_API int cmc_read_status(void* workspace, int clear, uint32_t* flags, void* stream);
 
-/* Tuning of the attention launches (cmc_two_tier_decode_attn,
- * cmc_decode_step, cmc_decode_step_rope) made afterwards, from any thread:
+/* Tuning of the attention launches (cmc_two_tier_decode_attn, cmc_decode_step,
+ * cmc_decode_step_rope and those over a cache in 8 bits) made afterwards, from any thread:
  * before its grid dependency wait every CTA asks L2 to prefetch the K/V boxes
  * of its first `tiles` tiles (64 keys each), so that under programmatic
  * dependent launch they stream in while the kernel before it on the stream
@@ -419,7 +419,9 @@ CMC_API int cmc_read_status(void* workspace, int clear, uint32_t* flags, void* s
  * CTAs take whole units), any other depth is taken as it is.  0 was best when
  * four independent requests' launches ran on four streams (their launches
  * already overlap); with 0, staging copies of 32 KB or more (cmc_stage_copies) also
- * let the launch after them start with their end only.  CMC_ERR_RANGE unless 0 <= tiles <= 64. */
+ * let the launch after them start with their end only.  CMC_ERR_RANGE unless 0 <= tiles <= 64.
+ * Over a cache in 8 bits a tile is a block of 32 keys, every warp prefetches, and three are the
+ * most it takes. */
 CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 
 /* Test hook for the failure path of the attention kernels (not part of the
