@@ -426,8 +426,8 @@ CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 
 /* Test hook for the failure path of the attention kernels (not part of the
  * method; off unless called).  With on != 0, every pipeline stage of the
- * attention launches made afterwards (cmc_two_tier_decode_attn,
- * cmc_decode_step, cmc_decode_step_rope, from any thread) expects 16 bytes
+ * attention launches made afterwards (cmc_two_tier_decode_attn, cmc_decode_step,
+ * cmc_decode_step_rope and those over a cache in 8 bits, from any thread) expects 16 bytes
  * more than its loads deliver, so no stage ever completes: each CTA's first
  * wait gives up after its 1 s limit, the CTA's other waits end at once (but for a
  * cluster's wait for what its CTAs store into each other, which is stalled
