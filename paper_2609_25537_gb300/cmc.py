@@ -587,7 +587,8 @@ def _kept(key: Tuple, value: Tuple) -> Tuple:
 
 
 def _as(dtype: torch.dtype, index: int, *tensors) -> bool:
-    """Whether all tensors (None: none) have this type and device and are contiguous."""
+    """Whether all tensors (None: none) have this type and device and are contiguous.
+    (Raises AttributeError for what is no tensor; a call then checks them one by one.)"""
     for t in tensors:
         if t is not None and (t.dtype is not dtype or t.get_device() != index
                               or not t.is_contiguous()):
@@ -608,7 +609,7 @@ def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor]
     _need(k, "k", torch.bfloat16, 5)
     dev = k.device
     index = dev.index
-    if not _as(torch.bfloat16, index, v) or v.shape != k.shape:
+    if not isinstance(v, torch.Tensor) or not _as(torch.bfloat16, index, v) or v.shape != k.shape:
         _need(v, "v", torch.bfloat16, 5, dev)
         raise ValueError("v must have the shape of k")
     rows = _need_rows(idx, count, k, 3, dev)
@@ -647,9 +648,11 @@ def dequantize_cache(kv: torch.Tensor, scales: torch.Tensor, idx: Optional[torch
     dev = kv.device
     index = dev.index
     rows = _need_rows(idx, None, kv, 4, dev)
-    key = ("dequantize", kv.shape, scales.shape, rows)
-    kept = _shapes_cache.get(key)
-    if kept is None or not _as(_E8M0, index, scales):
+    kept = None
+    if isinstance(scales, torch.Tensor) and _as(_E8M0, index, scales):
+        key = ("dequantize", kv.shape, scales.shape, rows)
+        kept = _shapes_cache.get(key)
+    if kept is None:
         B, L, Hkv, _, N, d = _need_q8(kv, scales, "cache", dev)
         dims = CmcDims(B, L, Hkv, Hkv, d, N, rows, 1)
         kept = _kept(key, ((B, L, Hkv, rows, d), dims, ctypes.byref(dims)))
@@ -681,11 +684,14 @@ def window_append_q8(ring_kv: torch.Tensor, ring_scales: torch.Tensor, pos: torc
     _need(ring_kv, "ring_kv", _E4M3, 6)
     dev = ring_kv.device
     index = dev.index
-    key = None
-    if (_as(_E8M0, index, ring_scales) and _as(torch.int64, index, pos)
-            and _as(torch.bfloat16, index, k_new, v_new)):
-        key = ("append", ring_kv.shape, ring_scales.shape, pos.shape, k_new.shape, v_new.shape)
-    kept = _shapes_cache.get(key) if key else None
+    kept = None
+    try:
+        if (_as(_E8M0, index, ring_scales) and _as(torch.int64, index, pos)
+                and _as(torch.bfloat16, index, k_new, v_new)):
+            key = ("append", ring_kv.shape, ring_scales.shape, pos.shape, k_new.shape, v_new.shape)
+            kept = _shapes_cache.get(key)
+    except AttributeError:
+        pass
     if kept is None:
         B, L, Hkv, _, W, d = _need_q8(ring_kv, ring_scales, "ring", dev)
         _need(pos, "pos", torch.int64, 1, dev)
@@ -771,13 +777,15 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     DecodeWorkspace(dims, device, q8=True); without one the call keeps one per stream and
     batch size, and a captured call gets one of its own, zero-filled at every replay."""
     kept, index = None, -1
-    if isinstance(q, torch.Tensor) and isinstance(ring_kv, torch.Tensor):
+    try:
         index = q.get_device()
         if (index >= 0 and _as(torch.bfloat16, index, q) and _as(_E4M3, index, ring_kv, tier1_kv)
                 and _as(_E8M0, index, ring_scales, tier1_scales) and _as(torch.int64, index, pos)):
             kept = _shapes_cache.get((q.shape, ring_kv.shape, ring_scales.shape, pos.shape,
                                       None if tier1_kv is None else tier1_kv.shape,
                                       None if tier1_scales is None else tier1_scales.shape))
+    except AttributeError:
+        pass
     if kept is None:
         kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, None,
                              "cmc_two_tier_decode_attn_q8")
@@ -817,7 +825,7 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     elif not rope_theta > 0:
         raise ValueError("rope_theta must be positive")
     kept, index = None, -1
-    if isinstance(q, torch.Tensor) and isinstance(k_new, torch.Tensor):
+    try:
         index = q.get_device()
         if (index >= 0 and _as(torch.bfloat16, index, q, k_new, v_new)
                 and _as(_E4M3, index, ring_kv, tier1_kv)
@@ -826,6 +834,8 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
                                       None if tier1_kv is None else tier1_kv.shape,
                                       None if tier1_scales is None else tier1_scales.shape,
                                       k_new.shape, v_new.shape))
+    except AttributeError:
+        pass
     if kept is None:
         kept = _attn_q8_kept(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, (k_new, v_new),
                              "cmc_decode_step_q8")

@@ -718,6 +718,16 @@ def test_binding_refusals(cuda_device):
     ]:
         with pytest.raises(exc):
             call()
+    # no tensor where one has to be, after calls of the same shapes that were right
+    for fn, good in ((cmc.quantize_cache, [bank, bank]), (cmc.dequantize_cache, [kv, scales]),
+                     (cmc.window_append_q8, [kv, scales, pos, row, row]),
+                     (attn, [q, kv.clone(), scales.clone(), kv, scales, pos]),
+                     (cmc.decode_step_q8, [q, kv.clone(), scales.clone(), kv, scales, pos, row, row])):
+        fn(*good)
+        for i in range(len(good)):
+            for bad in (None, [1, 2], good[i].cpu()):
+                with pytest.raises((TypeError, ValueError)):
+                    fn(*good[:i], bad, *good[i + 1:])
     small = cmc.DecodeWorkspace(cmc.CmcDims(1, 1, 2, 2, 64, 1, 0, 1), dev, q8=True)
     small.nbytes = 511
     with pytest.raises(cmc.CmcError):
