@@ -338,6 +338,7 @@ ATTN += [  # more units than resident CTAs: whole ones, cut ones, runs over many
     (2600, 1, 2, 1, 64, 0, 33, [(i * 11) % 50 - 2 for i in range(2600)]),
     (7, 64, 8, 8, 64, 33, 70, [0, 1, 31, 64, 69, 70, 135]),
     (170, 1, 64, 8, 128, 5, 20, [i % 25 for i in range(170)]),
+    (24, 8, 32, 8, 128, 30, 130, [0, -4, 260, 130, 129] + [(i * 37) % 150 for i in range(19)]),
     # several waves of whole units, the longest sequences first
     (64, 1, 8, 8, 128, 37, 1000, [(i * 131) % 1900 - 3 for i in range(64)]),
     (128, 6, 2, 1, 64, 0, 1060, [0, 5, 5, 1060, 1061, 3400] + [(i * 97) % 1800 for i in range(122)]),
