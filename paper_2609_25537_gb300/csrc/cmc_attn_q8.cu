@@ -485,7 +485,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       for (int e = 0; e < E; e += 2) to[e / 2] = pack_f16(x[h][e] * f, x[h][e + 1] * f);
       if (lane == 0) q_factor[hh] = e8m0_to_f32(qc) * p.scale_log2;
     }
-    if (FUSED && lane == 0) s_pos[warp] = pos;  // (so that every warp has it, not only asked for it)
+    // Every warp has pos before the count below says so, and has not only asked for it: the store waits for
+    // the load.  (Nothing reads it, so it has to be volatile to be there.)
+    if (FUSED && lane == 0) *static_cast<volatile long long*>(s_pos + warp) = pos;
     if (SOLO) __syncwarp();
     else __syncthreads();
     // The last to have read pos[b] advances it (in the end: the count takes a trip to L2).
