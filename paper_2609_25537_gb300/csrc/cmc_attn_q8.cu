@@ -79,8 +79,8 @@ struct Q8Smem {
   static constexpr int kQs = kQ + kUnits * G * D * 2;       // [unit][8] fp32
   static constexpr int kKnew = kQs + kUnits * 32;           // [unit][D] fp32
   static constexpr int kScale = kKnew + kUnits * D * 4;     // [warp][NST][2] words
-  static constexpr int kMl = kScale + kWarps * NST * 8;     // [warp][8 maxima, 8 sums]
-  static constexpr int kRecv = kMl + kWarps * 64;           // groups of 16 bytes, rank by rank
+  static constexpr int kMl = kScale + kWarps * NST * 8;     // [warp][8 maxima, 8 sums, 8 units]
+  static constexpr int kRecv = kMl + kWarps * 96;           // groups of 16 bytes, rank by rank
   static constexpr int kRecvMl = kRecv + (G * D / 4 + kMaxClusterCtas - 2) * 16;
   static constexpr int kSmall = SOLO ? kMl : kRecvMl + kMaxClusterCtas * G * 8;
   static constexpr int kBytes = kSmall + 1008 + kWarps * NST * kStage;
@@ -139,6 +139,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+
+// Stands for minus infinity where differences of two of them are taken.
+constexpr float kNone = -3e38f;
 
 // Live blocks of a unit whose sequence's state is sq.
 __device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState& sq) {
@@ -724,10 +727,14 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     }
 
     // ---- the four warps' states, then the cluster's CTAs' ----
-    // Every warp sums its l over the lanes and leaves O in true units in its first stage: 8 columns of
+    // Every warp sums its l over the lanes and leaves O in its first stage: 8 columns of
     // D floats, just the size of K's part, columns of odd pairs shifted so that the stores hit
     // distinct banks.  After a barrier each thread takes four rows of the head dimension of one
     // head, rescales and adds what the warps left, in warp order.
+    // A head's (O, l, m) and the unit's byte e stand for the output O 2^(e - 127) / l, and in a sum with
+    // others for O 2^(m + e) and l 2^m.  O and l hold the probabilities' 2^15 and the number of keys, so
+    // O 2^(e - 127) alone may be beyond fp32 where the output is not (values from 2^88 on), and 2^(e - 127) / l
+    // below it (values around 2^-120): O is divided by l first, or both are kept inside its range.
     {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -739,8 +746,20 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         // a head's 16-byte chunks are shifted by its number so that the stores hit distinct banks.
         float f[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          f[e] = l_run[e] > 0.f ? __fdividef(e_cur < 0 ? 1.f : e8m0_to_f32(e_cur), l_run[e]) : 0.f;
+        for (int e = 0; e < 2; ++e) {
+          float y = e_cur < 0 ? 0.f : static_cast<float>(e_cur - 127);
+          const float z = y < -80.f ? -64.f : y > 100.f ? 24.f : 0.f;
+          if (__any_sync(0xffffffffu, z != 0.f)) {
+            const float g = ex2(z);
+            y -= z;
+#pragma unroll
+            for (int j = 0; j < KS; ++j) {
+              o[j][e] *= g;
+              o[j][2 + e] *= g;
+            }
+          }
+          f[e] = l_run[e] > 0.f ? __fdividef(ex2(y), l_run[e]) : 0.f;
+        }
         uint32_t* row = reinterpret_cast<uint32_t*>(q_rows + gq * (D * 2));
 #pragma unroll
         for (int j = 0; j < KS; ++j) {
@@ -777,22 +796,22 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       float* ow = reinterpret_cast<float*>(stages);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const float f = e_cur < 0 ? 1.f : e8m0_to_f32(e_cur);
         float* col = ow + (2 * tq + e) * D;
         if (2 * tq + e < G) {
 #pragma unroll
           for (int j = 0; j < KS; ++j) {
-            col[(16 * j + gq) ^ (8 * tq)] = o[j][e] * f;
-            col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e] * f;
+            col[(16 * j + gq) ^ (8 * tq)] = o[j][e];
+            col[(16 * j + 8 + gq) ^ (8 * tq)] = o[j][2 + e];
           }
         }
       }
       if (gq == 0) {
-        float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 16 + 2 * tq;
+        float* ml = reinterpret_cast<float*>(smem + S::kMl) + warp * 24 + 2 * tq;
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
           ml[e] = m_run[e];
           ml[8 + e] = l_run[e];
+          ml[16 + e] = m_run[e] == -INFINITY ? kNone : m_run[e] + static_cast<float>(max(e_cur, 0));
         }
       }
       if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
@@ -815,25 +834,31 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       if (x >= NGR) break;
       const int hh = (4 * x) / D;
       const int c = (4 * x) % D;
-      float M = ml[hh];
+      float M = ml[hh], U = ml[16 + hh];
 #pragma unroll
-      for (int v = 1; v < kWarps; ++v) M = fmaxf(M, ml[v * 16 + hh]);
+      for (int v = 1; v < kWarps; ++v) {
+        M = fmaxf(M, ml[v * 24 + hh]);
+        U = fmaxf(U, ml[v * 24 + 16 + hh]);
+      }
       const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float Ls = 0.f;
 #pragma unroll
       for (int v = 0; v < kWarps; ++v) {
-        const float f = ex2(ml[v * 16 + hh] - Mr);
+        const float f = ex2(ml[v * 24 + 16 + hh] - U);
         const float* left = reinterpret_cast<const float*>(smem + s_left[v]);
         const float4 y = *reinterpret_cast<const float4*>(left + hh * D + (c ^ (8 * (hh >> 1))));
         acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
         acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-        Ls = fmaf(f, ml[v * 16 + 8 + hh], Ls);
+        Ls = fmaf(ex2(ml[v * 24 + hh] - Mr), ml[v * 24 + 8 + hh], Ls);
       }
+      // times 2^y, in two factors where it is far from 1
+      const float y = U - Mr - 127.f, y0 = fminf(fmaxf(y, -80.f), 100.f);
+      const float f0 = Ls > 0.f ? __fdividef(ex2(y0), Ls) : 0.f, f1 = ex2(y - y0);
+      acc = make_float4(acc.x * f0 * f1, acc.y * f0 * f1, acc.z * f0 * f1, acc.w * f0 * f1);
       if (cm == 1) {
-        const float inv = Ls > 0.f ? __fdividef(1.f, Ls) : 0.f;
         *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-            make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
+            make_uint2(pack_bf16_rn(acc.x, acc.y), pack_bf16_rn(acc.z, acc.w));
       } else {
         cacc[xi] = acc;
         cls[xi] = Ls;
@@ -841,8 +866,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       }
     }
     if (cm == 1) return;
-    // One share of the unit per CTA: stored into the peers' receive areas, to each the groups that
-    // peer finishes; then merged in rank order.
+    // One share of the unit per CTA: its output, and the maxima and sums that weigh it, stored into the
+    // peers' receive areas, to each the groups that peer finishes; then merged in rank order.
     const int SL = p.slice;
     const uint32_t recv_a = smem_addr(smem + S::kRecv), ml_a = smem_addr(smem + S::kRecvMl);
     const uint32_t bar_a = smem_addr(&recv_bar);
@@ -870,24 +895,29 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       for (int r = 0; r < kMaxClusterCtas; ++r)
         if (r < cm) M = fmaxf(M, pl[r * G].x);
       if (M == -INFINITY) M = 0.f;
-      float Ls = 0.f;
+      float w[kMaxClusterCtas], Ls = 0.f;
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r) {
+        if (r < cm) {
+          w[r] = ex2(pl[r * G].x - M) * pl[r * G].y;
+          Ls += w[r];
+        }
+      }
+      const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
       float4 O = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int r = 0; r < kMaxClusterCtas; ++r) {
         if (r < cm) {
-          const float2 mr = pl[r * G];
           const float4 o4 = *reinterpret_cast<const float4*>(smem + S::kRecv + (r * SL + x - x0) * 16);
-          const float f = ex2(mr.x - M);
-          Ls = fmaf(f, mr.y, Ls);
+          const float f = w[r] * inv;
           O.x = fmaf(f, o4.x, O.x);
           O.y = fmaf(f, o4.y, O.y);
           O.z = fmaf(f, o4.z, O.z);
           O.w = fmaf(f, o4.w, O.w);
         }
       }
-      const float inv = Ls > 0.f ? __frcp_rn(Ls) : 0.f;
       *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
-          make_uint2(pack_bf16_rn(O.x * inv, O.y * inv), pack_bf16_rn(O.z * inv, O.w * inv));
+          make_uint2(pack_bf16_rn(O.x, O.y), pack_bf16_rn(O.z, O.w));
     }
     if (tid == 0 && attn_aborted()) atomicOr(p.status, CMC_DEVFLAG_TIMEOUT);
   } while (SOLO);

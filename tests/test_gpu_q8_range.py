@@ -1,0 +1,132 @@
+"""Attention over the cache in 8 bits where values lie near the ends of
+bf16's range: every form of the launch (a warp, a CTA, a cluster per unit, the longest first), with
+several blocks a warp, against the fp64 oracle."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_25537_gb300 as cmc
+from oracle import q8
+from _gpu_helpers import to_f64
+
+pytestmark = pytest.mark.gpu
+
+E4M3, E8M0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+
+# form: B, L, Hkv, G, d, k, W, warps that share a unit's blocks, grid
+FORMS = {
+    "warp": (150, 1, 8, 2, 128, 64, 256, 1, 300),
+    "warp64": (230, 1, 8, 4, 64, 64, 256, 1, 460),
+    "cta": (29, 1, 8, 4, 128, 256, 512, 4, 232),
+    "cta64": (55, 1, 8, 8, 64, 256, 512, 4, 440),
+    "cta3": (39, 1, 8, 4, 128, 256, 512, 4, 312),  # three an SM, two stages a warp
+    "ordered": (64, 1, 8, 2, 128, 32, 480, 4, 512),  # several waves, the longest first
+    "cluster": (1, 1, 8, 4, 128, 2048, 2048, 32, 64),
+}
+
+
+def rounds(T1, T2, warps):
+    """Which block of its warp each block is: Tier-1's, the ring's."""
+    n1, n2 = (T1 + 31) // 32, (T2 + 31) // 32
+    j = np.arange(n1 + n2) // warps
+    return j[:n1], j[n1:]
+
+
+def make(rng, form, byte_of, key_of=None, most=448.0):
+    """A problem of full rings whose V blocks have the bytes byte_of(unit, round), None for a block of
+    zeros; key_of(unit, round) gives element 0 of the block's keys.  Values of V are up to `most` times the
+    power of two; keys are about 1."""
+    B, L, H, G, d, k, W, warps, grid = FORMS[form]
+    dims = cmc.CmcDims(B, L, G * H, H, d, k, k, W)
+    for fused in (False, True):
+        assert cmc.decode_attn_q8_plan(dims, fused) == grid
+    caches = []
+    for T, r in zip((k, W), rounds(k, W, warps)):
+        x = rng.standard_normal((B, L, H, 2, T, d), dtype=np.float32)
+        x[:, :, :, 0] *= 64.0
+        x[:, :, :, 1] *= most / 4
+        x = x.clip(-most, most)
+        scales = np.full((B, L, H, 2, q8.scale_bytes(T)), 0xFF, dtype=np.uint8)
+        scales[:, :, :, 0] = 121
+        for b in range(B):
+            for h in range(H):
+                for j, i in enumerate(r):
+                    byte = byte_of(b * H + h, i)
+                    rows = slice(32 * j, 32 * j + 32)
+                    if byte is None:
+                        x[b, 0, h, 1, rows] = 0.0
+                    scales[b, 0, h, 1, j] = byte or 0
+                    if key_of is not None:
+                        x[b, 0, h, 0, rows, 0] = key_of(b * H + h, i) * 64.0
+        codes = torch.from_numpy(x).to(E4M3).view(torch.uint8).numpy()
+        caches.append((codes, scales))
+    q = torch.from_numpy(rng.standard_normal((B, L, G * H, d)).astype(np.float32)).to(torch.bfloat16)
+    return q, *caches, np.full(B, 2 * W + 3, dtype=np.int64)
+
+
+def run(dev, q, t1, ring, pos, scale=None):
+    def put(codes, scales):
+        return (torch.from_numpy(codes).to(dev).view(E4M3), torch.from_numpy(scales).to(dev).view(E8M0))
+    return cmc.two_tier_decode_attn_q8(q.to(dev), *put(*t1), *put(*ring), torch.from_numpy(pos).to(dev),
+                                       scale=scale)
+
+
+def check(got, q, t1, ring, units, what, scale=None):
+    """Against the oracle, each output within what the roundings on the way to it may do:
+
+    * the output is rounded to bf16, 2^-8 of it (2^-134 where it is subnormal);
+    * a probability is rounded to fp16, 2^-11 of it or, relative to the largest, 2^-29, but for one
+      that becomes 0 by no more than itself;
+    * what lies 2^-64 below the largest of a head's tokens (their probability times their block's power of
+      two times 448) may be lost;
+    * a score is off by what fp16 leaves of the query and by fp32's roundings (2^-23 each; 2^x by 2^-21):
+      an error e of all scores changes the quotient by at most 2 e (1 + e) of the sum of p |v|.
+    """
+    B, L, Hq, d = q.shape
+    H = ring[0].shape[2]
+    G = Hq // H
+    scale = 1 / np.sqrt(d) if scale is None else scale
+    got, q = to_f64(got), to_f64(q)
+    for u in units:
+        b, g = u // H, u % H
+        x = [q8.values(c[b:b + 1, :, g:g + 1], s[b:b + 1, :, g:g + 1])[0, 0, 0] for c, s in (t1, ring)]
+        K, V = (np.concatenate([y[i] for y in x]) for i in range(2))
+        top = np.concatenate([np.repeat(np.array([q8.power(c) for c in s[b, 0, g, 1]]), 32)[:c.shape[4]]
+                              for c, s in (t1, ring)]) * 448.0
+        for h in range(g * G, g * G + G):
+            s = K @ q[b, 0, h] * scale
+            p = np.exp(s - s.max())
+            out, mag = (p @ y / p.sum() for y in (V, np.abs(V)))
+            a = np.abs(q[b, 0, h])
+            e = scale * (2.0 ** -30 * a.max() * np.abs(K).sum(axis=1)
+                         + (d + 8) * 2.0 ** -23 * (np.abs(K) @ a)).max()
+            bound = (2.0 ** -8 * np.abs(out) + 2.0 ** -134
+                     + (2.0 ** -11 + 2 * (e + 2.0 ** -21) * (1 + e)) * mag
+                     + (np.minimum(p, 2.0 ** -29) @ np.abs(V) + 2.0 ** -64 * (p * top).max()) / p.sum())
+            err = np.abs(got[b, 0, h] - out)
+            assert (err <= bound).all(), (what, u, h, got[b, 0, h, :4], out[:4])
+
+
+@pytest.mark.parametrize("byte", [226, 233, 240, 247])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_near_the_largest(cuda_device, form, byte):
+    """Sums of many large values, which times the probabilities' 2^15 are beyond fp32, and whose mean is not
+    (for byte 247 codes go up to 240: 2^128 is the first power of two that bf16 lacks)."""
+    rng = np.random.default_rng(3)
+    problem = make(rng, form, lambda u, i: byte, most=448.0 if byte < 247 else 240.0)
+    problem[0][...] = 0.0  # all keys count alike
+    for c, _ in problem[1:3]:
+        c[:, :, :, 1] &= 0x7F  # and no sum cancels
+    got = run(cuda_device, *problem)
+    assert torch.isfinite(got).all()
+    check(got, *problem[:3], range(2), "")
+
+
+@pytest.mark.parametrize("byte", [0, 3, 12])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_near_the_smallest(cuda_device, form, byte):
+    """Means around 2^-120, of which the smallest are subnormal in bf16."""
+    rng = np.random.default_rng(4)
+    problem = make(rng, form, lambda u, i: byte)
+    check(run(cuda_device, *problem), *problem[:3], range(2), "")
