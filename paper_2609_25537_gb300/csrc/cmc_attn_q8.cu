@@ -32,12 +32,17 @@
 //   O^T += V^T P^T  16 rows of the head dimension, the heads, the block's 32 keys in two k-steps
 //   q    is multiplied by a power of two so that its head's largest element is in (224, 448].  fp16
 //        holds a bf16 element exactly down to 2^-22 of that, and is off by 2^-33 of it below.
-//   p    relative to the largest so far, times 2^15: eleven significant bits down to 2^-29
-//        of the largest, off by 2^-40 of it below.
-// K's power of two joins the softmax scale.  V's cannot (it changes from block to
-// block): O is kept in units of 2^(E - 127) with E the byte of a recent block, and
-// rescaled, as for a new maximum, when a block's byte is above E or more than ten
-// below it; in between p takes the difference.
+//   p    is multiplied by V's power of two and divided by O's unit, times 2^15.
+// K's power of two joins the softmax scale; with it, a score s is that of 2^s.  V's, 2^(c - 127), changes from
+// block to block: each head's O is kept in units of 2^(U - 127), U a whole number, and p is 2^(s + c - U).  U is
+// raised, and O rescaled, where a block has an s + c above it, so that p never exceeds 1; and lowered where
+// all of a block's lie more than ten below, so that p has eleven significant bits down to 2^-19 of the block's
+// largest and is off by 2^-30 of that below (2^-28 and 2^-39 where U is the block's own).  U stays within 64 of the
+// largest that it has been, for O's sake: of tokens 2^-64 and less of the head's largest p 2^c
+// the smaller values are lost.
+// The sum l that divides has nothing to do with V: it takes the same p, times 2^(U - c), in units of 2^m, m the
+// maximum, and so that these stay within fp32, p is taken relative to no more than 2^44 times its maximum (it
+// is 0 in fp16 either way).  Scores s may be up to 2^23: beyond, fp32 holds no whole numbers next to them.
 //
 // The order of d in a k-step is free: lane t of a quad has the bytes 4 t .. 4 t + 3 of a
 // 16-byte chunk of a key's codes, and they are its four k.  So is the order of the keys, which
@@ -536,14 +541,14 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       qa[ks][0] = f.x;
       qa[ks][1] = f.y;
     }
+    float unit[2], unit_top[2];       // U; the largest so far
     float qs[2], m_run[2], l_run[2];  // softmax scale * log2(e) * the heads' powers of two; maxima, sums
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
       qs[e] = 2 * tq + e < G ? q_factor[2 * tq + e] : 0.f;
-      m_run[e] = -INFINITY;
+      m_run[e] = unit[e] = unit_top[e] = kNone;
       l_run[e] = 0.f;
     }
-    int e_cur = -1, e_top = -1;  // the byte O is in units of; the largest so far
     float o[KS][4];
 #pragma unroll
     for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
@@ -634,25 +639,27 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         }
         mx0 *= f0;
         mx1 *= f1;
-        // The unit of O: at least 2^-64 of the largest block's, so that O stays far inside fp32.
-        int e_new = e_cur;
-        if (vc != 255) {
-          e_top = max(e_top, vc);
-          const int want = max(vc, e_top - 64);
-          if (want > e_cur || want + 10 < e_cur) e_new = want;
-        }
+        // (a NaN for K or V, of the byte or among a block's scores, makes no maximum and no unit, but p NaN)
+        const float c = vc == 255 ? e8m0_to_f32(255) : static_cast<float>(vc);
+        const float a0 = mx0 + c, a1 = mx1 + c;
         const bool up0 = mx0 > m_run[0], up1 = mx1 > m_run[1];
-        if (__any_sync(0xffffffffu, up0 || up1 || e_new != e_cur)) {
-          // (with e_cur = -1, before the first block, O is zero)
-          const float fe = e_cur < 0 ? 1.f : recode_factor(e_cur, max(e_new, 0));
-          e_cur = e_new;
-          const float alpha0 = up0 ? ex2(m_run[0] - mx0) : 1.f;
-          const float alpha1 = up1 ? ex2(m_run[1] - mx1) : 1.f;
-          if (up0) m_run[0] = mx0;
-          if (up1) m_run[1] = mx1;
-          l_run[0] *= alpha0;
-          l_run[1] *= alpha1;
-          const float g0 = alpha0 * fe, g1 = alpha1 * fe;
+        const bool move0 = a0 > unit[0] || a0 + 10.f < unit[0], move1 = a1 > unit[1] || a1 + 10.f < unit[1];
+        if (__any_sync(0xffffffffu, up0 || up1 || move0 || move1)) {
+          if (up0) {
+            l_run[0] *= ex2(m_run[0] - mx0);
+            m_run[0] = mx0;
+          }
+          if (up1) {
+            l_run[1] *= ex2(m_run[1] - mx1);
+            m_run[1] = mx1;
+          }
+          const float u0 = move0 ? ceilf(fmaxf(a0, unit_top[0] - 64.f)) : unit[0];
+          const float u1 = move1 ? ceilf(fmaxf(a1, unit_top[1] - 64.f)) : unit[1];
+          const float g0 = ex2(unit[0] - u0), g1 = ex2(unit[1] - u1);
+          unit[0] = u0;
+          unit[1] = u1;
+          unit_top[0] = fmaxf(unit_top[0], u0);
+          unit_top[1] = fmaxf(unit_top[1], u1);
 #pragma unroll
           for (int j = 0; j < KS; ++j) {
             o[j][0] *= g0;
@@ -661,10 +668,9 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
             o[j][3] *= g1;
           }
         }
-        // 2^15 times the probabilities, times V's power of two in O's unit, 2^(vc - e_cur) <= 1
-        const float dv = vc == 255 ? e8m0_to_f32(255) : static_cast<float>(vc - e_cur);
-        const float ref0 = (m_run[0] == -INFINITY ? 0.f : m_run[0]) - 15.f - dv;
-        const float ref1 = (m_run[1] == -INFINITY ? 0.f : m_run[1]) - 15.f - dv;
+        float ref0 = unit[0] - (c + 15.f), ref1 = unit[1] - (c + 15.f);  // 2^15 p = 2^(s - ref)
+        if (ref0 > m_run[0] + 29.f) ref0 = m_run[0] + 29.f;
+        if (ref1 > m_run[1] + 29.f) ref1 = m_run[1] + 29.f;
         uint32_t pb[2][2];  // P^T as the B operand of k-step t: heads down, keys across
         float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
@@ -677,9 +683,8 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
             sum1 += p1;
             pb[t][r] = movmatrix_trans(pack_f16(p0, p1));
           }
-        const float back = ex2(-dv);
-        l_run[0] = fmaf(sum0, back, l_run[0]);
-        l_run[1] = fmaf(sum1, back, l_run[1]);
+        l_run[0] = fmaf(sum0, ex2(ref0 - m_run[0]), l_run[0]);
+        l_run[1] = fmaf(sum1, ex2(ref1 - m_run[1]), l_run[1]);
         // ---- O^T += V^T P^T: lane's V row is k = lane of the two k-steps ----
         {
           const int a = lane & 15;
@@ -731,10 +736,10 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
     // D floats, just the size of K's part, columns of odd pairs shifted so that the stores hit
     // distinct banks.  After a barrier each thread takes four rows of the head dimension of one
     // head, rescales and adds what the warps left, in warp order.
-    // A head's (O, l, m) and the unit's byte e stand for the output O 2^(e - 127) / l, and in a sum with
-    // others for O 2^(m + e) and l 2^m.  O and l hold the probabilities' 2^15 and the number of keys, so
-    // O 2^(e - 127) alone may be beyond fp32 where the output is not (values from 2^88 on), and 2^(e - 127) / l
-    // below it (values around 2^-120): O is divided by l first, or both are kept inside its range.
+    // A head's (O, U, l, m) stand for the output O 2^(U - 127 - 15) / (l 2^m), O having p's 2^15.
+    // O and l grow with the number of keys, so O 2^(U - 127 - m) alone may be beyond fp32 where the output is not
+    // (values from 2^88 on), and 2^(U - 127 - m) / l below it (values around 2^-120): O is divided by l first, or
+    // both are kept inside its range.
     {
 #pragma unroll
       for (int e = 0; e < 2; ++e)
@@ -747,7 +752,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         float f[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
-          float y = e_cur < 0 ? 0.f : static_cast<float>(e_cur - 127);
+          float y = unit[e] - m_run[e] - 142.f;
           const float z = y < -80.f ? -64.f : y > 100.f ? 24.f : 0.f;
           if (__any_sync(0xffffffffu, z != 0.f)) {
             const float g = ex2(z);
@@ -811,7 +816,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         for (int e = 0; e < 2; ++e) {
           ml[e] = m_run[e];
           ml[8 + e] = l_run[e];
-          ml[16 + e] = m_run[e] == -INFINITY ? kNone : m_run[e] + static_cast<float>(max(e_cur, 0));
+          ml[16 + e] = unit[e];
         }
       }
       if (lane == 0) s_left[warp] = static_cast<int>(stages - smem);
@@ -840,7 +845,6 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         M = fmaxf(M, ml[v * 24 + hh]);
         U = fmaxf(U, ml[v * 24 + 16 + hh]);
       }
-      const float Mr = M == -INFINITY ? 0.f : M;  // (a NaN among the warps' outputs stays one)
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
       float Ls = 0.f;
 #pragma unroll
@@ -850,10 +854,10 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
         const float4 y = *reinterpret_cast<const float4*>(left + hh * D + (c ^ (8 * (hh >> 1))));
         acc.x = fmaf(f, y.x, acc.x); acc.y = fmaf(f, y.y, acc.y);
         acc.z = fmaf(f, y.z, acc.z); acc.w = fmaf(f, y.w, acc.w);
-        Ls = fmaf(ex2(ml[v * 24 + hh] - Mr), ml[v * 24 + 8 + hh], Ls);
+        Ls = fmaf(ex2(ml[v * 24 + hh] - M), ml[v * 24 + 8 + hh], Ls);
       }
       // times 2^y, in two factors where it is far from 1
-      const float y = U - Mr - 127.f, y0 = fminf(fmaxf(y, -80.f), 100.f);
+      const float y = U - M - 142.f, y0 = fminf(fmaxf(y, -80.f), 100.f);
       const float f0 = Ls > 0.f ? __fdividef(ex2(y0), Ls) : 0.f, f1 = ex2(y - y0);
       acc = make_float4(acc.x * f0 * f1, acc.y * f0 * f1, acc.z * f0 * f1, acc.w * f0 * f1);
       if (cm == 1) {
@@ -890,11 +894,10 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       const int hh = (4 * x) / D;
       const int c = (4 * x) % D;
       const float2* pl = reinterpret_cast<const float2*>(smem + S::kRecvMl) + hh;
-      float M = -INFINITY;
+      float M = kNone;
 #pragma unroll
       for (int r = 0; r < kMaxClusterCtas; ++r)
         if (r < cm) M = fmaxf(M, pl[r * G].x);
-      if (M == -INFINITY) M = 0.f;
       float w[kMaxClusterCtas], Ls = 0.f;
 #pragma unroll
       for (int r = 0; r < kMaxClusterCtas; ++r) {

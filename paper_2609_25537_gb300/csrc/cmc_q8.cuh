@@ -33,11 +33,6 @@ __device__ __forceinline__ float e8m0_to_f32(int c) {
 }
 // 2^(127 - c), what values are multiplied by to give codes.
 __device__ __forceinline__ float code_factor(int c) { return e8m0_to_f32(c == 255 ? 255 : 254 - c); }
-// 2^(c_old - c), limited to fp32's normal powers.
-__device__ __forceinline__ float recode_factor(int c_old, int c) {
-  return c_old == 255 ? e8m0_to_f32(255)
-                      : __uint_as_float(static_cast<uint32_t>(min(max(127 + c_old - c, 1), 254)) << 23);
-}
 // The byte of a block from the bits of its largest finite magnitude (fp32):
 // 448 = 1.75 * 2^8.
 __device__ __forceinline__ int block_code(uint32_t amax_bits) {

@@ -1,4 +1,4 @@
-"""Attention over the cache in 8 bits where values lie near the ends of
+"""Attention over the cache in 8 bits where blocks' values differ by much, or lie near the ends of
 bf16's range: every form of the launch (a warp, a CTA, a cluster per unit, the longest first), with
 several blocks a warp, against the fp64 oracle."""
 
@@ -65,11 +65,14 @@ def make(rng, form, byte_of, key_of=None, most=448.0):
     return q, *caches, np.full(B, 2 * W + 3, dtype=np.int64)
 
 
-def run(dev, q, t1, ring, pos, scale=None):
+def device_args(dev, q, t1, ring, pos):
     def put(codes, scales):
         return (torch.from_numpy(codes).to(dev).view(E4M3), torch.from_numpy(scales).to(dev).view(E8M0))
-    return cmc.two_tier_decode_attn_q8(q.to(dev), *put(*t1), *put(*ring), torch.from_numpy(pos).to(dev),
-                                       scale=scale)
+    return [q.to(dev), *put(*t1), *put(*ring), torch.from_numpy(pos).to(dev)]
+
+
+def run(dev, *problem, scale=None):
+    return cmc.two_tier_decode_attn_q8(*device_args(dev, *problem), scale=scale)
 
 
 def check(got, q, t1, ring, units, what, scale=None):
@@ -108,6 +111,55 @@ def check(got, q, t1, ring, units, what, scale=None):
             assert (err <= bound).all(), (what, u, h, got[b, 0, h, :4], out[:4])
 
 
+# Bytes of V's blocks in the order in which a warp takes them (None: a block of zeros), repeated.
+PATTERNS = {
+    "zeros after 2^10": [128, None, 126, None],
+    "zeros after 2^62": [180, None, 176, None],
+    "zeros after 2^74": [192, None, 190, None],
+    "zeros after 2^122": [240, None, 240, None],
+    "zeros first": [None, 240, None, 120],
+    "rising": [40, 90, 150, 210],
+    "falling": [240, 170, 100, 30],
+    "forth and back": [240, 90, 90, 245],
+}
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_far_apart(cuda_device, form, fused):
+    """Neighbouring blocks of a warp with values 2^10 to 2^240 apart, and blocks of zeros between them; in the
+    fused step over the cache that it leaves."""
+    rng = np.random.default_rng(1)
+    lists = list(PATTERNS.values())
+    q, t1, ring, pos = make(rng, form, lambda u, i: lists[u % len(lists)][i % 4])
+    if fused:
+        B, L, H, _, d = FORMS[form][:5]
+        new = [torch.from_numpy(rng.standard_normal((B, L, H, d)).astype(np.float32)).to(torch.bfloat16)
+               for _ in range(2)]
+        args = device_args(cuda_device, q, t1, ring, pos)
+        got = cmc.decode_step_q8(*args, *(x.to(cuda_device) for x in new))
+        ring = [x.view(torch.uint8).cpu().numpy() for x in args[3:5]]
+    else:
+        got = run(cuda_device, q, t1, ring, pos)
+    for u, name in enumerate(PATTERNS):
+        check(got, q, t1, ring, [u], name)
+
+
+@pytest.mark.parametrize("order", [1, -1])
+@pytest.mark.parametrize("form", FORMS)
+def test_large_values_behind_small_probabilities(cuda_device, form, order):
+    """Every other block's values are 2^106 times as large, and its keys turn away from the first query
+    of each KV head, so that they count nothing for it (their probabilities are 2^-245 of the largest), and from no
+    other, for which nothing else counts."""
+    rng = np.random.default_rng(2)
+    q, t1, ring, pos = make(rng, form, lambda u, i: (227, 121)[::order][i % 2],
+                            lambda u, i: (-7.0, 0.0)[::order][i % 2])
+    G, d = FORMS[form][3:5]
+    q[..., 0] = 0.0
+    q[:, :, ::G, 0] = 280.0 * np.sqrt(d / 128)  # 280 * 7 / sqrt(128) = 173, 250 octaves
+    check(run(cuda_device, q, t1, ring, pos), q, t1, ring, range(2), "")
+
+
 @pytest.mark.parametrize("byte", [226, 233, 240, 247])
 @pytest.mark.parametrize("form", FORMS)
 def test_values_near_the_largest(cuda_device, form, byte):
@@ -130,3 +182,31 @@ def test_values_near_the_smallest(cuda_device, form, byte):
     rng = np.random.default_rng(4)
     problem = make(rng, form, lambda u, i: byte)
     check(run(cuda_device, *problem), *problem[:3], range(2), "")
+
+
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("form", FORMS)
+def test_large_scores(cuda_device, form, sign):
+    """Scores of two million, whose products are exact: tokens of the largest one share the output."""
+    rng = np.random.default_rng(5)
+    q, t1, ring, pos = make(rng, form, lambda u, i: 118 + u % 3)
+    q[...] = 0.0
+    q[..., 0] = sign * 2.0 ** 14
+    H = ring[0].shape[2]
+    for c, s in (t1, ring):
+        # keys of 64 to 120 in element 0 alone, for the negative sign -64 and up; scores in steps of 2^17
+        step = rng.integers(0, 8, c.shape[:3] + c.shape[4:5])
+        c[:, :, :, 0] = 0
+        c[:, :, :, 0, :, 0] = torch.from_numpy((64.0 + 8 * step).astype(np.float32)).to(E4M3).view(
+            torch.uint8).numpy()
+        s[:, :, :, 0] = 127
+    got = to_f64(run(cuda_device, q, t1, ring, pos, scale=1.0))
+    for u in range(3):
+        b, g = u // H, u % H
+        x = [q8.values(c[b:b + 1, :, g:g + 1], s[b:b + 1, :, g:g + 1])[0, 0, 0] for c, s in (t1, ring)]
+        K, V = (np.concatenate([y[i] for y in x]) for i in range(2))
+        best = K[:, 0] == (K[:, 0].max() if sign > 0 else K[:, 0].min())
+        want, mag = (y[best].mean(axis=0) for y in (V, np.abs(V)))
+        G = q.shape[2] // H
+        # equal scores get equal probabilities: roundings to fp16 and of the sums, then to bf16
+        assert (np.abs(got[b, 0, g * G:g * G + G] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag).all()
