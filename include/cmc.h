@@ -491,7 +491,8 @@ CMC_API int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int
 /*
  * Reads an 8-bit cache back to bf16: out row i is cache row idx[b, i], or row i
  * when idx is NULL, for i < k.  Exact (an e4m3 value has four significant bits)
- * but for values below bf16's smallest.
+ * but for values below bf16's smallest, and for 2^128 and more, which give an
+ * infinity (bf16 values of 248 * 2^120 and more round up to the former).
  *
  *   kv, scales    the format above with T = N
  *   idx           int32 [B, k] or NULL

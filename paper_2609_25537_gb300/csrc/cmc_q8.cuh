@@ -33,8 +33,8 @@ __device__ __forceinline__ float e8m0_to_f32(int c) {
 }
 // 2^(127 - c), what values are multiplied by to give codes.
 __device__ __forceinline__ float code_factor(int c) { return e8m0_to_f32(c == 255 ? 255 : 254 - c); }
-// The byte of a block from the bits of its largest finite magnitude (fp32):
-// 448 = 1.75 * 2^8.
+// The byte of a block from the bits of its largest finite magnitude (fp32, or with an exponent beyond:
+// held_bits): 448 = 1.75 * 2^8.
 __device__ __forceinline__ int block_code(uint32_t amax_bits) {
   return max(0, static_cast<int>(amax_bits >> 23) - 8 + ((amax_bits & 0x7FFFFFu) > 0x600000u ? 1 : 0));
 }
@@ -117,12 +117,16 @@ __device__ __forceinline__ uint32_t max_codes4(uint32_t m, uint32_t w) {
 __device__ __forceinline__ uint32_t max_codes16(uint32_t m, const uint4& x) {
   return max_codes4(max_codes4(max_codes4(max_codes4(m, x.x), x.y), x.z), x.w);
 }
-// The fp32 bits of the value of the larger of two largest magnitudes (max_codes16) of a block with byte c,
-// 0 if the byte is NaN.
+// The value of the larger of two largest magnitudes (max_codes16) of a block with byte c as fp32 bits, 0 if the
+// byte is NaN.  The code's bits get the byte's exponent in whole numbers, which goes past fp32's largest (bf16's
+// is stored as 2^128, and a byte may say up to 448 * 2^127); what falls below its smallest normal
+// value comes out too small, and gives the byte 0 as it should.
 __device__ __forceinline__ uint32_t held_bits(uint32_t m, int c) {
   float a, b;
   f16x2_f32(m, a, b);
-  return c == 255 ? 0u : finite_bits(fmaxf(a, b) * e8m0_to_f32(c));
+  const uint32_t bits = __float_as_uint(fmaxf(a, b)), down = static_cast<uint32_t>(max(127 - c, 0)) << 23;
+  if (c == 255 || bits <= down) return 0u;
+  return c >= 127 ? bits + (static_cast<uint32_t>(c - 127) << 23) : bits - down;
 }
 
 }  // namespace cmc

@@ -210,3 +210,29 @@ def test_large_scores(cuda_device, form, sign):
         G = q.shape[2] // H
         # equal scores get equal probabilities: roundings to fp16 and of the sums, then to bf16
         assert (np.abs(got[b, 0, g * G:g * G + G] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag).all()
+
+
+@pytest.mark.parametrize("fused", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_beside_the_largest_values(cuda_device, d, fused):
+    """A block set anew keeps tokens that bf16's largest value (255 * 2^120) rounded up to 2^128, and those
+    of the largest powers of two that the format has."""
+    W = 70
+    k = torch.randn(4, 1, 1, W, d).to(torch.bfloat16)
+    k[0, ..., 5, 3] = torch.finfo(torch.bfloat16).max
+    k[1, ..., 33:60, :] = -torch.finfo(torch.bfloat16).max
+    codes, scales = q8.quantize(to_f64(k), to_f64(k.flip(-1)), np.ones((4, W), dtype=bool))
+    scales[2, ..., :2], scales[3, ..., :2] = 250, 254
+    codes[2:, ..., 6, 1] = codes[2:, ..., 40, 1] = 0x7E  # 448
+    pos = np.array([2 * W, W + 32, 3 * W, 5 * W + 32], dtype=np.int64)  # first slots of blocks
+    row = torch.full((4, 1, 1, d), 0.25, dtype=torch.bfloat16)
+    q = torch.zeros(4, 1, 2, d, dtype=torch.bfloat16)
+    args = device_args(cuda_device, q, (codes[..., :0, :], scales[..., :0]), (codes, scales), pos)
+    if fused:
+        cmc.decode_step_q8(args[0], None, None, *args[3:], row.to(cuda_device), row.to(cuda_device))
+    else:
+        cmc.window_append_q8(*args[3:], row.to(cuda_device), row.to(cuda_device))
+    q8.append(codes, scales, pos, to_f64(row), to_f64(row))
+    assert scales[0, 0, 0, 0, 0] == scales[1, 0, 0, 1, 1] == 247
+    np.testing.assert_array_equal(args[4].view(torch.uint8).cpu().numpy(), scales)
+    np.testing.assert_array_equal(args[3].view(torch.uint8).cpu().numpy(), codes)
