@@ -391,6 +391,11 @@ def _scale(scale: Optional[float]) -> float:
     return 0.0 if scale is None else float(scale)
 
 
+def _offset(rope_offset: int) -> int:
+    """For the library: what it refuses stays refused, where ctypes would cut it to 64 bits."""
+    return rope_offset if 0 <= rope_offset <= 1 << 32 else -1
+
+
 @_ranged
 def two_tier_decode_attn(q, tier1_k, tier1_v, idx, ring_k, ring_v, pos, *,
                          scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
@@ -439,7 +444,7 @@ def decode_step(q, tier1_k, tier1_v, idx, ring_k, ring_v, pos, k_new, v_new, *,
         st = lib().cmc_decode_step_rope(
             _p(q), _p(tier1_k), _p(tier1_v), _p(idx), _p(ring_k), _p(ring_v), _p(pos),
             _p(k_new), _p(v_new), ctypes.byref(dims), _scale(scale), float(rope_theta),
-            int(rope_offset), _p(out), _p(ws.buf), ws.nbytes, stream)
+            _offset(int(rope_offset)), _p(out), _p(ws.buf), ws.nbytes, stream)
         if st:
             check(st, "cmc_decode_step_rope")
     return out
@@ -854,7 +859,7 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
     args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
             0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
             ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ref,
-            0.0 if scale is None else scale, rope_theta, rope_offset, out.data_ptr(),
+            0.0 if scale is None else scale, rope_theta, _offset(rope_offset), out.data_ptr(),
             workspace.ptr, workspace.nbytes, stream)
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
     if st:
