@@ -482,7 +482,7 @@ CMC_API int cmc_q8_scale_bytes(int rows);
  *                   a token is outside [0, N); that row holds none then
  *
  * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
- * launches nothing.
+ * launches nothing, and N may be 0 then.
  */
 CMC_API int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int32_t* idx,
                                const int64_t* count, const cmc_dims* dims, void* kv, void* scales,
@@ -500,7 +500,7 @@ CMC_API int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int
  *   status        as above; a row with a bad index is zeroed
  *
  * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
- * launches nothing.
+ * launches nothing, and N may be 0 then.
  */
 CMC_API int cmc_dequantize_cache(const void* kv, const void* scales, const int32_t* idx,
                                  const cmc_dims* dims, void* out_k, void* out_v, uint32_t* status,

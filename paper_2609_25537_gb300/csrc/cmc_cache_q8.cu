@@ -362,14 +362,14 @@ window_append_q8_kernel(uint8_t* ring, uint8_t* scales, int64_t* pos, const uint
 }
 
 // The sizes of a call that takes k rows out of N; an index may name rows more than
-// once, so k may be larger.
+// once, so k may be larger.  No rows can be taken out of none.
 static int check_rows(const cmc_dims* dims, bool by_index) {
   if (!dims) return CMC_ERR_NULL;
   cmc_dims m = *dims;
-  if (m.N < 1 || m.N > (1 << 24) || m.k > (1 << 24)) return CMC_ERR_SHAPE;
+  if (m.N < (m.k == 0 ? 0 : 1) || m.N > (1 << 24) || m.k > (1 << 24)) return CMC_ERR_SHAPE;
   m.Hq = m.Hkv;  // query heads and the window play no part here
   m.W = 1;
-  if (by_index && m.k > m.N) m.N = m.k;
+  if (m.N == 0 || (by_index && m.k > m.N)) m.N = m.k > 0 ? m.k : 1;
   return validate_dims(&m, true);
 }
 
