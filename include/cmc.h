@@ -434,7 +434,7 @@ CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
  * likewise and gives up after 3 s), the launch returns and the workspace's status
  * word gets CMC_DEVFLAG_TIMEOUT.
  * Outputs, ring and pos of such a call are invalid, and its workspace must be
- * zero-filled again.  on == 0 restores normal operation.  Always CMC_OK. */
+ * zero-filled again (but for the calls over a cache in 8 bits).  on == 0 restores normal operation.  Always CMC_OK. */
 CMC_API int cmc_test_stall_attention_waits(int on);
 
 /* ------------------------------------------------------------------------ *
@@ -526,9 +526,9 @@ CMC_API int cmc_window_append_q8(void* ring_kv, void* ring_scales, int64_t* pos,
 
 /* Bytes of workspace cmc_two_tier_decode_attn_q8 and cmc_decode_step_q8 need for
  * `dims`: the device status word (read by cmc_read_status) and one 8-byte counter per
- * sequence.  Zero-fill it once before its first use, and again after a call
- * that raised CMC_DEVFLAG_TIMEOUT; every other call leaves the counters at zero.
- * It depends on B alone, and a workspace of cmc_decode_attn_workspace_size for the
+ * sequence.  Zero-fill it once before its first use; every call leaves the counters at
+ * zero, one that raised CMC_DEVFLAG_TIMEOUT too (its outputs and ring are invalid, and its
+ * positions advanced).  It depends on B alone, and a workspace of cmc_decode_attn_workspace_size for the
  * same B will do as well. */
 CMC_API size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims);
 

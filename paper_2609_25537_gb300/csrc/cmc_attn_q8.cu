@@ -281,6 +281,19 @@ __device__ __forceinline__ void patch_block(const AttnQ8Params& p, uint8_t* stag
   __syncwarp();
 }
 
+// The units that a warp which gave up leaves alone are counted all the same, so that the counters come back
+// to zero: u, u + hop, ...
+static __device__ __noinline__ void count_left_units(unsigned long long* tickets, int64_t* pos, int u, int hop, int units,
+                                                     int LH) {
+  for (; u < units; u += hop) {
+    const int b = u / LH;
+    if (atomicAdd(tickets + b, 1ull) + 1 != static_cast<unsigned long long>(LH)) continue;
+    const long long last = *static_cast<volatile int64_t*>(pos + b);  // all others have read it
+    if (last >= 0) pos[b] = last + 1;
+    tickets[b] = 0ull;
+  }
+}
+
 // SOLO: a unit per warp, four a CTA, and no barrier but the warp's; the warp goes on with the unit
 // gridDim x 4 after its own, whose query, position and first blocks are then already on
 // their way.
@@ -787,7 +800,10 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
           if (!sq.bad) p.pos[b] = pos + 1;
           p.tickets[b] = 0ull;
         }
-        if (gave_up) return;
+        if (gave_up) {
+          if (FUSED && lane == 0) count_left_units(p.tickets, p.pos, u + hop, hop, p.units, p.LH);
+          return;
+        }
         __syncwarp();
         u += hop;
         if (u >= p.units) return;

@@ -1,10 +1,14 @@
 """The binding of the cache in 8 bits: arguments at the ends of their ranges, caches without a row, workspaces that
 a call chooses itself, waits that run out."""
 
+import numpy as np
 import pytest
 import torch
 
 import paper_2609_25537_gb300 as cmc
+from oracle import q8
+from test_gpu_q8_range import check
+from _gpu_helpers import to_f64
 
 pytestmark = pytest.mark.gpu
 
@@ -41,3 +45,73 @@ def test_a_cache_without_rows_is_read_back(cuda_device):
     for call in (lambda: cmc.dequantize_cache(kv, scales, one), lambda: cmc.quantize_cache(k, v, one)):
         with pytest.raises(cmc.CmcError, match="SHAPE"):
             call()
+
+
+# form: B, L, Hkv, G, d, k, W, grid
+STALLED = {
+    "cluster": (1, 1, 8, 4, 128, 2048, 2048, 64),
+    "cta": (29, 1, 8, 4, 128, 256, 512, 232),
+    "three CTAs an SM": (39, 1, 8, 4, 128, 256, 512, 312),
+    "longest first": (64, 1, 8, 2, 128, 32, 480, 512),
+    "a warp a unit": (150, 1, 8, 2, 128, 64, 256, 300),
+    "several units a warp": (8, 32, 8, 4, 128, 30, 130, 304),
+}
+
+
+class stalled:
+    """Within it every stage's wait runs out."""
+
+    def __enter__(self):
+        cmc.lib().cmc_test_stall_attention_waits(1)
+
+    def __exit__(self, *_):
+        cmc.lib().cmc_test_stall_attention_waits(0)
+
+
+def step_problem(dev, B, L, H, G, d, k, W, seed):
+    g = torch.Generator(device=dev).manual_seed(seed)
+
+    def rand(*shape):
+        return torch.randn(shape, generator=g, device=dev).to(torch.bfloat16)
+    t1 = cmc.quantize_cache(rand(B, L, H, k, d), rand(B, L, H, k, d))
+    ring = cmc.quantize_cache(rand(B, L, H, W, d), rand(B, L, H, W, d))
+    pos = W + torch.arange(B, device=dev) * 7
+    return [rand(B, L, G * H, d), *t1, *ring, pos, rand(B, L, H, d), rand(B, L, H, d)]
+
+
+@pytest.mark.parametrize("given", [True, False])
+@pytest.mark.parametrize("form", STALLED)
+def test_a_step_after_one_that_timed_out(cuda_device, form, given):
+    """The counters of the workspace are zero again, every position was advanced once, and the next step with
+    the same workspace, given or the call's own, is right without its being cleared."""
+    B, L, H, G, d, k, W, grid = STALLED[form]
+    dims = cmc.CmcDims(B, L, G * H, H, d, k, k, W)
+    assert cmc.decode_attn_q8_plan(dims) == grid
+    args = step_problem(cuda_device, B, L, H, G, d, k, W, 1)
+    before = [x.clone() for x in args]
+    ws = cmc.DecodeWorkspace(dims, cuda_device, q8=True) if given else None
+    cmc.decode_step_q8(*args, workspace=ws)  # the call's own exists from here on
+    for x, y in zip(args, before):
+        x.copy_(y)
+    torch.cuda.synchronize()
+    with stalled():
+        cmc.decode_step_q8(*args, workspace=ws)
+        torch.cuda.synchronize()
+    assert torch.equal(args[5], before[5] + 1)
+    if given:
+        assert ws.status() & cmc.DEVFLAG_TIMEOUT
+        assert not ws.buf.any()
+    for x, y in zip(args, before):
+        x.copy_(y)
+    got = cmc.decode_step_q8(*args, workspace=ws)
+    torch.cuda.synchronize()
+    ring, t1 = ([x.view(torch.uint8).cpu().numpy() for x in before[i:i + 2]] for i in (3, 1))
+    pos = before[5].cpu().numpy()
+    q8.append(*ring, pos, *(to_f64(x) for x in before[6:]))
+    assert np.array_equal(args[5].cpu().numpy(), pos)
+    for x, y in zip(args[3:5], ring):
+        np.testing.assert_array_equal(x.view(torch.uint8).cpu().numpy(), y)
+    if L == 1:
+        check(got, before[0].cpu(), t1, ring, range(3), form)
+    if given:
+        assert ws.status() == 0
