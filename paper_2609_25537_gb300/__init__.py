@@ -15,6 +15,7 @@ from .cmc import (  # noqa: F401
     decode_attn_plan,
     decode_attn_q8_plan,
     decode_attn_q8_workspace_size,
+    decode_q8_status,
     decode_attn_workspace_size,
     decode_step,
     decode_step_q8,

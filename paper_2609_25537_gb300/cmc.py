@@ -56,6 +56,7 @@ __all__ = [
     "decode_step_q8",
     "decode_attn_q8_plan",
     "decode_attn_q8_workspace_size",
+    "decode_q8_status",
     "q8_scale_bytes",
     "set_l2_prefetch_tiles",
     "dims_of",
@@ -766,6 +767,24 @@ def _attn_q8_workspace(kept: Dict, index: int, stream: int, dims: CmcDims) -> De
     return ws
 
 
+def decode_q8_status(device: Optional[torch.device] = None, clear: bool = True) -> int:
+    """DEVFLAG_* bits that the attention calls over a cache in 8 bits which were given no ``workspace`` have
+    raised on `device` (None: the current one) since the last clear; waits for all work on it.  Calls captured into a
+    graph are not among them: give those a workspace to see theirs."""
+    index = None if device is None else torch.device(device).index
+    if index is None:
+        index = torch.cuda.current_device()
+    flags = 0
+    with torch.cuda.device(index):
+        torch.cuda.synchronize()
+        for kept in list(_q8_workspaces.values()):
+            for (i, _), ws in list(kept.items()):
+                if i == index:
+                    flags |= ws.status(clear)
+        torch.cuda.synchronize()  # cleared before any stream's next call
+    return flags
+
+
 def _check_out(out: torch.Tensor, q: torch.Tensor) -> None:
     _need(out, "out", torch.bfloat16, 4, q.device)
     if out.shape != q.shape:
@@ -780,7 +799,8 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
     (tier1_kv and tier1_scales None: the ring alone); see
     cmc_two_tier_decode_attn_q8.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a
     DecodeWorkspace(dims, device, q8=True); without one the call keeps one per stream and
-    batch size, and a captured call gets one of its own, zero-filled at every replay."""
+    batch size (see :func:`decode_q8_status`), and a captured call gets one of its own, zero-filled at every
+    replay."""
     kept, index = None, -1
     try:
         index = q.get_device()

@@ -115,3 +115,24 @@ def test_a_step_after_one_that_timed_out(cuda_device, form, given):
         check(got, before[0].cpu(), t1, ring, range(3), form)
     if given:
         assert ws.status() == 0
+
+
+def test_flags_of_calls_without_a_workspace(cuda_device):
+    """Of all of a device, on any stream and of any batch size, until they are cleared."""
+    cmc.decode_q8_status()
+    assert cmc.decode_q8_status(cuda_device) == 0
+    one, two = (step_problem(cuda_device, B, 1, 2, 2, 64, 32, 64, 2) for B in (1, 3))
+    one[5].fill_(-4)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        cmc.two_tier_decode_attn_q8(*one[:6])
+    with stalled():
+        cmc.decode_step_q8(*two)
+        torch.cuda.synchronize()
+    both = cmc.DEVFLAG_BAD_POS | cmc.DEVFLAG_TIMEOUT
+    assert cmc.decode_q8_status("cuda", clear=False) == both
+    assert cmc.decode_q8_status() == both
+    assert cmc.decode_q8_status() == 0
+    cmc.decode_step_q8(*two)
+    assert cmc.decode_q8_status() == 0
