@@ -458,8 +458,11 @@ CMC_API int cmc_test_stall_attention_waits(int on);
  * as NaN.  c = 255 is NaN: the block's values are.  e4m3 and e8m0 are the types
  * that torch calls float8_e4m3fn and float8_e8m0fnu.
  *
- * A code is within 2^-4 of its value, relatively, for values down to 2^-15 of the
- * block's amax, and within 2^-19 of amax below.
+ * A value quantised with its block is off by at most 2^-4 of itself down to 2^-13 of the block's
+ * amax, and by 2^-17 of amax below (by 2^-137 where c = 0).  In a ring a block's c may be larger than its
+ * tokens need, and an append that raises it rounds the smaller codes again: all in all a value is
+ * off by at most 2^-4 of itself or 2^-9 * 2^(c - 127), whichever is more, with the largest c that its block has
+ * had since the token came.
  */
 
 /* S of the format above for T = rows tokens; 0 for rows < 0 or > 2^24. */
