@@ -426,13 +426,14 @@ CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 
 /* Test hook for the failure path of the attention kernels (not part of the
  * method; off unless called).  With on != 0, every pipeline stage of the
- * attention launches made afterwards (cmc_two_tier_decode_attn, cmc_decode_step,
- * cmc_decode_step_rope and those over a cache in 8 bits, from any thread) expects 16 bytes
+ * attention launches (cmc_two_tier_decode_attn, cmc_decode_step,
+ * cmc_decode_step_rope and those over a cache in 8 bits) and of cmc_quantize_cache
+ * made afterwards, from any thread, expects 16 bytes
  * more than its loads deliver, so no stage ever completes: each CTA's first
  * wait gives up after its 1 s limit, the CTA's other waits end at once (but for a
  * cluster's wait for what its CTAs store into each other, which is stalled
- * likewise and gives up after 3 s), the launch returns and the workspace's status
- * word gets CMC_DEVFLAG_TIMEOUT.
+ * likewise and gives up after 3 s), the launch returns and the workspace's (or the call's)
+ * status word gets CMC_DEVFLAG_TIMEOUT.
  * Outputs, ring and pos of such a call are invalid, and its workspace must be
  * zero-filled again (but for the calls over a cache in 8 bits).  on == 0 restores normal operation.  Always CMC_OK. */
 CMC_API int cmc_test_stall_attention_waits(int on);
@@ -482,7 +483,9 @@ CMC_API int cmc_q8_scale_bytes(int rows);
  *                   bank.  The padding bytes of scales are zeroed
  *   status          NULL, or a device uint32 word that receives
  *                   CMC_DEVFLAG_BAD_INDEX when an idx entry of a row that holds
- *                   a token is outside [0, N); that row holds none then
+ *                   a token is outside [0, N); that row holds none then; and
+ *                   CMC_DEVFLAG_TIMEOUT when the bounded wait for a copy into shared
+ *                   memory ran out, which is never expected: rows are left unwritten then
  *
  * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
  * launches nothing, and N may be 0 then.
@@ -500,7 +503,8 @@ CMC_API int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int
  *   kv, scales    the format above with T = N
  *   idx           int32 [B, k] or NULL
  *   out_k, out_v  bf16 [B, L, Hkv, k, d]  output; must not overlap the cache
- *   status        as above; a row with a bad index is zeroed
+ *   status        NULL, or a device uint32 word that receives CMC_DEVFLAG_BAD_INDEX; a row with a
+ *                 bad index is zeroed
  *
  * dims->Hq and W are ignored; k may exceed N when there is an idx.  k == 0
  * launches nothing, and N may be 0 then.

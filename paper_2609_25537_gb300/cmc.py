@@ -611,7 +611,8 @@ def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor]
     """An 8-bit cache (kv, scales) of rows of a bf16 bank or ring k, v [B, L, Hkv, N, d]:
     all N, or those that ``idx`` [B, k] names.  Rows from ``count[b]`` on (int64 [B]; a
     ring's pos will do) hold no token.  See cmc_quantize_cache.  Out-of-range
-    indices raise DEVFLAG_BAD_INDEX in ``workspace``'s status word when one is given."""
+    indices raise DEVFLAG_BAD_INDEX in ``workspace``'s status word, and a copy that did not arrive in time
+    DEVFLAG_TIMEOUT; without a workspace neither is reported."""
     _need(k, "k", torch.bfloat16, 5)
     dev = k.device
     index = dev.index

@@ -35,7 +35,7 @@ __global__ void __launch_bounds__(kRowThreads)
 quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict__ bank_v,
                 const int32_t* __restrict__ idx, const int64_t* __restrict__ count,
                 uint8_t* __restrict__ kv, uint8_t* __restrict__ scales, uint32_t* status,
-                long long jobs, int nb, int LH, int N, int k, int S) {
+                long long jobs, int nb, int LH, int N, int k, int S, uint32_t stall_tx) {
   constexpr int kStage = kQ8Block * D * 2;
   constexpr int NP = kStage / 512;  // passes of the warp over a block, 16 bytes a lane
   constexpr int RPP = 512 / (D * 2);  // rows of a pass
@@ -93,7 +93,7 @@ quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict_
     const uint16_t* bank = ((m.uw & 1) ? bank_v : bank_k) + (m.uw >> 1) * N * D;
     if (lane == 0) {
       held[s] = {m.uw, m.r0, rows};
-      mbar_arrive_expect_tx(&full[s], __popc(rows) * (D * 2));
+      mbar_arrive_expect_tx(&full[s], __popc(rows) * (D * 2) + stall_tx);
     }
     __syncwarp();
     const uint32_t to = smem_addr(stages + s * kStage);
@@ -413,7 +413,7 @@ int cmc_quantize_cache(const void* bank_k, const void* bank_v, const int32_t* id
                     static_cast<cudaStream_t>(stream), static_cast<const uint16_t*>(bank_k),
                     static_cast<const uint16_t*>(bank_v), idx, count,
                     static_cast<uint8_t*>(kv), static_cast<uint8_t*>(scales), status, jobs, nb,
-                    m.L * m.Hkv, m.N, m.k, q8_scale_bytes(m.k));
+                    m.L * m.Hkv, m.N, m.k, q8_scale_bytes(m.k), stall_tx_setting());
 }
 
 int cmc_dequantize_cache(const void* kv, const void* scales, const int32_t* idx, const cmc_dims* dims,

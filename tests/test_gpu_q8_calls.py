@@ -136,3 +136,21 @@ def test_flags_of_calls_without_a_workspace(cuda_device):
     assert cmc.decode_q8_status() == 0
     cmc.decode_step_q8(*two)
     assert cmc.decode_q8_status() == 0
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("N,by_index", [(70, False), (70, True), (3000, False)])
+def test_quantising_reports_a_wait_that_ran_out(cuda_device, d, N, by_index):
+    """With one stage a warp and with two (more blocks than one wave takes); the next call is right."""
+    bank = torch.randn(4, 4, 8, N, d, device=cuda_device).to(torch.bfloat16)
+    idx = torch.arange(N - 1, -1, -1, dtype=torch.int32, device=cuda_device).repeat(4, 1) if by_index else None
+    want = [x.clone().view(torch.uint8) for x in cmc.quantize_cache(bank, bank, idx)]
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(4, 1, 8, 8, d, 1, 0, 1), cuda_device, q8=True)
+    torch.cuda.synchronize()
+    with stalled():
+        cmc.quantize_cache(bank, bank, idx, workspace=ws)
+        flags = ws.status()
+    assert flags == cmc.DEVFLAG_TIMEOUT
+    for x, y in zip(cmc.quantize_cache(bank, bank, idx, workspace=ws), want):
+        assert torch.equal(x.view(torch.uint8), y)
+    assert ws.status() == 0
