@@ -94,6 +94,244 @@ struct AttnMaps {
   CUtensorMap t1k_box, t1v_box;    // Tier-1 [units * N, d] (identity selection only)
 };
 
+// fp32 partial record of one CTA's share of a unit: max[G], sum[G], then, from
+// a 16-byte aligned offset, the unnormalised output [G][d].
+__host__ __device__ constexpr int rec_out_offset(int G) { return (2 * G + 3) & ~3; }
+__host__ __device__ constexpr int rec_floats(int G, int D) { return rec_out_offset(G) + G * D; }
+
+// ---------------------------------------------------------------------------
+// PTX wrappers
+// ---------------------------------------------------------------------------
+
+__device__ __forceinline__ void ldsm_x4_t(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2,
+                                          uint32_t& r3) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
+               : "r"(addr));
+}
+
+// C[16x8] += A[16x16] B[16x8], bf16 inputs, fp32 accumulators (all 16 rows of A).
+__device__ __forceinline__ void mma_16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                          uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%0,%1,%2,%3};\n"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// C[16x8] = A[16x16] B[16x8]: the first step of an accumulator chain (its zeros
+// need no registers).
+__device__ __forceinline__ void mma_16816_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
+                                               uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+      "{%8,%9}, {%10,%10,%10,%10};\n"
+      : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+
+__device__ __forceinline__ void mbar_arrive(uint64_t* bar) {
+  asm volatile("{\n .reg .b64 st;\n mbarrier.arrive.shared::cta.b64 st, [%0];\n}\n" ::"r"(
+                   smem_addr(bar))
+               : "memory");
+}
+
+// A 2-D TMA box load into shared memory, completing on an mbarrier, with an
+// L2 cache policy (createpolicy) attached.
+__device__ __forceinline__ void tma_box_hint(uint32_t dst, const CUtensorMap* map, int col, int row,
+                                             uint64_t* bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1, {%2, %3}], [%4], %5;\n" ::"r"(dst),
+      "l"(map), "r"(col), "r"(row), "r"(smem_addr(bar)), "l"(policy)
+      : "memory");
+}
+
+// L2 prefetch of one TMA box and of a contiguous byte range.  These are hints:
+// no data reaches the issuing thread and the L2 stays coherent with the
+// previous kernel's writes, so they may be issued before the grid dependency
+// wait.
+__device__ __forceinline__ void tma_prefetch_l2(const CUtensorMap* map, int col, int row) {
+  asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];\n" ::"l"(map),
+               "r"(col), "r"(row)
+               : "memory");
+}
+__device__ __forceinline__ void bulk_prefetch_l2(const void* src, uint32_t bytes) {
+  asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t src_bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src), "r"(src_bytes));
+}
+__device__ __forceinline__ void cp_async16_hint(uint32_t dst, const void* src, uint32_t src_bytes,
+                                                uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;\n" ::"r"(dst), "l"(src),
+               "r"(src_bytes), "l"(policy));
+}
+__device__ __forceinline__ void cp_async16_all(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src),
+               "l"(policy));
+}
+__device__ __forceinline__ void cp_async_8(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8;\n" ::"r"(dst), "l"(src));
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;\n" ::); }
+
+// Named barrier over the consumer warps only (the producer warp never joins).
+__device__ __forceinline__ void consumer_sync() {
+  asm volatile("bar.sync 1, %0;\n" ::"n"(kWarps * 32) : "memory");
+}
+
+// ---------------------------------------------------------------------------
+// The walk over a launch's tiles
+// ---------------------------------------------------------------------------
+
+// Per-stage header words: rows of the tile that may hold a key, the new
+// token's ring slot and tile row (fused step; -1 if not in this tile),
+// whether any of the tile's rows holds no key (its V row must be zeroed), and
+// the bit masks of rows 0-31 / 32-63 whose Tier-1 index is out of range.
+// Stage 0's also holds, in its last two words, pos of the CTA's first sequence
+// on its way to the producer.
+enum { H_NROWS = 0, H_NEWSLOT = 1, H_NEWROW = 2, H_MASKED = 3, H_BADLO = 4, H_BADHI = 5, H_POS = 6 };
+
+// A consumer's wait for a stage.  One that gives up
+//  - marks the stage's header as that of a tile without keys: the barrier, stuck
+//    in its phase, reports the phase before as complete, which has the parity
+//    of the stage's next tile, so the warp's wait for that one passes;
+//  - ends the warp's hand-backs (`release` is 0 in lane 0 before): the producer,
+//    which then finds the abort flag up, refills no stage whose loads may not
+//    have landed.
+// That leaves the tile loop as it was.  A flag of the warp's own tested a tile
+// instead cost 0.3 % of a Llama-shaped step and 0.7 % of 8 x (30 + 130) keys, the
+// abort flag read by the producer a tile up to 1.7 %.
+__device__ __forceinline__ bool mbar_wait_stage(uint64_t* bar, uint32_t parity, int* header,
+                                                int& release) {
+  if (mbar_wait(bar, parity)) return true;
+  header[H_NROWS] = 0;
+  header[H_NEWROW] = -1;
+  header[H_MASKED] = 1;
+  release = 1;
+  return false;
+}
+
+__device__ __forceinline__ long long cta_first_tile(long long c, long long base, long long rem) {
+  return c * base + (c < rem ? c : rem);
+}
+__device__ __forceinline__ long long cta_of_tile(long long t, long long base, long long rem) {
+  const long long big = rem * (base + 1);
+  return t < big ? t / (base + 1) : rem + (t - big) / base;
+}
+// Partial-record slot (tile position within the unit) of CTA c's share of
+// the unit whose first tile is ut0: the position of c's first tile in it.
+__device__ __forceinline__ long long rec_slot(const AttnParams& p, long long c, long long ut0) {
+  const long long t = cta_first_tile(c, p.base, p.rem);
+  return t > ut0 ? t - ut0 : 0;
+}
+
+// The tile at a position of the flattened (unit, j) order, advanced one tile
+// at a time so that the main loop does no integer division.  Within a unit,
+// position j holds key tile lt = (j + rot) % tpu: ring tiles come first, so a
+// CTA's first loads need no idx entries.  A CTA of a cluster takes every
+// cm-th position of its one unit.  Units are numbered ((b L) + l) Hkv + g, so
+// a unit's query and output rows start at row u G of [B, L, Hq, d].
+struct TileCursor {
+  int u, j, lt, b;  // unit, position and key tile within it, the unit's sequence
+  int left;         // units of sequence b from u on
+  __device__ __forceinline__ void init(int unit, int pos, const AttnParams& p) {
+    u = unit;
+    j = pos;
+    lt = j + p.rot;
+    if (lt >= p.tpu) lt -= p.tpu;
+    b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
+    left = (b + 1) * p.LH - u;
+  }
+  __device__ __forceinline__ void next(const AttnParams& p) {
+    if (p.cm > 0) {
+      j += p.cm;
+    } else if (++j == p.tpu) {
+      j = 0;
+      ++u;
+      if (--left == 0) {
+        left = p.LH;
+        ++b;
+      }
+    }
+    lt = j + p.rot;
+    if (lt >= p.tpu) lt -= p.tpu;
+  }
+};
+
+// Rotary embedding: (cos, sin) of pairs i = lane and lane + 32 (i < d/2) at the new
+// token's position rope_offset + pos.  `turns` holds F_lane and F_(lane+32) (0 past d/2;
+// see rope_cos_sin), loaded from the kernel parameters before the grid dependency wait.
+template <int D>
+__device__ __forceinline__ void rope_pairs(const AttnParams& p, long long pos,
+                                           const unsigned long long (&turns)[2], int lane,
+                                           float2 (&cs)[2]) {
+  const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + pos);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int i = lane + 32 * e;
+    cs[e] = make_float2(1.f, 0.f);
+    if (i < D / 2) cs[e] = rope_cos_sin(pp, turns[e]);
+  }
+}
+
+// Fused step: a CTA has read pos[b] for its run of `tiles` tiles of sequence
+// b.  The run that brings the sequence's count to all of its tiles is the last
+// reader of pos[b]; it advances pos[b] and clears the count for the next call.
+__device__ __forceinline__ void seq_run_done(const AttnParams& p, int b, int tiles,
+                                             const SeqState& sq) {
+  const unsigned long long total = static_cast<unsigned long long>(p.LH) * p.tpu;
+  const unsigned long long old = atomicAdd(p.tickets + b, static_cast<unsigned long long>(tiles));
+  if (old + static_cast<unsigned long long>(tiles) == total) {
+    if (!sq.bad) p.pos[b] = sq.pos + 1;
+    p.tickets[b] = 0ull;
+  }
+}
+
+// Finishes the units that two_tier_attn_kernel split between CTAs: merges
+// their fp32 partial records (max, sum, output per head) with a log-sum-exp
+// rescale and writes the bf16 output.  Runs after two_tier_attn_kernel on the
+// same stream, only when some unit was split; one CTA per unit.
+template <int D, int G>
+static __global__ void __launch_bounds__(kThreads)
+two_tier_combine_kernel(const AttnParams p) {
+  asm volatile("griddepcontrol.wait;\n" ::: "memory");  // the attention kernel's records
+  asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+  const int u = blockIdx.x;
+  const long long ut0 = static_cast<long long>(u) * p.tpu;
+  const long long c0 = cta_of_tile(ut0, p.base, p.rem);
+  const long long c1 = cta_of_tile(ut0 + p.tpu - 1, p.base, p.rem);
+  if (c0 == c1) return;  // written by the attention kernel
+  // one record per CTA that holds part of the unit, at the slot of that
+  // CTA's first tile in the unit (slot 0 for c0)
+  const int nrec = static_cast<int>(c1 - c0 + 1);
+  constexpr int PW = rec_floats(G, D);
+  const float* recs = p.partials + ut0 * PW;
+  const long long out_base = static_cast<long long>(u) * (G * D);
+  for (int x = threadIdx.x; x < G * D / 2; x += blockDim.x) {
+    const int hh = (2 * x) / D;
+    const int c = (2 * x) % D;
+    float M = -INFINITY;
+    for (int r = 0; r < nrec; ++r) M = fmaxf(M, recs[rec_slot(p, c0 + r, ut0) * PW + hh]);
+    float Ls = 0.f, O0 = 0.f, O1 = 0.f;
+    if (M != -INFINITY) {
+      for (int r = 0; r < nrec; ++r) {
+        const float* pr = recs + rec_slot(p, c0 + r, ut0) * PW;
+        const float f = ex2(pr[hh] - M);
+        const float2 o2 = *reinterpret_cast<const float2*>(pr + rec_out_offset(G) + hh * D + c);
+        Ls = fmaf(f, pr[G + hh], Ls);
+        O0 = fmaf(f, o2.x, O0);
+        O1 = fmaf(f, o2.y, O1);
+      }
+    }
+    const float inv = Ls > 0.f ? 1.f / Ls : 0.f;
+    *reinterpret_cast<uint32_t*>(p.out + out_base + hh * D + c) = pack_bf16x2(O0 * inv, O1 * inv);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Shared-memory layout of one pipeline stage (1024-byte aligned)
 // ---------------------------------------------------------------------------
@@ -1120,6 +1358,77 @@ static WsLayout ws_layout(const cmc_dims& m) {
   return w;
 }
 
+// Launch plan of one attention call on the current device.
+struct AttnPlan {
+  long long ctas, base, rem;  // grid size; flat split: granules per CTA (the first `rem` take one more)
+  int gran;                   // flat split: tiles per granule
+  int cm;                     // > 0: clusters of cm CTAs per unit (DSMEM merge, no combine)
+  bool split;                 // flat split cuts some unit: the combine kernel runs
+};
+
+// The plan of units of `tpu` tiles each on the current device, `per_sm` CTAs of the
+// attention kernel resident on an SM.
+static inline void plan_grid(long long total_tiles, int tpu, int per_sm, AttnPlan* pl) {
+  // Grid.  With no more units than resident CTAs: m = resident CTAs per unit,
+  // at most one per tile and at most 8 (the portable cluster size).  m = 1:
+  // one CTA per unit, nothing is split.  m >= 2: clusters of m CTAs per unit,
+  // merged in distributed shared memory.  More units than resident CTAs: one
+  // wave of CTAs, each taking a run of whole units or, when that would leave
+  // too few CTAs for the last round, an equal share of the flattened tiles
+  // (stream-K; the combine kernel merges the units cut between CTAs).  (A flat split
+  // for few, long units -- m up to 38 at one sequence of one layer -- left
+  // about one tile per CTA and a combine over 38 records: 33.4 us against
+  // 9.4 us for clusters of 8 at k = 1024, W = 2048.)
+  const long long slots = static_cast<long long>(per_sm) * sm_count();
+  const long long units = total_tiles / tpu;
+  pl->cm = 0;
+  long long ctas;
+  if (units <= slots) {
+    long long m = slots / units;
+    if (m > tpu) m = tpu;
+    if (m > kMaxClusterCtas) m = kMaxClusterCtas;
+    if (m >= 2) pl->cm = static_cast<int>(m);
+    ctas = units * m;
+  } else {
+    ctas = slots;
+  }
+  if (ctas > total_tiles) ctas = total_tiles;
+  if (ctas < 1) ctas = 1;
+  pl->ctas = ctas;
+  pl->gran = 1;
+  pl->base = total_tiles / ctas;
+  pl->rem = total_tiles % ctas;
+  // More units than resident CTAs: whole units per CTA (contiguous runs, no
+  // combine launch) when they divide evenly or when at least half of the CTAs
+  // take one unit more -- enough CTAs then stream the last round to keep HBM
+  // busy; with fewer, those few CTAs would stream their extra unit alone and
+  // the balanced stream-K split with its combine is faster.  Measured at
+  // 128 + 512-key units: 312 units 21.1 us stream-K / 23.7 us whole units,
+  // 384 units 24.5 / 25.5, 448 units 26.0 / 26.2, 512 units 30.1 / 27.1.
+  const long long ru = units % ctas;
+  if (units > slots && (ru == 0 || 2 * ru >= ctas)) {
+    pl->gran = tpu;
+    pl->base = units / ctas;
+    pl->rem = ru;
+  }
+  // Flat split: is any unit cut between CTAs (a CTA boundary inside a unit)?
+  if (units <= slots && pl->cm == 0) {  // one CTA per unit: whole units, one each
+    pl->gran = tpu;
+    pl->base = 1;
+    pl->rem = 0;
+  }
+  if (pl->cm > 0) {
+    pl->base = tpu / pl->cm;
+    pl->rem = tpu % pl->cm;
+  }
+  pl->split = false;
+  for (long long c = 1; pl->cm == 0 && pl->gran == 1 && c < ctas && !pl->split; ++c) {
+    const long long t = c * pl->base + (c < pl->rem ? c : pl->rem);
+    pl->split = (t % tpu) != 0;
+  }
+}
+
+// A [rows, d] bf16 tensor viewed by boxes of 64 columns x box_rows rows,
 // 128-byte swizzle, zero fill outside the tensor.
 static bool encode_rows(CUtensorMap* map, const void* base, long long rows, int d, int box_rows) {
   EncodeTiledFn enc = encode_fn();

@@ -467,12 +467,7 @@ attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {
       float2 cs[E];
       const unsigned long long pp = static_cast<unsigned long long>(p.rope_offset + (sq.bad ? 0 : pos));
 #pragma unroll
-      for (int e = 0; e < E; ++e) {  // as rope_pairs
-        const int hi = static_cast<int>(static_cast<long long>(pp * turns[e]) >> 32);
-        float sn, cn;
-        sincospif(static_cast<float>(hi) * 4.656612873077393e-10f, &sn, &cn);
-        cs[e] = make_float2(cn, sn);
-      }
+      for (int e = 0; e < E; ++e) cs[e] = rope_cos_sin(pp, turns[e]);
 #pragma unroll
       for (int h = 0; h < HPW; ++h)
         if (h0 + HSTEP * h < G) rotate_part<E>(x[h], cs, lane);
