@@ -84,7 +84,7 @@ PROFILE_FILE = os.path.join(ROOT, "profiles", "decode_step_llama3_8b.json")
 # library's default)
 SINGLE_STREAM_PREFETCH = 5
 KERNEL_SOURCES = [os.path.join(ROOT, "paper_2609_25537_gb300", "csrc", f)
-                  for f in ("cmc_attn.cu", "cmc_internal.cuh")]
+                  for f in ("cmc_attn.cu", "cmc_attn.cuh", "cmc_internal.cuh")]
 
 
 # ----------------------------------------------------------------------------
