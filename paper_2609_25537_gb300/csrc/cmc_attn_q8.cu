@@ -154,19 +154,21 @@ __device__ __forceinline__ int live_blocks(const AttnQ8Params& p, const SeqState
 }
 
 // Half a row of the new token each for lanes 0-15 (K) and 16-31 (V): d / 16 neighbouring elements.
+// (Plain loads, here and below: the launch before may still have been writing the rows when this one began,
+// which the read-only path does not allow for.)
 template <int D>
 __device__ __forceinline__ uint4 load_new(const AttnQ8Params& p, int u, int lane) {
   const uint16_t* row = (lane < 16 ? p.k_new : p.v_new) + static_cast<long long>(u) * D + (lane & 15) * (D / 16);
-  if (D == 128) return __ldg(reinterpret_cast<const uint4*>(row));
-  const uint2 w = __ldg(reinterpret_cast<const uint2*>(row));
+  if (D == 128) return *reinterpret_cast<const uint4*>(row);
+  const uint2 w = *reinterpret_cast<const uint2*>(row);
   return make_uint4(w.x, w.y, 0u, 0u);
 }
 
 // A lane's E = d / 32 neighbouring elements of a row, and their values.
 template <int E>
 __device__ __forceinline__ uint2 load_part(const uint16_t* row, int lane) {
-  if (E == 4) return __ldg(reinterpret_cast<const uint2*>(row) + lane);
-  return make_uint2(__ldg(reinterpret_cast<const uint32_t*>(row) + lane), 0u);
+  if (E == 4) return reinterpret_cast<const uint2*>(row)[lane];
+  return make_uint2(reinterpret_cast<const uint32_t*>(row)[lane], 0u);
 }
 template <int E>
 __device__ __forceinline__ void unpack_part(const uint2& w, float (&x)[E]) {

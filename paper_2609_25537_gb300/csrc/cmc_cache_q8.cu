@@ -9,6 +9,8 @@
 
 namespace cmc {
 
+// (No __restrict__: it lets inputs be read on the read-only path, and the launch before may still have been
+// writing them when this one began.)
 constexpr int kRowThreads = 128;  // four warps, each with blocks of rows of its own
 constexpr int kRowWarps = kRowThreads / 32;
 
@@ -32,9 +34,9 @@ __device__ __forceinline__ uint32_t encode4_bf16(uint32_t a, uint32_t b, uint32_
 // 28.7 with one; 22.1 since blocks without a token are only written).
 template <int D, int NST>
 __global__ void __launch_bounds__(kRowThreads)
-quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict__ bank_v,
-                const int32_t* __restrict__ idx, const int64_t* __restrict__ count,
-                uint8_t* __restrict__ kv, uint8_t* __restrict__ scales, uint32_t* status,
+quantize_kernel(const uint16_t* bank_k, const uint16_t* bank_v,
+                const int32_t* idx, const int64_t* count,
+                uint8_t* kv, uint8_t* scales, uint32_t* status,
                 long long jobs, int nb, int LH, int N, int k, int S, uint32_t stall_tx) {
   constexpr int kStage = kQ8Block * D * 2;
   constexpr int NP = kStage / 512;  // passes of the warp over a block, 16 bytes a lane
@@ -188,9 +190,9 @@ quantize_kernel(const uint16_t* __restrict__ bank_k, const uint16_t* __restrict_
 // in all) 117.5 us, the copy rate; 2,048 blocks 5.2 us, of which 3.7 are HBM's.
 template <int D>
 __global__ void __launch_bounds__(kRowThreads)
-dequantize_kernel(const uint8_t* __restrict__ kv, const uint8_t* __restrict__ scales,
-                  const int32_t* __restrict__ idx, uint4* __restrict__ out_k,
-                  uint4* __restrict__ out_v, uint32_t* status, long long jobs, int nb, int LH, int N,
+dequantize_kernel(const uint8_t* kv, const uint8_t* scales,
+                  const int32_t* idx, uint4* out_k,
+                  uint4* out_v, uint32_t* status, long long jobs, int nb, int LH, int N,
                   int k, int S) {
   constexpr int CPR = D / 8;  // 8-code chunks of a row (16 bytes of the output)
   constexpr int RPP = 32 / CPR;
@@ -284,8 +286,8 @@ __device__ __forceinline__ int recode_block(uint8_t* block, uint32_t others, uin
 
 template <int D>
 __global__ void __launch_bounds__(kAppendThreads, 2)
-window_append_q8_kernel(uint8_t* ring, uint8_t* scales, int64_t* pos, const uint16_t* __restrict__ k_new,
-                        const uint16_t* __restrict__ v_new, int LH, int W, int S, int ctas) {
+window_append_q8_kernel(uint8_t* ring, uint8_t* scales, int64_t* pos, const uint16_t* k_new,
+                        const uint16_t* v_new, int LH, int W, int S, int ctas) {
   constexpr int E = D / 16;  // elements a lane has of its row
   pdl_wait();
   pdl_trigger();

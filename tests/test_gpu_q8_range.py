@@ -184,6 +184,32 @@ def test_values_near_the_smallest(cuda_device, form, byte):
     check(run(cuda_device, *problem), *problem[:3], range(2), "")
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_nan_reaches_what_it_touches_alone(cuda_device, form):
+    """A query with a NaN or an infinity: its head. A block whose byte for K or V is NaN, the last of a warp or all of
+    them: the heads of its unit. A NaN among the values: its column."""
+    rng = np.random.default_rng(6)
+    q, t1, ring, pos = make(rng, form, lambda u, i: 120 + i % 3)
+    G = FORMS[form][3]
+    q[0, 0, 0, 5] = float("nan")
+    q[0, 0, G + 1, 0] = -float("inf")  # (unit 1)
+    ring[1][0, 0, 2, 0, (ring[0].shape[4] - 1) // 32] = 255
+    ring[1][0, 0, 3, 1, (ring[0].shape[4] - 1) // 32] = 255
+    t1[1][0, 0, 4, 1, 0] = 255
+    t1[1][0, 0, 5] = ring[1][0, 0, 5] = 255
+    ring[0][0, 0, 6, 1, 40, 7] = 0xFF
+    got = run(cuda_device, q, t1, ring, pos)
+    want = torch.zeros(got.shape, dtype=torch.bool)
+    want[0, 0, 0] = want[0, 0, G + 1] = True
+    want[0, 0, 2 * G:6 * G] = True
+    want[0, 0, 6 * G:7 * G, 7] = True
+    assert torch.equal(torch.isnan(got).cpu(), want)
+    q[0, 0, 0, 5] = q[0, 0, G + 1, 0] = 0.0
+    ring[0][0, 0, 6, 1, 40, 7] = 0  # unit 7 has nothing of them, the others' heads without one are as ever
+    check(run(cuda_device, q, t1, ring, pos), q, t1, ring, [0, 1, 6, 7], "")
+    check(got, q, t1, ring, [7], "")
+
+
 @pytest.mark.parametrize("sign", [1, -1])
 @pytest.mark.parametrize("form", FORMS)
 def test_large_scores(cuda_device, form, sign):
