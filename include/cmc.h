@@ -555,7 +555,8 @@ CMC_API size_t cmc_decode_attn_q8_workspace_size(const cmc_dims* dims);
  * bits, or 2^-29 of the largest; a query element is exact down to 2^-22 of its head's largest.  Blocks of V
  * may differ in size as the format allows; of tokens that count 2^-64 or less of the one that counts
  * most (probability times largest value of the block) smaller elements may be lost.  Scores
- * scale q k may be up to 2^22.  A NaN among the tokens reaches the
+ * scale q k may be up to 2^22, and a query's largest element times a block's largest key element up
+ * to 2^100.  A NaN among the tokens reaches the
  * outputs of its KV head's queries; slots that hold no token may hold anything.
  * A sequence with pos[b] < 0 gets a zero output and sets CMC_DEVFLAG_BAD_POS.
  */

@@ -18,7 +18,7 @@
 // next unit, and what one CTA waits for (its first bytes, its merge) the others on the SM
 // cover.  The depth of the rings of stages sets how many those are: see plan_q8.  Rings of
 // different fill are evened out by taking the longest sequences first (p.order): a long
-// unit that starts last sets the time of the launch.  512 units of 312 to 2,304 keys 25.0 us (in the order of
+// unit that starts last sets the time of the launch.  512 units of 312 to 2,304 keys 24.8 us (in the order of
 // the batch 30.9), 1,024 48.8; full ones 48.9 and 97.8, which in batch order and the best variant take
 // 47.7 and 90.0: each CTA reads all positions, and sorts, before it knows its unit.  (Sharing out
 // the live blocks of all units evenly over the warps of one wave, with a kernel to merge the
@@ -300,7 +300,8 @@ static __device__ __noinline__ void count_left_units(unsigned long long* tickets
 // gridDim x 4 after its own, whose query, position and first blocks are then already on
 // their way.
 // Registers: three CTAs an SM take 168 a thread (two of them with 168 instead of 200 spill: 2,048 units of 640
-// keys 56 us and 54); with d = 64 four SOLO CTAs fit with 128.
+// keys 56 us and 54), and the fused ones spill 32 to 44 bytes; with d = 64 four SOLO CTAs fit with 128, of which
+// the fused ones spill 40 to 64.
 template <int D, int G, bool FUSED, int NST, bool SOLO>
 __global__ void __maxnreg__(SOLO ? (D == 64 ? 128 : 240) : NST == 2 ? 168 : 200)
 attn_q8_kernel(const __grid_constant__ Q8Maps maps, const AttnQ8Params p) {

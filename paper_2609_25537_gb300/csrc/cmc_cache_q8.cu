@@ -248,8 +248,10 @@ dequantize_kernel(const uint8_t* kv, const uint8_t* scales,
 // after a barrier over every thread that reads it.
 //
 // Latency bounds it: the position, then a row and its byte, then the block where it is taken, each a trip to
-// memory.  A single unit takes 1.8 us, 32 sequences of 256 units 11.1 us (HBM's part of that is 0.9;
-// with one row at a time a warp, and a changed block read by a lane a row, 29).
+// memory.  A single unit takes 1.7 to 2.1 us, 32 sequences of 256 units 6.9 us (HBM's part of that is 0.9),
+// and 11.1 where more of their blocks change (with one row at a time a warp, and a changed
+// block read by a lane a row, 29).  At d = 128 two blocks' chunks a lane do not fit 64 registers, which two CTAs
+// an SM leave: 64 bytes are spilled.
 constexpr int kAppendThreads = 512;
 constexpr int kAppendWarps = kAppendThreads / 32;
 constexpr int kAppendUnits = 2;
