@@ -341,6 +341,7 @@ class DecodeWorkspace:
         self.nbytes = n
         self.buf = torch.zeros(n, dtype=torch.uint8, device=device)
         self.ptr = self.buf.data_ptr()
+        self.index = self.buf.get_device()  # -1 on the host
 
     def status(self, clear: bool = True) -> int:
         """CMC_DEVFLAG_* bits raised by kernels since the last clear (synchronises)."""
@@ -349,6 +350,10 @@ class DecodeWorkspace:
                                    _stream(self.buf.device))
         check(st, "cmc_read_status")
         return int(flags.value)
+
+
+def _elsewhere_workspace(workspace: DecodeWorkspace, index: int) -> ValueError:
+    return ValueError(f"workspace is on {workspace.buf.device}, expected cuda:{index}")
 
 
 _ws_cache: Dict[Tuple, DecodeWorkspace] = {}
@@ -405,6 +410,8 @@ def two_tier_decode_attn(q, tier1_k, tier1_v, idx, ring_k, ring_v, pos, *,
     cmc_two_tier_decode_attn.  Returns bf16 [B, L, Hq, d]."""
     sizes, dev, out = _attn_args(q, tier1_k, tier1_v, idx, ring_k, ring_v, pos, out)
     dims, stream = CmcDims(*sizes), _stream(dev)
+    if workspace is not None and workspace.index != dev.index:
+        raise _elsewhere_workspace(workspace, dev.index)
     ws = workspace if workspace is not None else _workspace_for(sizes, dims, dev, stream)
     st = lib().cmc_two_tier_decode_attn(
         _p(q), _p(tier1_k), _p(tier1_v), _p(idx), _p(ring_k), _p(ring_v), _p(pos),
@@ -433,6 +440,8 @@ def decode_step(q, tier1_k, tier1_v, idx, ring_k, ring_v, pos, k_new, v_new, *,
     if k_new.shape != want or v_new.shape != want:
         raise ValueError(f"k_new/v_new must be {want}")
     dims, stream = CmcDims(*sizes), _stream(dev)
+    if workspace is not None and workspace.index != dev.index:
+        raise _elsewhere_workspace(workspace, dev.index)
     ws = workspace if workspace is not None else _workspace_for(sizes, dims, dev, stream)
     if rope_theta is None:
         st = lib().cmc_decode_step(
@@ -488,6 +497,8 @@ def tier1_gather(bank_k: torch.Tensor, bank_v: torch.Tensor, idx: torch.Tensor, 
         if tuple(t.shape) != want:
             raise ValueError(f"{name} must be {want}")
     dims = CmcDims(B, L, Hkv, Hkv, d, N, k, 1)
+    if workspace is not None and workspace.index != dev.index:
+        raise _elsewhere_workspace(workspace, dev.index)
     status = None if workspace is None else workspace.buf
     st = lib().cmc_tier1_gather(_p(bank_k), _p(bank_v), _p(idx), ctypes.byref(dims), _p(out_k),
                                 _p(out_v), _p(status), _stream(dev))
@@ -619,6 +630,8 @@ def quantize_cache(k: torch.Tensor, v: torch.Tensor, idx: Optional[torch.Tensor]
     if not isinstance(v, torch.Tensor) or not _as(torch.bfloat16, index, v) or v.shape != k.shape:
         _need(v, "v", torch.bfloat16, 5, dev)
         raise ValueError("v must have the shape of k")
+    if workspace is not None and workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
     rows = _need_rows(idx, count, k, 3, dev)
     key = ("quantize", k.shape, rows)
     kept = _shapes_cache.get(key)
@@ -654,6 +667,8 @@ def dequantize_cache(kv: torch.Tensor, scales: torch.Tensor, idx: Optional[torch
     _need(kv, "kv", _E4M3, 6)
     dev = kv.device
     index = dev.index
+    if workspace is not None and workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
     rows = _need_rows(idx, None, kv, 4, dev)
     kept = None
     if isinstance(scales, torch.Tensor) and _as(_E8M0, index, scales):
@@ -827,6 +842,8 @@ def two_tier_decode_attn_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos
             workspace = workspaces.get((index, stream))
         if workspace is None:
             workspace = _attn_q8_workspace(workspaces, index, stream, dims)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
     args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
             0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
             ring_scales.data_ptr(), pos.data_ptr(), ref, 0.0 if scale is None else scale,
@@ -877,6 +894,8 @@ def decode_step_q8(q, tier1_kv, tier1_scales, ring_kv, ring_scales, pos, k_new, 
             workspace = workspaces.get((index, stream))
         if workspace is None:
             workspace = _attn_q8_workspace(workspaces, index, stream, dims)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
     args = (q.data_ptr(), 0 if tier1_kv is None else tier1_kv.data_ptr(),
             0 if tier1_scales is None else tier1_scales.data_ptr(), ring_kv.data_ptr(),
             ring_scales.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ref,

@@ -154,3 +154,26 @@ def test_quantising_reports_a_wait_that_ran_out(cuda_device, d, N, by_index):
     for x, y in zip(cmc.quantize_cache(bank, bank, idx, workspace=ws), want):
         assert torch.equal(x.view(torch.uint8), y)
     assert ws.status() == 0
+
+
+def test_a_workspace_elsewhere_is_refused(cuda_device):
+    """On the host, whose memory a kernel cannot count on reaching; nothing is written."""
+    q, *t1, kv, scales, pos, k_new, v_new = step_problem(cuda_device, 2, 1, 2, 2, 64, 32, 64, 3)
+    before = [x.clone() for x in (kv, scales, pos)]
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 1, 4, 2, 64, 32, 32, 64), torch.device("cpu"))
+    first = torch.zeros(2, 1, dtype=torch.int32, device=cuda_device)
+    bank = torch.zeros(2, 1, 2, 5, 64, dtype=torch.bfloat16, device=cuda_device)
+    for call in (lambda: cmc.quantize_cache(bank, bank, workspace=ws),
+                 lambda: cmc.dequantize_cache(kv, scales, workspace=ws),
+                 lambda: cmc.two_tier_decode_attn_q8(q, *t1, kv, scales, pos, workspace=ws),
+                 lambda: cmc.decode_step_q8(q, *t1, kv, scales, pos, k_new, v_new, workspace=ws),
+                 # and in the calls over a bf16 cache
+                 lambda: cmc.tier1_gather(bank, bank, first, workspace=ws),
+                 lambda: cmc.two_tier_decode_attn(q, bank, bank, None, bank, bank, pos, workspace=ws),
+                 lambda: cmc.decode_step(q, bank, bank, None, bank, bank, pos, k_new, v_new, workspace=ws)):
+        with pytest.raises(ValueError, match="workspace is on cpu"):
+            call()
+    torch.cuda.synchronize()
+    for x, y in zip((kv, scales, pos), before):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    assert not ws.buf.any()
