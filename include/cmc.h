@@ -594,6 +594,156 @@ CMC_API int cmc_decode_step_q8(const void* q, const void* tier1_kv, const void* 
 CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas);
 
 /* ------------------------------------------------------------------------ *
+ * Prefill into the cache, weights of its tokens, eviction by weight (not    *
+ * steps of the paper's method: what a decoder does before its first decode  *
+ * step, and a way to keep the cache within a budget by what was attended to)*
+ * ------------------------------------------------------------------------ */
+
+/*
+ * Norm and rotary embedding of query and key heads, before they are attended with
+ * or cached.  For head row x (d elements) of layer l, at position p:
+ *     y = x / sqrt(mean(x^2) + eps) * w[l]                  (RMS norm, where w is given)
+ *     (y_i, y_(i + d/2)) turned by the angle p * rope_theta^(-2i/d)   (where rope_theta > 0)
+ * in fp32, rounded once.  Angles as for cmc_decode_step_rope, at
+ *     p = rope_offset + evicted[b] + pos[b] + t
+ * for token t of a call: pos[b] counts the tokens that the ring was given and evicted[b] those
+ * that cmc_evict_cache took out of it again.  A NULL cmc_qk_prep is neither norm nor rotation.
+ */
+typedef struct cmc_qk_prep {
+  const float* q_weight;  /* fp32 [L, d], 16-byte aligned, or NULL: no norm of the queries  */
+  const float* k_weight;  /* likewise of the keys                                           */
+  const int64_t* evicted; /* int64 [B], or NULL for zeros                                   */
+  double rope_theta;      /* 0: no rotation; else positive and finite                       */
+  int64_t rope_offset;    /* 0 .. 2^32, with a rope_theta                                   */
+  float eps;              /* >= 0 and finite, with a weight                                 */
+} cmc_qk_prep;
+
+/*
+ * cmc_qk_prep's norm and rotation of T tokens of every sequence and layer.
+ *
+ *   q      bf16 [B, L, T, Hq, d], of which only the heads of a token need be dense: tokens (in the
+ *          order b, l, t) are q_stride elements apart (q_stride >= Hq d, a multiple of 8), as
+ *          part of a projection's output [B, L, T, Hq + 2 Hkv, d], say
+ *   k      bf16 [B, L, T, Hkv, d], k_stride likewise
+ *   pos    int64 [B] (read only; any value)
+ *   out_q  bf16 [B, L, T, Hq, d] dense; may be q where that is dense too
+ *   out_k  bf16 [B, L, T, Hkv, d] dense; may be k likewise
+ *
+ * dims->N, k and W are ignored.  T == 0 launches nothing.  Limits: 0 <= T <= 2^24, L * T < 2^27.
+ */
+CMC_API int cmc_qk_norm_rope(const void* q, int64_t q_stride, const void* k, int64_t k_stride, int T,
+                             const int64_t* pos, const cmc_dims* dims, const cmc_qk_prep* prep,
+                             void* out_q, void* out_k, void* stream);
+
+/* Bytes of workspace cmc_window_prefill and cmc_evict_cache need for B sequences: the device status
+ * word and one 8-byte counter per sequence.  Zero-fill it once before its first use; every call leaves
+ * the counters at zero.  Any attention workspace for the same B will do as well. */
+CMC_API size_t cmc_cache_workspace_size(int B);
+
+/*
+ * Prefill of the ring: cmc_qk_norm_rope of the first count[b] of T tokens of every sequence, whose keys
+ * and values are appended to the ring, as count[b] calls of cmc_window_append would: token t goes to
+ * slot (pos[b] + t) mod W, of more than W tokens the last W stay, and pos[b] grows by count[b].
+ *
+ *   q, k            as for cmc_qk_norm_rope; q may be NULL (no queries)
+ *   v               bf16 [B, L, T, Hkv, d], v_stride like k_stride; values are stored as they are
+ *   ring_k, ring_v  bf16 [B, L, Hkv, W, d]   updated in place
+ *   ring_weight     fp32 [B, L, Hkv, W], or NULL: the weights of the slots written become 0
+ *   pos             int64 [B]; updated
+ *   count           int64 [B] (values are clamped to [0, T]), or NULL for T each
+ *   out_q           bf16 [B, L, T, Hq, d] dense (may be q where that is dense); tokens from count[b] on
+ *                   are not written
+ *   workspace       see cmc_cache_workspace_size
+ *
+ * dims->N and k are ignored.  A sequence with pos[b] < 0 is left unchanged, its out_q too, and
+ * CMC_DEVFLAG_BAD_POS is set.  T == 0 launches nothing.  Limits as for cmc_qk_norm_rope.
+ */
+CMC_API int cmc_window_prefill(const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                               const void* v, int64_t v_stride, int T, void* ring_k, void* ring_v,
+                               float* ring_weight, int64_t* pos, const int64_t* count,
+                               const cmc_dims* dims, const cmc_qk_prep* prep, void* out_q,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
+/* Bytes of workspace the two calls below need for `dims`: the device status word, one 8-byte counter per
+ * sequence and, for units too long for a cluster's shared memory (from 147,456 / G keys on, G = Hq / Hkv),
+ * 4 G bytes a key.  Zero-fill it once before its first use; every call leaves the
+ * counters at zero. */
+CMC_API size_t cmc_decode_attn_weighted_workspace_size(const cmc_dims* dims);
+
+/*
+ * cmc_two_tier_decode_attn over rows 0 .. k-1 of Tier-1 and the ring (no index), which also adds to each
+ * key's weight the probabilities that the queries of its KV head gave it:
+ *     weight[b,l,g,j] += sum over the Hq/Hkv heads h of g of softmax_j(scale * q[b,l,h] . key_j)
+ *
+ *   tier1_k, tier1_v, tier1_weight  bf16 [B, L, Hkv, N, d], fp32 [B, L, Hkv, N]; may be NULL when k == 0
+ *   ring_k, ring_v, ring_weight     bf16 [B, L, Hkv, W, d], fp32 [B, L, Hkv, W]
+ *   workspace                       see cmc_decode_attn_weighted_workspace_size
+ *
+ * Other arguments as there.  Weights are updated in place, in fp32 and in a fixed order; those of rows that
+ * hold no token are neither read nor written.  A NaN among the keys reaches the outputs and the
+ * weights of its KV head.  A sequence with pos[b] < 0 gets a zero output, its
+ * weights stay, and CMC_DEVFLAG_BAD_POS is set.
+ */
+CMC_API int cmc_two_tier_decode_attn_weighted(const void* q, const void* tier1_k, const void* tier1_v,
+                                              float* tier1_weight, const void* ring_k,
+                                              const void* ring_v, float* ring_weight,
+                                              const int64_t* pos, const cmc_dims* dims, float scale,
+                                              void* out, void* workspace, size_t workspace_bytes,
+                                              void* stream);
+
+/*
+ * One fused decode step: cmc_window_append, the new token's weight set to 0, then
+ * cmc_two_tier_decode_attn_weighted, in one launch; with a `prep` (may be NULL) q and k_new are given before
+ * its norm and rotation, at position rope_offset + evicted[b] + pos[b] (pos before the append).  The
+ * prepared key is rounded to bf16, as it is stored and attended to; the prepared query is held to 16
+ * significant bits.  A sequence with pos[b] < 0 is left unchanged, its output is zero and
+ * CMC_DEVFLAG_BAD_POS is set.
+ */
+CMC_API int cmc_decode_step_weighted(const void* q, const void* tier1_k, const void* tier1_v,
+                                     float* tier1_weight, void* ring_k, void* ring_v,
+                                     float* ring_weight, int64_t* pos, const void* k_new,
+                                     const void* v_new, const cmc_dims* dims, float scale,
+                                     const cmc_qk_prep* prep, void* out, void* workspace,
+                                     size_t workspace_bytes, void* stream);
+
+/* Launch plan of the two calls above for `dims` on the current device (fused == 0: the attention, else the
+ * step): *ctas receives the grid size of their one kernel, a CTA or a cluster of up to 8 for every (sequence,
+ * layer, KV head) unit. */
+CMC_API int cmc_decode_attn_weighted_plan(const cmc_dims* dims, int fused, int* ctas);
+
+/*
+ * Eviction by weight: of the tokens that a cache holds for a sequence, every (layer, KV head) unit keeps
+ * `keep` of its own choice: the `recent` youngest and, of the others, those of the largest weight (equal weights:
+ * the older; -0 equals +0; a NaN is below every other value).  They are moved together, in order of age, with their
+ * weights.
+ *
+ * The cache has T = dims->N rows a unit.  pos == NULL: all T hold tokens, in order of age.  Else the cache is a ring
+ * (dims->N its W): n = min(pos[b], T) rows hold tokens, from row 0 on or, when pos[b] > T, from row
+ * pos[b] mod T on and around.  A sequence with n <= keep keeps all of its tokens (m = min(n, keep) in the following).
+ *
+ *   k, v, weight        bf16 [B, L, Hkv, T, d], fp32 [B, L, Hkv, T]
+ *   dims->k             keep, 1 <= keep <= T
+ *   dims->W             rows of the output, >= keep
+ *   recent              0 .. keep
+ *   out_k, out_v, out_weight  bf16 [B, L, Hkv, W, d], fp32 [B, L, Hkv, W]: rows 0 .. m-1 are written.
+ *                       In place: all three the inputs' own (with dims->W == dims->N); otherwise they must
+ *                       not overlap the inputs
+ *   idx_out             int32 [B, L, Hkv, keep]: the rows that were kept, then -1
+ *   out_pos             int64 [B] or NULL: m, what the ring of the output holds; may be pos
+ *   evicted             int64 [B] or NULL: grows by pos[b] - m (T - m without pos), so that
+ *                       evicted[b] + out_pos[b] is the number of the next token as before
+ *   workspace           see cmc_cache_workspace_size
+ *
+ * dims->Hq is ignored.  A sequence with pos[b] < 0, or in place one whose ring starts elsewhere than at row 0
+ * (pos[b] > T and pos[b] mod T != 0), is left as it is: out_pos[b] = pos[b], its idx_out is -1, and
+ * CMC_DEVFLAG_BAD_POS is set.
+ */
+CMC_API int cmc_evict_cache(const void* k, const void* v, const float* weight, const int64_t* pos,
+                            const cmc_dims* dims, int recent, void* out_k, void* out_v,
+                            float* out_weight, int32_t* idx_out, int64_t* out_pos, int64_t* evicted,
+                            void* workspace, size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------ *
  * Staging copies for a serving loop (not a step of the paper's method: the  *
  * input and output traffic of the decode loop around it)                    *
  * ------------------------------------------------------------------------ */

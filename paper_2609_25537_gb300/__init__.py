@@ -18,11 +18,16 @@ from .cmc import (  # noqa: F401
     decode_q8_status,
     decode_attn_workspace_size,
     decode_step,
+    decode_attn_weighted_plan,
+    decode_attn_weighted_workspace_size,
     decode_step_q8,
+    decode_step_weighted,
     denoise,
     dequantize_cache,
     dims_of,
+    evict_cache,
     q8_scale_bytes,
+    qk_norm_rope,
     quantize_cache,
     question_select,
     score_select,
@@ -32,7 +37,10 @@ from .cmc import (  # noqa: F401
     tier1_gather,
     two_tier_decode_attn,
     two_tier_decode_attn_q8,
+    two_tier_decode_attn_weighted,
+    weighted_cache_status,
     window_append,
     window_append_q8,
+    window_prefill,
 )
 from ._lib import CmcError, EXPORTS, LIB_PATH, lib  # noqa: F401

@@ -42,6 +42,14 @@ EXPORTS = (
     "cmc_two_tier_decode_attn_q8",
     "cmc_decode_step_q8",
     "cmc_decode_attn_q8_plan",
+    "cmc_qk_norm_rope",
+    "cmc_cache_workspace_size",
+    "cmc_window_prefill",
+    "cmc_decode_attn_weighted_workspace_size",
+    "cmc_two_tier_decode_attn_weighted",
+    "cmc_decode_step_weighted",
+    "cmc_decode_attn_weighted_plan",
+    "cmc_evict_cache",
     "cmc_stage_copies",
     "cmc_score_select_static",
 )
@@ -74,6 +82,13 @@ class CmcDims(ctypes.Structure):
         return tuple(getattr(self, f) for f, _ in self._fields_)
 
 
+class CmcQkPrep(ctypes.Structure):
+    """Mirror of `cmc_qk_prep` (include/cmc.h)."""
+    _fields_ = [("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("evicted", ctypes.c_void_p), ("rope_theta", ctypes.c_double),
+                ("rope_offset", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
 class CmcError(RuntimeError):
     def __init__(self, status: int, where: str, cuda_error: int = 0):
         self.status = status
@@ -89,6 +104,7 @@ _lock = threading.Lock()
 
 _vp = ctypes.c_void_p
 _i = ctypes.c_int
+_i64 = ctypes.c_int64
 _sz = ctypes.c_size_t
 _dims_p = ctypes.POINTER(CmcDims)
 
@@ -128,6 +144,18 @@ _SIGNATURES = {
     "cmc_decode_step_q8": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p, ctypes.c_float,
                                 ctypes.c_double, ctypes.c_int64, _vp, _vp, _sz, _vp]),
     "cmc_decode_attn_q8_plan": (_i, [_dims_p, _i, ctypes.POINTER(_i)]),
+    "cmc_qk_norm_rope": (_i, [_vp, _i64, _vp, _i64, _i, _vp, _dims_p, _vp, _vp, _vp, _vp]),
+    "cmc_cache_workspace_size": (_sz, [_i]),
+    "cmc_window_prefill": (_i, [_vp, _i64, _vp, _i64, _vp, _i64, _i, _vp, _vp, _vp, _vp, _vp, _dims_p,
+                                _vp, _vp, _vp, _sz, _vp]),
+    "cmc_decode_attn_weighted_workspace_size": (_sz, [_dims_p]),
+    "cmc_two_tier_decode_attn_weighted": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p,
+                                               ctypes.c_float, _vp, _vp, _sz, _vp]),
+    "cmc_decode_step_weighted": (_i, [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _dims_p,
+                                      ctypes.c_float, _vp, _vp, _vp, _sz, _vp]),
+    "cmc_decode_attn_weighted_plan": (_i, [_dims_p, _i, ctypes.POINTER(_i)]),
+    "cmc_evict_cache": (_i, [_vp, _vp, _vp, _vp, _dims_p, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz,
+                             _vp]),
     "cmc_stage_copies": (_i, [_vp, _i, _i, _vp]),
     "cmc_score_select_static": (_i, [_vp, _vp, _i, _i, _i, _i, _vp, _vp]),
 }

@@ -18,6 +18,10 @@ and of the cache in 8 bits (T tokens, see cmc.h for the format):
   kv            float8_e4m3fn  [B, L, Hkv, 2, T, d]   keys, then values
   scales        float8_e8m0fnu [B, L, Hkv, 2, q8_scale_bytes(T)]
 
+and where the cache's tokens have weights (what they received in attention):
+
+  tier1_weight  fp32 [B, L, Hkv, N]    ring_weight  fp32 [B, L, Hkv, W]
+
 Tier-1 selection in the attention calls: an ``idx`` tensor [B, k] gathers
 rows of the bank by index at every step; ``idx=None`` takes every row of
 ``tier1_k``/``tier1_v`` in order (k = N), which is how the dense Tier-1 cache
@@ -33,7 +37,7 @@ from typing import Dict, Optional, Tuple
 
 import torch
 
-from ._lib import CmcCopy, CmcDims, check, lib, DEVFLAG_BAD_INDEX, DEVFLAG_BAD_POS, DEVFLAG_TIMEOUT
+from ._lib import CmcCopy, CmcDims, CmcQkPrep, check, lib, DEVFLAG_BAD_INDEX, DEVFLAG_BAD_POS, DEVFLAG_TIMEOUT
 
 __all__ = [
     "CmcDims",
@@ -58,6 +62,14 @@ __all__ = [
     "decode_attn_q8_workspace_size",
     "decode_q8_status",
     "q8_scale_bytes",
+    "qk_norm_rope",
+    "window_prefill",
+    "two_tier_decode_attn_weighted",
+    "decode_step_weighted",
+    "evict_cache",
+    "decode_attn_weighted_plan",
+    "decode_attn_weighted_workspace_size",
+    "weighted_cache_status",
     "set_l2_prefetch_tiles",
     "dims_of",
     "stage_copies",
@@ -326,15 +338,24 @@ def decode_attn_q8_workspace_size(dims: CmcDims) -> int:
     return int(lib().cmc_decode_attn_q8_workspace_size(ctypes.byref(dims)))
 
 
+def decode_attn_weighted_workspace_size(dims: CmcDims) -> int:
+    return int(lib().cmc_decode_attn_weighted_workspace_size(ctypes.byref(dims)))
+
+
 class DecodeWorkspace:
     """Zero-filled device workspace for the attention entry points (with ``q8`` for
-    those over a cache in 8 bits).
+    those over a cache in 8 bits, with ``weighted`` for those that accumulate weights; any
+    of the three for :func:`window_prefill` and :func:`evict_cache` of as many sequences).
 
     Holds the device status word and the fp32 partial results of keys split
     between CTAs.  Calls sharing one workspace must be ordered on one stream."""
 
-    def __init__(self, dims: CmcDims, device: torch.device, q8: bool = False):
-        n = decode_attn_q8_workspace_size(dims) if q8 else decode_attn_workspace_size(dims)
+    def __init__(self, dims: CmcDims, device: torch.device, q8: bool = False, weighted: bool = False):
+        if q8 and weighted:
+            raise ValueError("a workspace is of one kind: q8 or weighted")
+        n = (decode_attn_q8_workspace_size(dims) if q8
+             else decode_attn_weighted_workspace_size(dims) if weighted
+             else decode_attn_workspace_size(dims))
         if n == 0:
             raise ValueError(f"unsupported dims {dims.key()}")
         self.dims = dims
@@ -914,6 +935,453 @@ def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> int:
     check(lib().cmc_decode_attn_q8_plan(ctypes.byref(dims), 1 if fused else 0, ctypes.byref(ctas)),
           "cmc_decode_attn_q8_plan")
     return int(ctas.value)
+
+
+# ----------------------------------------------------------------------------
+# Prefill into the cache, weights of its tokens, eviction by weight
+# ----------------------------------------------------------------------------
+
+_F32 = torch.float32
+_weighted_workspaces: Dict[Tuple, Dict[Tuple[int, int], DecodeWorkspace]] = {}
+
+
+def _int32(x: int) -> int:
+    """For the library: what it refuses stays refused, where ctypes would cut it to 32 bits."""
+    return x if 0 <= x < 1 << 31 else -1
+
+
+def _kept_workspaces(dims: CmcDims) -> Dict:
+    """The workspaces that calls of these sizes choose themselves, by device and stream: one for all calls
+    of a batch size, but for units so long that the workspace goes by their size."""
+    n = decode_attn_weighted_workspace_size(dims)
+    base = int(lib().cmc_cache_workspace_size(dims.B))
+    return _weighted_workspaces.setdefault((dims.B,) if n == base else dims.key(), {})
+
+
+def _own_workspace(kept: Dict, index: int, stream: int, dims: CmcDims) -> DecodeWorkspace:
+    """A workspace for a call that is given none.  One is kept per stream; a call that is being
+    captured gets one of its graph's own, since the kept ones are zero-filled once, outside
+    of it, and other calls use them.  (The default stream, 0, is never captured.)"""
+    if stream and torch._C._cuda_isCurrentStreamCapturing():
+        return DecodeWorkspace(dims, torch.device("cuda", index), weighted=True)
+    ws = kept.get((index, stream))
+    if ws is None:
+        ws = kept[index, stream] = DecodeWorkspace(dims, torch.device("cuda", index), weighted=True)
+    return ws
+
+
+def weighted_cache_status(device: Optional[torch.device] = None, clear: bool = True) -> int:
+    """DEVFLAG_* bits that the calls of this section which were given no ``workspace`` have raised on
+    `device` (None: the current one) since the last clear; waits for all work on it.  Calls captured
+    into a graph are not among them: give those a workspace to see theirs."""
+    index = None if device is None else torch.device(device).index
+    if index is None:
+        index = torch.cuda.current_device()
+    flags = 0
+    with torch.cuda.device(index):
+        torch.cuda.synchronize()
+        for kept in list(_weighted_workspaces.values()):
+            for (i, _), ws in list(kept.items()):
+                if i == index:
+                    flags |= ws.status(clear)
+        torch.cuda.synchronize()  # cleared before any stream's next call
+    return flags
+
+
+def _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, B, L, d, dev):
+    """The cmc_qk_prep of a call, by reference, or None for neither norm nor rotation."""
+    if rope_theta is None:
+        if q_weight is None and k_weight is None:
+            return None
+        rope_theta = 0.0
+    elif not rope_theta > 0:
+        raise ValueError("rope_theta must be positive")
+    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
+        if t is not None:
+            _need(t, name, _F32, 2, dev)
+            if t.shape != (L, d):
+                raise ValueError(f"{name} must be {(L, d)}")
+    if evicted is not None:
+        _need_evicted(evicted, B, dev)
+    return ctypes.byref(CmcQkPrep(0 if q_weight is None else q_weight.data_ptr(),
+                                  0 if k_weight is None else k_weight.data_ptr(),
+                                  0 if evicted is None else evicted.data_ptr(), rope_theta,
+                                  _offset(rope_offset), eps))
+
+
+def _need_evicted(evicted, B, dev) -> None:
+    _need(evicted, "evicted", torch.int64, 1, dev)
+    if evicted.shape[0] != B:
+        raise ValueError("evicted must be [B]")
+
+
+def _need_tokens(t, name, B, L, T, d, dev) -> Tuple[int, int]:
+    """Checks the heads of T tokens, bf16 [B, L, T, H, d] (or, with T = 1, [B, L, H, d]): (H, elements from one
+    token to the next).  Only a token's heads need be dense."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dtype is not torch.bfloat16 or t.device != dev:
+        _need(t, name, torch.bfloat16, 5, dev)
+    shape = t.shape if t.dim() == 5 else t.shape[:2] + (1,) + t.shape[2:]
+    if t.dim() not in (4, 5) or shape[:3] != (B, L, T) or shape[4] != d:
+        raise ValueError(f"{name} must be [{B}, {L}, {T}, heads, {d}], got shape {tuple(t.shape)}")
+    stride = t.stride() if t.dim() == 5 else t.stride()[:2] + (0,) + t.stride()[2:]
+    H = shape[3]
+    step = None  # from one token to the next: that of the innermost dimension with several
+    below = 1
+    for n, s in ((T, stride[2]), (L, stride[1]), (B, stride[0])):
+        if n > 1:
+            if step is None:
+                step = s // below if s % below == 0 else -1
+            if s != step * below:
+                step = -1
+                break
+            below *= n
+    if step is None:
+        step = H * d
+    if (d > 1 and stride[4] != 1) or (H > 1 and stride[3] != d) or step < H * d:
+        raise ValueError(f"{name}: a token's heads must be dense and tokens evenly spaced, got strides {t.stride()}")
+    return H, step
+
+
+def _tokens_like(t, shape, name, dev, given):
+    """The output of a call for heads of `shape`: the tensor given, checked, or a new one."""
+    if given is None:
+        return torch.empty(shape, dtype=torch.bfloat16, device=dev)
+    _need(given, name, torch.bfloat16, len(shape), dev)
+    if given.shape != shape:
+        raise ValueError(f"{name} must be {tuple(shape)}")
+    return given
+
+
+def _token_sizes(t, name) -> Tuple[int, int, int, int]:
+    """(B, L, T, d) of the heads of tokens, [B, L, T, H, d] or [B, L, H, d]."""
+    if not isinstance(t, torch.Tensor) or t.dim() not in (4, 5):
+        _need(t, name, torch.bfloat16, 5)
+    if t.dim() == 5:
+        B, L, T, _, d = t.shape
+    else:
+        (B, L, _, d), T = t.shape, 1
+    return B, L, T, d
+
+
+def _need_pos(pos, B, dev) -> None:
+    _need(pos, "pos", torch.int64, 1, dev)
+    if pos.shape[0] != B:
+        raise ValueError(f"pos shape {tuple(pos.shape)} does not match batch {B}")
+
+
+@_ranged
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, pos: torch.Tensor, *,
+                 q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                 eps: float = 1e-6, rope_theta: Optional[float] = None, rope_offset: int = 0,
+                 evicted: Optional[torch.Tensor] = None, out_q: Optional[torch.Tensor] = None,
+                 out_k: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """RMS norm (where gains q_weight, k_weight fp32 [L, d] are given) and rotary embedding (where
+    rope_theta is) of query heads q [B, L, T, Hq, d] and key heads k [B, L, T, Hkv, d], or of one
+    token's [B, L, H, d], at positions rope_offset + evicted[b] + pos[b] + t; see cmc_qk_norm_rope.  q and k
+    may be parts of a projection's output.  Returns both, dense; out_q and out_k may be q and k."""
+    B, L, T, d = _token_sizes(q, "q")
+    dev = q.device
+    index = dev.index
+    if not isinstance(k, torch.Tensor):
+        _need(k, "k", torch.bfloat16, 5)
+    key = ("norm", q.shape, q.stride(), k.shape, k.stride())
+    kept = _shapes_cache.get(key)
+    if (kept is None or q.dtype is not torch.bfloat16 or k.dtype is not torch.bfloat16
+            or k.get_device() != index):
+        Hq, sq = _need_tokens(q, "q", B, L, T, d, dev)
+        Hkv, sk = _need_tokens(k, "k", B, L, T, d, dev)
+        dims = CmcDims(B, L, Hq, Hkv, d, 1, 0, 1)
+        kept = _kept(key, (sq, sk, ctypes.byref(dims), dims))
+    sq, sk, dims, _ = kept
+    _need_pos(pos, B, dev)
+    prep = _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, B, L, d, dev)
+    out_q = _tokens_like(q, q.shape, "out_q", dev, out_q)
+    out_k = _tokens_like(k, k.shape, "out_k", dev, out_k)
+    fn = lib().cmc_qk_norm_rope
+    args = (q.data_ptr(), sq, k.data_ptr(), sk, T, pos.data_ptr(), dims, prep, out_q.data_ptr(),
+            out_k.data_ptr(), _raw_stream(index))
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_qk_norm_rope")
+    return out_q, out_k
+
+
+@_ranged
+def window_prefill(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, ring_k: torch.Tensor,
+                   ring_v: torch.Tensor, pos: torch.Tensor, *,
+                   ring_weight: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None,
+                   q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                   eps: float = 1e-6, rope_theta: Optional[float] = None, rope_offset: int = 0,
+                   evicted: Optional[torch.Tensor] = None, out_q: Optional[torch.Tensor] = None,
+                   workspace: Optional[DecodeWorkspace] = None) -> Optional[torch.Tensor]:
+    """Appends the first count[b] (int64 [B]; None: all) of T tokens k, v [B, L, T, Hkv, d] to the ring, in place, after the
+    norm and rotation of :func:`qk_norm_rope`, and returns the queries q [B, L, T, Hq, d] likewise (None: no
+    queries); see cmc_window_prefill.  The weights of the slots written become 0.  Rows of the queries from count[b]
+    on are not written (of a new tensor they are undefined)."""
+    B, L, T, d = _token_sizes(k, "k")
+    dev = k.device
+    index = dev.index
+    if not isinstance(v, torch.Tensor) or not isinstance(ring_k, torch.Tensor):
+        _need(v, "v", torch.bfloat16, 5)
+        _need(ring_k, "ring_k", torch.bfloat16, 5)
+    if q is not None and not isinstance(q, torch.Tensor):
+        _need(q, "q", torch.bfloat16, 5)
+    key = ("prefill", None if q is None else q.shape, None if q is None else q.stride(), k.shape, k.stride(),
+           v.shape, v.stride(), ring_k.shape)
+    kept = _shapes_cache.get(key)
+    if (kept is None or k.dtype is not torch.bfloat16 or v.dtype is not torch.bfloat16
+            or v.get_device() != index
+            or (q is not None and (q.dtype is not torch.bfloat16 or q.get_device() != index))):
+        Hkv, sk = _need_tokens(k, "k", B, L, T, d, dev)
+        Hv, sv = _need_tokens(v, "v", B, L, T, d, dev)
+        if Hv != Hkv:
+            raise ValueError("v must have the heads of k")
+        Hq, sq = (Hkv, 0) if q is None else _need_tokens(q, "q", B, L, T, d, dev)
+        _need(ring_k, "ring_k", torch.bfloat16, 5, dev)
+        W = ring_k.shape[3]
+        if ring_k.shape != (B, L, Hkv, W, d):
+            raise ValueError(f"ring_k must be {(B, L, Hkv, W, d)}, got shape {tuple(ring_k.shape)}")
+        dims = CmcDims(B, L, Hq, Hkv, d, 1, 0, W)
+        own = CmcDims(B, 1, 1, 1, 64, 1, 0, 1)  # a workspace that goes by the batch size alone
+        kept = _kept(key, (sq, sk, sv, ctypes.byref(dims), own, _kept_workspaces(own), dims))
+    sq, sk, sv, ref, own, workspaces, _ = kept
+    _need(ring_k, "ring_k", torch.bfloat16, 5, dev)
+    _need(ring_v, "ring_v", torch.bfloat16, 5, dev)
+    if ring_v.shape != ring_k.shape:
+        raise ValueError("ring_v must have the shape of ring_k")
+    _need_pos(pos, B, dev)
+    if ring_weight is not None:
+        _need_weight(ring_weight, "ring_weight", ring_k, dev)
+    if count is not None:
+        _need(count, "count", torch.int64, 1, dev)
+        if count.shape[0] != B:
+            raise ValueError("count must be [B]")
+    prep = _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, B, L, d, dev)
+    if q is not None:
+        out_q = _tokens_like(q, q.shape, "out_q", dev, out_q)
+    elif out_q is not None:
+        raise ValueError("out_q without q")
+    stream = _raw_stream(index)
+    if workspace is None:
+        workspace = _own_workspace(workspaces, index, stream, own)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
+    fn = lib().cmc_window_prefill
+    args = (_p(q), sq, k.data_ptr(), sk, v.data_ptr(), sv, T, ring_k.data_ptr(), ring_v.data_ptr(),
+            _p(ring_weight), pos.data_ptr(), _p(count), ref, prep, _p(out_q), workspace.ptr,
+            workspace.nbytes, stream)
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_window_prefill")
+    return out_q
+
+
+def _need_weight(weight, name, rows, dev) -> None:
+    """Checks the weights that go with rows [B, L, Hkv, T, d]."""
+    _need(weight, name, _F32, 4, dev)
+    if weight.shape != rows.shape[:4]:
+        raise ValueError(f"{name} must be {tuple(rows.shape[:4])}, got shape {tuple(weight.shape)}")
+
+
+def _weighted_kept(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, new, key) -> Tuple:
+    """Checks the tensors of a weighted attention call one by one; what the call keeps for shapes like
+    these: (dims by reference, dims, the workspaces by device and stream)."""
+    _need(q, "q", torch.bfloat16, 4)
+    dev = q.device
+    B, L, Hq, d = q.shape
+    for t, name in ((ring_k, "ring_k"), (ring_v, "ring_v")):
+        _need(t, name, torch.bfloat16, 5, dev)
+    Hkv, W = ring_k.shape[2], ring_k.shape[3]
+    if ring_k.shape != (B, L, Hkv, W, d) or ring_v.shape != ring_k.shape:
+        raise ValueError(f"inconsistent shapes: q {tuple(q.shape)}, ring {tuple(ring_k.shape)}, "
+                         f"{tuple(ring_v.shape)}")
+    _need_weight(ring_weight, "ring_weight", ring_k, dev)
+    k = 0
+    if tier1_k is not None or tier1_v is not None or tier1_weight is not None:
+        for t, name in ((tier1_k, "tier1_k"), (tier1_v, "tier1_v")):
+            _need(t, name, torch.bfloat16, 5, dev)
+        k = tier1_k.shape[3]
+        if tier1_k.shape != (B, L, Hkv, k, d) or tier1_v.shape != tier1_k.shape:
+            raise ValueError(f"inconsistent shapes: q {tuple(q.shape)}, tier1 {tuple(tier1_k.shape)}, "
+                             f"{tuple(tier1_v.shape)}")
+        _need_weight(tier1_weight, "tier1_weight", tier1_k, dev)
+    _need_pos(pos, B, dev)
+    if new is not None:
+        _need_new(*new, (B, L, Hkv, d), dev)
+    dims = CmcDims(B, L, Hq, Hkv, d, max(k, 1), k, W)
+    if decode_attn_weighted_workspace_size(dims) == 0:
+        raise ValueError(f"unsupported dims {dims.key()}")
+    kept = (ctypes.byref(dims), dims, _kept_workspaces(dims))
+    return kept if key is None else _kept(key, kept)
+
+
+def _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, new):
+    """Checks of a weighted attention call, most of them once for each combination of shapes."""
+    kept, key = None, None
+    try:
+        index = q.get_device()
+        k_new, v_new = (None, None) if new is None else new
+        if (index >= 0 and _as(torch.bfloat16, index, q, tier1_k, tier1_v, ring_k, ring_v, k_new, v_new)
+                and _as(_F32, index, tier1_weight, ring_weight) and _as(torch.int64, index, pos)):
+            key = ("weighted", q.shape, None if tier1_k is None else tier1_k.shape,
+                   None if tier1_v is None else tier1_v.shape,
+                   None if tier1_weight is None else tier1_weight.shape, ring_k.shape, ring_v.shape,
+                   ring_weight.shape, pos.shape, None if new is None else (k_new.shape, v_new.shape))
+            kept = _shapes_cache.get(key)
+    except AttributeError:
+        pass
+    if kept is None:
+        kept = _weighted_kept(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, new, key)
+    return kept
+
+
+@_ranged
+def two_tier_decode_attn_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, *,
+                                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                                  workspace: Optional[DecodeWorkspace] = None) -> torch.Tensor:
+    """Decode attention over [Tier-1 | occupied ring slots] (tier1_* None: the ring alone) that adds to each
+    key's weight, in place, the probabilities that its KV head's queries gave it; see
+    cmc_two_tier_decode_attn_weighted.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a DecodeWorkspace(dims,
+    device, weighted=True); without one the call keeps one per stream (see :func:`weighted_cache_status`), and a
+    captured call gets one of its own, zero-filled at every replay."""
+    ref, dims, workspaces = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight,
+                                           pos, None)
+    index = q.get_device()
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_out(out, q)
+    stream = _raw_stream(index)
+    if workspace is None:
+        workspace = _own_workspace(workspaces, index, stream, dims)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
+    fn = lib().cmc_two_tier_decode_attn_weighted
+    args = (q.data_ptr(), _p(tier1_k), _p(tier1_v), _p(tier1_weight), ring_k.data_ptr(), ring_v.data_ptr(),
+            ring_weight.data_ptr(), pos.data_ptr(), ref, 0.0 if scale is None else scale, out.data_ptr(),
+            workspace.ptr, workspace.nbytes, stream)
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_two_tier_decode_attn_weighted")
+    return out
+
+
+@_ranged
+def decode_step_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, k_new, v_new, *,
+                         scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                         workspace: Optional[DecodeWorkspace] = None,
+                         q_weight: Optional[torch.Tensor] = None,
+                         k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                         rope_theta: Optional[float] = None, rope_offset: int = 0,
+                         evicted: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Fused decode step with weights: append (k_new, v_new), whose weight starts at 0, then attend as
+    :func:`two_tier_decode_attn_weighted`; see cmc_decode_step_weighted.  Updates ring_k, ring_v, pos and the
+    weights in place.  With q_weight, k_weight or rope_theta, q and k_new are given before the norm and
+    rotation of :func:`qk_norm_rope`, at position rope_offset + evicted[b] + pos[b]."""
+    ref, dims, workspaces = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight,
+                                           pos, (k_new, v_new))
+    index = q.get_device()
+    prep = _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, dims.B, dims.L, dims.d, q.device)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _check_out(out, q)
+    stream = _raw_stream(index)
+    if workspace is None:
+        workspace = _own_workspace(workspaces, index, stream, dims)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
+    fn = lib().cmc_decode_step_weighted
+    args = (q.data_ptr(), _p(tier1_k), _p(tier1_v), _p(tier1_weight), ring_k.data_ptr(), ring_v.data_ptr(),
+            ring_weight.data_ptr(), pos.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ref,
+            0.0 if scale is None else scale, prep, out.data_ptr(), workspace.ptr, workspace.nbytes, stream)
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_decode_step_weighted")
+    return out
+
+
+def decode_attn_weighted_plan(dims: CmcDims, fused: bool = True) -> int:
+    """Grid size of the weighted attention (always one kernel); see cmc_decode_attn_weighted_plan."""
+    ctas = ctypes.c_int(0)
+    check(lib().cmc_decode_attn_weighted_plan(ctypes.byref(dims), 1 if fused else 0, ctypes.byref(ctas)),
+          "cmc_decode_attn_weighted_plan")
+    return int(ctas.value)
+
+
+@_ranged
+def evict_cache(k: torch.Tensor, v: torch.Tensor, weight: torch.Tensor, keep: int, *,
+                pos: Optional[torch.Tensor] = None, recent: int = 0,
+                evicted: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None,
+                out_v: Optional[torch.Tensor] = None, out_weight: Optional[torch.Tensor] = None,
+                out_pos: Optional[torch.Tensor] = None, workspace: Optional[DecodeWorkspace] = None
+                ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Keeps, of the tokens of a cache k, v [B, L, Hkv, T, d] (all T rows, or with ``pos`` a ring's), the ``recent``
+    youngest and the heaviest others, ``keep`` in all for every unit, moved together in order of age; see
+    cmc_evict_cache.  Returns (k, v, weight, idx, pos): the cache, by default new tensors of ``keep`` rows (rows that
+    no token is kept for are not written), the rows kept, int32 [B, L, Hkv, keep] then -1, and the tokens
+    that each sequence holds now, int64 [B].  ``out_k``, ``out_v``, ``out_weight`` may be larger than ``keep`` rows,
+    or k, v and weight themselves (a ring that has not wrapped, or ends at its last row); ``out_pos`` may be
+    pos.  ``evicted`` (int64 [B]) grows by the tokens taken out."""
+    _need(k, "k", torch.bfloat16, 5)
+    dev = k.device
+    index = dev.index
+    _need(v, "v", torch.bfloat16, 5, dev)
+    if v.shape != k.shape:
+        raise ValueError("v must have the shape of k")
+    _need_weight(weight, "weight", k, dev)
+    B, L, Hkv, T, d = k.shape
+    keep, recent = _int32(int(keep)), _int32(int(recent))
+    if not 1 <= keep <= T:
+        keep = -1  # refused by the library
+    if pos is not None:
+        _need_pos(pos, B, dev)
+    if evicted is not None:
+        _need_evicted(evicted, B, dev)
+    given = [t for t in (out_k, out_v, out_weight) if t is not None]
+    rows = max(keep, 1)
+    if given:
+        rows = given[0].shape[3] if isinstance(given[0], torch.Tensor) and given[0].dim() in (4, 5) else rows
+    want = (B, L, Hkv, rows, d)
+    if out_k is None:
+        out_k = torch.empty(want, dtype=torch.bfloat16, device=dev)
+    if out_v is None:
+        out_v = torch.empty(want, dtype=torch.bfloat16, device=dev)
+    if out_weight is None:
+        out_weight = torch.empty(want[:4], dtype=_F32, device=dev)
+    if given:
+        for t, name in ((out_k, "out_k"), (out_v, "out_v")):
+            _need(t, name, torch.bfloat16, 5, dev)
+            if t.shape != want:
+                raise ValueError(f"{name} must be {want}")
+        _need_weight(out_weight, "out_weight", out_k, dev)
+    idx = torch.empty((B, L, Hkv, max(keep, 0)), dtype=torch.int32, device=dev)
+    if out_pos is None:
+        out_pos = torch.empty(B, dtype=torch.int64, device=dev)
+    else:
+        _need(out_pos, "out_pos", torch.int64, 1, dev)
+        if out_pos.shape[0] != B:
+            raise ValueError("out_pos must be [B]")
+    key = ("evict", k.shape, rows, keep)
+    kept = _shapes_cache.get(key)
+    if kept is None:
+        dims = CmcDims(B, L, Hkv, Hkv, d, T, keep, rows)
+        own = CmcDims(B, 1, 1, 1, 64, 1, 0, 1)  # a workspace that goes by the batch size alone
+        kept = _kept(key, (ctypes.byref(dims), own, _kept_workspaces(own), dims))
+    ref, own, workspaces, _ = kept
+    stream = _raw_stream(index)
+    if workspace is None:
+        workspace = _own_workspace(workspaces, index, stream, own)
+    elif workspace.index != index:
+        raise _elsewhere_workspace(workspace, index)
+    fn = lib().cmc_evict_cache
+    args = (k.data_ptr(), v.data_ptr(), weight.data_ptr(), _p(pos), ref, recent, out_k.data_ptr(),
+            out_v.data_ptr(), out_weight.data_ptr(), idx.data_ptr(), out_pos.data_ptr(), _p(evicted),
+            workspace.ptr, workspace.nbytes, stream)
+    st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)
+    if st:
+        check(st, "cmc_evict_cache")
+    return out_k, out_v, out_weight, idx, out_pos
 
 
 # ----------------------------------------------------------------------------

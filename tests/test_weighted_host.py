@@ -1,0 +1,269 @@
+"""The cache with weights on the host: pins of its oracle, and the refusals of its entry points."""
+
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_25537_gb300 as cmc
+from oracle import weighted as ow
+from paper_2609_25537_gb300.build import build
+from paper_2609_25537_gb300._lib import CmcQkPrep
+
+OK, NULL, SHAPE, RANGE, ALIGN, WORKSPACE = 0, 1, 2, 3, 4, 5
+FAKE = 0x10000  # 16-byte aligned, never dereferenced: these calls fail before any launch
+BIG = 1 << 40
+
+host_only = pytest.mark.skipif(torch.cuda.is_available(),
+                               reason="fake-pointer argument checks run only without a GPU")
+
+
+@pytest.fixture(scope="module")
+def L():
+    build()
+    return cmc.lib()
+
+
+# ---- pins of the oracle ----
+
+def test_bf16_rounding_is_torchs():
+    rng = np.random.default_rng(0)
+    x = (rng.standard_normal(4000) * 2.0 ** rng.integers(-140, 60, 4000)).astype(np.float32)
+    x = np.concatenate([x, np.float32([0.0, 1.00390625, 1.01171875, 2.0 ** -133, 1.5 * 2.0 ** -133])])
+    want = torch.from_numpy(x).to(torch.bfloat16).to(torch.float64).numpy()
+    np.testing.assert_array_equal(ow.to_bf16(x), want)
+
+
+def test_norm_closed_forms():
+    x = np.array([[3.0, 4.0, 0.0, 0.0]])
+    np.testing.assert_allclose(ow.heads(x, np.ones(4), eps=0.0), x / 2.5)
+    np.testing.assert_allclose(ow.heads(x, np.array([1.0, 2.0, 3.0, 4.0]), eps=0.0), [[1.2, 3.2, 0.0, 0.0]])
+    np.testing.assert_allclose(ow.heads(np.zeros((1, 4)), np.ones(4)), 0.0)
+    x = np.random.default_rng(0).standard_normal((5, 3, 64))
+    want = torch.nn.functional.rms_norm(torch.from_numpy(x), (64,), eps=1e-6).numpy()
+    np.testing.assert_allclose(ow.heads(x, np.ones((5, 64))), want, rtol=1e-12)
+
+
+def test_rotation_is_a_complex_product():
+    rng = np.random.default_rng(1)
+    x, p = rng.standard_normal((6, 2, 64)), np.array([0, 1, -5, 1000, 123456, 2 ** 31])
+    got = ow.heads(x, theta=1e4, p=p)
+    for n, at in enumerate(p):
+        for i in range(32):
+            z = (x[n, :, i] + 1j * x[n, :, i + 32]) * np.exp(1j * (float(at) * 1e4 ** (-i / 32)))
+            # the angle itself is rounded in this form: at * 2^-52
+            tol = 1e-12 + abs(float(at)) * 2.0 ** -50
+            np.testing.assert_allclose(got[n, :, i], z.real, atol=tol * 4)
+            np.testing.assert_allclose(got[n, :, i + 32], z.imag, atol=tol * 4)
+    np.testing.assert_allclose(got[0], x[0])
+
+
+def test_prefill_is_a_run_of_appends():
+    k = np.arange(6.0).reshape(1, 1, 6, 1, 1)
+    ring, ringv, w, pos = np.zeros((1, 1, 1, 4, 1)), np.zeros((1, 1, 1, 4, 1)), np.ones((1, 1, 1, 4)), np.array([3])
+    ow.prefill(k, -k, ring, ringv, w, pos, np.array([6]))
+    assert pos[0] == 9 and not w.any()  # tokens 2 .. 5 are numbers 5 .. 8
+    np.testing.assert_array_equal(ring.ravel(), [5, 2, 3, 4])
+    np.testing.assert_array_equal(ringv.ravel(), [-5, -2, -3, -4])
+    w[:] = 1
+    ow.prefill(k, k, ring, ringv, w, pos, np.array([2]))
+    np.testing.assert_array_equal(ring.ravel(), [5, 0, 1, 4])
+    np.testing.assert_array_equal(w.ravel(), [1, 0, 0, 1])
+
+
+def test_weights_grow_by_one_per_query():
+    rng = np.random.default_rng(2)
+    q = rng.standard_normal((2, 1, 4, 8))
+    t1 = [rng.standard_normal((2, 1, 2, 3, 8)) for _ in range(2)] + [np.zeros((2, 1, 2, 3))]
+    ring = [rng.standard_normal((2, 1, 2, 5, 8)) for _ in range(2)] + [np.zeros((2, 1, 2, 5))]
+    out, _, _, _ = ow.attend(q, t1, ring, np.array([2, 9]), 0.3)
+    np.testing.assert_allclose(t1[2].sum(-1) + ring[2].sum(-1), 2.0)
+    assert not ring[2][0, ..., 2:].any()
+    k = torch.from_numpy(np.concatenate([t1[0], ring[0]], axis=3))[1, 0].repeat_interleave(2, 0)
+    v = torch.from_numpy(np.concatenate([t1[1], ring[1]], axis=3))[1, 0].repeat_interleave(2, 0)
+    want = torch.nn.functional.scaled_dot_product_attention(torch.from_numpy(q[1, 0])[:, None], k, v, scale=0.3)
+    np.testing.assert_allclose(out[1, 0], want[:, 0].numpy(), rtol=1e-12)
+
+
+def test_eviction_by_hand():
+    w = np.float32([[[[5, 1, 4, 1, 3]]]])
+    idx, held = ow.evict(w, 3)
+    assert idx.ravel().tolist() == [0, 2, 4] and held.tolist() == [3]
+    assert ow.evict(w, 4)[0].ravel().tolist() == [0, 1, 2, 4]  # equal weights: the older
+    assert ow.evict(w, 3, recent=2)[0].ravel().tolist() == [0, 3, 4]
+    assert ow.evict(w, 3, recent=2, pos=np.array([4]))[0].ravel().tolist() == [0, 2, 3]
+    assert ow.evict(w, 3, pos=np.array([2]))[0].ravel().tolist() == [0, 1, -1]
+    # wrapped: tokens 2 .. 6 in rows 2, 3, 4, 0, 1
+    assert ow.evict(w, 3, recent=1, pos=np.array([7]))[0].ravel().tolist() == [2, 0, 1]
+    assert ow.evict(w, 2, pos=np.array([7]))[0].ravel().tolist() == [2, 0]
+    assert ow.evict(np.float32([[[[np.nan, -np.inf, -0.0, 0.0]]]]), 2)[0].ravel().tolist() == [2, 3]
+    assert ow.evict(np.float32([[[[np.nan, -np.inf, -0.0, 0.0]]]]), 3)[0].ravel().tolist() == [1, 2, 3]
+
+
+# ---- refusals ----
+
+def _dims(**kw):
+    base = dict(B=2, L=3, Hq=8, Hkv=2, d=128, N=100, k=10, W=16)
+    base.update(kw)
+    return ctypes.byref(cmc.CmcDims(*(base[f] for f, _ in cmc.CmcDims._fields_)))
+
+
+def test_workspace_sizes(L):
+    # a 256-byte status header, 8 bytes per sequence padded to 256
+    assert L.cmc_cache_workspace_size(2) == 512 and L.cmc_cache_workspace_size(40) == 768
+    assert L.cmc_cache_workspace_size(0) == L.cmc_cache_workspace_size(65536) == 0
+
+    def f(**kw):
+        return L.cmc_decode_attn_weighted_workspace_size(_dims(**kw))
+    assert f() == f(L=65, k=100, W=5000, d=64) == 512
+    assert f(d=96) == 0 and f(Hq=6) == 0 and f(k=101) == 0
+    # G = 4: 36,864 keys fit a cluster's shared memory; beyond, 4 G bytes a key, rounded up to 128 keys a CTA
+    assert f(k=0, W=36864) == 512
+    assert f(k=0, W=36865) == 512 + 2 * 3 * 2 * 8 * 37 * 128 * 16
+
+
+def _prep(**kw):
+    base = dict(q_weight=0, k_weight=0, evicted=0, rope_theta=1e4, rope_offset=0, eps=1e-6)
+    base.update(kw)
+    return ctypes.byref(CmcQkPrep(**base))
+
+
+def _norm(L, q=FAKE, qs=1024, k=FAKE, ks=256, T=4, pos=FAKE, dims=None, prep=None, oq=FAKE, ok=FAKE):
+    return L.cmc_qk_norm_rope(q, qs, k, ks, T, pos, dims or _dims(), prep, oq, ok, None)
+
+
+@host_only
+def test_norm_argument_checks(L):
+    assert _norm(L, T=0) == OK  # nothing to do
+    assert _norm(L, T=-1) == SHAPE
+    assert _norm(L, T=(1 << 24) + 1) == SHAPE
+    assert _norm(L, T=1 << 24, dims=_dims(L=8)) == SHAPE
+    for name in ("q", "k", "pos", "oq", "ok"):
+        assert _norm(L, **{name: 0}) == NULL
+        assert _norm(L, **{name: FAKE + 4}) == ALIGN
+    assert _norm(L, dims=_dims(d=96)) == SHAPE
+    assert _norm(L, dims=_dims(Hq=6)) == SHAPE
+    assert _norm(L, qs=1016) == SHAPE and _norm(L, ks=248) == SHAPE and _norm(L, qs=-1024) == SHAPE
+    assert _norm(L, qs=1028) == ALIGN and _norm(L, ks=260) == ALIGN
+    for theta in (-1.0, float("inf"), float("nan")):
+        assert _norm(L, prep=_prep(rope_theta=theta)) == RANGE
+    for offset in (-1, (1 << 32) + 1):
+        assert _norm(L, prep=_prep(rope_offset=offset)) == RANGE
+    for eps in (-1.0, float("inf"), float("nan")):
+        assert _norm(L, prep=_prep(q_weight=FAKE, eps=eps)) == RANGE
+        assert _norm(L, prep=_prep(k_weight=FAKE, eps=eps)) == RANGE
+    assert _norm(L, prep=_prep(q_weight=FAKE + 4)) == ALIGN
+    assert _norm(L, prep=_prep(k_weight=FAKE + 4)) == ALIGN
+    assert _norm(L, prep=_prep(evicted=FAKE + 4)) == ALIGN
+    assert L.cmc_qk_norm_rope(FAKE, 1024, FAKE, 256, 4, FAKE, None, None, FAKE, FAKE, None) == NULL
+
+
+def _prefill(L, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, T=4, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE,
+             count=FAKE, dims=None, prep=None, oq=FAKE, ws=FAKE, wsb=512):
+    return L.cmc_window_prefill(q, qs, k, ks, v, vs, T, rk, rv, rw, pos, count, dims or _dims(), prep, oq, ws,
+                                wsb, None)
+
+
+@host_only
+def test_prefill_argument_checks(L):
+    assert _prefill(L, T=0) == OK
+    assert _prefill(L, T=0, q=0, oq=0, rw=0, count=0) == OK
+    for name in ("k", "v", "rk", "rv", "pos", "oq"):
+        assert _prefill(L, **{name: 0}) == NULL
+    for name in ("q", "k", "v", "rk", "rv", "pos", "oq", "count", "ws"):
+        assert _prefill(L, **{name: FAKE + 4}) == ALIGN
+    assert _prefill(L, rw=FAKE + 2) == ALIGN
+    assert _prefill(L, dims=_dims(W=0)) == SHAPE
+    assert _prefill(L, vs=248) == SHAPE and _prefill(L, vs=260) == ALIGN
+    assert _prefill(L, ws=0) == WORKSPACE and _prefill(L, wsb=511) == WORKSPACE
+    assert _prefill(L, prep=_prep(rope_theta=-1.0)) == RANGE
+
+
+def _attend(L, q=FAKE, tk=FAKE, tv=FAKE, tw=FAKE, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE, dims=None, out=FAKE,
+            ws=FAKE, wsb=512):
+    return L.cmc_two_tier_decode_attn_weighted(q, tk, tv, tw, rk, rv, rw, pos, dims or _dims(), 0.0, out, ws,
+                                               wsb, None)
+
+
+def _step(L, q=FAKE, tk=FAKE, tv=FAKE, tw=FAKE, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE, kn=FAKE, vn=FAKE, dims=None,
+          prep=None, out=FAKE, ws=FAKE, wsb=512):
+    return L.cmc_decode_step_weighted(q, tk, tv, tw, rk, rv, rw, pos, kn, vn, dims or _dims(), 0.0, prep, out, ws,
+                                      wsb, None)
+
+
+@host_only
+@pytest.mark.parametrize("call", [_attend, _step])
+def test_weighted_attention_argument_checks(L, call):
+    names = ["q", "tk", "tv", "tw", "rk", "rv", "rw", "pos", "out"] + (["kn", "vn"] if call is _step else [])
+    for name in names:
+        assert call(L, **{name: 0}) == NULL
+        assert call(L, **{name: FAKE + 2}) == ALIGN
+    assert call(L, dims=_dims(k=0), tk=0, tv=0, tw=0, ws=0) == WORKSPACE  # none of Tier-1 is looked at
+    assert call(L, ws=0) == WORKSPACE and call(L, wsb=511) == WORKSPACE and call(L, ws=FAKE + 8) == ALIGN
+    assert call(L, dims=_dims(k=101)) == RANGE
+    for bad in (dict(B=0), dict(d=32), dict(Hq=6), dict(Hq=32), dict(W=0), dict(N=0, k=0)):
+        assert call(L, dims=_dims(**bad)) == SHAPE
+    assert call(L, dims=_dims(W=40000), wsb=512) == WORKSPACE
+
+
+@host_only
+def test_step_prep_checks(L):
+    assert _step(L, prep=_prep(rope_theta=float("nan"))) == RANGE
+    assert _step(L, prep=_prep(rope_offset=-1)) == RANGE
+    assert _step(L, prep=_prep(q_weight=FAKE, eps=-1.0)) == RANGE
+    assert _step(L, prep=_prep(evicted=FAKE + 2)) == ALIGN
+
+
+def _evict(L, k=BIG, v=2 * BIG, w=3 * BIG, pos=0, dims=None, recent=0, ok=4 * BIG, ov=5 * BIG, ow=6 * BIG, idx=7 * BIG,
+           op=0, ev=0, ws=FAKE, wsb=512):
+    return L.cmc_evict_cache(k, v, w, pos, dims or _dims(), recent, ok, ov, ow, idx, op, ev, ws, wsb, None)
+
+
+@host_only
+def test_evict_argument_checks(L):
+    for name in ("k", "v", "w", "ok", "ov", "ow", "idx"):
+        assert _evict(L, **{name: 0}) == NULL
+    for name in ("k", "v", "ok", "ov", "ws"):
+        assert _evict(L, **{name: FAKE + 8}) == ALIGN
+    for name in ("w", "ow", "idx"):
+        assert _evict(L, **{name: FAKE + 2}) == ALIGN
+    for name in ("pos", "op", "ev"):
+        assert _evict(L, **{name: FAKE + 4}) == ALIGN
+    for bad in (dict(k=0), dict(k=101), dict(W=9), dict(k=-1)):
+        assert _evict(L, dims=_dims(**bad)) == RANGE
+    assert _evict(L, recent=-1) == RANGE and _evict(L, recent=11) == RANGE
+    assert _evict(L, dims=_dims(d=96)) == SHAPE and _evict(L, dims=_dims(N=0, k=0)) == SHAPE
+    assert _evict(L, ws=0) == WORKSPACE and _evict(L, wsb=511) == WORKSPACE
+    # in place: all three or none, and as many rows
+    assert _evict(L, ok=BIG) == RANGE and _evict(L, ov=2 * BIG) == RANGE and _evict(L, ow=3 * BIG) == RANGE
+    assert _evict(L, ok=BIG, ov=2 * BIG, ow=3 * BIG) == RANGE  # W != N
+    # part of the input
+    assert _evict(L, ok=BIG + 256) == RANGE and _evict(L, ow=3 * BIG + 4) == RANGE and _evict(L, ov=BIG + 512) == RANGE
+
+
+@host_only
+def test_plan_argument_checks(L):
+    assert L.cmc_decode_attn_weighted_plan(None, 1, ctypes.byref(ctypes.c_int())) == NULL
+    assert L.cmc_decode_attn_weighted_plan(_dims(), 1, None) == NULL
+    assert L.cmc_decode_attn_weighted_plan(_dims(d=32), 0, ctypes.byref(ctypes.c_int())) == SHAPE
+
+
+def test_tensors_on_the_host_are_refused(L):
+    x = torch.zeros(1, 1, 2, 4, 64, dtype=torch.bfloat16)
+    w, pos = torch.zeros(1, 1, 2, 4), torch.zeros(1, dtype=torch.int64)
+    q = torch.zeros(1, 1, 4, 64, dtype=torch.bfloat16)
+    row = q[:, :, :2].contiguous()
+    for call in (lambda: cmc.qk_norm_rope(q, row, pos), lambda: cmc.window_prefill(q, row, row, x, x, pos),
+                 lambda: cmc.two_tier_decode_attn_weighted(q, None, None, None, x, x, w, pos),
+                 lambda: cmc.decode_step_weighted(q, x, x, w, x, x, w, pos, row, row),
+                 lambda: cmc.evict_cache(x, x, w, 2)):
+        with pytest.raises(ValueError, match="CUDA tensor"):
+            call()
+    for call in (lambda: cmc.qk_norm_rope(None, row, pos), lambda: cmc.qk_norm_rope(q, "k", pos),
+                 lambda: cmc.window_prefill(q, None, row, x, x, pos),
+                 lambda: cmc.window_prefill(q, row, 3, x, x, pos),
+                 lambda: cmc.two_tier_decode_attn_weighted(None, None, None, None, x, x, w, pos),
+                 lambda: cmc.evict_cache([1], x, w, 2)):
+        with pytest.raises(TypeError):
+            call()
