@@ -665,9 +665,9 @@ CMC_API int cmc_window_prefill(const void* q, int64_t q_stride, const void* k, i
                                void* workspace, size_t workspace_bytes, void* stream);
 
 /* Bytes of workspace the two calls below need for `dims`: the device status word, one 8-byte counter per
- * sequence and, for units too long for a cluster's shared memory (from 147,456 / G keys on, G = Hq / Hkv),
- * 4 G bytes a key.  Zero-fill it once before its first use; every call leaves the
- * counters at zero. */
+ * sequence and, for units that may be too long for a cluster's shared memory (more than 46,080, 30,720, 18,432 or 9,216
+ * keys with Hq / Hkv = 1, 2, 4 or 8), 4 (Hq / Hkv + 1) bytes a key.  Zero-fill it once before its first use; every
+ * call leaves the counters at zero. */
 CMC_API size_t cmc_decode_attn_weighted_workspace_size(const cmc_dims* dims);
 
 /*

@@ -3,29 +3,28 @@
 //   out[h]    = sum_j p_hj v_j,   p_hj = 2^(s_hj - M_h) / l_h,   s = scale log2(e) q_h . k_j
 //   weight[j] += sum of p_hj over the G query heads of the KV head
 // The probabilities need the final maximum M and sum l, which one pass over the keys knows only at its
-// end.  So each CTA keeps the products q . k of its keys in shared memory (4 G bytes a key, beside the key's 4 d bytes
-// in HBM), and when its unit's M and l are known goes over them once more.
+// end.  So each CTA keeps the products q . k of its keys, and their weights, in shared memory (4 G + 4 bytes a key,
+// beside the key's 4 d bytes in HBM), and when its unit's M and l are known goes over them once more.
 //
 // Bound: HBM, 4 d + 8 bytes a key against 4 G d flops.  A unit (sequence, layer, KV head) is taken by a CTA of
-// eight warps or a cluster of up to eight CTAs; its keys are cut into blocks of 16, ceil(k / 16) of Tier-1, then those of
-// the ring's occupied slots, and warp w of the unit's 8 cm takes blocks w, w + 8 cm, ...
-//
-// K and V go from HBM straight to the registers that feed the products: no stage in shared memory, no
-// barrier, and rows that hold no key are simply not read.  With the products of cmc_attn.cu,
+// four warps, a cluster of up to eight such CTAs, or, where there are many short ones, by one warp.  Its keys are cut
+// into blocks of 32, ceil(k / 32) of Tier-1, then those of the ring's occupied slots, and warp w of the unit's n takes
+// blocks w, w + n, ...  The warps have nothing to do with each other until the end: each copies its own blocks' rows (cp.async,
+// 16 bytes a lane) into a stage of its own, K and V of one block, and requests the next block's K as soon as the products
+// have read this one's, its V likewise.  Rows that hold no token are not read, their places are filled with zeros.  Twelve
+// warps of 16 KB an SM keep enough on the way.  The two products are those of cmc_attn.cu,
 //   S^T = K Q^T     16 keys as the M rows, the G query heads (padded to 8) as the columns
-//   O^T += V^T P^T  16 rows of the head dimension, the heads, the 16 keys as the k-step
-// (mma.sync m16n8k16; 4 flops a byte: the tensor pipe is all but idle), the order of d within the first and of the
-// M rows of the second is free, and chosen so that 16-byte loads fill the fragments:
-//   K: lane (g, t) = (lane / 4, lane % 4) has chunk 4 i + t (elements 32 i + 8 t ..) of rows g and g + 8; its four words are
-//      the k pairs of steps 2 i and 2 i + 1, and Q's fragments are the same chunks of row g of Q.
-//   V: lane (g, t) has chunk 8 h + g of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9; words of two rows make pairs of keys (prmt), and
-//      row g / g + 8 of product 4 h + w is column 64 h + 8 g + 2 w / + 1.
-// The next block's K is requested when S^T has taken this one's, its V when O^T has.
+//   O^T += V^T P^T  16 rows of the head dimension, the heads, 16 keys as the k-step
+// (mma.sync m16n8k16, ldmatrix; 4 flops a byte: the tensor pipe is all but idle).
+//
+// What a warp does with a block is a chain of latencies, so that its length and the warps an SM holds set the rate, not the
+// bytes on the way: 32 layers of 128 + 512 keys, fused step with norm and rotation, 13.7 us (12.9 at the copy rate), with blocks of 16
+// keys fed from registers 17.7 (six warps a CTA) to 22.6, through private stages with two or three blocks on the way 21.6 to 30.
 //
 // The new token (fused step) is read from k_new and v_new where its slot's row would be, by the warp that has
-// the block, which stores it to the ring as well.  With norm or rotary embedding two warps first
-// prepare q and the new key; q is then held as the sum of two bf16 (products off by 2^-17 of a term: the
-// probabilities are sums in fp32 that outlive the call), the key rounded to bf16 as it is stored.
+// the block, which stores it to the ring as well.  With norm or rotary embedding the warps first
+// prepare q and the new key, a row a warp, while their blocks are on the way; q is then held as the sum of two bf16 (products off
+// by 2^-16 of a term: the weights are sums in fp32 that outlive the call), the key rounded to bf16 as it is stored.
 #include <algorithm>
 #include <atomic>
 
@@ -33,12 +32,14 @@
 
 namespace cmc {
 
-constexpr int kWWarps = 8;
-constexpr int kWThreads = 32 * kWWarps;
-constexpr int kBlkKeys = 16;
-// Products that a CTA keeps in shared memory, in bytes; two CTAs share an SM at that.  Units too long for a cluster of
-// eight at that keep them in the workspace.
-constexpr int kScoreBytes = 73728;
+constexpr int kBlkKeys = 32;
+// Products and weights that a CTA keeps in shared memory, in bytes: as many as leave two CTAs of four warps on an SM.
+// Units too long for a cluster of eight at that keep them in the workspace (us a launch at 40 KB / 64 KB / 10 KB: 64 units of
+// 16,384 keys 79 / 98 / 103, of 20,480 keys 125 / 152 / 126), but where there is no more than a CTA an SM.
+constexpr int score_cap(int G) { return G == 8 ? 41472 : 46080; }
+constexpr int kScoreMost = 131072;
+// Blocks of a unit that is given to one warp, at most (see launch_weighted).
+constexpr int kSoloBlocks = 16;
 
 struct WeightedParams {
   const uint16_t* q;      // [B, L, Hq, d]
@@ -66,19 +67,20 @@ struct WeightedParams {
 
 __host__ __device__ constexpr int wrow_floats(int D) { return D + 4; }
 
-// Shared memory: Q as bf16 sums and the prepared key (with PREP), the warps' states, a cluster's record, then
-// the products.
-template <int D, int G, bool PREP>
+// Shared memory: the warps' stages (a block's K and V each), Q as bf16 sums and the prepared key (with PREP), the warps' maxima and
+// sums, a cluster's record, then the products.  At the end a warp's stage holds its output.
+template <int D, int G, bool PREP, int NW>
 struct WSmem {
-  static constexpr int kQ = 0;                                     // [2][8][D] bf16: high and low parts
-  static constexpr int kNew = kQ + (PREP ? 2 * 8 * D * 2 : 0);     // [D] bf16
-  static constexpr int kTab = kNew + (PREP ? D * 2 : 0);           // [2][D / 2] (cos, sin)
-  static constexpr int kM = kTab + (PREP ? 2 * D * 4 : 0);         // [warp][8] maxima, [warp][8] sums
-  static constexpr int kO = kM + kWWarps * 16 * 4;                 // [warp][G][wrow_floats(D)]
-  static constexpr int kRec = kO + kWWarps * G * wrow_floats(D) * 4;  // [G][D] output, [8][2] maximum and sum
-  static constexpr int kFin = kRec + (G * D + 16) * 4;             // [8] final maxima, [8] 1 / sums
+  static constexpr int kBlk = kBlkKeys * D * 4;                    // K and V of a block
+  static constexpr int kQ = NW * kBlk;                             // [2][G][D] bf16: high and low parts
+  static constexpr int kNew = kQ + (PREP ? 2 * G * D * 2 : 0);     // [D] bf16
+  static constexpr int kM = kNew + (PREP ? D * 2 : 0);             // [warp][8] maxima, [warp][8] sums
+  static constexpr int kRecMl = kM + NW * 16 * 4;                  // a cluster's record: [8][2] maxima and sums,
+  static constexpr int kRec = kBlk / 2;                            // and, in a stage when all are done, [G][D] output
+  static constexpr int kFin = kRecMl + 16 * 4;                     // [8] final maxima, [8] 1 / sums
   static constexpr int kScores = kFin + 16 * 4;
   static_assert(kScores % 16 == 0, "read by 16 bytes");
+  static_assert(G * wrow_floats(D) * 4 <= kBlk / 2 && G * D * 4 <= kBlk / 2, "a stage holds an output and a record");
 };
 
 __device__ __forceinline__ void wmma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
@@ -90,15 +92,28 @@ __device__ __forceinline__ void wmma(float (&c)[4], uint32_t a0, uint32_t a1, ui
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// A 16-byte load of what a launch reads once.
-__device__ __forceinline__ uint4 ld_once(const uint16_t* p, uint64_t policy) {
-  uint4 r;
-  asm volatile("ld.global.L1::no_allocate.L2::cache_hint.v4.u32 {%0,%1,%2,%3}, [%4], %5;\n"
-               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
-               : "l"(p), "l"(policy)
+// 16 bytes of what a launch reads once, or as many zeros, into shared memory.
+__device__ __forceinline__ void copy_once(uint32_t dst, const uint16_t* src, bool valid, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;\n" ::"r"(dst), "l"(src),
+               "r"(valid ? 16 : 0), "l"(policy)
                : "memory");
-  return r;
 }
+__device__ __forceinline__ void copy_once(uint32_t dst, const uint16_t* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;\n" ::"r"(dst), "l"(src),
+               "l"(policy)
+               : "memory");
+}
+__device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t& r0, uint32_t& r1, uint32_t& r2, uint32_t& r3) {
+  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];\n"
+               : "=r"(r0), "=r"(r1), "=r"(r2), "=r"(r3)
+               : "r"(addr)
+               : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
+
+// A maximum that differences are taken from: 0 where there is none (no key, or NaN alone: 2^x of
+// those is then 0 and NaN).
+__device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
 __device__ __forceinline__ float ld_peer_f32(uint32_t addr) {
   float v;
@@ -118,7 +133,8 @@ __device__ __forceinline__ float4 ld_peer_f4(uint32_t addr) {
 struct Blk {
   const uint16_t* k;
   const uint16_t* v;
-  int rows;     // 1 .. 16
+  float* w;
+  int rows;     // 1 .. 32
   int new_row;  // the new token's, or -1
 };
 
@@ -130,148 +146,160 @@ __device__ __forceinline__ Blk blk_of(const WeightedParams& p, long long u, int 
     const long long e = (u * p.N + blk * kBlkKeys) * D;
     r.k = p.t1k + e;
     r.v = p.t1v + e;
+    r.w = p.t1w + (u * p.N + blk * kBlkKeys);
     r.rows = min(p.k - blk * kBlkKeys, kBlkKeys);
   } else {
     const int s0 = (blk - p.nb1) * kBlkKeys;
     const long long e = (u * p.W + s0) * D;
     r.k = p.ring_k + e;
     r.v = p.ring_v + e;
+    r.w = p.ring_w + (u * p.W + s0);
     r.rows = min(count - s0, kBlkKeys);
     if (new_slot >= s0 && new_slot < s0 + kBlkKeys) r.new_row = new_slot - s0;
   }
   return r;
 }
 
-// K of a block: chunks 4 i + t of rows g and g + 8.  `newk`: the new token's row.
+// Offset of 16-byte chunk c of row r within K or V of a stage: columns of 128 bytes, the chunks of a row in the
+// order c ^ (r & 7), so that eight rows of a chunk lie in different banks.
 template <int D>
-__device__ __forceinline__ void load_k(const Blk& b, const uint16_t* newk, uint16_t* to, int g, int t,
-                                       uint64_t pol, uint4 (&kr)[2][D / 32]) {
-  if (b.rows == kBlkKeys && b.new_row < 0) {
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) kr[h][i] = ld_once(b.k + (g + 8 * h) * D + 32 * i + 8 * t, pol);
-    return;
-  }
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int row = g + 8 * h;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      const int c = 32 * i + 8 * t;
-      kr[h][i] = make_uint4(0u, 0u, 0u, 0u);
-      if (row == b.new_row) {
-        kr[h][i] = *reinterpret_cast<const uint4*>(newk + c);
-        *reinterpret_cast<uint4*>(to + c) = kr[h][i];
-      } else if (row < b.rows) {
-        kr[h][i] = ld_once(b.k + row * D + c, pol);
-      }
-    }
-  }
+__device__ __forceinline__ uint32_t swz(int r, int c) {
+  return static_cast<uint32_t>((c >> 3) * (kBlkKeys * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
 }
 
-// V of a block: chunks 8 h + g of rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9.
+// Requests the rows of K or of V of a block into a stage: eight lanes to 128 bytes of a row, four rows at a time.
+// Rows that hold no token are filled with zeros.  `fresh`: the new token's row, or NULL where it is put in later.
 template <int D>
-__device__ __forceinline__ void load_v(const Blk& b, const uint16_t* newv, uint16_t* to, int g, int t,
-                                       uint64_t pol, uint4 (&vr)[4][D / 64]) {
-  if (b.rows == kBlkKeys && b.new_row < 0) {
+__device__ __forceinline__ void request_rows(const uint16_t* base, int rows, int new_row, const uint16_t* fresh, int lane,
+                                             uint64_t pol, uint32_t to) {
+  const int sub = lane >> 3, c = lane & 7;
+  const uint16_t* src = base + sub * D + c * 8;
+  const uint32_t even = to + sub * 128 + ((c ^ sub) << 4), odd = to + sub * 128 + ((c ^ (sub + 4)) << 4);
+  if (rows == kBlkKeys && new_row < 0) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kBlkKeys / 4; ++j)
 #pragma unroll
       for (int h = 0; h < D / 64; ++h)
-        vr[j][h] = ld_once(b.v + (2 * t + (j & 1) + 8 * (j >> 1)) * D + 64 * h + 8 * g, pol);
+        copy_once((j & 1 ? odd : even) + j * 512 + h * (kBlkKeys * 128), src + j * 4 * D + h * 64, pol);
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int row = 2 * t + (j & 1) + 8 * (j >> 1);
+  for (int j = 0; j < kBlkKeys / 4; ++j) {
+    const int row = 4 * j + sub;
+    const bool is_new = row == new_row;
+    const bool valid = row < rows && !(is_new && fresh == nullptr);
+    const uint16_t* from = valid ? (is_new ? fresh + c * 8 : src + j * 4 * D) : base;
 #pragma unroll
-    for (int h = 0; h < D / 64; ++h) {
-      const int c = 64 * h + 8 * g;
-      vr[j][h] = make_uint4(0u, 0u, 0u, 0u);
-      if (row == b.new_row) {
-        vr[j][h] = *reinterpret_cast<const uint4*>(newv + c);
-        *reinterpret_cast<uint4*>(to + c) = vr[j][h];
-      } else if (row < b.rows) {
-        vr[j][h] = ld_once(b.v + row * D + c, pol);
-      }
-    }
+    for (int h = 0; h < D / 64; ++h)
+      copy_once((j & 1 ? odd : even) + j * 512 + h * (kBlkKeys * 128), from + (valid ? h * 64 : 0), valid, pol);
   }
 }
 
-// Norm and rotation of the unit's G query heads (warp 0, and of the new key's row warp 1), into shared memory.
-template <int D, int G>
-__device__ __forceinline__ void prepare(const WeightedParams& p, long long u, int b, long long pos, int warp,
-                                        int lane, uint8_t* smem) {
-  using S = WSmem<D, G, true>;
-  using P = Prep<D>;
-  const int c = lane % P::kLanes, sub = lane / P::kLanes;
-  const int l = static_cast<int>(u / p.Hkv % p.L);
-  const float* w = warp == 0 ? p.prep.q_weight : p.prep.k_weight;
-  if (w) w += static_cast<long long>(l) * D;
-  float2 cs[8];
-  if (p.prep.rope) {
-    unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos);
-    if (p.prep.evicted) at += static_cast<unsigned long long>(p.prep.evicted[b]);
-    float2* tab = reinterpret_cast<float2*>(smem + S::kTab) + warp * (D / 2);
-    prep_table<D>(p.prep, at, lane, tab);
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) cs[e] = tab[8 * c + e];
-  }
-  const int rows = warp == 0 ? 8 : 1;
-  const uint16_t* src = warp == 0 ? p.q + u * G * D : p.k_new + u * D;
-#pragma unroll 1
-  for (int r0 = 0; r0 < rows; r0 += P::kRows) {
-    const int r = r0 + sub;
-    uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-    if (r < (warp == 0 ? G : 1)) {
-      lo = *reinterpret_cast<const uint4*>(src + r * D + 8 * c);
-      hi = *reinterpret_cast<const uint4*>(src + r * D + D / 2 + 8 * c);
-    }
-    float x[16];
-    prep_unpack(lo, hi, x);
-    prep_norm<D>(x, w, p.prep.eps, c);
-    if (p.prep.rope) prep_rotate(x, cs);
-    const uint4 a = prep_pack(x), z = prep_pack(x + 8);
-    if (warp == 1) {
-      if (r < 1) {
-        uint16_t* to = reinterpret_cast<uint16_t*>(smem + S::kNew);
-        *reinterpret_cast<uint4*>(to + 8 * c) = a;
-        *reinterpret_cast<uint4*>(to + D / 2 + 8 * c) = z;
-      }
-    } else if (r < 8) {
-      uint16_t* to = reinterpret_cast<uint16_t*>(smem + S::kQ) + r * D;
-      *reinterpret_cast<uint4*>(to + 8 * c) = a;
-      *reinterpret_cast<uint4*>(to + D / 2 + 8 * c) = z;
-      float ah[8], zh[8];
-      unpack8(a, ah);
-      unpack8(z, zh);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {  // what is left (nothing that can be held where the high part is infinite)
-        x[e] = fabsf(ah[e]) < INFINITY ? x[e] - ah[e] : 0.f;
-        x[8 + e] = fabsf(zh[e]) < INFINITY ? x[8 + e] - zh[e] : 0.f;
-      }
-      to += 8 * D;
-      *reinterpret_cast<uint4*>(to + 8 * c) = prep_pack(x);
-      *reinterpret_cast<uint4*>(to + D / 2 + 8 * c) = prep_pack(x + 8);
-    }
-  }
-}
+// Norm and rotation of the unit's G query heads and of the new key, a row a warp, into shared memory.  Lane i
+// < d / 4 has elements 2 i, 2 i + 1 and their partners d / 2 further on.  Everything that it reads is requested at once
+// (`turns` before the grid dependency wait), and the norm does not wait for pos: what is left on the way to the first
+// products is one trip for pos, two sines and cosines a lane and a barrier.  (With d / 16 lanes to a row and two warps for all
+// of them, as prefill_kernel has it, that took 2 us.)
+template <int D, int G, int NW>
+struct Preparer {
+  static constexpr int kRows = (G + NW) / NW;  // rows of a warp
+  unsigned long long turns[2];
+  uint32_t row[kRows][2];
+  float2 gain[2][2];  // of the queries, of the key
+  long long moved;
 
-template <int D, int G, bool FUSED, bool PREP>
-__global__ void __launch_bounds__(kWThreads, 2)
+  __device__ __forceinline__ void tables(const WeightedParams& p, int lane) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int i = (2 * lane + e) % (D / 2);
+      turns[e] = p.prep.rope_slot >= 0 ? g_rope_tables[p.prep.rope_slot][i] : p.prep.rope_turns[i];
+    }
+  }
+  __device__ __forceinline__ void request(const WeightedParams& p, long long u, int b, int warp, int lane) {
+    moved = p.prep.evicted ? p.prep.evicted[b] : 0;
+    const int e = 2 * lane % (D / 2);
+    const size_t l = static_cast<unsigned>(u) % static_cast<unsigned>(p.LH) / static_cast<unsigned>(p.Hkv);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const float* w = x == 0 ? p.prep.q_weight : p.prep.k_weight;
+      if (w != nullptr) {
+        gain[x][0] = *reinterpret_cast<const float2*>(w + l * D + e);
+        gain[x][1] = *reinterpret_cast<const float2*>(w + l * D + D / 2 + e);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int r = warp + i * NW;
+      row[i][0] = row[i][1] = 0u;
+      if (r <= G && lane < D / 4) {
+        const uint16_t* src = r < G ? p.q + (u * G + r) * D : p.k_new + u * D;
+        row[i][0] = *reinterpret_cast<const uint32_t*>(src + e);
+        row[i][1] = *reinterpret_cast<const uint32_t*>(src + D / 2 + e);
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const WeightedParams& p, long long pos, int warp, int lane,
+                                         uint8_t* smem) {
+    using S = WSmem<D, G, true, NW>;
+    const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos) +
+                                  static_cast<unsigned long long>(moved);
+    float2 cs[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) cs[e] = p.prep.rope ? rope_cos_sin(at, turns[e]) : make_float2(1.f, 0.f);
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int r = warp + i * NW;
+      if (r > G) break;
+      float x[4] = {bf16lo_to_f32(row[i][0]), bf16hi_to_f32(row[i][0]), bf16lo_to_f32(row[i][1]), bf16hi_to_f32(row[i][1])};
+      if ((r < G ? p.prep.q_weight : p.prep.k_weight) != nullptr) {
+        float s = fmaf(x[0], x[0], x[1] * x[1]) + fmaf(x[2], x[2], x[3] * x[3]);
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+        const float f = 1.f / sqrtf(fmaf(s, 1.f / D, p.prep.eps));
+        const float2 g0 = r < G ? gain[0][0] : gain[1][0], g1 = r < G ? gain[0][1] : gain[1][1];
+        x[0] *= f * g0.x;
+        x[1] *= f * g0.y;
+        x[2] *= f * g1.x;
+        x[3] *= f * g1.y;
+      }
+      if (p.prep.rope) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float lo = x[e], hi = x[2 + e];
+          x[e] = fmaf(lo, cs[e].x, -hi * cs[e].y);
+          x[2 + e] = fmaf(hi, cs[e].x, lo * cs[e].y);
+        }
+      }
+      if (lane >= D / 4) continue;
+      uint16_t* to = reinterpret_cast<uint16_t*>(smem + (r < G ? S::kQ + r * D * 2 : S::kNew)) + 2 * lane;
+      const uint32_t a = pack_bf16_rn(x[0], x[1]), z = pack_bf16_rn(x[2], x[3]);
+      *reinterpret_cast<uint32_t*>(to) = a;
+      *reinterpret_cast<uint32_t*>(to + D / 2) = z;
+      if (r < G) {  // what is left (nothing that can be held where the high part is infinite)
+        const float h[4] = {bf16lo_to_f32(a), bf16hi_to_f32(a), bf16lo_to_f32(z), bf16hi_to_f32(z)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fabsf(h[e]) < INFINITY ? x[e] - h[e] : 0.f;
+        to += G * D;
+        *reinterpret_cast<uint32_t*>(to) = pack_bf16_rn(x[0], x[1]);
+        *reinterpret_cast<uint32_t*>(to + D / 2) = pack_bf16_rn(x[2], x[3]);
+      }
+    }
+  }
+};
+
+// NW warps a CTA, whose registers allow twelve on an SM.
+template <int D, int G, bool FUSED, bool PREP, int NW>
+__global__ void __launch_bounds__(32 * NW, 12 / NW)
 weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
-  using S = WSmem<D, G, PREP>;
+  using S = WSmem<D, G, PREP, NW>;
+  constexpr int kThreadsOfCta = 32 * NW;
   constexpr int DP = wrow_floats(D);
-  constexpr int KC = D / 32;  // K chunks of a lane and row
-  constexpr int VH = D / 64;  // V chunks of a lane and row
+  constexpr int KS = D / 16;  // k-steps of S^T, m-tiles of O^T
   extern __shared__ __align__(16) uint8_t smem[];
   float* merge_m = reinterpret_cast<float*>(smem + S::kM);
-  float* merge_l = merge_m + kWWarps * 8;
-  float* merge_o = reinterpret_cast<float*>(smem + S::kO);
+  float* merge_l = merge_m + NW * 8;
   float* rec_o = reinterpret_cast<float*>(smem + S::kRec);
-  float* rec_ml = rec_o + G * D;
+  float* rec_ml = reinterpret_cast<float*>(smem + S::kRecMl);
   float* fin_m = reinterpret_cast<float*>(smem + S::kFin);
   float* fin_r = fin_m + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -279,8 +307,8 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   const long long u = blockIdx.x / static_cast<unsigned>(p.cm);
   const int rank = static_cast<int>(blockIdx.x - u * p.cm);
   const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
-  const int stride = p.cm * kWWarps;
-  const int first = rank * kWWarps + warp;
+  const int stride = p.cm * NW;
+  const int first = rank * NW + warp;
 
   // The warp's first blocks, into L2: hints, which may come before the wait.
   if (lane < 2 * p.prefetch) {
@@ -297,6 +325,8 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     if (rows > 0)
       asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(base), "r"(rows * D * 2) : "memory");
   }
+  Preparer<D, G, NW> prep;
+  if (PREP) prep.tables(p, lane);  // written long before this launch
   pdl_wait();
   pdl_trigger();
 
@@ -304,11 +334,47 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   asm volatile("ld.global.cg.s64 %0, [%1];\n" : "=l"(pos) : "l"(p.pos + b) : "memory");
   const uint16_t* newk = FUSED ? p.k_new + u * D : nullptr;
   const uint16_t* newv = FUSED ? p.v_new + u * D : nullptr;
-  uint4 qa[KC];
+  uint32_t qa[KS][2], ql[PREP ? KS : 1][2];  // Q^T fragments: column g, rows 16 i + 2 t and + 8; what high parts leave
 #pragma unroll
-  for (int i = 0; i < KC; ++i) {
-    qa[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (!PREP && g < G) qa[i] = *reinterpret_cast<const uint4*>(p.q + (u * G + g) * D + 32 * i + 8 * t);
+  for (int i = 0; i < KS; ++i)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      qa[i][h] = 0u;
+      if (PREP) ql[PREP ? i : 0][h] = 0u;
+      if (!PREP && g < G) qa[i][h] = *reinterpret_cast<const uint32_t*>(p.q + (u * G + g) * D + 16 * i + 8 * h + 2 * t);
+    }
+  if (PREP) prep.request(p, u, b, warp, lane);
+  // Blocks of Tier-1 do not wait for pos.
+  const uint64_t pol = policy_evict_first();
+  // The products of this CTA's keys, [iteration][warp][16 keys][G], then their weights, [iteration][warp][16 keys].
+  const int slots = p.iters * NW * kBlkKeys;
+  float* scores = p.scratch ? p.scratch + static_cast<long long>(blockIdx.x) * slots * (G + 1)
+                            : reinterpret_cast<float*>(smem + S::kScores);
+  float* weights = scores + static_cast<long long>(slots) * G;
+  const uint32_t stage = smem_addr(smem) + warp * S::kBlk;
+  // Requests K, or V and the weights, of the block of iteration n, if the warp has one, into the warp's stage.
+  auto request_k = [&](int blk, int last, int count, int new_slot, const uint16_t* fresh) {
+    if (blk < last) {
+      const Blk x = blk_of<D>(p, u, blk, count, new_slot);
+      request_rows<D>(x.k, x.rows, x.new_row, fresh, lane, pol, stage);
+    }
+    copy_commit();
+  };
+  auto request_v = [&](int n, int blk, int last, int count, int new_slot, const uint16_t* fresh) {
+    if (blk < last) {
+      const Blk x = blk_of<D>(p, u, blk, count, new_slot);
+      request_rows<D>(x.v, x.rows, x.new_row, fresh, lane, pol,
+                      stage + S::kBlk / 2);
+      const bool valid = lane < x.rows && lane != x.new_row;
+      float* w = weights + (n * NW + warp) * kBlkKeys + lane;
+      if (p.scratch) *w = valid ? x.w[lane] : 0.f;
+      else cp_async_4(smem_addr(w), valid ? x.w + lane : x.w, valid ? 4u : 0u);
+    }
+    copy_commit();
+  };
+  if (first < p.nb1) {
+    request_k(first, p.nb1, 0, -1, nullptr);
+    request_v(0, first, p.nb1, 0, -1, nullptr);
   }
   const bool bad = pos < 0;
   int count = 0, new_slot = -1;
@@ -323,129 +389,160 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     }
   }
   const int nblk = bad ? 0 : p.nb1 + (count + kBlkKeys - 1) / kBlkKeys;
-  if (PREP) {
-    newk = reinterpret_cast<const uint16_t*>(smem + S::kNew);
-    if (warp < 2) prepare<D, G>(p, u, b, pos, warp, lane, smem);
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < KC; ++i)
-      qa[i] = *reinterpret_cast<const uint4*>(smem + S::kQ + (g * D + 32 * i + 8 * t) * 2);
-  }
   uint16_t* put_k = p.ring_k + (u * p.W + new_slot) * D;  // (not used without a new token)
   uint16_t* put_v = p.ring_v + (u * p.W + new_slot) * D;
-
-  // The products of this CTA's keys: [iteration][warp][16 keys][G].
-  float* scores = p.scratch ? p.scratch + static_cast<long long>(blockIdx.x) * p.iters * kWWarps * kBlkKeys * G
-                            : reinterpret_cast<float*>(smem + S::kScores);
-
+  if (PREP) newk = nullptr;  // put in when it is prepared
+  if (first >= p.nb1) {
+    request_k(first, nblk, count, new_slot, newk);
+    request_v(0, first, nblk, count, new_slot, newv);
+  }
+  const uint16_t* prepared = nullptr;
+  if (PREP) {
+    prepared = reinterpret_cast<const uint16_t*>(smem + S::kNew);
+    prep.finish(p, pos, warp, lane, smem);
+    __syncthreads();
+    if (g < G) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint8_t* at = smem + S::kQ + (g * D + 16 * i + 8 * h + 2 * t) * 2;
+          qa[i][h] = *reinterpret_cast<const uint32_t*>(at);
+          if (PREP) ql[PREP ? i : 0][h] = *reinterpret_cast<const uint32_t*>(at + G * D * 2);
+        }
+    }
+  }
   float m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
-  float o[4 * VH][4];
+  float o[KS][4];
 #pragma unroll
-  for (int j = 0; j < 4 * VH; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
-  uint4 kr[2][KC], vr[4][VH];
-  const uint64_t pol = policy_evict_first();
-  int blk = first;
-  Blk cur;
-  if (blk < nblk) {
-    cur = blk_of<D>(p, u, blk, count, new_slot);
-    load_k<D>(cur, newk, put_k, g, t, pol, kr);
-    load_v<D>(cur, newv, put_v, g, t, pol, vr);
-  }
+  for (int j = 0; j < KS; ++j) o[j][0] = o[j][1] = o[j][2] = o[j][3] = 0.f;
   float* sc = scores + (warp * kBlkKeys + g) * G + 2 * t;
-  while (blk < nblk) {
-    float sa[2][4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) sa[0][e] = sa[1][e] = 0.f;
-#pragma unroll
-    for (int i = 0; i < KC; ++i) {
-      wmma(sa[0], kr[0][i].x, kr[1][i].x, kr[0][i].y, kr[1][i].y, qa[i].x, qa[i].y);
-      wmma(sa[1], kr[0][i].z, kr[1][i].z, kr[0][i].w, kr[1][i].w, qa[i].z, qa[i].w);
+  // ldmatrix: lanes 0-7 / 8-15 / 16-23 / 24-31 give the rows of keys 0-7 / 8-15 / 0-7 / 8-15 at chunks 2 i / same / 2 i + 1 /
+  // same of K; of V (transposed) keys 0-7 / 0-7 / 8-15 / 8-15 at chunks 2 j / 2 j + 1 / same / same
+  const uint32_t k_at = ((lane & 7) + ((lane >> 3) & 1) * 8) * 128, k_x = ((lane >> 4) ^ (lane & 7)) << 4;
+  const uint32_t v_at = ((lane & 7) + (lane >> 4) * 8) * 128, v_x = (((lane >> 3) & 1) ^ (lane & 7)) << 4;
+  int n = 0;
+#pragma unroll 1
+  for (int blk = first; blk < nblk; blk += stride, ++n) {
+    const Blk cur = blk_of<D>(p, u, blk, count, new_slot);
+    const uint32_t sK = stage, sV = stage + S::kBlk / 2;
+    cp_async_wait<1>();  // K has landed, V may not
+    __syncwarp();
+    if (FUSED && cur.new_row >= 0) {  // this warp has the new token: its key goes to the ring
+      if (lane < D / 8) {
+        uint4* at = reinterpret_cast<uint4*>(smem + (sK - smem_addr(smem)) + swz<D>(cur.new_row, lane));
+        if (PREP) *at = *reinterpret_cast<const uint4*>(prepared + 8 * lane);
+        *reinterpret_cast<uint4*>(put_k + 8 * lane) = *at;
+      }
+      __syncwarp();
     }
-    if (PREP) {
+    // ---- S^T = K Q^T, two products of 16 keys, each in two accumulator chains ----
+    float sa[2][2][4];
 #pragma unroll
-      for (int i = 0; i < KC; ++i) {
-        const uint4 ql = *reinterpret_cast<const uint4*>(smem + S::kQ + ((8 + g) * D + 32 * i + 8 * t) * 2);
-        wmma(sa[0], kr[0][i].x, kr[1][i].x, kr[0][i].y, kr[1][i].y, ql.x, ql.y);
-        wmma(sa[1], kr[0][i].z, kr[1][i].z, kr[0][i].w, kr[1][i].w, ql.z, ql.w);
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sa[h][0][e] = sa[h][1][e] = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int i = 0; i < KS; ++i) {
+        uint32_t a0, a1, a2, a3;
+        ldsm_x4(sK + k_at + h * 2048 + (i >> 2) * (kBlkKeys * 128) + (((i & 3) * 32) ^ k_x), a0, a1, a2, a3);
+        wmma(sa[h][i & 1], a0, a1, a2, a3, qa[i][0], qa[i][1]);
+        if (PREP) wmma(sa[h][i & 1], a0, a1, a2, a3, ql[PREP ? i : 0][0], ql[PREP ? i : 0][1]);
       }
     }
-    const int rows = cur.rows;
-    const int next = blk + stride;
-    Blk nb;
-    if (next < nblk) {
-      nb = blk_of<D>(p, u, next, count, new_slot);
-      load_k<D>(nb, newk, put_k, g, t, pol, kr);
-    }
-    float v[4];  // keys g (0, 1) and g + 8 (2, 3), heads 2 t and 2 t + 1
+    __syncwarp();  // the stage's K is read
+    request_k(blk + stride, nblk, count, new_slot, newk);
+    float v[2][4];  // keys 16 h + g (0, 1) and + 8 (2, 3), heads 2 t and 2 t + 1
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = sa[0][e] + sa[1][e];
-    if (g >= rows) v[0] = v[1] = -INFINITY;
-    if (g + 8 >= rows) v[2] = v[3] = -INFINITY;
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[h][e] = sa[h][0][e] + sa[h][1][e];
+    if (cur.rows < kBlkKeys) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        if (16 * h + g >= cur.rows) v[h][0] = v[h][1] = -INFINITY;
+        if (16 * h + 8 + g >= cur.rows) v[h][2] = v[h][3] = -INFINITY;
+      }
+    }
     if (2 * t < G) {
-      if (G == 1) {
-        sc[0] = v[0];
-        sc[8] = v[2];
-      } else {
-        *reinterpret_cast<float2*>(sc) = make_float2(v[0], v[1]);
-        *reinterpret_cast<float2*>(sc + 8 * G) = make_float2(v[2], v[3]);
-      }
-    }
-    sc += kWWarps * kBlkKeys * G;
-    float mx0 = fmaxf(v[0], v[2]), mx1 = fmaxf(v[1], v[3]);
 #pragma unroll
-    for (int off = 4; off < 32; off <<= 1) {
-      mx0 = fmaxf(mx0, __shfl_xor_sync(0xffffffffu, mx0, off));
-      mx1 = fmaxf(mx1, __shfl_xor_sync(0xffffffffu, mx1, off));
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          if (G == 1) sc[16 * h + 8 * r] = v[h][2 * r];
+          else *reinterpret_cast<float2*>(sc + (16 * h + 8 * r) * G) = make_float2(v[h][2 * r], v[h][2 * r + 1]);
+        }
     }
-    mx0 *= p.scale_log2;
-    mx1 *= p.scale_log2;
-    const bool up0 = mx0 > m_run[0], up1 = mx1 > m_run[1];
+    sc += NW * kBlkKeys * G;
+    __syncwarp();
+    // ---- online softmax in the log2 domain.  The maximum over the keys is only taken where some key is above the one
+    // so far. ----
+    float mx[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e)
+      mx[e] = fmaxf(fmaxf(v[0][e], v[0][2 + e]), fmaxf(v[1][e], v[1][2 + e])) * p.scale_log2;
+    const bool up0 = mx[0] > m_run[0], up1 = mx[1] > m_run[1];
     if (__any_sync(0xffffffffu, up0 || up1)) {
-      const float alpha0 = up0 ? ex2(m_run[0] - mx0) : 1.f;
-      const float alpha1 = up1 ? ex2(m_run[1] - mx1) : 1.f;
-      if (up0) m_run[0] = mx0;
-      if (up1) m_run[1] = mx1;
-      l_run[0] *= alpha0;
-      l_run[1] *= alpha1;
 #pragma unroll
-      for (int j = 0; j < 4 * VH; ++j) {
-        o[j][0] *= alpha0;
-        o[j][1] *= alpha1;
-        o[j][2] *= alpha0;
-        o[j][3] *= alpha1;
+      for (int off = 4; off < 32; off <<= 1) {
+        mx[0] = fmaxf(mx[0], __shfl_xor_sync(0xffffffffu, mx[0], off));
+        mx[1] = fmaxf(mx[1], __shfl_xor_sync(0xffffffffu, mx[1], off));
+      }
+      float alpha[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const bool up = mx[e] > m_run[e];
+        alpha[e] = up ? ex2(m_run[e] - mx[e]) : 1.f;
+        if (up) m_run[e] = mx[e];
+        l_run[e] *= alpha[e];
+      }
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        o[j][0] *= alpha[0];
+        o[j][1] *= alpha[1];
+        o[j][2] *= alpha[0];
+        o[j][3] *= alpha[1];
       }
     }
-    float pr[4] = {0.f, 0.f, 0.f, 0.f};
-    if (m_run[0] != -INFINITY) {
-      pr[0] = ex2(fmaf(v[0], p.scale_log2, -m_run[0]));
-      pr[2] = ex2(fmaf(v[2], p.scale_log2, -m_run[0]));
-    }
-    if (m_run[1] != -INFINITY) {
-      pr[1] = ex2(fmaf(v[1], p.scale_log2, -m_run[1]));
-      pr[3] = ex2(fmaf(v[3], p.scale_log2, -m_run[1]));
-    }
-    l_run[0] += pr[0] + pr[2];
-    l_run[1] += pr[1] + pr[3];
-    // P^T as the B operand: packed to bf16 (outputs are bf16; the sums are not rounded) and transposed
-    const uint32_t pb0 = movmatrix_trans(pack_bf16_rn(pr[0], pr[1]));
-    const uint32_t pb1 = movmatrix_trans(pack_bf16_rn(pr[2], pr[3]));
+    uint32_t pb[2][2];
+    {
+      float pr[2][4];
+      const float m0 = finite_max(m_run[0]), m1 = finite_max(m_run[1]);
 #pragma unroll
-    for (int h = 0; h < VH; ++h) {
-      const uint32_t* r0 = reinterpret_cast<const uint32_t*>(&vr[0][h]);
-      const uint32_t* r1 = reinterpret_cast<const uint32_t*>(&vr[1][h]);
-      const uint32_t* r2 = reinterpret_cast<const uint32_t*>(&vr[2][h]);
-      const uint32_t* r3 = reinterpret_cast<const uint32_t*>(&vr[3][h]);
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int w = 0; w < 4; ++w)
-        wmma(o[4 * h + w], __byte_perm(r0[w], r1[w], 0x5410), __byte_perm(r0[w], r1[w], 0x7632),
-             __byte_perm(r2[w], r3[w], 0x5410), __byte_perm(r2[w], r3[w], 0x7632), pb0, pb1);
+        for (int e = 0; e < 4; ++e) pr[h][e] = ex2(fmaf(v[h][e], p.scale_log2, -(e & 1 ? m1 : m0)));
+      l_run[0] += (pr[0][0] + pr[0][2]) + (pr[1][0] + pr[1][2]);
+      l_run[1] += (pr[0][1] + pr[0][3]) + (pr[1][1] + pr[1][3]);
+      // P^T as the B operand: packed to bf16 (outputs are bf16; the sums are not rounded) and transposed
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        pb[h][0] = movmatrix_trans(pack_bf16_rn(pr[h][0], pr[h][1]));
+        pb[h][1] = movmatrix_trans(pack_bf16_rn(pr[h][2], pr[h][3]));
+      }
     }
-    if (next < nblk) {
-      load_v<D>(nb, newv, put_v, g, t, pol, vr);
-      cur = nb;
+    cp_async_wait<1>();  // V has
+    __syncwarp();
+    if (FUSED && cur.new_row >= 0 && lane < D / 8)
+      *reinterpret_cast<uint4*>(put_v + 8 * lane) =
+          *reinterpret_cast<const uint4*>(smem + (sV - smem_addr(smem)) + swz<D>(cur.new_row, lane));
+    // ---- O^T += V^T P^T ----
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < KS; ++j) {
+        uint32_t a0, a1, a2, a3;
+        ldsm_x4_trans(sV + v_at + h * 2048 + (j >> 2) * (kBlkKeys * 128) + (((j & 3) * 32) ^ v_x), a0, a1, a2, a3);
+        wmma(o[j], a0, a1, a2, a3, pb[h][0], pb[h][1]);
+      }
     }
-    blk = next;
+    __syncwarp();  // the stage's V is read
+    request_v(n + 1, blk + stride, nblk, count, new_slot, newv);
   }
+  cp_async_wait<0>();  // (a bad sequence's blocks of Tier-1 were requested too)
+  __syncwarp();
 
   // ---- the warps' states ----
 #pragma unroll
@@ -457,12 +554,12 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   for (int e = 0; e < 2; ++e) {
     const int hh = 2 * t + e;
     if (hh < G) {
-      float* ow = merge_o + (warp * G + hh) * DP + 8 * g;
+      float* ow = reinterpret_cast<float*>(smem + warp * S::kBlk) + hh * DP + g;
 #pragma unroll
-      for (int h = 0; h < VH; ++h)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          *reinterpret_cast<float2*>(ow + 64 * h + 2 * w) = make_float2(o[4 * h + w][e], o[4 * h + w][2 + e]);
+      for (int j = 0; j < KS; ++j) {
+        ow[16 * j] = o[j][e];
+        ow[16 * j + 8] = o[j][2 + e];
+      }
       if (g == 0) {
         merge_m[warp * 8 + hh] = m_run[e];
         merge_l[warp * 8 + hh] = l_run[e];
@@ -470,67 +567,34 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     }
   }
 
-  // This CTA's keys once more: key x of its iterations' blocks.  The first weights are requested
-  // before the merge.
-  const int mine = nblk > rank * kWWarps ? (nblk - rank * kWWarps + stride - 1) / stride : 0;  // iterations
-  const int nkeys = mine * kWWarps * kBlkKeys;
-  auto weight_of = [&](int x) -> float* {
-    const int w = (x / kBlkKeys) % kWWarps;
-    const int bk = rank * kWWarps + w + x / (kBlkKeys * kWWarps) * stride;
-    const int r = x % kBlkKeys;
-    if (bk < p.nb1) return bk * kBlkKeys + r < p.k ? p.t1w + u * p.N + bk * kBlkKeys + r : nullptr;
-    const int s = (bk - p.nb1) * kBlkKeys + r;
-    return bk < nblk && s < count ? p.ring_w + u * p.W + s : nullptr;
-  };
-  const float* fresh = FUSED && new_slot >= 0 ? p.ring_w + u * p.W + new_slot : nullptr;
-  constexpr int kAhead = 4;
-  float* wp[kAhead];
-  float wv[kAhead];
-#pragma unroll
-  for (int e = 0; e < kAhead; ++e) {
-    const int x = tid + e * kWThreads;
-    wp[e] = x < nkeys ? weight_of(x) : nullptr;
-    wv[e] = wp[e] && wp[e] != fresh ? *wp[e] : 0.f;
-  }
   __syncthreads();
-  if (FUSED && tid == 0) {
-    // every thread of the CTA has read pos; the last CTA of the sequence to come here advances it
-    __threadfence();
-    if (atomicAdd(p.tickets + b, 1ull) + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
-      if (!bad) p.pos[b] = pos + 1;
-      p.tickets[b] = 0ull;
-    }
-  }
-  if (bad && tid == 0 && rank == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
 
   // ---- merge: four columns of one head a thread, the warps in order ----
   constexpr int NGR = G * D / 4;
   const long long out_base = u * (G * D);
-  for (int x = tid; x < NGR; x += kWThreads) {
+  for (int x = tid; x < NGR; x += kThreadsOfCta) {
     const int hh = (4 * x) / D, c = (4 * x) % D;
     float M = merge_m[hh];
 #pragma unroll
-    for (int w = 1; w < kWWarps; ++w) M = fmaxf(M, merge_m[w * 8 + hh]);
+    for (int w = 1; w < NW; ++w) M = fmaxf(M, merge_m[w * 8 + hh]);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float Ls = 0.f;
-    if (M != -INFINITY) {
 #pragma unroll
-      for (int w = 0; w < kWWarps; ++w) {
-        const float f = ex2(merge_m[w * 8 + hh] - M);
-        const float4 y = *reinterpret_cast<const float4*>(merge_o + (w * G + hh) * DP + c);
-        acc.x = fmaf(f, y.x, acc.x);
-        acc.y = fmaf(f, y.y, acc.y);
-        acc.z = fmaf(f, y.z, acc.z);
-        acc.w = fmaf(f, y.w, acc.w);
-        Ls = fmaf(f, merge_l[w * 8 + hh], Ls);
-      }
+    for (int w = 0; w < NW; ++w) {
+      const float f = ex2(merge_m[w * 8 + hh] - finite_max(M));
+      const float4 y = *reinterpret_cast<const float4*>(smem + w * S::kBlk + (hh * DP + c) * 4);
+      acc.x = fmaf(f, y.x, acc.x);
+      acc.y = fmaf(f, y.y, acc.y);
+      acc.z = fmaf(f, y.z, acc.z);
+      acc.w = fmaf(f, y.w, acc.w);
+      Ls = fmaf(f, merge_l[w * 8 + hh], Ls);
     }
     if (p.cm == 1) {
       const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
       *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
           make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
       if (c == 0) {
-        fin_m[hh] = M;
+        fin_m[hh] = finite_max(M);
         fin_r[hh] = inv;
       }
     } else {
@@ -551,31 +615,29 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       M = -INFINITY;
       Ls = 0.f;
       for (int r = 0; r < p.cm; ++r) M = fmaxf(M, ld_peer_f32(peer_smem(ml_a + 8 * hh, r)));
-      if (M == -INFINITY) return;
+      M = finite_max(M);
       for (int r = 0; r < p.cm; ++r)
         Ls = fmaf(ex2(ld_peer_f32(peer_smem(ml_a + 8 * hh, r)) - M), ld_peer_f32(peer_smem(ml_a + 8 * hh + 4, r)), Ls);
     };
-    for (int x = rank * SL + tid; x < x1; x += kWThreads) {
+    for (int x = rank * SL + tid; x < x1; x += kThreadsOfCta) {
       const int hh = (4 * x) / D, c = (4 * x) % D;
       float M, Ls;
       merged(hh, M, Ls);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (M != -INFINITY) {
-        for (int r = 0; r < p.cm; ++r) {
-          const float f = ex2(ld_peer_f32(peer_smem(ml_a + 8 * hh, r)) - M);
-          const float4 y = ld_peer_f4(peer_smem(o_a + (hh * D + c) * 4, r));
-          acc.x = fmaf(f, y.x, acc.x);
-          acc.y = fmaf(f, y.y, acc.y);
-          acc.z = fmaf(f, y.z, acc.z);
-          acc.w = fmaf(f, y.w, acc.w);
-        }
+      for (int r = 0; r < p.cm; ++r) {
+        const float f = ex2(ld_peer_f32(peer_smem(ml_a + 8 * hh, r)) - M);
+        const float4 y = ld_peer_f4(peer_smem(o_a + (hh * D + c) * 4, r));
+        acc.x = fmaf(f, y.x, acc.x);
+        acc.y = fmaf(f, y.y, acc.y);
+        acc.z = fmaf(f, y.z, acc.z);
+        acc.w = fmaf(f, y.w, acc.w);
       }
       const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
       *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
           make_uint2(pack_bf16_rn(acc.x * inv, acc.y * inv), pack_bf16_rn(acc.z * inv, acc.w * inv));
     }
-    if (tid >= kWThreads - G) {  // the heads' final maxima and sums, for the weights
-      const int hh = tid - (kWThreads - G);
+    if (tid >= kThreadsOfCta - G) {  // the heads' final maxima and sums, for the weights
+      const int hh = tid - (kThreadsOfCta - G);
       float M, Ls;
       merged(hh, M, Ls);
       fin_m[hh] = M;
@@ -592,25 +654,29 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     M[h] = fin_m[h];
     R[h] = fin_r[h];
   }
-  for (int x0 = tid; x0 < nkeys; x0 += kAhead * kWThreads) {
-    if (x0 != tid) {
+  // Key x is row x % 16 of the block that warp x / 16 % 8 took in iteration x / 128.
+  const int iters = nblk > rank * NW ? (nblk - rank * NW + stride - 1) / stride : 0;
+  for (int x = tid; x < iters * NW * kBlkKeys; x += kThreadsOfCta) {
+    const int blk = rank * NW + x / kBlkKeys % NW + x / (kBlkKeys * NW) * stride;
+    const int r = x % kBlkKeys;
+    const int key = (blk < p.nb1 ? blk : blk - p.nb1) * kBlkKeys + r;
+    if (blk >= nblk || key >= (blk < p.nb1 ? p.k : count)) continue;
+    const float* s = scores + static_cast<long long>(x) * G;
+    float sum = 0.f;
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e) {
-        const int x = x0 + e * kWThreads;
-        wp[e] = x < nkeys ? weight_of(x) : nullptr;
-        wv[e] = wp[e] && wp[e] != fresh ? *wp[e] : 0.f;
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < kAhead; ++e) {
-      if (!wp[e]) continue;
-      const float* s = scores + static_cast<long long>(x0 + e * kWThreads) * G;
-      float sum = 0.f;
-#pragma unroll
-      for (int h = 0; h < G; ++h) sum = fmaf(ex2(fmaf(s[h], p.scale_log2, -M[h])), R[h], sum);
-      *wp[e] = wv[e] + sum;
+    for (int h = 0; h < G; ++h) sum = fmaf(ex2(fmaf(s[h], p.scale_log2, -M[h])), R[h], sum);
+    (blk < p.nb1 ? p.t1w + u * p.N : p.ring_w + u * p.W)[key] = weights[x] + sum;
+  }
+  if (FUSED && tid == 0) {
+    // every thread of the CTA has read pos; the last CTA of the sequence to come here advances it (last of
+    // all: the fence and the atomic are two trips to L2)
+    __threadfence();
+    if (atomicAdd(p.tickets + b, 1ull) + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
+      if (!bad) p.pos[b] = pos + 1;
+      p.tickets[b] = 0ull;
     }
   }
+  if (bad && tid == 0 && rank == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
   if (p.cm > 1) cluster_wait();  // no peer reads this CTA's memory any more
 }
 
@@ -618,38 +684,44 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
 // Host side
 // ---------------------------------------------------------------------------
 
-// Blocks that a warp of a cluster of cm CTAs takes at most.
-static int iters_of(const cmc_dims& m, int cm) {
-  const long long nblk = (static_cast<long long>(m.k) + kBlkKeys - 1) / kBlkKeys +
-                         (static_cast<long long>(m.W) + kBlkKeys - 1) / kBlkKeys;
-  return static_cast<int>((nblk + cm * kWWarps - 1) / (cm * kWWarps));
+static long long blocks_of(const cmc_dims& m) {
+  return (static_cast<long long>(m.k) + kBlkKeys - 1) / kBlkKeys + (static_cast<long long>(m.W) + kBlkKeys - 1) / kBlkKeys;
 }
-static size_t score_bytes(const cmc_dims& m, int cm) {
-  return static_cast<size_t>(iters_of(m, cm)) * kWWarps * kBlkKeys * (m.Hq / m.Hkv) * 4;
+// Blocks that each of a unit's `warps` takes at most, and the bytes of a CTA's products and weights.
+static long long iters_of(const cmc_dims& m, int warps) { return (blocks_of(m) + warps - 1) / warps; }
+static size_t score_bytes(const cmc_dims& m, int cm, int nw) {
+  return static_cast<size_t>(iters_of(m, cm * nw)) * nw * kBlkKeys * (m.Hq / m.Hkv + 1) * 4;
 }
-static bool needs_scratch(const cmc_dims& m) { return score_bytes(m, kMaxClusterCtas) > kScoreBytes; }
+constexpr int kWarpsMost = 4;  // of a CTA
+static bool needs_scratch(const cmc_dims& m) { return score_bytes(m, kMaxClusterCtas, kWarpsMost) > static_cast<size_t>(score_cap(m.Hq / m.Hkv)); }
 static size_t weighted_ws(const cmc_dims& m) {
   const size_t units = static_cast<size_t>(m.B) * m.L * m.Hkv;
-  return ws_partials_off(m.B) + (needs_scratch(m) ? units * kMaxClusterCtas * score_bytes(m, kMaxClusterCtas) : 0);
+  return ws_partials_off(m.B) +
+         (needs_scratch(m) ? units * kMaxClusterCtas * score_bytes(m, kMaxClusterCtas, kWarpsMost) : 0);
 }
 
-// CTAs per unit: as many as it takes to fill the device, at most one per eight blocks; more where the unit's
-// products would not go into shared memory.
-static int plan_cm(const cmc_dims& m, int per_sm) {
+// What an SM holds of a kernel by its registers and threads, and by its shared memory.
+constexpr int kSmemPerSm = 233472, kSmemReserved = 1024;
+
+// CTAs of four warps per unit: the most that are resident together, with two blocks a warp at least (a cluster's merge
+// costs more than a block: 2 units of 5 blocks 3.9 us with two CTAs, 2.5 with one); more where the unit's products would not
+// go into shared memory.
+static int plan_cm(const cmc_dims& m, int per_sm, int fixed_smem) {
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  long long cm = static_cast<long long>(per_sm) * sm_count() / units;
-  const long long nblk = (static_cast<long long>(m.k) + kBlkKeys - 1) / kBlkKeys +
-                         (static_cast<long long>(m.W) + kBlkKeys - 1) / kBlkKeys;
-  cm = std::min(cm, (nblk + kWWarps - 1) / kWWarps);
-  cm = std::max(1LL, std::min<long long>(cm, kMaxClusterCtas));
-  while (cm < kMaxClusterCtas && score_bytes(m, static_cast<int>(cm)) > kScoreBytes) ++cm;
-  return static_cast<int>(cm);
+  const size_t cap = score_cap(m.Hq / m.Hkv);
+  int cm = static_cast<int>(std::max(1LL, std::min<long long>(blocks_of(m) / (2 * kWarpsMost), kMaxClusterCtas)));
+  for (; cm > 1; --cm) {
+    const long long smem = fixed_smem + static_cast<long long>(std::min(score_bytes(m, cm, kWarpsMost), cap)) + kSmemReserved;
+    if (units * cm <= std::min<long long>(per_sm, kSmemPerSm / smem) * sm_count()) break;
+  }
+  while (cm < kMaxClusterCtas && score_bytes(m, cm, kWarpsMost) > cap) ++cm;
+  return cm;
 }
 
-template <int D, int G, bool FUSED, bool PREP>
+template <int D, int G, bool FUSED, bool PREP, int NW>
 static int per_sm_of(int* out) {
-  constexpr int smem = WSmem<D, G, PREP>::kScores + kScoreBytes;
-  auto kern = weighted_attn_kernel<D, G, FUSED, PREP>;
+  constexpr int smem = WSmem<D, G, PREP, NW>::kScores + kScoreMost;
+  auto kern = weighted_attn_kernel<D, G, FUSED, PREP, NW>;
   static std::atomic<int> known[64];
   int dev = 0;
   int st = record_cuda_error(cudaGetDevice(&dev));
@@ -658,7 +730,7 @@ static int per_sm_of(int* out) {
   if (per_sm <= 0) {
     st = record_cuda_error(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     if (st != CMC_OK) return st;
-    st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, kWThreads, smem));
+    st = record_cuda_error(cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, kern, 32 * NW, 0));
     if (st != CMC_OK) return st;
     if (per_sm < 1) per_sm = 1;
     if (dev >= 0 && dev < 64) known[dev].store(per_sm, std::memory_order_release);
@@ -667,37 +739,53 @@ static int per_sm_of(int* out) {
   return CMC_OK;
 }
 
-template <int D, int G, bool FUSED, bool PREP>
-static int launch_weighted(WeightedParams& p, const cmc_dims& m, cudaStream_t s, int* ctas) {
-  int per_sm = 1;
-  int st = per_sm_of<D, G, FUSED, PREP>(&per_sm);
-  if (st != CMC_OK) return st;
-  const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  p.cm = plan_cm(m, per_sm);
-  if (ctas) {
-    *ctas = static_cast<int>(units * p.cm);
-    return CMC_OK;
-  }
-  p.iters = iters_of(m, p.cm);
-  size_t bytes = score_bytes(m, p.cm);
-  if (bytes > kScoreBytes) bytes = 0;  // in the workspace
+template <int D, int G, bool FUSED, bool PREP, int NW>
+static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cudaStream_t s) {
+  p.cm = cm;
+  p.iters = static_cast<int>(iters_of(m, cm * NW));
+  size_t bytes = score_bytes(m, cm, NW);
+  const long long ctas = static_cast<long long>(m.B) * m.L * m.Hkv * cm;
+  if (bytes > static_cast<size_t>(ctas <= sm_count() ? kScoreMost : score_cap(G))) bytes = 0;  // in the workspace
   else p.scratch = nullptr;
   p.prefetch = std::min({l2_prefetch_setting(), 3, p.iters});
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
   attr[1].id = cudaLaunchAttributeClusterDimension;
-  attr[1].val.clusterDim.x = static_cast<unsigned>(p.cm);
+  attr[1].val.clusterDim.x = static_cast<unsigned>(cm);
   attr[1].val.clusterDim.y = 1;
   attr[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(units * p.cm));
-  cfg.blockDim = dim3(kWThreads);
-  cfg.dynamicSmemBytes = WSmem<D, G, PREP>::kScores + bytes;
+  cfg.gridDim = dim3(static_cast<unsigned>(ctas));
+  cfg.blockDim = dim3(32 * NW);
+  cfg.dynamicSmemBytes = WSmem<D, G, PREP, NW>::kScores + bytes;
   cfg.stream = s;
   cfg.attrs = attr;
-  cfg.numAttrs = p.cm > 1 ? 2 : 1;
-  return record_cuda_error(cudaLaunchKernelEx(&cfg, weighted_attn_kernel<D, G, FUSED, PREP>, p));
+  cfg.numAttrs = cm > 1 ? 2 : 1;
+  return record_cuda_error(cudaLaunchKernelEx(&cfg, weighted_attn_kernel<D, G, FUSED, PREP, NW>, p));
+}
+
+// A CTA of four warps a unit, or a cluster of them; a warp a unit where there are more units than CTAs are resident
+// and none has more than kSoloBlocks blocks.  (us a step with rotation, four warps / one, d = 128, G = 4, blocks 4, 8, 12, 20:
+//    512 units  10.6 / 10.7   16.9 / 15.3   22.9 / 20.1   31.4 / 29.2
+//  1,024        18.2 / 13.5   28.8 / 22.2   42.8 / 29.4   58.6 / 64.8
+//  2,048        31.6 / 27.7   50.4 / 44.3   77.6 / 57.5  106.1 / 107.1
+//    256         6.5 /  8.7    8.3 / 18.2    9.8 / 21.9   14.7 / 27.9)
+template <int D, int G, bool FUSED, bool PREP>
+static int launch_weighted(WeightedParams& p, const cmc_dims& m, cudaStream_t s, int* ctas) {
+  int per_sm = 1;
+  int st = per_sm_of<D, G, FUSED, PREP, kWarpsMost>(&per_sm);
+  if (st != CMC_OK) return st;
+  const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
+  const bool solo = units > static_cast<long long>(per_sm) * sm_count() && blocks_of(m) <= kSoloBlocks;
+  const int cm = solo ? 1 : plan_cm(m, per_sm, WSmem<D, G, PREP, kWarpsMost>::kScores);
+  if (ctas) {
+    *ctas = static_cast<int>(units * cm);
+    return CMC_OK;
+  }
+  if (!solo) return launch_weighted_cm<D, G, FUSED, PREP, kWarpsMost>(p, m, cm, s);
+  st = per_sm_of<D, G, FUSED, PREP, 1>(&per_sm);
+  return st != CMC_OK ? st : launch_weighted_cm<D, G, FUSED, PREP, 1>(p, m, cm, s);
 }
 
 template <bool FUSED, bool PREP>

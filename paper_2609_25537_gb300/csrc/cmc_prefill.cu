@@ -115,7 +115,9 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
       float x[16];
       prep_unpack(a[e][0], a[e][1], x);
       const float* w = is_v ? nullptr : r < nq ? p.prep.q_weight : p.prep.k_weight;
-      prep_norm<D>(x, w ? w + static_cast<long long>(l) * D : nullptr, p.prep.eps, c);
+      float4 gain[4];
+      if (w) prep_gains<D>(w + static_cast<long long>(l) * D, c, gain);
+      prep_norm<D>(x, gain, w != nullptr, p.prep.eps);
       if (p.prep.rope) prep_rotate(x, cs);
       if (!is_v) {
         a[e][0] = prep_pack(x);

@@ -46,27 +46,31 @@ __device__ __forceinline__ void prep_table(const PrepParams& p, unsigned long lo
   }
 }
 
-// One row's share of a lane: x[0..7] and x[8..15] are elements 8 c .. and d / 2 + 8 c ...
-// `w` (this layer's d gains) may be NULL.  All lanes of the warp take part.
+// A lane's share of a row of gains.
 template <int D>
-__device__ __forceinline__ void prep_norm(float (&x)[16], const float* w, float eps, int c) {
+__device__ __forceinline__ void prep_gains(const float* w, int c, float4 (&g)[4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) g[e] = *reinterpret_cast<const float4*>(w + (e >> 1) * (D / 2) + 8 * c + 4 * (e & 1));
+}
+
+// One row's share of a lane: x[0..7] and x[8..15] are elements 8 c .. and d / 2 + 8 c ...  `norm` differs
+// between the rows of a warp, all of whose lanes take part.
+template <int D>
+__device__ __forceinline__ void prep_norm(float (&x)[16], const float4 (&g)[4], bool norm, float eps) {
   float s = 0.f;
 #pragma unroll
   for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
 #pragma unroll
   for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  if (w == nullptr) return;
+  if (!norm) return;
   const float r = 1.f / sqrtf(fmaf(s, 1.f / D, eps));
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
-#pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float4 g = *reinterpret_cast<const float4*>(w + h * (D / 2) + 8 * c + 4 * e);
-      x[8 * h + 4 * e + 0] *= r * g.x;
-      x[8 * h + 4 * e + 1] *= r * g.y;
-      x[8 * h + 4 * e + 2] *= r * g.z;
-      x[8 * h + 4 * e + 3] *= r * g.w;
-    }
+  for (int e = 0; e < 4; ++e) {
+    x[4 * e + 0] *= r * g[e].x;
+    x[4 * e + 1] *= r * g[e].y;
+    x[4 * e + 2] *= r * g[e].z;
+    x[4 * e + 3] *= r * g[e].w;
+  }
 }
 
 // cs: (cos, sin) of pairs 8 c .. 8 c + 7.

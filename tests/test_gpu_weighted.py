@@ -398,11 +398,13 @@ def test_nan_among_the_keys_reaches_its_kv_head_only(cuda_device):
     assert torch.equal(t1[2][1], clean[2][1]) and torch.equal(ring[2][0, 0, 0], clean[5][0, 0, 0])
 
 
-def test_units_whose_products_go_to_the_workspace(cuda_device):
-    """G = 8: more than 18,432 keys a unit."""
-    case = (2, 1, 1, 8, 64, 12000, 9000, [8999, 5])
-    dims = cmc.CmcDims(2, 1, 8, 1, 64, 12000, 12000, 9000)
-    assert cmc.decode_attn_weighted_workspace_size(dims) > 2 * 21000 * 32
+@pytest.mark.parametrize("B, H", [(2, 1), (5, 4)])
+def test_units_whose_products_go_to_the_workspace(cuda_device, B, H):
+    """G = 8: more than 9,216 keys a unit; with up to a CTA an SM they stay in shared memory all the same."""
+    case = (B, 1, H, 8, 64, 6000, 5000, [4999, 5])
+    dims = cmc.CmcDims(B, 1, 8 * H, H, 64, 6000, 6000, 5000)
+    assert cmc.decode_attn_weighted_workspace_size(dims) > B * H * 11000 * 36
+    assert cmc.decode_attn_weighted_plan(dims) == B * H * 8
     q, t1, ring, pos, g = attention_problem(cuda_device, case, 9)
     before = [f64(x) for x in (q, *t1, *ring, pos)]
     ws = cmc.DecodeWorkspace(dims, cuda_device, weighted=True)

@@ -118,9 +118,13 @@ def test_workspace_sizes(L):
         return L.cmc_decode_attn_weighted_workspace_size(_dims(**kw))
     assert f() == f(L=65, k=100, W=5000, d=64) == 512
     assert f(d=96) == 0 and f(Hq=6) == 0 and f(k=101) == 0
-    # G = 4: 36,864 keys fit a cluster's shared memory; beyond, 4 G bytes a key, rounded up to 128 keys a CTA
-    assert f(k=0, W=36864) == 512
-    assert f(k=0, W=36865) == 512 + 2 * 3 * 2 * 8 * 37 * 128 * 16
+    # G = 4: 18,432 keys fit a cluster's shared memory; beyond, 4 (G + 1) bytes a key, rounded up to 128 keys a CTA
+    assert f(k=0, W=18432) == f(N=16000, k=8192, W=10240) == 512
+    assert f(k=0, W=18433) == 512 + 2 * 3 * 2 * 8 * 19 * 128 * 20
+    assert f(k=0, W=9216, Hq=16) == 512
+    assert f(k=0, W=9217, Hq=16) == 512 + 2 * 3 * 2 * 8 * 10 * 128 * 36
+    assert f(k=0, W=30720, Hq=4) == f(k=0, W=46080, Hq=2) == 512
+    assert f(k=0, W=30721, Hq=4) > 512 and f(k=0, W=46081, Hq=2) > 512
 
 
 def _prep(**kw):
