@@ -1,11 +1,18 @@
 // Norm and rotary embedding of the heads of many tokens, alone (cmc_qk_norm_rope) and with the
 // append of their keys and values to the Tier-2 ring (cmc_window_prefill).
+//
+// Bound: HBM, every head's row read once and written once (4 d bytes against some 10 d flops).  A warp takes a
+// token: (cos, sin) of its position and the layer's gains go to shared memory once, then its heads' rows pass through
+// registers.  What limits the rate beside HBM is the instructions of a row (issue slots 70 % taken), so more warps
+// with fewer rows in flight each are better: 8,192 tokens of 32 + 8 heads of 128, us a launch at 4 warps a CTA: two rows a lane
+// group and 8 CTAs an SM 30.3 (83 % of the copy rate), three and 6 33.9, four and 6 33.7.
 #include "cmc_prep.cuh"
 
 namespace cmc {
 
-constexpr int kPrefillWarps = 8;
-constexpr int kPrefillBatch = 4;  // rows a lane group has in flight
+constexpr int kPrefillWarps = 4;
+constexpr int kPrefillPerSm = 8;  // CTAs on an SM, by registers
+constexpr int kPrefillBatch = 2;  // rows a lane group has in flight
 
 struct PrefillParams {
   const uint16_t* q;  // token rows of Hq heads, q_stride elements apart; NULL: no queries
@@ -26,111 +33,198 @@ struct PrefillParams {
   PrepParams prep;
 };
 
+// A head's row is taken by d / 16 lanes: lane c of them has 16-byte chunks c and c + d / 16, which are
+// elements 8 c .. 8 c + 7 and their partners d / 2 further on, so that the rotation needs nothing from
+// another lane and the norm one sum over the group.
+template <int D>
+struct Prep {
+  static constexpr int kLanes = D / 16;         // lanes of one row
+  static constexpr int kRows = 32 / kLanes;     // rows that a warp takes at once
+};
+
+// What the rows of a token have in common, in shared memory, a warp's own, in the order in which the lanes of a row
+// read it, so that they do not meet in a bank (side by side as the elements are, that was what bound the kernel: 88 % of L1's
+// rate, 42 us for 8,192 tokens of 32 + 8 heads).
+template <int D>
+struct __align__(16) TokenTable {
+  static constexpr int kL = Prep<D>::kLanes;
+  float4 turn[4][kL];        // [j][c]: (cos, sin) of pairs 8 c + 2 j and + 1
+  float4 gain[2][2][2][kL];  // of the queries, of the keys: [half][q][c]: elements 8 c + 4 q .. + 3 of a half
+};
+
+// Two chunks of a row, normed by r times the gains (where NORM; a row without gains has r = 1 and takes none) and turned.
+// Four elements and their partners at a time: the registers go to rows on the way.
+template <int D>
+__device__ __forceinline__ void prep_chunks(uint4 (&a)[2], bool norm, float r, const float4 (&gain)[2][2][Prep<D>::kLanes],
+                                            bool rope, const float4 (&turn)[4][Prep<D>::kLanes], int c) {
+  uint32_t* lo = reinterpret_cast<uint32_t*>(&a[0]);
+  uint32_t* hi = reinterpret_cast<uint32_t*>(&a[1]);
+#pragma unroll
+  for (int q = 0; q < 2; ++q) {
+    float x[4] = {bf16lo_to_f32(lo[2 * q]), bf16hi_to_f32(lo[2 * q]), bf16lo_to_f32(lo[2 * q + 1]), bf16hi_to_f32(lo[2 * q + 1])};
+    float y[4] = {bf16lo_to_f32(hi[2 * q]), bf16hi_to_f32(hi[2 * q]), bf16lo_to_f32(hi[2 * q + 1]), bf16hi_to_f32(hi[2 * q + 1])};
+    if (norm) {
+      const float4 g = gain[0][q][c], h = gain[1][q][c];
+      x[0] *= r * g.x; x[1] *= r * g.y; x[2] *= r * g.z; x[3] *= r * g.w;
+      y[0] *= r * h.x; y[1] *= r * h.y; y[2] *= r * h.z; y[3] *= r * h.w;
+    }
+    if (rope) {
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        const float4 t = turn[2 * q + e / 2][c];
+        const float x0 = x[e], x1 = x[e + 1];
+        x[e] = fmaf(x0, t.x, -y[e] * t.y);
+        y[e] = fmaf(y[e], t.x, x0 * t.y);
+        x[e + 1] = fmaf(x1, t.z, -y[e + 1] * t.w);
+        y[e + 1] = fmaf(y[e + 1], t.z, x1 * t.w);
+      }
+    }
+    lo[2 * q] = pack_bf16_rn(x[0], x[1]);
+    lo[2 * q + 1] = pack_bf16_rn(x[2], x[3]);
+    hi[2 * q] = pack_bf16_rn(y[0], y[1]);
+    hi[2 * q + 1] = pack_bf16_rn(y[2], y[3]);
+  }
+}
+
+// 1 / sqrt(mean of squares + eps) of a row, given to all of its lanes.
+template <int D>
+__device__ __forceinline__ float prep_rms(const uint4 (&a)[2], float eps) {
+  float s = 0.f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float x[8];
+    unpack8(a[h], x);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
+  }
+#pragma unroll
+  for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  return 1.f / sqrtf(fmaf(s, 1.f / D, eps));
+}
+
 // A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.
 template <int D, bool RING>
-__global__ void __launch_bounds__(32 * kPrefillWarps)
+__global__ void __launch_bounds__(32 * kPrefillWarps, kPrefillPerSm)
 prefill_kernel(const __grid_constant__ PrefillParams p) {
   using P = Prep<D>;
-  __shared__ float2 table[kPrefillWarps][D / 2];
-  __shared__ long long pos_s;
+  __shared__ TokenTable<D> tables[kPrefillWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int c = lane % P::kLanes, sub = lane / P::kLanes;
+  TokenTable<D>& table = tables[warp];
   const int b = blockIdx.y;
+  const unsigned item = blockIdx.x * kPrefillWarps + warp;
+  const unsigned tok = item / static_cast<unsigned>(p.parts);  // l T + t
+  const int part = static_cast<int>(item - tok * p.parts);
+  const int l = static_cast<int>(tok / static_cast<unsigned>(p.T));
+  const int t = static_cast<int>(tok - static_cast<unsigned>(l) * p.T);
+  // Rows: Hq of q, Hkv of k, and with a ring Hkv of v.
+  const int nq = p.q ? p.Hq : 0;
+  const int all = nq + (RING ? 2 : 1) * p.Hkv;
+  const int per = ((all + P::kRows - 1) / P::kRows + p.parts - 1) / p.parts;  // steps of a warp
+  const int first = part * per;
+  const long long row0 = (static_cast<long long>(b) * p.L + l) * p.T + t;
+  const uint16_t* qrow = p.q + row0 * p.q_stride + 8 * c;
+  const uint16_t* krow = p.k + row0 * p.k_stride + 8 * c;
+  const uint16_t* vrow = p.v + row0 * p.v_stride + 8 * c;
+  unsigned long long turns[D / 64];
+  if (p.prep.rope)
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e)
+      turns[e] = p.prep.rope_slot >= 0 ? g_rope_tables[p.prep.rope_slot][lane + 32 * e] : p.prep.rope_turns[lane + 32 * e];
   pdl_wait();
   pdl_trigger();
-  if (threadIdx.x == 0) pos_s = *static_cast<volatile const int64_t*>(p.pos + b);
-  __syncthreads();
-  const long long pos = pos_s;
-  int n = p.T;
-  if (RING && p.count) {
-    const long long c = p.count[b];
-    n = c < 0 ? 0 : c < p.T ? static_cast<int>(c) : p.T;
-  }
-  if (RING && threadIdx.x == 0) {
-    // the last of the sequence's CTAs to have read pos advances it
-    __threadfence();
-    if (atomicAdd(p.tickets + b, 1ull) + 1 == gridDim.x) {
-      if (pos >= 0) p.pos[b] = pos + n;
-      else atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-      p.tickets[b] = 0ull;
-    }
-  }
-  if (RING && pos < 0) return;
-  const long long item = static_cast<long long>(blockIdx.x) * kPrefillWarps + warp;
-  const long long tok = item / p.parts;  // l T + t
-  const int part = static_cast<int>(item - tok * p.parts);
-  const int l = static_cast<int>(tok / p.T);
-  const int t = static_cast<int>(tok - static_cast<long long>(l) * p.T);
-  if (l >= p.L || t >= n) return;
-  const int c = lane % P::kLanes, sub = lane / P::kLanes;
 
-  float2 cs[8];
-  if (p.prep.rope) {
-    unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos + t);
-    if (p.prep.evicted) at += static_cast<unsigned long long>(p.prep.evicted[b]);
-    prep_table<D>(p.prep, at, lane, table[warp]);
-    __syncwarp();
-#pragma unroll
-    for (int e = 0; e < 8; ++e) cs[e] = table[warp][8 * c + e];
-  }
-
-  // Rows: Hq of q, Hkv of k, and with a ring Hkv of v.  Those of k and v that the ring does not
-  // keep are left out.
-  const bool kept = !RING || t >= n - p.W;
-  long long slot = 0;
-  if (RING && kept) {
-    const unsigned long long at = static_cast<unsigned long long>(pos) + static_cast<unsigned long long>(t);
-    slot = (at >> 32) == 0 ? static_cast<unsigned>(at) % static_cast<unsigned>(p.W)
-                           : static_cast<long long>(at % static_cast<unsigned>(p.W));
-  }
-  const int nq = p.q ? p.Hq : 0;
-  const int rows = nq + (kept ? (RING ? 2 : 1) * p.Hkv : 0);
-  const int steps = (rows + P::kRows - 1) / P::kRows;
-  const int per = (steps + p.parts - 1) / p.parts;
-  const int s1 = min(steps, (part + 1) * per);
-  const long long row0 = (static_cast<long long>(b) * p.L + l) * p.T + t;
-  const uint16_t* qrow = p.q + row0 * p.q_stride;
-  const uint16_t* krow = p.k + row0 * p.k_stride;
-  const uint16_t* vrow = RING ? p.v + row0 * p.v_stride : nullptr;
-  const long long unit0 = (static_cast<long long>(b) * p.L + l) * p.Hkv;
-  for (int s0 = part * per; s0 < s1; s0 += kPrefillBatch) {
-    uint4 a[kPrefillBatch][2];
+  // Everything that comes before the first rows' arithmetic is requested together, the first rows with it where their
+  // number does not depend on what is read.
+  const long long pos = *static_cast<volatile const int64_t*>(p.pos + b);
+  const long long moved = p.prep.evicted ? p.prep.evicted[b] : 0;
+  long long count = p.T;
+  if (RING && p.count) count = p.count[b];
+  uint4 a[kPrefillBatch][2];
+  auto load = [&](int s0, int end, int rows) {
 #pragma unroll
     for (int e = 0; e < kPrefillBatch; ++e) {
       const int r = (s0 + e) * P::kRows + sub;
       a[e][0] = a[e][1] = make_uint4(0u, 0u, 0u, 0u);
-      if (s0 + e < s1 && r < rows) {
-        const uint16_t* src = r < nq             ? qrow + static_cast<long long>(r) * D
-                              : r < nq + p.Hkv ? krow + static_cast<long long>(r - nq) * D
-                                               : vrow + static_cast<long long>(r - nq - p.Hkv) * D;
-        a[e][0] = *reinterpret_cast<const uint4*>(src + 8 * c);
-        a[e][1] = *reinterpret_cast<const uint4*>(src + D / 2 + 8 * c);
+      if (s0 + e < end && r < rows) {
+        const uint16_t* src = r < nq             ? qrow + r * D
+                              : r < nq + p.Hkv ? krow + (r - nq) * D
+                                               : vrow + (r - nq - p.Hkv) * D;
+        a[e][0] = *reinterpret_cast<const uint4*>(src);
+        a[e][1] = *reinterpret_cast<const uint4*>(src + D / 2);
+      }
+    }
+  };
+  const bool early = l < p.L && (!RING || (!p.count && t >= p.T - p.W));
+  if (early) load(first, min(first + per, (all + P::kRows - 1) / P::kRows), all);
+  const int n = count < 0 ? 0 : count < p.T ? static_cast<int>(count) : p.T;
+  if (l < p.L && t < n && !(RING && pos < 0)) {
+    if (p.prep.rope) {
+      const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos + t) +
+                                    static_cast<unsigned long long>(moved);
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) {
+        const int i = lane + 32 * e;
+        reinterpret_cast<float2*>(&table.turn[i % 8 / 2][i / 8])[i % 2] = rope_cos_sin(at, turns[e]);
       }
     }
 #pragma unroll
-    for (int e = 0; e < kPrefillBatch; ++e) {
-      if (s0 + e >= s1) break;
-      const int r = (s0 + e) * P::kRows + sub;
-      const int h = r < nq ? r : r < nq + p.Hkv ? r - nq : r - nq - p.Hkv;
-      const bool is_v = r >= nq + p.Hkv;
-      float x[16];
-      prep_unpack(a[e][0], a[e][1], x);
-      const float* w = is_v ? nullptr : r < nq ? p.prep.q_weight : p.prep.k_weight;
-      float4 gain[4];
-      if (w) prep_gains<D>(w + static_cast<long long>(l) * D, c, gain);
-      prep_norm<D>(x, gain, w != nullptr, p.prep.eps);
-      if (p.prep.rope) prep_rotate(x, cs);
-      if (!is_v) {
-        a[e][0] = prep_pack(x);
-        a[e][1] = prep_pack(x + 8);
+    for (int x = 0; x < 2; ++x) {
+      const float* w = x == 0 ? p.prep.q_weight : p.prep.k_weight;
+      if (w && lane < D / 4)
+        table.gain[x][lane / (D / 8)][lane % 2][lane % (D / 8) / 2] =
+            *reinterpret_cast<const float4*>(w + static_cast<long long>(l) * D + 4 * lane);
+    }
+    __syncwarp();
+    const bool norm = p.prep.q_weight || p.prep.k_weight;
+    // Rows of k and v that the ring does not keep are left out.
+    const bool kept = !RING || t >= n - p.W;
+    long long slot = 0;
+    if (RING && kept) {
+      const unsigned long long at = static_cast<unsigned long long>(pos) + static_cast<unsigned long long>(t);
+      slot = (at >> 32) == 0 ? static_cast<unsigned>(at) % static_cast<unsigned>(p.W)
+                             : static_cast<long long>(at % static_cast<unsigned>(p.W));
+    }
+    const int rows = kept ? all : nq;
+    const int end = min(first + per, (rows + P::kRows - 1) / P::kRows);
+    const long long unit0 = (static_cast<long long>(b) * p.L + l) * p.Hkv;
+    uint16_t* to_q = p.out_q + row0 * p.Hq * D + 8 * c;
+    uint16_t* to_k = RING ? p.ring_k + (unit0 * p.W + slot) * D + 8 * c : p.out_k + row0 * p.Hkv * D + 8 * c;
+    uint16_t* to_v = p.ring_v + (unit0 * p.W + slot) * D + 8 * c;
+    const long long step = RING ? static_cast<long long>(p.W) * D : D;  // from one KV head's row to the next
+    for (int s0 = first; s0 < end; s0 += kPrefillBatch) {
+      if (s0 > first || !early) load(s0, end, rows);
+#pragma unroll
+      for (int e = 0; e < kPrefillBatch; ++e) {
+        if (s0 + e >= end) break;
+        const int r = (s0 + e) * P::kRows + sub;
+        const bool is_v = r >= nq + p.Hkv;
+        const bool is_q = r < nq;
+        float f = 1.f;
+        if (norm) f = prep_rms<D>(a[e], p.prep.eps);
+        if (!is_v)
+          prep_chunks<D>(a[e], (is_q ? p.prep.q_weight : p.prep.k_weight) != nullptr, f, table.gain[is_q ? 0 : 1],
+                         p.prep.rope != 0, table.turn, c);
+        if (r < rows) {
+          uint16_t* dst = r < nq    ? to_q + r * D
+                          : is_v ? to_v + (r - nq - p.Hkv) * step
+                                 : to_k + (r - nq) * step;
+          *reinterpret_cast<uint4*>(dst) = a[e][0];
+          *reinterpret_cast<uint4*>(dst + D / 2) = a[e][1];
+          if (RING && is_v && c == 0 && p.ring_weight) p.ring_weight[(unit0 + r - nq - p.Hkv) * p.W + slot] = 0.f;
+        }
       }
-      if (r < rows) {
-        uint16_t* dst;
-        if (r < nq) dst = p.out_q + (row0 * p.Hq + h) * D;
-        else if (RING) dst = (is_v ? p.ring_v : p.ring_k) + ((unit0 + h) * p.W + slot) * D;
-        else dst = p.out_k + (row0 * p.Hkv + h) * D;
-        *reinterpret_cast<uint4*>(dst + 8 * c) = a[e][0];
-        *reinterpret_cast<uint4*>(dst + D / 2 + 8 * c) = a[e][1];
-        if (RING && is_v && c == 0 && p.ring_weight) p.ring_weight[(unit0 + h) * p.W + slot] = 0.f;
+    }
+  }
+  if (RING) {
+    __syncthreads();  // every thread of the CTA has read pos
+    if (threadIdx.x == 0) {
+      // the last of the sequence's CTAs to come here advances it
+      __threadfence();
+      if (atomicAdd(p.tickets + b, 1ull) + 1 == gridDim.x) {
+        if (pos >= 0) p.pos[b] = pos + n;
+        else atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+        p.tickets[b] = 0ull;
       }
     }
   }

@@ -5,10 +5,6 @@
 //   out_(i+d/2) = y_(i + d/2) cos a_i + y_i sin a_i,   a_i = p theta^(-2i/d)
 // all in fp32; the caller rounds once, to bf16 (a model that rounds between the two has one
 // rounding more).
-//
-// A head's row is taken by d / 16 lanes: lane c of them has 16-byte chunks c and c + d / 16, which are
-// elements 8 c .. 8 c + 7 and their partners d / 2 further on, so that the rotation needs nothing from
-// another lane and the norm one sum over the group.
 #pragma once
 
 #include "cmc_attn.cuh"
@@ -26,78 +22,6 @@ struct PrepParams {
   long long rope_offset;
   unsigned long long rope_turns[64];
 };
-
-template <int D>
-struct Prep {
-  static constexpr int kLanes = D / 16;         // lanes of one row
-  static constexpr int kRows = 32 / kLanes;     // rows that a warp takes at once
-};
-
-// (cos, sin) of the d / 2 pairs at position p, into the warp's table.  The caller's __syncwarp
-// lets the warp read it.
-template <int D>
-__device__ __forceinline__ void prep_table(const PrepParams& p, unsigned long long at, int lane, float2* tab) {
-#pragma unroll
-  for (int e = 0; e < D / 64; ++e) {
-    const int i = lane + 32 * e;
-    const unsigned long long turns =
-        p.rope_slot >= 0 ? g_rope_tables[p.rope_slot][i] : p.rope_turns[i];
-    tab[i] = rope_cos_sin(at, turns);
-  }
-}
-
-// A lane's share of a row of gains.
-template <int D>
-__device__ __forceinline__ void prep_gains(const float* w, int c, float4 (&g)[4]) {
-#pragma unroll
-  for (int e = 0; e < 4; ++e) g[e] = *reinterpret_cast<const float4*>(w + (e >> 1) * (D / 2) + 8 * c + 4 * (e & 1));
-}
-
-// One row's share of a lane: x[0..7] and x[8..15] are elements 8 c .. and d / 2 + 8 c ...  `norm` differs
-// between the rows of a warp, all of whose lanes take part.
-template <int D>
-__device__ __forceinline__ void prep_norm(float (&x)[16], const float4 (&g)[4], bool norm, float eps) {
-  float s = 0.f;
-#pragma unroll
-  for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
-#pragma unroll
-  for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  if (!norm) return;
-  const float r = 1.f / sqrtf(fmaf(s, 1.f / D, eps));
-#pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    x[4 * e + 0] *= r * g[e].x;
-    x[4 * e + 1] *= r * g[e].y;
-    x[4 * e + 2] *= r * g[e].z;
-    x[4 * e + 3] *= r * g[e].w;
-  }
-}
-
-// cs: (cos, sin) of pairs 8 c .. 8 c + 7.
-__device__ __forceinline__ void prep_rotate(float (&x)[16], const float2 (&cs)[8]) {
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const float lo = x[e], hi = x[8 + e];
-    x[e] = fmaf(lo, cs[e].x, -hi * cs[e].y);
-    x[8 + e] = fmaf(hi, cs[e].x, lo * cs[e].y);
-  }
-}
-
-__device__ __forceinline__ void prep_unpack(const uint4& lo, const uint4& hi, float (&x)[16]) {
-  float a[8], b[8];
-  unpack8(lo, a);
-  unpack8(hi, b);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    x[e] = a[e];
-    x[8 + e] = b[e];
-  }
-}
-
-__device__ __forceinline__ uint4 prep_pack(const float* x) {
-  return make_uint4(pack_bf16_rn(x[0], x[1]), pack_bf16_rn(x[2], x[3]), pack_bf16_rn(x[4], x[5]),
-                    pack_bf16_rn(x[6], x[7]));
-}
 
 // ---------------------------------------------------------------------------
 // Host side
