@@ -942,6 +942,7 @@ def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> int:
 # ----------------------------------------------------------------------------
 
 _F32 = torch.float32
+_byref = ctypes.byref
 _weighted_workspaces: Dict[Tuple, Dict[Tuple[int, int], DecodeWorkspace]] = {}
 
 
@@ -996,17 +997,21 @@ def _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, B, L, d, de
         rope_theta = 0.0
     elif not rope_theta > 0:
         raise ValueError("rope_theta must be positive")
-    for t, name in ((q_weight, "q_weight"), (k_weight, "k_weight")):
-        if t is not None:
-            _need(t, name, _F32, 2, dev)
-            if t.shape != (L, d):
-                raise ValueError(f"{name} must be {(L, d)}")
+    qw = kw = moved = 0
+    if q_weight is not None:
+        _need(q_weight, "q_weight", _F32, 2, dev)
+        if q_weight.shape != (L, d):
+            raise ValueError(f"q_weight must be {(L, d)}")
+        qw = q_weight.data_ptr()
+    if k_weight is not None:
+        _need(k_weight, "k_weight", _F32, 2, dev)
+        if k_weight.shape != (L, d):
+            raise ValueError(f"k_weight must be {(L, d)}")
+        kw = k_weight.data_ptr()
     if evicted is not None:
         _need_evicted(evicted, B, dev)
-    return ctypes.byref(CmcQkPrep(0 if q_weight is None else q_weight.data_ptr(),
-                                  0 if k_weight is None else k_weight.data_ptr(),
-                                  0 if evicted is None else evicted.data_ptr(), rope_theta,
-                                  _offset(rope_offset), eps))
+        moved = evicted.data_ptr()
+    return _byref(CmcQkPrep(qw, kw, moved, rope_theta, _offset(rope_offset), eps))
 
 
 def _need_evicted(evicted, B, dev) -> None:
@@ -1045,7 +1050,7 @@ def _need_tokens(t, name, B, L, T, d, dev) -> Tuple[int, int]:
 def _tokens_like(t, shape, name, dev, given):
     """The output of a call for heads of `shape`: the tensor given, checked, or a new one."""
     if given is None:
-        return torch.empty(shape, dtype=torch.bfloat16, device=dev)
+        return torch.empty_like(t) if t.is_contiguous() else torch.empty(shape, dtype=torch.bfloat16, device=dev)
     _need(given, name, torch.bfloat16, len(shape), dev)
     if given.shape != shape:
         raise ValueError(f"{name} must be {tuple(shape)}")
@@ -1309,6 +1314,42 @@ def decode_attn_weighted_plan(dims: CmcDims, fused: bool = True) -> int:
     return int(ctas.value)
 
 
+def _evict_kept(k, v, weight, keep, pos, evicted, out_k, out_v, out_weight, out_pos, key) -> Tuple:
+    """Checks the tensors of an eviction one by one; what the call keeps for shapes like these: (dims by
+    reference, the dims of its workspace, the workspaces by device and stream, dims, the shapes of the outputs' rows and
+    of the index)."""
+    dev = k.device
+    _need(v, "v", torch.bfloat16, 5, dev)
+    if v.shape != k.shape:
+        raise ValueError("v must have the shape of k")
+    _need_weight(weight, "weight", k, dev)
+    B, L, Hkv, T, d = k.shape
+    keep = int(keep)
+    if not 1 <= keep <= T:
+        keep = -1  # refused by the library
+    if pos is not None:
+        _need_pos(pos, B, dev)
+    if evicted is not None:
+        _need_evicted(evicted, B, dev)
+    if out_pos is not None:
+        _need(out_pos, "out_pos", torch.int64, 1, dev)
+        if out_pos.shape[0] != B:
+            raise ValueError("out_pos must be [B]")
+    given = [(t, name, dtype, ndim) for t, name, dtype, ndim in
+             ((out_k, "out_k", torch.bfloat16, 5), (out_v, "out_v", torch.bfloat16, 5),
+              (out_weight, "out_weight", _F32, 4)) if t is not None]
+    for t, name, dtype, ndim in given:
+        _need(t, name, dtype, ndim, dev)
+    want = (B, L, Hkv, given[0][0].shape[3] if given else max(keep, 1), d)
+    for t, name, _, ndim in given:
+        if t.shape != want[:ndim]:
+            raise ValueError(f"{name} must be {want[:ndim]}")
+    dims = CmcDims(B, L, Hkv, Hkv, d, T, keep, want[3])
+    own = CmcDims(B, 1, 1, 1, 64, 1, 0, 1)  # a workspace that goes by the batch size alone
+    kept = (_byref(dims), own, _kept_workspaces(own), dims, want, (B, L, Hkv, max(keep, 0)))
+    return kept if key is None else _kept(key, kept)
+
+
 @_ranged
 def evict_cache(k: torch.Tensor, v: torch.Tensor, weight: torch.Tensor, keep: int, *,
                 pos: Optional[torch.Tensor] = None, recent: int = 0,
@@ -1326,56 +1367,36 @@ def evict_cache(k: torch.Tensor, v: torch.Tensor, weight: torch.Tensor, keep: in
     _need(k, "k", torch.bfloat16, 5)
     dev = k.device
     index = dev.index
-    _need(v, "v", torch.bfloat16, 5, dev)
-    if v.shape != k.shape:
-        raise ValueError("v must have the shape of k")
-    _need_weight(weight, "weight", k, dev)
-    B, L, Hkv, T, d = k.shape
-    keep, recent = _int32(int(keep)), _int32(int(recent))
-    if not 1 <= keep <= T:
-        keep = -1  # refused by the library
-    if pos is not None:
-        _need_pos(pos, B, dev)
-    if evicted is not None:
-        _need_evicted(evicted, B, dev)
-    given = [t for t in (out_k, out_v, out_weight) if t is not None]
-    rows = max(keep, 1)
-    if given:
-        rows = given[0].shape[3] if isinstance(given[0], torch.Tensor) and given[0].dim() in (4, 5) else rows
-    want = (B, L, Hkv, rows, d)
+    kept = key = None
+    try:
+        if (_as(torch.bfloat16, index, v, out_k, out_v) and _as(_F32, index, weight, out_weight)
+                and _as(torch.int64, index, pos, evicted, out_pos)):
+            key = ("evict", k.shape, v.shape, weight.shape, keep, None if out_k is None else out_k.shape,
+                   None if out_v is None else out_v.shape, None if out_weight is None else out_weight.shape,
+                   None if pos is None else pos.shape, None if evicted is None else evicted.shape,
+                   None if out_pos is None else out_pos.shape)
+            kept = _shapes_cache.get(key)
+    except AttributeError:
+        pass
+    if kept is None:
+        kept = _evict_kept(k, v, weight, keep, pos, evicted, out_k, out_v, out_weight, out_pos, key)
+    ref, own, workspaces, _, want, idx_shape = kept
     if out_k is None:
         out_k = torch.empty(want, dtype=torch.bfloat16, device=dev)
     if out_v is None:
         out_v = torch.empty(want, dtype=torch.bfloat16, device=dev)
     if out_weight is None:
         out_weight = torch.empty(want[:4], dtype=_F32, device=dev)
-    if given:
-        for t, name in ((out_k, "out_k"), (out_v, "out_v")):
-            _need(t, name, torch.bfloat16, 5, dev)
-            if t.shape != want:
-                raise ValueError(f"{name} must be {want}")
-        _need_weight(out_weight, "out_weight", out_k, dev)
-    idx = torch.empty((B, L, Hkv, max(keep, 0)), dtype=torch.int32, device=dev)
+    idx = torch.empty(idx_shape, dtype=torch.int32, device=dev)
     if out_pos is None:
-        out_pos = torch.empty(B, dtype=torch.int64, device=dev)
-    else:
-        _need(out_pos, "out_pos", torch.int64, 1, dev)
-        if out_pos.shape[0] != B:
-            raise ValueError("out_pos must be [B]")
-    key = ("evict", k.shape, rows, keep)
-    kept = _shapes_cache.get(key)
-    if kept is None:
-        dims = CmcDims(B, L, Hkv, Hkv, d, T, keep, rows)
-        own = CmcDims(B, 1, 1, 1, 64, 1, 0, 1)  # a workspace that goes by the batch size alone
-        kept = _kept(key, (ctypes.byref(dims), own, _kept_workspaces(own), dims))
-    ref, own, workspaces, _ = kept
+        out_pos = torch.empty(k.shape[0], dtype=torch.int64, device=dev) if pos is None else torch.empty_like(pos)
     stream = _raw_stream(index)
     if workspace is None:
         workspace = _own_workspace(workspaces, index, stream, own)
     elif workspace.index != index:
         raise _elsewhere_workspace(workspace, index)
     fn = lib().cmc_evict_cache
-    args = (k.data_ptr(), v.data_ptr(), weight.data_ptr(), _p(pos), ref, recent, out_k.data_ptr(),
+    args = (k.data_ptr(), v.data_ptr(), weight.data_ptr(), _p(pos), ref, _int32(int(recent)), out_k.data_ptr(),
             out_v.data_ptr(), out_weight.data_ptr(), idx.data_ptr(), out_pos.data_ptr(), _p(evicted),
             workspace.ptr, workspace.nbytes, stream)
     st = fn(*args) if index == _current_device() else _elsewhere(index, fn, *args)

@@ -27,10 +27,35 @@ struct PrepParams {
 // Host side
 // ---------------------------------------------------------------------------
 
-// Checks a cmc_qk_prep (NULL: neither norm nor rotation) and fills in the launch's parameters.
+// The device table of (theta, d), as rope_slot finds it; the last one that a thread asked for is found without its locks
+// (a slot once written stays as it is).
+static int rope_slot_again(double theta, int d, cudaStream_t s, unsigned long long (&turns)[64]) {
+  struct Last {
+    double theta;
+    int d, dev, slot;
+  };
+  static thread_local Last last = {0.0, 0, -1, -1};
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    dev = -1;
+  }
+  if (dev >= 0 && last.dev == dev && last.d == d && last.theta == theta) return last.slot;
+  rope_turns_table(theta, d, turns);
+  const int slot = rope_slot(theta, d, turns, s);
+  if (slot >= 0) last = {theta, d, dev, slot};
+  return slot;
+}
+
+// Checks a cmc_qk_prep (NULL: neither norm nor rotation) and fills in the launch's parameters (rope_turns only where there is
+// no device table).
 static int prep_params(const cmc_qk_prep* q, int d, cudaStream_t s, PrepParams* p) {
-  memset(p, 0, sizeof(*p));
+  p->q_weight = p->k_weight = nullptr;
+  p->evicted = nullptr;
+  p->eps = 0.f;
+  p->rope = 0;
   p->rope_slot = -1;
+  p->rope_offset = 0;
   if (!q) return CMC_OK;
   if (!aligned16(q->q_weight) || !aligned16(q->k_weight) ||
       (reinterpret_cast<uintptr_t>(q->evicted) & 7))
@@ -45,8 +70,7 @@ static int prep_params(const cmc_qk_prep* q, int d, cudaStream_t s, PrepParams* 
     if (q->rope_offset < 0 || q->rope_offset > (1LL << 32)) return CMC_ERR_RANGE;
     p->rope = 1;
     p->rope_offset = q->rope_offset;
-    rope_turns_table(q->rope_theta, d, p->rope_turns);
-    p->rope_slot = rope_slot(q->rope_theta, d, p->rope_turns, s);
+    p->rope_slot = rope_slot_again(q->rope_theta, d, s, p->rope_turns);
   }
   return CMC_OK;
 }
