@@ -21,8 +21,9 @@
  *  - Every tensor argument is a DEVICE pointer to memory the caller owns.  The
  *    library allocates no memory and keeps no state between calls apart from
  *    the thread-local last CUDA error, per-device counts of SMs and of what
- *    they hold of a kernel, the rotary frequency tables of cmc_decode_step_rope
- *    and of cmc_decode_step_q8 (for each at most 16 on the host and 16 per device,
+ *    they hold of a kernel, the rotary frequency tables of cmc_decode_step_rope,
+ *    of cmc_decode_step_q8, of cmc_decode_step_weighted, and of cmc_qk_norm_rope and
+ *    cmc_window_prefill (for each at most 16 on the host and 16 per device,
  *    each written once per (theta, d)), the static score array of cmc_score_select_static and
  *    two process-wide settings of the attention launches
  *    (cmc_set_l2_prefetch_tiles, cmc_test_stall_attention_waits).
@@ -409,7 +410,7 @@ CMC_API int cmc_decode_step_rope(const void* q, const void* tier1_k, const void*
 CMC_API int cmc_read_status(void* workspace, int clear, uint32_t* flags, void* stream);
 
 /* Tuning of the attention launches (cmc_two_tier_decode_attn, cmc_decode_step,
- * cmc_decode_step_rope and those over a cache in 8 bits) made afterwards, from any thread:
+ * cmc_decode_step_rope, those over a cache in 8 bits and those that accumulate weights) made afterwards, from any thread:
  * before its grid dependency wait every CTA asks L2 to prefetch the K/V boxes
  * of its first `tiles` tiles (64 keys each), so that under programmatic
  * dependent launch they stream in while the kernel before it on the stream
@@ -420,8 +421,8 @@ CMC_API int cmc_read_status(void* workspace, int clear, uint32_t* flags, void* s
  * four independent requests' launches ran on four streams (their launches
  * already overlap); with 0, staging copies of 32 KB or more (cmc_stage_copies) also
  * let the launch after them start with their end only.  CMC_ERR_RANGE unless 0 <= tiles <= 64.
- * Over a cache in 8 bits a tile is a block of 32 keys, every warp prefetches, and three are the
- * most it takes. */
+ * Over a cache in 8 bits, and where weights are accumulated, a tile is a block of 32 keys, every warp
+ * prefetches, and three are the most it takes. */
 CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 
 /* Test hook for the failure path of the attention kernels (not part of the
@@ -680,8 +681,9 @@ CMC_API size_t cmc_decode_attn_weighted_workspace_size(const cmc_dims* dims);
  *   workspace                       see cmc_decode_attn_weighted_workspace_size
  *
  * Other arguments as there.  Weights are updated in place, in fp32 and in a fixed order; those of rows that
- * hold no token are neither read nor written.  A NaN among the keys reaches the outputs and the
- * weights of its KV head.  A sequence with pos[b] < 0 gets a zero output, its
+ * hold no token are neither read nor written, and the rows may hold anything.  A score that is NaN or plus infinity gives
+ * NaN in its head's output and in all weights of its KV head; one of minus infinity counts nothing.  A NaN or infinity among the
+ * values reaches the outputs alone.  A sequence with pos[b] < 0 gets a zero output, its
  * weights stay, and CMC_DEVFLAG_BAD_POS is set.
  */
 CMC_API int cmc_two_tier_decode_attn_weighted(const void* q, const void* tier1_k, const void* tier1_v,

@@ -257,6 +257,9 @@ ATTEND = [  # B, L, Hkv, G, d, k, W, positions (cycled)
     (5, 1, 2, 1, 64, 0, 300, [0, -1, 299, 2 ** 33 + 5, 7]), (1, 1, 3, 4, 128, 700, 900, [900]),
     (1, 1, 1, 4, 64, 2048, 2000, [1999]), (40, 2, 8, 4, 64, 30, 40, [3, 39, 40, 100]), (2, 1, 1, 8, 128, 3000, 1, [0, 1]),
     (1, 1, 1, 2, 128, 100, 20000, [19983]),
+    # many short units: a warp each
+    (60, 1, 8, 8, 128, 40, 70, [0, 1, 69, 70, 2 ** 35, -7]), (20, 3, 8, 1, 128, 0, 33, [32, 31, 64]),
+    (58, 1, 8, 2, 64, 250, 220, [219, 5, 64]),
 ]
 
 
@@ -398,6 +401,51 @@ def test_nan_among_the_keys_reaches_its_kv_head_only(cuda_device):
     assert torch.equal(t1[2][1], clean[2][1]) and torch.equal(ring[2][0, 0, 0], clean[5][0, 0, 0])
 
 
+@pytest.mark.parametrize("B, G", [(1, 4), (480, 1), (480, 2)])
+def test_scores_and_values_that_are_not_finite(cuda_device, B, G):
+    """In a CTA's and in a warp's unit: what they reach, and what they leave as it was."""
+    q, t1, ring, pos, _ = attention_problem(cuda_device, (B, 1, 2, G, 64, 40, 50, [50]), 8, poison=False)
+    clean = [x.clone() for x in (*t1, *ring)]
+    want = cmc.two_tier_decode_attn_weighted(q, *clean, pos)
+
+    def run(change):
+        x = [y.clone() for y in (q, *t1, *ring)]
+        change(x)
+        return cmc.two_tier_decode_attn_weighted(*x, pos), x[3], x[6]
+
+    def same(out, w1, w2, heads, kv):
+        """The outputs of `heads`, and the weights of the KV heads `kv`, of sequence 0; everything of the others."""
+        for h in heads:
+            assert torch.equal(out[0, 0, h], want[0, 0, h])
+        for g in kv:
+            assert torch.equal(w1[0, 0, g], clean[2][0, 0, g]) and torch.equal(w2[0, 0, g], clean[5][0, 0, g])
+        assert torch.equal(out[1:], want[1:]) and torch.equal(w1[1:], clean[2][1:]) and torch.equal(w2[1:], clean[5][1:])
+
+    def nan_query(x):
+        x[0][0, 0, 0, 7] = float("nan")
+    out, w1, w2 = run(nan_query)
+    assert out[0, 0, 0].isnan().all() and w1[0, 0, 0].isnan().all() and w2[0, 0, 0].isnan().all()
+    same(out, w1, w2, range(1, 2 * G), [1])
+
+    def infinite_scores(sign):
+        def change(x):
+            x[0][0, 0, :, 3] = 1.0
+            x[1][0, 0, 0, 5, :] = 0.0
+            x[1][0, 0, 0, 5, 3] = sign * float("inf")
+            x[0][0, 0, :, 4:] = 0.0  # so that no infinity meets a zero of the keys, nor an infinity the other sign
+        return change
+    out, w1, w2 = run(infinite_scores(1.0))
+    assert out[0, 0, :G].isnan().all() and w1[0, 0, 0].isnan().all() and not out[0, 0, G:].isnan().any()
+    out, w1, w2 = run(infinite_scores(-1.0))
+    assert not out.isnan().any() and w1[0, 0, 0, 5] == t1[2][0, 0, 0, 5] and (w1[0, 0, 0, :5] > t1[2][0, 0, 0, :5]).all()
+
+    def nan_value(x):
+        x[5][0, 0, 1, 4, 9] = float("nan")
+    out, w1, w2 = run(nan_value)
+    assert out[0, 0, G:, 9].isnan().all() and not out[0, 0, G:, :9].isnan().any()
+    same(out, w1, w2, range(G), [0, 1])
+
+
 @pytest.mark.parametrize("B, H", [(2, 1), (5, 4)])
 def test_units_whose_products_go_to_the_workspace(cuda_device, B, H):
     """G = 8: more than 9,216 keys a unit; with up to a CTA an SM they stay in shared memory all the same."""
@@ -480,6 +528,9 @@ EVICT = [  # B, L, Hkv, d, T, keep, recent, positions (None: all rows)
     (2, 1, 2, 128, 640, 333, 333, [1281, 700]), (1, 1, 2, 128, 4097, 2050, 17, None), (1, 1, 1, 64, 16384, 5000, 100, [16384]),
     (1, 1, 2, 64, 16385, 300, 0, [40000]), (2, 1, 1, 128, 30000, 29999, 1, [30000, 29999]), (30, 4, 8, 64, 33, 16, 3, [33, 20, 70]),
     (2, 1, 1, 64, 50, 20, 4, [-1, 2 ** 40 + 3]),
+    # keys that fill shared memory, and that do not fit; more units than SMs
+    (1, 1, 2, 64, 49152, 100, 7, None), (1, 1, 2, 64, 49153, 20000, 64, [49153]), (2, 1, 1, 64, 100000, 65, 0, [170001, 90000]),
+    (500, 1, 1, 64, 3000, 64, 9, [2999, 70, 5000]),
 ]
 
 
@@ -702,6 +753,32 @@ def test_a_captured_run(cuda_device, given):
             assert torch.equal(x, y), i
     if given:
         assert ws.status() == 0 and not ws.buf.any()
+
+
+def test_a_rotation_first_asked_for_in_a_capture(cuda_device):
+    """A frequency that the device has no table of yet: the captured call carries its own, and gives the bits of the
+    eager ones after it."""
+    g = gen(cuda_device, 23)
+    q, k = randn(g, 2, 1, 5, 8, 64), randn(g, 2, 1, 5, 2, 64)
+    pos = torch.tensor([3, 10 ** 6], device=cuda_device)
+    case = (2, 1, 2, 4, 64, 8, 16, [3, 20])
+    args, t1, ring, p, _ = attention_problem(cuda_device, case, 24, poison=False)
+    new = [randn(g, 2, 1, 2, 64) for _ in range(2)]
+    state = [x.clone() for x in (*t1, *ring, p)]
+    ws = cmc.DecodeWorkspace(cmc.CmcDims(2, 1, 8, 2, 64, 8, 8, 16), cuda_device, weighted=True)
+    theta = 12345.678
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        a = cmc.qk_norm_rope(q, k, pos, rope_theta=theta)
+        b = cmc.decode_step_weighted(args, *t1, *ring, p, *new, rope_theta=theta, workspace=ws)
+    graph.replay()
+    torch.cuda.synchronize()
+    c = cmc.qk_norm_rope(q, k, pos, rope_theta=theta)
+    d = cmc.decode_step_weighted(args, *state, *new, rope_theta=theta)
+    for x, y in zip((*a, b, *t1, *ring, p), (*c, d, *state)):
+        assert torch.equal(x, y)
+    assert ws.status() == 0
 
 
 def test_streams_have_workspaces_of_their_own(cuda_device):
