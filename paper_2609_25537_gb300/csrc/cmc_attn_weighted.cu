@@ -568,6 +568,10 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   }
 
   __syncthreads();
+  // Every thread of the CTA has read pos (and used it); the last of the sequence's CTAs to say so advances it, in the end: the
+  // answer takes a trip to L2.
+  unsigned long long ticket = 0;
+  if (FUSED && tid == 0) ticket = atomicAdd(p.tickets + b, 1ull);
 
   // ---- merge: four columns of one head a thread, the warps in order ----
   constexpr int NGR = G * D / 4;
@@ -667,14 +671,9 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     for (int h = 0; h < G; ++h) sum = fmaf(ex2(fmaf(s[h], p.scale_log2, -M[h])), R[h], sum);
     (blk < p.nb1 ? p.t1w + u * p.N : p.ring_w + u * p.W)[key] = weights[x] + sum;
   }
-  if (FUSED && tid == 0) {
-    // every thread of the CTA has read pos; the last CTA of the sequence to come here advances it (last of
-    // all: the fence and the atomic are two trips to L2)
-    __threadfence();
-    if (atomicAdd(p.tickets + b, 1ull) + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
-      if (!bad) p.pos[b] = pos + 1;
-      p.tickets[b] = 0ull;
-    }
+  if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
+    if (!bad) p.pos[b] = pos + 1;
+    p.tickets[b] = 0ull;
   }
   if (bad && tid == 0 && rank == 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
   if (p.cm > 1) cluster_wait();  // no peer reads this CTA's memory any more

@@ -252,10 +252,13 @@ __device__ __forceinline__ void choose(const EvictParams& p, long long u, const 
   }
 }
 
-// One thread of each of a sequence's CTAs, when all threads of the CTA have read pos: the last to come writes what depends on it.
-__device__ __forceinline__ void held_done(const EvictParams& p, int b, const Held& h) {
-  __threadfence();
-  if (atomicAdd(p.tickets + b, 1ull) + 1 != static_cast<unsigned long long>(p.LH)) return;
+// One thread of each of a sequence's CTAs counts itself when all threads of the CTA have read pos (and used it), and in the end, the
+// answer having taken a trip to L2, the last of them writes what depends on it.
+__device__ __forceinline__ unsigned long long held_read(const EvictParams& p, int b) {
+  return atomicAdd(p.tickets + b, 1ull);
+}
+__device__ __forceinline__ void held_done(const EvictParams& p, int b, const Held& h, unsigned long long ticket) {
+  if (ticket + 1 != static_cast<unsigned long long>(p.LH)) return;
   if (h.bad) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
   if (p.out_pos) p.out_pos[b] = h.bad ? h.pos : h.m;
   if (p.evicted && !h.bad) p.evicted[b] += h.pos - h.m;
@@ -356,8 +359,10 @@ evict_kernel(const __grid_constant__ EvictParams p) {
   const Held h = held_of(p, b);
   choose<kEvictThreads, CACHED>(p, u, h, sm, keys_s);
   __syncthreads();  // the rows are known
+  unsigned long long ticket = 0;
+  if (threadIdx.x == 0) ticket = held_read(p, b);
   copy_rows<D>(p, u, 0, h.m);
-  if (threadIdx.x == 0) held_done(p, b, h);  // (last of all: the fence and the atomic are two trips to L2)
+  if (threadIdx.x == 0) held_done(p, b, h, ticket);
 }
 
 template <bool CACHED>
@@ -373,7 +378,7 @@ evict_choose_kernel(const __grid_constant__ EvictParams p) {
   const Held h = held_of(p, b);
   choose<kChooseThreads, CACHED>(p, u, h, sm, keys_s);
   __syncthreads();
-  if (threadIdx.x == 0) held_done(p, b, h);
+  if (threadIdx.x == 0) held_done(p, b, h, held_read(p, b));
 }
 
 // The copy after evict_choose_kernel, which has written pos already: rows that stay empty are known by their -1.

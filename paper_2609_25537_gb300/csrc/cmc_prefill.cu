@@ -158,7 +158,16 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
   const bool early = l < p.L && (!RING || (!p.count && t >= p.T - p.W));
   if (early) load(first, min(first + per, (all + P::kRows - 1) / P::kRows), all);
   const int n = count < 0 ? 0 : count < p.T ? static_cast<int>(count) : p.T;
-  if (l < p.L && t < n && !(RING && pos < 0)) {
+  const bool live = l < p.L && t < n && !(RING && pos < 0);
+  unsigned long long ticket = 0, tickets = 0;
+  if (RING) {
+    // The sequence's L n tokens, `parts` warps each, are counted where all threads of a CTA have read pos (and used it);
+    // the CTA that completes the count advances it, in the end: the answer takes a trip to L2.
+    tickets = static_cast<unsigned long long>(__syncthreads_count(live && lane == 0));
+    if (threadIdx.x == 0 && tickets != 0) ticket = atomicAdd(p.tickets + b, tickets);
+    if (threadIdx.x == 0 && blockIdx.x == 0 && pos < 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
+  }
+  if (live) {
     if (p.prep.rope) {
       const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos + t) +
                                     static_cast<unsigned long long>(moved);
@@ -216,17 +225,10 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
       }
     }
   }
-  if (RING) {
-    __syncthreads();  // every thread of the CTA has read pos
-    if (threadIdx.x == 0) {
-      // the last of the sequence's CTAs to come here advances it
-      __threadfence();
-      if (atomicAdd(p.tickets + b, 1ull) + 1 == gridDim.x) {
-        if (pos >= 0) p.pos[b] = pos + n;
-        else atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
-        p.tickets[b] = 0ull;
-      }
-    }
+  if (RING && threadIdx.x == 0 && tickets != 0 &&
+      ticket + tickets == static_cast<unsigned long long>(p.L) * static_cast<unsigned>(n) * static_cast<unsigned>(p.parts)) {
+    p.pos[b] = pos + n;
+    p.tickets[b] = 0ull;
   }
 }
 
