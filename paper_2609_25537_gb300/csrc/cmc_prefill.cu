@@ -2,10 +2,10 @@
 // append of their keys and values to the Tier-2 ring (cmc_window_prefill).
 //
 // Bound: HBM, every head's row read once and written once (4 d bytes against some 10 d flops).  A warp takes a
-// token: (cos, sin) of its position and the layer's gains go to shared memory once, then its heads' rows pass through
-// registers.  What limits the rate beside HBM is the instructions of a row (issue slots 70 % taken), so more warps
-// with fewer rows in flight each are better: 8,192 tokens of 32 + 8 heads of 128, us a launch at 4 warps a CTA: two rows a lane
-// group and 8 CTAs an SM 30.3 (83 % of the copy rate), three and 6 33.9, four and 6 33.7.
+// token: what its position and the layer's gains make of a row goes to shared memory once, then its heads' rows pass through
+// registers.  What limits the rate beside HBM is the instructions of a row, and rows on their way: 8 sequences of 4,096 tokens
+// of 32 + 2 x 8 heads of 128 into rings of 2,048 slots, us a launch at two rows a lane group and 8 CTAs of four warps an SM 111 (90 %
+// of the copy rate), three and 6 112, two and 6 120, one and 8 123; 8,192 tokens' queries and keys alone 31.0 (81 %).
 #include "cmc_prep.cuh"
 
 namespace cmc {
@@ -42,51 +42,36 @@ struct Prep {
   static constexpr int kRows = 32 / kLanes;     // rows that a warp takes at once
 };
 
-// What the rows of a token have in common, in shared memory, a warp's own, in the order in which the lanes of a row
-// read it, so that they do not meet in a bank (side by side as the elements are, that was what bound the kernel: 88 % of L1's
+// What the rows of a token have in common, in shared memory, a warp's own: for pair i, with gains g and h of its
+// elements, (g cos a, h sin a, h cos a, g sin a) for the queries and for the keys.  In the order in which the lanes of a row read
+// it, so that they do not meet in a bank (side by side as the elements are, that was what bound the kernel: 88 % of L1's
 // rate, 42 us for 8,192 tokens of 32 + 8 heads).
 template <int D>
 struct __align__(16) TokenTable {
-  static constexpr int kL = Prep<D>::kLanes;
-  float4 turn[4][kL];        // [j][c]: (cos, sin) of pairs 8 c + 2 j and + 1
-  float4 gain[2][2][2][kL];  // of the queries, of the keys: [half][q][c]: elements 8 c + 4 q .. + 3 of a half
+  float4 pair[2][8][Prep<D>::kLanes];  // [queries, keys][e][c]: pair 8 c + e
 };
 
-// Two chunks of a row, normed by r times the gains (where NORM; a row without gains has r = 1 and takes none) and turned.
-// Four elements and their partners at a time: the registers go to rows on the way.
+// Two chunks of a row: x' = r (x g cos - y h sin), y' = r (y h cos + x g sin) with rotation, r x g and r y h without.
 template <int D>
-__device__ __forceinline__ void prep_chunks(uint4 (&a)[2], bool norm, float r, const float4 (&gain)[2][2][Prep<D>::kLanes],
-                                            bool rope, const float4 (&turn)[4][Prep<D>::kLanes], int c) {
+__device__ __forceinline__ void prep_chunks(uint4 (&a)[2], float r, bool rope, const float4 (&pair)[8][Prep<D>::kLanes], int c) {
   uint32_t* lo = reinterpret_cast<uint32_t*>(&a[0]);
   uint32_t* hi = reinterpret_cast<uint32_t*>(&a[1]);
 #pragma unroll
-  for (int q = 0; q < 2; ++q) {
-    float x[4] = {bf16lo_to_f32(lo[2 * q]), bf16hi_to_f32(lo[2 * q]), bf16lo_to_f32(lo[2 * q + 1]), bf16hi_to_f32(lo[2 * q + 1])};
-    float y[4] = {bf16lo_to_f32(hi[2 * q]), bf16hi_to_f32(hi[2 * q]), bf16lo_to_f32(hi[2 * q + 1]), bf16hi_to_f32(hi[2 * q + 1])};
-    if (norm) {
-      const float4 g = gain[0][q][c], h = gain[1][q][c];
-      x[0] *= r * g.x; x[1] *= r * g.y; x[2] *= r * g.z; x[3] *= r * g.w;
-      y[0] *= r * h.x; y[1] *= r * h.y; y[2] *= r * h.z; y[3] *= r * h.w;
-    }
-    if (rope) {
+  for (int q = 0; q < 4; ++q) {
+    float x[2] = {bf16lo_to_f32(lo[q]), bf16hi_to_f32(lo[q])}, y[2] = {bf16lo_to_f32(hi[q]), bf16hi_to_f32(hi[q])};
 #pragma unroll
-      for (int e = 0; e < 4; e += 2) {
-        const float4 t = turn[2 * q + e / 2][c];
-        const float x0 = x[e], x1 = x[e + 1];
-        x[e] = fmaf(x0, t.x, -y[e] * t.y);
-        y[e] = fmaf(y[e], t.x, x0 * t.y);
-        x[e + 1] = fmaf(x1, t.z, -y[e + 1] * t.w);
-        y[e + 1] = fmaf(y[e + 1], t.z, x1 * t.w);
-      }
+    for (int e = 0; e < 2; ++e) {
+      const float4 t = pair[2 * q + e][c];
+      const float u = x[e], v = y[e];
+      x[e] = r * (rope ? fmaf(u, t.x, -v * t.y) : u * t.x);
+      y[e] = r * (rope ? fmaf(v, t.z, u * t.w) : v * t.z);
     }
-    lo[2 * q] = pack_bf16_rn(x[0], x[1]);
-    lo[2 * q + 1] = pack_bf16_rn(x[2], x[3]);
-    hi[2 * q] = pack_bf16_rn(y[0], y[1]);
-    hi[2 * q + 1] = pack_bf16_rn(y[2], y[3]);
+    lo[q] = pack_bf16_rn(x[0], x[1]);
+    hi[q] = pack_bf16_rn(y[0], y[1]);
   }
 }
 
-// 1 / sqrt(mean of squares + eps) of a row, given to all of its lanes.
+// 1 / sqrt(mean of squares + eps) of a row, given to all of its lanes (rsqrtf: 2^-22).
 template <int D>
 __device__ __forceinline__ float prep_rms(const uint4 (&a)[2], float eps) {
   float s = 0.f;
@@ -99,7 +84,7 @@ __device__ __forceinline__ float prep_rms(const uint4 (&a)[2], float eps) {
   }
 #pragma unroll
   for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  return 1.f / sqrtf(fmaf(s, 1.f / D, eps));
+  return rsqrtf(fmaf(s, 1.f / D, eps));
 }
 
 // A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.
@@ -168,24 +153,23 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
     if (threadIdx.x == 0 && blockIdx.x == 0 && pos < 0) atomicOr(p.status, CMC_DEVFLAG_BAD_POS);
   }
   if (live) {
-    if (p.prep.rope) {
-      const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos + t) +
-                                    static_cast<unsigned long long>(moved);
+    const bool rope = p.prep.rope != 0, norm = p.prep.q_weight || p.prep.k_weight;
+    const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos + t) +
+                                  static_cast<unsigned long long>(moved);
+    if (rope || norm) {
 #pragma unroll
       for (int e = 0; e < D / 64; ++e) {
         const int i = lane + 32 * e;
-        reinterpret_cast<float2*>(&table.turn[i % 8 / 2][i / 8])[i % 2] = rope_cos_sin(at, turns[e]);
-      }
-    }
+        const float2 cs = rope ? rope_cos_sin(at, turns[e]) : make_float2(1.f, 0.f);
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const float* w = x == 0 ? p.prep.q_weight : p.prep.k_weight;
-      if (w && lane < D / 4)
-        table.gain[x][lane / (D / 8)][lane % 2][lane % (D / 8) / 2] =
-            *reinterpret_cast<const float4*>(w + static_cast<long long>(l) * D + 4 * lane);
+        for (int x = 0; x < 2; ++x) {
+          const float* w = x == 0 ? p.prep.q_weight : p.prep.k_weight;
+          const float g = w ? w[static_cast<long long>(l) * D + i] : 1.f, h = w ? w[static_cast<long long>(l) * D + D / 2 + i] : 1.f;
+          table.pair[x][i % 8][i / 8] = make_float4(g * cs.x, h * cs.y, h * cs.x, g * cs.y);
+        }
+      }
+      __syncwarp();
     }
-    __syncwarp();
-    const bool norm = p.prep.q_weight || p.prep.k_weight;
     // Rows of k and v that the ring does not keep are left out.
     const bool kept = !RING || t >= n - p.W;
     long long slot = 0;
@@ -210,10 +194,11 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
         const bool is_v = r >= nq + p.Hkv;
         const bool is_q = r < nq;
         float f = 1.f;
-        if (norm) f = prep_rms<D>(a[e], p.prep.eps);
-        if (!is_v)
-          prep_chunks<D>(a[e], (is_q ? p.prep.q_weight : p.prep.k_weight) != nullptr, f, table.gain[is_q ? 0 : 1],
-                         p.prep.rope != 0, table.turn, c);
+        if (norm) {
+          f = prep_rms<D>(a[e], p.prep.eps);
+          if ((is_q ? p.prep.q_weight : p.prep.k_weight) == nullptr) f = 1.f;
+        }
+        if ((rope || norm) && !is_v) prep_chunks<D>(a[e], f, rope, table.pair[is_q ? 0 : 1], c);
         if (r < rows) {
           uint16_t* dst = r < nq    ? to_q + r * D
                           : is_v ? to_v + (r - nq - p.Hkv) * step
