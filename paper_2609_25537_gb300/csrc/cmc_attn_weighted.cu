@@ -115,9 +115,9 @@ __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_gr
 // those is then 0 and NaN).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-__device__ __forceinline__ float ld_peer_f32(uint32_t addr) {
-  float v;
-  asm volatile("ld.shared::cluster.f32 %0, [%1];\n" : "=f"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ float2 ld_peer_f2(uint32_t addr) {
+  float2 v;
+  asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];\n" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ float4 ld_peer_f4(uint32_t addr) {
@@ -615,26 +615,40 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     const uint32_t o_a = smem_addr(rec_o), ml_a = smem_addr(rec_ml);
     const int SL = (NGR + p.cm - 1) / p.cm;
     const int x1 = min((rank + 1) * SL, NGR);
+    // A head's maximum and sum, and what each rank's share of it counts; all ranks' are requested at once (one after the other
+    // they were 2 us of a cluster of eight).
+    float f[kMaxClusterCtas];
     auto merged = [&](int hh, float& M, float& Ls) {
-      M = -INFINITY;
-      Ls = 0.f;
-      for (int r = 0; r < p.cm; ++r) M = fmaxf(M, ld_peer_f32(peer_smem(ml_a + 8 * hh, r)));
+      float2 ml[kMaxClusterCtas];
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r)
+        ml[r] = r < p.cm ? ld_peer_f2(peer_smem(ml_a + 8 * hh, r)) : make_float2(-INFINITY, 0.f);
+      M = ml[0].x;
+#pragma unroll
+      for (int r = 1; r < kMaxClusterCtas; ++r) M = fmaxf(M, ml[r].x);
       M = finite_max(M);
-      for (int r = 0; r < p.cm; ++r)
-        Ls = fmaf(ex2(ld_peer_f32(peer_smem(ml_a + 8 * hh, r)) - M), ld_peer_f32(peer_smem(ml_a + 8 * hh + 4, r)), Ls);
+      Ls = 0.f;
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r) {
+        f[r] = ex2(ml[r].x - M);
+        Ls = fmaf(f[r], ml[r].y, Ls);
+      }
     };
     for (int x = rank * SL + tid; x < x1; x += kThreadsOfCta) {
       const int hh = (4 * x) / D, c = (4 * x) % D;
+      float4 y[kMaxClusterCtas];
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r)
+        y[r] = r < p.cm ? ld_peer_f4(peer_smem(o_a + (hh * D + c) * 4, r)) : make_float4(0.f, 0.f, 0.f, 0.f);
       float M, Ls;
       merged(hh, M, Ls);
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int r = 0; r < p.cm; ++r) {
-        const float f = ex2(ld_peer_f32(peer_smem(ml_a + 8 * hh, r)) - M);
-        const float4 y = ld_peer_f4(peer_smem(o_a + (hh * D + c) * 4, r));
-        acc.x = fmaf(f, y.x, acc.x);
-        acc.y = fmaf(f, y.y, acc.y);
-        acc.z = fmaf(f, y.z, acc.z);
-        acc.w = fmaf(f, y.w, acc.w);
+#pragma unroll
+      for (int r = 0; r < kMaxClusterCtas; ++r) {
+        acc.x = fmaf(f[r], y[r].x, acc.x);
+        acc.y = fmaf(f[r], y[r].y, acc.y);
+        acc.z = fmaf(f[r], y[r].z, acc.z);
+        acc.w = fmaf(f[r], y[r].w, acc.w);
       }
       const float inv = Ls == 0.f ? 0.f : 1.f / Ls;
       *reinterpret_cast<uint2*>(p.out + out_base + hh * D + c) =
