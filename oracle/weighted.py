@@ -6,6 +6,8 @@ indices, counts and the rounding to bf16 that a stored key has."""
 
 from __future__ import annotations
 
+import decimal
+import functools
 import math
 
 import numpy as np
@@ -19,6 +21,16 @@ def to_bf16(x):
     return np.rint(x / step) * step
 
 
+@functools.lru_cache(maxsize=8)
+def turns_of(theta, h):
+    """theta^(-i/h) / (2 pi) of i = 0 .. h - 1, in units of 2^-128."""
+    with decimal.localcontext() as c:
+        c.prec = 60
+        two_pi = 2 * decimal.Decimal("3.14159265358979323846264338327950288419716939937510582097494459")
+        ln = decimal.Decimal(theta).ln()
+        return [int((-ln * i / h).exp() / two_pi * (1 << 128) + decimal.Decimal("0.5")) for i in range(h)]
+
+
 def heads(x, weight=None, eps=1e-6, theta=None, p=None):
     """x [..., H, d] with gains `weight` [..., d] (one for each leading index, None: no norm), turned at positions
     p [...] (integers) where theta is given."""
@@ -28,12 +40,12 @@ def heads(x, weight=None, eps=1e-6, theta=None, p=None):
         y = y / np.sqrt((y * y).mean(axis=-1, keepdims=True) + eps) * np.asarray(weight, dtype=np.float64)[..., None, :]
     if theta is not None:
         h = d // 2
-        turns = np.array([float(theta) ** (-i / h) / (2 * math.pi) for i in range(h)])
-        # the fractional turn, with p split so that each product is exact enough
-        p = np.asarray(p, dtype=np.int64)
-        hi, lo = p >> 16, p & 0xFFFF
-        t16 = np.array([math.fmod(t * 65536.0, 1.0) for t in turns])
-        a = 2 * math.pi * np.mod(np.mod(hi[..., None] * t16, 1.0) + lo[..., None] * turns, 1.0)
+        shape = np.shape(p)
+        # the fractional turn, in integers: a position of 2^40 takes more digits of the frequency than a double has
+        turns = turns_of(float(theta), h)
+        each, place = np.unique(np.asarray(p, dtype=np.int64), return_inverse=True)
+        a = np.array([[int(v) * f % (1 << 128) / (1 << 128) for f in turns] for v in each]).reshape(len(each), h)
+        a = 2 * math.pi * a[place.reshape(shape)]
         c, s = np.cos(a)[..., None, :], np.sin(a)[..., None, :]
         y = np.concatenate([y[..., :h] * c - y[..., h:] * s, y[..., h:] * c + y[..., :h] * s], axis=-1)
     return y
