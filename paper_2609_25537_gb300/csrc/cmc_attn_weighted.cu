@@ -33,6 +33,7 @@
 namespace cmc {
 
 constexpr int kBlkKeys = 32;
+constexpr int kWarpsMost = 4;  // of a CTA
 // Products and weights that a CTA keeps in shared memory, in bytes: as many as leave two CTAs of four warps on an SM.
 // Units too long for a cluster of eight at that keep them in the workspace (us a launch at 40 KB / 64 KB / 10 KB: 64 units of
 // 16,384 keys 79 / 98 / 103, of 20,480 keys 125 / 152 / 126), but where there is no more than a CTA an SM.
@@ -56,7 +57,7 @@ struct WeightedParams {
   uint32_t* status;
   unsigned long long* tickets;
   float* scratch;         // products of a unit too long for shared memory, or NULL
-  int L, Hkv, N, k, W, LH;
+  int B, L, Hkv, N, k, W, LH;
   int cm;                 // CTAs per unit
   int nb1;                // blocks of Tier-1
   int iters;              // blocks a warp takes at most
@@ -288,7 +289,7 @@ struct Preparer {
 };
 
 // NW warps a CTA, whose registers allow twelve on an SM.
-template <int D, int G, bool FUSED, bool PREP, int NW>
+template <int D, int G, bool FUSED, bool PREP, int NW, bool ORDER>
 __global__ void __launch_bounds__(32 * NW, 12 / NW)
 weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   using S = WSmem<D, G, PREP, NW>;
@@ -304,14 +305,14 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   float* fin_r = fin_m + 8;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int g = lane >> 2, t = lane & 3;
-  const long long u = blockIdx.x / static_cast<unsigned>(p.cm);
+  long long u = blockIdx.x / static_cast<unsigned>(p.cm);
   const int rank = static_cast<int>(blockIdx.x - u * p.cm);
-  const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
+  int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
   const int stride = p.cm * NW;
   const int first = rank * NW + warp;
 
-  // The warp's first blocks, into L2: hints, which may come before the wait.
-  if (lane < 2 * p.prefetch) {
+  // The warp's first blocks, into L2: hints, which may come before the wait (where the unit is known).
+  if (!ORDER && lane < 2 * p.prefetch) {
     const int blk = first + (lane >> 1) * stride;
     const uint16_t* base = nullptr;
     int rows = 0;
@@ -329,6 +330,36 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   if (PREP) prep.tables(p, lane);  // written long before this launch
   pdl_wait();
   pdl_trigger();
+  if (ORDER) {
+    // The unit of place u / LH in the sequences' order by length, the longest first: a long unit that starts last sets the
+    // time of the launch.  All CTAs see the same positions, which the last of them advances in the end.
+    int* live = reinterpret_cast<int*>(smem);  // of the stages, which hold nothing yet
+    int* seq = live + kThreadsOfCta;
+    int mine = -2;
+    if (tid < p.B) {
+      long long x;
+      asm volatile("ld.global.cg.s64 %0, [%1];\n" : "=l"(x) : "l"(p.pos + tid) : "memory");
+      mine = static_cast<int>(x < 0 ? -1 : x < p.W ? x : p.W);
+    }
+    live[tid] = mine;
+    __syncthreads();
+    if (tid < p.B) {
+      int place = 0;
+#pragma unroll 4
+      for (int i = 0; i < p.B; i += 4) {
+        const int4 x = *reinterpret_cast<const int4*>(live + i);
+        place += (x.x > mine || (x.x == mine && i < tid)) + (x.y > mine || (x.y == mine && i + 1 < tid)) +
+                 (x.z > mine || (x.z == mine && i + 2 < tid)) + (x.w > mine || (x.w == mine && i + 3 < tid));
+      }
+      if (place == b) *seq = tid;
+    }
+    __syncthreads();
+    // (A reduction, so that the compiler knows the sequence for the same in all lanes.)
+    const int s0 = static_cast<int>(__reduce_max_sync(0xffffffffu, static_cast<unsigned>(*seq)));
+    __syncthreads();
+    u += static_cast<long long>(s0 - b) * p.LH;
+    b = s0;
+  }
 
   long long pos;
   asm volatile("ld.global.cg.s64 %0, [%1];\n" : "=l"(pos) : "l"(p.pos + b) : "memory");
@@ -571,7 +602,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   // Every thread of the CTA has read pos (and used it); the last of the sequence's CTAs to say so advances it, in the end: the
   // answer takes a trip to L2.
   unsigned long long ticket = 0;
-  if (FUSED && tid == 0) ticket = atomicAdd(p.tickets + b, 1ull);
+  if (FUSED && tid == 0) ticket = atomicAdd(p.tickets + (ORDER ? 0 : b), 1ull);
 
   // ---- merge: four columns of one head a thread, the warps in order ----
   constexpr int NGR = G * D / 4;
@@ -685,7 +716,18 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     for (int h = 0; h < G; ++h) sum = fmaf(ex2(fmaf(s[h], p.scale_log2, -M[h])), R[h], sum);
     (blk < p.nb1 ? p.t1w + u * p.N : p.ring_w + u * p.W)[key] = weights[x] + sum;
   }
-  if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
+  if (FUSED && ORDER) {
+    if (warp == 0) {
+      ticket = __shfl_sync(0xffffffffu, ticket, 0);
+      if (ticket + 1 == gridDim.x) {
+        for (int i = lane; i < p.B; i += 32) {
+          const long long x = *static_cast<volatile int64_t*>(p.pos + i);
+          if (x >= 0) p.pos[i] = x + 1;
+        }
+        if (lane == 0) p.tickets[0] = 0ull;
+      }
+    }
+  } else if (FUSED && tid == 0 && ticket + 1 == static_cast<unsigned long long>(p.LH) * p.cm) {
     if (!bad) p.pos[b] = pos + 1;
     p.tickets[b] = 0ull;
   }
@@ -705,7 +747,6 @@ static long long iters_of(const cmc_dims& m, int warps) { return (blocks_of(m) +
 static size_t score_bytes(const cmc_dims& m, int cm, int nw) {
   return static_cast<size_t>(iters_of(m, cm * nw)) * nw * kBlkKeys * (m.Hq / m.Hkv + 1) * 4;
 }
-constexpr int kWarpsMost = 4;  // of a CTA
 static bool needs_scratch(const cmc_dims& m) { return score_bytes(m, kMaxClusterCtas, kWarpsMost) > static_cast<size_t>(score_cap(m.Hq / m.Hkv)); }
 static size_t weighted_ws(const cmc_dims& m) {
   const size_t units = static_cast<size_t>(m.B) * m.L * m.Hkv;
@@ -731,10 +772,10 @@ static int plan_cm(const cmc_dims& m, int per_sm, int fixed_smem) {
   return cm;
 }
 
-template <int D, int G, bool FUSED, bool PREP, int NW>
+template <int D, int G, bool FUSED, bool PREP, int NW, bool ORDER>
 static int per_sm_of(int* out) {
   constexpr int smem = WSmem<D, G, PREP, NW>::kScores + kScoreMost;
-  auto kern = weighted_attn_kernel<D, G, FUSED, PREP, NW>;
+  auto kern = weighted_attn_kernel<D, G, FUSED, PREP, NW, ORDER>;
   static std::atomic<int> known[64];
   int dev = 0;
   int st = record_cuda_error(cudaGetDevice(&dev));
@@ -752,7 +793,7 @@ static int per_sm_of(int* out) {
   return CMC_OK;
 }
 
-template <int D, int G, bool FUSED, bool PREP, int NW>
+template <int D, int G, bool FUSED, bool PREP, int NW, bool ORDER>
 static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cudaStream_t s) {
   p.cm = cm;
   p.iters = static_cast<int>(iters_of(m, cm * NW));
@@ -775,7 +816,7 @@ static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cuda
   cfg.stream = s;
   cfg.attrs = attr;
   cfg.numAttrs = cm > 1 ? 2 : 1;
-  return record_cuda_error(cudaLaunchKernelEx(&cfg, weighted_attn_kernel<D, G, FUSED, PREP, NW>, p));
+  return record_cuda_error(cudaLaunchKernelEx(&cfg, weighted_attn_kernel<D, G, FUSED, PREP, NW, ORDER>, p));
 }
 
 // A CTA of four warps a unit, or a cluster of them; a warp a unit where there are more units than CTAs are resident
@@ -784,10 +825,14 @@ static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cuda
 //  1,024        18.2 / 13.5   28.8 / 22.2   42.8 / 29.4   58.6 / 64.8
 //  2,048        31.6 / 27.7   50.4 / 44.3   77.6 / 57.5  106.1 / 107.1
 //    256         6.5 /  8.7    8.3 / 18.2    9.8 / 21.9   14.7 / 27.9)
+// Several waves of CTAs of four warps start with the longest sequences (ORDER): ordering them, a thread a sequence, costs a CTA
+// a microsecond and the prefetch before the wait, so that calls of equal lengths lose by it where clusters are used.  (us a
+// launch without / with it, G = 4: 64 sequences x 8 heads of 256 + 128..2,048 keys 50.3 / 43.7, 32 + 60..1,000 25.0 / 19.5,
+// 8 x 8 of 256 + 1,024..16,384 37.8 / 33.4; 64 units of 16,384 77.9 / 85.4, 512 of 6,144 246 / 250.)
 template <int D, int G, bool FUSED, bool PREP>
 static int launch_weighted(WeightedParams& p, const cmc_dims& m, cudaStream_t s, int* ctas) {
   int per_sm = 1;
-  int st = per_sm_of<D, G, FUSED, PREP, kWarpsMost>(&per_sm);
+  int st = per_sm_of<D, G, FUSED, PREP, kWarpsMost, false>(&per_sm);
   if (st != CMC_OK) return st;
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
   const bool solo = units > static_cast<long long>(per_sm) * sm_count() && blocks_of(m) <= kSoloBlocks;
@@ -796,9 +841,15 @@ static int launch_weighted(WeightedParams& p, const cmc_dims& m, cudaStream_t s,
     *ctas = static_cast<int>(units * cm);
     return CMC_OK;
   }
-  if (!solo) return launch_weighted_cm<D, G, FUSED, PREP, kWarpsMost>(p, m, cm, s);
-  st = per_sm_of<D, G, FUSED, PREP, 1>(&per_sm);
-  return st != CMC_OK ? st : launch_weighted_cm<D, G, FUSED, PREP, 1>(p, m, cm, s);
+  if (solo) {
+    st = per_sm_of<D, G, FUSED, PREP, 1, false>(&per_sm);
+    return st != CMC_OK ? st : launch_weighted_cm<D, G, FUSED, PREP, 1, false>(p, m, cm, s);
+  }
+  if (units * cm > static_cast<long long>(per_sm) * sm_count() && m.B > 1 && m.B <= 32 * kWarpsMost) {
+    st = per_sm_of<D, G, FUSED, PREP, kWarpsMost, true>(&per_sm);
+    return st != CMC_OK ? st : launch_weighted_cm<D, G, FUSED, PREP, kWarpsMost, true>(p, m, cm, s);
+  }
+  return launch_weighted_cm<D, G, FUSED, PREP, kWarpsMost, false>(p, m, cm, s);
 }
 
 template <bool FUSED, bool PREP>
@@ -865,7 +916,7 @@ static int run_weighted(const void* q, const void* t1k, const void* t1v, float* 
   p.status = reinterpret_cast<uint32_t*>(ws);
   p.tickets = reinterpret_cast<unsigned long long*>(ws + kWsHeader);
   p.scratch = reinterpret_cast<float*>(ws + ws_partials_off(m.B));
-  p.L = m.L; p.Hkv = m.Hkv; p.N = m.N; p.k = m.k; p.W = m.W; p.LH = m.L * m.Hkv;
+  p.B = m.B; p.L = m.L; p.Hkv = m.Hkv; p.N = m.N; p.k = m.k; p.W = m.W; p.LH = m.L * m.Hkv;
   p.cm = 1;
   p.nb1 = (m.k + kBlkKeys - 1) / kBlkKeys;
   const float sc = scale > 0.f ? scale : 1.0f / sqrtf(static_cast<float>(m.d));
