@@ -2,14 +2,16 @@
 // head) unit the heaviest and the youngest tokens are kept and moved together, in order of age.
 //
 // Bound: HBM, the kept rows read and written (8 d bytes each) beside 4 bytes a token to choose by.  Two parts.  The
-// choice of a unit is a CTA's: the order-preserving 32-bit keys of its tokens' weights go to shared memory, a radix select of up to three passes
-// (11, 11 and 10 bits) finds the threshold, and every kept token gets its number from what the warps and lanes
-// before it keep.  The copy moves blocks of rows.  Enough units for the SMs: a CTA of 256 threads does both, its copy beside
-// others' choices (256 units of 512 tokens, 256 kept: 16.8 us, of which the choice is 3.5, in all CTAs at once; 10.2 at the copy
-// rate).  Few long ones: a kernel of CTAs of 1,024 threads chooses, and a second one copies with
-// all SMs: 64 units of 16,384 tokens, 2,048 kept, 36 us, 11 and 20 of them the two kernels', 20.9 at the copy rate.  (Both in clusters of
-// four: 38.8 where the CTAs summed their histograms in distributed shared memory, which alone took 2.7 a pass, and
-// 42 where each chose by itself.)
+// choice of a unit is a CTA's: the order-preserving 32-bit keys of its tokens' weights go to shared memory, a radix
+// select of up to three passes (11, 11 and 10 bits) finds the threshold, and every kept token gets its number from
+// what the warps and lanes before it keep.  The copy moves blocks of rows.  Enough units for the SMs: a CTA of 256
+// threads does both, its copy beside others' choices and the youngest rows, which need none, on their way to L2
+// meanwhile (256 units of 512 tokens, 256 kept, 64 of them for their age: 15.1 us, without that prefetch 15.8; the
+// choice is 3.5, in all CTAs at once; 10.2 at the copy rate).  Few long ones: a kernel of CTAs of 1,024 threads
+// chooses, and a second one copies with all SMs: 64 units of 16,384 tokens, 2,048 kept, 35 us, 11 and 20 of them the
+// two kernels', 20.9 at the copy rate.  (Both in clusters of four: 38.8 where the CTAs summed their histograms in
+// distributed shared memory, which alone took 2.7 a pass, and 42 where each chose by itself; 38.7 with the rows above
+// the first pass's bin prefetched one by one.)
 //
 // The i-th token kept is never older than the i-th of all, so in place (output and input the same tensors, the oldest
 // token in row 0) a row is written only where rows of the same or of earlier blocks were read, and a barrier over the
@@ -25,6 +27,7 @@ constexpr int kEvictThreads = 256;   // of a CTA that copies
 constexpr int kChooseThreads = 1024;  // of one that only chooses
 constexpr int kEvictBatch = 4;       // rows of K and of V that a thread has in flight
 constexpr int kEvictBins = 2048;     // 11 bits a pass
+constexpr int kEvictAhead = 65536;   // bytes of K, and of V, of a unit that are prefetched into L2
 constexpr int kEvictKeys = 49152;    // keys held in shared memory; of longer units the weights are read again
 
 struct EvictParams {
@@ -345,6 +348,18 @@ __device__ __forceinline__ void copy_rows(const EvictParams& p, long long u, int
   }
 }
 
+// The rows that stay whatever the weights are, the youngest, into L2 while the others are chosen: one of four threads takes K or
+// V, and the rows before the ring's end or those behind it.
+template <int D>
+__device__ __forceinline__ void prefetch_young(const EvictParams& p, long long u, const Held& h, int part) {
+  const int rows = min(h.young, kEvictAhead / (2 * D));
+  const int r0 = h.old + h.f >= p.T ? h.old + h.f - p.T : h.old + h.f;
+  const int to_end = min(rows, p.T - r0);
+  const int n = part & 2 ? rows - to_end : to_end;
+  const uint16_t* base = (part & 1 ? p.v : p.k) + (u * p.T + (part & 2 ? 0 : r0)) * D;
+  if (n > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(base), "r"(n * D * 2) : "memory");
+}
+
 // A unit's choice and copy.
 template <int D, bool CACHED>
 __global__ void __launch_bounds__(kEvictThreads, 2)
@@ -357,6 +372,7 @@ evict_kernel(const __grid_constant__ EvictParams p) {
   pdl_wait();
   pdl_trigger();
   const Held h = held_of(p, b);
+  if (threadIdx.x >= kEvictThreads - 4 && h.need != 0 && h.need != h.old) prefetch_young<D>(p, u, h, threadIdx.x & 3);
   choose<kEvictThreads, CACHED>(p, u, h, sm, keys_s);
   __syncthreads();  // the rows are known
   unsigned long long ticket = 0;
