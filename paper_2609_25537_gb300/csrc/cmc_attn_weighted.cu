@@ -7,7 +7,7 @@
 // beside the key's 4 d bytes in HBM), and when its unit's M and l are known goes over them once more.
 //
 // Bound: HBM, 4 d + 8 bytes a key against 4 G d flops.  A unit (sequence, layer, KV head) is taken by a CTA of
-// four warps, a cluster of up to eight such CTAs, or, where there are many short ones, by one warp.  Its keys are cut
+// four warps, a cluster of up to eight such CTAs, or, where there are many short ones, by one warp or two.  Its keys are cut
 // into blocks of 32, ceil(k / 32) of Tier-1, then those of the ring's occupied slots, and warp w of the unit's n takes
 // blocks w, w + n, ...  The warps have nothing to do with each other until the end: each copies its own blocks' rows (cp.async,
 // 16 bytes a lane) into a stage of its own, K and V of one block, and requests the next block's K as soon as the products
@@ -39,7 +39,7 @@ constexpr int kWarpsMost = 4;  // of a CTA
 // 16,384 keys 79 / 98 / 103, of 20,480 keys 125 / 152 / 126), but where there is no more than a CTA an SM.
 constexpr int score_cap(int G) { return G == 8 ? 41472 : 46080; }
 constexpr int kScoreMost = 131072;
-// Blocks of a unit that is given to one warp, at most (see launch_weighted).
+// Blocks of a unit that is given to one warp or two, at most (see launch_weighted).
 constexpr int kSoloBlocks = 16;
 
 struct WeightedParams {
@@ -377,7 +377,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   if (PREP) prep.request(p, u, b, warp, lane);
   // Blocks of Tier-1 do not wait for pos.
   const uint64_t pol = policy_evict_first();
-  // The products of this CTA's keys, [iteration][warp][16 keys][G], then their weights, [iteration][warp][16 keys].
+  // The products of this CTA's keys, [iteration][warp][32 keys][G], then their weights, [iteration][warp][32 keys].
   const int slots = p.iters * NW * kBlkKeys;
   float* scores = p.scratch ? p.scratch + static_cast<long long>(blockIdx.x) * slots * (G + 1)
                             : reinterpret_cast<float*>(smem + S::kScores);
@@ -703,7 +703,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     M[h] = fin_m[h];
     R[h] = fin_r[h];
   }
-  // Key x is row x % 16 of the block that warp x / 16 % 8 took in iteration x / 128.
+  // Key x is row x % 32 of the block that warp x / 32 % NW took in iteration x / (32 NW).
   const int iters = nblk > rank * NW ? (nblk - rank * NW + stride - 1) / stride : 0;
   for (int x = tid; x < iters * NW * kBlkKeys; x += kThreadsOfCta) {
     const int blk = rank * NW + x / kBlkKeys % NW + x / (kBlkKeys * NW) * stride;
@@ -819,12 +819,17 @@ static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cuda
   return record_cuda_error(cudaLaunchKernelEx(&cfg, weighted_attn_kernel<D, G, FUSED, PREP, NW, ORDER>, p));
 }
 
-// A CTA of four warps a unit, or a cluster of them; a warp a unit where there are more units than CTAs are resident
-// and none has more than kSoloBlocks blocks.  (us a step with rotation, four warps / one, d = 128, G = 4, blocks 4, 8, 12, 20:
+// A CTA of four warps a unit, or a cluster of them; a warp a unit, or two if all of those are resident together, where there are
+// more units than CTAs of four and none has more than kSoloBlocks blocks.  (us a step with rotation, four warps / one, d = 128,
+// G = 4, blocks 4, 8, 12, 20:
 //    512 units  10.6 / 10.7   16.9 / 15.3   22.9 / 20.1   31.4 / 29.2
 //  1,024        18.2 / 13.5   28.8 / 22.2   42.8 / 29.4   58.6 / 64.8
 //  2,048        31.6 / 27.7   50.4 / 44.3   77.6 / 57.5  106.1 / 107.1
-//    256         6.5 /  8.7    8.3 / 18.2    9.8 / 21.9   14.7 / 27.9)
+//    256         6.5 /  8.7    8.3 / 18.2    9.8 / 21.9   14.7 / 27.9
+// One / two, blocks 2, 6, 12, 16:
+//    512         6.0 /  6.0   12.3 / 10.2   20.7 / 18.4   26.2 / 23.7
+//    720         6.6 /  6.4   15.1 / 12.2   24.4 / 21.1   30.7 / 28.1
+// and of 20 blocks, rings full / of different fill, four / two: 31.0 / 26.3, 12.9 / 15.7: the longest unit counts.)
 // Several waves of CTAs of four warps start with the longest sequences (ORDER): ordering them, a thread a sequence, costs a CTA
 // a microsecond and the prefetch before the wait, so that calls of equal lengths lose by it where clusters are used.  (us a
 // launch without / with it, G = 4: 64 sequences x 8 heads of 256 + 128..2,048 keys 50.3 / 43.7, 32 + 60..1,000 25.0 / 19.5,
@@ -835,13 +840,22 @@ static int launch_weighted(WeightedParams& p, const cmc_dims& m, cudaStream_t s,
   int st = per_sm_of<D, G, FUSED, PREP, kWarpsMost, false>(&per_sm);
   if (st != CMC_OK) return st;
   const long long units = static_cast<long long>(m.B) * m.L * m.Hkv;
-  const bool solo = units > static_cast<long long>(per_sm) * sm_count() && blocks_of(m) <= kSoloBlocks;
-  const int cm = solo ? 1 : plan_cm(m, per_sm, WSmem<D, G, PREP, kWarpsMost>::kScores);
+  const bool brief = units > static_cast<long long>(per_sm) * sm_count() && blocks_of(m) <= kSoloBlocks;
+  bool two = false;
+  if (brief) {
+    int per_sm2 = 1;
+    st = per_sm_of<D, G, FUSED, PREP, 2, false>(&per_sm2);
+    if (st != CMC_OK) return st;
+    const long long smem = WSmem<D, G, PREP, 2>::kScores + static_cast<long long>(score_bytes(m, 1, 2)) + kSmemReserved;
+    two = units <= std::min<long long>(per_sm2, kSmemPerSm / smem) * sm_count();
+  }
+  const int cm = brief ? 1 : plan_cm(m, per_sm, WSmem<D, G, PREP, kWarpsMost>::kScores);
   if (ctas) {
     *ctas = static_cast<int>(units * cm);
     return CMC_OK;
   }
-  if (solo) {
+  if (brief && two) return launch_weighted_cm<D, G, FUSED, PREP, 2, false>(p, m, cm, s);
+  if (brief) {
     st = per_sm_of<D, G, FUSED, PREP, 1, false>(&per_sm);
     return st != CMC_OK ? st : launch_weighted_cm<D, G, FUSED, PREP, 1, false>(p, m, cm, s);
   }

@@ -260,6 +260,9 @@ ATTEND = [  # B, L, Hkv, G, d, k, W, positions (cycled)
     # many short units: a warp each
     (60, 1, 8, 8, 128, 40, 70, [0, 1, 69, 70, 2 ** 35, -7]), (20, 3, 8, 1, 128, 0, 33, [32, 31, 64]),
     (58, 1, 8, 2, 64, 250, 220, [219, 5, 64]),
+    # two warps each
+    (60, 1, 8, 4, 128, 40, 70, [0, 1, 69, 70, 2 ** 35, -7]), (31, 3, 8, 8, 64, 100, 200, [199, 31, 200, 3, -1]),
+    (465, 1, 1, 1, 128, 3, 500, [0, 499, 5000, 80]), (250, 1, 2, 2, 128, 0, 20, [5, 19, 20]),
     # several waves, which start with the longest sequences: up to 128 sequences, a CTA a unit and a cluster
     (61, 1, 8, 1, 64, 200, 400, [3, 399, -5, 400, 77, 0, 2 ** 40, 210]), (128, 1, 4, 2, 64, 40, 520, [100, 519, 7, 520, -1, 33]),
     (129, 2, 2, 1, 64, 30, 540, [100, 539, 7, 540, -1]), (120, 1, 1, 8, 64, 100, 4400, [17, 4399, 0, 9999, 300, -2, 2222]),
