@@ -628,7 +628,8 @@ typedef struct cmc_qk_prep {
  *   k      bf16 [B, L, T, Hkv, d], k_stride likewise
  *   pos    int64 [B] (read only; any value)
  *   out_q  bf16 [B, L, T, Hq, d] dense; may be q where that is dense too
- *   out_k  bf16 [B, L, T, Hkv, d] dense; may be k likewise
+ *   out_k  bf16 [B, L, T, Hkv, d] dense; may be k likewise.  Outputs otherwise meet neither inputs nor each
+ *          other (CMC_ERR_RANGE)
  *
  * dims->N, k and W are ignored.  T == 0 launches nothing.  Limits: 0 <= T <= 2^24, L * T < 2^27.
  */
@@ -656,6 +657,7 @@ CMC_API size_t cmc_cache_workspace_size(int B);
  *                   are not written
  *   workspace       see cmc_cache_workspace_size
  *
+ * The rings and out_q meet neither the inputs nor each other, but for out_q and q (CMC_ERR_RANGE).
  * dims->N and k are ignored.  A sequence with pos[b] < 0 is left unchanged, its out_q too, and
  * CMC_DEVFLAG_BAD_POS is set.  T == 0 launches nothing.  Limits as for cmc_qk_norm_rope.
  */
@@ -709,7 +711,7 @@ CMC_API int cmc_decode_step_weighted(const void* q, const void* tier1_k, const v
                                      size_t workspace_bytes, void* stream);
 
 /* Launch plan of the two calls above for `dims` on the current device (fused == 0: the attention, else the
- * step): *ctas receives the grid size of their one kernel, a CTA or a cluster of up to 8 for every (sequence,
+ * step without a prep): *ctas receives the grid size of their one kernel, a CTA or a cluster of up to 8 for every (sequence,
  * layer, KV head) unit. */
 CMC_API int cmc_decode_attn_weighted_plan(const cmc_dims* dims, int fused, int* ctas);
 

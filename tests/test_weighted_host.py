@@ -133,7 +133,7 @@ def _prep(**kw):
     return ctypes.byref(CmcQkPrep(**base))
 
 
-def _norm(L, q=FAKE, qs=1024, k=FAKE, ks=256, T=4, pos=FAKE, dims=None, prep=None, oq=FAKE, ok=FAKE):
+def _norm(L, q=BIG, qs=1024, k=2 * BIG, ks=256, T=4, pos=FAKE, dims=None, prep=None, oq=3 * BIG, ok=4 * BIG):
     return L.cmc_qk_norm_rope(q, qs, k, ks, T, pos, dims or _dims(), prep, oq, ok, None)
 
 
@@ -161,10 +161,20 @@ def test_norm_argument_checks(L):
     assert _norm(L, prep=_prep(k_weight=FAKE + 4)) == ALIGN
     assert _norm(L, prep=_prep(evicted=FAKE + 4)) == ALIGN
     assert L.cmc_qk_norm_rope(FAKE, 1024, FAKE, 256, 4, FAKE, None, None, FAKE, FAKE, None) == NULL
+    # outputs that meet inputs (24 tokens of 2,048 and 512 bytes), but for heads prepared where they are
+    bad = _prep(rope_theta=-1.0)
+    evil = _prep(q_weight=FAKE + 4)  # refused after these
+    for change in (dict(oq=BIG + 2048), dict(oq=BIG - 16), dict(oq=BIG, qs=1536), dict(oq=2 * BIG), dict(ok=BIG + 24 * 2048 - 16),
+                   dict(ok=2 * BIG, ks=264), dict(ok=3 * BIG), dict(oq=4 * BIG - 24 * 2048 + 16)):
+        assert _norm(L, prep=evil, **change) == RANGE
+    for change in (dict(oq=BIG, ok=2 * BIG), dict(oq=BIG + 24 * 2048), dict(ok=BIG + 24 * 2048), dict(oq=4 * BIG - 24 * 2048),
+                   dict(q=BIG, k=BIG + 2048, qs=1536, ks=1536), dict(k=BIG)):
+        assert _norm(L, prep=evil, **change) == ALIGN
+        assert _norm(L, prep=bad, **change) == RANGE
 
 
-def _prefill(L, q=FAKE, qs=1024, k=FAKE, ks=256, v=FAKE, vs=256, T=4, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE,
-             count=FAKE, dims=None, prep=None, oq=FAKE, ws=FAKE, wsb=512):
+def _prefill(L, q=BIG, qs=1024, k=2 * BIG, ks=256, v=3 * BIG, vs=256, T=4, rk=4 * BIG, rv=5 * BIG, rw=FAKE, pos=FAKE,
+             count=FAKE, dims=None, prep=None, oq=6 * BIG, ws=FAKE, wsb=512):
     return L.cmc_window_prefill(q, qs, k, ks, v, vs, T, rk, rv, rw, pos, count, dims or _dims(), prep, oq, ws,
                                 wsb, None)
 
@@ -182,6 +192,12 @@ def test_prefill_argument_checks(L):
     assert _prefill(L, vs=248) == SHAPE and _prefill(L, vs=260) == ALIGN
     assert _prefill(L, ws=0) == WORKSPACE and _prefill(L, wsb=511) == WORKSPACE
     assert _prefill(L, prep=_prep(rope_theta=-1.0)) == RANGE
+    evil = _prep(q_weight=FAKE + 4)
+    for change in (dict(rk=2 * BIG), dict(rv=3 * BIG + 512), dict(rk=5 * BIG), dict(oq=5 * BIG + 16), dict(rv=BIG), dict(oq=3 * BIG),
+                   dict(oq=BIG, qs=1536)):
+        assert _prefill(L, prep=evil, **change) == RANGE
+    for change in (dict(oq=BIG), dict(v=2 * BIG), dict(q=0, oq=0), dict(rv=4 * BIG + 2 * 3 * 2 * 16 * 256)):
+        assert _prefill(L, prep=evil, **change) == ALIGN
 
 
 def _attend(L, q=FAKE, tk=FAKE, tv=FAKE, tw=FAKE, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE, dims=None, out=FAKE,
