@@ -422,7 +422,7 @@ CMC_API int cmc_read_status(void* workspace, int clear, uint32_t* flags, void* s
  * already overlap); with 0, staging copies of 32 KB or more (cmc_stage_copies) also
  * let the launch after them start with their end only.  CMC_ERR_RANGE unless 0 <= tiles <= 64.
  * Over a cache in 8 bits, and where weights are accumulated, a tile is a block of 32 keys, every warp
- * prefetches, and three are the most it takes. */
+ * prefetches, and three, or where weights are accumulated two, are the most it takes. */
 CMC_API int cmc_set_l2_prefetch_tiles(int tiles);
 
 /* Test hook for the failure path of the attention kernels (not part of the

@@ -39,6 +39,11 @@ constexpr int kWarpsMost = 4;  // of a CTA
 // 16,384 keys 79 / 98 / 103, of 20,480 keys 125 / 152 / 126), but where there is no more than a CTA an SM.
 constexpr int score_cap(int G) { return G == 8 ? 41472 : 46080; }
 constexpr int kScoreMost = 131072;
+// Blocks a warp prefetches, at most.  What it holds of the ring is not known then, so that more of them fetch rows without a token:
+// us a launch with none / one / two / three, 256 units of 128 + 512 keys, rings full 15.5 / 13.7 / 13.1 / 13.5, of different fill
+// 10.1 / 9.0 / 9.1 / 10.5.  A warp with a unit of its own takes one block of the ring alone: 2,048 units of 30 + 8..130 keys, step with
+// rotation, 17.4 / 17.2 / 18.2 / 21.4, with one of the ring among two 17.4; of 128 + 256 keys, full, 62.5 / 59.3 / 57.3 / 58.2, 57.2.
+constexpr int kPrefetchMost = 2;
 // Blocks of a unit that is given to one warp or two, at most (see launch_weighted).
 constexpr int kSoloBlocks = 16;
 
@@ -319,7 +324,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     if (blk < p.nb1) {
       base = ((lane & 1) ? p.t1v : p.t1k) + (u * p.N + blk * kBlkKeys) * D;
       rows = min(p.k - blk * kBlkKeys, kBlkKeys);
-    } else if ((blk - p.nb1) * kBlkKeys < p.W) {
+    } else if ((NW > 1 || lane < 2) && (blk - p.nb1) * kBlkKeys < p.W) {
       base = ((lane & 1) ? p.ring_v : p.ring_k) + (u * p.W + (blk - p.nb1) * kBlkKeys) * D;
       rows = min(p.W - (blk - p.nb1) * kBlkKeys, kBlkKeys);
     }
@@ -801,7 +806,7 @@ static int launch_weighted_cm(WeightedParams& p, const cmc_dims& m, int cm, cuda
   const long long ctas = static_cast<long long>(m.B) * m.L * m.Hkv * cm;
   if (bytes > static_cast<size_t>(ctas <= sm_count() ? kScoreMost : score_cap(G))) bytes = 0;  // in the workspace
   else p.scratch = nullptr;
-  p.prefetch = std::min({l2_prefetch_setting(), 3, p.iters});
+  p.prefetch = std::min({l2_prefetch_setting(), kPrefetchMost, p.iters});
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[0].val.programmaticStreamSerializationAllowed = 1;
