@@ -42,7 +42,8 @@ constexpr int kScoreMost = 131072;
 // Blocks a warp prefetches, at most.  What it holds of the ring is not known then, so that more of them fetch rows without a token:
 // us a launch with none / one / two / three, 256 units of 128 + 512 keys, rings full 15.5 / 13.7 / 13.1 / 13.5, of different fill
 // 10.1 / 9.0 / 9.1 / 10.5.  A warp with a unit of its own takes one block of the ring alone: 2,048 units of 30 + 8..130 keys, step with
-// rotation, 17.4 / 17.2 / 18.2 / 21.4, with one of the ring among two 17.4; of 128 + 256 keys, full, 62.5 / 59.3 / 57.3 / 58.2, 57.2.
+// rotation, 17.4 / 17.2 / 18.2 / 21.4, with one of the ring among two 17.4, and 16.5 where the second is prefetched as soon as it is
+// known to hold tokens; of 128 + 256 keys, full, 62.5 / 59.3 / 57.3 / 58.2, 57.2.
 constexpr int kPrefetchMost = 2;
 // Blocks of a unit that is given to one warp or two, at most (see launch_weighted).
 constexpr int kSoloBlocks = 16;
@@ -425,6 +426,10 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     }
   }
   const int nblk = bad ? 0 : p.nb1 + (count + kBlkKeys - 1) / kBlkKeys;
+  if (NW == 1 && lane < 2 && p.prefetch > 1 && first + stride >= p.nb1 && first + stride < nblk) {  // the second, now known
+    const Blk x = blk_of<D>(p, u, first + stride, count, new_slot);
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(lane ? x.v : x.k), "r"(x.rows * D * 2) : "memory");
+  }
   uint16_t* put_k = p.ring_k + (u * p.W + new_slot) * D;  // (not used without a new token)
   uint16_t* put_v = p.ring_v + (u * p.W + new_slot) * D;
   if (PREP) newk = nullptr;  // put in when it is prepared
