@@ -6,7 +6,7 @@
 // select of up to three passes (11, 11 and 10 bits) finds the threshold, and every kept token gets its number from
 // what the warps and lanes before it keep.  The copy moves blocks of rows.  Enough units for the SMs: a CTA of 256
 // threads does both, its copy beside others' choices and the youngest rows, which need none, on their way to L2
-// meanwhile (256 units of 512 tokens, 256 kept, 64 of them for their age: 15.1 us, without that prefetch 15.8; the
+// meanwhile (256 units of 512 tokens, 256 kept, 64 of them for their age: 14.4 us, without that prefetch 15.1; the
 // choice is 3.5, in all CTAs at once; 10.2 at the copy rate).  Few long ones: a kernel of CTAs of 1,024 threads
 // chooses, and a second one copies with all SMs: 64 units of 16,384 tokens, 2,048 kept, 35 us, 11 and 20 of them the
 // two kernels', 20.9 at the copy rate.  (Both in clusters of four: 38.8 where the CTAs summed their histograms in
@@ -27,7 +27,7 @@ constexpr int kEvictThreads = 256;   // of a CTA that copies
 constexpr int kChooseThreads = 1024;  // of one that only chooses
 constexpr int kEvictBatch = 4;       // rows of K and of V that a thread has in flight
 constexpr int kEvictBins = 2048;     // 11 bits a pass
-constexpr int kEvictAhead = 65536;   // bytes of K, and of V, of a unit that are prefetched into L2
+constexpr int kEvictAhead = 65536;   // bytes of K, of V and of the weights of a unit that are prefetched into L2
 constexpr int kEvictKeys = 49152;    // keys held in shared memory; of longer units the weights are read again
 
 struct EvictParams {
@@ -360,6 +360,14 @@ __device__ __forceinline__ void prefetch_young(const EvictParams& p, long long u
   if (n > 0) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(base), "r"(n * D * 2) : "memory");
 }
 
+// A unit's weights, into L2: a hint, which may come before the wait (256 units of 512 tokens 15.0 us without, 14.4 with; where a
+// kernel of its own chooses it changes nothing).
+__device__ __forceinline__ void prefetch_weights(const EvictParams& p, long long u) {
+  const uintptr_t at = reinterpret_cast<uintptr_t>(p.weight + u * p.T);
+  const uintptr_t from = (at + 15) & ~static_cast<uintptr_t>(15), to = (at + min(4ll * p.T, static_cast<long long>(kEvictAhead))) & ~static_cast<uintptr_t>(15);
+  if (to > from) asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;\n" ::"l"(from), "r"(static_cast<uint32_t>(to - from)) : "memory");
+}
+
 // A unit's choice and copy.
 template <int D, bool CACHED>
 __global__ void __launch_bounds__(kEvictThreads, 2)
@@ -368,6 +376,7 @@ evict_kernel(const __grid_constant__ EvictParams p) {
   __shared__ ChooseSmem<kEvictThreads> sm;
   const long long u = blockIdx.x;
   const int b = static_cast<int>(static_cast<unsigned>(u) / static_cast<unsigned>(p.LH));
+  if (threadIdx.x == 0) prefetch_weights(p, u);
   for (int i = threadIdx.x; i < kEvictBins; i += kEvictThreads) sm.bins[i] = 0u;
   pdl_wait();
   pdl_trigger();
