@@ -413,9 +413,8 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     request_k(first, p.nb1, 0, -1, nullptr);
     request_v(0, first, p.nb1, 0, -1, nullptr);
   }
-  const bool bad = pos < 0;
-  int count = 0, new_slot = -1;
-  if (!bad) {
+  int count = -1, new_slot = -1;
+  if (pos >= 0) {
     if (FUSED) {
       count = static_cast<int>(pos + 1 < p.W ? pos + 1 : p.W);
       new_slot = (pos >> 32) == 0
@@ -425,6 +424,11 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       count = static_cast<int>(pos < p.W ? pos : p.W);
     }
   }
+  // The same in all lanes, as pos is; a reduction, so that the compiler knows it too: the loop below has instructions that a
+  // warp executes as one (ldmatrix, mma, movmatrix), and what decides how often it runs, and which of its branches, comes from here.
+  count = __reduce_max_sync(0xffffffffu, count);
+  new_slot = __reduce_max_sync(0xffffffffu, new_slot);
+  const bool bad = count < 0;
   const int nblk = bad ? 0 : p.nb1 + (count + kBlkKeys - 1) / kBlkKeys;
   if (NW == 1 && lane < 2 && p.prefetch > 1 && first + stride >= p.nb1 && first + stride < nblk) {  // the second, now known
     const Blk x = blk_of<D>(p, u, first + stride, count, new_slot);
@@ -558,6 +562,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       l_run[0] += (pr[0][0] + pr[0][2]) + (pr[1][0] + pr[1][2]);
       l_run[1] += (pr[0][1] + pr[0][3]) + (pr[1][1] + pr[1][3]);
       // P^T as the B operand: packed to bf16 (outputs are bf16; the sums are not rounded) and transposed
+      __syncwarp();  // converged for movmatrix
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         pb[h][0] = movmatrix_trans(pack_bf16_rn(pr[h][0], pr[h][1]));
@@ -566,9 +571,12 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     }
     cp_async_wait<1>();  // V has
     __syncwarp();
-    if (FUSED && cur.new_row >= 0 && lane < D / 8)
-      *reinterpret_cast<uint4*>(put_v + 8 * lane) =
-          *reinterpret_cast<const uint4*>(smem + (sV - smem_addr(smem)) + swz<D>(cur.new_row, lane));
+    if (FUSED && cur.new_row >= 0) {  // its value too
+      if (lane < D / 8)
+        *reinterpret_cast<uint4*>(put_v + 8 * lane) =
+            *reinterpret_cast<const uint4*>(smem + (sV - smem_addr(smem)) + swz<D>(cur.new_row, lane));
+      __syncwarp();  // converged for ldmatrix
+    }
     // ---- O^T += V^T P^T ----
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
