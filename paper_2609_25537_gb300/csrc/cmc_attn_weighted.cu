@@ -481,7 +481,8 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       }
       __syncwarp();
     }
-    // ---- S^T = K Q^T, two products of 16 keys, each in two accumulator chains ----
+    // ---- S^T = K Q^T, two products of 16 keys, each in two accumulator chains: the even and the odd steps, or (PREP) the
+    // queries' high and low parts ----
     float sa[2][2][4];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
@@ -493,8 +494,8 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       for (int i = 0; i < KS; ++i) {
         uint32_t a0, a1, a2, a3;
         ldsm_x4(sK + k_at + h * 2048 + (i >> 2) * (kBlkKeys * 128) + (((i & 3) * 32) ^ k_x), a0, a1, a2, a3);
-        wmma(sa[h][i & 1], a0, a1, a2, a3, qa[i][0], qa[i][1]);
-        if (PREP) wmma(sa[h][i & 1], a0, a1, a2, a3, ql[PREP ? i : 0][0], ql[PREP ? i : 0][1]);
+        wmma(sa[h][PREP ? 0 : i & 1], a0, a1, a2, a3, qa[i][0], qa[i][1]);
+        if (PREP) wmma(sa[h][1], a0, a1, a2, a3, ql[PREP ? i : 0][0], ql[PREP ? i : 0][1]);
       }
     }
     __syncwarp();  // the stage's K is read
@@ -503,7 +504,11 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[h][e] = sa[h][0][e] + sa[h][1][e];
+      for (int e = 0; e < 4; ++e) {
+        v[h][e] = sa[h][0][e] + sa[h][1][e];
+        // An infinite key has its score from the high part: the low one has any sign, or is 0, and their sum would be NaN.
+        if (PREP && !(fabsf(sa[h][0][e]) < INFINITY)) v[h][e] = sa[h][0][e];
+      }
     if (cur.rows < kBlkKeys) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {

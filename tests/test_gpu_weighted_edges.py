@@ -73,3 +73,73 @@ def test_new_tokens_at_every_place_of_a_block(cuda_device, unit, d, G, prepared)
     ctas = cmc.decode_attn_weighted_plan(cmc.CmcDims(B, 1, H * G, H, d, k, k, 70))
     assert ctas == B * H * (2 if unit == "a cluster" else 1)
     check_step(cuda_device, (B, 1, H, G, d, k, 70, list(range(70))), prepared, 40)
+
+
+def step_inputs(dev, case, form, seed):
+    """Arguments of a step of one form, and its queries as the formula prepares them."""
+    B, L, H, G, d, k, W, _ = case
+    q, t1, ring, pos, g = attention_problem(dev, case, seed, poison=False)
+    q.view(B, L, H, G, d)[:] = q.view(B, L, H, G, d)[:, :, :, :1].clone()  # the heads of a KV head alike
+    new = [randn(g, B, L, H, d), randn(g, B, L, H, d)]
+    opts, qw, p = {}, None, None
+    if form in ("norm", "both"):
+        qw, kw = (1 + 0.5 * torch.randn(L, d, generator=g, device=dev) for _ in range(2))
+        opts.update(q_weight=qw, k_weight=kw, eps=1e-5)
+    if form in ("rope", "both"):
+        opts.update(rope_theta=THETA, rope_offset=0)
+        p = ow.positions(f64(pos), None, 0, 1)
+    return q, t1, ring, pos, new, opts, f64(q) if form == "plain" else prepared_queries(q, qw, 1e-5, p)
+
+
+@pytest.mark.parametrize("form", ["plain", "norm", "rope", "both"])
+@pytest.mark.parametrize("G, d", [(1, 64), (4, 128), (8, 64)])
+@pytest.mark.parametrize("unit", ["a CTA", "a cluster", "a warp"])
+def test_keys_of_a_step_that_are_not_finite(cuda_device, unit, G, d, form):
+    """A key whose score is minus infinity counts nothing, whatever norm and rotation make of the query; one of plus infinity
+    or NaN gives NaN in its KV head's outputs and weights, and leaves the others as they were."""
+    B, H, k = PLACES[unit]
+    case = (B, 1, H, G, d, k, 70, [0, 69, 70, 30, 500])
+    q, t1, ring, pos, new, opts, qq = step_inputs(cuda_device, case, form, 41)
+    start = [x.clone() for x in (*t1, *ring, pos)]
+
+    def run(change):
+        x = [y.clone() for y in start]
+        change(x)
+        out = cmc.decode_step_weighted(q, *x, *new, **opts)
+        return out, x
+
+    want, clean = run(lambda x: None)
+    # sequences 0 (position 0, where a rotation leaves the query as it is) and 1, a few elements of the query each
+    spots = [(b, row, i) for b in (0, 1) for row, i in zip(range(5, 13), range(3, d, d // 8))]
+
+    def infinite(sign):
+        def change(x):
+            for b, row, i in spots:
+                x[0][b, 0, 0, row, i] = sign * float("inf") * (1 if qq[b, 0, 0, i] > 0 else -1)
+        return change
+    out, x = run(infinite(-1.0))
+    assert not out.isnan().any() and not x[2].isnan().any() and not x[5].isnan().any()
+    rows = f64(start[0])
+    for b, row, i in spots:  # as good as no key: a score of -200
+        rows[b, 0, 0, row] = -200 * math.sqrt(d) * qq[b, 0, 0] / (qq[b, 0, 0] ** 2).sum()
+        assert x[2][b, 0, 0, row] == start[2][b, 0, 0, row]
+    before = [rows] + [f64(y) for y in start[1:3]]
+    left = [f64(y) for y in x[3:6]]
+    w = f64(start[5])
+    n = f64(start[6])
+    for b in range(B):
+        w[b, :, :, int(n[b] % 70)] = 0.0
+    check_attention(out, x[2], x[5], qq, before, left[:2] + [w], n + 1, 1 / math.sqrt(d), prepared=form != "plain")
+
+    def nan(x):
+        for b in (0, 1):
+            x[0][b, 0, 0, 7, 11] = float("nan")
+    for change in (infinite(1.0), nan):
+        out, x = run(change)
+        for b in (0, 1):
+            assert out[b, 0, :G].isnan().all() and x[2][b, 0, 0].isnan().all()
+            live = min(int(x[6][b]), 70)
+            assert x[5][b, 0, 0, :live].isnan().all() and not x[5][b, 0, 0, live:].isnan().any()
+            assert torch.equal(out[b, 0, G:], want[b, 0, G:]) and torch.equal(x[2][b, 0, 1:], clean[2][b, 0, 1:])
+            assert torch.equal(x[5][b, 0, 1:], clean[5][b, 0, 1:])
+        assert torch.equal(out[2:], want[2:]) and torch.equal(x[2][2:], clean[2][2:]) and torch.equal(x[5][2:], clean[5][2:])
