@@ -730,15 +730,15 @@ CMC_API int cmc_decode_attn_weighted_plan(const cmc_dims* dims, int fused, int* 
  *   dims->W             rows of the output, >= keep
  *   recent              0 .. keep
  *   out_k, out_v, out_weight  bf16 [B, L, Hkv, W, d], fp32 [B, L, Hkv, W]: rows 0 .. m-1 are written.
- *                       In place: all three the inputs' own (with dims->W == dims->N); otherwise they must
- *                       not overlap the inputs
+ *                       In place: all three the inputs' own (with dims->W == dims->N)
  *   idx_out             int32 [B, L, Hkv, keep]: the rows that were kept, then -1
  *   out_pos             int64 [B] or NULL: m, what the ring of the output holds; may be pos
  *   evicted             int64 [B] or NULL: grows by pos[b] - m (T - m without pos), so that
  *                       evicted[b] + out_pos[b] is the number of the next token as before
  *   workspace           see cmc_cache_workspace_size
  *
- * dims->Hq is ignored.  A sequence with pos[b] < 0, or in place one whose ring starts elsewhere than at row 0
+ * What is written (the workspace too) otherwise meets neither what is read nor anything else that is written
+ * (CMC_ERR_RANGE).  dims->Hq is ignored.  A sequence with pos[b] < 0, or in place one whose ring starts elsewhere than at row 0
  * (pos[b] > T and pos[b] mod T != 0), is left as it is: out_pos[b] = pos[b], its idx_out is -1, and
  * CMC_DEVFLAG_BAD_POS is set.
  */

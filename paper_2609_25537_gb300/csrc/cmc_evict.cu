@@ -476,11 +476,6 @@ static int launch_evict(const EvictParams& p0, long long units, cudaStream_t s) 
   return launch_evict_kernel(evict_copy_kernel<D>, units * cm, kEvictThreads, 0, p.in_place ? p.cm : 1, s, p);
 }
 
-static bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
-}
-
 }  // namespace cmc
 
 extern "C" {
@@ -509,11 +504,20 @@ int cmc_evict_cache(const void* k, const void* v, const float* weight, const int
   EvictParams p;
   p.in_place = k == out_k || v == out_v || weight == out_weight;
   if (p.in_place && !(k == out_k && v == out_v && weight == out_weight && m.W == m.N)) return CMC_ERR_RANGE;
-  const size_t in = static_cast<size_t>(units) * m.N, out = static_cast<size_t>(units) * m.W;
-  if (!p.in_place && (overlap(k, in * m.d * 2, out_k, out * m.d * 2) || overlap(k, in * m.d * 2, out_v, out * m.d * 2) ||
-                      overlap(v, in * m.d * 2, out_k, out * m.d * 2) || overlap(v, in * m.d * 2, out_v, out * m.d * 2) ||
-                      overlap(weight, in * 4, out_weight, out * 4)))
-    return CMC_ERR_RANGE;
+  // Rows are read while others are written, and idx is read back as the rows to copy: what is written meets nothing else, but
+  // for the cache in place and out_pos in pos.
+  const size_t in = static_cast<size_t>(units) * m.N, out = static_cast<size_t>(units) * m.W, row = m.d * 2, each = static_cast<size_t>(m.B) * 8;
+  const Range reads[] = {{k, in * row}, {v, in * row}, {weight, in * 4}, {pos, each}};
+  const Range writes[] = {{out_k, out * row}, {out_v, out * row}, {out_weight, out * 4}, {idx_out, static_cast<size_t>(units) * m.k * 4},
+                          {out_pos, each}, {evicted, each}, {workspace, ws_partials_off(m.B)}};
+  for (int o = 0; o < 7; ++o) {
+    for (int i = 0; i < 4; ++i) {
+      const bool there = same(writes[o], reads[i]) && ((p.in_place && o < 3 && i < 3) || (o == 4 && i == 3));
+      if (!there && meet(writes[o], reads[i])) return CMC_ERR_RANGE;
+    }
+    for (int i = 0; i < o; ++i)  // (a cache whose K is its V too is moved as one in place)
+      if (meet(writes[o], writes[i]) && !(p.in_place && o == 1 && i == 0 && same(writes[0], writes[1]))) return CMC_ERR_RANGE;
+  }
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);
   p.weight = weight;

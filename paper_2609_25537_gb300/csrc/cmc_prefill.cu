@@ -221,15 +221,6 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
 // Host side
 // ---------------------------------------------------------------------------
 
-struct Range {
-  const void* at;
-  long long bytes;
-};
-static bool meet(const Range& a, const Range& b) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
-}
-
 static int run_prefill(const void* q, int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                        int64_t v_stride, int T, void* ring_k, void* ring_v, float* ring_weight,
                        int64_t* pos, const int64_t* count, const cmc_dims* dims, const cmc_qk_prep* prep,
@@ -261,8 +252,8 @@ static int run_prefill(const void* q, int64_t q_stride, const void* k, int64_t k
   }
   // Warps read and write in any order: an output meets no input, but for heads prepared where they are, and no other output.
   const long long tokens = items * m.B;
-  auto heads = [&](const void* a, long long stride, long long row) { return Range{a, ((tokens - 1) * stride + row) * 2}; };
-  const long long ring_bytes = static_cast<long long>(m.B) * m.L * m.Hkv * m.W * m.d * 2;
+  auto heads = [&](const void* a, long long stride, long long row) { return Range{a, static_cast<size_t>((tokens - 1) * stride + row) * 2}; };
+  const size_t ring_bytes = static_cast<size_t>(m.B) * m.L * m.Hkv * m.W * m.d * 2;
   const Range in[] = {heads(q, q_stride, qd), heads(k, k_stride, kd), heads(v, v_stride, kd)};
   const Range outs[] = {heads(out_q, qd, qd), heads(out_k, kd, kd), {ring_k, ring_bytes}, {ring_v, ring_bytes}};
   for (int o = 0; o < 4; ++o) {

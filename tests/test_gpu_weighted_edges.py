@@ -143,3 +143,19 @@ def test_keys_of_a_step_that_are_not_finite(cuda_device, unit, G, d, form):
             assert torch.equal(out[b, 0, G:], want[b, 0, G:]) and torch.equal(x[2][b, 0, 1:], clean[2][b, 0, 1:])
             assert torch.equal(x[5][b, 0, 1:], clean[5][b, 0, 1:])
         assert torch.equal(out[2:], want[2:]) and torch.equal(x[2][2:], clean[2][2:]) and torch.equal(x[5][2:], clean[5][2:])
+
+
+def test_eviction_refuses_outputs_that_meet(cuda_device):
+    k = torch.zeros(2, 1, 2, 10, 64, dtype=torch.bfloat16, device=cuda_device)
+    v, w = k.clone(), torch.zeros(2, 1, 2, 10, device=cuda_device)
+    pos = torch.full((2,), 10, device=cuda_device)
+    a, b, c = k[..., :6, :].contiguous(), v[..., :6, :].contiguous(), w[..., :6].contiguous()
+    for kw in (dict(out_k=a, out_v=a, out_weight=c), dict(out_k=k, out_v=v, out_weight=k.view(torch.float32).view(-1)[:40].view(2, 1, 2, 10)),
+               dict(evicted=pos), dict(out_pos=c.view(torch.int64).view(-1)[:2], out_k=a, out_v=b, out_weight=c)):
+        with pytest.raises(cmc.CmcError, match="RANGE"):
+            cmc.evict_cache(k, v, w, 5, pos=pos, **kw)
+    # K that is V too: moved together in place
+    k.copy_(torch.arange(10, device=cuda_device, dtype=torch.bfloat16)[:, None].expand(k.shape))
+    w[..., [1, 4, 5, 8]] = 1.0
+    cmc.evict_cache(k, k, w, 4, pos=pos, out_k=k, out_v=k, out_weight=w, out_pos=pos)
+    assert pos.tolist() == [4, 4] and k[0, 0, 0, :4, 0].tolist() == [1.0, 4.0, 5.0, 8.0]

@@ -263,6 +263,39 @@ def test_evict_argument_checks(L):
 
 
 @host_only
+def test_evict_overlaps(L):
+    """What is written meets nothing else; idx, which is read back as the rows to copy, above all.  units = 12: k and v 307,200
+    bytes, weight 4,800; outputs of 16 rows 49,152 and 768, idx 480."""
+    CUDA = 6  # all checks passed: no device
+    assert _evict(L) == CUDA
+    rows, ws = 12 * 16 * 256, dict(ws=8 * BIG)
+    for at in (BIG, 2 * BIG + 307200 - 4, 3 * BIG + 4796, 4 * BIG, 5 * BIG + rows - 4, 6 * BIG + 764, 4 * BIG - 476):
+        assert _evict(L, idx=at) == RANGE
+    assert _evict(L, ok=4 * BIG, ov=4 * BIG) == RANGE and _evict(L, ov=4 * BIG + rows - 16) == RANGE
+    for at in (BIG, 2 * BIG + 16, 4 * BIG + rows - 4, 5 * BIG - 764):
+        assert _evict(L, ow=at) == RANGE
+    assert _evict(L, ok=3 * BIG) == RANGE and _evict(L, ov=3 * BIG + 4784) == RANGE
+    for name in ("op", "ev"):
+        for at in (BIG, 2 * BIG, 3 * BIG + 8, 4 * BIG, 5 * BIG, 6 * BIG + 760, 7 * BIG + 472):
+            assert _evict(L, pos=9 * BIG, **{name: at}) == RANGE
+    assert _evict(L, pos=9 * BIG, ev=9 * BIG) == RANGE and _evict(L, pos=9 * BIG, op=9 * BIG + 8) == RANGE
+    assert _evict(L, op=9 * BIG, ev=9 * BIG + 8) == RANGE and _evict(L, op=9 * BIG, ev=9 * BIG) == RANGE
+    assert _evict(L, pos=9 * BIG, idx=9 * BIG + 12) == RANGE and _evict(L, pos=9 * BIG, ok=9 * BIG) == RANGE
+    for change in (dict(pos=8 * BIG + 504), dict(op=8 * BIG), dict(idx=8 * BIG - 476), dict(k=8 * BIG), dict(ow=8 * BIG + 508)):
+        assert _evict(L, **{**ws, **change}) == RANGE
+    # side by side, in place, pos in place, inputs that are one another
+    for change in (dict(idx=4 * BIG + rows), dict(idx=4 * BIG - 480), dict(ov=4 * BIG + rows), dict(ow=5 * BIG - 768),
+                   dict(pos=9 * BIG, op=9 * BIG), dict(pos=9 * BIG, op=9 * BIG, ev=9 * BIG + 16), dict(k=2 * BIG),
+                   dict(v=BIG + 256), dict(dims=_dims(W=100), ok=BIG, ov=2 * BIG, ow=3 * BIG),
+                   dict(dims=_dims(W=100), k=2 * BIG, ok=2 * BIG, ov=2 * BIG, ow=3 * BIG)):
+        assert _evict(L, **change) == CUDA
+    place = dict(dims=_dims(W=100), ok=BIG, ov=2 * BIG, ow=3 * BIG)
+    for change in (dict(idx=BIG + 307200 - 4), dict(idx=3 * BIG), dict(v=BIG + 256, ov=BIG + 256), dict(w=BIG + 512, ow=BIG + 512),
+                   dict(op=2 * BIG), dict(ev=3 * BIG)):
+        assert _evict(L, **{**place, **change}) == RANGE
+
+
+@host_only
 def test_plan_argument_checks(L):
     assert L.cmc_decode_attn_weighted_plan(None, 1, ctypes.byref(ctypes.c_int())) == NULL
     assert L.cmc_decode_attn_weighted_plan(_dims(), 1, None) == NULL
