@@ -258,7 +258,7 @@ static int run_prefill(const void* q, int64_t q_stride, const void* k, int64_t k
   const Range outs[] = {heads(out_q, qd, qd), heads(out_k, kd, kd), {ring_k, ring_bytes}, {ring_v, ring_bytes}};
   for (int o = 0; o < 4; ++o) {
     for (int i = 0; i < 3; ++i) {
-      const bool there = i == o && in[i].at == outs[o].at && in[i].bytes == outs[o].bytes;
+      const bool there = i == o && o < 2 && same(in[i], outs[o]);  // out_q in q, out_k in k
       if (!there && meet(outs[o], in[i])) return CMC_ERR_RANGE;
     }
     for (int i = 0; i < o; ++i)

@@ -200,6 +200,15 @@ def test_prefill_argument_checks(L):
         assert _prefill(L, prep=evil, **change) == ALIGN
 
 
+@host_only
+def test_prefill_refuses_a_ring_in_the_values(L):
+    """Prepared keys over values that other warps have not read yet: dense, as many slots as tokens."""
+    evil = _prep(q_weight=FAKE + 4)  # refused after these
+    for change in (dict(rk=3 * BIG), dict(rv=3 * BIG), dict(rk=2 * BIG), dict(rv=2 * BIG), dict(rk=3 * BIG + 512)):
+        assert _prefill(L, T=16, prep=evil, **change) == RANGE
+    assert _prefill(L, T=16, prep=evil) == ALIGN and _prefill(L, T=16, prep=evil, oq=BIG) == ALIGN
+
+
 def _attend(L, q=FAKE, tk=FAKE, tv=FAKE, tw=FAKE, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE, dims=None, out=FAKE,
             ws=FAKE, wsb=512):
     return L.cmc_two_tier_decode_attn_weighted(q, tk, tv, tw, rk, rv, rw, pos, dims or _dims(), 0.0, out, ws,
