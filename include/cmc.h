@@ -628,8 +628,8 @@ typedef struct cmc_qk_prep {
  *   k      bf16 [B, L, T, Hkv, d], k_stride likewise
  *   pos    int64 [B] (read only; any value)
  *   out_q  bf16 [B, L, T, Hq, d] dense; may be q where that is dense too
- *   out_k  bf16 [B, L, T, Hkv, d] dense; may be k likewise.  Outputs otherwise meet neither inputs nor each
- *          other (CMC_ERR_RANGE)
+ *   out_k  bf16 [B, L, T, Hkv, d] dense; may be k likewise.  Outputs otherwise meet nothing that is read (pos and
+ *          what the prep names too) and not each other (CMC_ERR_RANGE)
  *
  * dims->N, k and W are ignored.  T == 0 launches nothing.  Limits: 0 <= T <= 2^24, L * T < 2^27.
  */
@@ -657,7 +657,8 @@ CMC_API size_t cmc_cache_workspace_size(int B);
  *                   are not written
  *   workspace       see cmc_cache_workspace_size
  *
- * The rings and out_q meet neither the inputs nor each other, but for out_q and q (CMC_ERR_RANGE).
+ * What is written (the rings, their weights, out_q, pos and the workspace) meets nothing that is read and nothing else that
+ * is written, but for out_q and q (CMC_ERR_RANGE).
  * dims->N and k are ignored.  A sequence with pos[b] < 0 is left unchanged, its out_q too, and
  * CMC_DEVFLAG_BAD_POS is set.  T == 0 launches nothing.  Limits as for cmc_qk_norm_rope.
  */

@@ -268,6 +268,12 @@ static int run_prefill(const void* q, int64_t q_stride, const void* k, int64_t k
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   st = prep_params(prep, m.d, s, &p.prep);
   if (st != CMC_OK) return st;
+  // Nor do the weights, the positions and the workspace meet anything, or the outputs what the preparation reads.
+  const size_t each = static_cast<size_t>(m.B) * 8, gains = static_cast<size_t>(m.L) * m.d * 4;
+  const Range more_in[] = {{count, each}, {p.prep.evicted, each}, {p.prep.q_weight, gains}, {p.prep.k_weight, gains}, {ring ? nullptr : pos, each}};
+  const Range more_outs[] = {{ring_weight, ring_bytes / (2 * m.d) * 4}, {ring ? pos : nullptr, each}, {workspace, ring ? ws_partials_off(m.B) : 0}};
+  if (any_meet(outs, more_in) || any_meet(more_outs, in) || any_meet(more_outs, outs) || any_meet(more_outs, more_in) || any_meet(more_outs))
+    return CMC_ERR_RANGE;
   p.q = static_cast<const uint16_t*>(q);
   p.k = static_cast<const uint16_t*>(k);
   p.v = static_cast<const uint16_t*>(v);

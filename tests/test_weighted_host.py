@@ -209,6 +209,30 @@ def test_prefill_refuses_a_ring_in_the_values(L):
     assert _prefill(L, T=16, prep=evil) == ALIGN and _prefill(L, T=16, prep=evil, oq=BIG) == ALIGN
 
 
+@host_only
+def test_prefill_and_norm_overlaps(L):
+    """Weights, positions, counts, gains and the workspace: 24 tokens, rings of 16 slots, 49,152 bytes each, weights 768."""
+    CUDA = 6  # all checks passed: no device
+    a = dict(rw=7 * BIG, pos=8 * BIG, count=8 * BIG + 64, ws=9 * BIG)
+    prep = dict(q_weight=10 * BIG, k_weight=10 * BIG + 1536, evicted=8 * BIG + 16, rope_theta=1e4)
+    assert _prefill(L, prep=_prep(**prep), **a) == CUDA
+    assert _prefill(L, **{**a, "count": 0, "rw": 0}) == CUDA
+    for change in (dict(count=8 * BIG), dict(count=8 * BIG + 8), dict(rw=4 * BIG), dict(rw=5 * BIG + 49148), dict(rw=6 * BIG),
+                   dict(rw=BIG), dict(rw=3 * BIG + 8), dict(rw=8 * BIG - 764), dict(rw=9 * BIG + 508), dict(pos=4 * BIG),
+                   dict(pos=9 * BIG + 504), dict(pos=2 * BIG), dict(pos=6 * BIG + 8), dict(ws=5 * BIG), dict(ws=BIG), dict(count=4 * BIG),
+                   dict(count=7 * BIG + 760), dict(ws=8 * BIG + 64)):
+        assert _prefill(L, prep=_prep(**prep), **{**a, **change}) == RANGE, change
+    for change in (dict(evicted=8 * BIG), dict(evicted=7 * BIG), dict(evicted=9 * BIG), dict(q_weight=4 * BIG), dict(k_weight=7 * BIG - 1520),
+                   dict(q_weight=6 * BIG), dict(k_weight=9 * BIG + 16)):
+        assert _prefill(L, prep=_prep(**{**prep, **change}), **a) == RANGE, change
+    assert _prefill(L, prep=_prep(**{**prep, "k_weight": 10 * BIG, "evicted": 8 * BIG + 64}), **a) == CUDA  # what is read may meet
+    assert _norm(L) == CUDA and _norm(L, pos=BIG) == CUDA
+    for change in (dict(pos=3 * BIG), dict(pos=4 * BIG + 24 * 512 - 8)):
+        assert _norm(L, **change) == RANGE
+    for change in (dict(q_weight=3 * BIG), dict(k_weight=4 * BIG + 16), dict(evicted=3 * BIG + 8)):
+        assert _norm(L, prep=_prep(**change)) == RANGE
+
+
 def _attend(L, q=FAKE, tk=FAKE, tv=FAKE, tw=FAKE, rk=FAKE, rv=FAKE, rw=FAKE, pos=FAKE, dims=None, out=FAKE,
             ws=FAKE, wsb=512):
     return L.cmc_two_tier_decode_attn_weighted(q, tk, tv, tw, rk, rv, rw, pos, dims or _dims(), 0.0, out, ws,
