@@ -688,6 +688,8 @@ CMC_API size_t cmc_decode_attn_weighted_workspace_size(const cmc_dims* dims);
  * NaN in its head's output and in all weights of its KV head; one of minus infinity counts nothing.  A NaN or infinity among the
  * values reaches the outputs alone.  A sequence with pos[b] < 0 gets a zero output, its
  * weights stay, and CMC_DEVFLAG_BAD_POS is set.
+ * out may be q; otherwise what is written (out, the weights, the workspace) meets nothing that is read and nothing else
+ * that is written (CMC_ERR_RANGE).
  */
 CMC_API int cmc_two_tier_decode_attn_weighted(const void* q, const void* tier1_k, const void* tier1_v,
                                               float* tier1_weight, const void* ring_k,
@@ -702,7 +704,8 @@ CMC_API int cmc_two_tier_decode_attn_weighted(const void* q, const void* tier1_k
  * its norm and rotation, at position rope_offset + evicted[b] + pos[b] (pos before the append).  The
  * prepared key is rounded to bf16, as it is stored and attended to; the prepared query is held to 16
  * significant bits.  A sequence with pos[b] < 0 is left unchanged, its output is zero and
- * CMC_DEVFLAG_BAD_POS is set.
+ * CMC_DEVFLAG_BAD_POS is set.  The rings and pos are among what is written, the new token and what the prep names among
+ * what is read.
  */
 CMC_API int cmc_decode_step_weighted(const void* q, const void* tier1_k, const void* tier1_v,
                                      float* tier1_weight, void* ring_k, void* ring_v,

@@ -938,6 +938,19 @@ static int run_weighted(const void* q, const void* t1k, const void* t1v, float* 
   WeightedParams p;
   st = prep_params(fused ? prep : nullptr, m.d, s, &p.prep);
   if (st != CMC_OK) return st;
+  // CTAs read and write in any order: what is written meets nothing else, but that a unit's output may take its queries' place (they
+  // have all been read when it is stored).
+  const size_t units = static_cast<size_t>(m.B) * m.L * m.Hkv, row = m.d * 2, each = static_cast<size_t>(m.B) * 8;
+  const size_t bank = m.k > 0 ? units * m.N : 0, ring = units * m.W, gains = static_cast<size_t>(m.L) * m.d * 4;
+  const Range heads = {q, units * (m.Hq / m.Hkv) * row}, outputs = {out, heads.bytes};
+  const Range reads[] = {{t1k, bank * row}, {t1v, bank * row}, {k_new, units * row}, {v_new, units * row}, {p.prep.q_weight, gains},
+                         {p.prep.k_weight, gains}, {p.prep.evicted, each}, {fused ? nullptr : ring_k, ring * row},
+                         {fused ? nullptr : ring_v, ring * row}, {fused ? nullptr : pos, each}};
+  const Range writes[] = {outputs, {t1w, bank * 4}, {ring_w, ring * 4}, {workspace, weighted_ws(m)}, {fused ? ring_k : nullptr, ring * row},
+                          {fused ? ring_v : nullptr, ring * row}, {fused ? pos : nullptr, each}};
+  if (any_meet(writes, reads) || any_meet(writes)) return CMC_ERR_RANGE;
+  for (const Range& w : writes)
+    if (meet(w, heads) && !same(w, heads)) return CMC_ERR_RANGE;
   p.q = static_cast<const uint16_t*>(q);
   p.t1k = static_cast<const uint16_t*>(t1k);
   p.t1v = static_cast<const uint16_t*>(t1v);

@@ -33,7 +33,7 @@ struct Range {
 };
 inline bool meet(const Range& a, const Range& b) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
-  return a.at && b.at && x < y + b.bytes && y < x + a.bytes;
+  return a.at && b.at && a.bytes && b.bytes && x < y + b.bytes && y < x + a.bytes;
 }
 inline bool same(const Range& a, const Range& b) { return a.at == b.at && a.bytes == b.bytes; }
 // Whether one of `a` meets one of `b`, or another of `a`.

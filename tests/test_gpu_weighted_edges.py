@@ -159,3 +159,26 @@ def test_eviction_refuses_outputs_that_meet(cuda_device):
     w[..., [1, 4, 5, 8]] = 1.0
     cmc.evict_cache(k, k, w, 4, pos=pos, out_k=k, out_v=k, out_weight=w, out_pos=pos)
     assert pos.tolist() == [4, 4] and k[0, 0, 0, :4, 0].tolist() == [1.0, 4.0, 5.0, 8.0]
+
+
+@pytest.mark.parametrize("unit", list(PLACES))
+@pytest.mark.parametrize("prepared", [False, True])
+def test_outputs_in_the_queries_place(cuda_device, unit, prepared):
+    """The one overlap that is allowed, in every variant; others are refused and change nothing."""
+    B, H, k = PLACES[unit]
+    form = "both" if prepared else "plain"
+    q, t1, ring, pos, new, opts, _ = step_inputs(cuda_device, (B, 1, H, 4, 64, k, 70, list(range(70))), form, 42)
+    state = [x.clone() for x in (*t1, *ring, pos)]
+    want = cmc.decode_step_weighted(q, *state, *new, **opts)
+    args = [*t1, *ring, pos]
+    before = [x.clone() for x in args]
+    inside = ring[0].view(-1)[:q.numel()].view(q.shape)
+    for change in (dict(out=inside), dict(out=t1[1].view(-1)[:q.numel()].view(q.shape))):
+        with pytest.raises(cmc.CmcError, match="RANGE"):
+            cmc.decode_step_weighted(q, *args, *new, **opts, **change)
+    for x, y in zip(args, before):
+        assert torch.equal(x, y)
+    got = cmc.decode_step_weighted(q, *args, *new, out=q, **opts)
+    assert got is q and torch.equal(got, want)
+    for x, y in zip(args, state):
+        assert torch.equal(x, y)

@@ -261,6 +261,37 @@ def test_weighted_attention_argument_checks(L, call):
 
 
 @host_only
+@pytest.mark.parametrize("call", [_attend, _step])
+def test_weighted_attention_overlaps(L, call):
+    """48 query heads' rows, 12,288 bytes; Tier-1 of 12 x 100 rows, 307,200 and 4,800; rings of 12 x 16, 49,152 and 768; new rows
+    3,072."""
+    CUDA = 6  # all checks passed: no device
+    a = dict(q=BIG, tk=2 * BIG, tv=3 * BIG, tw=4 * BIG, rk=5 * BIG, rv=6 * BIG, rw=7 * BIG, pos=8 * BIG, out=9 * BIG, ws=10 * BIG)
+    step = call is _step
+    if step:
+        a.update(kn=11 * BIG, vn=12 * BIG)
+    assert call(L, **a) == CUDA
+    bad = [dict(out=BIG + 16), dict(out=BIG - 16), dict(out=2 * BIG), dict(out=3 * BIG + 307184), dict(out=4 * BIG), dict(out=5 * BIG),
+           dict(out=6 * BIG + 49136), dict(out=7 * BIG), dict(out=10 * BIG + 496), dict(out=8 * BIG), dict(rw=4 * BIG), dict(rw=4 * BIG + 4796),
+           dict(tw=2 * BIG), dict(tw=6 * BIG), dict(rw=BIG), dict(rw=8 * BIG - 764), dict(rw=3 * BIG), dict(tw=10 * BIG), dict(ws=5 * BIG),
+           dict(ws=8 * BIG), dict(ws=2 * BIG + 307184)]
+    ring_reads = [dict(rk=6 * BIG), dict(rk=2 * BIG), dict(rv=3 * BIG + 307184), dict(rk=BIG), dict(pos=BIG), dict(pos=2 * BIG)]
+    good = [dict(out=BIG), dict(out=BIG + 12288), dict(rw=4 * BIG + 4800), dict(rw=8 * BIG - 768), dict(tk=3 * BIG),
+            dict(dims=_dims(k=0), tk=9 * BIG, tv=9 * BIG, tw=9 * BIG), dict(out=10 * BIG + 512)]
+    if step:
+        bad += ring_reads + [dict(kn=5 * BIG), dict(vn=6 * BIG + 49136), dict(kn=9 * BIG), dict(vn=7 * BIG), dict(kn=10 * BIG),
+                             dict(prep=_prep(evicted=8 * BIG)), dict(prep=_prep(q_weight=9 * BIG)), dict(prep=_prep(k_weight=7 * BIG)),
+                             dict(prep=_prep(evicted=4 * BIG))]
+        good += [dict(kn=12 * BIG), dict(vn=BIG), dict(prep=_prep(q_weight=BIG, evicted=8 * BIG + 16))]
+    else:
+        good += ring_reads
+    for change in bad:
+        assert call(L, **{**a, **change}) == RANGE, change
+    for change in good:
+        assert call(L, **{**a, **change}) == CUDA, change
+
+
+@host_only
 def test_step_prep_checks(L):
     assert _step(L, prep=_prep(rope_theta=float("nan"))) == RANGE
     assert _step(L, prep=_prep(rope_offset=-1)) == RANGE
