@@ -608,7 +608,8 @@ CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas);
  * in fp32, rounded once.  Angles as for cmc_decode_step_rope, at
  *     p = rope_offset + evicted[b] + pos[b] + t
  * for token t of a call: pos[b] counts the tokens that the ring was given and evicted[b] those
- * that cmc_evict_cache took out of it again.  A NULL cmc_qk_prep is neither norm nor rotation.
+ * that cmc_evict_cache took out of it again.  A NULL cmc_qk_prep is neither norm nor rotation.  A token at one position has
+ * the same key bit for bit from cmc_qk_norm_rope, cmc_window_prefill and cmc_decode_step_weighted.
  */
 typedef struct cmc_qk_prep {
   const float* q_weight;  /* fp32 [L, d], 16-byte aligned, or NULL: no norm of the queries  */

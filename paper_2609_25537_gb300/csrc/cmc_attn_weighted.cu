@@ -253,30 +253,27 @@ struct Preparer {
     float2 cs[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e) cs[e] = p.prep.rope ? rope_cos_sin(at, turns[e]) : make_float2(1.f, 0.f);
+    float4 pair[2][2];  // of the queries, of the key
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const bool norm = (x == 0 ? p.prep.q_weight : p.prep.k_weight) != nullptr;
+      pair[x][0] = pair_factors(norm ? gain[x][0].x : 1.f, norm ? gain[x][1].x : 1.f, cs[0]);
+      pair[x][1] = pair_factors(norm ? gain[x][0].y : 1.f, norm ? gain[x][1].y : 1.f, cs[1]);
+    }
 #pragma unroll
     for (int i = 0; i < kRows; ++i) {
       const int r = warp + i * NW;
       if (r > G) break;
       float x[4] = {bf16lo_to_f32(row[i][0]), bf16hi_to_f32(row[i][0]), bf16lo_to_f32(row[i][1]), bf16hi_to_f32(row[i][1])};
+      float f = 1.f;
       if ((r < G ? p.prep.q_weight : p.prep.k_weight) != nullptr) {
-        float s = fmaf(x[0], x[0], x[1] * x[1]) + fmaf(x[2], x[2], x[3] * x[3]);
+        float s = quad_squares(x[0], x[1], x[2], x[3]);
 #pragma unroll
         for (int off = 1; off < 32; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        const float f = 1.f / sqrtf(fmaf(s, 1.f / D, p.prep.eps));
-        const float2 g0 = r < G ? gain[0][0] : gain[1][0], g1 = r < G ? gain[0][1] : gain[1][1];
-        x[0] *= f * g0.x;
-        x[1] *= f * g0.y;
-        x[2] *= f * g1.x;
-        x[3] *= f * g1.y;
+        f = rms_factor<D>(s, p.prep.eps);
       }
-      if (p.prep.rope) {
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float lo = x[e], hi = x[2 + e];
-          x[e] = fmaf(lo, cs[e].x, -hi * cs[e].y);
-          x[2 + e] = fmaf(hi, cs[e].x, lo * cs[e].y);
-        }
-      }
+      prep_pair(x[0], x[2], f, p.prep.rope, r < G ? pair[0][0] : pair[1][0]);
+      prep_pair(x[1], x[3], f, p.prep.rope, r < G ? pair[0][1] : pair[1][1]);
       if (lane >= D / 4) continue;
       uint16_t* to = reinterpret_cast<uint16_t*>(smem + (r < G ? S::kQ + r * D * 2 : S::kNew)) + 2 * lane;
       const uint32_t a = pack_bf16_rn(x[0], x[1]), z = pack_bf16_rn(x[2], x[3]);

@@ -51,7 +51,7 @@ struct __align__(16) TokenTable {
   float4 pair[2][8][Prep<D>::kLanes];  // [queries, keys][e][c]: pair 8 c + e
 };
 
-// Two chunks of a row: x' = r (x g cos - y h sin), y' = r (y h cos + x g sin) with rotation, r x g and r y h without.
+// Two chunks of a row, in place, by its factor r.
 template <int D>
 __device__ __forceinline__ void prep_chunks(uint4 (&a)[2], float r, bool rope, const float4 (&pair)[8][Prep<D>::kLanes], int c) {
   uint32_t* lo = reinterpret_cast<uint32_t*>(&a[0]);
@@ -60,31 +60,25 @@ __device__ __forceinline__ void prep_chunks(uint4 (&a)[2], float r, bool rope, c
   for (int q = 0; q < 4; ++q) {
     float x[2] = {bf16lo_to_f32(lo[q]), bf16hi_to_f32(lo[q])}, y[2] = {bf16lo_to_f32(hi[q]), bf16hi_to_f32(hi[q])};
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const float4 t = pair[2 * q + e][c];
-      const float u = x[e], v = y[e];
-      x[e] = r * (rope ? fmaf(u, t.x, -v * t.y) : u * t.x);
-      y[e] = r * (rope ? fmaf(v, t.z, u * t.w) : v * t.z);
-    }
+    for (int e = 0; e < 2; ++e) prep_pair(x[e], y[e], r, rope, pair[2 * q + e][c]);
     lo[q] = pack_bf16_rn(x[0], x[1]);
     hi[q] = pack_bf16_rn(y[0], y[1]);
   }
 }
 
-// 1 / sqrt(mean of squares + eps) of a row, given to all of its lanes (rsqrtf: 2^-22).
+// A row's norm, given to all of its lanes, four quads each.
 template <int D>
 __device__ __forceinline__ float prep_rms(const uint4 (&a)[2], float eps) {
-  float s = 0.f;
+  const uint32_t* lo = reinterpret_cast<const uint32_t*>(&a[0]);
+  const uint32_t* hi = reinterpret_cast<const uint32_t*>(&a[1]);
+  float quad[4];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    float x[8];
-    unpack8(a[h], x);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s = fmaf(x[e], x[e], s);
-  }
+  for (int q = 0; q < 4; ++q)
+    quad[q] = quad_squares(bf16lo_to_f32(lo[q]), bf16hi_to_f32(lo[q]), bf16lo_to_f32(hi[q]), bf16hi_to_f32(hi[q]));
+  float s = (quad[0] + quad[1]) + (quad[2] + quad[3]);
 #pragma unroll
   for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  return rsqrtf(fmaf(s, 1.f / D, eps));
+  return rms_factor<D>(s, eps);
 }
 
 // A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.
@@ -165,7 +159,7 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
         for (int x = 0; x < 2; ++x) {
           const float* w = x == 0 ? p.prep.q_weight : p.prep.k_weight;
           const float g = w ? w[static_cast<long long>(l) * D + i] : 1.f, h = w ? w[static_cast<long long>(l) * D + D / 2 + i] : 1.f;
-          table.pair[x][i % 8][i / 8] = make_float4(g * cs.x, h * cs.y, h * cs.x, g * cs.y);
+          table.pair[x][i % 8][i / 8] = pair_factors(g, h, cs);
         }
       }
       __syncwarp();

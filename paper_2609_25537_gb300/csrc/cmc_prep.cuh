@@ -4,7 +4,7 @@
 //   out_i       = y_i cos a_i - y_(i + d/2) sin a_i
 //   out_(i+d/2) = y_(i + d/2) cos a_i + y_i sin a_i,   a_i = p theta^(-2i/d)
 // all in fp32; the caller rounds once, to bf16 (a model that rounds between the two has one
-// rounding more).
+// rounding more).  The callers have a row in different lanes, d / 16 or d / 4 to a row, and take the same steps.
 #pragma once
 
 #include "cmc_attn.cuh"
@@ -22,6 +22,34 @@ struct PrepParams {
   long long rope_offset;
   unsigned long long rope_turns[64];
 };
+
+// ---------------------------------------------------------------------------
+// Device side: the arithmetic, operation by operation, so that a token has the same key bit for bit whichever call prepares it
+// ---------------------------------------------------------------------------
+
+// Sum of squares of a row.  Quad j, elements 2 j, 2 j + 1 and their partners d / 2 further on, in this order; the d / 4 quads in a
+// tree of neighbours: 0 with 1, 2 with 3, then their sums, and so on (a butterfly over lanes gives all of them the same).
+__device__ __forceinline__ float quad_squares(float x0, float x1, float y0, float y1) {
+  return fmaf(y1, y1, fmaf(y0, y0, fmaf(x1, x1, __fmul_rn(x0, x0))));
+}
+
+// 1 / sqrt(mean of squares + eps) (rsqrtf: 2^-22).
+template <int D>
+__device__ __forceinline__ float rms_factor(float squares, float eps) {
+  return rsqrtf(fmaf(squares, 1.f / D, eps));
+}
+
+// What a pair's gains g, h and its angle make of it: (g cos a, h sin a, h cos a, g sin a).
+__device__ __forceinline__ float4 pair_factors(float g, float h, float2 cos_sin) {
+  return make_float4(__fmul_rn(g, cos_sin.x), __fmul_rn(h, cos_sin.y), __fmul_rn(h, cos_sin.x), __fmul_rn(g, cos_sin.y));
+}
+
+// Elements x and y of a pair, by their row's factor r and the pair's t.
+__device__ __forceinline__ void prep_pair(float& x, float& y, float r, bool rope, const float4& t) {
+  const float u = __fmul_rn(r, x), v = __fmul_rn(r, y);
+  x = rope ? fmaf(u, t.x, -__fmul_rn(v, t.y)) : __fmul_rn(u, t.x);
+  y = rope ? fmaf(v, t.z, __fmul_rn(u, t.w)) : __fmul_rn(v, t.z);
+}
 
 // ---------------------------------------------------------------------------
 // Host side

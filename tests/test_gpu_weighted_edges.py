@@ -182,3 +182,25 @@ def test_outputs_in_the_queries_place(cuda_device, unit, prepared):
     assert got is q and torch.equal(got, want)
     for x, y in zip(args, state):
         assert torch.equal(x, y)
+
+
+@pytest.mark.parametrize("form", ["norm", "rope", "both"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_token_has_the_same_key_prefilled_and_stepped(cuda_device, d, form):
+    """Bit for bit, in each variant of the step, and as qk_norm_rope gives it."""
+    for B, H, k in PLACES.values():
+        q, t1, ring, pos, g = attention_problem(cuda_device, (B, 3, H, 1, d, k, 70, [0, 3, 10 ** 6, 69, 2 ** 33]), 43, poison=False)
+        k_new, v_new = randn(g, B, 3, H, d, scale=2.0), randn(g, B, 3, H, d)
+        opts = {}
+        if form in ("norm", "both"):
+            opts.update(q_weight=1 + torch.randn(3, d, generator=g, device=cuda_device), k_weight=1 + torch.randn(3, d, generator=g, device=cuda_device))
+        if form in ("rope", "both"):
+            opts.update(rope_theta=THETA, rope_offset=k)
+        other = [x.clone() for x in (ring[0], ring[1], pos)]
+        _, key = cmc.qk_norm_rope(q, k_new, pos, **opts)
+        cmc.window_prefill(None, k_new, v_new, *other, **opts)
+        cmc.decode_step_weighted(q, *t1, *ring, pos, k_new, v_new, **opts)
+        for x, y in zip(other, (ring[0], ring[1], pos)):
+            assert torch.equal(x, y)
+        slot = ((pos - 1) % 70).tolist()
+        assert torch.equal(key, torch.stack([ring[0][b, :, :, s] for b, s in enumerate(slot)]))
