@@ -605,7 +605,8 @@ CMC_API int cmc_decode_attn_q8_plan(const cmc_dims* dims, int fused, int* ctas);
  * or cached.  For head row x (d elements) of layer l, at position p:
  *     y = x / sqrt(mean(x^2) + eps) * w[l]                  (RMS norm, where w is given)
  *     (y_i, y_(i + d/2)) turned by the angle p * rope_theta^(-2i/d)   (where rope_theta > 0)
- * in fp32, rounded once.  Angles as for cmc_decode_step_rope, at
+ * in fp32, rounded once; rows may be of any magnitude that bf16 holds (a row with an infinity: NaN there, and 0 elsewhere).  Angles as
+ * for cmc_decode_step_rope, at
  *     p = rope_offset + evicted[b] + pos[b] + t
  * for token t of a call: pos[b] counts the tokens that the ring was given and evicted[b] those
  * that cmc_evict_cache took out of it again.  A NULL cmc_qk_prep is neither norm nor rotation.  A token at one position has

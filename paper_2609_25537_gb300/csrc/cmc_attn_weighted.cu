@@ -202,6 +202,14 @@ __device__ __forceinline__ void request_rows(const uint16_t* base, int rows, int
   }
 }
 
+// The sum of squares of a row, four elements a lane.
+__device__ __forceinline__ float row_squares(const float (&x)[4], float by) {
+  float s = quad_squares(by * x[0], by * x[1], by * x[2], by * x[3]);
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
+  return s;
+}
+
 // Norm and rotation of the unit's G query heads and of the new key, a row a warp, into shared memory.  Lane i
 // < d / 4 has elements 2 i, 2 i + 1 and their partners d / 2 further on.  Everything that it reads is requested at once
 // (`turns` before the grid dependency wait), and the norm does not wait for pos: what is left on the way to the first
@@ -245,7 +253,7 @@ struct Preparer {
       }
     }
   }
-  __device__ __forceinline__ void finish(const WeightedParams& p, long long pos, int warp, int lane,
+  __device__ __forceinline__ void finish(const WeightedParams& p, long long u, long long pos, int warp, int lane,
                                          uint8_t* smem) {
     using S = WSmem<D, G, true, NW>;
     const unsigned long long at = static_cast<unsigned long long>(p.prep.rope_offset + pos) +
@@ -260,21 +268,10 @@ struct Preparer {
       pair[x][0] = pair_factors(norm ? gain[x][0].x : 1.f, norm ? gain[x][1].x : 1.f, cs[0]);
       pair[x][1] = pair_factors(norm ? gain[x][0].y : 1.f, norm ? gain[x][1].y : 1.f, cs[1]);
     }
-#pragma unroll
-    for (int i = 0; i < kRows; ++i) {
-      const int r = warp + i * NW;
-      if (r > G) break;
-      float x[4] = {bf16lo_to_f32(row[i][0]), bf16hi_to_f32(row[i][0]), bf16lo_to_f32(row[i][1]), bf16hi_to_f32(row[i][1])};
-      float f = 1.f;
-      if ((r < G ? p.prep.q_weight : p.prep.k_weight) != nullptr) {
-        float s = quad_squares(x[0], x[1], x[2], x[3]);
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-        f = rms_factor<D>(s, p.prep.eps);
-      }
+    auto turn_and_put = [&](int r, float (&x)[4], float f) {
       prep_pair(x[0], x[2], f, p.prep.rope, r < G ? pair[0][0] : pair[1][0]);
       prep_pair(x[1], x[3], f, p.prep.rope, r < G ? pair[0][1] : pair[1][1]);
-      if (lane >= D / 4) continue;
+      if (lane >= D / 4) return;
       uint16_t* to = reinterpret_cast<uint16_t*>(smem + (r < G ? S::kQ + r * D * 2 : S::kNew)) + 2 * lane;
       const uint32_t a = pack_bf16_rn(x[0], x[1]), z = pack_bf16_rn(x[2], x[3]);
       *reinterpret_cast<uint32_t*>(to) = a;
@@ -286,6 +283,41 @@ struct Preparer {
         to += G * D;
         *reinterpret_cast<uint32_t*>(to) = pack_bf16_rn(x[0], x[1]);
         *reinterpret_cast<uint32_t*>(to + D / 2) = pack_bf16_rn(x[2], x[3]);
+      }
+    };
+    auto has_norm = [&](int r) { return (r < G ? p.prep.q_weight : p.prep.k_weight) != nullptr; };
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < kRows; ++i) {
+      const int r = warp + i * NW;
+      if (r > G) break;
+      float x[4] = {bf16lo_to_f32(row[i][0]), bf16hi_to_f32(row[i][0]), bf16lo_to_f32(row[i][1]), bf16hi_to_f32(row[i][1])};
+      float f = 1.f;
+      if (has_norm(r)) {
+        const float mean = row_mean<D>(row_squares(x, 1.f), p.prep.eps);
+        f = rsqrtf(mean);
+        odd |= odd_mean(mean);
+      }
+      turn_and_put(r, x, f);
+    }
+    if (odd) {  // a row whose mean is odd (the same in all lanes): the warp's rows again, from memory
+#pragma unroll 1
+      for (int r = warp; r <= G; r += NW) {
+        if (!has_norm(r)) continue;
+        const uint16_t* src = (r < G ? p.q + (u * G + r) * D : p.k_new + u * D) + 2 * lane % (D / 2);
+        const uint32_t lo = lane < D / 4 ? *reinterpret_cast<const uint32_t*>(src) : 0u;
+        const uint32_t hi = lane < D / 4 ? *reinterpret_cast<const uint32_t*>(src + D / 2) : 0u;
+        __syncwarp();
+        float x[4] = {bf16lo_to_f32(lo), bf16hi_to_f32(lo), bf16lo_to_f32(hi), bf16hi_to_f32(hi)};
+        const float mean = row_mean<D>(row_squares(x, 1.f), p.prep.eps);
+        if (!odd_mean(mean)) continue;
+        const float by = odd_scale(mean);
+        float f = rsqrtf(row_mean<D>(row_squares(x, by), p.prep.eps, by));
+        if (by < 1.f) f *= by;
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] *= by;
+        turn_and_put(r, x, f);
       }
     }
   }
@@ -441,7 +473,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
   const uint16_t* prepared = nullptr;
   if (PREP) {
     prepared = reinterpret_cast<const uint16_t*>(smem + S::kNew);
-    prep.finish(p, pos, warp, lane, smem);
+    prep.finish(p, u, pos, warp, lane, smem);
     __syncthreads();
     if (g < G) {
 #pragma unroll

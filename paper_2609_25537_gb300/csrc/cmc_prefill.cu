@@ -4,8 +4,8 @@
 // Bound: HBM, every head's row read once and written once (4 d bytes against some 10 d flops).  A warp takes a
 // token: what its position and the layer's gains make of a row goes to shared memory once, then its heads' rows pass through
 // registers.  What limits the rate beside HBM is the instructions of a row, and rows on their way: 8 sequences of 4,096 tokens
-// of 32 + 2 x 8 heads of 128 into rings of 2,048 slots, us a launch at two rows a lane group and 8 CTAs of four warps an SM 111 (90 %
-// of the copy rate), three and 6 112, two and 6 120, one and 8 123; 8,192 tokens' queries and keys alone 31.0 (81 %).
+// of 32 + 2 x 8 heads of 128 into rings of 2,048 slots, us a launch at two rows a lane group and 8 CTAs of four warps an SM 110.5 (91 %
+// of the copy rate), three and 6 112, two and 6 120, one and 8 123; 8,192 tokens' queries and keys alone 31.4 (80 %).
 #include "cmc_prep.cuh"
 
 namespace cmc {
@@ -66,23 +66,44 @@ __device__ __forceinline__ void prep_chunks(uint4 (&a)[2], float r, bool rope, c
   }
 }
 
-// A row's norm, given to all of its lanes, four quads each.
+// The sum of squares of a row taken `by` times as large, given to all of its lanes, four quads each.
 template <int D>
-__device__ __forceinline__ float prep_rms(const uint4 (&a)[2], float eps) {
-  const uint32_t* lo = reinterpret_cast<const uint32_t*>(&a[0]);
-  const uint32_t* hi = reinterpret_cast<const uint32_t*>(&a[1]);
+__device__ __forceinline__ float prep_squares(const uint4& a, const uint4& b, float by) {
+  const uint32_t* lo = reinterpret_cast<const uint32_t*>(&a);
+  const uint32_t* hi = reinterpret_cast<const uint32_t*>(&b);
   float quad[4];
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    quad[q] = quad_squares(bf16lo_to_f32(lo[q]), bf16hi_to_f32(lo[q]), bf16lo_to_f32(hi[q]), bf16hi_to_f32(hi[q]));
+    quad[q] = quad_squares(by * bf16lo_to_f32(lo[q]), by * bf16hi_to_f32(lo[q]), by * bf16lo_to_f32(hi[q]), by * bf16hi_to_f32(hi[q]));
   float s = (quad[0] + quad[1]) + (quad[2] + quad[3]);
 #pragma unroll
   for (int off = 1; off < Prep<D>::kLanes; off <<= 1) s += __shfl_xor_sync(0xffffffffu, s, off);
-  return rms_factor<D>(s, eps);
+  return s;
 }
 
-// A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.
-template <int D, bool RING>
+// The factor of a row whose mean is odd (all of a warp's lanes come here, for the sum); one of the smallest elements is taken 2^80 times
+// as large.
+template <int D>
+__device__ __forceinline__ float prep_odd_row(uint4 (&a)[2], float mean, float eps) {
+  const float by = odd_scale(mean);
+  const float f = rsqrtf(row_mean<D>(prep_squares<D>(a[0], a[1], by), eps, by));
+  if (by < 1.f) return f * by;
+  if (odd_mean(mean)) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t* x = reinterpret_cast<uint32_t*>(&a[h]);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) x[q] = pack_bf16_rn(by * bf16lo_to_f32(x[q]), by * bf16hi_to_f32(x[q]));
+    }
+  }
+  return f;
+}
+
+// A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.  Rows whose mean is odd: an
+// instruction a row keeps the oddest mean, and a warp that has met one takes its rows again in the end, which costs nothing that can be
+// measured.  Where rows are written over (PLACE: queries or keys prepared where they are) each is looked at at once, with a vote: 8
+// sequences of 4,096 tokens 117 us for 110.5, of 1,024 without a ring 33.5 for 31.5.
+template <int D, bool RING, bool PLACE>
 __global__ void __launch_bounds__(32 * kPrefillWarps, kPrefillPerSm)
 prefill_kernel(const __grid_constant__ PrefillParams p) {
   using P = Prep<D>;
@@ -179,6 +200,16 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
     uint16_t* to_k = RING ? p.ring_k + (unit0 * p.W + slot) * D + 8 * c : p.out_k + row0 * p.Hkv * D + 8 * c;
     uint16_t* to_v = p.ring_v + (unit0 * p.W + slot) * D + 8 * c;
     const long long step = RING ? static_cast<long long>(p.W) * D : D;  // from one KV head's row to the next
+    auto store = [&](int r, const uint4 (&x)[2]) {
+      const bool is_v = r >= nq + p.Hkv;
+      uint16_t* dst = r < nq    ? to_q + r * D
+                      : is_v ? to_v + (r - nq - p.Hkv) * step
+                             : to_k + (r - nq) * step;
+      *reinterpret_cast<uint4*>(dst) = x[0];
+      *reinterpret_cast<uint4*>(dst + D / 2) = x[1];
+      if (RING && is_v && c == 0 && p.ring_weight) p.ring_weight[(unit0 + r - nq - p.Hkv) * p.W + slot] = 0.f;
+    };
+    uint32_t odd = 0;  // the most that a row's mean, as a place among floats, is above kOddMean (modulo 2^32: or below)
     for (int s0 = first; s0 < end; s0 += kPrefillBatch) {
       if (s0 > first || !early) load(s0, end, rows);
 #pragma unroll
@@ -189,18 +220,39 @@ prefill_kernel(const __grid_constant__ PrefillParams p) {
         const bool is_q = r < nq;
         float f = 1.f;
         if (norm) {
-          f = prep_rms<D>(a[e], p.prep.eps);
-          if ((is_q ? p.prep.q_weight : p.prep.k_weight) == nullptr) f = 1.f;
+          const bool plain = is_v || (is_q ? p.prep.q_weight : p.prep.k_weight) == nullptr;
+          const float mean = row_mean<D>(prep_squares<D>(a[e][0], a[e][1], 1.f), p.prep.eps);
+          f = rsqrtf(mean);
+          if (PLACE) {  // at once, since the row is not there any more later
+            const bool mine = !plain && odd_mean(mean);
+            if (__any_sync(0xffffffffu, mine)) {
+              uint4 x[2] = {a[e][0], a[e][1]};
+              const float g = prep_odd_row<D>(x, mean, p.prep.eps);
+              if (mine) {
+                f = g;
+                a[e][0] = x[0];
+                a[e][1] = x[1];
+              }
+            }
+          } else {
+            odd = __viaddmax_u32(__float_as_uint(mean), 0u - kOddMean, odd);
+          }
+          if (plain) f = 1.f;
         }
         if ((rope || norm) && !is_v) prep_chunks<D>(a[e], f, rope, table.pair[is_q ? 0 : 1], c);
-        if (r < rows) {
-          uint16_t* dst = r < nq    ? to_q + r * D
-                          : is_v ? to_v + (r - nq - p.Hkv) * step
-                                 : to_k + (r - nq) * step;
-          *reinterpret_cast<uint4*>(dst) = a[e][0];
-          *reinterpret_cast<uint4*>(dst + D / 2) = a[e][1];
-          if (RING && is_v && c == 0 && p.ring_weight) p.ring_weight[(unit0 + r - nq - p.Hkv) * p.W + slot] = 0.f;
-        }
+        if (r < rows) store(r, a[e]);
+      }
+    }
+    if (!PLACE && __any_sync(0xffffffffu, odd >= kOddMeans)) {  // some row's mean is odd: those that have a norm again
+#pragma unroll 1
+      for (int s0 = first; s0 < end; ++s0) {
+        load(s0, s0 + 1, rows);
+        const int r = s0 * P::kRows + sub;
+        const bool has = r < min(rows, nq + p.Hkv) && (r < nq ? p.prep.q_weight : p.prep.k_weight) != nullptr;
+        const float mean = row_mean<D>(prep_squares<D>(a[0][0], a[0][1], 1.f), p.prep.eps);
+        const float f = prep_odd_row<D>(a[0], mean, p.prep.eps);
+        prep_chunks<D>(a[0], f, rope, table.pair[r < nq ? 0 : 1], c);
+        if (has && odd_mean(mean)) store(r, a[0]);
       }
     }
   }
@@ -292,8 +344,11 @@ static int run_prefill(const void* q, int64_t q_stride, const void* k, int64_t k
   p.parts = static_cast<int>(wanted < 1 ? 1 : wanted > steps ? steps : wanted);
   const long long ctas = (items * p.parts + kPrefillWarps - 1) / kPrefillWarps;
   const dim3 grid(static_cast<unsigned>(ctas), static_cast<unsigned>(m.B));
-  auto kern = ring ? (m.d == 128 ? prefill_kernel<128, true> : prefill_kernel<64, true>)
-                   : (m.d == 128 ? prefill_kernel<128, false> : prefill_kernel<64, false>);
+  const bool place = (q && q == out_q) || k == out_k;
+  auto kern = ring ? (place ? (m.d == 128 ? prefill_kernel<128, true, true> : prefill_kernel<64, true, true>)
+                            : (m.d == 128 ? prefill_kernel<128, true, false> : prefill_kernel<64, true, false>))
+                   : (place ? (m.d == 128 ? prefill_kernel<128, false, true> : prefill_kernel<64, false, true>)
+                            : (m.d == 128 ? prefill_kernel<128, false, false> : prefill_kernel<64, false, false>));
   return launch_pdl(kern, grid, dim3(32 * kPrefillWarps), 0, s, p);
 }
 

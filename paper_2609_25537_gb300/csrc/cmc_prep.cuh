@@ -33,11 +33,19 @@ __device__ __forceinline__ float quad_squares(float x0, float x1, float y0, floa
   return fmaf(y1, y1, fmaf(y0, y0, fmaf(x1, x1, __fmul_rn(x0, x0))));
 }
 
-// 1 / sqrt(mean of squares + eps) (rsqrtf: 2^-22).
+// Mean of squares + eps, of a row whose elements were taken `by` times as large; 1 / sqrt of it is the row's factor (rsqrtf: 2^-22).
 template <int D>
-__device__ __forceinline__ float rms_factor(float squares, float eps) {
-  return rsqrtf(fmaf(squares, 1.f / D, eps));
+__device__ __forceinline__ float row_mean(float squares, float eps, float by = 1.f) {
+  return fmaf(squares, 1.f / D, __fmul_rn(__fmul_rn(eps, by), by));
 }
+
+// Squares of elements of 2^60 and more may add up to infinity, and those of a row below 2^-45 lose their bits where no eps counts
+// more.  A mean that is then infinite, below 2^-96 or NaN shows it: the squares are summed once more of elements taken 2^-70 or 2^80
+// times as large (what 2^-70 leaves nothing of counts nothing in such a sum), and the smallest rows stay 2^80 times as large, since
+// their factor may be more than fp32 holds.
+constexpr uint32_t kOddMean = 0x0F800000u, kOddMeans = 0x7F800000u - kOddMean;  // 2^-96, and how many floats there are from it to infinity
+__device__ __forceinline__ bool odd_mean(float mean) { return __float_as_uint(mean) - kOddMean >= kOddMeans; }
+__device__ __forceinline__ float odd_scale(float mean) { return mean < 1.f ? 0x1p80f : 0x1p-70f; }
 
 // What a pair's gains g, h and its angle make of it: (g cos a, h sin a, h cos a, g sin a).
 __device__ __forceinline__ float4 pair_factors(float g, float h, float2 cos_sin) {

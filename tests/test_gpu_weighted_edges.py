@@ -204,3 +204,60 @@ def test_a_token_has_the_same_key_prefilled_and_stepped(cuda_device, d, form):
             assert torch.equal(x, y)
         slot = ((pos - 1) % 70).tolist()
         assert torch.equal(key, torch.stack([ring[0][b, :, :, s] for b, s in enumerate(slot)]))
+
+
+@pytest.mark.parametrize("eps", [0.0, 1e-30, 1e-6, 1e3])
+@pytest.mark.parametrize("d", [64, 128])
+def test_norms_of_rows_of_any_magnitude(cuda_device, d, eps):
+    """Rows whose squares fp32 does not hold, from bf16's smallest values to its largest, alone and next to small elements; the
+    same bits from all three calls."""
+    g = gen(cuda_device, 44)
+    B, T, H = 3, 40, 7
+    x = torch.randn(B, 1, T, H, d, generator=g, device=cuda_device, dtype=torch.float64).clamp(-3.9, 3.9)
+    size = torch.randint(-133, 126, (B, 1, T, H, 1), generator=g, device=cuda_device)
+    size[0, 0, :16, 0, 0] = torch.tensor([-133, -132, -127, -126, -100, -64, -63, -62, -48, -45, 58, 59, 63, 64, 120, 125], device=cuda_device)
+    size[1, :, :, 0] = size[1, :, :, 0].clamp(min=-60)
+    x = x * torch.exp2(size.double())
+    x[1, :, :, 0] *= torch.exp2(-60.0 * torch.rand(T, d, generator=g, device=cuda_device).double())  # elements far apart
+    x[2, :, 3, 1], x[2, :, 4, 1] = 3.3895313892515355e38, -9.183549615799121e-41  # the largest and the smallest
+    x[2, :, 5, 1] = 0.0
+    x[2, :, 5, 1, 7] = 3.3895313892515355e38
+    x = x.to(torch.bfloat16)
+    assert x.isfinite().all()
+    pos = torch.tensor([0, 5, 10 ** 6], device=cuda_device)
+    kw = 1 + 0.5 * torch.rand(1, d, generator=g, device=cuda_device)
+    opts = dict(q_weight=kw, k_weight=kw, eps=eps)
+    heads = f64(x)
+    if eps == 0.0:  # rows without a value have no norm
+        assert (heads != 0).any(-1).all()
+    for rope in ({}, dict(rope_theta=THETA)):
+        p = ow.positions(f64(pos), None, 0, T) if rope else None
+        oq, ok = cmc.qk_norm_rope(x, x, pos, **opts, **rope)
+        check_heads(ok, heads, kw, p, "norm", eps=eps)
+        assert torch.equal(oq, ok)
+        place = [x.clone(), x.clone()]
+        cmc.qk_norm_rope(*place, pos, out_q=place[0], out_k=place[1], **opts, **rope)
+        assert torch.equal(place[0], ok) and torch.equal(place[1], ok)
+        place = x.clone()
+        cmc.window_prefill(place, x, x, *(torch.zeros(B, 1, H, T, d, dtype=torch.bfloat16, device=cuda_device) for _ in range(2)),
+                           pos.clone(), out_q=place, **opts, **rope)
+        assert torch.equal(place, oq)
+        ring = [torch.zeros(B, 1, H, T, d, dtype=torch.bfloat16, device=cuda_device) for _ in range(2)]
+        at = pos.clone()
+        cmc.window_prefill(None, x, x, *ring, at, **opts, **rope)
+        for b in range(B):
+            slots = (pos[b] + torch.arange(T, device=cuda_device)) % T
+            assert torch.equal(ring[0][b, :, :, slots], ok[b].transpose(1, 2)) and torch.equal(ring[1][b, :, :, slots], x[b].transpose(1, 2))
+        w = torch.zeros(B, 1, H, T, device=cuda_device)
+        ring = [torch.zeros_like(y) for y in ring]
+        at = pos.clone()
+        for t in range(T):
+            row = x[:, :, t].contiguous()
+            cmc.decode_step_weighted(row, None, None, None, *ring, w, at, row, torch.zeros_like(row), **opts, **rope)
+        for b in range(B):
+            slots = (pos[b] + torch.arange(T, device=cuda_device)) % T
+            assert torch.equal(ring[0][b, :, :, slots], ok[b].transpose(1, 2))
+    # a norm of the queries alone: keys and values of any magnitude are left as they are
+    oq, ok = cmc.qk_norm_rope(x, x, pos, q_weight=kw, eps=eps)
+    check_heads(oq, heads, kw, None, "queries", eps=eps)
+    assert torch.equal(ok, x)
