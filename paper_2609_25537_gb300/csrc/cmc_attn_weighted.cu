@@ -1,6 +1,6 @@
 // Decode attention over [Tier-1 | Tier-2] that adds to each key's weight the probabilities it gets
 // (cmc_two_tier_decode_attn_weighted), and the decode step around it (cmc_decode_step_weighted):
-//   out[h]    = sum_j p_hj v_j,   p_hj = 2^(s_hj - M_h) / l_h,   s = scale log2(e) q_h . k_j
+//   out[h]    = sum_j p_hj v_j,   p_hj = 2^(c (s_hj - M_h)) / l_h,   s = q_h . k_j, c = scale log2(e)
 //   weight[j] += sum of p_hj over the G query heads of the KV head
 // The probabilities need the final maximum M and sum l, which one pass over the keys knows only at its
 // end.  So each CTA keeps the products q . k of its keys, and their weights, in shared memory (4 G + 4 bytes a key,
@@ -118,8 +118,9 @@ __device__ __forceinline__ void ldsm_x4_trans(uint32_t addr, uint32_t& r0, uint3
 }
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;\n" ::: "memory"); }
 
-// A maximum that differences are taken from: 0 where there is none (no key, or NaN alone: 2^x of
-// those is then 0 and NaN).
+// Maxima are those of the products; a difference from one is scaled, not the products first, since what rounding leaves of two equal scores
+// of 2^31 and more is a power of two that fp32 does not hold.  A maximum that differences are taken from: 0 where there is none (no key, or
+// NaN alone: 2^x of those is then 0 and NaN).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
 __device__ __forceinline__ float2 ld_peer_f2(uint32_t addr) {
@@ -556,12 +557,12 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     }
     sc += NW * kBlkKeys * G;
     __syncwarp();
-    // ---- online softmax in the log2 domain.  The maximum over the keys is only taken where some key is above the one
+    // ---- online softmax.  The maximum over the keys is only taken where some key is above the one
     // so far. ----
     float mx[2];
 #pragma unroll
     for (int e = 0; e < 2; ++e)
-      mx[e] = fmaxf(fmaxf(v[0][e], v[0][2 + e]), fmaxf(v[1][e], v[1][2 + e])) * p.scale_log2;
+      mx[e] = fmaxf(fmaxf(v[0][e], v[0][2 + e]), fmaxf(v[1][e], v[1][2 + e]));
     const bool up0 = mx[0] > m_run[0], up1 = mx[1] > m_run[1];
     if (__any_sync(0xffffffffu, up0 || up1)) {
 #pragma unroll
@@ -573,7 +574,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const bool up = mx[e] > m_run[e];
-        alpha[e] = up ? ex2(m_run[e] - mx[e]) : 1.f;
+        alpha[e] = up ? ex2((m_run[e] - mx[e]) * p.scale_log2) : 1.f;
         if (up) m_run[e] = mx[e];
         l_run[e] *= alpha[e];
       }
@@ -592,7 +593,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) pr[h][e] = ex2(fmaf(v[h][e], p.scale_log2, -(e & 1 ? m1 : m0)));
+        for (int e = 0; e < 4; ++e) pr[h][e] = ex2((v[h][e] - (e & 1 ? m1 : m0)) * p.scale_log2);
       l_run[0] += (pr[0][0] + pr[0][2]) + (pr[1][0] + pr[1][2]);
       l_run[1] += (pr[0][1] + pr[0][3]) + (pr[1][1] + pr[1][3]);
       // P^T as the B operand: packed to bf16 (outputs are bf16; the sums are not rounded) and transposed
@@ -668,7 +669,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     float Ls = 0.f;
 #pragma unroll
     for (int w = 0; w < NW; ++w) {
-      const float f = ex2(merge_m[w * 8 + hh] - finite_max(M));
+      const float f = ex2((merge_m[w * 8 + hh] - finite_max(M)) * p.scale_log2);
       const float4 y = *reinterpret_cast<const float4*>(smem + w * S::kBlk + (hh * DP + c) * 4);
       acc.x = fmaf(f, y.x, acc.x);
       acc.y = fmaf(f, y.y, acc.y);
@@ -713,7 +714,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
       Ls = 0.f;
 #pragma unroll
       for (int r = 0; r < kMaxClusterCtas; ++r) {
-        f[r] = ex2(ml[r].x - M);
+        f[r] = ex2((ml[r].x - M) * p.scale_log2);
         Ls = fmaf(f[r], ml[r].y, Ls);
       }
     };
@@ -765,7 +766,7 @@ weighted_attn_kernel(const __grid_constant__ WeightedParams p) {
     const float* s = scores + static_cast<long long>(x) * G;
     float sum = 0.f;
 #pragma unroll
-    for (int h = 0; h < G; ++h) sum = fmaf(ex2(fmaf(s[h], p.scale_log2, -M[h])), R[h], sum);
+    for (int h = 0; h < G; ++h) sum = fmaf(ex2((s[h] - M[h]) * p.scale_log2), R[h], sum);
     (blk < p.nb1 ? p.t1w + u * p.N : p.ring_w + u * p.W)[key] = weights[x] + sum;
   }
   if (FUSED && ORDER) {

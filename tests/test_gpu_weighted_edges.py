@@ -261,3 +261,32 @@ def test_norms_of_rows_of_any_magnitude(cuda_device, d, eps):
     oq, ok = cmc.qk_norm_rope(x, x, pos, q_weight=kw, eps=eps)
     check_heads(oq, heads, kw, None, "queries", eps=eps)
     assert torch.equal(ok, x)
+
+
+@pytest.mark.parametrize("unit", list(PLACES))
+@pytest.mark.parametrize("G, d", [(1, 64), (4, 128), (8, 64)])
+def test_finite_scores_of_any_size(cuda_device, unit, G, d):
+    """Scores of 2^33 and more, exact in fp32: all goes to the largest, a half each to two that are equal."""
+    B, H, k = PLACES[unit]
+    g = gen(cuda_device, 45)
+    q = torch.zeros(B, 1, H * G, d, dtype=torch.bfloat16, device=cuda_device)
+    q[..., 9] = 2.0 ** 20
+    q[..., 9] *= torch.tensor([1.0, -1.0, 1.0, 2.0 ** 30], device=cuda_device).repeat(H * G)[:H * G]
+    size = torch.randint(-200, 200, (B, 1, H, k + 70), generator=g, device=cuda_device)
+    size[..., 3], size[..., k - 4] = 250, -250
+    size[:, :, :, k + 8] = size[:, :, :, 3]  # (slots 0 to 9 of the ring are occupied)
+    keys = torch.zeros(B, 1, H, k + 70, d, dtype=torch.bfloat16, device=cuda_device)
+    keys[..., 9] = size * 2.0 ** 20
+    values = torch.randint(-60, 60, keys.shape, generator=g, device=cuda_device).to(torch.bfloat16)
+    w = torch.rand(B, 1, H, k + 70, generator=g, device=cuda_device).round(decimals=1)
+    pos = torch.full((B,), 10, device=cuda_device)
+    parts = [[x[:, :, :, :k].contiguous(), x[:, :, :, k:].contiguous()] for x in (keys, values, w)]
+    out = cmc.two_tier_decode_attn_weighted(q, *(x[0] for x in parts), *(x[1] for x in parts), pos)
+    up = ((values[:, :, :, 3].float() + values[:, :, :, k + 8].float()) / 2).to(torch.bfloat16)
+    down = values[:, :, :, k - 4]
+    sign = q[..., 9].view(B, 1, H, G, 1) > 0
+    assert torch.equal(out.view(B, 1, H, G, d), torch.where(sign, up[:, :, :, None], down[:, :, :, None]))
+    given = torch.zeros_like(w)
+    given[..., 3] = given[..., k + 8] = 0.5 * sign.sum((3, 4))
+    given[..., k - 4] = (~sign).sum((3, 4))
+    assert torch.equal(torch.cat([parts[2][0], parts[2][1]], dim=-1), w + given)
