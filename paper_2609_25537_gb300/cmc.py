@@ -358,11 +358,14 @@ class DecodeWorkspace:
              else decode_attn_workspace_size(dims))
         if n == 0:
             raise ValueError(f"unsupported dims {dims.key()}")
+        self._set(dims, torch.zeros(n, dtype=torch.uint8, device=device))
+
+    def _set(self, dims: CmcDims, buf: torch.Tensor) -> None:
         self.dims = dims
-        self.nbytes = n
-        self.buf = torch.zeros(n, dtype=torch.uint8, device=device)
-        self.ptr = self.buf.data_ptr()
-        self.index = self.buf.get_device()  # -1 on the host
+        self.nbytes = buf.numel()
+        self.buf = buf
+        self.ptr = buf.data_ptr()
+        self.index = buf.get_device()  # -1 on the host
 
     def status(self, clear: bool = True) -> int:
         """CMC_DEVFLAG_* bits raised by kernels since the last clear (synchronises)."""
@@ -943,7 +946,7 @@ def decode_attn_q8_plan(dims: CmcDims, fused: bool = True) -> int:
 
 _F32 = torch.float32
 _byref = ctypes.byref
-_weighted_workspaces: Dict[Tuple, Dict[Tuple[int, int], DecodeWorkspace]] = {}
+_weighted_workspaces: Dict[int, Dict[Tuple[int, int], DecodeWorkspace]] = {}
 
 
 def _int32(x: int) -> int:
@@ -952,22 +955,31 @@ def _int32(x: int) -> int:
 
 
 def _kept_workspaces(dims: CmcDims) -> Dict:
-    """The workspaces that calls of these sizes choose themselves, by device and stream: one for all calls
-    of a batch size, but for units so long that the workspace goes by their size."""
-    n = decode_attn_weighted_workspace_size(dims)
-    base = int(lib().cmc_cache_workspace_size(dims.B))
-    return _weighted_workspaces.setdefault((dims.B,) if n == base else dims.key(), {})
+    """The workspaces that calls of this batch size choose themselves, by device and stream."""
+    return _weighted_workspaces.setdefault(dims.B, {})
 
 
-def _own_workspace(kept: Dict, index: int, stream: int, dims: CmcDims) -> DecodeWorkspace:
-    """A workspace for a call that is given none.  One is kept per stream; a call that is being
-    captured gets one of its graph's own, since the kept ones are zero-filled once, outside
-    of it, and other calls use them.  (The default stream, 0, is never captured.)"""
+def _new_workspace(dims: CmcDims, index: int, before: Optional[DecodeWorkspace]) -> DecodeWorkspace:
+    """A workspace whose flags and counters are those of the one `before`, or zero; what lies behind them, the products of
+    long units, may hold anything."""
+    ws = DecodeWorkspace.__new__(DecodeWorkspace)
+    ws._set(dims, torch.empty(decode_attn_weighted_workspace_size(dims), dtype=torch.uint8,
+                              device=torch.device("cuda", index)))
+    head = ws.buf[:int(lib().cmc_cache_workspace_size(dims.B))]
+    head.zero_() if before is None else head.copy_(before.buf[:head.numel()])
+    return ws
+
+
+def _own_workspace(kept: Dict, index: int, stream: int, dims: CmcDims, need: int) -> DecodeWorkspace:
+    """A workspace of `need` bytes for a call that is given none.  One is kept per batch size and stream, and replaced by
+    a larger one where a call's units are too long for it; a call that is being captured gets one of its graph's
+    own, since the kept ones are zeroed once, outside of it, and other calls use them.  (The
+    default stream, 0, is never captured.)"""
     if stream and torch._C._cuda_isCurrentStreamCapturing():
-        return DecodeWorkspace(dims, torch.device("cuda", index), weighted=True)
+        return _new_workspace(dims, index, None)
     ws = kept.get((index, stream))
-    if ws is None:
-        ws = kept[index, stream] = DecodeWorkspace(dims, torch.device("cuda", index), weighted=True)
+    if ws is None or ws.nbytes < need:
+        ws = kept[index, stream] = _new_workspace(dims, index, ws)
     return ws
 
 
@@ -1168,7 +1180,7 @@ def window_prefill(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
         raise ValueError("out_q without q")
     stream = _raw_stream(index)
     if workspace is None:
-        workspace = _own_workspace(workspaces, index, stream, own)
+        workspace = _own_workspace(workspaces, index, stream, own, 0)
     elif workspace.index != index:
         raise _elsewhere_workspace(workspace, index)
     fn = lib().cmc_window_prefill
@@ -1190,7 +1202,7 @@ def _need_weight(weight, name, rows, dev) -> None:
 
 def _weighted_kept(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight, pos, new, key) -> Tuple:
     """Checks the tensors of a weighted attention call one by one; what the call keeps for shapes like
-    these: (dims by reference, dims, the workspaces by device and stream)."""
+    these: (dims by reference, dims, the workspaces by device and stream, the bytes of one)."""
     _need(q, "q", torch.bfloat16, 4)
     dev = q.device
     B, L, Hq, d = q.shape
@@ -1214,9 +1226,10 @@ def _weighted_kept(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weigh
     if new is not None:
         _need_new(*new, (B, L, Hkv, d), dev)
     dims = CmcDims(B, L, Hq, Hkv, d, max(k, 1), k, W)
-    if decode_attn_weighted_workspace_size(dims) == 0:
+    need = decode_attn_weighted_workspace_size(dims)
+    if need == 0:
         raise ValueError(f"unsupported dims {dims.key()}")
-    kept = (ctypes.byref(dims), dims, _kept_workspaces(dims))
+    kept = (ctypes.byref(dims), dims, _kept_workspaces(dims), need)
     return kept if key is None else _kept(key, kept)
 
 
@@ -1247,10 +1260,11 @@ def two_tier_decode_attn_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, rin
     """Decode attention over [Tier-1 | occupied ring slots] (tier1_* None: the ring alone) that adds to each
     key's weight, in place, the probabilities that its KV head's queries gave it; see
     cmc_two_tier_decode_attn_weighted.  Returns bf16 [B, L, Hq, d].  ``workspace`` is a DecodeWorkspace(dims,
-    device, weighted=True); without one the call keeps one per stream (see :func:`weighted_cache_status`), and a
-    captured call gets one of its own, zero-filled at every replay."""
-    ref, dims, workspaces = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight,
-                                           pos, None)
+    device, weighted=True); without one the call keeps one per batch size and stream, as large as the longest units have
+    asked for (see :func:`weighted_cache_status`), and a captured call gets one of its own, its flags and counters
+    zeroed at every replay."""
+    ref, dims, workspaces, need = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v,
+                                                 ring_weight, pos, None)
     index = q.get_device()
     if out is None:
         out = torch.empty_like(q)
@@ -1258,7 +1272,7 @@ def two_tier_decode_attn_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, rin
         _check_out(out, q)
     stream = _raw_stream(index)
     if workspace is None:
-        workspace = _own_workspace(workspaces, index, stream, dims)
+        workspace = _own_workspace(workspaces, index, stream, dims, need)
     elif workspace.index != index:
         raise _elsewhere_workspace(workspace, index)
     fn = lib().cmc_two_tier_decode_attn_weighted
@@ -1283,8 +1297,8 @@ def decode_step_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring
     :func:`two_tier_decode_attn_weighted`; see cmc_decode_step_weighted.  Updates ring_k, ring_v, pos and the
     weights in place.  With q_weight, k_weight or rope_theta, q and k_new are given before the norm and
     rotation of :func:`qk_norm_rope`, at position rope_offset + evicted[b] + pos[b]."""
-    ref, dims, workspaces = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring_weight,
-                                           pos, (k_new, v_new))
+    ref, dims, workspaces, need = _weighted_call(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v,
+                                                 ring_weight, pos, (k_new, v_new))
     index = q.get_device()
     prep = _prep(q_weight, k_weight, eps, rope_theta, rope_offset, evicted, dims.B, dims.L, dims.d, q.device)
     if out is None:
@@ -1293,7 +1307,7 @@ def decode_step_weighted(q, tier1_k, tier1_v, tier1_weight, ring_k, ring_v, ring
         _check_out(out, q)
     stream = _raw_stream(index)
     if workspace is None:
-        workspace = _own_workspace(workspaces, index, stream, dims)
+        workspace = _own_workspace(workspaces, index, stream, dims, need)
     elif workspace.index != index:
         raise _elsewhere_workspace(workspace, index)
     fn = lib().cmc_decode_step_weighted
@@ -1392,7 +1406,7 @@ def evict_cache(k: torch.Tensor, v: torch.Tensor, weight: torch.Tensor, keep: in
         out_pos = torch.empty(k.shape[0], dtype=torch.int64, device=dev) if pos is None else torch.empty_like(pos)
     stream = _raw_stream(index)
     if workspace is None:
-        workspace = _own_workspace(workspaces, index, stream, own)
+        workspace = _own_workspace(workspaces, index, stream, own, 0)
     elif workspace.index != index:
         raise _elsewhere_workspace(workspace, index)
     fn = lib().cmc_evict_cache

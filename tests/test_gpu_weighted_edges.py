@@ -290,3 +290,63 @@ def test_finite_scores_of_any_size(cuda_device, unit, G, d):
     given[..., 3] = given[..., k + 8] = 0.5 * sign.sum((3, 4))
     given[..., k - 4] = (~sign).sum((3, 4))
     assert torch.equal(torch.cat([parts[2][0], parts[2][1]], dim=-1), w + given)
+
+
+def long_units(dev, W, seed, B=1, H=160, poison=True):
+    """Units whose products go to the workspace (G = 8, d = 64: more than 9,216 keys, and more CTAs than an SM each)."""
+    case = (B, 1, H, 8, 64, 40, W, [W + 5])
+    dims = cmc.CmcDims(B, 1, 8 * H, H, 64, 40, 40, W)
+    assert cmc.decode_attn_weighted_plan(dims) > torch.cuda.get_device_properties(dev).multi_processor_count
+    assert cmc.decode_attn_weighted_workspace_size(dims) > 36 * B * H * W
+    return attention_problem(dev, case, seed, poison)[:4], dims
+
+
+def test_workspaces_of_long_units_do_not_pile_up(cuda_device):
+    """One for each batch size and stream, as large as the longest has asked for; its flags are those of all calls."""
+    stream = torch.cuda.Stream()
+    cmc.weighted_cache_status()
+    with torch.cuda.stream(stream):
+        before = torch.cuda.memory_allocated()
+        for W in (10240, 9500, 9984, 10200, 9300):
+            (q, t1, ring, pos), dims = long_units(cuda_device, W, 46, H=24)
+            pos.fill_(-1 if W == 9984 else W)
+            cmc.two_tier_decode_attn_weighted(q, *t1, *ring, pos)
+            size = cmc.decode_attn_weighted_workspace_size(dims)
+            most = max(size, most) if W != 10240 else size
+            del q, t1, ring, pos
+        stream.synchronize()
+        assert torch.cuda.memory_allocated() - before <= most + (1 << 20)
+        # a larger one after a flag, and the right results in it
+        (q, t1, ring, pos), dims = long_units(cuda_device, 10400, 47, H=24)
+        given = [x.clone() for x in (*t1, *ring)]
+        out = cmc.two_tier_decode_attn_weighted(q, *t1, *ring, pos)
+        ws = cmc.DecodeWorkspace(dims, cuda_device, weighted=True)
+        want = cmc.two_tier_decode_attn_weighted(q, *given, pos, workspace=ws)
+        assert torch.equal(out, want) and torch.equal(t1[2], given[2]) and torch.equal(ring[2], given[5])
+    assert cmc.weighted_cache_status() == cmc.DEVFLAG_BAD_POS and cmc.weighted_cache_status() == 0
+
+
+def test_a_captured_call_finds_anything_behind_its_counters(cuda_device):
+    """Its own workspace: the flags and counters are zeroed at every replay, the products' place holds what was there."""
+    (q, t1, ring, pos), dims = long_units(cuda_device, 9300, 48, H=24)
+    state = [x.clone() for x in (*t1, *ring, pos)]
+    new = [torch.ones(1, 1, 24, 64, dtype=torch.bfloat16, device=cuda_device) for _ in range(2)]
+    want = cmc.decode_step_weighted(q, *state, *new)
+    out = torch.empty_like(q)
+    start = [x.clone() for x in (*t1, *ring, pos)]
+    args = [*t1, *ring, pos]
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        for _ in range(2):
+            bad = torch.full((cmc.decode_attn_weighted_workspace_size(dims) // 4,), float("nan"), device=cuda_device)
+            del bad
+        cmc.decode_step_weighted(q, *args, *new, out=out)
+    for _ in range(3):
+        for x, y in zip(args, start):
+            x.copy_(y)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
+        for x, y in zip(args, state):
+            assert torch.equal(x, y)
