@@ -350,3 +350,28 @@ def test_a_captured_call_finds_anything_behind_its_counters(cuda_device):
         assert torch.equal(out, want)
         for x, y in zip(args, state):
             assert torch.equal(x, y)
+
+
+# B, L, Hkv, G, d, k, W, positions: units too long for shared memory, on more CTAs than SMs (of which a unit takes eight), so that their
+# products and weights go to the workspace; the last two on so many that the longest sequences start first
+LONG = {"G 8": (9, 1, 4, 8, 64, 300, 9000, [8999, -1, 0, 40, 9000, 9001, 5000, 31, 2 ** 33 + 7]),
+        "G 4": (5, 1, 4, 4, 128, 33, 18432, [18431, -7, 18500, 100, 0]),
+        "G 2": (3, 7, 1, 2, 64, 0, 30721, [30720, 11, 30721]), "G 1": (5, 1, 4, 1, 64, 46000, 100, [99, 0, 100, -1, 65]),
+        "G 8, ordered": (16, 2, 2, 8, 128, 40, 9200, [9199, 17, 9200, -1, 4000]), "G 4, ordered": (60, 1, 1, 4, 64, 18000, 500, [499, 0, -3, 500, 77])}
+
+
+@pytest.mark.parametrize("prepared", [False, True])
+@pytest.mark.parametrize("name", list(LONG))
+def test_steps_of_units_whose_products_go_to_the_workspace(cuda_device, name, prepared):
+    case = LONG[name]
+    B, L, H, G, d, k, W, positions = case
+    sms = torch.cuda.get_device_properties(cuda_device).multi_processor_count
+    dims = cmc.CmcDims(B, L, H * G, H, d, max(k, 1), k, W)
+    ctas = cmc.decode_attn_weighted_plan(dims)
+    assert ctas == 8 * B * L * H and ctas > sms * (3 if "ordered" in name else 1)
+    head = int(cmc.lib().cmc_cache_workspace_size(B))
+    assert cmc.decode_attn_weighted_workspace_size(dims) >= head + 4 * (G + 1) * B * L * H * (k + W)
+    ws = cmc.DecodeWorkspace(dims, cuda_device, weighted=True)
+    ws.buf[head:] = 255  # NaN: nothing is read there that the call has not written
+    check_step(cuda_device, case, prepared, 49, workspace=ws)
+    assert ws.status() == (cmc.DEVFLAG_BAD_POS if min(positions) < 0 else 0) and not ws.buf[256:head].any()
