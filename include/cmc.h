@@ -652,7 +652,9 @@ CMC_API size_t cmc_cache_workspace_size(int B);
  *   q, k            as for cmc_qk_norm_rope; q may be NULL (no queries)
  *   v               bf16 [B, L, T, Hkv, d], v_stride like k_stride; values are stored as they are
  *   ring_k, ring_v  bf16 [B, L, Hkv, W, d]   updated in place
- *   ring_weight     fp32 [B, L, Hkv, W], or NULL: the weights of the slots written become 0
+ *   ring_weight     fp32 [B, L, Hkv, W], or NULL: the weights of the slots written become 0 (what a prompt's own
+ *                   queries give its tokens is for the caller to add, who attends with them: an eviction before the first
+ *                   weighted decode step otherwise goes by age)
  *   pos             int64 [B]; updated
  *   count           int64 [B] (values are clamped to [0, T]), or NULL for T each
  *   out_q           bf16 [B, L, T, Hq, d] dense (may be q where that is dense); tokens from count[b] on
@@ -685,7 +687,8 @@ CMC_API size_t cmc_decode_attn_weighted_workspace_size(const cmc_dims* dims);
  *   ring_k, ring_v, ring_weight     bf16 [B, L, Hkv, W, d], fp32 [B, L, Hkv, W]
  *   workspace                       see cmc_decode_attn_weighted_workspace_size
  *
- * Other arguments as there.  Weights are updated in place, in fp32 and in a fixed order; those of rows that
+ * Other arguments as there.  For the outputs the probabilities are rounded to bf16, as there; for the weights they are not.  Weights
+ * are updated in place, in fp32 and in a fixed order; those of rows that
  * hold no token are neither read nor written, and the rows may hold anything.  A score that is NaN or plus infinity gives
  * NaN in its head's output and in all weights of its KV head; one of minus infinity counts nothing.  A NaN or infinity among the
  * values reaches the outputs alone.  A sequence with pos[b] < 0 gets a zero output, its

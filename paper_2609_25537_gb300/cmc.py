@@ -1133,8 +1133,9 @@ def window_prefill(q: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor, 
                    workspace: Optional[DecodeWorkspace] = None) -> Optional[torch.Tensor]:
     """Appends the first count[b] (int64 [B]; None: all) of T tokens k, v [B, L, T, Hkv, d] to the ring, in place, after the
     norm and rotation of :func:`qk_norm_rope`, and returns the queries q [B, L, T, Hq, d] likewise (None: no
-    queries); see cmc_window_prefill.  The weights of the slots written become 0.  Rows of the queries from count[b]
-    on are not written (of a new tensor they are undefined)."""
+    queries); see cmc_window_prefill.  The weights of the slots written become 0 (what the prompt's own queries give its
+    tokens is for the caller to add).  Rows of the queries from count[b] on are not written (of a new tensor they are
+    undefined)."""
     B, L, T, d = _token_sizes(k, "k")
     dev = k.device
     index = dev.index

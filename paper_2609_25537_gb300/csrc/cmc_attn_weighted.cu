@@ -18,7 +18,7 @@
 // (mma.sync m16n8k16, ldmatrix; 4 flops a byte: the tensor pipe is all but idle).
 //
 // What a warp does with a block is a chain of latencies, so that its length and the warps an SM holds set the rate, not the
-// bytes on the way: 32 layers of 128 + 512 keys, fused step with norm and rotation, 13.0 us (12.9 at the copy rate), with blocks of 16
+// bytes on the way: 32 layers of 128 + 512 keys, fused step with norm and rotation, 13.1 us (12.9 at the copy rate), with blocks of 16
 // keys fed from registers 17.7 (six warps a CTA) to 22.6, through private stages with two or three blocks on the way 21.6 to 30.
 //
 // The new token (fused step) is read from k_new and v_new where its slot's row would be, by the warp that has

@@ -462,7 +462,11 @@ static int launch_evict(const EvictParams& p0, long long units, cudaStream_t s) 
     if (dev >= 0 && dev < 64) configured[dev].store(1, std::memory_order_release);
   }
   // CTAs that copy a unit: as many as it takes to have about three on each SM, at most one a block, in place no
-  // more than a cluster has.
+  // more than a cluster has.  One, which then chooses as well, where there are units enough or the rows that are kept are one block:
+  // what it costs goes by the length of the unit too, which the rule does not look at.  (us with one kernel, 64 rows of d = 128 kept /
+  // with two, 65 kept: 1, 8 and 64 units of 4,096 tokens 7.0 / 8.1, 7.5 / 8.6, 7.6 / 10.7, of 16,384 16.8 / 10.9, 17.4 / 11.2,
+  // 17.8 / 11.6.)  In place against apart: 256 units of 512 tokens, 256 kept, 14.3 / 13.6, 64 of 2,048, 1,024 kept, 30.2 / 23.1, 64 of
+  // 16,384, 2,048 kept, 43.0 / 35.2: a barrier over the unit's CTAs a round.
   const long long blocks = (p.keep + kBlock - 1) / kBlock;
   long long cm = std::max(1LL, std::min<long long>(blocks, 3 * sm_count() / units));
   if (p.in_place && cm > kMaxClusterCtas) cm = kMaxClusterCtas;
