@@ -264,7 +264,7 @@ def test_weighted_attention_argument_checks(L, call):
 @pytest.mark.parametrize("call", [_attend, _step])
 def test_weighted_attention_overlaps(L, call):
     """48 query heads' rows, 12,288 bytes; Tier-1 of 12 x 100 rows, 307,200 and 4,800; rings of 12 x 16, 49,152 and 768; new rows
-    3,072."""
+    a quarter of the queries'."""
     CUDA = 6  # all checks passed: no device
     a = dict(q=BIG, tk=2 * BIG, tv=3 * BIG, tw=4 * BIG, rk=5 * BIG, rv=6 * BIG, rw=7 * BIG, pos=8 * BIG, out=9 * BIG, ws=10 * BIG)
     step = call is _step
