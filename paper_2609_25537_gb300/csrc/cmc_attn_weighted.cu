@@ -29,6 +29,7 @@
 #include <atomic>
 
 #include "cmc_prep.cuh"
+#include "cmc_ranges.cuh"
 
 namespace cmc {
 

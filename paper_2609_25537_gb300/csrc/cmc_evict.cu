@@ -20,6 +20,7 @@
 #include <atomic>
 
 #include "cmc_attn.cuh"
+#include "cmc_ranges.cuh"
 
 namespace cmc {
 

@@ -7,6 +7,7 @@
 // of 32 + 2 x 8 heads of 128 into rings of 2,048 slots, us a launch at two rows a lane group and 8 CTAs of four warps an SM 110.5 (91 %
 // of the copy rate), three and 6 112, two and 6 120, one and 8 123; 8,192 tokens' queries and keys alone 31.4 (80 %).
 #include "cmc_prep.cuh"
+#include "cmc_ranges.cuh"
 
 namespace cmc {
 
@@ -101,8 +102,9 @@ __device__ __forceinline__ float prep_odd_row(uint4 (&a)[2], float mean, float e
 
 // A warp takes a token's heads, or one of `parts` equal shares of them, d / 16 lanes to a head's row.  Rows whose mean is odd: an
 // instruction a row keeps the oddest mean, and a warp that has met one takes its rows again in the end, which costs nothing that can be
-// measured.  Where rows are written over (PLACE: queries or keys prepared where they are) each is looked at at once, with a vote: 8
-// sequences of 4,096 tokens 117 us for 110.5, of 1,024 without a ring 33.5 for 31.5.
+// measured.  Where rows are written over (PLACE: queries or keys prepared where they are) each is looked at at once, with a vote, which
+// also spills 8 to 28 bytes at the 64 registers that eight CTAs leave: 8 sequences of 4,096 tokens 117 us for 110.5, of 1,024 without a
+// ring 33.5 for 31.5.
 template <int D, bool RING, bool PLACE>
 __global__ void __launch_bounds__(32 * kPrefillWarps, kPrefillPerSm)
 prefill_kernel(const __grid_constant__ PrefillParams p) {
